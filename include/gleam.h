@@ -274,6 +274,71 @@ GLEAM_API int gleam_l1_loss(const void* x, const void* ref, double* loss, void* 
                             uint32_t layout);
 GLEAM_API uint64_t gleam_l1_loss_workspace_size(void);
 
+/* ---- operators of the learned prior: layer norm, dropout, and the residual tail that joins them ------------
+ * The learned half of an unrolled step is built from residual blocks.  These calls are what such a block needs next to its
+ * convolutions or matrix products.  Every activation array is (outer, features, inner), last index fastest, inner slices
+ * contiguous; the norm is over the features of each of the outer * inner positions.  inner = 1 are rows of features (tokens,
+ * maps with the features last), inner = n0 n1 n2 are feature maps with the features in front of the voxels.
+ *
+ *   layer norm     m = mean_c x,  v = mean_c (x - m)^2,  r = 1 / sqrt(v + eps),  y = (x - m) r weight + bias
+ *   its VJP        h = (x - m) r,  g = grad_y weight,  grad_x = r (g - mean_c g - h mean_c (g h)),
+ *                  grad_weight = sum of grad_y h,  grad_bias = sum of grad_y  over all positions
+ *   dropout        out = [residual +] (dropped ? 0 : x s),  s = 1 / (1 - p) rounded to 32 bits (0 for p = 1);  its VJP
+ *                  grad_x = (dropped ? 0 : grad_out s); the cotangent of residual is grad_out itself
+ *   tail           sum = residual + dropout(x) in the arrays' type (the stored residual stream),  y = layer norm of sum
+ *   its VJP        grad_residual = [grad_sum +] VJP of the norm,  grad_x = its dropout VJP (from the unrounded value)
+ *
+ * No mask is stored: element i = (o * features + c) * inner + k takes word i mod 4 of Philox4x32-10 (Salmon et al., "Parallel
+ * random numbers: as easy as 1, 2, 3", 2011) with the 128-bit counter (offset + i / 4, *step) and the key seed, and is dropped
+ * if that word is less than floor(p 2^32).  A call with n elements uses ceil(n / 4) counters from offset; sites that shall not
+ * share their masks take ranges that do not meet.  The VJP is given the same p, seed, offset and step.  A dropped element is
+ * selected, not multiplied: it is 0 (or exactly the residual) also where x is infinite or NaN.
+ *
+ * x, residual, sum, y and their cotangents have type dtype; weight, bias and their gradients weight_dtype (GLEAM_F32 or
+ * dtype); mean and rstd are float32, one per position (o * inner + k).  All sums are in 32 bits.  weight and bias may be null (1
+ * and 0); mean and rstd may be null in a forward call whose VJP is not wanted; grad_sum, grad_weight, grad_bias and residual
+ * (dropout) may be null.  An output may be exactly an input of the same pitch; any other overlap between an output, the
+ * workspace and another argument is GLEAM_ERR_ALIAS.  outer = 0 or inner = 0 is a call on nothing: gradients of weights are
+ * cleared, nothing else is done.  Results are deterministic.  Two calls whose GPU work may overlap (other streams, captured
+ * graphs) need workspaces of their own.
+ */
+#define GLEAM_FEATURE_DIMS_VERSION 1
+enum { GLEAM_F32 = 0, GLEAM_F16 = 1, GLEAM_BF16 = 2 };
+typedef struct {
+    int32_t struct_version;   /* GLEAM_FEATURE_DIMS_VERSION */
+    int32_t dtype;            /* GLEAM_F32, GLEAM_F16 or GLEAM_BF16 */
+    int32_t weight_dtype;     /* GLEAM_F32 or dtype */
+    float eps;                /* >= 0; not used by the dropout calls and the VJPs */
+    int64_t outer, features, inner;
+    int64_t pitch[5];         /* elements from one outer slice to the next, for each activation array in the order of the call's
+                                 arguments (x, residual, ... including outputs, not weights and statistics); 0 = contiguous */
+    void* stream;
+    void* workspace;          /* gleam_layer_norm_workspace_size() bytes, 256-byte aligned; the VJPs with weight gradients alone */
+    uint64_t workspace_bytes;
+} gleam_feature_dims;
+typedef struct {
+    double p;                 /* 0 <= p <= 1 */
+    uint64_t seed, offset;
+    const uint64_t* step;     /* device, upper half of the counter, read when the kernel runs (so that a captured call draws
+                                 anew at every replay); null = 0 */
+} gleam_dropout_args;
+GLEAM_API int gleam_layer_norm_forward(const void* x, const void* weight, const void* bias, void* y, float* mean, float* rstd,
+                                       const gleam_feature_dims* dims);
+GLEAM_API int gleam_layer_norm_vjp(const void* grad_y, const void* x, const void* weight, const float* mean, const float* rstd,
+                                   void* grad_x, void* grad_weight, void* grad_bias, const gleam_feature_dims* dims);
+GLEAM_API int gleam_dropout_forward(const void* x, const void* residual, void* out, const gleam_dropout_args* dropout,
+                                    const gleam_feature_dims* dims);
+GLEAM_API int gleam_dropout_vjp(const void* grad_out, void* grad_x, const gleam_dropout_args* dropout,
+                                const gleam_feature_dims* dims);
+GLEAM_API int gleam_dropout_add_layer_norm_forward(const void* x, const void* residual, const void* weight, const void* bias,
+                                                   void* sum, void* y, float* mean, float* rstd,
+                                                   const gleam_dropout_args* dropout, const gleam_feature_dims* dims);
+GLEAM_API int gleam_dropout_add_layer_norm_vjp(const void* grad_y, const void* grad_sum, const void* sum, const void* weight,
+                                               const float* mean, const float* rstd, void* grad_x, void* grad_residual,
+                                               void* grad_weight, void* grad_bias, const gleam_dropout_args* dropout,
+                                               const gleam_feature_dims* dims);
+GLEAM_API int gleam_layer_norm_workspace_size(const gleam_feature_dims* dims, uint64_t* bytes);
+
 /* ---- gradients of Eq. 3 with respect to the step size and the measurements --------------------------
  * out = x - eta A^H (A x - y) is linear in eta and affine in y.  For a cotangent g = grad_out of the
  * output (conjugate-Wirtinger convention, as for gleam_dc_vjp):
@@ -341,7 +406,8 @@ enum {
     GLEAM_K_COL_INV = 8,
     GLEAM_K_CG_VEC = 9,       /* image-sized vector kernels of the conjugate-gradient solve */
     GLEAM_K_FUSED3D = 10,     /* persistent kernel of the separable 3-D path (all three passes) */
-    GLEAM_K_CLASSES = 11
+    GLEAM_K_PRIOR = 11,       /* layer norm, dropout and residual tail of the learned prior */
+    GLEAM_K_CLASSES = 12
 };
 GLEAM_API uint64_t gleam_dc_launch_count(void);
 /* FP32 FMA throughput of the current device in TFLOP/s (2 flop per FMA), from a kernel of independent FMA

@@ -11,3 +11,12 @@ from .binding import (  # noqa: F401
     gleam_dc_prepare, gleam_dc_forward_prepared, gleam_dc_forward_aty, gleam_dc_adjoint, gleam_dc_check_status, gleam_dc_debug_fused, gleam_dc_fused_wait_stats, gleam_dc_set_fused, gleam_dc_grad_eta, gleam_dc_grad_y, gleam_dc_grad_workspace_size, gleam_dc_forward_layout, gleam_dc_vjp_layout,
     gleam_l1_loss, gleam_l1_loss_workspace_size, gleam_measure_fp32_peak, gleam_dc_rowtile_split, GLEAM_X_CHANNELS, GLEAM_OUT_CHANNELS, GLEAM_LOSS_FLOAT, ModlCG, gleam_modl_cg_forward, gleam_modl_cg_vjp, gleam_modl_cg_workspace_size,
 )
+from .binding import (  # noqa: F401
+    GLEAM_BF16, GLEAM_F16, GLEAM_F32, gleam_dropout_add_layer_norm_forward, gleam_dropout_add_layer_norm_vjp, gleam_dropout_args,
+    gleam_dropout_forward, gleam_dropout_vjp, gleam_feature_dims, gleam_layer_norm_forward, gleam_layer_norm_vjp,
+    gleam_layer_norm_workspace_size, make_dropout_args, make_feature_dims,
+)
+from .prior_ops import (  # noqa: F401
+    DropoutGenerator, dropout, dropout_add_layer_norm, dropout_add_layer_norm_forward, dropout_add_layer_norm_vjp,
+    dropout_forward, dropout_vjp, layer_norm, layer_norm_forward, layer_norm_vjp,
+)

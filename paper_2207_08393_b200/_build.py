@@ -67,7 +67,11 @@ def build(force: bool = False, verbose: bool = False) -> str:
         obj = os.path.join(BUILD, "kernels_tile%d.o" % ry)
         jobs.append((["nvcc"] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) +
                      ["-DGLEAM_TILE_RY=%d" % ry, "-c", os.path.join(CSRC, "kernels_tile.cu"), "-o", obj], obj))
-    for name in ("gleam_dc", "kernels_fused", "modl_cg"):
+    for kind in range(3):                      # float32, float16, bfloat16
+        obj = os.path.join(BUILD, "kernels_prior%d.o" % kind)
+        jobs.append((["nvcc"] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) +
+                     ["-DGLEAM_PRIOR_TYPE=%d" % kind, "-c", os.path.join(CSRC, "kernels_prior.cu"), "-o", obj], obj))
+    for name in ("gleam_dc", "kernels_fused", "modl_cg", "prior_ops"):
         obj = os.path.join(BUILD, name + ".o")
         jobs.append((["nvcc"] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) +
                      ["-c", os.path.join(CSRC, name + ".cu"), "-o", obj], obj))

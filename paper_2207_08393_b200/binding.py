@@ -31,6 +31,10 @@ GLEAM_LOSS_FLOAT = 4
 GLEAM_MASK_FULL = 0
 GLEAM_MASK_READOUT_INVARIANT = 1
 
+GLEAM_F32 = 0
+GLEAM_F16 = 1
+GLEAM_BF16 = 2
+
 EXPORTS = ["gleam_dc_forward", "gleam_dc_vjp", "gleam_dc_workspace_size", "gleam_dc_length_supported",
            "gleam_status_string", "gleam_version", "gleam_dc_forward_host", "gleam_dc_vjp_host",
            "gleam_dc_host_arena_size", "gleam_dc_launch_count", "gleam_dc_profile_begin", "gleam_dc_profile_end",
@@ -40,10 +44,13 @@ EXPORTS = ["gleam_dc_forward", "gleam_dc_vjp", "gleam_dc_workspace_size", "gleam
            "gleam_dc_check_status", "gleam_dc_debug_fused", "gleam_dc_fused_wait_stats", "gleam_dc_set_fused",
            "gleam_dc_grad_eta", "gleam_dc_grad_y", "gleam_dc_grad_workspace_size",
            "gleam_dc_forward_layout", "gleam_dc_vjp_layout", "gleam_l1_loss", "gleam_l1_loss_workspace_size",
-           "gleam_measure_fp32_peak", "gleam_dc_rowtile_split"]
+           "gleam_measure_fp32_peak", "gleam_dc_rowtile_split",
+           "gleam_layer_norm_forward", "gleam_layer_norm_vjp", "gleam_layer_norm_workspace_size",
+           "gleam_dropout_forward", "gleam_dropout_vjp",
+           "gleam_dropout_add_layer_norm_forward", "gleam_dropout_add_layer_norm_vjp"]
 
 KERNEL_CLASSES = ["zmap", "col_z", "row_fused", "row_fwd", "col_mid_sep", "row_inv", "col_mid_full", "col_fwd",
-                  "col_inv", "cg_vec", "fused3d"]
+                  "col_inv", "cg_vec", "fused3d", "prior"]
 
 
 class gleam_dims(ctypes.Structure):
@@ -59,6 +66,31 @@ class gleam_dims(ctypes.Structure):
         ("stream", ctypes.c_void_p),
         ("workspace", ctypes.c_void_p),
         ("workspace_bytes", ctypes.c_uint64),
+    ]
+
+
+class gleam_feature_dims(ctypes.Structure):
+    _fields_ = [
+        ("struct_version", ctypes.c_int32),
+        ("dtype", ctypes.c_int32),
+        ("weight_dtype", ctypes.c_int32),
+        ("eps", ctypes.c_float),
+        ("outer", ctypes.c_int64),
+        ("features", ctypes.c_int64),
+        ("inner", ctypes.c_int64),
+        ("pitch", ctypes.c_int64 * 5),
+        ("stream", ctypes.c_void_p),
+        ("workspace", ctypes.c_void_p),
+        ("workspace_bytes", ctypes.c_uint64),
+    ]
+
+
+class gleam_dropout_args(ctypes.Structure):
+    _fields_ = [
+        ("p", ctypes.c_double),
+        ("seed", ctypes.c_uint64),
+        ("offset", ctypes.c_uint64),
+        ("step", ctypes.c_void_p),
     ]
 
 
@@ -146,6 +178,21 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         lib.gleam_dc_set_fused.restype = None
         lib.gleam_dc_debug_fused.argtypes = [ctypes.c_int32, u64]
         lib.gleam_dc_debug_fused.restype = None
+        fp, mp = ctypes.POINTER(gleam_feature_dims), ctypes.POINTER(gleam_dropout_args)
+        lib.gleam_layer_norm_workspace_size.argtypes = [fp, ctypes.POINTER(u64)]
+        lib.gleam_layer_norm_workspace_size.restype = i32
+        lib.gleam_layer_norm_forward.argtypes = [vp, vp, vp, vp, vp, vp, fp]
+        lib.gleam_layer_norm_forward.restype = i32
+        lib.gleam_layer_norm_vjp.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, fp]
+        lib.gleam_layer_norm_vjp.restype = i32
+        lib.gleam_dropout_forward.argtypes = [vp, vp, vp, mp, fp]
+        lib.gleam_dropout_forward.restype = i32
+        lib.gleam_dropout_vjp.argtypes = [vp, vp, mp, fp]
+        lib.gleam_dropout_vjp.restype = i32
+        lib.gleam_dropout_add_layer_norm_forward.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, mp, fp]
+        lib.gleam_dropout_add_layer_norm_forward.restype = i32
+        lib.gleam_dropout_add_layer_norm_vjp.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, mp, fp]
+        lib.gleam_dropout_add_layer_norm_vjp.restype = i32
         lib.gleam_dc_launch_count.argtypes = []
         lib.gleam_dc_launch_count.restype = u64
         lib.gleam_dc_profile_begin.argtypes = []
@@ -311,6 +358,69 @@ def gleam_dc_set_fused(on: bool) -> None:
 def gleam_dc_debug_fused(withhold_item: int = -1, wait_limit_ns: int = 0) -> None:
     """Test aid: withhold one item of the persistent 3-D kernel and / or shorten its wait limit."""
     load_library().gleam_dc_debug_fused(int(withhold_item), int(wait_limit_ns))
+
+
+def make_feature_dims(dtype, weight_dtype, outer, features, inner, eps=0.0, pitch=(), stream=None, workspace=None,
+                      workspace_bytes=0) -> gleam_feature_dims:
+    """Fills a ``gleam_feature_dims``; ``pitch`` lists the pitches of the call's activation arrays (missing or 0 = contiguous),
+    ``stream`` and ``workspace`` are as for ``make_dims``."""
+    if stream is not None and not isinstance(stream, int):
+        stream = stream.cuda_stream
+    if workspace is not None and not isinstance(workspace, int):
+        workspace_bytes = workspace.numel() * workspace.element_size()
+        workspace = workspace.data_ptr()
+    return gleam_feature_dims(1, dtype, weight_dtype, eps, outer, features, inner, tuple(pitch), stream or None,
+                              workspace or None, workspace_bytes)
+
+
+def make_dropout_args(p, seed=0, offset=0, step=None) -> gleam_dropout_args:
+    """``step``: a one-element int64 CUDA tensor, a raw address or None."""
+    low = 0xFFFFFFFFFFFFFFFF
+    return gleam_dropout_args(float(p), int(seed) & low, int(offset) & low, _addr(step) or None)
+
+
+def gleam_layer_norm_workspace_size(dims: gleam_feature_dims) -> int:
+    out = ctypes.c_uint64(0)
+    _check((_lib or load_library()).gleam_layer_norm_workspace_size(ctypes.byref(dims), ctypes.byref(out)))
+    return int(out.value)
+
+
+def gleam_layer_norm_forward(x, weight, bias, y, mean, rstd, dims: gleam_feature_dims) -> None:
+    """y = (x - mean) rstd weight + bias over the features of each position; mean and rstd (float32) may be None."""
+    _check((_lib or load_library()).gleam_layer_norm_forward(_addr(x), _addr(weight), _addr(bias), _addr(y), _addr(mean),
+                                                             _addr(rstd), ctypes.byref(dims)))
+
+
+def gleam_layer_norm_vjp(grad_y, x, weight, mean, rstd, grad_x, grad_weight, grad_bias, dims: gleam_feature_dims) -> None:
+    _check((_lib or load_library()).gleam_layer_norm_vjp(_addr(grad_y), _addr(x), _addr(weight), _addr(mean), _addr(rstd),
+                                                         _addr(grad_x), _addr(grad_weight), _addr(grad_bias),
+                                                         ctypes.byref(dims)))
+
+
+def gleam_dropout_forward(x, residual, out, dropout: gleam_dropout_args, dims: gleam_feature_dims) -> None:
+    """out = [residual +] dropout(x); residual may be None."""
+    _check((_lib or load_library()).gleam_dropout_forward(_addr(x), _addr(residual), _addr(out), ctypes.byref(dropout),
+                                                          ctypes.byref(dims)))
+
+
+def gleam_dropout_vjp(grad_out, grad_x, dropout: gleam_dropout_args, dims: gleam_feature_dims) -> None:
+    _check((_lib or load_library()).gleam_dropout_vjp(_addr(grad_out), _addr(grad_x), ctypes.byref(dropout),
+                                                      ctypes.byref(dims)))
+
+
+def gleam_dropout_add_layer_norm_forward(x, residual, weight, bias, total, y, mean, rstd, dropout: gleam_dropout_args,
+                                         dims: gleam_feature_dims) -> None:
+    """total = residual + dropout(x), y = layer norm of total."""
+    _check((_lib or load_library()).gleam_dropout_add_layer_norm_forward(
+        _addr(x), _addr(residual), _addr(weight), _addr(bias), _addr(total), _addr(y), _addr(mean), _addr(rstd),
+        ctypes.byref(dropout), ctypes.byref(dims)))
+
+
+def gleam_dropout_add_layer_norm_vjp(grad_y, grad_sum, total, weight, mean, rstd, grad_x, grad_residual, grad_weight,
+                                     grad_bias, dropout: gleam_dropout_args, dims: gleam_feature_dims) -> None:
+    _check((_lib or load_library()).gleam_dropout_add_layer_norm_vjp(
+        _addr(grad_y), _addr(grad_sum), _addr(total), _addr(weight), _addr(mean), _addr(rstd), _addr(grad_x),
+        _addr(grad_residual), _addr(grad_weight), _addr(grad_bias), ctypes.byref(dropout), ctypes.byref(dims)))
 
 
 def gleam_dc_host_arena_size(dims: gleam_dims) -> int:

@@ -1,0 +1,20 @@
+// Launches of the prior's operators, one set for each element type (kernels_prior.cu).
+#pragma once
+#include <cuda_runtime.h>
+#include "prior_common.cuh"
+
+namespace gleam {
+namespace prior {
+
+struct Ops {
+    cudaError_t (*forward)(const Args& a, bool tail, cudaStream_t s);
+    cudaError_t (*vjp)(const Args& a, bool tail, cudaStream_t s);
+    cudaError_t (*dropout)(const Args& a, cudaStream_t s);
+};
+extern const Ops ops_f32, ops_f16, ops_bf16;
+
+// Rows of partial sums of the weights' gradients that a VJP writes.
+int weight_parts(const Args& a);
+
+}  // namespace prior
+}  // namespace gleam

@@ -1,0 +1,415 @@
+"""Operators of the learned prior on torch tensors: layer norm, dropout, and the residual tail that joins them.
+
+Two layers over the C calls (include/gleam.h states the formulas and the definition of the dropout mask):
+
+* ``*_forward`` / ``*_vjp``: one C call each on plain tensors; outputs are allocated, the workspace comes from torch's
+  allocator for the current stream, nothing is kept between calls;
+* ``layer_norm``, ``dropout``, ``dropout_add_layer_norm``: the same as autograd nodes.
+
+Tensors are CUDA tensors of float32, float16 or bfloat16, all of one type and shape; weights are float32 or of that type.
+``dim`` is the axis of the features.  A tensor may be a slice of a wider one along an axis before ``dim`` or along ``dim`` itself,
+or hold the features last in memory (``torch.channels_last``); any other order is refused.  No result depends on the layout
+but the dropout mask, which numbers the elements in memory order.
+"""
+from __future__ import annotations
+
+import torch
+
+from . import binding as _b
+
+_DTYPES = {torch.float32: _b.GLEAM_F32, torch.float16: _b.GLEAM_F16, torch.bfloat16: _b.GLEAM_BF16}
+
+
+class _View:
+    """(outer, features, inner) view of a tensor's memory; ``last`` where the features are last in memory but not in the shape."""
+    __slots__ = ("outer", "features", "inner", "pitch", "last")
+
+    def __init__(self, outer, features, inner, pitch, last):
+        self.outer, self.features, self.inner, self.pitch, self.last = outer, features, inner, pitch, last
+
+
+def _numel(sizes):
+    n = 1
+    for s in sizes:
+        n *= s
+    return n
+
+
+def _slices(shape, strides, dim):
+    """(outer, inner, pitch) if the axes from ``dim`` on are contiguous and those before step evenly, else None.  An axis of
+    length one steps anywhere."""
+    want = 1
+    for k in range(len(shape) - 1, dim - 1, -1):
+        if shape[k] != 1:
+            if strides[k] != want:
+                return None
+            want *= shape[k]
+    outer, pitch = 1, 0
+    for k in range(dim - 1, -1, -1):
+        if shape[k] == 1:
+            continue
+        if outer == 1:
+            pitch = strides[k]
+            if pitch < want:
+                return None
+        elif strides[k] != pitch * outer:
+            return None
+        outer *= shape[k]
+    return outer, _numel(shape[dim + 1:]), 0 if pitch == want else pitch
+
+
+def _view(t, dim):
+    shape = t.shape
+    if t.is_contiguous() or t.numel() == 0:
+        return _View(_numel(shape[:dim]), shape[dim], _numel(shape[dim + 1:]), 0, False)
+    got = _slices(shape, t.stride(), dim)
+    if got is not None:
+        return _View(got[0], shape[dim], got[1], got[2], False)
+    m = t.movedim(dim, -1)
+    got = _slices(m.shape, m.stride(), len(shape) - 1)
+    if got is not None:
+        return _View(got[0], shape[dim], 1, got[2], True)
+    raise ValueError("memory order not supported (shape %s, strides %s, features at axis %d): call .contiguous()"
+                     % (tuple(shape), tuple(t.stride()), dim))
+
+
+def _like(t, dim, view):
+    """A dense tensor of the same shape, type and order."""
+    if not view.last:
+        return torch.empty(t.shape, dtype=t.dtype, device=t.device)
+    shape = list(t.shape)
+    shape.append(shape.pop(dim))
+    return torch.empty(shape, dtype=t.dtype, device=t.device).movedim(-1, dim)
+
+
+def _check_kind(x):
+    if not isinstance(x, torch.Tensor) or not x.is_cuda:
+        raise ValueError("expected CUDA tensors: there is no CPU fallback")
+    if x.dtype not in _DTYPES:
+        raise ValueError("type %s is not supported" % x.dtype)
+
+
+def _features_axis(x, dim):
+    _check_kind(x)
+    if x.dim() == 0 or not -x.dim() <= dim < x.dim():
+        raise ValueError("no axis %d in shape %s" % (dim, tuple(x.shape)))
+    dim %= x.dim()
+    if x.shape[dim] == 0:
+        raise ValueError("no features (shape %s)" % (tuple(x.shape),))
+    return dim
+
+
+def _same_kind(x, t, what):
+    if t.shape != x.shape or t.dtype != x.dtype or t.device != x.device:
+        raise ValueError("%s: %s %s on %s where %s %s on %s is wanted" % (what, tuple(t.shape), t.dtype, t.device,
+                                                                         tuple(x.shape), x.dtype, x.device))
+
+
+def _same(x, t, view, dim, what):
+    """The view of another activation tensor of the same call."""
+    _same_kind(x, t, what)
+    v = _view(t, dim)
+    if (v.outer, v.inner) != (view.outer, view.inner):
+        raise ValueError("%s has its elements in another order than the first tensor" % what)
+    return v
+
+
+def _match(x, t, dim):
+    """``t`` itself if the calls take it next to ``x``, else a copy in x's order (cotangents come in any order)."""
+    view = _view(x, dim)
+    try:
+        v = _view(t, dim)
+        if (v.outer, v.inner) == (view.outer, view.inner):
+            return t
+    except ValueError:
+        pass
+    return _like(x, dim, view).copy_(t)
+
+
+def _weight_type(x, features, *vectors):
+    """The type of the weights.  None stands for ones or zeros."""
+    kind = None
+    for w in vectors:
+        if w is None:
+            continue
+        if w.shape != (features,) or w.device != x.device or not w.is_contiguous():
+            raise ValueError("weights: a contiguous vector of %d features on %s is wanted" % (features, x.device))
+        if w.dtype not in (torch.float32, x.dtype) or kind not in (None, w.dtype):
+            raise ValueError("weights: %s where float32 or %s is wanted, the same for all" % (w.dtype, x.dtype))
+        kind = w.dtype
+    return torch.float32 if kind is None else kind
+
+
+def _check_statistics(x, dim, mean, rstd):
+    shape = x.shape[:dim] + x.shape[dim + 1:]
+    for t in (mean, rstd):
+        if t.shape != shape or t.dtype != torch.float32 or t.device != x.device or not t.is_contiguous():
+            raise ValueError("statistics: contiguous float32 of shape %s is wanted" % (tuple(shape),))
+
+
+def _stream(x):
+    """Handle of the current stream of the tensor's device."""
+    if x.get_device() != torch.cuda.current_device():
+        return torch.cuda.current_stream(x.device).cuda_stream
+    return _b._current_stream_handle()
+
+
+def _dims(x, wtype, view, eps, pitches):
+    return _b.gleam_feature_dims(1, _DTYPES[x.dtype], _DTYPES[wtype], eps, view.outer, view.features, view.inner, pitches,
+                                 _stream(x) or None, None, 0)
+
+
+class _On:
+    """The tensor's device as the current one, for a call's duration."""
+    __slots__ = ("other",)
+
+    def __init__(self, x):
+        self.other = None if x.get_device() == torch.cuda.current_device() else torch.cuda.device(x.device)
+
+    def __enter__(self):
+        if self.other is not None:
+            self.other.__enter__()
+
+    def __exit__(self, *a):
+        if self.other is not None:
+            self.other.__exit__(*a)
+
+
+def _drop_args(x, p, seed, offset, step):
+    if not 0.0 <= p <= 1.0:
+        raise ValueError("p = %r is not a probability" % (p,))
+    if step is not None and (step.dtype != torch.int64 or step.numel() != 1 or step.device != x.device):
+        raise ValueError("step: one int64 value on %s is wanted" % x.device)
+    return _b.make_dropout_args(p, seed, offset, step)
+
+
+def _workspace(x, dims, wanted):
+    """Scratch of a VJP from torch's allocator, put into ``dims``; the caller holds it until the call is made."""
+    if not wanted:
+        return None
+    ws = torch.empty(max(_b.gleam_layer_norm_workspace_size(dims), 256), dtype=torch.uint8, device=x.device)
+    dims.workspace, dims.workspace_bytes = ws.data_ptr(), ws.numel()
+    return ws
+
+
+def layer_norm_forward(x, weight=None, bias=None, eps=1e-5, dim=-1):
+    """(y, mean, rstd): y = (x - mean) rstd weight + bias over axis ``dim``; mean and rstd are float32 without that axis."""
+    dim = _features_axis(x, dim)
+    v = _view(x, dim)
+    wtype = _weight_type(x, v.features, weight, bias)
+    y = _like(x, dim, v)
+    mean = torch.empty(x.shape[:dim] + x.shape[dim + 1:], dtype=torch.float32, device=x.device)
+    rstd = torch.empty_like(mean)
+    with _On(x):
+        _b.gleam_layer_norm_forward(x, weight, bias, y, mean, rstd, _dims(x, wtype, v, eps, (v.pitch,)))
+    return y, mean, rstd
+
+
+def layer_norm_vjp(grad_y, x, weight, mean, rstd, dim=-1, weight_grad=True, bias_grad=True):
+    """(grad_x, grad_weight, grad_bias) of ``layer_norm_forward``; the last two are None where they are not wanted."""
+    dim = _features_axis(x, dim)
+    v = _view(x, dim)
+    vg = _same(x, grad_y, v, dim, "grad_y")
+    wtype = _weight_type(x, v.features, weight)
+    _check_statistics(x, dim, mean, rstd)
+    gx = _like(x, dim, v)
+    gw = torch.empty(v.features, dtype=wtype, device=x.device) if weight_grad else None
+    gb = torch.empty(v.features, dtype=wtype, device=x.device) if bias_grad else None
+    with _On(x):
+        dims = _dims(x, wtype, v, 0.0, (vg.pitch, v.pitch))
+        ws = _workspace(x, dims, weight_grad or bias_grad)
+        _b.gleam_layer_norm_vjp(grad_y, x, weight, mean, rstd, gx, gw, gb, dims)
+    del ws
+    return gx, gw, gb
+
+
+def _memory_order(x):
+    """The axes from the slowest to the fastest in memory."""
+    strides = x.stride()
+    return sorted(range(x.dim()), key=lambda k: -strides[k])
+
+
+def _flat(first, *others):
+    """(outer, elements of a slice, pitches) for a call that knows no features; the tensors have one memory order."""
+    if all(t.is_contiguous() for t in (first,) + others):
+        return 1, first.numel(), [0] * (1 + len(others))
+    axes = _memory_order(first)
+    tensors = [t.permute(axes) for t in (first,) + others]
+    for dim in range(first.dim()):
+        got = [_slices(t.shape, t.stride(), dim) for t in tensors]
+        if None not in got:
+            return got[0][0], _numel(tensors[0].shape[dim:]), [g[2] for g in got]
+    raise ValueError("memory order not supported (shape %s, strides %s): call .contiguous()"
+                     % (tuple(first.shape), " and ".join(str(tuple(t.stride())) for t in (first,) + others)))
+
+
+def dropout_forward(x, p, seed, offset, residual=None, step=None):
+    """[residual +] dropout(x).  The call takes ceil(x.numel() / 4) counters from ``offset``."""
+    _check_kind(x)
+    others = ()
+    if residual is not None:
+        _same_kind(x, residual, "residual")
+        others = (residual,)
+    outer, slice_, pitch = (1, 0, [0, 0]) if x.numel() == 0 else _flat(x, *others)
+    args = _drop_args(x, p, seed, offset, step)
+    if x.is_contiguous():
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    else:                                            # dense, in x's order
+        axes = _memory_order(x)
+        out = torch.empty([x.shape[k] for k in axes], dtype=x.dtype, device=x.device)
+        out = out.permute([axes.index(k) for k in range(x.dim())])
+    with _On(x):
+        dims = _b.gleam_feature_dims(1, _DTYPES[x.dtype], _b.GLEAM_F32, 0.0, outer, 1, slice_, tuple(pitch),
+                                     _stream(x) or None, None, 0)
+        _b.gleam_dropout_forward(x, residual, out, args, dims)
+    return out
+
+
+def dropout_vjp(grad_out, p, seed, offset, step=None):
+    """Gradient with respect to x of ``dropout_forward`` with the same arguments (that of residual is grad_out itself);
+    grad_out has x's memory order."""
+    return dropout_forward(grad_out, p, seed, offset, None, step)
+
+
+def dropout_add_layer_norm_forward(x, residual, weight, bias, p, seed, offset, eps=1e-5, dim=-1, step=None):
+    """(y, total, mean, rstd): total = residual + dropout(x), y = layer norm of total over axis ``dim``."""
+    dim = _features_axis(x, dim)
+    v = _view(x, dim)
+    vr = _same(x, residual, v, dim, "residual")
+    wtype = _weight_type(x, v.features, weight, bias)
+    args = _drop_args(x, p, seed, offset, step)
+    y, total = _like(x, dim, v), _like(x, dim, v)
+    mean = torch.empty(x.shape[:dim] + x.shape[dim + 1:], dtype=torch.float32, device=x.device)
+    rstd = torch.empty_like(mean)
+    with _On(x):
+        _b.gleam_dropout_add_layer_norm_forward(x, residual, weight, bias, total, y, mean, rstd, args,
+                                                _dims(x, wtype, v, eps, (v.pitch, vr.pitch)))
+    return y, total, mean, rstd
+
+
+def dropout_add_layer_norm_vjp(grad_y, grad_total, total, weight, mean, rstd, p, seed, offset, dim=-1, step=None,
+                               weight_grad=True, bias_grad=True):
+    """(grad_x, grad_residual, grad_weight, grad_bias); ``grad_total`` (None: zero) is the cotangent of total."""
+    dim = _features_axis(total, dim)
+    v = _view(total, dim)
+    vg = _same(total, grad_y, v, dim, "grad_y")
+    vs = v if grad_total is None else _same(total, grad_total, v, dim, "grad_total")
+    wtype = _weight_type(total, v.features, weight)
+    _check_statistics(total, dim, mean, rstd)
+    args = _drop_args(total, p, seed, offset, step)
+    gx, gr = _like(total, dim, v), _like(total, dim, v)
+    gw = torch.empty(v.features, dtype=wtype, device=total.device) if weight_grad else None
+    gb = torch.empty(v.features, dtype=wtype, device=total.device) if bias_grad else None
+    with _On(total):
+        dims = _dims(total, wtype, v, 0.0, (vg.pitch, vs.pitch, v.pitch))
+        ws = _workspace(total, dims, weight_grad or bias_grad)
+        _b.gleam_dropout_add_layer_norm_vjp(grad_y, grad_total, total, weight, mean, rstd, gx, gr, gw, gb, args, dims)
+    del ws
+    return gx, gr, gw, gb
+
+
+# ---- autograd ------------------------------------------------------------------------------------------------------------
+
+class DropoutGenerator:
+    """Counter ranges for the dropout sites of a model: every call takes the range behind the last one, so no two share a mask.
+
+    ``capturable=True`` adds a counter on the device that the kernels read when they run: a captured training step ends with
+    ``advance()`` inside the graph, and every replay draws new masks with the ranges it was captured with.  The counter must
+    not move between a forward call and its backward pass, and the generator lives as long as a graph that reads it.
+    """
+
+    def __init__(self, seed, device="cuda", capturable=False):
+        self.seed, self.offset = int(seed), 0
+        self.step = torch.zeros(1, dtype=torch.int64, device=device) if capturable else None
+
+    def take(self, numel):
+        offset = self.offset
+        self.offset += (int(numel) + 3) // 4
+        return offset
+
+    def advance(self):
+        if self.step is None:
+            raise RuntimeError("advance() needs capturable=True")
+        self.step.add_(1)
+
+
+class _LayerNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, eps, dim):
+        y, mean, rstd = layer_norm_forward(x, weight, bias, eps, dim)
+        ctx.save_for_backward(x, weight, mean, rstd)
+        ctx.dim = dim
+        return y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad):
+        x, weight, mean, rstd = ctx.saved_tensors
+        dim = ctx.dim % x.dim()
+        gx, gw, gb = layer_norm_vjp(_match(x, grad, dim), x, weight, mean, rstd, dim, ctx.needs_input_grad[1],
+                                    ctx.needs_input_grad[2])
+        return gx, gw, gb, None, None
+
+
+class _Dropout(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, residual, p, seed, offset, step):
+        out = dropout_forward(x, p, seed, offset, residual, step)
+        ctx.save_for_backward(step)
+        ctx.args = p, seed, offset
+        ctx.axes = _memory_order(x)
+        return out
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad):
+        (step,) = ctx.saved_tensors
+        gx = None
+        if ctx.needs_input_grad[0]:
+            axes = ctx.axes                              # the mask numbers elements in x's memory order
+            gx = dropout_vjp(grad.permute(axes).contiguous(), *ctx.args, step=step)
+            gx = gx.permute([axes.index(k) for k in range(len(axes))])
+        return gx, grad, None, None, None, None
+
+
+class _Tail(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, residual, weight, bias, p, seed, offset, eps, dim, step):
+        y, total, mean, rstd = dropout_add_layer_norm_forward(x, residual, weight, bias, p, seed, offset, eps, dim, step)
+        ctx.save_for_backward(total, weight, mean, rstd, step)
+        ctx.args, ctx.dim = (p, seed, offset), dim
+        ctx.set_materialize_grads(False)
+        return y, total
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad_y, grad_total):
+        total, weight, mean, rstd, step = ctx.saved_tensors
+        dim = ctx.dim % total.dim()
+        none = (None,) * 6
+        if grad_y is None and grad_total is None:
+            return (None,) * 4 + none
+        grad_y = torch.zeros_like(total) if grad_y is None else _match(total, grad_y, dim)
+        if grad_total is not None:
+            grad_total = _match(total, grad_total, dim)
+        gx, gr, gw, gb = dropout_add_layer_norm_vjp(grad_y, grad_total, total, weight, mean, rstd, *ctx.args, dim, step,
+                                                    ctx.needs_input_grad[2], ctx.needs_input_grad[3])
+        return (gx, gr, gw, gb) + none
+
+
+def layer_norm(x, weight=None, bias=None, eps=1e-5, dim=-1):
+    """Layer norm over axis ``dim`` with gradients for x, weight and bias."""
+    return _LayerNorm.apply(x, weight, bias, eps, dim)
+
+
+def dropout(x, p, generator: DropoutGenerator, residual=None):
+    """[residual +] dropout(x) with the next range of the generator; the backward pass draws the mask again."""
+    return _Dropout.apply(x, residual, p, generator.seed, generator.take(x.numel()), generator.step)
+
+
+def dropout_add_layer_norm(x, residual, weight, bias, p, generator=None, eps=1e-5, dim=-1):
+    """(y, total) of the residual tail, with gradients; ``generator`` may be None where p is 0."""
+    if generator is None and p != 0:
+        raise ValueError("dropout needs a generator")
+    seed, offset, step = (0, 0, None) if generator is None else (generator.seed, generator.take(x.numel()), generator.step)
+    return _Tail.apply(x, residual, weight, bias, p, seed, offset, eps, dim, step)

@@ -1,0 +1,206 @@
+"""Operators of the learned prior without a GPU: the definition of the mask, host-side refusals of the C calls, and the views
+that the torch layer makes of strided tensors."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2207_08393_b200 as g
+from oracle import prior_oracle as po
+from paper_2207_08393_b200 import _build, binding, prior_ops
+
+
+@pytest.fixture(scope="module")
+def lib():
+    _build.build()
+    return g.load_library()
+
+
+@pytest.mark.parametrize("counter,key,out", [       # published test vectors of Philox4x32-10
+    ((0, 0, 0, 0), (0, 0), (0x6627E8D5, 0xE169C58D, 0xBC57AC4C, 0x9B00DBD8)),
+    ((0xFFFFFFFF,) * 4, (0xFFFFFFFF,) * 2, (0x408F276D, 0x41C83B0E, 0xA20BC7C6, 0x6D5451FD)),
+    ((0x243F6A88, 0x85A308D3, 0x13198A2E, 0x03707344), (0xA4093822, 0x299F31D0), (0xD16CFE09, 0x94FDCCEB, 0x5001E420, 0x24126EA1)),
+])
+def test_philox_known_answers(counter, key, out):
+    assert tuple(po.philox(counter, key)) == out
+
+
+@pytest.mark.parametrize("offset,step", [(0, 0), (2 ** 32 - 2, 5), (2 ** 64 - 3, 2 ** 40 + 1)])
+def test_vectorised_words_are_philox(offset, step):
+    seed = 0x0123456789ABCDEF
+    got = po.words(23, seed, offset, step)
+    for i in range(23):
+        block = (offset + i // 4) % 2 ** 64
+        ref = po.philox((block & 0xFFFFFFFF, block >> 32, step & 0xFFFFFFFF, step >> 32), (seed & 0xFFFFFFFF, seed >> 32))
+        assert int(got[i]) == ref[i % 4]
+
+
+def test_the_oracle_gradient_is_the_difference_quotient():
+    rng = np.random.default_rng(0)
+    x, w, b, dy = rng.normal(size=(2, 5, 3)), rng.normal(size=5), rng.normal(size=5), rng.normal(size=(2, 5, 3))
+    y, mean, rstd = po.layer_norm(x, w, b, 1e-3)
+    gx, gw, gb = po.layer_norm_vjp(dy, x, w, mean, rstd)
+    f = lambda x, w, b: float((po.layer_norm(x, w, b, 1e-3)[0] * dy).sum())
+    for which, grad in ((0, gx), (1, gw), (2, gb)):
+        args = [x, w, b]
+        for at in np.ndindex(args[which].shape):
+            up, down = [a.copy() for a in args], [a.copy() for a in args]
+            up[which][at] += 1e-6
+            down[which][at] -= 1e-6
+            assert abs((f(*up) - f(*down)) / 2e-6 - grad[at]) < 1e-6
+
+
+def test_struct_layout_matches_the_header():
+    d = binding.gleam_feature_dims
+    assert (d.eps.offset, d.outer.offset, d.pitch.offset, d.stream.offset) == (12, 16, 40, 80)
+    assert ctypes.sizeof(d) == 104 and ctypes.sizeof(binding.gleam_dropout_args) == 32
+
+
+A = 1 << 30                                         # addresses that are never dereferenced
+BAD, NULL = binding.GLEAM_ERR_BAD_DIMS, binding.GLEAM_ERR_NULL_POINTER
+
+
+def feature_dims(**kw):
+    args = dict(dtype=0, weight_dtype=0, outer=4, features=8, inner=1, eps=1e-5)
+    args.update(kw)
+    return g.make_feature_dims(**args)
+
+
+def status(call, *args):
+    with pytest.raises(g.GleamError) as e:
+        call(*args)
+    return e.value.status
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(dtype=3), BAD), (dict(dtype=-1), BAD), (dict(weight_dtype=1), BAD), (dict(dtype=1, weight_dtype=2), BAD),
+    (dict(features=0), BAD), (dict(outer=-1), BAD), (dict(inner=-2), BAD), (dict(pitch=[7]), BAD), (dict(pitch=[0, -8]), BAD),
+    (dict(features=(1 << 24) + 1), BAD), (dict(inner=1 << 50), BAD), (dict(outer=1 << 45), BAD), (dict(pitch=[1 << 47]), BAD),
+    (dict(eps=-1.0), BAD), (dict(eps=float("nan")), BAD), (dict(eps=float("inf")), BAD),
+])
+def test_bad_dims(lib, kw, code):
+    d = feature_dims(**kw)
+    assert status(g.gleam_layer_norm_forward, A, None, None, 2 * A, None, None, d) == code
+    if "eps" not in kw:
+        assert status(g.gleam_layer_norm_workspace_size, d) == code
+        assert status(g.gleam_dropout_forward, A, None, 2 * A, g.make_dropout_args(0.5), d) == code
+    d.struct_version = 7
+    assert status(g.gleam_layer_norm_forward, A, None, None, 2 * A, None, None, d) == BAD
+
+
+@pytest.mark.parametrize("p", [-0.1, 1.0000001, float("nan")])
+def test_bad_probabilities(lib, p):
+    assert status(g.gleam_dropout_forward, A, None, 2 * A, g.make_dropout_args(p), feature_dims()) == BAD
+    assert status(g.gleam_dropout_add_layer_norm_forward, A, 2 * A, None, None, 3 * A, 4 * A, None, None,
+                  g.make_dropout_args(p), feature_dims()) == BAD
+
+
+def test_null_pointers(lib):
+    d, m = feature_dims(), g.make_dropout_args(0.5)
+    for at in (0, 3):
+        args = [A, None, None, 2 * A, None, None, d]
+        args[at] = None
+        assert status(g.gleam_layer_norm_forward, *args) == NULL
+    for at in (0, 1, 3, 4, 5):
+        args = [A, 2 * A, None, 3 * A, 4 * A, 5 * A, None, None, d]
+        args[at] = None
+        assert status(g.gleam_layer_norm_vjp, *args) == NULL
+    for at in (0, 2):
+        args = [A, None, 2 * A, m, d]
+        args[at] = None
+        assert status(g.gleam_dropout_forward, *args) == NULL
+    for at in (0, 1, 4, 5):
+        args = [A, 2 * A, None, None, 3 * A, 4 * A, None, None, m, d]
+        args[at] = None
+        assert status(g.gleam_dropout_add_layer_norm_forward, *args) == NULL
+    for at in (0, 2, 4, 5, 6, 7):
+        args = [A, None, 2 * A, None, 3 * A, 4 * A, 5 * A, 6 * A, None, None, m, d]
+        args[at] = None
+        assert status(g.gleam_dropout_add_layer_norm_vjp, *args) == NULL
+    lib = g.load_library()
+    assert lib.gleam_dropout_vjp(A, 2 * A, None, ctypes.byref(d)) == NULL
+    assert lib.gleam_dropout_vjp(A, 2 * A, ctypes.byref(m), None) == NULL
+    assert lib.gleam_layer_norm_workspace_size(ctypes.byref(d), None) == NULL
+
+
+def test_misaligned_pointers_and_workspace(lib):
+    d = feature_dims()
+    assert status(g.gleam_layer_norm_forward, A + 2, None, None, 2 * A, None, None, d) == BAD
+    assert status(g.gleam_layer_norm_forward, A, 3 * A + 2, None, 2 * A, None, None, d) == BAD
+    assert status(g.gleam_dropout_forward, A, None, 2 * A, g.make_dropout_args(0.5, step=3 * A + 4), d) == BAD
+    args = (A, 2 * A, None, 3 * A, 4 * A, 5 * A, 6 * A, None)
+    assert status(g.gleam_layer_norm_vjp, *args, d) == NULL                                   # a weight gradient needs scratch
+    assert status(g.gleam_layer_norm_vjp, *args, feature_dims(workspace=7 * A, workspace_bytes=8)) == binding.GLEAM_ERR_WORKSPACE_TOO_SMALL
+    assert status(g.gleam_layer_norm_vjp, *args, feature_dims(workspace=7 * A + 16, workspace_bytes=1 << 20)) == BAD
+
+
+def test_calls_on_nothing_need_no_pointers(lib):
+    for kw in (dict(outer=0), dict(inner=0)):
+        d, m = feature_dims(**kw), g.make_dropout_args(0.5)
+        assert g.gleam_layer_norm_workspace_size(d) == 0
+        g.gleam_layer_norm_forward(None, None, None, None, None, None, d)
+        g.gleam_dropout_forward(None, None, None, m, d)
+        g.gleam_dropout_vjp(None, None, m, d)
+        g.gleam_layer_norm_vjp(None, None, None, None, None, None, None, None, d)
+        g.gleam_dropout_add_layer_norm_forward(None, None, None, None, None, None, None, None, m, d)
+
+
+def test_cpu_tensors_are_refused():
+    x = torch.zeros(4, 8)
+    with pytest.raises(ValueError, match="no CPU fallback"):
+        g.layer_norm_forward(x)
+    with pytest.raises(ValueError, match="no CPU fallback"):
+        g.dropout_forward(x, 0.5, 0, 0)
+
+
+def address(view, o, c, k):
+    pitch = view.pitch or view.features * view.inner
+    return o * pitch + (c * view.inner + k)
+
+
+@pytest.mark.parametrize("make,dim", [
+    (lambda: torch.empty(3, 4, 5), 1), (lambda: torch.empty(3, 4, 5), 0), (lambda: torch.empty(3, 4, 5), 2),
+    (lambda: torch.empty(3, 9, 5)[:, 2:6], 1),                       # features of a wider array
+    (lambda: torch.empty(6, 4, 5)[::2], 1),                          # every other slice
+    (lambda: torch.empty(3, 7, 4, 5)[:, 1:2], 2),
+    (lambda: torch.empty(2, 4, 3, 5).to(memory_format=torch.channels_last), 1),
+    (lambda: torch.empty(7, 4).t(), 0),                              # features last in memory
+    (lambda: torch.empty(7, 6)[:, :4], 1),
+    (lambda: torch.empty(1, 4, 5).expand(1, 4, 5), 1),
+    (lambda: torch.empty(5), 0),
+])
+def test_views_address_the_elements(make, dim):
+    t = make()
+    v = prior_ops._view(t, dim)
+    index = torch.arange(t.numel()).view(t.shape)
+    assert v.outer * v.features * v.inner == t.numel() and v.features == t.shape[dim]
+    flat = [sum(i * s for i, s in zip(at, t.stride())) for at in np.ndindex(*t.shape)]
+    order = (index.movedim(dim, -1) if v.last else index).reshape(v.outer, v.features, v.inner)
+    for o in range(v.outer):
+        for c in range(v.features):
+            for k in range(v.inner):
+                assert flat[int(order[o, c, k])] == address(v, o, c, k)
+    like = prior_ops._like(t, dim, v)
+    assert like.shape == t.shape and prior_ops._view(like, dim).pitch in (0, v.features * v.inner)
+    assert (prior_ops._view(like, dim).outer, prior_ops._view(like, dim).inner) == (v.outer, v.inner)
+
+
+@pytest.mark.parametrize("make,dim", [
+    (lambda: torch.empty(4, 3, 5).transpose(0, 2), 1),
+    (lambda: torch.empty(1, 4, 5).expand(3, 4, 5), 1),               # the same memory three times
+    (lambda: torch.empty(3, 4, 10)[:, :, ::2], 1),
+    (lambda: torch.empty(4, 6, 4, 5)[::2, ::3], 2),                  # uneven steps before the features
+])
+def test_other_orders_are_refused(make, dim):
+    with pytest.raises(ValueError, match="contiguous"):
+        prior_ops._view(make(), dim)
+
+
+def test_generator_ranges_do_not_meet():
+    gen = prior_ops.DropoutGenerator(3, device="cpu", capturable=True)
+    assert [gen.take(n) for n in (1, 4, 5, 0, 8)] == [0, 1, 2, 4, 4] and gen.offset == 6
+    gen.advance()
+    assert int(gen.step) == 1
+    with pytest.raises(RuntimeError):
+        prior_ops.DropoutGenerator(3, device="cpu").advance()

@@ -369,7 +369,7 @@ class _Dropout(torch.autograd.Function):
             axes = ctx.axes                              # the mask numbers elements in x's memory order
             gx = dropout_vjp(grad.permute(axes).contiguous(), *ctx.args, step=step)
             gx = gx.permute([axes.index(k) for k in range(len(axes))])
-        return gx, grad, None, None, None, None
+        return gx, grad if ctx.needs_input_grad[1] else None, None, None, None, None
 
 
 class _Tail(torch.autograd.Function):

@@ -1,7 +1,13 @@
 // Instantiation unit of the prior's operators for one element type: GLEAM_PRIOR_TYPE is 0 (float32), 1 (float16) or 2 (bfloat16).
 #include "dc_entry.h"
 #include "prior_entry.h"
+#include "prior_dropout.cuh"
 #include "prior_norm.cuh"
+#include "prior_rows.cuh"
+
+#include <initializer_list>
+#include <type_traits>
+#include <utility>
 
 namespace gleam {
 namespace prior {
@@ -23,10 +29,84 @@ using T = __nv_bfloat16;
 static unsigned bounded(long long n, long long most) { return (unsigned)(n < 1 ? 1 : n < most ? n : most); }
 constexpr long long GRID = 1ll << 20;                    // blocks of a launch at most; the kernels stride over what is beyond
 
-static cudaError_t forward(const Args& a, bool tail, cudaStream_t s) {
+using yes = std::true_type;
+using no = std::false_type;
+template <int N> using number = std::integral_constant<int, N>;
+
+// Whether all the arrays (null: absent) start at 16 bytes and, where they step, step by multiples of them more than `beyond`.
+static bool packed(const Args& a, long long beyond, std::initializer_list<std::pair<const void*, long long>> arrays) {
+    for (const auto& v : arrays)
+        if (v.first && ((uintptr_t)v.first % 16 != 0 || (a.outer > 1 && (v.second - beyond) % VEC<T> != 0))) return false;
+    return true;
+}
+
+// How rows are dealt to teams of threads (prior_rows.cuh); fits = false where a row is too long for one.
+struct RowPlan {
+    bool fits, edges;
+    int team, items, warps, teams, threads;      // lanes of a team (0: warps of it), pieces a thread, teams and threads a block
+    unsigned grid;
+};
+static RowPlan row_plan(const Args& a, bool vjp) {
+    RowPlan p{};
+    constexpr int V = VEC<T>, WARPS = ROW_TEAMS_THREADS / 32;
+    p.edges = !a.aligned || a.features % V != 0;
+    const long long pieces = p.edges ? (a.features + 2 * (V - 1)) / V : a.features / V;
+    // eight features a thread where that is at most 16 warps (registers), else sixteen
+    const int few = 8 / V, many = 16 / V;
+    p.items = pieces <= 32 ? 1 : pieces <= 32ll * few * WARPS ? few : many;
+    if (pieces > 32ll * many * WARPS) return p;
+    p.fits = true;
+    if (pieces <= 32 * p.items) {
+        p.team = p.items > 1 || pieces > 16 ? 32 : pieces > 8 ? 16 : pieces > 4 ? 8 : 4;
+        p.warps = 1;
+        p.teams = ROW_TEAMS_THREADS / p.team;
+        p.threads = ROW_TEAMS_THREADS;
+    } else {
+        p.team = 0;
+        p.warps = (int)((pieces + 32 * p.items - 1) / (32 * p.items));
+        p.teams = WARPS / p.warps;
+        p.threads = p.teams * p.warps * 32;
+    }
+    const long long need = (a.outer + p.teams - 1) / p.teams;
+    long long most = vjp || p.items * V > 8 ? SMS : 2 * SMS;      // blocks that are resident at once
+    // the rows of a team lie alike if teams go on by multiples of V rows
+    if (p.edges) while (most * p.teams % V) --most;
+    p.grid = (unsigned)(need < most ? need : most);
+    // a few rows per team in one block: it writes the weights' gradients itself
+    if (vjp && (a.gw || a.gb) && need > 1 && need <= 4 && (!p.edges || p.teams % V == 0)) p.grid = 1;
+    return p;
+}
+
+template <bool VJP, bool TAIL, bool EDGES>
+static auto row_kernel(const RowPlan& p) {
+    auto pick = [&](auto team, auto items) {
+        constexpr int G = decltype(team)::value, I = decltype(items)::value;
+        if constexpr (VJP) return row_team_vjp<T, G, I, EDGES, TAIL>;
+        else return row_team_forward<T, G, I, EDGES, TAIL>;
+    };
+    constexpr int FEW = 8 / VEC<T>, MANY = 16 / VEC<T>;
+    switch (p.team) {
+        case 4: return pick(number<4>{}, number<1>{});
+        case 8: return pick(number<8>{}, number<1>{});
+        case 16: return pick(number<16>{}, number<1>{});
+        case 32: return p.items == 1 ? pick(number<32>{}, number<1>{}) : pick(number<32>{}, number<FEW>{});
+        default: return p.items == FEW ? pick(number<0>{}, number<FEW>{}) : pick(number<0>{}, number<MANY>{});
+    }
+}
+template <bool VJP>
+static auto row_kernel(const RowPlan& p, bool tail) {
+    return tail ? (p.edges ? row_kernel<VJP, true, true>(p) : row_kernel<VJP, true, false>(p))
+                : (p.edges ? row_kernel<VJP, false, true>(p) : row_kernel<VJP, false, false>(p));
+}
+
+static cudaError_t forward(const Args& given, bool tail, cudaStream_t s) {
+    Args a = given;
     if (a.inner == 1) {
+        a.aligned = packed(a, a.features, {{a.x, a.px}, {a.res, a.pres}, {a.out, a.pout}, {a.out2, a.pout2}});
+        const RowPlan p = row_plan(a, false);
         const dim3 grid(bounded(a.outer, GRID));
-        if (tail) PRIOR_LAUNCH(row_forward<T, true>, grid, dim3(ROW_THREADS), 0, s, a);
+        if (p.fits) PRIOR_LAUNCH(row_kernel<false>(p, tail), dim3(p.grid), dim3(p.threads), p.teams * p.warps * 6 * sizeof(float), s, a, p.warps, p.teams);
+        else if (tail) PRIOR_LAUNCH(row_forward<T, true>, grid, dim3(ROW_THREADS), 0, s, a);
         else PRIOR_LAUNCH(row_forward<T, false>, grid, dim3(ROW_THREADS), 0, s, a);
     } else {
         const dim3 grid(bounded((a.outer * a.inner + 31) / 32, GRID));
@@ -36,14 +116,34 @@ static cudaError_t forward(const Args& a, bool tail, cudaStream_t s) {
     return prof_mark(-1, s);
 }
 
-static cudaError_t vjp(const Args& a, bool tail, cudaStream_t s) {
+static cudaError_t weight_grads_from(const Args& a, int parts, cudaStream_t s) {
+    PRIOR_LAUNCH(weight_grads<T>, dim3((unsigned)((a.features + 31) / 32), 2), dim3(256), 0, s, a, parts);
+    return cudaSuccess;
+}
+
+static cudaError_t vjp(const Args& given, bool tail, cudaStream_t s) {
+    Args a = given;
+    cudaError_t e;
+    if (a.inner == 1) {
+        a.aligned = packed(a, a.features, {{a.x, a.px}, {a.res, a.pres}, {a.gsum, a.pgsum}, {a.out, a.pout}, {a.out2, a.pout2}});
+        const RowPlan p = row_plan(a, true);
+        if (p.fits) {
+            size_t shared = p.teams * p.warps * 6 * sizeof(float);
+            if (p.teams > 1 && shared < 2 * (size_t)a.features * sizeof(float)) shared = 2 * (size_t)a.features * sizeof(float);
+            PRIOR_LAUNCH(row_kernel<true>(p, tail), dim3(p.grid), dim3(p.threads), shared, s, a, p.warps, p.teams);
+            if ((a.gw || a.gb) && p.grid > 1 && (e = weight_grads_from(a, (int)p.grid, s)) != cudaSuccess) return e;
+            return prof_mark(-1, s);
+        }
+    }
     // the weights' gradients first: grad_x may take grad_y's place
     if (a.gw || a.gb) {
-        const int parts = weight_parts(a);
         const unsigned pieces = (unsigned)((a.features + 31) / 32);
+        // enough blocks to fill the GPU over the pieces of features, each with some hundred positions at least
+        const long long wide = a.inner == 1 ? pieces : a.features, share = (a.outer * a.inner + 255) / 256, fill = (8 * SMS + wide - 1) / wide;
+        const int parts = (int)bounded(fill < share ? fill : share, PARTS_MOST);
         if (a.inner == 1) PRIOR_LAUNCH(row_weight_sums<T>, dim3(pieces, parts), dim3(256), 0, s, a);
         else PRIOR_LAUNCH(map_weight_sums<T>, dim3((unsigned)a.features, parts), dim3(256), 0, s, a);
-        PRIOR_LAUNCH(weight_grads<T>, dim3(pieces, 2), dim3(256), 0, s, a, parts);
+        if ((e = weight_grads_from(a, parts, s)) != cudaSuccess) return e;
     }
     if (a.inner == 1) {
         const dim3 grid(bounded(a.outer, GRID));
@@ -57,9 +157,22 @@ static cudaError_t vjp(const Args& a, bool tail, cudaStream_t s) {
     return prof_mark(-1, s);
 }
 
-static cudaError_t dropout(const Args& a, cudaStream_t s) {
-    const long long n = a.outer * a.features * a.inner;
-    PRIOR_LAUNCH(dropout_kernel<T>, dim3(bounded((n + 255) / 256, GRID)), dim3(256), 0, s, a);
+static cudaError_t dropout(const Args& given, cudaStream_t s) {
+    Args a = given;
+    long long slice = a.features * a.inner;
+    const long long n = a.outer * slice;
+    if (a.px == slice && a.pout == slice && (!a.res || a.pres == slice)) { a.outer = 1; a.features = 1; a.inner = slice = n; }
+    const bool aligned = packed(a, 0, {{a.x, a.px}, {a.res, a.pres}, {a.out, a.pout}}), whole = slice % VEC<T> == 0;
+    const long long blocks = ((n + VEC<T> - 1) / VEC<T> + DROP_THREADS - 1) / DROP_THREADS;
+    if (blocks > 0x7fffffffll) return cudaErrorInvalidConfiguration;
+    const int form = !aligned ? DROP_ELEMENTS : a.outer == 1 ? (whole ? DROP_FLAT : DROP_FLAT_END) : whole ? DROP_SLICES : DROP_ELEMENTS;
+    auto pick = [&](auto res, auto drop) {
+        constexpr bool R = decltype(res)::value, D = decltype(drop)::value;
+        return form == DROP_FLAT ? dropout_kernel<T, R, D, DROP_FLAT> : form == DROP_FLAT_END ? dropout_kernel<T, R, D, DROP_FLAT_END>
+             : form == DROP_SLICES ? dropout_kernel<T, R, D, DROP_SLICES> : dropout_kernel<T, R, D, DROP_ELEMENTS>;
+    };
+    auto kernel = a.res ? (a.dropping ? pick(yes{}, yes{}) : pick(yes{}, no{})) : (a.dropping ? pick(no{}, yes{}) : pick(no{}, no{}));
+    PRIOR_LAUNCH(kernel, dim3((unsigned)blocks), dim3(DROP_THREADS), 0, s, a);
     return prof_mark(-1, s);
 }
 

@@ -26,9 +26,11 @@ struct Args {
     float eps, scale;        // scale = 1 / (1 - p)
     uint32_t last;           // elements whose word is at most this are dropped
     int dropping;            // whether any is
+    int aligned;             // rows: all arrays lie alike against multiples of 16 bytes
     int weight_f32;          // weights and their gradients are float32, else of the arrays' type
-    uint64_t seed, offset;
+    uint64_t offset;
     const unsigned long long* step;
+    uint32_t keys[20];       // the mask's round keys: constants of the launch, operands of its exclusive ors
 };
 
 __device__ __forceinline__ float to_float(float v) { return v; }
@@ -39,41 +41,95 @@ template <> __device__ __forceinline__ float from_float<float>(float v) { return
 template <> __device__ __forceinline__ __half from_float<__half>(float v) { return __float2half_rn(v); }
 template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 
+// Sixteen bytes of an array, as they lie in memory and as numbers.
+template <class T> constexpr int VEC = 16 / sizeof(T);
+template <class T> struct alignas(16) Pack { T e[VEC<T>]; };
+template <class T>
+__device__ __forceinline__ Pack<T> load_pack(const T* p) { return *reinterpret_cast<const Pack<T>*>(p); }
+template <class T>
+__device__ __forceinline__ void store_pack(T* p, const Pack<T>& v) { *reinterpret_cast<Pack<T>*>(p) = v; }
+
+__device__ __forceinline__ void unpack(const Pack<float>& p, float (&v)[4]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = p.e[j];
+}
+__device__ __forceinline__ void unpack(const Pack<__half>& p, float (&v)[8]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const float2 f = __half22float2(reinterpret_cast<const __half2*>(&p)[j]);
+        v[2 * j] = f.x; v[2 * j + 1] = f.y;
+    }
+}
+__device__ __forceinline__ void unpack(const Pack<__nv_bfloat16>& p, float (&v)[8]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const uint32_t w = reinterpret_cast<const uint32_t*>(&p)[j];
+        v[2 * j] = __uint_as_float(w << 16); v[2 * j + 1] = __uint_as_float(w & 0xffff0000u);
+    }
+}
+template <class T> __device__ __forceinline__ Pack<T> pack(const float (&v)[VEC<T>]);
+template <> __device__ __forceinline__ Pack<float> pack<float>(const float (&v)[4]) {
+    Pack<float> p;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) p.e[j] = v[j];
+    return p;
+}
+template <> __device__ __forceinline__ Pack<__half> pack<__half>(const float (&v)[8]) {
+    Pack<__half> p;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) reinterpret_cast<__half2*>(&p)[j] = __floats2half2_rn(v[2 * j], v[2 * j + 1]);
+    return p;
+}
+template <> __device__ __forceinline__ Pack<__nv_bfloat16> pack<__nv_bfloat16>(const float (&v)[8]) {
+    Pack<__nv_bfloat16> p;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) reinterpret_cast<__nv_bfloat162*>(&p)[j] = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]);
+    return p;
+}
+
+// residual + dropout(x) in the arrays' type: one fused multiply-add, then one rounding to the stored type.
+template <class T>
+__device__ __forceinline__ T tail_sum(float x, float res, bool dropped, float scale) {
+    return from_float<T>(dropped ? res : fmaf(x, scale, res));
+}
+
 template <class T>
 __device__ __forceinline__ float weight_at(const void* w, int f32, long long c) {
     return f32 ? static_cast<const float*>(w)[c] : to_float(static_cast<const T*>(w)[c]);
 }
 
+template <class T>
+__device__ __forceinline__ void store_weight_grad(void* to, int f32, long long c, float v) {
+    if (f32) static_cast<float*>(to)[c] = v;
+    else static_cast<T*>(to)[c] = from_float<T>(v);
+}
+
 // The dropout mask.  Philox4x32-10 (Salmon, Moraes, Dror, Shaw, "Parallel random numbers: as easy as 1, 2, 3", 2011): ten
 // rounds that multiply two words of the counter by constants and exchange the halves of the products, with two key words
-// that advance by constants.  Four elements share a counter, so an element costs 5 products and 5 three-way exclusive ors.
+// that advance by constants from round to round.  Four elements share a counter, so an element costs 5 products of 32 x 32
+// bits and 5 three-way exclusive ors; the round keys come ready from the host.
 struct Mask {
-    uint32_t k0, k1, s0, s1, last;
-    uint64_t offset;
-    __device__ __forceinline__ explicit Mask(const Args& a) {
-        k0 = (uint32_t)a.seed; k1 = (uint32_t)(a.seed >> 32);
+    const Args& a;
+    uint32_t s0, s1;
+    __device__ __forceinline__ explicit Mask(const Args& args) : a(args) {
         const unsigned long long step = a.step ? *a.step : 0ull;
         s0 = (uint32_t)step; s1 = (uint32_t)(step >> 32);
-        last = a.last; offset = a.offset;
     }
     __device__ __forceinline__ uint4 words(uint64_t block) const {
-        block += offset;
-        uint32_t c0 = (uint32_t)block, c1 = (uint32_t)(block >> 32), c2 = s0, c3 = s1, q0 = k0, q1 = k1;
+        block += a.offset;
+        uint32_t c0 = (uint32_t)block, c1 = (uint32_t)(block >> 32), c2 = s0, c3 = s1;
 #pragma unroll
         for (int r = 0; r < 10; ++r) {
             const uint64_t p0 = (uint64_t)c0 * 0xD2511F53u, p1 = (uint64_t)c2 * 0xCD9E8D57u;
-            c0 = (uint32_t)(p1 >> 32) ^ c1 ^ q0; c1 = (uint32_t)p1;
-            c2 = (uint32_t)(p0 >> 32) ^ c3 ^ q1; c3 = (uint32_t)p0;
-            q0 += 0x9E3779B9u; q1 += 0xBB67AE85u;
+            c0 = (uint32_t)(p1 >> 32) ^ c1 ^ a.keys[2 * r]; c1 = (uint32_t)p1;
+            c2 = (uint32_t)(p0 >> 32) ^ c3 ^ a.keys[2 * r + 1]; c3 = (uint32_t)p0;
         }
         return make_uint4(c0, c1, c2, c3);
     }
-    __device__ __forceinline__ bool dropped(uint32_t word) const { return word <= last; }
-    __device__ __forceinline__ bool dropped_at(uint64_t i) const {
-        const uint4 w = words(i >> 2);
-        const uint32_t lane = (uint32_t)i & 3u;
-        return dropped(lane == 0 ? w.x : lane == 1 ? w.y : lane == 2 ? w.z : w.w);
+    __device__ __forceinline__ bool dropped(const uint4& w, int lane) const {
+        return (lane == 0 ? w.x : lane == 1 ? w.y : lane == 2 ? w.z : w.w) <= a.last;
     }
+    __device__ __forceinline__ bool dropped_at(uint64_t i) const { return dropped(words(i >> 2), (int)(i & 3u)); }
 };
 
 // Sums of a pair over the block in a fixed order, in every thread.  One barrier before and one after the exchange.

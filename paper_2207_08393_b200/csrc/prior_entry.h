@@ -13,8 +13,13 @@ struct Ops {
 };
 extern const Ops ops_f32, ops_f16, ops_bf16;
 
-// Rows of partial sums of the weights' gradients that a VJP writes.
-int weight_parts(const Args& a);
+// Rows of partial sums of the weights' gradients that a VJP writes at most.
+constexpr int SMS = 148;
+constexpr int PARTS_MOST = 2 * SMS;
+inline int parts_most(const Args& a) {
+    const long long positions = a.outer * a.inner;
+    return (int)(positions < PARTS_MOST ? positions : PARTS_MOST);
+}
 
 }  // namespace prior
 }  // namespace gleam

@@ -11,16 +11,10 @@ namespace prior {
 
 constexpr int ROW_THREADS = 256, MAP_WARPS = 8;
 
-// residual + dropout(x) in the arrays' type: one fused multiply-add, then one rounding to the stored type.
-template <class T>
-__device__ __forceinline__ T tail_sum(float x, float res, bool dropped, float scale) {
-    return from_float<T>(dropped ? res : fmaf(x, scale, res));
-}
-
 // ---- rows (inner == 1), any number of features: a block per row, which it reads again for each sum -------------------------
 
 template <class T, bool TAIL>
-__global__ void __launch_bounds__(ROW_THREADS) row_forward(const Args a) {
+__global__ void __launch_bounds__(ROW_THREADS) row_forward(const __grid_constant__ Args a) {
     grid_dependency_wait();
     __shared__ float buf[2 * (ROW_THREADS / 32)];
     const Mask mask(a);
@@ -63,7 +57,7 @@ __global__ void __launch_bounds__(ROW_THREADS) row_forward(const Args a) {
 }
 
 template <class T, bool TAIL>
-__global__ void __launch_bounds__(ROW_THREADS) row_vjp(const Args a) {
+__global__ void __launch_bounds__(ROW_THREADS) row_vjp(const __grid_constant__ Args a) {
     grid_dependency_wait();
     __shared__ float buf[2 * (ROW_THREADS / 32)];
     const Mask mask(a);
@@ -99,7 +93,7 @@ __global__ void __launch_bounds__(ROW_THREADS) row_vjp(const Args a) {
 
 // Partial sums of the weights' gradients: 32 features and a share of the rows per block.
 template <class T>
-__global__ void __launch_bounds__(256) row_weight_sums(const Args a) {
+__global__ void __launch_bounds__(256) row_weight_sums(const __grid_constant__ Args a) {
     grid_dependency_wait();
     __shared__ float buf[2][8][32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -138,7 +132,7 @@ __device__ __forceinline__ Pair warps_sum(Pair v, float (&buf)[2][MAP_WARPS][32]
 }
 
 template <class T, bool TAIL>
-__global__ void __launch_bounds__(MAP_WARPS * 32) map_forward(const Args a) {
+__global__ void __launch_bounds__(MAP_WARPS * 32) map_forward(const __grid_constant__ Args a) {
     grid_dependency_wait();
     __shared__ float buf[2][MAP_WARPS][32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -187,7 +181,7 @@ __global__ void __launch_bounds__(MAP_WARPS * 32) map_forward(const Args a) {
 }
 
 template <class T, bool TAIL>
-__global__ void __launch_bounds__(MAP_WARPS * 32) map_vjp(const Args a) {
+__global__ void __launch_bounds__(MAP_WARPS * 32) map_vjp(const __grid_constant__ Args a) {
     grid_dependency_wait();
     __shared__ float buf[2][MAP_WARPS][32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -229,7 +223,7 @@ __global__ void __launch_bounds__(MAP_WARPS * 32) map_vjp(const Args a) {
 
 // Partial sums of the weights' gradients: one feature and a share of the positions per block.
 template <class T>
-__global__ void __launch_bounds__(256) map_weight_sums(const Args a) {
+__global__ void __launch_bounds__(256) map_weight_sums(const __grid_constant__ Args a) {
     grid_dependency_wait();
     __shared__ float buf[16];
     const long long c = blockIdx.x, positions = a.outer * a.inner;
@@ -247,7 +241,7 @@ __global__ void __launch_bounds__(256) map_weight_sums(const Args a) {
 
 // The weights' gradients from the partial sums: 32 features of one of the two per block, whose warps share the parts.
 template <class T>
-__global__ void __launch_bounds__(256) weight_grads(const Args a, int parts) {
+__global__ void __launch_bounds__(256) weight_grads(const __grid_constant__ Args a, int parts) {
     grid_dependency_wait();
     __shared__ float buf[8][32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -262,25 +256,7 @@ __global__ void __launch_bounds__(256) weight_grads(const Args a, int parts) {
     t = 0.f;
 #pragma unroll
     for (int w = 0; w < 8; ++w) t += buf[w][lane];
-    if (a.weight_f32) static_cast<float*>(to)[c] = t;
-    else static_cast<T*>(to)[c] = from_float<T>(t);
-}
-
-// ---- dropout alone -----------------------------------------------------------------------------------------------------
-
-template <class T>
-__global__ void __launch_bounds__(256) dropout_kernel(const Args a) {
-    grid_dependency_wait();
-    const Mask mask(a);
-    const long long slice = a.features * a.inner, n = a.outer * slice, stride = (long long)gridDim.x * 256;
-    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += stride) {
-        const long long o = i / slice, e = i - o * slice;
-        const bool gone = a.dropping && mask.dropped_at((uint64_t)i);
-        const float x = to_float(static_cast<const T*>(a.x)[o * a.px + e]);
-        T* out = static_cast<T*>(a.out) + o * a.pout + e;
-        if (a.res) *out = tail_sum<T>(x, to_float(static_cast<const T*>(a.res)[o * a.pres + e]), gone, a.scale);
-        else *out = from_float<T>(gone ? 0.f : x * a.scale);
-    }
+    store_weight_grad<T>(to, a.weight_f32, c, t);
 }
 
 }  // namespace prior

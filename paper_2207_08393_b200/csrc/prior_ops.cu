@@ -13,15 +13,6 @@ static const Ops* find_ops(int dtype) {
     return dtype == GLEAM_F32 ? &ops_f32 : dtype == GLEAM_F16 ? &ops_f16 : dtype == GLEAM_BF16 ? &ops_bf16 : nullptr;
 }
 
-// Enough blocks to fill the GPU over the pieces of features, each with some hundred positions at least.
-int weight_parts(const Args& a) {
-    const long long positions = a.outer * a.inner;
-    const long long pieces = a.inner == 1 ? (a.features + 31) / 32 : a.features;
-    const long long fill = (1184 + pieces - 1) / pieces, share = (positions + 255) / 256;
-    const long long n = fill < share ? fill : share;
-    return (int)(n < 1 ? 1 : n);
-}
-
 // An activation array of a call.
 struct Array {
     const void* p;
@@ -96,7 +87,9 @@ static int take_dropout(const gleam_dropout_args* m, Args* a) {
     const uint64_t limit = (uint64_t)std::floor(m->p * 4294967296.0);
     a->dropping = limit > 0;
     a->last = limit > 0 ? (uint32_t)(limit - 1) : 0;
-    a->seed = m->seed; a->offset = m->offset;
+    a->offset = m->offset;
+    uint32_t k0 = (uint32_t)m->seed, k1 = (uint32_t)(m->seed >> 32);
+    for (int r = 0; r < 10; ++r, k0 += 0x9E3779B9u, k1 += 0xBB67AE85u) { a->keys[2 * r] = k0; a->keys[2 * r + 1] = k1; }
     a->step = (const unsigned long long*)m->step;
     return GLEAM_OK;
 }
@@ -133,7 +126,7 @@ static int check_memory(const Call& c, const Small* small, int count) {
     return GLEAM_OK;
 }
 
-static uint64_t part_bytes(const Args& a) { return (uint64_t)weight_parts(a) * 2u * (uint64_t)a.features * sizeof(float); }
+static uint64_t part_bytes(const Args& a) { return (uint64_t)parts_most(a) * 2u * (uint64_t)a.features * sizeof(float); }
 
 static int status_of(cudaError_t e) { return e == cudaSuccess ? GLEAM_OK : GLEAM_ERR_CUDA; }
 

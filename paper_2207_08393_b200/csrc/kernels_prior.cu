@@ -1,5 +1,6 @@
 // Instantiation unit of the prior's operators for one element type: GLEAM_PRIOR_TYPE is 0 (float32), 1 (float16) or 2 (bfloat16).
 #include "dc_entry.h"
+#include "launch_state.cuh"
 #include "prior_entry.h"
 #include "prior_dropout.cuh"
 #include "prior_norm.cuh"
@@ -43,70 +44,84 @@ static bool packed(const Args& a, long long beyond, std::initializer_list<std::p
 // How rows are dealt to teams of threads (prior_rows.cuh); fits = false where a row is too long for one.
 struct RowPlan {
     bool fits, edges;
-    int team, items, warps, teams, threads;      // lanes of a team (0: warps of it), pieces a thread, teams and threads a block
-    unsigned grid;
+    int team, items, warps, teams, threads;      // lanes of a team (0: warps of it), pieces a thread, warps a team, teams and threads a block
 };
-static RowPlan row_plan(const Args& a, bool vjp) {
+static RowPlan row_plan(const Args& a) {
     RowPlan p{};
-    constexpr int V = VEC<T>, WARPS = ROW_TEAMS_THREADS / 32;
+    constexpr int V = VEC<T>, MOST = ROW_FEATURES / V;
     p.edges = !a.aligned || a.features % V != 0;
     const long long pieces = p.edges ? (a.features + 2 * (V - 1)) / V : a.features / V;
-    // eight features a thread where that is at most 16 warps (registers), else sixteen
-    const int few = 8 / V, many = 16 / V;
-    p.items = pieces <= 32 ? 1 : pieces <= 32ll * few * WARPS ? few : many;
-    if (pieces > 32ll * many * WARPS) return p;
+    if (pieces > 32ll * MOST * ROW_BLOCK_WARPS) return p;
     p.fits = true;
-    if (pieces <= 32 * p.items) {
-        p.team = p.items > 1 || pieces > 16 ? 32 : pieces > 8 ? 16 : pieces > 4 ? 8 : 4;
-        p.warps = 1;
-        p.teams = ROW_TEAMS_THREADS / p.team;
-        p.threads = ROW_TEAMS_THREADS;
-    } else {
-        p.team = 0;
-        p.warps = (int)((pieces + 32 * p.items - 1) / (32 * p.items));
-        p.teams = WARPS / p.warps;
-        p.threads = p.teams * p.warps * 32;
-    }
-    const long long need = (a.outer + p.teams - 1) / p.teams;
-    long long most = vjp || p.items * V > 8 ? SMS : 2 * SMS;      // blocks that are resident at once
-    // the rows of a team lie alike if teams go on by multiples of V rows
-    if (p.edges) while (most * p.teams % V) --most;
-    p.grid = (unsigned)(need < most ? need : most);
-    // a few rows per team in one block: it writes the weights' gradients itself
-    if (vjp && (a.gw || a.gb) && need > 1 && need <= 4 && (!p.edges || p.teams % V == 0)) p.grid = 1;
+    p.items = 1;
+    while (p.items < MOST && pieces > 32 * p.items) p.items *= 2;
+    p.warps = (int)((pieces + 32 * p.items - 1) / (32 * p.items));
+    p.team = p.warps > 1 ? 0 : p.items > 1 || pieces > 16 ? 32 : pieces > 8 ? 16 : pieces > 4 ? 8 : 4;
+    p.teams = p.team ? ROW_BLOCK / p.team : ROW_BLOCK_WARPS / p.warps;
+    p.threads = p.team ? ROW_BLOCK : p.teams * p.warps * 32;
     return p;
 }
+// Blocks of the launch, of which `most` are on the GPU at once.
+static int row_grid(const Args& a, const RowPlan& p, bool vjp, int most) {
+    constexpr int V = VEC<T>;
+    if (vjp && most > PARTS_MOST) most = PARTS_MOST;
+    if (p.edges && p.items > 1) {                // V blocks at a time: the rows of a block begin alike
+        const long long need = ((a.outer + V - 1) / V + p.teams - 1) / p.teams;
+        return (int)(V * (need < most / V ? need : most / V));
+    }
+    const long long need = (a.outer + p.teams - 1) / p.teams;
+    // a few rows per team in one block: it writes the weights' gradients itself
+    if (vjp && (a.gw || a.gb) && need <= 4 && (!p.edges || p.teams % V == 0)) return 1;
+    if (need <= most) return (int)need;
+    if (p.edges) while (most * p.teams % V) --most;      // the rows of a team begin alike if teams go on by multiples of V rows
+    return most;
+}
 
+template <auto KERNEL> static PerDevice kernel_state;
+
+template <bool VJP, bool TAIL, bool EDGES, int TEAM, int ITEMS>
+static cudaError_t launch_rows(const Args& a, const RowPlan& p, int* blocks, cudaStream_t s) {
+    constexpr size_t PER_THREAD = 16 * ((VJP ? 2 : 1) + TAIL) * ITEMS * row_stages<T, VJP, TAIL, ITEMS>(), SM_BYTES = 227 * 1024;
+    constexpr auto KERNEL = [] { if constexpr (VJP) return row_team_vjp<T, TEAM, ITEMS, EDGES, TAIL>; else return row_team_forward<T, TEAM, ITEMS, EDGES, TAIL>; }();
+    const size_t weights = ITEMS > 1 ? (VJP ? 1 : 2) * sizeof(float) * p.warps * 32 * ITEMS * VEC<T> : 0;
+    size_t shared = EXCHANGE_BYTES + PER_THREAD * p.threads + weights;
+    const size_t sums = 2 * (size_t)a.features * sizeof(float);          // a block of several teams adds up their weights' gradients
+    if (VJP && p.teams > 1 && shared < sums) shared = sums;
+    const cudaError_t e = ensure_smem(KERNEL, SM_BYTES, kernel_state<KERNEL>);
+    if (e != cudaSuccess) return e;
+    const int fit = (int)(SM_BYTES / (shared + 1024)), resident = fit < row_blocks<T, VJP, ITEMS>() ? fit : row_blocks<T, VJP, ITEMS>();
+    *blocks = row_grid(a, p, VJP, SMS * (resident > 0 ? resident : 1));
+    PRIOR_LAUNCH(KERNEL, dim3((unsigned)*blocks), dim3(p.threads), shared, s, a, p.warps, p.teams);
+    return cudaSuccess;
+}
 template <bool VJP, bool TAIL, bool EDGES>
-static auto row_kernel(const RowPlan& p) {
-    auto pick = [&](auto team, auto items) {
-        constexpr int G = decltype(team)::value, I = decltype(items)::value;
-        if constexpr (VJP) return row_team_vjp<T, G, I, EDGES, TAIL>;
-        else return row_team_forward<T, G, I, EDGES, TAIL>;
-    };
-    constexpr int FEW = 8 / VEC<T>, MANY = 16 / VEC<T>;
+static cudaError_t launch_rows(const Args& a, const RowPlan& p, int* blocks, cudaStream_t s) {
+    constexpr int MOST = ROW_FEATURES / VEC<T>;
     switch (p.team) {
-        case 4: return pick(number<4>{}, number<1>{});
-        case 8: return pick(number<8>{}, number<1>{});
-        case 16: return pick(number<16>{}, number<1>{});
-        case 32: return p.items == 1 ? pick(number<32>{}, number<1>{}) : pick(number<32>{}, number<FEW>{});
-        default: return p.items == FEW ? pick(number<0>{}, number<FEW>{}) : pick(number<0>{}, number<MANY>{});
+        case 4: return launch_rows<VJP, TAIL, EDGES, 4, 1>(a, p, blocks, s);
+        case 8: return launch_rows<VJP, TAIL, EDGES, 8, 1>(a, p, blocks, s);
+        case 16: return launch_rows<VJP, TAIL, EDGES, 16, 1>(a, p, blocks, s);
+        case 32: return p.items == 1 ? launch_rows<VJP, TAIL, EDGES, 32, 1>(a, p, blocks, s) : p.items == 2 ? launch_rows<VJP, TAIL, EDGES, 32, 2>(a, p, blocks, s)
+                      : p.items == 4 ? launch_rows<VJP, TAIL, EDGES, 32, 4>(a, p, blocks, s) : launch_rows<VJP, TAIL, EDGES, 32, MOST>(a, p, blocks, s);
+        default: return launch_rows<VJP, TAIL, EDGES, 0, MOST>(a, p, blocks, s);
     }
 }
 template <bool VJP>
-static auto row_kernel(const RowPlan& p, bool tail) {
-    return tail ? (p.edges ? row_kernel<VJP, true, true>(p) : row_kernel<VJP, true, false>(p))
-                : (p.edges ? row_kernel<VJP, false, true>(p) : row_kernel<VJP, false, false>(p));
+static cudaError_t launch_rows(const Args& a, const RowPlan& p, bool tail, int* blocks, cudaStream_t s) {
+    return tail ? (p.edges ? launch_rows<VJP, true, true>(a, p, blocks, s) : launch_rows<VJP, true, false>(a, p, blocks, s))
+                : (p.edges ? launch_rows<VJP, false, true>(a, p, blocks, s) : launch_rows<VJP, false, false>(a, p, blocks, s));
 }
 
 static cudaError_t forward(const Args& given, bool tail, cudaStream_t s) {
     Args a = given;
+    cudaError_t e;
     if (a.inner == 1) {
         a.aligned = packed(a, a.features, {{a.x, a.px}, {a.res, a.pres}, {a.out, a.pout}, {a.out2, a.pout2}});
-        const RowPlan p = row_plan(a, false);
+        const RowPlan p = row_plan(a);
+        int blocks = 0;
+        if (p.fits) return (e = launch_rows<false>(a, p, tail, &blocks, s)) != cudaSuccess ? e : prof_mark(-1, s);
         const dim3 grid(bounded(a.outer, GRID));
-        if (p.fits) PRIOR_LAUNCH(row_kernel<false>(p, tail), dim3(p.grid), dim3(p.threads), p.teams * p.warps * 6 * sizeof(float), s, a, p.warps, p.teams);
-        else if (tail) PRIOR_LAUNCH(row_forward<T, true>, grid, dim3(ROW_THREADS), 0, s, a);
+        if (tail) PRIOR_LAUNCH(row_forward<T, true>, grid, dim3(ROW_THREADS), 0, s, a);
         else PRIOR_LAUNCH(row_forward<T, false>, grid, dim3(ROW_THREADS), 0, s, a);
     } else {
         const dim3 grid(bounded((a.outer * a.inner + 31) / 32, GRID));
@@ -126,12 +141,11 @@ static cudaError_t vjp(const Args& given, bool tail, cudaStream_t s) {
     cudaError_t e;
     if (a.inner == 1) {
         a.aligned = packed(a, a.features, {{a.x, a.px}, {a.res, a.pres}, {a.gsum, a.pgsum}, {a.out, a.pout}, {a.out2, a.pout2}});
-        const RowPlan p = row_plan(a, true);
+        const RowPlan p = row_plan(a);
         if (p.fits) {
-            size_t shared = p.teams * p.warps * 6 * sizeof(float);
-            if (p.teams > 1 && shared < 2 * (size_t)a.features * sizeof(float)) shared = 2 * (size_t)a.features * sizeof(float);
-            PRIOR_LAUNCH(row_kernel<true>(p, tail), dim3(p.grid), dim3(p.threads), shared, s, a, p.warps, p.teams);
-            if ((a.gw || a.gb) && p.grid > 1 && (e = weight_grads_from(a, (int)p.grid, s)) != cudaSuccess) return e;
+            int blocks = 0;
+            if ((e = launch_rows<true>(a, p, tail, &blocks, s)) != cudaSuccess) return e;
+            if ((a.gw || a.gb) && blocks > 1 && (e = weight_grads_from(a, blocks, s)) != cudaSuccess) return e;
             return prof_mark(-1, s);
         }
     }

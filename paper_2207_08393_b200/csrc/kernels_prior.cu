@@ -44,19 +44,18 @@ static bool packed(const Args& a, long long beyond, std::initializer_list<std::p
 // How rows are dealt to teams of threads (prior_rows.cuh); fits = false where a row is too long for one.
 struct RowPlan {
     bool fits, edges;
-    int team, items, warps, teams, threads;      // lanes of a team (0: warps of it), pieces a thread, warps a team, teams and threads a block
+    int team, warps, teams, threads;             // lanes of a team (0: warps of it), warps a team, teams and threads a block
 };
 static RowPlan row_plan(const Args& a) {
     RowPlan p{};
-    constexpr int V = VEC<T>, MOST = ROW_FEATURES / V;
+    constexpr int V = VEC<T>, ITEMS = ROW_ITEMS<T>;
     p.edges = !a.aligned || a.features % V != 0;
     const long long pieces = p.edges ? (a.features + 2 * (V - 1)) / V : a.features / V;
-    if (pieces > 32ll * MOST * ROW_BLOCK_WARPS) return p;
+    if (pieces > 32ll * ITEMS * ROW_BLOCK_WARPS) return p;
     p.fits = true;
-    p.items = 1;
-    while (p.items < MOST && pieces > 32 * p.items) p.items *= 2;
-    p.warps = (int)((pieces + 32 * p.items - 1) / (32 * p.items));
-    p.team = p.warps > 1 ? 0 : p.items > 1 || pieces > 16 ? 32 : pieces > 8 ? 16 : pieces > 4 ? 8 : 4;
+    p.warps = (int)((pieces + 32 * ITEMS - 1) / (32 * ITEMS));
+    p.team = p.warps > 1 ? 0 : 2;
+    while (p.team && pieces > p.team * ITEMS) p.team *= 2;
     p.teams = p.team ? ROW_BLOCK / p.team : ROW_BLOCK_WARPS / p.warps;
     p.threads = p.team ? ROW_BLOCK : p.teams * p.warps * 32;
     return p;
@@ -64,46 +63,43 @@ static RowPlan row_plan(const Args& a) {
 // Blocks of the launch, of which `most` are on the GPU at once.
 static int row_grid(const Args& a, const RowPlan& p, bool vjp, int most) {
     constexpr int V = VEC<T>;
-    if (vjp && most > PARTS_MOST) most = PARTS_MOST;
-    if (p.edges && p.items > 1) {                // V blocks at a time: the rows of a block begin alike
+    if (p.edges) {                               // V blocks at a time: the rows of a block begin alike
         const long long need = ((a.outer + V - 1) / V + p.teams - 1) / p.teams;
         return (int)(V * (need < most / V ? need : most / V));
     }
     const long long need = (a.outer + p.teams - 1) / p.teams;
     // a few rows per team in one block: it writes the weights' gradients itself
-    if (vjp && (a.gw || a.gb) && need <= 4 && (!p.edges || p.teams % V == 0)) return 1;
-    if (need <= most) return (int)need;
-    if (p.edges) while (most * p.teams % V) --most;      // the rows of a team begin alike if teams go on by multiples of V rows
-    return most;
+    if (vjp && (a.gw || a.gb) && need <= 4) return 1;
+    return (int)(need < most ? need : most);
 }
 
 template <auto KERNEL> static PerDevice kernel_state;
 
-template <bool VJP, bool TAIL, bool EDGES, int TEAM, int ITEMS>
+template <bool VJP, bool TAIL, bool EDGES, int TEAM>
 static cudaError_t launch_rows(const Args& a, const RowPlan& p, int* blocks, cudaStream_t s) {
-    constexpr size_t PER_THREAD = 16 * ((VJP ? 2 : 1) + TAIL) * ITEMS * row_stages<T, VJP, TAIL, ITEMS>(), SM_BYTES = 227 * 1024;
-    constexpr auto KERNEL = [] { if constexpr (VJP) return row_team_vjp<T, TEAM, ITEMS, EDGES, TAIL>; else return row_team_forward<T, TEAM, ITEMS, EDGES, TAIL>; }();
-    const size_t weights = ITEMS > 1 ? (VJP ? 1 : 2) * sizeof(float) * p.warps * 32 * ITEMS * VEC<T> : 0;
+    constexpr size_t PER_THREAD = sizeof(T) * ROW_FEATURES * ((VJP ? 2 : 1) + TAIL) * row_stages(VJP, TAIL, sizeof(T)), SM_BYTES = 227 * 1024;
+    constexpr auto KERNEL = [] { if constexpr (VJP) return row_team_vjp<T, TEAM, EDGES, TAIL>; else return row_team_forward<T, TEAM, EDGES, TAIL>; }();
+    const size_t weights = (VJP ? 1 : 2) * sizeof(float) * ROW_FEATURES * (p.team ? p.team : p.warps * 32);
+    // a block of several teams adds up their weights' gradients
+    const size_t sums = VJP && p.teams > 1 ? 2 * sizeof(float) * ROW_FEATURES * p.threads : 0;
     size_t shared = EXCHANGE_BYTES + PER_THREAD * p.threads + weights;
-    const size_t sums = 2 * (size_t)a.features * sizeof(float);          // a block of several teams adds up their weights' gradients
-    if (VJP && p.teams > 1 && shared < sums) shared = sums;
+    if (shared < sums) shared = sums;
     const cudaError_t e = ensure_smem(KERNEL, SM_BYTES, kernel_state<KERNEL>);
     if (e != cudaSuccess) return e;
-    const int fit = (int)(SM_BYTES / (shared + 1024)), resident = fit < row_blocks<T, VJP, ITEMS>() ? fit : row_blocks<T, VJP, ITEMS>();
-    *blocks = row_grid(a, p, VJP, SMS * (resident > 0 ? resident : 1));
+    const int fit = (int)(SM_BYTES / (shared + 1024)), resident = fit < 1 ? 1 : fit < row_blocks(VJP) ? fit : row_blocks(VJP);
+    *blocks = row_grid(a, p, VJP, SMS * resident);
     PRIOR_LAUNCH(KERNEL, dim3((unsigned)*blocks), dim3(p.threads), shared, s, a, p.warps, p.teams);
     return cudaSuccess;
 }
 template <bool VJP, bool TAIL, bool EDGES>
 static cudaError_t launch_rows(const Args& a, const RowPlan& p, int* blocks, cudaStream_t s) {
-    constexpr int MOST = ROW_FEATURES / VEC<T>;
     switch (p.team) {
-        case 4: return launch_rows<VJP, TAIL, EDGES, 4, 1>(a, p, blocks, s);
-        case 8: return launch_rows<VJP, TAIL, EDGES, 8, 1>(a, p, blocks, s);
-        case 16: return launch_rows<VJP, TAIL, EDGES, 16, 1>(a, p, blocks, s);
-        case 32: return p.items == 1 ? launch_rows<VJP, TAIL, EDGES, 32, 1>(a, p, blocks, s) : p.items == 2 ? launch_rows<VJP, TAIL, EDGES, 32, 2>(a, p, blocks, s)
-                      : p.items == 4 ? launch_rows<VJP, TAIL, EDGES, 32, 4>(a, p, blocks, s) : launch_rows<VJP, TAIL, EDGES, 32, MOST>(a, p, blocks, s);
-        default: return launch_rows<VJP, TAIL, EDGES, 0, MOST>(a, p, blocks, s);
+        case 2: return launch_rows<VJP, TAIL, EDGES, 2>(a, p, blocks, s);
+        case 4: return launch_rows<VJP, TAIL, EDGES, 4>(a, p, blocks, s);
+        case 8: return launch_rows<VJP, TAIL, EDGES, 8>(a, p, blocks, s);
+        case 16: return launch_rows<VJP, TAIL, EDGES, 16>(a, p, blocks, s);
+        case 32: return launch_rows<VJP, TAIL, EDGES, 32>(a, p, blocks, s);
+        default: return launch_rows<VJP, TAIL, EDGES, 0>(a, p, blocks, s);
     }
 }
 template <bool VJP>
@@ -132,7 +128,7 @@ static cudaError_t forward(const Args& given, bool tail, cudaStream_t s) {
 }
 
 static cudaError_t weight_grads_from(const Args& a, int parts, cudaStream_t s) {
-    PRIOR_LAUNCH(weight_grads<T>, dim3((unsigned)((a.features + 31) / 32), 2), dim3(256), 0, s, a, parts);
+    PRIOR_LAUNCH(weight_grads<T>, dim3((unsigned)((a.features + 31) / 32), 2), dim3(GRAD_WARPS * 32), 0, s, a, parts);
     return cudaSuccess;
 }
 

@@ -49,41 +49,55 @@ __device__ __forceinline__ Pack<T> load_pack(const T* p) { return *reinterpret_c
 template <class T>
 __device__ __forceinline__ void store_pack(T* p, const Pack<T>& v) { *reinterpret_cast<Pack<T>*>(p) = v; }
 
-__device__ __forceinline__ void unpack(const Pack<float>& p, float (&v)[4]) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = p.e[j];
+// Two numbers in a register pair: sm_100 multiplies and adds both with one instruction, each rounded as by itself.  What these
+// kernels spend their issue slots on is this arithmetic.
+struct Two {
+    unsigned long long bits;
+    Two() = default;
+    __device__ __forceinline__ Two(float lo, float hi) { asm("mov.b64 %0, {%1, %2};" : "=l"(bits) : "f"(lo), "f"(hi)); }
+    __device__ __forceinline__ explicit Two(float both) : Two(both, both) {}
+    __device__ __forceinline__ float lo() const { float l, h; asm("mov.b64 {%0, %1}, %2;" : "=f"(l), "=f"(h) : "l"(bits)); return l; }
+    __device__ __forceinline__ float hi() const { float l, h; asm("mov.b64 {%0, %1}, %2;" : "=f"(l), "=f"(h) : "l"(bits)); return h; }
+    __device__ __forceinline__ float sum() const { return lo() + hi(); }
+};
+__device__ __forceinline__ Two operator+(Two a, Two b) { Two r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.bits) : "l"(a.bits), "l"(b.bits)); return r; }
+__device__ __forceinline__ Two operator*(Two a, Two b) { Two r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.bits) : "l"(a.bits), "l"(b.bits)); return r; }
+__device__ __forceinline__ Two fma2(Two a, Two b, Two c) { Two r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.bits) : "l"(a.bits), "l"(b.bits), "l"(c.bits)); return r; }
+
+__device__ __forceinline__ void unpack(const Pack<float>& p, Two (&v)[2]) {
+    v[0] = Two(p.e[0], p.e[1]); v[1] = Two(p.e[2], p.e[3]);
 }
-__device__ __forceinline__ void unpack(const Pack<__half>& p, float (&v)[8]) {
+__device__ __forceinline__ void unpack(const Pack<__half>& p, Two (&v)[4]) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const float2 f = __half22float2(reinterpret_cast<const __half2*>(&p)[j]);
-        v[2 * j] = f.x; v[2 * j + 1] = f.y;
+        v[j] = Two(f.x, f.y);
     }
 }
-__device__ __forceinline__ void unpack(const Pack<__nv_bfloat16>& p, float (&v)[8]) {
+__device__ __forceinline__ void unpack(const Pack<__nv_bfloat16>& p, Two (&v)[4]) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const uint32_t w = reinterpret_cast<const uint32_t*>(&p)[j];
-        v[2 * j] = __uint_as_float(w << 16); v[2 * j + 1] = __uint_as_float(w & 0xffff0000u);
+        v[j] = Two(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
     }
 }
-template <class T> __device__ __forceinline__ Pack<T> pack(const float (&v)[VEC<T>]);
-template <> __device__ __forceinline__ Pack<float> pack<float>(const float (&v)[4]) {
+template <class T> __device__ __forceinline__ Pack<T> pack(const Two (&v)[VEC<T> / 2]);
+template <> __device__ __forceinline__ Pack<float> pack<float>(const Two (&v)[2]) {
     Pack<float> p;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) p.e[j] = v[j];
+    for (int j = 0; j < 2; ++j) { p.e[2 * j] = v[j].lo(); p.e[2 * j + 1] = v[j].hi(); }
     return p;
 }
-template <> __device__ __forceinline__ Pack<__half> pack<__half>(const float (&v)[8]) {
+template <> __device__ __forceinline__ Pack<__half> pack<__half>(const Two (&v)[4]) {
     Pack<__half> p;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) reinterpret_cast<__half2*>(&p)[j] = __floats2half2_rn(v[2 * j], v[2 * j + 1]);
+    for (int j = 0; j < 4; ++j) reinterpret_cast<__half2*>(&p)[j] = __floats2half2_rn(v[j].lo(), v[j].hi());
     return p;
 }
-template <> __device__ __forceinline__ Pack<__nv_bfloat16> pack<__nv_bfloat16>(const float (&v)[8]) {
+template <> __device__ __forceinline__ Pack<__nv_bfloat16> pack<__nv_bfloat16>(const Two (&v)[4]) {
     Pack<__nv_bfloat16> p;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) reinterpret_cast<__nv_bfloat162*>(&p)[j] = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]);
+    for (int j = 0; j < 4; ++j) reinterpret_cast<__nv_bfloat162*>(&p)[j] = __floats2bfloat162_rn(v[j].lo(), v[j].hi());
     return p;
 }
 
@@ -128,6 +142,22 @@ struct Mask {
     }
     __device__ __forceinline__ bool dropped(const uint4& w, int lane) const {
         return (lane == 0 ? w.x : lane == 1 ? w.y : lane == 2 ? w.z : w.w) <= a.last;
+    }
+    // v = r + s v [s v] for the elements that are kept, r [0] for the others; the first one is element 4 * block
+    template <bool RES, bool DROP, int N>
+    __device__ __forceinline__ void apply(uint64_t block, Two (&v)[N], const Two (&r)[N]) const {
+        const Two scale(a.scale);
+#pragma unroll
+        for (int q = 0; q < N / 2; ++q) {
+            uint4 w;
+            if (DROP) w = words(block + q);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                Two& x = v[2 * q + h];
+                const Two kept = RES ? fma2(x, scale, r[2 * q + h]) : x * scale, gone = RES ? r[2 * q + h] : Two(0.f);
+                x = DROP ? Two(dropped(w, 2 * h) ? gone.lo() : kept.lo(), dropped(w, 2 * h + 1) ? gone.hi() : kept.hi()) : kept;
+            }
+        }
     }
     __device__ __forceinline__ bool dropped_at(uint64_t i) const { return dropped(words(i >> 2), (int)(i & 3u)); }
 };

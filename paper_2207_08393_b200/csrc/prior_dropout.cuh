@@ -39,19 +39,10 @@ __global__ void __launch_bounds__(DROP_THREADS) dropout_kernel(const __grid_cons
     if (FORM == DROP_FLAT || FORM == DROP_SLICES || (FORM == DROP_FLAT_END && i + V <= n)) {
         Pack<T> xv = load_pack(x + (o * a.px + e)), rv;
         if (RES) rv = load_pack(res + (o * a.pres + e));
-        uint4 words[V / 4];
-        if (DROP) {
-#pragma unroll
-            for (int q = 0; q < V / 4; ++q) words[q] = mask.words((uint64_t)(i >> 2) + q);
-        }
-        float v[V], r[V];
+        Two v[V / 2], r[V / 2];
         unpack(xv, v);
         if (RES) unpack(rv, r);
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const float kept = RES ? fmaf(v[j], a.scale, r[j]) : v[j] * a.scale;
-            v[j] = DROP && mask.dropped(words[j / 4], j % 4) ? (RES ? r[j] : 0.f) : kept;
-        }
+        mask.apply<RES, DROP>((uint64_t)(i >> 2), v, r);
         store_pack(out + (o * a.pout + e), pack<T>(v));
         return;
     }

@@ -239,24 +239,28 @@ __global__ void __launch_bounds__(256) map_weight_sums(const __grid_constant__ A
     if (threadIdx.x < 2) a.part[((long long)blockIdx.y * 2 + threadIdx.x) * a.features + c] = threadIdx.x ? s.b : s.a;
 }
 
-// The weights' gradients from the partial sums: 32 features of one of the two per block, whose warps share the parts.
+// The weights' gradients from the partial sums: 32 features of one of the two per block, whose 32 warps share the parts.  Bound by
+// the latency of a few rounds of loads (with eight warps, one load at a time, 15 us for 296 parts).
+constexpr int GRAD_WARPS = 32;
 template <class T>
-__global__ void __launch_bounds__(256) weight_grads(const __grid_constant__ Args a, int parts) {
+__global__ void __launch_bounds__(GRAD_WARPS * 32) weight_grads(const __grid_constant__ Args a, int parts) {
     grid_dependency_wait();
-    __shared__ float buf[8][32];
+    __shared__ float buf[GRAD_WARPS][33];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const long long c = (long long)blockIdx.x * 32 + lane;
+    const long long c0 = (long long)blockIdx.x * 32, c = c0 + lane;
     float t = 0.f;
-    if (c < a.features)
-        for (int p = warp; p < parts; p += 8) t += a.part[((long long)p * 2 + blockIdx.y) * a.features + c];
-    buf[warp][lane] = t;
+    if (c < a.features) {
+        const float* part = a.part + blockIdx.y * a.features + c;
+#pragma unroll 5
+        for (int p = warp; p < parts; p += GRAD_WARPS) t += part[(long long)p * 2 * a.features];
+    }
+    buf[lane][warp] = t;
     __syncthreads();
+    // warp f adds up feature f's 32 sums
+    t = buf[warp][lane];
+    for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
     void* to = blockIdx.y ? a.gb : a.gw;
-    if (warp != 0 || c >= a.features || !to) return;
-    t = 0.f;
-#pragma unroll
-    for (int w = 0; w < 8; ++w) t += buf[w][lane];
-    store_weight_grad<T>(to, a.weight_f32, c, t);
+    if (lane == 0 && to && c0 + warp < a.features) store_weight_grad<T>(to, a.weight_f32, c0 + warp, t);
 }
 
 }  // namespace prior

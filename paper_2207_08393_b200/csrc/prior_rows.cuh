@@ -1,22 +1,28 @@
 // Layer norm and the residual tail on rows: a row stays with a team of threads that passes over every array once.
 //
-// A team is 4, 8, 16 or 32 lanes of a warp, or a few warps; a thread has ITEMS pieces of 16 bytes of its row.  Pieces begin at
-// multiples of 16 bytes of the array, not of the row: where rows begin anywhere (EDGES), a team's rows are those that begin at
-// the same place inside a piece, so that a thread's features are the same ones in each of its rows, and so are their weights
-// and, in a VJP, the sums of their gradients, which it keeps in registers.  The teams of a block add those sums up at its
-// end, and weight_grads (prior_norm.cuh) adds up the blocks.
+// A team is 2 to 32 lanes of a warp, or a few warps; a thread has up to 32 features of its row, in pieces of 16 bytes.  Pieces begin
+// at multiples of 16 bytes of the array, not of the row: where rows begin anywhere (EDGES), the rows of a block are those that
+// begin at the same place inside a piece, so that a thread's features are the same ones in each of its rows.  In a VJP it
+// keeps the sums of their weights' gradients in registers; the teams of a block add those sums up at its end, and
+// weight_grads (prior_norm.cuh) adds up the blocks.
 //
-// Bound by memory where a thread has many features.  What a row costs each thread apart from its features (about a
-// hundred instructions: the sums across lanes, the ring, the statistics) counts with few: with eight features a thread and a
-// team of four warps, rows of 1024 in bf16 were bound by issue at 47 instructions a feature.  So a thread takes up to 32
-// features before a second warp joins its team.
+// Bound by memory, if the instructions are few: what a row costs each thread apart from its features (about a hundred: the
+// sums across lanes, the ring, the statistics) is shared by 32 features, and the arithmetic is done two numbers at a time.
+// 51200 rows of 1024 in bf16, forward and VJP: eight features a thread with loads into registers 216 us, fetched ahead 177, 32
+// features a thread 142, two numbers at a time 96 (37 + 59; the bytes take 80 at copy rate).
 #pragma once
 #include "prior_common.cuh"
+
+#include <type_traits>
 
 namespace gleam {
 namespace prior {
 
+using True = std::true_type;
+using False = std::false_type;
+
 constexpr int ROW_BLOCK = 256, ROW_BLOCK_WARPS = ROW_BLOCK / 32, ROW_FEATURES = 32;    // threads a block, features a thread at most
+template <class T> constexpr int ROW_ITEMS = ROW_FEATURES / VEC<T>;                     // pieces a thread
 
 __device__ __forceinline__ void team_barrier(int team, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "r"(threads) : "memory"); }
 __device__ __forceinline__ void copy16(uint32_t to, const void* from) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory"); }
@@ -34,50 +40,60 @@ __device__ __forceinline__ float inverse_root(float x) {
     return e == e ? fmaf(0.5f * r, e, r) : r;
 }
 
-// Where a thread stands: its team (in the block and in the grid), its place in it, and its features.
-template <class T, int TEAM, int ITEMS, bool EDGES>
+// Where a thread stands: its team (in the block and in the grid), its place in it, and its features.  Each warp of a team has
+// neighbouring pieces, so that only the first and the last one meet the ends of the row; the others are `full` and check nothing.
+template <class T, int TEAM, bool EDGES>
 struct RowPlace {
-    static constexpr int V = VEC<T>;
+    static constexpr int V = VEC<T>, ITEMS = ROW_ITEMS<T>, STEP = TEAM ? TEAM : 32;
     int width, team, t, phase;           // threads of a team, team in the block, thread in the team, where its rows begin in a piece
-    long long row, rows_apart;
+    int first_piece, first;              // the thread's first piece and the feature that it begins with
+    bool full;
+    long long row, rows_apart, lead;     // lead: from the row of the warp's first team to this one's; its lanes, which shuffle, loop together
     __device__ __forceinline__ RowPlace(const Args& a, int warps, int teams) {
         width = TEAM ? TEAM : warps * 32;
         team = threadIdx.x / width;
         t = threadIdx.x - team * width;
         rows_apart = (long long)gridDim.x * teams;
-        // several pieces a thread: all rows of a block lie alike, for its teams share the weights
-        if (EDGES && ITEMS > 1) row = blockIdx.x % V + (long long)V * ((long long)(blockIdx.x / V) * teams + team);
+        if (EDGES) row = blockIdx.x % V + (long long)V * ((long long)(blockIdx.x / V) * teams + team);
         else row = (long long)blockIdx.x * teams + team;
+        lead = TEAM ? (EDGES ? V : 1) * ((threadIdx.x & 31) / TEAM) : 0;
         phase = EDGES ? (int)(row % V) * (int)(a.features % V) % V : 0;
+        first_piece = TEAM ? t : (t >> 5) * (32 * ITEMS) + (t & 31);
+        first = first_piece * V - phase;
+        full = __all_sync(0xffffffffu, first >= 0 && feature(ITEMS - 1) + V <= (int)a.features && (!EDGES || a.aligned));
     }
-    __device__ __forceinline__ int piece(int k) const { return t + k * width; }
-    __device__ __forceinline__ int feature(int k) const { return piece(k) * V - phase; }
+    __device__ __forceinline__ int piece(int k) const { return first_piece + k * STEP; }
+    __device__ __forceinline__ int feature(int k) const { return first + k * STEP * V; }
 };
 
-// What is left of a piece with its first feature at c in a row of n: all of it, or some.
-template <class T, bool EDGES>
-__device__ __forceinline__ bool whole(int c, int n) { return EDGES ? c >= 0 && c + VEC<T> <= n : c < n; }
-template <class T, bool EDGES>
-__device__ __forceinline__ bool partly(int c, int n) { return EDGES && c < n && c + VEC<T> > 0; }
+// Whether a piece with its first feature at c lies in a row of n, or some of it does.
+template <class T, bool FULL, bool EDGES>
+__device__ __forceinline__ bool whole(int c, int n) { return FULL || (EDGES ? c >= 0 && c + VEC<T> <= n : c < n); }
+template <class T, bool FULL, bool EDGES>
+__device__ __forceinline__ bool partly(int c, int n) { return !FULL && EDGES && c < n && c + VEC<T> > 0; }
 
-template <class T, bool EDGES>
-__device__ __forceinline__ void store_piece(T* row, int c, int n, bool packed, const Pack<T>& p) {
-    if (whole<T, EDGES>(c, n) && (!EDGES || packed)) {
-        store_pack(row + c, p);
-    } else if (partly<T, EDGES>(c, n)) {
+template <class T, bool FULL, bool EDGES>
+__device__ __forceinline__ void store_piece(T* at, int c, int n, bool packed, const Pack<T>& p) {
+    if (whole<T, FULL, EDGES>(c, n) && (FULL || !EDGES || packed)) {
+        store_pack(at, p);
+    } else if (partly<T, FULL, EDGES>(c, n)) {
 #pragma unroll
         for (int j = 0; j < VEC<T>; ++j)
-            if ((unsigned)(c + j) < (unsigned)n) row[c + j] = p.e[j];
+            if ((unsigned)(c + j) < (unsigned)n) at[j] = p.e[j];
     }
 }
-// The numbers of a piece; those beyond the row are 0.
-template <class T, bool EDGES>
-__device__ __forceinline__ void take(const Pack<T>& p, int c, int n, float (&v)[VEC<T>]) {
-    unpack(p, v);
-    if (!whole<T, EDGES>(c, n)) {
+// The numbers of a piece; those beyond the row become 0.
+template <class T, bool FULL, bool EDGES>
+__device__ __forceinline__ void only_inside(int c, int n, Two (&v)[VEC<T> / 2]) {
+    if (whole<T, FULL, EDGES>(c, n)) return;
 #pragma unroll
-        for (int j = 0; j < VEC<T>; ++j) v[j] = EDGES && (unsigned)(c + j) < (unsigned)n ? v[j] : 0.f;
-    }
+    for (int j = 0; j < VEC<T>; j += 2)
+        v[j / 2] = Two(EDGES && (unsigned)(c + j) < (unsigned)n ? v[j / 2].lo() : 0.f, EDGES && (unsigned)(c + j + 1) < (unsigned)n ? v[j / 2].hi() : 0.f);
+}
+template <class T, bool FULL, bool EDGES>
+__device__ __forceinline__ void take(const Pack<T>& p, int c, int n, Two (&v)[VEC<T> / 2]) {
+    unpack(p, v);
+    only_inside<T, FULL, EDGES>(c, n, v);
 }
 
 template <int TEAM>
@@ -87,37 +103,37 @@ __device__ __forceinline__ float lanes_sum(float v) {
     return v;
 }
 
-// A vector of the weights as the team's pieces hold it: with one piece a thread in registers, else in shared memory, where the
-// quarters of the pieces lie one behind another (no bank conflicts).  The threads of a block fill it together.
-template <class T, int TEAM, int ITEMS, bool EDGES>
+// A vector of the weights as the pieces hold it, in shared memory; the quarters of the pieces lie one behind another (no bank
+// conflicts).  The threads of a block fill it together, eight loads each at a time (one at a time, filling took longer than the
+// rows of a small call: 2049 rows of 4096, 15 us).
+template <class T, int TEAM, bool EDGES>
 struct Weights {
     static constexpr int V = VEC<T>;
-    float own[V];
-    const float4* shared;
+    const ulonglong2* shared;
     int pieces;
     template <class Place>
-    __device__ __forceinline__ Weights(const void* w, const Args& a, float missing, const Place& at, float* room) : shared(nullptr), pieces(at.width * ITEMS) {
-        const int n = (int)a.features;
-        auto one = [&](int c) { return (unsigned)c >= (unsigned)n ? 0.f : w ? weight_at<T>(w, a.weight_f32, c) : missing; };
-        if (ITEMS == 1) {
+    __device__ __forceinline__ Weights(const void* w, const Args& a, float missing, const Place& at, float* room)
+        : shared(reinterpret_cast<const ulonglong2*>(room)), pieces(at.width * Place::ITEMS) {
+        const int n = (int)a.features, threads = (int)blockDim.x;
+        for (int i0 = threadIdx.x; i0 < pieces * V; i0 += 8 * threads) {
+            float v[8];
 #pragma unroll
-            for (int j = 0; j < V; ++j) own[j] = one(at.feature(0) + j);
-        } else {
-            for (int i = threadIdx.x; i < pieces * V; i += blockDim.x)
-                room[((i % V) / 4 * pieces + i / V) * 4 + i % 4] = one(i - at.phase);
-            shared = reinterpret_cast<const float4*>(room);
+            for (int u = 0; u < 8; ++u) {
+                const int c = i0 + u * threads - at.phase;
+                v[u] = (unsigned)c >= (unsigned)n ? 0.f : w ? weight_at<T>(w, a.weight_f32, c) : missing;
+            }
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const int i = i0 + u * threads;
+                if (i < pieces * V) room[((i % V) / 4 * pieces + i / V) * 4 + i % 4] = v[u];
+            }
         }
     }
-    __device__ __forceinline__ void get(int piece, float (&v)[V]) const {
-        if (ITEMS == 1) {
+    __device__ __forceinline__ void get(int piece, Two (&v)[V / 2]) const {
 #pragma unroll
-            for (int j = 0; j < V; ++j) v[j] = own[j];
-        } else {
-#pragma unroll
-            for (int q = 0; q < V / 4; ++q) {
-                const float4 f = shared[q * pieces + piece];
-                v[4 * q] = f.x; v[4 * q + 1] = f.y; v[4 * q + 2] = f.z; v[4 * q + 3] = f.w;
-            }
+        for (int q = 0; q < V / 4; ++q) {
+            const ulonglong2 f = shared[q * pieces + piece];
+            v[2 * q].bits = f.x; v[2 * q + 1].bits = f.y;
         }
     }
 };
@@ -141,69 +157,78 @@ constexpr int EXCHANGE_BYTES = 2 * ROW_BLOCK_WARPS * sizeof(float4);
 // A thread's pieces of the rows to come, in shared memory: copied there by the thread itself, STAGES - 1 rows ahead, and read
 // by it alone, so that no barrier is needed.  (Rows of 1024 in bf16, forward and VJP, teams of four warps: 216 us with loads into
 // registers, 177 with the ring.)
-template <class T, int ARRAYS, int ITEMS, int STAGES, bool EDGES>
+template <class T, int TEAM, int ARRAYS, int STAGES, bool EDGES>
 struct Ring {
+    static constexpr int ITEMS = ROW_ITEMS<T>;
     Pack<T>* base;
     uint32_t address;
-    __device__ __forceinline__ explicit Ring(void* shared) {
+    int threads;
+    __device__ __forceinline__ explicit Ring(void* shared) : threads(TEAM ? ROW_BLOCK : (int)blockDim.x) {
         base = static_cast<Pack<T>*>(shared) + threadIdx.x;
         address = (uint32_t)__cvta_generic_to_shared(base);
     }
-    __device__ __forceinline__ int place(int stage, int array, int k) const { return ((stage * ARRAYS + array) * ITEMS + k) * (int)blockDim.x; }
+    __device__ __forceinline__ int place(int stage, int array, int k) const { return ((stage * ARRAYS + array) * ITEMS + k) * threads; }
     __device__ __forceinline__ Pack<T> get(int stage, int array, int k) const { return base[place(stage, array, k)]; }
-    // Piece k of row r of an array, its first feature at c.  A piece over the row's ends is copied whole, with its neighbours'
-    // elements, where the array has them.
-    __device__ __forceinline__ void fetch(int stage, int array, int k, const void* from, long long pitch, long long r, int c, const Args& a) {
+    // The pieces of row r of an array.  A piece over the row's ends is copied whole, with its neighbours' elements, where the
+    // array has them.
+    template <bool FULL, class Place>
+    __device__ __forceinline__ void fetch(int stage, int array, const void* from, long long pitch, long long r, const Place& at, const Args& a) {
         const int n = (int)a.features;
-        if (!whole<T, EDGES>(c, n) && !partly<T, EDGES>(c, n)) return;
-        const T* row = static_cast<const T*>(from) + r * pitch;
-        if (!EDGES || (a.aligned && r * pitch + c >= 0 && r * pitch + c + VEC<T> <= (a.outer - 1) * pitch + n)) {
-            copy16(address + 16u * place(stage, array, k), row + c);
-        } else {
-            Pack<T> p;
+        const T* mine = static_cast<const T*>(from) + (r * pitch + at.first);
 #pragma unroll
-            for (int j = 0; j < VEC<T>; ++j) p.e[j] = (unsigned)(c + j) < (unsigned)n ? row[c + j] : from_float<T>(0.f);
-            base[place(stage, array, k)] = p;
+        for (int k = 0; k < ITEMS; ++k) {
+            const int c = at.feature(k);
+            const T* p = mine + k * Place::STEP * VEC<T>;
+            if (whole<T, FULL, EDGES>(c, n) && (FULL || !EDGES || a.aligned)) {
+                copy16(address + 16u * place(stage, array, k), p);
+            } else if (whole<T, FULL, EDGES>(c, n) || partly<T, FULL, EDGES>(c, n)) {
+                if (a.aligned && r * pitch + c >= 0 && r * pitch + c + VEC<T> <= (a.outer - 1) * pitch + n) {
+                    copy16(address + 16u * place(stage, array, k), p);
+                } else {
+                    Pack<T> v;
+#pragma unroll
+                    for (int j = 0; j < VEC<T>; ++j) v.e[j] = (unsigned)(c + j) < (unsigned)n ? p[j] : from_float<T>(0.f);
+                    base[place(stage, array, k)] = v;
+                }
+            }
         }
     }
 };
 
 // Blocks on an SM (registers) and rows in the ring: four, or as many as the shared memory holds beside the weights.
-template <class T, bool VJP, int ITEMS> constexpr int row_blocks() { return VJP ? 2 : 3; }
-template <class T, bool VJP, bool TAIL, int ITEMS>
-constexpr int row_stages() {
-    const int stage = ROW_BLOCK * 16 * ITEMS * ((VJP ? 2 : 1) + TAIL), room = 196 * 1024 / row_blocks<T, VJP, ITEMS>();
+constexpr int row_blocks(bool vjp) { return vjp ? 1 : 3; }
+constexpr int row_stages(bool vjp, bool tail, int size) {
+    const int stage = ROW_BLOCK * ROW_FEATURES * size * ((vjp ? 2 : 1) + tail), room = 192 * 1024 / row_blocks(vjp);
     return room / stage >= 4 ? 4 : room / stage >= 3 ? 3 : 2;
 }
 
-template <class T, int TEAM, int ITEMS, bool EDGES, bool TAIL>
-__global__ void __launch_bounds__(ROW_BLOCK, row_blocks<T, false, ITEMS>()) row_team_forward(const __grid_constant__ Args a, int warps, int teams) {
+template <class T, int TEAM, bool EDGES, bool TAIL>
+__global__ void __launch_bounds__(ROW_BLOCK, row_blocks(false)) row_team_forward(const __grid_constant__ Args a, int warps, int teams) {
     grid_dependency_wait();
     extern __shared__ __align__(16) float shared[];
-    constexpr int V = VEC<T>, STAGES = row_stages<T, false, TAIL, ITEMS>(), ARRAYS = TAIL ? 2 : 1;
-    const RowPlace<T, TEAM, ITEMS, EDGES> at(a, warps, teams);
+    constexpr int V = VEC<T>, ITEMS = ROW_ITEMS<T>, STAGES = row_stages(false, TAIL, sizeof(T)), ARRAYS = TAIL ? 2 : 1;
+    using Place = RowPlace<T, TEAM, EDGES>;
+    const Place at(a, warps, teams);
     Exchange exchange(shared, warps, at.team, at.t);
     float* room = shared + EXCHANGE_BYTES / 4;
-    Ring<T, ARRAYS, ITEMS, STAGES, EDGES> ring(room);
-    room += ARRAYS * ITEMS * STAGES * 4 * blockDim.x;
+    Ring<T, TEAM, ARRAYS, STAGES, EDGES> ring(room);
+    room += ARRAYS * ITEMS * STAGES * 4 * ring.threads;
     const Mask mask(a);
     const int n = (int)a.features;
     const bool packed = a.aligned;
     const float count = (float)n, inv_count = 1.f / count;
-    auto fetch = [&](long long r, int stage) {
+    auto fetch = [&](auto full, long long r, int stage) {
+        constexpr bool FULL = decltype(full)::value;
         if (r < a.outer) {
-#pragma unroll
-            for (int k = 0; k < ITEMS; ++k) {
-                ring.fetch(stage, 0, k, a.x, a.px, r, at.feature(k), a);
-                if (TAIL) ring.fetch(stage, 1, k, a.res, a.pres, r, at.feature(k), a);
-            }
+            ring.template fetch<FULL>(stage, 0, a.x, a.px, r, at, a);
+            if (TAIL) ring.template fetch<FULL>(stage, 1, a.res, a.pres, r, at, a);
         }
         copies_commit();
     };
 #pragma unroll
-    for (int i = 0; i < STAGES - 1; ++i) fetch(at.row + i * at.rows_apart, i);
-    const Weights<T, TEAM, ITEMS, EDGES> weight(a.weight, a, 1.f, at, room), bias(a.bias, a, 0.f, at, room + at.width * ITEMS * V);
-    if (ITEMS > 1) __syncthreads();
+    for (int i = 0; i < STAGES - 1; ++i) fetch(False{}, at.row + i * at.rows_apart, i);
+    const Weights<T, TEAM, EDGES> weight(a.weight, a, 1.f, at, room), bias(a.bias, a, 0.f, at, room + at.width * ITEMS * V);
+    __syncthreads();
     float here = 0.f;                              // features of the row that this warp has
     if (!TEAM) {
         int mine = 0;
@@ -212,59 +237,51 @@ __global__ void __launch_bounds__(ROW_BLOCK, row_blocks<T, false, ITEMS>()) row_
         here = (float)__reduce_add_sync(0xffffffffu, mine);
     }
     const float inv_here = here > 0.f ? 1.f / here : 0.f;
-    // the lanes of a warp go on together
-    const long long lead = TEAM && TEAM < 32 ? (threadIdx.x & 31) / TEAM : 0;
     int stage = 0;
-    for (long long r = at.row; r - lead < a.outer; r += at.rows_apart) {
+    auto one_row = [&](auto full, long long r) {
+        constexpr bool FULL = decltype(full)::value;
         const bool live = !TEAM || TEAM == 32 || r < a.outer;
-        fetch(r + (STAGES - 1) * at.rows_apart, stage == 0 ? STAGES - 1 : stage - 1);
+        fetch(full, r + (STAGES - 1) * at.rows_apart, stage == 0 ? STAGES - 1 : stage - 1);
         copies_wait<STAGES - 1>();
-        float v[ITEMS][V];
+        Two v[ITEMS][V / 2];
+        T* sum = TAIL ? static_cast<T*>(a.out2) + (r * a.pout2 + at.first) : nullptr;
+        const uint64_t block = TAIL ? (uint64_t)((r * n - at.phase) / 4) + (uint32_t)(at.first_piece * (V / 4)) : 0;
 #pragma unroll
         for (int k = 0; k < ITEMS; ++k) {
             const int c = at.feature(k);
-            if (!TAIL) {
-                take<T, EDGES>(ring.get(stage, 0, k), c, live ? n : 0, v[k]);
-            } else {
-                float xs[V], rs[V];
-                uint4 words[V / 4];
-                if (a.dropping) {
-#pragma unroll
-                    for (int q = 0; q < V / 4; ++q) words[q] = mask.words((uint64_t)((r * n - at.phase) / 4) + (uint32_t)(at.piece(k) * (V / 4) + q));
-                }
-                unpack(ring.get(stage, 0, k), xs);
+            unpack(ring.get(stage, 0, k), v[k]);
+            if (TAIL) {
+                Two rs[V / 2];
                 unpack(ring.get(stage, 1, k), rs);
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    const float kept = fmaf(xs[j], a.scale, rs[j]);
-                    rs[j] = a.dropping && mask.dropped(words[j / 4], j % 4) ? rs[j] : kept;
-                }
-                const Pack<T> stored = pack<T>(rs);
-                take<T, EDGES>(stored, c, live ? n : 0, v[k]);
-                if (live) store_piece<T, EDGES>(static_cast<T*>(a.out2) + r * a.pout2, c, n, packed, stored);
+                if (a.dropping) mask.apply<true, true>(block + (uint32_t)(k * Place::STEP * (V / 4)), v[k], rs);
+                else mask.apply<true, false>(0, v[k], rs);
+                const Pack<T> stored = pack<T>(v[k]);
+                unpack(stored, v[k]);
+                if (live) store_piece<T, FULL, EDGES>(sum + k * Place::STEP * V, c, n, packed, stored);
             }
+            only_inside<T, FULL, EDGES>(c, n, v[k]);
         }
         stage = stage + 1 == STAGES ? 0 : stage + 1;
-        float s = 0.f;
+        Two pair(0.f);
 #pragma unroll
         for (int k = 0; k < ITEMS; ++k)
 #pragma unroll
-            for (int j = 0; j < V; ++j) s += v[k][j];
-        s = lanes_sum<TEAM>(s);
+            for (int j = 0; j < V / 2; ++j) pair = pair + v[k][j];
+        float s = lanes_sum<TEAM>(pair.sum());
         auto deviations = [&](float m) {
-            float q = 0.f;
+            Two q(0.f);
+            const Two less(-m);
 #pragma unroll
             for (int k = 0; k < ITEMS; ++k) {
                 const int c = at.feature(k);
-                if (whole<T, EDGES>(c, n)) {
+                Two d[V / 2];
 #pragma unroll
-                    for (int j = 0; j < V; ++j) { const float d = v[k][j] - m; q = fmaf(d, d, q); }
-                } else if (partly<T, EDGES>(c, n)) {
+                for (int j = 0; j < V / 2; ++j) d[j] = v[k][j] + less;
+                only_inside<T, FULL, EDGES>(c, n, d);
 #pragma unroll
-                    for (int j = 0; j < V; ++j) { const float d = (unsigned)(c + j) < (unsigned)n ? v[k][j] - m : 0.f; q = fmaf(d, d, q); }
-                }
+                for (int j = 0; j < V / 2; ++j) q = fma2(d[j], d[j], q);
             }
-            return lanes_sum<TEAM>(q);
+            return lanes_sum<TEAM>(q.sum());
         };
         float mean, q;
         if (TEAM) {
@@ -280,131 +297,130 @@ __global__ void __launch_bounds__(ROW_BLOCK, row_blocks<T, false, ITEMS>()) row_
             for (int u = 0; u < warps; ++u) { const float4 f = set[u]; const float d = f.z - mean; q += fmaf(f.w * d, d, f.y); }
         }
         const float rstd = inverse_root(q * inv_count + a.eps);
-        if (!live) continue;
-        T* y = static_cast<T*>(a.out) + r * a.pout;
+        if (!live) return;
+        T* y = static_cast<T*>(a.out) + (r * a.pout + at.first);
 #pragma unroll
         for (int k = 0; k < ITEMS; ++k) {
-            float w[V], b[V];
+            Two w[V / 2], b[V / 2];
             weight.get(at.piece(k), w);
             bias.get(at.piece(k), b);
 #pragma unroll
-            for (int j = 0; j < V; ++j) v[k][j] = fmaf((v[k][j] - mean) * rstd, w[j], b[j]);
-            store_piece<T, EDGES>(y, at.feature(k), n, packed, pack<T>(v[k]));
+            for (int j = 0; j < V / 2; ++j) v[k][j] = fma2((v[k][j] + Two(-mean)) * Two(rstd), w[j], b[j]);
+            store_piece<T, FULL, EDGES>(y + k * Place::STEP * V, at.feature(k), n, packed, pack<T>(v[k]));
         }
         if (at.t == 0) {
             if (a.mean) a.mean[r] = mean;
             if (a.rstd) a.rstd[r] = rstd;
         }
-    }
+    };
+    if (at.full) for (long long r = at.row; r - at.lead < a.outer; r += at.rows_apart) one_row(True{}, r);
+    else for (long long r = at.row; r - at.lead < a.outer; r += at.rows_apart) one_row(False{}, r);
 }
 
-template <class T, int TEAM, int ITEMS, bool EDGES, bool TAIL>
-__global__ void __launch_bounds__(ROW_BLOCK, row_blocks<T, true, ITEMS>()) row_team_vjp(const __grid_constant__ Args a, int warps, int teams) {
+template <class T, int TEAM, bool EDGES, bool TAIL>
+__global__ void __launch_bounds__(ROW_BLOCK, row_blocks(true)) row_team_vjp(const __grid_constant__ Args a, int warps, int teams) {
     grid_dependency_wait();
     extern __shared__ __align__(16) float shared[];
-    constexpr int V = VEC<T>, STAGES = row_stages<T, true, TAIL, ITEMS>(), ARRAYS = TAIL ? 3 : 2;
-    const RowPlace<T, TEAM, ITEMS, EDGES> at(a, warps, teams);
+    constexpr int V = VEC<T>, ITEMS = ROW_ITEMS<T>, STAGES = row_stages(true, TAIL, sizeof(T)), ARRAYS = TAIL ? 3 : 2;
+    using Place = RowPlace<T, TEAM, EDGES>;
+    const Place at(a, warps, teams);
     Exchange exchange(shared, warps, at.team, at.t);
     float* room = shared + EXCHANGE_BYTES / 4;
-    Ring<T, ARRAYS, ITEMS, STAGES, EDGES> ring(room);
-    room += ARRAYS * ITEMS * STAGES * 4 * blockDim.x;
+    Ring<T, TEAM, ARRAYS, STAGES, EDGES> ring(room);
+    room += ARRAYS * ITEMS * STAGES * 4 * ring.threads;
     const Mask mask(a);
     const int n = (int)a.features;
     const bool packed = a.aligned, added = TAIL && a.gsum;
     const float inv_count = 1.f / (float)n;
-    auto fetch = [&](long long r, int stage) {
+    auto fetch = [&](auto full, long long r, int stage) {
+        constexpr bool FULL = decltype(full)::value;
         if (r < a.outer) {
-#pragma unroll
-            for (int k = 0; k < ITEMS; ++k) {
-                ring.fetch(stage, 0, k, a.x, a.px, r, at.feature(k), a);
-                ring.fetch(stage, 1, k, a.res, a.pres, r, at.feature(k), a);
-                if (added) ring.fetch(stage, 2, k, a.gsum, a.pgsum, r, at.feature(k), a);
-            }
+            ring.template fetch<FULL>(stage, 0, a.x, a.px, r, at, a);
+            ring.template fetch<FULL>(stage, 1, a.res, a.pres, r, at, a);
+            if (added) ring.template fetch<FULL>(stage, 2, a.gsum, a.pgsum, r, at, a);
         }
         copies_commit();
     };
 #pragma unroll
-    for (int i = 0; i < STAGES - 1; ++i) fetch(at.row + i * at.rows_apart, i);
+    for (int i = 0; i < STAGES - 1; ++i) fetch(False{}, at.row + i * at.rows_apart, i);
     float mean_next = 0.f, rstd_next = 0.f;
     if (at.row < a.outer) { mean_next = a.mean[at.row]; rstd_next = a.rstd[at.row]; }
-    const Weights<T, TEAM, ITEMS, EDGES> weight(a.weight, a, 1.f, at, room);
-    if (ITEMS > 1) __syncthreads();
-    float gw[ITEMS][V], gb[ITEMS][V];
+    const Weights<T, TEAM, EDGES> weight(a.weight, a, 1.f, at, room);
+    __syncthreads();
+    Two gw[ITEMS][V / 2], gb[ITEMS][V / 2];
 #pragma unroll
     for (int k = 0; k < ITEMS; ++k)
 #pragma unroll
-        for (int j = 0; j < V; ++j) gw[k][j] = gb[k][j] = 0.f;
-    const long long lead = TEAM && TEAM < 32 ? (threadIdx.x & 31) / TEAM : 0;
+        for (int j = 0; j < V / 2; ++j) gw[k][j] = gb[k][j] = Two(0.f);
     int stage = 0;
-    for (long long r = at.row; r - lead < a.outer; r += at.rows_apart) {
+    auto one_row = [&](auto full, long long r) {
+        constexpr bool FULL = decltype(full)::value;
         const bool live = !TEAM || TEAM == 32 || r < a.outer;
-        fetch(r + (STAGES - 1) * at.rows_apart, stage == 0 ? STAGES - 1 : stage - 1);
+        fetch(full, r + (STAGES - 1) * at.rows_apart, stage == 0 ? STAGES - 1 : stage - 1);
         const float mean = mean_next, rstd = rstd_next;
         if (r + at.rows_apart < a.outer) { mean_next = a.mean[r + at.rows_apart]; rstd_next = a.rstd[r + at.rows_apart]; }
         copies_wait<STAGES - 1>();
         const int used = stage;
         stage = stage + 1 == STAGES ? 0 : stage + 1;
-        float s1 = 0.f, s2 = 0.f;
+        Two p1(0.f), p2(0.f);
+        const Two less(-mean), root(rstd);
 #pragma unroll
         for (int k = 0; k < ITEMS; ++k) {
             const int c = at.feature(k);
-            if (!live || !(whole<T, EDGES>(c, n) || partly<T, EDGES>(c, n))) continue;
-            float g[V], v[V], w[V];
-            take<T, EDGES>(ring.get(used, 0, k), c, n, g);
-            take<T, EDGES>(ring.get(used, 1, k), c, n, v);
+            if (!live || !(whole<T, FULL, EDGES>(c, n) || partly<T, FULL, EDGES>(c, n))) continue;
+            Two g[V / 2], v[V / 2], w[V / 2];
+            take<T, FULL, EDGES>(ring.get(used, 0, k), c, n, g);
+            take<T, FULL, EDGES>(ring.get(used, 1, k), c, n, v);
             weight.get(at.piece(k), w);
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
+            for (int j = 0; j < V / 2; ++j) {
                 // beyond the row g is 0
-                const float h = (v[j] - mean) * rstd, d = g[j] * w[j];
-                gw[k][j] = fmaf(g[j], h, gw[k][j]);
-                gb[k][j] += g[j];
-                s1 += d;
-                s2 = fmaf(d, h, s2);
+                const Two h = (v[j] + less) * root, d = g[j] * w[j];
+                gw[k][j] = fma2(g[j], h, gw[k][j]);
+                gb[k][j] = gb[k][j] + g[j];
+                p1 = p1 + d;
+                p2 = fma2(d, h, p2);
             }
         }
-        s1 = lanes_sum<TEAM>(s1);
-        s2 = lanes_sum<TEAM>(s2);
+        float s1 = lanes_sum<TEAM>(p1.sum()), s2 = lanes_sum<TEAM>(p2.sum());
         if (!TEAM) {
             const float4* set = exchange.put(make_float4(s1, s2, 0.f, 0.f), at.t);
             s1 = s2 = 0.f;
             for (int u = 0; u < warps; ++u) { s1 += set[u].x; s2 += set[u].y; }
         }
-        if (!live) continue;
+        if (!live) return;
         // rstd (g w - mean(g w) - h mean(g w h))
         const float c1 = -rstd * (s1 * inv_count), c2 = -rstd * (s2 * inv_count);
-        T* out = static_cast<T*>(a.out) + r * a.pout;
-        T* out2 = TAIL ? static_cast<T*>(a.out2) + r * a.pout2 : nullptr;
+        T* out = static_cast<T*>(a.out) + (r * a.pout + at.first);
+        T* out2 = TAIL ? static_cast<T*>(a.out2) + (r * a.pout2 + at.first) : nullptr;
+        const uint64_t block = TAIL ? (uint64_t)((r * n - at.phase) / 4) + (uint32_t)(at.first_piece * (V / 4)) : 0;
 #pragma unroll
         for (int k = 0; k < ITEMS; ++k) {
             const int c = at.feature(k);
-            float g[V], v[V], w[V];
+            Two g[V / 2], v[V / 2], w[V / 2];
             unpack(ring.get(used, 0, k), g);
             unpack(ring.get(used, 1, k), v);
             weight.get(at.piece(k), w);
 #pragma unroll
-            for (int j = 0; j < V; ++j) v[j] = fmaf((v[j] - mean) * rstd, c2, fmaf(g[j] * w[j], rstd, c1));
+            for (int j = 0; j < V / 2; ++j) v[j] = fma2((v[j] + less) * root, Two(c2), fma2(g[j] * w[j], root, Two(c1)));
             if (TAIL) {
                 if (added) {
                     unpack(ring.get(used, 2, k), g);
 #pragma unroll
-                    for (int j = 0; j < V; ++j) v[j] += g[j];
+                    for (int j = 0; j < V / 2; ++j) v[j] = v[j] + g[j];
                 }
-                store_piece<T, EDGES>(out2, c, n, packed, pack<T>(v));
-                if (a.dropping) {
-#pragma unroll
-                    for (int q = 0; q < V / 4; ++q) {
-                        const uint4 words = mask.words((uint64_t)((r * n - at.phase) / 4) + (uint32_t)(at.piece(k) * (V / 4) + q));
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) v[4 * q + j] = mask.dropped(words, j) ? 0.f : v[4 * q + j] * a.scale;
-                    }
-                }
+                store_piece<T, FULL, EDGES>(out2 + k * Place::STEP * V, c, n, packed, pack<T>(v));
+                if (a.dropping) mask.apply<false, true>(block + (uint32_t)(k * Place::STEP * (V / 4)), v, v);
             }
-            store_piece<T, EDGES>(out, c, n, packed, pack<T>(v));
+            store_piece<T, FULL, EDGES>(out + k * Place::STEP * V, c, n, packed, pack<T>(v));
         }
-    }
+    };
+    if (at.full) for (long long r = at.row; r - at.lead < a.outer; r += at.rows_apart) one_row(True{}, r);
+    else for (long long r = at.row; r - at.lead < a.outer; r += at.rows_apart) one_row(False{}, r);
     if (!a.gw && !a.gb) return;
+    auto half = [](Two v, int j) { return j % 2 ? v.hi() : v.lo(); };
     auto put = [&](int c, int which, float v) {
+        if ((unsigned)c >= (unsigned)n) return;
         if (gridDim.x > 1) a.part[((long long)blockIdx.x * 2 + which) * n + c] = v;
         else if (which ? a.gb : a.gw) store_weight_grad<T>(which ? a.gb : a.gw, a.weight_f32, c, v);
     };
@@ -412,29 +428,29 @@ __global__ void __launch_bounds__(ROW_BLOCK, row_blocks<T, true, ITEMS>()) row_t
 #pragma unroll
         for (int k = 0; k < ITEMS; ++k)
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                const int c = at.feature(k) + j;
-                if ((unsigned)c < (unsigned)n) { put(c, 0, gw[k][j]); put(c, 1, gb[k][j]); }
-            }
+            for (int j = 0; j < V; ++j) { put(at.feature(k) + j, 0, half(gw[k][j / 2], j)); put(at.feature(k) + j, 1, half(gb[k][j / 2], j)); }
         return;
     }
-    // sums over the block's teams, one team after another
     __syncthreads();
     float* total = shared;
-    for (int c = threadIdx.x; c < 2 * n; c += blockDim.x) total[c] = 0.f;
-    for (int u = 0; u < teams; ++u) {
-        __syncthreads();
-        if (at.team != u) continue;
+    // the teams' features are the same ones: every team leaves its sums, then each thread adds up those of some features
+    const int mine = 2 * ITEMS * V * at.width;
 #pragma unroll
-        for (int k = 0; k < ITEMS; ++k)
+    for (int k = 0; k < ITEMS; ++k)
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                const int c = at.feature(k) + j;
-                if ((unsigned)c < (unsigned)n) { total[c] += gw[k][j]; total[n + c] += gb[k][j]; }
-            }
-    }
+        for (int j = 0; j < V; ++j) {
+            total[at.team * mine + (2 * (k * V + j)) * at.width + at.t] = half(gw[k][j / 2], j);
+            total[at.team * mine + (2 * (k * V + j) + 1) * at.width + at.t] = half(gb[k][j / 2], j);
+        }
     __syncthreads();
-    for (int c = threadIdx.x; c < n; c += blockDim.x) { put(c, 0, total[c]); put(c, 1, total[n + c]); }
+    for (int i = threadIdx.x; i < mine; i += blockDim.x) {
+        float s = 0.f;
+#pragma unroll 8
+        for (int u = 0; u < teams; ++u) s += total[u * mine + i];
+        const int slot = i / at.width, t = i - slot * at.width, which = slot & 1, k = (slot >> 1) / V, j = (slot >> 1) % V;
+        const int piece = (TEAM ? t : (t >> 5) * (32 * ITEMS) + (t & 31)) + k * Place::STEP;
+        put(piece * V - at.phase + j, which, s);
+    }
 }
 
 }  // namespace prior

@@ -368,6 +368,41 @@ def test_outputs_in_place_of_inputs(shape, dtype):
     assert torch.equal(ty, gx) and torch.equal(ts, gr)
 
 
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("features,inner", [(16, 1), (32, 1), (64, 1), (100, 1), (128, 1), (512, 1), (1000, 1), (1024, 1), (4096, 1), (24, 20), (60, 33), (100, 512)])
+@pytest.mark.parametrize("outer", [1, 3, 5, 37])
+def test_what_lies_behind_the_last_slice_stays(outer, features, inner, dtype):
+    """Every output in a buffer of its own that goes on behind the last slice: the canary there stays, whatever part of a warp
+    or block the last rows fill."""
+    import paper_2207_08393_b200 as g
+    from paper_2207_08393_b200 import binding, prior_ops
+    shape, n, room = (outer, features, inner), outer * features * inner, 8192
+    x, res, dy, ds = (make(shape, dtype, k)[0] for k in range(4))
+    w, _, b, _ = weights(features, "float32", 4)
+    bufs = [torch.full((n + room,), -7.0, dtype=x.dtype, device="cuda") for _ in range(5)]
+    total, y, gx, gr, drop = (t[:n].view(shape) for t in bufs)
+    stats = [torch.full((outer * inner + room,), -7.0, device="cuda") for _ in range(2)]
+    mean, rstd = (t[:outer * inner].view(outer, inner) for t in stats)
+    grads = [torch.full((features + room,), -7.0, device="cuda") for _ in range(2)]
+    m = g.make_dropout_args(0.3, 5, 1)
+    dims = lambda: binding.make_feature_dims(prior_ops._DTYPES[x.dtype], 0, outer, features, inner, EPS, stream=torch.cuda.current_stream())
+    g.gleam_dropout_add_layer_norm_forward(x, res, w, b, total, y, mean, rstd, m, dims())
+    dd = dims()
+    size = g.gleam_layer_norm_workspace_size(dd)
+    ws = torch.full((size + room,), 77, dtype=torch.uint8, device="cuda")
+    dd.workspace, dd.workspace_bytes = ws.data_ptr(), size
+    g.gleam_dropout_add_layer_norm_vjp(dy, ds, total, w, mean, rstd, gx, gr, grads[0], grads[1], m, dd)
+    g.gleam_dropout_forward(x, res, drop, m, dims())
+    ref = g.dropout_add_layer_norm_forward(x, res, w, b, 0.3, 5, 1, EPS, dim=1)
+    back = g.dropout_add_layer_norm_vjp(dy, ds, ref[1], w, ref[2], ref[3], 0.3, 5, 1, dim=1)
+    for t, c in ((total, ref[1]), (y, ref[0]), (mean, ref[2]), (rstd, ref[3]), (gx, back[0]), (gr, back[1]),
+                 (grads[0][:features], back[2]), (grads[1][:features], back[3]), (drop, ref[1])):
+        assert torch.equal(t, c)
+    for t, k in [(t, n) for t in bufs] + [(t, outer * inner) for t in stats] + [(t, features) for t in grads]:
+        assert bool((t[k:] == -7.0).all())
+    assert bool((ws[size:] == 77).all())
+
+
 def test_overlaps_are_refused():
     import paper_2207_08393_b200 as g
     from paper_2207_08393_b200 import binding

@@ -3,6 +3,7 @@
 #include "launch_state.cuh"
 #include "prior_entry.h"
 #include "prior_dropout.cuh"
+#include "prior_maps.cuh"
 #include "prior_norm.cuh"
 #include "prior_rows.cuh"
 
@@ -108,6 +109,53 @@ static cudaError_t launch_rows(const Args& a, const RowPlan& p, bool tail, int* 
                 : (p.edges ? launch_rows<VJP, false, true>(a, p, blocks, s) : launch_rows<VJP, false, false>(a, p, blocks, s));
 }
 
+// How maps are dealt to tiles (prior_maps.cuh); vp = 0 where the features of a tile do not fit.
+struct MapPlan { int vp, items, warps; size_t shared; };
+static MapPlan map_plan(const Args& a, bool vjp, bool tail, std::initializer_list<std::pair<const void*, long long>> arrays) {
+    MapPlan p{};
+    if (a.features > 32 * MAP_TILE_WARPS) return p;
+    p.items = a.features <= 8 * MAP_TILE_WARPS ? 8 : a.features <= 16 * MAP_TILE_WARPS ? 16 : 32;
+    p.warps = (int)((a.features + p.items - 1) / p.items);
+    const int copies = (vjp ? 2 : 1) + tail;
+    // pieces of 16 bytes where two tiles fit on an SM, else of 8 and 4
+    for (int vp = 16 / (int)sizeof(T); vp >= 1; vp /= 2) {
+        bool ok = a.inner % vp == 0;
+        for (const auto& v : arrays) ok = ok && (!v.first || ((uintptr_t)v.first % (vp * sizeof(T)) == 0 && (a.outer == 1 || v.second % vp == 0)));
+        const size_t bytes = sizeof(float) * (map_exchange_floats(vp, p.warps) + 2 * (size_t)p.warps * p.items) + sizeof(T) * vp * 32 * (size_t)p.warps * p.items * copies;
+        if (!ok || bytes > (vp * sizeof(T) > 4 ? 112 : 226) * 1024u) continue;
+        p.vp = vp; p.shared = bytes;
+        return p;
+    }
+    return p;
+}
+template <bool VJP, bool TAIL, int VP, int ITEMS>
+static cudaError_t launch_maps(const Args& a, const MapPlan& p, int* blocks, cudaStream_t s) {
+    constexpr auto KERNEL = [] { if constexpr (VJP) return map_tile_vjp<T, VP, ITEMS, TAIL>; else return map_tile_forward<T, VP, ITEMS, TAIL>; }();
+    constexpr size_t SM_BYTES = 227 * 1024;
+    cudaError_t e = ensure_smem(KERNEL, SM_BYTES, kernel_state<KERNEL>);
+    if (e != cudaSuccess) return e;
+    const long long tiles = (a.outer * a.inner / VP + 31) / 32;
+    int fit = (int)(SM_BYTES / (p.shared + 1024));
+    const int threads = p.warps * 32, held = (ITEMS <= 8 ? 1024 : 512) / threads;     // threads that the registers of an SM hold
+    if (fit > held) fit = held;
+    const long long most = (long long)SMS * (fit < 1 ? 1 : fit);
+    *blocks = (int)(tiles < most ? tiles : most);
+    if (VJP && *blocks > MAP_PARTS_MOST) *blocks = MAP_PARTS_MOST;
+    PRIOR_LAUNCH(KERNEL, dim3((unsigned)*blocks), dim3(threads), p.shared, s, a);
+    return cudaSuccess;
+}
+template <bool VJP, bool TAIL, int VP>
+static cudaError_t launch_maps(const Args& a, const MapPlan& p, int* blocks, cudaStream_t s) {
+    return p.items == 8 ? launch_maps<VJP, TAIL, VP, 8>(a, p, blocks, s) : p.items == 16 ? launch_maps<VJP, TAIL, VP, 16>(a, p, blocks, s)
+                                                                                         : launch_maps<VJP, TAIL, VP, 32>(a, p, blocks, s);
+}
+template <bool VJP, bool TAIL>
+static cudaError_t launch_maps(const Args& a, const MapPlan& p, int* blocks, cudaStream_t s) {
+    if constexpr (sizeof(T) == 2) if (p.vp == 8) return launch_maps<VJP, TAIL, 8>(a, p, blocks, s);
+    return p.vp == 4 ? launch_maps<VJP, TAIL, 4>(a, p, blocks, s) : p.vp == 2 ? launch_maps<VJP, TAIL, 2>(a, p, blocks, s)
+                                                                             : launch_maps<VJP, TAIL, 1>(a, p, blocks, s);
+}
+
 static cudaError_t forward(const Args& given, bool tail, cudaStream_t s) {
     Args a = given;
     cudaError_t e;
@@ -120,6 +168,9 @@ static cudaError_t forward(const Args& given, bool tail, cudaStream_t s) {
         if (tail) PRIOR_LAUNCH(row_forward<T, true>, grid, dim3(ROW_THREADS), 0, s, a);
         else PRIOR_LAUNCH(row_forward<T, false>, grid, dim3(ROW_THREADS), 0, s, a);
     } else {
+        const MapPlan p = map_plan(a, false, tail, {{a.x, a.px}, {a.res, a.pres}, {a.out, a.pout}, {a.out2, a.pout2}});
+        int blocks = 0;
+        if (p.vp) return (e = tail ? launch_maps<false, true>(a, p, &blocks, s) : launch_maps<false, false>(a, p, &blocks, s)) != cudaSuccess ? e : prof_mark(-1, s);
         const dim3 grid(bounded((a.outer * a.inner + 31) / 32, GRID));
         if (tail) PRIOR_LAUNCH(map_forward<T, true>, grid, dim3(MAP_WARPS * 32), 0, s, a);
         else PRIOR_LAUNCH(map_forward<T, false>, grid, dim3(MAP_WARPS * 32), 0, s, a);
@@ -141,6 +192,14 @@ static cudaError_t vjp(const Args& given, bool tail, cudaStream_t s) {
         if (p.fits) {
             int blocks = 0;
             if ((e = launch_rows<true>(a, p, tail, &blocks, s)) != cudaSuccess) return e;
+            if ((a.gw || a.gb) && blocks > 1 && (e = weight_grads_from(a, blocks, s)) != cudaSuccess) return e;
+            return prof_mark(-1, s);
+        }
+    } else {
+        const MapPlan p = map_plan(a, true, tail, {{a.x, a.px}, {a.res, a.pres}, {a.gsum, a.pgsum}, {a.out, a.pout}, {a.out2, a.pout2}});
+        if (p.vp) {
+            int blocks = 0;
+            if ((e = tail ? launch_maps<true, true>(a, p, &blocks, s) : launch_maps<true, false>(a, p, &blocks, s)) != cudaSuccess) return e;
             if ((a.gw || a.gb) && blocks > 1 && (e = weight_grads_from(a, blocks, s)) != cudaSuccess) return e;
             return prof_mark(-1, s);
         }

@@ -15,10 +15,10 @@ extern const Ops ops_f32, ops_f16, ops_bf16;
 
 // Rows of partial sums of the weights' gradients that a VJP writes at most (its blocks come eight at a time in one form).
 constexpr int SMS = 148;
-constexpr int PARTS_MOST = 2 * SMS;
+constexpr int PARTS_MOST = 2 * SMS, MAP_PARTS_MOST = 8 * SMS;
 inline int parts_most(const Args& a) {
-    const long long positions = a.outer * a.inner;
-    return (int)(positions + 7 < PARTS_MOST ? positions + 7 : PARTS_MOST);
+    const long long positions = a.outer * a.inner, most = a.inner == 1 ? PARTS_MOST : MAP_PARTS_MOST;
+    return (int)(positions + 7 < most ? positions + 7 : most);
 }
 
 }  // namespace prior

@@ -1,0 +1,356 @@
+// Layer norm and the residual tail on feature maps (inner > 1): a tile of neighbouring positions with all their features in
+// shared memory, so that every array passes once.
+//
+// A tile is 32 pieces of VP positions; lane l of every warp has piece l, and each warp ITEMS neighbouring features of it.  What a
+// thread will work on it copies into shared memory itself (no barrier); the warps exchange sums for each position, which the
+// first threads of the block add up, one position each.  A VJP keeps the sums of its features' weights in registers over all of its
+// block's tiles and adds them across lanes at the end; weight_grads (prior_norm.cuh) adds up the blocks.
+#pragma once
+#include "prior_rows.cuh"
+
+namespace gleam {
+namespace prior {
+
+// VP positions of one feature as they lie in memory, and the pairs of numbers that they become (one position: half a pair).
+template <class T, int VP> struct alignas(VP * sizeof(T)) Piece { T e[VP]; };
+template <int VP> constexpr int PAIRS = (VP + 1) / 2;
+
+template <class T, int VP>
+__device__ __forceinline__ void unpack(const Piece<T, VP>& p, Two (&v)[PAIRS<VP>]) {
+    if constexpr (VP == 1) v[0] = Two(to_float(p.e[0]), 0.f);
+    else {
+#pragma unroll
+        for (int j = 0; j < VP / 2; ++j) {
+            if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+                const uint32_t w = reinterpret_cast<const uint32_t*>(&p)[j];
+                v[j] = Two(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+            } else if constexpr (std::is_same<T, __half>::value) {
+                const float2 f = __half22float2(reinterpret_cast<const __half2*>(&p)[j]);
+                v[j] = Two(f.x, f.y);
+            } else {
+                v[j] = Two(p.e[2 * j], p.e[2 * j + 1]);
+            }
+        }
+    }
+}
+template <class T, int VP>
+__device__ __forceinline__ Piece<T, VP> piece_of(const Two (&v)[PAIRS<VP>]) {
+    Piece<T, VP> p;
+    if constexpr (VP == 1) p.e[0] = from_float<T>(v[0].lo());
+    else {
+#pragma unroll
+        for (int j = 0; j < VP / 2; ++j) {
+            if constexpr (std::is_same<T, __nv_bfloat16>::value) reinterpret_cast<__nv_bfloat162*>(&p)[j] = __floats2bfloat162_rn(v[j].lo(), v[j].hi());
+            else if constexpr (std::is_same<T, __half>::value) reinterpret_cast<__half2*>(&p)[j] = __floats2half2_rn(v[j].lo(), v[j].hi());
+            else { p.e[2 * j] = v[j].lo(); p.e[2 * j + 1] = v[j].hi(); }
+        }
+    }
+    return p;
+}
+// Mask::apply for the VP elements from number i on, which share a counter (VP = 8: two).
+template <bool RES, int VP>
+__device__ __forceinline__ void drop_piece(const Mask& mask, uint64_t i, Two (&v)[PAIRS<VP>], const Two (&r)[PAIRS<VP>]) {
+    if constexpr (VP >= 4) mask.apply<RES, true>(i >> 2, v, r);
+    else {
+        const uint4 w = mask.words(i >> 2);
+        const int at = (int)(i & 3u);
+        const Two kept = RES ? fma2(v[0], Two(mask.a.scale), r[0]) : v[0] * Two(mask.a.scale), gone = RES ? r[0] : Two(0.f);
+        v[0] = Two(mask.dropped(w, at) ? gone.lo() : kept.lo(), VP == 2 && mask.dropped(w, at + 1) ? gone.hi() : kept.hi());
+    }
+}
+
+constexpr int MAP_TILE_WARPS = 16;                       // warps of a block at most
+
+// A block's view of its tiles.
+template <class T, int VP, int ITEMS, int ARRAYS>
+struct MapTile {
+    using P = Piece<T, VP>;
+    P* slots;                            // this thread's pieces: (array, item), a block's width apart
+    int lane, warp, first, items;        // first feature and number of features of the warp
+    long long pieces, o, k;              // pieces of an array; slice and position in it of this lane's piece of the tile
+    bool live;
+    __device__ __forceinline__ MapTile(const Args& a, void* shared) {
+        slots = static_cast<P*>(shared) + threadIdx.x;
+        lane = threadIdx.x & 31; warp = threadIdx.x >> 5;
+        first = warp * ITEMS;
+        items = min(ITEMS, (int)a.features - first);
+        pieces = a.outer * a.inner / VP;
+        o = k = 0; live = false;
+    }
+    __device__ __forceinline__ P& slot(int array, int j) const { return slots[(array * ITEMS + j) * (int)blockDim.x]; }
+    __device__ __forceinline__ void go(long long tile, const Args& a) {
+        const long long p = tile * 32 + lane, row = a.inner / VP;
+        live = p < pieces;
+        o = !live ? 0 : pieces <= 0xffffffffll ? (uint32_t)p / (uint32_t)row : p / row;
+        k = live ? (p - o * row) * VP : 0;
+    }
+    __device__ __forceinline__ const T* at(const void* array, long long pitch, const Args& a) const {
+        return static_cast<const T*>(array) + (o * pitch + first * a.inner + k);
+    }
+    __device__ __forceinline__ T* at(void* array, long long pitch, const Args& a) const {
+        return static_cast<T*>(array) + (o * pitch + first * a.inner + k);
+    }
+    __device__ __forceinline__ void fetch(int array, const void* from, long long pitch, const Args& a) const {
+        if (!live) return;
+        const T* p = at(from, pitch, a);
+        if constexpr (sizeof(P) >= 4) {
+#pragma unroll
+            for (int j = 0; j < ITEMS; ++j) {
+                if (j >= items) break;
+                const uint32_t to = (uint32_t)__cvta_generic_to_shared(&slot(array, j));
+                if constexpr (sizeof(P) == 16) copy16(to, p);
+                else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(p), "n"(sizeof(P) < 4 ? 4 : (int)sizeof(P)) : "memory");
+                p += a.inner;
+            }
+        } else {                                         // two bytes: too few for a copy
+            T v[ITEMS];
+#pragma unroll
+            for (int j = 0; j < ITEMS; ++j) if (j < items) v[j] = p[j * a.inner];
+#pragma unroll
+            for (int j = 0; j < ITEMS; ++j) if (j < items) slot(array, j).e[0] = v[j];
+        }
+    }
+    // number of the first element of feature j's piece
+    __device__ __forceinline__ uint64_t element(int j, const Args& a) const { return (uint64_t)((o * a.features + first + j) * a.inner + k); }
+};
+
+// Two sums for each position of the tile, as (2, warps, 32 VP) floats; `mine` adds a position's up, of which `per_warp` gets
+// every warp's pair; what it leaves in the first two rows is read back by all.
+template <int VP, class F>
+__device__ __forceinline__ void map_exchange(float* sums, int warps, int lane, int warp, const Two (&a)[PAIRS<VP>], const Two (&b)[PAIRS<VP>], Two (&ra)[PAIRS<VP>],
+                                             Two (&rb)[PAIRS<VP>], F&& add_up) {
+    constexpr int N = 32 * VP;
+    auto put = [&](float* row, const Two (&v)[PAIRS<VP>]) {
+        if constexpr (VP == 1) row[lane] = v[0].lo();
+        else {
+#pragma unroll
+            for (int j = 0; j < VP / 2; ++j) *reinterpret_cast<unsigned long long*>(row + j * 64 + 2 * lane) = v[j].bits;
+        }
+    };
+    auto get = [&](const float* row, Two (&v)[PAIRS<VP>]) {
+        if constexpr (VP == 1) v[0] = Two(row[lane], 0.f);
+        else {
+#pragma unroll
+            for (int j = 0; j < VP / 2; ++j) v[j].bits = *reinterpret_cast<const unsigned long long*>(row + j * 64 + 2 * lane);
+        }
+    };
+    put(sums + warp * N, a);
+    put(sums + (warps + warp) * N, b);
+    __syncthreads();
+    // position i of the exchange: pair j of the lanes, lane, half
+    for (int i = threadIdx.x; i < N; i += blockDim.x) add_up(i, sums + i, sums + warps * N + i, sums + 2 * warps * N + i, N);
+    __syncthreads();
+    get(sums + 2 * warps * N, ra);
+    get(sums + (2 * warps + 1) * N, rb);
+}
+// Floats of the exchange.
+constexpr size_t map_exchange_floats(int vp, int warps) { return (size_t)(2 * warps + 2) * 32 * vp; }
+
+template <class T, int VP, int ITEMS, bool TAIL>
+__global__ void __launch_bounds__(MAP_TILE_WARPS * 32, ITEMS <= 8 ? 2 : 1) map_tile_forward(const __grid_constant__ Args a) {
+    grid_dependency_wait();
+    extern __shared__ __align__(16) float shared[];
+    const int warps = blockDim.x >> 5, n = (int)a.features;
+    float* sums = shared;
+    float* wt = sums + map_exchange_floats(VP, warps);
+    float* bs = wt + warps * ITEMS;
+    MapTile<T, VP, ITEMS, TAIL ? 2 : 1> t(a, bs + warps * ITEMS);
+    for (int c = threadIdx.x; c < warps * ITEMS; c += blockDim.x) {
+        wt[c] = c >= n ? 0.f : a.weight ? weight_at<T>(a.weight, a.weight_f32, c) : 1.f;
+        bs[c] = c < n && a.bias ? weight_at<T>(a.bias, a.weight_f32, c) : 0.f;
+    }
+    const Mask mask(a);
+    const float count = (float)n, inv_count = 1.f / count, here = (float)t.items, inv_here = 1.f / here;
+    const long long tiles = (t.pieces + 31) / 32;
+    auto fetch = [&](long long tile) {
+        if (tile < tiles) {
+            t.go(tile, a);
+            t.fetch(0, a.x, a.px, a);
+            if (TAIL) t.fetch(1, a.res, a.pres, a);
+        }
+        copies_commit();
+    };
+    fetch(blockIdx.x);
+    __syncthreads();                                     // the weights
+    for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+        copies_wait<0>();
+        Two s[PAIRS<VP>], q[PAIRS<VP>];
+#pragma unroll
+        for (int i = 0; i < PAIRS<VP>; ++i) s[i] = q[i] = Two(0.f);
+        T* sum = TAIL ? t.at(a.out2, a.pout2, a) : nullptr;
+#pragma unroll
+        for (int j = 0; j < ITEMS; ++j) {
+            if (j >= t.items || !t.live) break;
+            Two v[PAIRS<VP>];
+            unpack<T, VP>(t.slot(0, j), v);
+            if (TAIL) {
+                Two r[PAIRS<VP>];
+                unpack<T, VP>(t.slot(1, j), r);
+                if (a.dropping) drop_piece<true, VP>(mask, t.element(j, a), v, r);
+                else {
+#pragma unroll
+                    for (int i = 0; i < PAIRS<VP>; ++i) v[i] = v[i] + r[i];
+                }
+                const Piece<T, VP> stored = piece_of<T, VP>(v);
+                unpack<T, VP>(stored, v);
+                t.slot(0, j) = stored;
+                *reinterpret_cast<Piece<T, VP>*>(sum + j * a.inner) = stored;
+            }
+#pragma unroll
+            for (int i = 0; i < PAIRS<VP>; ++i) s[i] = s[i] + v[i];
+        }
+        // every warp's mean m_w and squared deviations from it; the sum of (d + m_w - m)^2 is that of d^2 and n_w (m_w - m)^2
+#pragma unroll
+        for (int j = 0; j < ITEMS; ++j) {
+            if (j >= t.items || !t.live) break;
+            Two v[PAIRS<VP>];
+            unpack<T, VP>(t.slot(0, j), v);
+#pragma unroll
+            for (int i = 0; i < PAIRS<VP>; ++i) { const Two d = fma2(s[i], Two(-inv_here), v[i]); q[i] = fma2(d, d, q[i]); }
+        }
+        Two mean[PAIRS<VP>], rstd[PAIRS<VP>];
+        map_exchange<VP>(sums, warps, t.lane, t.warp, s, q, mean, rstd, [&](int, const float* ps, const float* pq, float* to, int N) {
+            float all = 0.f, dev = 0.f;
+            for (int u = 0; u < warps; ++u) all += ps[u * N];
+            const float m = quotient(all, count, inv_count);
+            for (int u = 0; u < warps; ++u) {
+                const float nw = (float)min(ITEMS, n - u * ITEMS), d = ps[u * N] * (1.f / nw) - m;
+                dev += fmaf(nw * d, d, pq[u * N]);
+            }
+            to[0] = m; to[N] = inverse_root(dev * inv_count + a.eps);
+        });
+        if (t.live) {
+            T* y = t.at(a.out, a.pout, a);
+#pragma unroll
+            for (int j = 0; j < ITEMS; ++j) {
+                if (j >= t.items) break;
+                Two v[PAIRS<VP>];
+                unpack<T, VP>(t.slot(0, j), v);
+                const Two w(wt[t.first + j]), b(bs[t.first + j]), minus(-1.f);
+#pragma unroll
+                for (int i = 0; i < PAIRS<VP>; ++i) v[i] = fma2(fma2(mean[i], minus, v[i]) * rstd[i], w, b);
+                *reinterpret_cast<Piece<T, VP>*>(y + j * a.inner) = piece_of<T, VP>(v);
+            }
+            if (t.warp == 0 && (a.mean || a.rstd)) {
+                const long long at = t.o * a.inner + t.k;
+#pragma unroll
+                for (int i = 0; i < VP; ++i) {
+                    if (a.mean) a.mean[at + i] = i % 2 ? mean[i / 2].hi() : mean[i / 2].lo();
+                    if (a.rstd) a.rstd[at + i] = i % 2 ? rstd[i / 2].hi() : rstd[i / 2].lo();
+                }
+            }
+        }
+        fetch(tile + gridDim.x);
+    }
+}
+
+template <class T, int VP, int ITEMS, bool TAIL>
+__global__ void __launch_bounds__(MAP_TILE_WARPS * 32, ITEMS <= 8 ? 2 : 1) map_tile_vjp(const __grid_constant__ Args a) {
+    grid_dependency_wait();
+    extern __shared__ __align__(16) float shared[];
+    const int warps = blockDim.x >> 5, n = (int)a.features;
+    float* sums = shared;
+    float* wt = sums + map_exchange_floats(VP, warps);
+    MapTile<T, VP, ITEMS, TAIL ? 3 : 2> t(a, wt + warps * ITEMS * 2);
+    for (int c = threadIdx.x; c < warps * ITEMS; c += blockDim.x) wt[c] = c >= n ? 0.f : a.weight ? weight_at<T>(a.weight, a.weight_f32, c) : 1.f;
+    const Mask mask(a);
+    const bool added = TAIL && a.gsum;
+    const float inv_count = 1.f / (float)n;
+    const long long tiles = (t.pieces + 31) / 32;
+    Two less[PAIRS<VP>], rstd[PAIRS<VP>];
+    auto fetch = [&](long long tile) {
+        if (tile < tiles) {
+            t.go(tile, a);
+            t.fetch(0, a.x, a.px, a);
+            t.fetch(1, a.res, a.pres, a);
+            if (added) t.fetch(2, a.gsum, a.pgsum, a);
+            if (t.live) {
+                const long long at = t.o * a.inner + t.k;
+                if constexpr (VP == 1) { less[0] = Two(-a.mean[at], 0.f); rstd[0] = Two(a.rstd[at], 0.f); }
+                else {
+#pragma unroll
+                    for (int i = 0; i < VP / 2; ++i) { less[i] = Two(-a.mean[at + 2 * i], -a.mean[at + 2 * i + 1]); rstd[i] = Two(a.rstd[at + 2 * i], a.rstd[at + 2 * i + 1]); }
+                }
+            }
+        }
+        copies_commit();
+    };
+    fetch(blockIdx.x);
+    float gw[ITEMS], gb[ITEMS];
+#pragma unroll
+    for (int j = 0; j < ITEMS; ++j) gw[j] = gb[j] = 0.f;
+    __syncthreads();                                     // the weights
+    for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+        copies_wait<0>();
+        Two s1[PAIRS<VP>], s2[PAIRS<VP>];
+#pragma unroll
+        for (int i = 0; i < PAIRS<VP>; ++i) s1[i] = s2[i] = Two(0.f);
+#pragma unroll
+        for (int j = 0; j < ITEMS; ++j) {
+            if (j >= t.items || !t.live) break;
+            Two g[PAIRS<VP>], v[PAIRS<VP>], sw(0.f), sb(0.f);
+            unpack<T, VP>(t.slot(0, j), g);
+            unpack<T, VP>(t.slot(1, j), v);
+            const Two w(wt[t.first + j]);
+#pragma unroll
+            for (int i = 0; i < PAIRS<VP>; ++i) {
+                const Two h = (v[i] + less[i]) * rstd[i], d = g[i] * w;
+                sw = fma2(g[i], h, sw);
+                sb = sb + g[i];
+                s1[i] = s1[i] + d;
+                s2[i] = fma2(d, h, s2[i]);
+            }
+            gw[j] += sw.sum(); gb[j] += sb.sum();
+        }
+        Two c1[PAIRS<VP>], c2[PAIRS<VP>];
+        map_exchange<VP>(sums, warps, t.lane, t.warp, s1, s2, c1, c2, [&](int, const float* p1, const float* p2, float* to, int N) {
+            float all1 = 0.f, all2 = 0.f;
+            for (int u = 0; u < warps; ++u) { all1 += p1[u * N]; all2 += p2[u * N]; }
+            to[0] = -all1 * inv_count; to[N] = -all2 * inv_count;
+        });
+        if (t.live) {
+            T* out = t.at(a.out, a.pout, a);
+            T* out2 = TAIL ? t.at(a.out2, a.pout2, a) : nullptr;
+#pragma unroll
+            for (int j = 0; j < ITEMS; ++j) {
+                if (j >= t.items) break;
+                Two g[PAIRS<VP>], v[PAIRS<VP>];
+                unpack<T, VP>(t.slot(0, j), g);
+                unpack<T, VP>(t.slot(1, j), v);
+                const Two w(wt[t.first + j]);
+                // rstd (g w - mean(g w) - h mean(g w h))
+#pragma unroll
+                for (int i = 0; i < PAIRS<VP>; ++i) v[i] = fma2((v[i] + less[i]) * rstd[i], c2[i], fma2(g[i], w, c1[i])) * rstd[i];
+                if (TAIL) {
+                    if (added) {
+                        unpack<T, VP>(t.slot(2, j), g);
+#pragma unroll
+                        for (int i = 0; i < PAIRS<VP>; ++i) v[i] = v[i] + g[i];
+                    }
+                    *reinterpret_cast<Piece<T, VP>*>(out2 + j * a.inner) = piece_of<T, VP>(v);
+                    if (a.dropping) drop_piece<false, VP>(mask, t.element(j, a), v, v);
+                }
+                *reinterpret_cast<Piece<T, VP>*>(out + j * a.inner) = piece_of<T, VP>(v);
+            }
+        }
+        fetch(tile + gridDim.x);
+    }
+    if (!a.gw && !a.gb) return;
+#pragma unroll
+    for (int j = 0; j < ITEMS; ++j) {
+        if (j >= t.items) break;
+        const float w = lanes_sum<32>(gw[j]), b = lanes_sum<32>(gb[j]);
+        const int c = t.first + j;
+        if (t.lane != 0) continue;
+        if (gridDim.x > 1) {
+            a.part[(long long)blockIdx.x * 2 * n + c] = w;
+            a.part[((long long)blockIdx.x * 2 + 1) * n + c] = b;
+        } else {
+            if (a.gw) store_weight_grad<T>(a.gw, a.weight_f32, c, w);
+            if (a.gb) store_weight_grad<T>(a.gb, a.weight_f32, c, b);
+        }
+    }
+}
+
+}  // namespace prior
+}  // namespace gleam

@@ -114,7 +114,8 @@ struct MapPlan { int vp, items, warps; size_t shared; };
 static MapPlan map_plan(const Args& a, bool vjp, bool tail, std::initializer_list<std::pair<const void*, long long>> arrays) {
     MapPlan p{};
     if (a.features > 32 * MAP_TILE_WARPS) return p;
-    p.items = a.features <= 8 * MAP_TILE_WARPS ? 8 : a.features <= 16 * MAP_TILE_WARPS ? 16 : 32;
+    // a VJP has two sums more for each feature in registers: fewer threads, with 128 each
+    p.items = !vjp && a.features <= 8 * MAP_TILE_WARPS ? 8 : a.features <= 16 * MAP_TILE_WARPS ? 16 : 32;
     p.warps = (int)((a.features + p.items - 1) / p.items);
     const int copies = (vjp ? 2 : 1) + tail;
     // pieces of 16 bytes where two tiles fit on an SM, else of 8 and 4
@@ -146,8 +147,8 @@ static cudaError_t launch_maps(const Args& a, const MapPlan& p, int* blocks, cud
 }
 template <bool VJP, bool TAIL, int VP>
 static cudaError_t launch_maps(const Args& a, const MapPlan& p, int* blocks, cudaStream_t s) {
-    return p.items == 8 ? launch_maps<VJP, TAIL, VP, 8>(a, p, blocks, s) : p.items == 16 ? launch_maps<VJP, TAIL, VP, 16>(a, p, blocks, s)
-                                                                                         : launch_maps<VJP, TAIL, VP, 32>(a, p, blocks, s);
+    if constexpr (!VJP) if (p.items == 8) return launch_maps<VJP, TAIL, VP, 8>(a, p, blocks, s);
+    return p.items == 16 ? launch_maps<VJP, TAIL, VP, 16>(a, p, blocks, s) : launch_maps<VJP, TAIL, VP, 32>(a, p, blocks, s);
 }
 template <bool VJP, bool TAIL>
 static cudaError_t launch_maps(const Args& a, const MapPlan& p, int* blocks, cudaStream_t s) {

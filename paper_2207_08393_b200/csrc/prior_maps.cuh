@@ -90,29 +90,34 @@ struct MapTile {
     __device__ __forceinline__ T* at(void* array, long long pitch, const Args& a) const {
         return static_cast<T*>(array) + (o * pitch + first * a.inner + k);
     }
+    // Whether all of the warp's features and lanes are there: then nothing is checked.
+    __device__ __forceinline__ bool full() const { return items == ITEMS && __all_sync(0xffffffffu, live); }
+    template <bool FULL> __device__ __forceinline__ bool has(int j) const { return FULL || (live && j < items); }
+    template <bool FULL>
     __device__ __forceinline__ void fetch(int array, const void* from, long long pitch, const Args& a) const {
-        if (!live) return;
         const T* p = at(from, pitch, a);
         if constexpr (sizeof(P) >= 4) {
 #pragma unroll
-            for (int j = 0; j < ITEMS; ++j) {
-                if (j >= items) break;
+            for (int j = 0; j < ITEMS; ++j, p += a.inner) {
+                if (!has<FULL>(j)) continue;
                 const uint32_t to = (uint32_t)__cvta_generic_to_shared(&slot(array, j));
                 if constexpr (sizeof(P) == 16) copy16(to, p);
                 else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(p), "n"(sizeof(P) < 4 ? 4 : (int)sizeof(P)) : "memory");
-                p += a.inner;
             }
         } else {                                         // two bytes: too few for a copy
             T v[ITEMS];
 #pragma unroll
-            for (int j = 0; j < ITEMS; ++j) if (j < items) v[j] = p[j * a.inner];
+            for (int j = 0; j < ITEMS; ++j, p += a.inner) if (has<FULL>(j)) v[j] = *p;
 #pragma unroll
-            for (int j = 0; j < ITEMS; ++j) if (j < items) slot(array, j).e[0] = v[j];
+            for (int j = 0; j < ITEMS; ++j) if (has<FULL>(j)) slot(array, j).e[0] = v[j];
         }
     }
-    // number of the first element of feature j's piece
-    __device__ __forceinline__ uint64_t element(int j, const Args& a) const { return (uint64_t)((o * a.features + first + j) * a.inner + k); }
+    // number of the first element of the warp's first feature
+    __device__ __forceinline__ uint64_t element(const Args& a) const { return (uint64_t)((o * a.features + first) * a.inner + k); }
 };
+
+// Rounding can leave a sum of squares below zero; a NaN stays.
+__device__ __forceinline__ float not_negative(float v) { return v < 0.f ? 0.f : v; }
 
 // Two sums for each position of the tile, as (2, warps, 32 VP) floats; `mine` adds a position's up, of which `per_warp` gets
 // every warp's pair; what it leaves in the first two rows is read back by all.
@@ -160,92 +165,117 @@ __global__ void __launch_bounds__(MAP_TILE_WARPS * 32, ITEMS <= 8 ? 2 : 1) map_t
         bs[c] = c < n && a.bias ? weight_at<T>(a.bias, a.weight_f32, c) : 0.f;
     }
     const Mask mask(a);
-    const float count = (float)n, inv_count = 1.f / count, here = (float)t.items, inv_here = 1.f / here;
+    const float inv_count = 1.f / (float)n, here = (float)t.items, inv_here = 1.f / here;
     const long long tiles = (t.pieces + 31) / 32;
+    bool full = false;
     auto fetch = [&](long long tile) {
         if (tile < tiles) {
             t.go(tile, a);
-            t.fetch(0, a.x, a.px, a);
-            if (TAIL) t.fetch(1, a.res, a.pres, a);
+            full = t.full();
+            if (full) {
+                t.template fetch<true>(0, a.x, a.px, a);
+                if (TAIL) t.template fetch<true>(1, a.res, a.pres, a);
+            } else {
+                t.template fetch<false>(0, a.x, a.px, a);
+                if (TAIL) t.template fetch<false>(1, a.res, a.pres, a);
+            }
         }
         copies_commit();
+    };
+    // the warp's features of every position: their mean and squared deviations from it.  Both are taken from the first feature on;
+    // as that is one of them, what the difference cancels is at most as many times the result as there are features.
+    auto statistics = [&](auto whole_tile, Two (&mean)[PAIRS<VP>], Two (&dev)[PAIRS<VP>]) {
+        constexpr bool FULL = decltype(whole_tile)::value;
+        Two pivot[PAIRS<VP>], s[PAIRS<VP>], q[PAIRS<VP>];
+#pragma unroll
+        for (int i = 0; i < PAIRS<VP>; ++i) pivot[i] = s[i] = q[i] = Two(0.f);
+        T* sum = TAIL ? t.at(a.out2, a.pout2, a) : nullptr;
+        uint64_t element = TAIL ? t.element(a) : 0;
+#pragma unroll
+        for (int j = 0; j < ITEMS; ++j) {
+            if (t.template has<FULL>(j)) {
+                Two v[PAIRS<VP>];
+                unpack<T, VP>(t.slot(0, j), v);
+                if (TAIL) {
+                    Two r[PAIRS<VP>];
+                    unpack<T, VP>(t.slot(1, j), r);
+                    if (a.dropping) drop_piece<true, VP>(mask, element, v, r);
+                    else {
+#pragma unroll
+                        for (int i = 0; i < PAIRS<VP>; ++i) v[i] = v[i] + r[i];
+                    }
+                    const Piece<T, VP> stored = piece_of<T, VP>(v);
+                    unpack<T, VP>(stored, v);
+                    t.slot(0, j) = stored;
+                    *reinterpret_cast<Piece<T, VP>*>(sum) = stored;
+                }
+#pragma unroll
+                for (int i = 0; i < PAIRS<VP>; ++i) {
+                    if (j == 0) pivot[i] = v[i] * Two(-1.f);
+                    else { const Two d = v[i] + pivot[i]; s[i] = s[i] + d; q[i] = fma2(d, d, q[i]); }
+                }
+            }
+            sum += a.inner; element += a.inner;
+        }
+#pragma unroll
+        for (int i = 0; i < PAIRS<VP>; ++i) {
+            mean[i] = fma2(s[i], Two(inv_here), pivot[i] * Two(-1.f));
+            dev[i] = fma2(s[i] * Two(-inv_here), s[i], q[i]);
+        }
+    };
+    auto normalise = [&](auto whole_tile, const Two (&mean)[PAIRS<VP>], const Two (&rstd)[PAIRS<VP>]) {
+        constexpr bool FULL = decltype(whole_tile)::value;
+        T* y = t.at(a.out, a.pout, a);
+        Two less[PAIRS<VP>];
+#pragma unroll
+        for (int i = 0; i < PAIRS<VP>; ++i) less[i] = mean[i] * Two(-1.f);
+#pragma unroll
+        for (int j = 0; j < ITEMS; ++j, y += a.inner) {
+            if (!t.template has<FULL>(j)) continue;
+            Two v[PAIRS<VP>];
+            unpack<T, VP>(t.slot(0, j), v);
+            const Two w(wt[t.first + j]), b(bs[t.first + j]);
+#pragma unroll
+            for (int i = 0; i < PAIRS<VP>; ++i) v[i] = fma2((v[i] + less[i]) * rstd[i], w, b);
+            *reinterpret_cast<Piece<T, VP>*>(y) = piece_of<T, VP>(v);
+        }
+        if (t.warp == 0 && t.live && (a.mean || a.rstd)) {
+            const long long at = t.o * a.inner + t.k;
+#pragma unroll
+            for (int i = 0; i < VP; ++i) {
+                if (a.mean) a.mean[at + i] = i % 2 ? mean[i / 2].hi() : mean[i / 2].lo();
+                if (a.rstd) a.rstd[at + i] = i % 2 ? rstd[i / 2].hi() : rstd[i / 2].lo();
+            }
+        }
     };
     fetch(blockIdx.x);
     __syncthreads();                                     // the weights
     for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
         copies_wait<0>();
-        Two s[PAIRS<VP>], q[PAIRS<VP>];
-#pragma unroll
-        for (int i = 0; i < PAIRS<VP>; ++i) s[i] = q[i] = Two(0.f);
-        T* sum = TAIL ? t.at(a.out2, a.pout2, a) : nullptr;
-#pragma unroll
-        for (int j = 0; j < ITEMS; ++j) {
-            if (j >= t.items || !t.live) break;
-            Two v[PAIRS<VP>];
-            unpack<T, VP>(t.slot(0, j), v);
-            if (TAIL) {
-                Two r[PAIRS<VP>];
-                unpack<T, VP>(t.slot(1, j), r);
-                if (a.dropping) drop_piece<true, VP>(mask, t.element(j, a), v, r);
-                else {
-#pragma unroll
-                    for (int i = 0; i < PAIRS<VP>; ++i) v[i] = v[i] + r[i];
-                }
-                const Piece<T, VP> stored = piece_of<T, VP>(v);
-                unpack<T, VP>(stored, v);
-                t.slot(0, j) = stored;
-                *reinterpret_cast<Piece<T, VP>*>(sum + j * a.inner) = stored;
+        Two mean[PAIRS<VP>], dev[PAIRS<VP>], rstd[PAIRS<VP>];
+        if (full) statistics(True{}, mean, dev);
+        else statistics(False{}, mean, dev);
+        // from the warps' means and deviations those of all, again relative to the first: the sum of (d + m_w - m)^2 is that of
+        // d^2 and n_w (m_w - m)^2
+        map_exchange<VP>(sums, warps, t.lane, t.warp, mean, dev, mean, rstd, [&](int, const float* pm, const float* pd, float* to, int N) {
+            const float m0 = pm[0];
+            float lin = 0.f, all = pd[0];
+            for (int u = 1; u < warps; ++u) {
+                const float nw = (float)min(ITEMS, n - u * ITEMS), d = pm[u * N] - m0;
+                lin = fmaf(nw, d, lin);
+                all += fmaf(nw * d, d, pd[u * N]);
             }
-#pragma unroll
-            for (int i = 0; i < PAIRS<VP>; ++i) s[i] = s[i] + v[i];
-        }
-        // every warp's mean m_w and squared deviations from it; the sum of (d + m_w - m)^2 is that of d^2 and n_w (m_w - m)^2
-#pragma unroll
-        for (int j = 0; j < ITEMS; ++j) {
-            if (j >= t.items || !t.live) break;
-            Two v[PAIRS<VP>];
-            unpack<T, VP>(t.slot(0, j), v);
-#pragma unroll
-            for (int i = 0; i < PAIRS<VP>; ++i) { const Two d = fma2(s[i], Two(-inv_here), v[i]); q[i] = fma2(d, d, q[i]); }
-        }
-        Two mean[PAIRS<VP>], rstd[PAIRS<VP>];
-        map_exchange<VP>(sums, warps, t.lane, t.warp, s, q, mean, rstd, [&](int, const float* ps, const float* pq, float* to, int N) {
-            float all = 0.f, dev = 0.f;
-            for (int u = 0; u < warps; ++u) all += ps[u * N];
-            const float m = quotient(all, count, inv_count);
-            for (int u = 0; u < warps; ++u) {
-                const float nw = (float)min(ITEMS, n - u * ITEMS), d = ps[u * N] * (1.f / nw) - m;
-                dev += fmaf(nw * d, d, pq[u * N]);
-            }
-            to[0] = m; to[N] = inverse_root(dev * inv_count + a.eps);
+            to[0] = fmaf(lin, inv_count, m0);
+            to[N] = inverse_root(not_negative(fmaf(-lin * inv_count, lin, all)) * inv_count + a.eps);
         });
-        if (t.live) {
-            T* y = t.at(a.out, a.pout, a);
-#pragma unroll
-            for (int j = 0; j < ITEMS; ++j) {
-                if (j >= t.items) break;
-                Two v[PAIRS<VP>];
-                unpack<T, VP>(t.slot(0, j), v);
-                const Two w(wt[t.first + j]), b(bs[t.first + j]), minus(-1.f);
-#pragma unroll
-                for (int i = 0; i < PAIRS<VP>; ++i) v[i] = fma2(fma2(mean[i], minus, v[i]) * rstd[i], w, b);
-                *reinterpret_cast<Piece<T, VP>*>(y + j * a.inner) = piece_of<T, VP>(v);
-            }
-            if (t.warp == 0 && (a.mean || a.rstd)) {
-                const long long at = t.o * a.inner + t.k;
-#pragma unroll
-                for (int i = 0; i < VP; ++i) {
-                    if (a.mean) a.mean[at + i] = i % 2 ? mean[i / 2].hi() : mean[i / 2].lo();
-                    if (a.rstd) a.rstd[at + i] = i % 2 ? rstd[i / 2].hi() : rstd[i / 2].lo();
-                }
-            }
-        }
+        if (full) normalise(True{}, mean, rstd);
+        else normalise(False{}, mean, rstd);
         fetch(tile + gridDim.x);
     }
 }
 
 template <class T, int VP, int ITEMS, bool TAIL>
-__global__ void __launch_bounds__(MAP_TILE_WARPS * 32, ITEMS <= 8 ? 2 : 1) map_tile_vjp(const __grid_constant__ Args a) {
+__global__ void __launch_bounds__(MAP_TILE_WARPS * 32, 1) map_tile_vjp(const __grid_constant__ Args a) {
     grid_dependency_wait();
     extern __shared__ __align__(16) float shared[];
     const int warps = blockDim.x >> 5, n = (int)a.features;
@@ -258,12 +288,20 @@ __global__ void __launch_bounds__(MAP_TILE_WARPS * 32, ITEMS <= 8 ? 2 : 1) map_t
     const float inv_count = 1.f / (float)n;
     const long long tiles = (t.pieces + 31) / 32;
     Two less[PAIRS<VP>], rstd[PAIRS<VP>];
+    bool full = false;
     auto fetch = [&](long long tile) {
         if (tile < tiles) {
             t.go(tile, a);
-            t.fetch(0, a.x, a.px, a);
-            t.fetch(1, a.res, a.pres, a);
-            if (added) t.fetch(2, a.gsum, a.pgsum, a);
+            full = t.full();
+            if (full) {
+                t.template fetch<true>(0, a.x, a.px, a);
+                t.template fetch<true>(1, a.res, a.pres, a);
+                if (added) t.template fetch<true>(2, a.gsum, a.pgsum, a);
+            } else {
+                t.template fetch<false>(0, a.x, a.px, a);
+                t.template fetch<false>(1, a.res, a.pres, a);
+                if (added) t.template fetch<false>(2, a.gsum, a.pgsum, a);
+            }
             if (t.live) {
                 const long long at = t.o * a.inner + t.k;
                 if constexpr (VP == 1) { less[0] = Two(-a.mean[at], 0.f); rstd[0] = Two(a.rstd[at], 0.f); }
@@ -275,19 +313,16 @@ __global__ void __launch_bounds__(MAP_TILE_WARPS * 32, ITEMS <= 8 ? 2 : 1) map_t
         }
         copies_commit();
     };
-    fetch(blockIdx.x);
     float gw[ITEMS], gb[ITEMS];
 #pragma unroll
     for (int j = 0; j < ITEMS; ++j) gw[j] = gb[j] = 0.f;
-    __syncthreads();                                     // the weights
-    for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-        copies_wait<0>();
-        Two s1[PAIRS<VP>], s2[PAIRS<VP>];
+    auto sum_up = [&](auto whole_tile, Two (&s1)[PAIRS<VP>], Two (&s2)[PAIRS<VP>]) {
+        constexpr bool FULL = decltype(whole_tile)::value;
 #pragma unroll
         for (int i = 0; i < PAIRS<VP>; ++i) s1[i] = s2[i] = Two(0.f);
 #pragma unroll
         for (int j = 0; j < ITEMS; ++j) {
-            if (j >= t.items || !t.live) break;
+            if (!t.template has<FULL>(j)) continue;
             Two g[PAIRS<VP>], v[PAIRS<VP>], sw(0.f), sb(0.f);
             unpack<T, VP>(t.slot(0, j), g);
             unpack<T, VP>(t.slot(1, j), v);
@@ -295,25 +330,22 @@ __global__ void __launch_bounds__(MAP_TILE_WARPS * 32, ITEMS <= 8 ? 2 : 1) map_t
 #pragma unroll
             for (int i = 0; i < PAIRS<VP>; ++i) {
                 const Two h = (v[i] + less[i]) * rstd[i], d = g[i] * w;
-                sw = fma2(g[i], h, sw);
-                sb = sb + g[i];
+                sw = i ? fma2(g[i], h, sw) : g[i] * h;
+                sb = i ? sb + g[i] : g[i];
                 s1[i] = s1[i] + d;
                 s2[i] = fma2(d, h, s2[i]);
             }
             gw[j] += sw.sum(); gb[j] += sb.sum();
         }
-        Two c1[PAIRS<VP>], c2[PAIRS<VP>];
-        map_exchange<VP>(sums, warps, t.lane, t.warp, s1, s2, c1, c2, [&](int, const float* p1, const float* p2, float* to, int N) {
-            float all1 = 0.f, all2 = 0.f;
-            for (int u = 0; u < warps; ++u) { all1 += p1[u * N]; all2 += p2[u * N]; }
-            to[0] = -all1 * inv_count; to[N] = -all2 * inv_count;
-        });
-        if (t.live) {
-            T* out = t.at(a.out, a.pout, a);
-            T* out2 = TAIL ? t.at(a.out2, a.pout2, a) : nullptr;
+    };
+    auto gradient = [&](auto whole_tile, const Two (&c1)[PAIRS<VP>], const Two (&c2)[PAIRS<VP>]) {
+        constexpr bool FULL = decltype(whole_tile)::value;
+        T* out = t.at(a.out, a.pout, a);
+        T* out2 = TAIL ? t.at(a.out2, a.pout2, a) : nullptr;
+        uint64_t element = TAIL ? t.element(a) : 0;
 #pragma unroll
-            for (int j = 0; j < ITEMS; ++j) {
-                if (j >= t.items) break;
+        for (int j = 0; j < ITEMS; ++j, out += a.inner) {
+            if (t.template has<FULL>(j)) {
                 Two g[PAIRS<VP>], v[PAIRS<VP>];
                 unpack<T, VP>(t.slot(0, j), g);
                 unpack<T, VP>(t.slot(1, j), v);
@@ -327,12 +359,28 @@ __global__ void __launch_bounds__(MAP_TILE_WARPS * 32, ITEMS <= 8 ? 2 : 1) map_t
 #pragma unroll
                         for (int i = 0; i < PAIRS<VP>; ++i) v[i] = v[i] + g[i];
                     }
-                    *reinterpret_cast<Piece<T, VP>*>(out2 + j * a.inner) = piece_of<T, VP>(v);
-                    if (a.dropping) drop_piece<false, VP>(mask, t.element(j, a), v, v);
+                    *reinterpret_cast<Piece<T, VP>*>(out2) = piece_of<T, VP>(v);
+                    if (a.dropping) drop_piece<false, VP>(mask, element, v, v);
                 }
-                *reinterpret_cast<Piece<T, VP>*>(out + j * a.inner) = piece_of<T, VP>(v);
+                *reinterpret_cast<Piece<T, VP>*>(out) = piece_of<T, VP>(v);
             }
+            if (TAIL) { out2 += a.inner; element += a.inner; }
         }
+    };
+    fetch(blockIdx.x);
+    __syncthreads();                                     // the weights
+    for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+        copies_wait<0>();
+        Two c1[PAIRS<VP>], c2[PAIRS<VP>];
+        if (full) sum_up(True{}, c1, c2);
+        else sum_up(False{}, c1, c2);
+        map_exchange<VP>(sums, warps, t.lane, t.warp, c1, c2, c1, c2, [&](int, const float* p1, const float* p2, float* to, int N) {
+            float all1 = 0.f, all2 = 0.f;
+            for (int u = 0; u < warps; ++u) { all1 += p1[u * N]; all2 += p2[u * N]; }
+            to[0] = -all1 * inv_count; to[N] = -all2 * inv_count;
+        });
+        if (full) gradient(True{}, c1, c2);
+        else gradient(False{}, c1, c2);
         fetch(tile + gridDim.x);
     }
     if (!a.gw && !a.gb) return;

@@ -191,31 +191,34 @@ __global__ void __launch_bounds__(MAP_TILE_WARPS * 32, ITEMS <= 8 ? 2 : 1) map_t
         for (int i = 0; i < PAIRS<VP>; ++i) pivot[i] = s[i] = q[i] = Two(0.f);
         T* sum = TAIL ? t.at(a.out2, a.pout2, a) : nullptr;
         uint64_t element = TAIL ? t.element(a) : 0;
+        auto value = [&](int j, Two (&v)[PAIRS<VP>]) {
+            unpack<T, VP>(t.slot(0, j), v);
+            if (!TAIL) return;
+            Two r[PAIRS<VP>];
+            unpack<T, VP>(t.slot(1, j), r);
+            if (a.dropping) drop_piece<true, VP>(mask, element, v, r);
+            else {
 #pragma unroll
-        for (int j = 0; j < ITEMS; ++j) {
-            if (t.template has<FULL>(j)) {
-                Two v[PAIRS<VP>];
-                unpack<T, VP>(t.slot(0, j), v);
-                if (TAIL) {
-                    Two r[PAIRS<VP>];
-                    unpack<T, VP>(t.slot(1, j), r);
-                    if (a.dropping) drop_piece<true, VP>(mask, element, v, r);
-                    else {
-#pragma unroll
-                        for (int i = 0; i < PAIRS<VP>; ++i) v[i] = v[i] + r[i];
-                    }
-                    const Piece<T, VP> stored = piece_of<T, VP>(v);
-                    unpack<T, VP>(stored, v);
-                    t.slot(0, j) = stored;
-                    *reinterpret_cast<Piece<T, VP>*>(sum) = stored;
-                }
-#pragma unroll
-                for (int i = 0; i < PAIRS<VP>; ++i) {
-                    if (j == 0) pivot[i] = v[i] * Two(-1.f);
-                    else { const Two d = v[i] + pivot[i]; s[i] = s[i] + d; q[i] = fma2(d, d, q[i]); }
-                }
+                for (int i = 0; i < PAIRS<VP>; ++i) v[i] = v[i] + r[i];
             }
+            const Piece<T, VP> stored = piece_of<T, VP>(v);
+            unpack<T, VP>(stored, v);
+            t.slot(0, j) = stored;
+            *reinterpret_cast<Piece<T, VP>*>(sum) = stored;
             sum += a.inner; element += a.inner;
+        };
+        if (t.template has<FULL>(0)) {
+            value(0, pivot);
+#pragma unroll
+            for (int i = 0; i < PAIRS<VP>; ++i) pivot[i] = pivot[i] * Two(-1.f);
+            // two at a time: more of the mask's code than that does not stay in the instruction cache
+#pragma unroll 2
+            for (int j = 1; j < (FULL ? ITEMS : t.items); ++j) {
+                Two v[PAIRS<VP>];
+                value(j, v);
+#pragma unroll
+                for (int i = 0; i < PAIRS<VP>; ++i) { const Two d = v[i] + pivot[i]; s[i] = s[i] + d; q[i] = fma2(d, d, q[i]); }
+            }
         }
 #pragma unroll
         for (int i = 0; i < PAIRS<VP>; ++i) {
@@ -229,9 +232,8 @@ __global__ void __launch_bounds__(MAP_TILE_WARPS * 32, ITEMS <= 8 ? 2 : 1) map_t
         Two less[PAIRS<VP>];
 #pragma unroll
         for (int i = 0; i < PAIRS<VP>; ++i) less[i] = mean[i] * Two(-1.f);
-#pragma unroll
-        for (int j = 0; j < ITEMS; ++j, y += a.inner) {
-            if (!t.template has<FULL>(j)) continue;
+#pragma unroll 4
+        for (int j = 0; j < (FULL ? ITEMS : t.live ? t.items : 0); ++j, y += a.inner) {
             Two v[PAIRS<VP>];
             unpack<T, VP>(t.slot(0, j), v);
             const Two w(wt[t.first + j]), b(bs[t.first + j]);
@@ -343,28 +345,26 @@ __global__ void __launch_bounds__(MAP_TILE_WARPS * 32, 1) map_tile_vjp(const __g
         T* out = t.at(a.out, a.pout, a);
         T* out2 = TAIL ? t.at(a.out2, a.pout2, a) : nullptr;
         uint64_t element = TAIL ? t.element(a) : 0;
+#pragma unroll 2
+        for (int j = 0; j < (FULL ? ITEMS : t.live ? t.items : 0); ++j, out += a.inner) {
+            Two g[PAIRS<VP>], v[PAIRS<VP>];
+            unpack<T, VP>(t.slot(0, j), g);
+            unpack<T, VP>(t.slot(1, j), v);
+            const Two w(wt[t.first + j]);
+            // rstd (g w - mean(g w) - h mean(g w h))
 #pragma unroll
-        for (int j = 0; j < ITEMS; ++j, out += a.inner) {
-            if (t.template has<FULL>(j)) {
-                Two g[PAIRS<VP>], v[PAIRS<VP>];
-                unpack<T, VP>(t.slot(0, j), g);
-                unpack<T, VP>(t.slot(1, j), v);
-                const Two w(wt[t.first + j]);
-                // rstd (g w - mean(g w) - h mean(g w h))
+            for (int i = 0; i < PAIRS<VP>; ++i) v[i] = fma2((v[i] + less[i]) * rstd[i], c2[i], fma2(g[i], w, c1[i])) * rstd[i];
+            if (TAIL) {
+                if (added) {
+                    unpack<T, VP>(t.slot(2, j), g);
 #pragma unroll
-                for (int i = 0; i < PAIRS<VP>; ++i) v[i] = fma2((v[i] + less[i]) * rstd[i], c2[i], fma2(g[i], w, c1[i])) * rstd[i];
-                if (TAIL) {
-                    if (added) {
-                        unpack<T, VP>(t.slot(2, j), g);
-#pragma unroll
-                        for (int i = 0; i < PAIRS<VP>; ++i) v[i] = v[i] + g[i];
-                    }
-                    *reinterpret_cast<Piece<T, VP>*>(out2) = piece_of<T, VP>(v);
-                    if (a.dropping) drop_piece<false, VP>(mask, element, v, v);
+                    for (int i = 0; i < PAIRS<VP>; ++i) v[i] = v[i] + g[i];
                 }
-                *reinterpret_cast<Piece<T, VP>*>(out) = piece_of<T, VP>(v);
+                *reinterpret_cast<Piece<T, VP>*>(out2) = piece_of<T, VP>(v);
+                if (a.dropping) drop_piece<false, VP>(mask, element, v, v);
+                out2 += a.inner; element += a.inner;
             }
-            if (TAIL) { out2 += a.inner; element += a.inner; }
+            *reinterpret_cast<Piece<T, VP>*>(out) = piece_of<T, VP>(v);
         }
     };
     fetch(blockIdx.x);

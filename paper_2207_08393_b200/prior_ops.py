@@ -126,13 +126,13 @@ def _match(x, t, dim):
     return _like(x, dim, view).copy_(t)
 
 
-def _weight_type(x, features, *vectors):
+def _weight_type(x, features, weight, bias=None):
     """The type of the weights.  None stands for ones or zeros."""
     kind = None
-    for w in vectors:
+    for w in (weight, bias):
         if w is None:
             continue
-        if w.shape != (features,) or w.device != x.device or not w.is_contiguous():
+        if w.dim() != 1 or w.numel() != features or w.get_device() != x.get_device() or not w.is_contiguous():
             raise ValueError("weights: a contiguous vector of %d features on %s is wanted" % (features, x.device))
         if w.dtype not in (torch.float32, x.dtype) or kind not in (None, w.dtype):
             raise ValueError("weights: %s where float32 or %s is wanted, the same for all" % (w.dtype, x.dtype))
@@ -140,23 +140,10 @@ def _weight_type(x, features, *vectors):
     return torch.float32 if kind is None else kind
 
 
-def _check_statistics(x, dim, mean, rstd):
-    shape = x.shape[:dim] + x.shape[dim + 1:]
+def _check_statistics(x, shape, mean, rstd):
     for t in (mean, rstd):
-        if t.shape != shape or t.dtype != torch.float32 or t.device != x.device or not t.is_contiguous():
+        if t.shape != shape or t.dtype != torch.float32 or t.get_device() != x.get_device() or not t.is_contiguous():
             raise ValueError("statistics: contiguous float32 of shape %s is wanted" % (tuple(shape),))
-
-
-def _stream(x):
-    """Handle of the current stream of the tensor's device."""
-    if x.get_device() != torch.cuda.current_device():
-        return torch.cuda.current_stream(x.device).cuda_stream
-    return _b._current_stream_handle()
-
-
-def _dims(x, wtype, view, eps, pitches):
-    return _b.gleam_feature_dims(1, _DTYPES[x.dtype], _DTYPES[wtype], eps, view.outer, view.features, view.inner, pitches,
-                                 _stream(x) or None, None, 0)
 
 
 class _On:
@@ -164,7 +151,7 @@ class _On:
     __slots__ = ("other",)
 
     def __init__(self, x):
-        self.other = None if x.get_device() == torch.cuda.current_device() else torch.cuda.device(x.device)
+        self.other = None if x.get_device() == _current_device() else torch.cuda.device(x.device)
 
     def __enter__(self):
         if self.other is not None:
@@ -173,6 +160,72 @@ class _On:
     def __exit__(self, *a):
         if self.other is not None:
             self.other.__exit__(*a)
+
+
+def _current_device():
+    """torch.cuda.current_device() without its checks where torch offers that (not part of its documented interface)."""
+    try:
+        return torch._C._cuda_getDevice()
+    except AttributeError:
+        return torch.cuda.current_device()
+
+
+class _Call:
+    """What a call on contiguous tensors of one shape and type takes, apart from addresses: the structure to copy, the shape of
+    the statistics, the bytes of a VJP's scratch.  Kept by shape and type: filling these takes longer than the kernels of a small
+    call (tail of 20 x 160, forward and VJP: 64 us)."""
+    __slots__ = ("dim", "features", "stats", "template", "scratch")
+
+    def __init__(self, x, dim, wtype, eps):
+        self.dim = _features_axis(x, dim)
+        v = _View(_numel(x.shape[:self.dim]), x.shape[self.dim], _numel(x.shape[self.dim + 1:]), 0, False)
+        self.features = v.features
+        self.stats = torch.Size(x.shape[:self.dim] + x.shape[self.dim + 1:])
+        d = _dims(x, wtype, v, eps, ())
+        d.stream = None
+        self.scratch = max(_b.gleam_layer_norm_workspace_size(d), 256)
+        self.template = bytes(d)
+
+
+_CALLS = {}
+_CALLS_MOST = 256                                # beyond that the table starts over
+_new_dims = _b.gleam_feature_dims.from_buffer_copy
+
+
+def _call(x, dim, wtype, eps):
+    key = (x.shape, x.dtype, dim, wtype, eps)
+    c = _CALLS.get(key)
+    if c is None:
+        c = _Call(x, dim, wtype, eps)
+        if len(_CALLS) >= _CALLS_MOST:
+            _CALLS.clear()
+        _CALLS[key] = c
+    return c
+
+
+def _plain(x, *others):
+    """Whether all tensors are contiguous CUDA tensors of x's shape and type on the current device (None: not there)."""
+    if not isinstance(x, torch.Tensor) or not x.is_cuda or not x.is_contiguous() or x.numel() == 0 or x.dtype not in _DTYPES:
+        return False
+    device = x.get_device()
+    if device != _current_device():
+        return False
+    for t in others:
+        if t is not None and not (t.is_contiguous() and t.shape == x.shape and t.dtype is x.dtype and t.get_device() == device):
+            return False
+    return True
+
+
+def _dims(x, wtype, view, eps, pitches):
+    return _b.gleam_feature_dims(1, _DTYPES[x.dtype], _DTYPES[wtype], eps, view.outer, view.features, view.inner, pitches,
+                                 _stream(x) or None, None, 0)
+
+
+def _stream(x):
+    """Handle of the current stream of the tensor's device."""
+    if x.get_device() != _current_device():
+        return torch.cuda.current_stream(x.device).cuda_stream
+    return _b._current_stream_handle()
 
 
 def _drop_args(x, p, seed, offset, step):
@@ -192,33 +245,71 @@ def _workspace(x, dims, wanted):
     return ws
 
 
+class _Prepared:
+    """Views, outputs' layout and structure of one norm call on the tensors x, *others: the general way, or from the kept
+    table where all are plain."""
+    __slots__ = ("dim", "features", "wtype", "stats", "view", "dims", "scratch")
+
+    def __init__(self, x, dim, eps, weight, bias, *others):
+        if _plain(x, *[t for t, _ in others]):
+            self.wtype = _weight_type(x, weight.numel() if weight is not None else bias.numel() if bias is not None else 0, weight, bias)
+            c = _call(x, dim, self.wtype, eps)
+            if (weight is not None and weight.numel() != c.features) or (bias is not None and bias.numel() != c.features):
+                _weight_type(x, c.features, weight, bias)                # raises
+            self.dim, self.features, self.stats, self.view, self.scratch = c.dim, c.features, c.stats, None, c.scratch
+            self.dims = _new_dims(c.template)
+            self.dims.stream = _b._current_stream_handle() or None
+            return
+        self.dim = dim = _features_axis(x, dim)
+        self.view = v = _view(x, dim)
+        views = [v if t is None else _same(x, t, v, dim, what) for t, what in others]
+        self.features = v.features
+        self.wtype = _weight_type(x, v.features, weight, bias)
+        self.stats = x.shape[:dim] + x.shape[dim + 1:]
+        self.scratch = None
+        self.dims = _dims(x, self.wtype, v, eps, tuple([u.pitch for u in views]))
+
+    def like(self, x):
+        return torch.empty_like(x) if self.view is None else _like(x, self.dim, self.view)
+
+    def vector(self, x):
+        return torch.empty(self.features, dtype=self.wtype, device=x.device)
+
+    def statistics(self, x):
+        return torch.empty(self.stats, dtype=torch.float32, device=x.device), torch.empty(self.stats, dtype=torch.float32, device=x.device)
+
+    def workspace(self, x, wanted):
+        if not wanted:
+            return None
+        if self.scratch is None:
+            return _workspace(x, self.dims, True)
+        ws = torch.empty(self.scratch, dtype=torch.uint8, device=x.device)
+        self.dims.workspace, self.dims.workspace_bytes = ws.data_ptr(), self.scratch
+        return ws
+
+
+# A contiguous array's pitch is 0 in the structure, so that the order of the arguments does not matter to the kept one.
+
 def layer_norm_forward(x, weight=None, bias=None, eps=1e-5, dim=-1):
     """(y, mean, rstd): y = (x - mean) rstd weight + bias over axis ``dim``; mean and rstd are float32 without that axis."""
-    dim = _features_axis(x, dim)
-    v = _view(x, dim)
-    wtype = _weight_type(x, v.features, weight, bias)
-    y = _like(x, dim, v)
-    mean = torch.empty(x.shape[:dim] + x.shape[dim + 1:], dtype=torch.float32, device=x.device)
-    rstd = torch.empty_like(mean)
+    c = _Prepared(x, dim, eps, weight, bias, (None, "x"))
+    y = c.like(x)
+    mean, rstd = c.statistics(x)
     with _On(x):
-        _b.gleam_layer_norm_forward(x, weight, bias, y, mean, rstd, _dims(x, wtype, v, eps, (v.pitch,)))
+        _b.gleam_layer_norm_forward(x, weight, bias, y, mean, rstd, c.dims)
     return y, mean, rstd
 
 
 def layer_norm_vjp(grad_y, x, weight, mean, rstd, dim=-1, weight_grad=True, bias_grad=True):
     """(grad_x, grad_weight, grad_bias) of ``layer_norm_forward``; the last two are None where they are not wanted."""
-    dim = _features_axis(x, dim)
-    v = _view(x, dim)
-    vg = _same(x, grad_y, v, dim, "grad_y")
-    wtype = _weight_type(x, v.features, weight)
-    _check_statistics(x, dim, mean, rstd)
-    gx = _like(x, dim, v)
-    gw = torch.empty(v.features, dtype=wtype, device=x.device) if weight_grad else None
-    gb = torch.empty(v.features, dtype=wtype, device=x.device) if bias_grad else None
+    c = _Prepared(x, dim, 0.0, weight, None, (grad_y, "grad_y"), (None, "x"))
+    _check_statistics(x, c.stats, mean, rstd)
+    gx = c.like(x)
+    gw = c.vector(x) if weight_grad else None
+    gb = c.vector(x) if bias_grad else None
     with _On(x):
-        dims = _dims(x, wtype, v, 0.0, (vg.pitch, v.pitch))
-        ws = _workspace(x, dims, weight_grad or bias_grad)
-        _b.gleam_layer_norm_vjp(grad_y, x, weight, mean, rstd, gx, gw, gb, dims)
+        ws = c.workspace(x, weight_grad or bias_grad)
+        _b.gleam_layer_norm_vjp(grad_y, x, weight, mean, rstd, gx, gw, gb, c.dims)
     del ws
     return gx, gw, gb
 
@@ -245,19 +336,23 @@ def _flat(first, *others):
 
 def dropout_forward(x, p, seed, offset, residual=None, step=None):
     """[residual +] dropout(x).  The call takes ceil(x.numel() / 4) counters from ``offset``."""
-    _check_kind(x)
-    others = ()
-    if residual is not None:
-        _same_kind(x, residual, "residual")
-        others = (residual,)
-    outer, slice_, pitch = (1, 0, [0, 0]) if x.numel() == 0 else _flat(x, *others)
+    if _plain(x, residual):
+        outer, slice_, pitch = 1, x.numel(), ()
+        out = torch.empty_like(x)
+    else:
+        _check_kind(x)
+        others = ()
+        if residual is not None:
+            _same_kind(x, residual, "residual")
+            others = (residual,)
+        outer, slice_, pitch = (1, 0, ()) if x.numel() == 0 else _flat(x, *others)
+        if x.is_contiguous():
+            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        else:                                        # dense, in x's order
+            axes = _memory_order(x)
+            out = torch.empty([x.shape[k] for k in axes], dtype=x.dtype, device=x.device)
+            out = out.permute([axes.index(k) for k in range(x.dim())])
     args = _drop_args(x, p, seed, offset, step)
-    if x.is_contiguous():
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    else:                                            # dense, in x's order
-        axes = _memory_order(x)
-        out = torch.empty([x.shape[k] for k in axes], dtype=x.dtype, device=x.device)
-        out = out.permute([axes.index(k) for k in range(x.dim())])
     with _On(x):
         dims = _b.gleam_feature_dims(1, _DTYPES[x.dtype], _b.GLEAM_F32, 0.0, outer, 1, slice_, tuple(pitch),
                                      _stream(x) or None, None, 0)
@@ -273,37 +368,27 @@ def dropout_vjp(grad_out, p, seed, offset, step=None):
 
 def dropout_add_layer_norm_forward(x, residual, weight, bias, p, seed, offset, eps=1e-5, dim=-1, step=None):
     """(y, total, mean, rstd): total = residual + dropout(x), y = layer norm of total over axis ``dim``."""
-    dim = _features_axis(x, dim)
-    v = _view(x, dim)
-    vr = _same(x, residual, v, dim, "residual")
-    wtype = _weight_type(x, v.features, weight, bias)
+    c = _Prepared(x, dim, eps, weight, bias, (None, "x"), (residual, "residual"))
     args = _drop_args(x, p, seed, offset, step)
-    y, total = _like(x, dim, v), _like(x, dim, v)
-    mean = torch.empty(x.shape[:dim] + x.shape[dim + 1:], dtype=torch.float32, device=x.device)
-    rstd = torch.empty_like(mean)
+    y, total = c.like(x), c.like(x)
+    mean, rstd = c.statistics(x)
     with _On(x):
-        _b.gleam_dropout_add_layer_norm_forward(x, residual, weight, bias, total, y, mean, rstd, args,
-                                                _dims(x, wtype, v, eps, (v.pitch, vr.pitch)))
+        _b.gleam_dropout_add_layer_norm_forward(x, residual, weight, bias, total, y, mean, rstd, args, c.dims)
     return y, total, mean, rstd
 
 
 def dropout_add_layer_norm_vjp(grad_y, grad_total, total, weight, mean, rstd, p, seed, offset, dim=-1, step=None,
                                weight_grad=True, bias_grad=True):
     """(grad_x, grad_residual, grad_weight, grad_bias); ``grad_total`` (None: zero) is the cotangent of total."""
-    dim = _features_axis(total, dim)
-    v = _view(total, dim)
-    vg = _same(total, grad_y, v, dim, "grad_y")
-    vs = v if grad_total is None else _same(total, grad_total, v, dim, "grad_total")
-    wtype = _weight_type(total, v.features, weight)
-    _check_statistics(total, dim, mean, rstd)
+    c = _Prepared(total, dim, 0.0, weight, None, (grad_y, "grad_y"), (grad_total, "grad_total"), (None, "total"))
+    _check_statistics(total, c.stats, mean, rstd)
     args = _drop_args(total, p, seed, offset, step)
-    gx, gr = _like(total, dim, v), _like(total, dim, v)
-    gw = torch.empty(v.features, dtype=wtype, device=total.device) if weight_grad else None
-    gb = torch.empty(v.features, dtype=wtype, device=total.device) if bias_grad else None
+    gx, gr = c.like(total), c.like(total)
+    gw = c.vector(total) if weight_grad else None
+    gb = c.vector(total) if bias_grad else None
     with _On(total):
-        dims = _dims(total, wtype, v, 0.0, (vg.pitch, vs.pitch, v.pitch))
-        ws = _workspace(total, dims, weight_grad or bias_grad)
-        _b.gleam_dropout_add_layer_norm_vjp(grad_y, grad_total, total, weight, mean, rstd, gx, gr, gw, gb, args, dims)
+        ws = c.workspace(total, weight_grad or bias_grad)
+        _b.gleam_dropout_add_layer_norm_vjp(grad_y, grad_total, total, weight, mean, rstd, gx, gr, gw, gb, args, c.dims)
     del ws
     return gx, gr, gw, gb
 

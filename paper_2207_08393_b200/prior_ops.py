@@ -272,18 +272,23 @@ class _Prepared:
     def like(self, x):
         return torch.empty_like(x) if self.view is None else _like(x, self.dim, self.view)
 
-    def vector(self, x):
-        return torch.empty(self.features, dtype=self.wtype, device=x.device)
+    def vectors(self, x, weight, *wanted):
+        out = [None, None]
+        for k, w in enumerate(wanted):
+            if w:
+                out[k] = torch.empty_like(weight) if weight is not None else x.new_empty(self.features, dtype=self.wtype)
+        return out
 
     def statistics(self, x):
-        return torch.empty(self.stats, dtype=torch.float32, device=x.device), torch.empty(self.stats, dtype=torch.float32, device=x.device)
+        mean = x.new_empty(self.stats, dtype=torch.float32)
+        return mean, torch.empty_like(mean)
 
     def workspace(self, x, wanted):
         if not wanted:
             return None
         if self.scratch is None:
             return _workspace(x, self.dims, True)
-        ws = torch.empty(self.scratch, dtype=torch.uint8, device=x.device)
+        ws = x.new_empty(self.scratch, dtype=torch.uint8)
         self.dims.workspace, self.dims.workspace_bytes = ws.data_ptr(), self.scratch
         return ws
 
@@ -305,8 +310,7 @@ def layer_norm_vjp(grad_y, x, weight, mean, rstd, dim=-1, weight_grad=True, bias
     c = _Prepared(x, dim, 0.0, weight, None, (grad_y, "grad_y"), (None, "x"))
     _check_statistics(x, c.stats, mean, rstd)
     gx = c.like(x)
-    gw = c.vector(x) if weight_grad else None
-    gb = c.vector(x) if bias_grad else None
+    gw, gb = c.vectors(x, weight, weight_grad, bias_grad)
     with _On(x):
         ws = c.workspace(x, weight_grad or bias_grad)
         _b.gleam_layer_norm_vjp(grad_y, x, weight, mean, rstd, gx, gw, gb, c.dims)
@@ -384,8 +388,7 @@ def dropout_add_layer_norm_vjp(grad_y, grad_total, total, weight, mean, rstd, p,
     _check_statistics(total, c.stats, mean, rstd)
     args = _drop_args(total, p, seed, offset, step)
     gx, gr = c.like(total), c.like(total)
-    gw = c.vector(total) if weight_grad else None
-    gb = c.vector(total) if bias_grad else None
+    gw, gb = c.vectors(total, weight, weight_grad, bias_grad)
     with _On(total):
         ws = c.workspace(total, weight_grad or bias_grad)
         _b.gleam_dropout_add_layer_norm_vjp(grad_y, grad_total, total, weight, mean, rstd, gx, gr, gw, gb, args, c.dims)

@@ -49,16 +49,22 @@ struct RowPlan {
 };
 static RowPlan row_plan(const Args& a) {
     RowPlan p{};
-    constexpr int V = VEC<T>, ITEMS = ROW_ITEMS<T>;
+    constexpr int V = VEC<T>, ITEMS = ROW_ITEMS<T, 32>, SHARED_ITEMS = ROW_ITEMS<T, 0>;
     p.edges = !a.aligned || a.features % V != 0;
     const long long pieces = p.edges ? (a.features + 2 * (V - 1)) / V : a.features / V;
-    if (pieces > 32ll * ITEMS * ROW_BLOCK_WARPS) return p;
+    if (pieces > SHARED_ITEMS * ROW_BLOCK_MOST) return p;
     p.fits = true;
-    p.warps = (int)((pieces + 32 * ITEMS - 1) / (32 * ITEMS));
-    p.team = p.warps > 1 ? 0 : 2;
-    while (p.team && pieces > p.team * ITEMS) p.team *= 2;
-    p.teams = p.team ? ROW_BLOCK / p.team : ROW_BLOCK_WARPS / p.warps;
-    p.threads = p.team ? ROW_BLOCK : p.teams * p.warps * 32;
+    p.warps = 1;
+    if (pieces > 32 * ITEMS) {
+        p.warps = (int)((pieces + 32 * SHARED_ITEMS - 1) / (32 * SHARED_ITEMS));
+        p.teams = p.warps > ROW_BLOCK / 32 ? 1 : ROW_BLOCK / 32 / p.warps;
+        p.threads = p.teams * p.warps * 32;
+        return p;
+    }
+    p.team = 2;
+    while (pieces > p.team * ITEMS) p.team *= 2;
+    p.teams = ROW_BLOCK / p.team;
+    p.threads = ROW_BLOCK;
     return p;
 }
 // Blocks of the launch, of which `most` are on the GPU at once.
@@ -78,17 +84,22 @@ template <auto KERNEL> static PerDevice kernel_state;
 
 template <bool VJP, bool TAIL, bool EDGES, int TEAM>
 static cudaError_t launch_rows(const Args& a, const RowPlan& p, int* blocks, cudaStream_t s) {
-    constexpr size_t PER_THREAD = sizeof(T) * ROW_FEATURES * ((VJP ? 2 : 1) + TAIL) * row_stages(VJP, TAIL, sizeof(T)), SM_BYTES = 227 * 1024;
+    constexpr int FEATURES = row_features(TEAM);
+    constexpr size_t PER_THREAD = sizeof(T) * FEATURES * ((VJP ? 2 : 1) + TAIL) * row_stages(VJP, TAIL, sizeof(T), TEAM), SM_BYTES = 227 * 1024;
     constexpr auto KERNEL = [] { if constexpr (VJP) return row_team_vjp<T, TEAM, EDGES, TAIL>; else return row_team_forward<T, TEAM, EDGES, TAIL>; }();
-    const size_t weights = (VJP ? 1 : 2) * sizeof(float) * ROW_FEATURES * (p.team ? p.team : p.warps * 32);
+    const size_t weights = (VJP ? 1 : 2) * sizeof(float) * FEATURES * (p.team ? p.team : p.warps * 32);
     // a block of several teams adds up their weights' gradients
-    const size_t sums = VJP && p.teams > 1 ? 2 * sizeof(float) * ROW_FEATURES * p.threads : 0;
+    const size_t sums = VJP && p.teams > 1 ? 2 * sizeof(float) * FEATURES * p.threads : 0;
     size_t shared = EXCHANGE_BYTES + PER_THREAD * p.threads + weights;
     if (shared < sums) shared = sums;
     const cudaError_t e = ensure_smem(KERNEL, SM_BYTES, kernel_state<KERNEL>);
     if (e != cudaSuccess) return e;
-    const int fit = (int)(SM_BYTES / (shared + 1024)), resident = fit < 1 ? 1 : fit < row_blocks(VJP) ? fit : row_blocks(VJP);
-    *blocks = row_grid(a, p, VJP, SMS * resident);
+    // blocks that are resident at once: what registers and shared memory hold
+    int resident = row_blocks(VJP, TEAM) * row_block(TEAM) / p.threads;
+    const int fit = (int)(SM_BYTES / (shared + 1024));
+    if (resident > fit) resident = fit;
+    if (VJP && resident > PARTS_MOST / SMS) resident = PARTS_MOST / SMS;
+    *blocks = row_grid(a, p, VJP, SMS * (resident > 0 ? resident : 1));
     PRIOR_LAUNCH(KERNEL, dim3((unsigned)*blocks), dim3(p.threads), shared, s, a, p.warps, p.teams);
     return cudaSuccess;
 }

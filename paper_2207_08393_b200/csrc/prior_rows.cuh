@@ -21,8 +21,12 @@ namespace prior {
 using True = std::true_type;
 using False = std::false_type;
 
-constexpr int ROW_BLOCK = 256, ROW_BLOCK_WARPS = ROW_BLOCK / 32, ROW_FEATURES = 32;    // threads a block, features a thread at most
-template <class T> constexpr int ROW_ITEMS = ROW_FEATURES / VEC<T>;                     // pieces a thread
+constexpr int ROW_BLOCK = 256, ROW_BLOCK_MOST = 512;     // threads a block: of teams inside a warp, and at most (one long row)
+// Features a thread: 32 in a team inside a warp, 16 where warps share a row.  There the latency of a row's steps counts, and twice
+// the warps on an SM hide it (2049 rows of 4096 and 4099 in float32, forward and VJP, with 32: 12.9 + 28.9 and 27.2 + 55.2 us).
+constexpr int row_features(int team) { return team ? 32 : 16; }
+constexpr int row_block(int team) { return team ? ROW_BLOCK : ROW_BLOCK_MOST; }
+template <class T, int TEAM> constexpr int ROW_ITEMS = row_features(TEAM) / VEC<T>;     // pieces a thread
 
 __device__ __forceinline__ void team_barrier(int team, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "r"(threads) : "memory"); }
 __device__ __forceinline__ void copy16(uint32_t to, const void* from) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory"); }
@@ -44,7 +48,7 @@ __device__ __forceinline__ float inverse_root(float x) {
 // neighbouring pieces, so that only the first and the last one meet the ends of the row; the others are `full` and check nothing.
 template <class T, int TEAM, bool EDGES>
 struct RowPlace {
-    static constexpr int V = VEC<T>, ITEMS = ROW_ITEMS<T>, STEP = TEAM ? TEAM : 32;
+    static constexpr int V = VEC<T>, ITEMS = ROW_ITEMS<T, TEAM>, STEP = TEAM ? TEAM : 32;
     int width, team, t, phase;           // threads of a team, team in the block, thread in the team, where its rows begin in a piece
     int first_piece, first;              // the thread's first piece and the feature that it begins with
     bool full;
@@ -152,14 +156,14 @@ struct Exchange {
         return set;
     }
 };
-constexpr int EXCHANGE_BYTES = 2 * ROW_BLOCK_WARPS * sizeof(float4);
+constexpr int EXCHANGE_BYTES = 2 * ROW_BLOCK_MOST / 32 * sizeof(float4);
 
 // A thread's pieces of the rows to come, in shared memory: copied there by the thread itself, STAGES - 1 rows ahead, and read
 // by it alone, so that no barrier is needed.  (Rows of 1024 in bf16, forward and VJP, teams of four warps: 216 us with loads into
 // registers, 177 with the ring.)
 template <class T, int TEAM, int ARRAYS, int STAGES, bool EDGES>
 struct Ring {
-    static constexpr int ITEMS = ROW_ITEMS<T>;
+    static constexpr int ITEMS = ROW_ITEMS<T, TEAM>;
     Pack<T>* base;
     uint32_t address;
     int threads;
@@ -195,18 +199,19 @@ struct Ring {
     }
 };
 
-// Blocks on an SM (registers) and rows in the ring: four, or as many as the shared memory holds beside the weights.
-constexpr int row_blocks(bool vjp) { return vjp ? 1 : 3; }
-constexpr int row_stages(bool vjp, bool tail, int size) {
-    const int stage = ROW_BLOCK * ROW_FEATURES * size * ((vjp ? 2 : 1) + tail), room = 192 * 1024 / row_blocks(vjp);
-    return room / stage >= 4 ? 4 : room / stage >= 3 ? 3 : 2;
+// Blocks of row_block(team) threads on an SM (registers), and rows in the ring: four, or as many as the shared memory holds beside
+// the weights; two where warps share a row, for two blocks.
+constexpr int row_blocks(bool vjp, int team) { return team ? (vjp ? 1 : 3) : vjp ? 1 : 2; }
+constexpr int row_stages(bool vjp, bool tail, int size, int team) {
+    const int stage = ROW_BLOCK * row_features(team) * size * ((vjp ? 2 : 1) + tail), room = 192 * 1024 / row_blocks(vjp, team);
+    return !team ? 2 : room / stage >= 4 ? 4 : room / stage >= 3 ? 3 : 2;
 }
 
 template <class T, int TEAM, bool EDGES, bool TAIL>
-__global__ void __launch_bounds__(ROW_BLOCK, row_blocks(false)) row_team_forward(const __grid_constant__ Args a, int warps, int teams) {
+__global__ void __launch_bounds__(row_block(TEAM), row_blocks(false, TEAM)) row_team_forward(const __grid_constant__ Args a, int warps, int teams) {
     grid_dependency_wait();
     extern __shared__ __align__(16) float shared[];
-    constexpr int V = VEC<T>, ITEMS = ROW_ITEMS<T>, STAGES = row_stages(false, TAIL, sizeof(T)), ARRAYS = TAIL ? 2 : 1;
+    constexpr int V = VEC<T>, ITEMS = ROW_ITEMS<T, TEAM>, STAGES = row_stages(false, TAIL, sizeof(T), TEAM), ARRAYS = TAIL ? 2 : 1;
     using Place = RowPlace<T, TEAM, EDGES>;
     const Place at(a, warps, teams);
     Exchange exchange(shared, warps, at.team, at.t);
@@ -318,10 +323,10 @@ __global__ void __launch_bounds__(ROW_BLOCK, row_blocks(false)) row_team_forward
 }
 
 template <class T, int TEAM, bool EDGES, bool TAIL>
-__global__ void __launch_bounds__(ROW_BLOCK, row_blocks(true)) row_team_vjp(const __grid_constant__ Args a, int warps, int teams) {
+__global__ void __launch_bounds__(row_block(TEAM), row_blocks(true, TEAM)) row_team_vjp(const __grid_constant__ Args a, int warps, int teams) {
     grid_dependency_wait();
     extern __shared__ __align__(16) float shared[];
-    constexpr int V = VEC<T>, ITEMS = ROW_ITEMS<T>, STAGES = row_stages(true, TAIL, sizeof(T)), ARRAYS = TAIL ? 3 : 2;
+    constexpr int V = VEC<T>, ITEMS = ROW_ITEMS<T, TEAM>, STAGES = row_stages(true, TAIL, sizeof(T), TEAM), ARRAYS = TAIL ? 3 : 2;
     using Place = RowPlace<T, TEAM, EDGES>;
     const Place at(a, warps, teams);
     Exchange exchange(shared, warps, at.team, at.t);

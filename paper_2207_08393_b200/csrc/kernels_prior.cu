@@ -148,7 +148,7 @@ static cudaError_t launch_maps(const Args& a, const MapPlan& p, int* blocks, cud
     if (e != cudaSuccess) return e;
     const long long tiles = (a.outer * a.inner / VP + 31) / 32;
     int fit = (int)(SM_BYTES / (p.shared + 1024));
-    const int threads = p.warps * 32, held = (ITEMS <= 8 ? 1024 : 512) / threads;     // threads that the registers of an SM hold
+    const int threads = p.warps * 32, held = (!VJP && ITEMS <= 16 ? 1024 : 512) / threads;     // threads that the registers of an SM hold
     if (fit > held) fit = held;
     const long long most = (long long)SMS * (fit < 1 ? 1 : fit);
     *blocks = (int)(tiles < most ? tiles : most);

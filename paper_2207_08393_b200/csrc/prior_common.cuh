@@ -129,9 +129,9 @@ struct Mask {
         const unsigned long long step = a.step ? *a.step : 0ull;
         s0 = (uint32_t)step; s1 = (uint32_t)(step >> 32);
     }
-    __device__ __forceinline__ uint4 words(uint64_t block) const {
-        block += a.offset;
-        uint32_t c0 = (uint32_t)block, c1 = (uint32_t)(block >> 32), c2 = s0, c3 = s1;
+    __device__ __forceinline__ uint64_t counter(uint64_t block) const { return block + a.offset; }       // of elements 4 * block on
+    __device__ __forceinline__ uint4 words(uint64_t counter) const {
+        uint32_t c0 = (uint32_t)counter, c1 = (uint32_t)(counter >> 32), c2 = s0, c3 = s1;
 #pragma unroll
         for (int r = 0; r < 10; ++r) {
             const uint64_t p0 = (uint64_t)c0 * 0xD2511F53u, p1 = (uint64_t)c2 * 0xCD9E8D57u;
@@ -143,14 +143,14 @@ struct Mask {
     __device__ __forceinline__ bool dropped(const uint4& w, int lane) const {
         return (lane == 0 ? w.x : lane == 1 ? w.y : lane == 2 ? w.z : w.w) <= a.last;
     }
-    // v = r + s v [s v] for the elements that are kept, r [0] for the others; the first one is element 4 * block
+    // v = r + s v [s v] for the elements that are kept, r [0] for the others; the first four have this counter
     template <bool RES, bool DROP, int N>
-    __device__ __forceinline__ void apply(uint64_t block, Two (&v)[N], const Two (&r)[N]) const {
+    __device__ __forceinline__ void apply(uint64_t counter, Two (&v)[N], const Two (&r)[N]) const {
         const Two scale(a.scale);
 #pragma unroll
         for (int q = 0; q < N / 2; ++q) {
             uint4 w;
-            if (DROP) w = words(block + q);
+            if (DROP) w = words(counter + q);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 Two& x = v[2 * q + h];
@@ -159,7 +159,7 @@ struct Mask {
             }
         }
     }
-    __device__ __forceinline__ bool dropped_at(uint64_t i) const { return dropped(words(i >> 2), (int)(i & 3u)); }
+    __device__ __forceinline__ bool dropped_at(uint64_t i) const { return dropped(words(counter(i >> 2)), (int)(i & 3u)); }
 };
 
 // Sums of a pair over the block in a fixed order, in every thread.  One barrier before and one after the exchange.

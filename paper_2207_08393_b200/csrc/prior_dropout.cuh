@@ -42,7 +42,7 @@ __global__ void __launch_bounds__(DROP_THREADS) dropout_kernel(const __grid_cons
         Two v[V / 2], r[V / 2];
         unpack(xv, v);
         if (RES) unpack(rv, r);
-        mask.apply<RES, DROP>((uint64_t)(i >> 2), v, r);
+        mask.apply<RES, DROP>(mask.counter((uint64_t)(i >> 2)), v, r);
         store_pack(out + (o * a.pout + e), pack<T>(v));
         return;
     }
@@ -51,7 +51,7 @@ __global__ void __launch_bounds__(DROP_THREADS) dropout_kernel(const __grid_cons
 #pragma unroll 1
         for (int q = 0; q < V / 4; ++q) {
             uint4 words = make_uint4(0u, 0u, 0u, 0u);
-            if (DROP) words = mask.words((uint64_t)(i >> 2) + q);
+            if (DROP) words = mask.words(mask.counter((uint64_t)(i >> 2) + q));
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 if (i + 4 * q + j >= n) return;

@@ -47,13 +47,21 @@ __device__ __forceinline__ Piece<T, VP> piece_of(const Two (&v)[PAIRS<VP>]) {
     }
     return p;
 }
-// Mask::apply for the VP elements from number i on, which share a counter (VP = 8: two).
+// Where the elements of a piece stand in the mask: by counter where a piece begins one (VP >= 4, inner a multiple of four), else
+// by element.
+template <int VP>
+struct MaskPlace {
+    uint64_t at;
+    __device__ __forceinline__ MaskPlace(const Args& a, uint64_t element) : at(VP >= 4 ? (element >> 2) + a.offset : element) {}
+    __device__ __forceinline__ void next(const Args& a) { at += VP >= 4 ? a.inner >> 2 : a.inner; }
+};
+// v = r + s v [s v] for the kept elements of a piece, r [0] for the others.
 template <bool RES, int VP>
-__device__ __forceinline__ void drop_piece(const Mask& mask, uint64_t i, Two (&v)[PAIRS<VP>], const Two (&r)[PAIRS<VP>]) {
-    if constexpr (VP >= 4) mask.apply<RES, true>(i >> 2, v, r);
+__device__ __forceinline__ void drop_piece(const Mask& mask, const MaskPlace<VP>& place, Two (&v)[PAIRS<VP>], const Two (&r)[PAIRS<VP>]) {
+    if constexpr (VP >= 4) mask.apply<RES, true>(place.at, v, r);
     else {
-        const uint4 w = mask.words(i >> 2);
-        const int at = (int)(i & 3u);
+        const uint4 w = mask.words(mask.counter(place.at >> 2));
+        const int at = (int)(place.at & 3u);
         const Two kept = RES ? fma2(v[0], Two(mask.a.scale), r[0]) : v[0] * Two(mask.a.scale), gone = RES ? r[0] : Two(0.f);
         v[0] = Two(mask.dropped(w, at) ? gone.lo() : kept.lo(), VP == 2 && mask.dropped(w, at + 1) ? gone.hi() : kept.hi());
     }
@@ -65,19 +73,21 @@ constexpr int MAP_TILE_WARPS = 16;                       // warps of a block at 
 template <class T, int VP, int ITEMS, int ARRAYS>
 struct MapTile {
     using P = Piece<T, VP>;
-    P* slots;                            // this thread's pieces: (array, item), a block's width apart
+    P* slots;                            // this thread's pieces, a warp's width apart: the warps' shares lie one behind another
+    uint32_t address;
     int lane, warp, first, items;        // first feature and number of features of the warp
     long long pieces, o, k;              // pieces of an array; slice and position in it of this lane's piece of the tile
     bool live;
     __device__ __forceinline__ MapTile(const Args& a, void* shared) {
-        slots = static_cast<P*>(shared) + threadIdx.x;
         lane = threadIdx.x & 31; warp = threadIdx.x >> 5;
+        slots = static_cast<P*>(shared) + warp * (ARRAYS * ITEMS * 32) + lane;
+        address = (uint32_t)__cvta_generic_to_shared(slots);
         first = warp * ITEMS;
         items = min(ITEMS, (int)a.features - first);
         pieces = a.outer * a.inner / VP;
         o = k = 0; live = false;
     }
-    __device__ __forceinline__ P& slot(int array, int j) const { return slots[(array * ITEMS + j) * (int)blockDim.x]; }
+    __device__ __forceinline__ P& slot(int array, int j) const { return slots[(array * ITEMS + j) * 32]; }
     __device__ __forceinline__ void go(long long tile, const Args& a) {
         const long long p = tile * 32 + lane, row = a.inner / VP;
         live = p < pieces;
@@ -100,7 +110,7 @@ struct MapTile {
 #pragma unroll
             for (int j = 0; j < ITEMS; ++j, p += a.inner) {
                 if (!has<FULL>(j)) continue;
-                const uint32_t to = (uint32_t)__cvta_generic_to_shared(&slot(array, j));
+                const uint32_t to = address + (array * ITEMS + j) * 32 * (uint32_t)sizeof(P);
                 if constexpr (sizeof(P) == 16) copy16(to, p);
                 else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(p), "n"(sizeof(P) < 4 ? 4 : (int)sizeof(P)) : "memory");
             }
@@ -152,7 +162,7 @@ __device__ __forceinline__ void map_exchange(float* sums, int warps, int lane, i
 constexpr size_t map_exchange_floats(int vp, int warps) { return (size_t)(2 * warps + 2) * 32 * vp; }
 
 template <class T, int VP, int ITEMS, bool TAIL>
-__global__ void __launch_bounds__(MAP_TILE_WARPS * 32, ITEMS <= 8 ? 2 : 1) map_tile_forward(const __grid_constant__ Args a) {
+__global__ void __launch_bounds__(MAP_TILE_WARPS * 32, ITEMS <= 16 ? 2 : 1) map_tile_forward(const __grid_constant__ Args a) {
     grid_dependency_wait();
     extern __shared__ __align__(16) float shared[];
     const int warps = blockDim.x >> 5, n = (int)a.features;
@@ -190,13 +200,13 @@ __global__ void __launch_bounds__(MAP_TILE_WARPS * 32, ITEMS <= 8 ? 2 : 1) map_t
 #pragma unroll
         for (int i = 0; i < PAIRS<VP>; ++i) pivot[i] = s[i] = q[i] = Two(0.f);
         T* sum = TAIL ? t.at(a.out2, a.pout2, a) : nullptr;
-        uint64_t element = TAIL ? t.element(a) : 0;
+        MaskPlace<VP> place(a, TAIL ? t.element(a) : 0);
         auto value = [&](int j, Two (&v)[PAIRS<VP>]) {
             unpack<T, VP>(t.slot(0, j), v);
             if (!TAIL) return;
             Two r[PAIRS<VP>];
             unpack<T, VP>(t.slot(1, j), r);
-            if (a.dropping) drop_piece<true, VP>(mask, element, v, r);
+            if (a.dropping) drop_piece<true, VP>(mask, place, v, r);
             else {
 #pragma unroll
                 for (int i = 0; i < PAIRS<VP>; ++i) v[i] = v[i] + r[i];
@@ -205,7 +215,7 @@ __global__ void __launch_bounds__(MAP_TILE_WARPS * 32, ITEMS <= 8 ? 2 : 1) map_t
             unpack<T, VP>(stored, v);
             t.slot(0, j) = stored;
             *reinterpret_cast<Piece<T, VP>*>(sum) = stored;
-            sum += a.inner; element += a.inner;
+            sum += a.inner; place.next(a);
         };
         if (t.template has<FULL>(0)) {
             value(0, pivot);
@@ -344,7 +354,7 @@ __global__ void __launch_bounds__(MAP_TILE_WARPS * 32, 1) map_tile_vjp(const __g
         constexpr bool FULL = decltype(whole_tile)::value;
         T* out = t.at(a.out, a.pout, a);
         T* out2 = TAIL ? t.at(a.out2, a.pout2, a) : nullptr;
-        uint64_t element = TAIL ? t.element(a) : 0;
+        MaskPlace<VP> place(a, TAIL ? t.element(a) : 0);
 #pragma unroll 2
         for (int j = 0; j < (FULL ? ITEMS : t.live ? t.items : 0); ++j, out += a.inner) {
             Two g[PAIRS<VP>], v[PAIRS<VP>];
@@ -361,8 +371,8 @@ __global__ void __launch_bounds__(MAP_TILE_WARPS * 32, 1) map_tile_vjp(const __g
                     for (int i = 0; i < PAIRS<VP>; ++i) v[i] = v[i] + g[i];
                 }
                 *reinterpret_cast<Piece<T, VP>*>(out2) = piece_of<T, VP>(v);
-                if (a.dropping) drop_piece<false, VP>(mask, element, v, v);
-                out2 += a.inner; element += a.inner;
+                if (a.dropping) drop_piece<false, VP>(mask, place, v, v);
+                out2 += a.inner; place.next(a);
             }
             *reinterpret_cast<Piece<T, VP>*>(out) = piece_of<T, VP>(v);
         }

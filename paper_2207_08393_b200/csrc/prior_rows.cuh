@@ -164,14 +164,13 @@ constexpr int EXCHANGE_BYTES = 2 * ROW_BLOCK_MOST / 32 * sizeof(float4);
 template <class T, int TEAM, int ARRAYS, int STAGES, bool EDGES>
 struct Ring {
     static constexpr int ITEMS = ROW_ITEMS<T, TEAM>;
-    Pack<T>* base;
+    Pack<T>* base;                       // the warps' shares lie one behind another, their threads' pieces a warp's width apart
     uint32_t address;
-    int threads;
-    __device__ __forceinline__ explicit Ring(void* shared) : threads(TEAM ? ROW_BLOCK : (int)blockDim.x) {
-        base = static_cast<Pack<T>*>(shared) + threadIdx.x;
+    __device__ __forceinline__ explicit Ring(void* shared) {
+        base = static_cast<Pack<T>*>(shared) + (threadIdx.x >> 5) * (STAGES * ARRAYS * ITEMS * 32) + (threadIdx.x & 31);
         address = (uint32_t)__cvta_generic_to_shared(base);
     }
-    __device__ __forceinline__ int place(int stage, int array, int k) const { return ((stage * ARRAYS + array) * ITEMS + k) * threads; }
+    static __device__ __forceinline__ int place(int stage, int array, int k) { return ((stage * ARRAYS + array) * ITEMS + k) * 32; }
     __device__ __forceinline__ Pack<T> get(int stage, int array, int k) const { return base[place(stage, array, k)]; }
     // The pieces of row r of an array.  A piece over the row's ends is copied whole, with its neighbours' elements, where the
     // array has them.
@@ -217,7 +216,7 @@ __global__ void __launch_bounds__(row_block(TEAM), row_blocks(false, TEAM)) row_
     Exchange exchange(shared, warps, at.team, at.t);
     float* room = shared + EXCHANGE_BYTES / 4;
     Ring<T, TEAM, ARRAYS, STAGES, EDGES> ring(room);
-    room += ARRAYS * ITEMS * STAGES * 4 * ring.threads;
+    room += ARRAYS * ITEMS * STAGES * 4 * blockDim.x;
     const Mask mask(a);
     const int n = (int)a.features;
     const bool packed = a.aligned;
@@ -250,7 +249,7 @@ __global__ void __launch_bounds__(row_block(TEAM), row_blocks(false, TEAM)) row_
         copies_wait<STAGES - 1>();
         Two v[ITEMS][V / 2];
         T* sum = TAIL ? static_cast<T*>(a.out2) + (r * a.pout2 + at.first) : nullptr;
-        const uint64_t block = TAIL ? (uint64_t)((r * n - at.phase) / 4) + (uint32_t)(at.first_piece * (V / 4)) : 0;
+        const uint64_t counter = TAIL ? mask.counter((uint64_t)((r * n - at.phase) >> 2) + (uint32_t)(at.first_piece * (V / 4))) : 0;
 #pragma unroll
         for (int k = 0; k < ITEMS; ++k) {
             const int c = at.feature(k);
@@ -258,7 +257,7 @@ __global__ void __launch_bounds__(row_block(TEAM), row_blocks(false, TEAM)) row_
             if (TAIL) {
                 Two rs[V / 2];
                 unpack(ring.get(stage, 1, k), rs);
-                if (a.dropping) mask.apply<true, true>(block + (uint32_t)(k * Place::STEP * (V / 4)), v[k], rs);
+                if (a.dropping) mask.apply<true, true>(counter + (uint32_t)(k * Place::STEP * (V / 4)), v[k], rs);
                 else mask.apply<true, false>(0, v[k], rs);
                 const Pack<T> stored = pack<T>(v[k]);
                 unpack(stored, v[k]);
@@ -332,7 +331,7 @@ __global__ void __launch_bounds__(row_block(TEAM), row_blocks(true, TEAM)) row_t
     Exchange exchange(shared, warps, at.team, at.t);
     float* room = shared + EXCHANGE_BYTES / 4;
     Ring<T, TEAM, ARRAYS, STAGES, EDGES> ring(room);
-    room += ARRAYS * ITEMS * STAGES * 4 * ring.threads;
+    room += ARRAYS * ITEMS * STAGES * 4 * blockDim.x;
     const Mask mask(a);
     const int n = (int)a.features;
     const bool packed = a.aligned, added = TAIL && a.gsum;
@@ -398,7 +397,7 @@ __global__ void __launch_bounds__(row_block(TEAM), row_blocks(true, TEAM)) row_t
         const float c1 = -rstd * (s1 * inv_count), c2 = -rstd * (s2 * inv_count);
         T* out = static_cast<T*>(a.out) + (r * a.pout + at.first);
         T* out2 = TAIL ? static_cast<T*>(a.out2) + (r * a.pout2 + at.first) : nullptr;
-        const uint64_t block = TAIL ? (uint64_t)((r * n - at.phase) / 4) + (uint32_t)(at.first_piece * (V / 4)) : 0;
+        const uint64_t counter = TAIL ? mask.counter((uint64_t)((r * n - at.phase) >> 2) + (uint32_t)(at.first_piece * (V / 4))) : 0;
 #pragma unroll
         for (int k = 0; k < ITEMS; ++k) {
             const int c = at.feature(k);
@@ -415,7 +414,7 @@ __global__ void __launch_bounds__(row_block(TEAM), row_blocks(true, TEAM)) row_t
                     for (int j = 0; j < V / 2; ++j) v[j] = v[j] + g[j];
                 }
                 store_piece<T, FULL, EDGES>(out2 + k * Place::STEP * V, c, n, packed, pack<T>(v));
-                if (a.dropping) mask.apply<false, true>(block + (uint32_t)(k * Place::STEP * (V / 4)), v, v);
+                if (a.dropping) mask.apply<false, true>(counter + (uint32_t)(k * Place::STEP * (V / 4)), v, v);
             }
             store_piece<T, FULL, EDGES>(out + k * Place::STEP * V, c, n, packed, pack<T>(v));
         }

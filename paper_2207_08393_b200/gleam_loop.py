@@ -16,6 +16,7 @@ import torch
 import torch.nn as nn
 
 from . import binding as _b
+from . import prior_ops as _p
 
 
 class _DCFunction(torch.autograd.Function):
@@ -80,23 +81,45 @@ class DataConsistencyStep:
 
 
 class ResidualPrior(nn.Module):
-    """The learned proximal block: residual blocks of two (ReLU -> 3x3 convolution) pairs, no normalisation,
-    on the two real channels of a 2-D image (frames are folded into the batch)."""
+    """The learned proximal block: residual blocks of two (ReLU -> 3x3 convolution) pairs on the two real channels of a 2-D
+    image (frames are folded into the batch).  As the paper has it there is no normalisation.
 
-    def __init__(self, features=16, blocks=2):
+    For deeper priors, ``norm`` puts a layer norm over the features of every voxel in front of each block and of the last
+    convolution, and ``dropout`` regularises what a block adds (while training).  Residual add, dropout and the next block's norm
+    are then one operator of the library (``prior_ops.dropout_add_layer_norm``), which stores no mask: the backward pass
+    draws it again from ``generator`` (a ``prior_ops.DropoutGenerator``, shared by all priors of a network)."""
+
+    def __init__(self, features=16, blocks=2, norm=False, dropout=0.0, generator=None):
         super().__init__()
+        if not 0.0 <= dropout <= 1.0:
+            raise ValueError("dropout = %r is not a probability" % (dropout,))
+        if dropout > 0.0 and generator is None:
+            raise ValueError("dropout needs a generator")
         self.head = nn.Conv2d(2, features, 3, padding=1)
         self.blocks = nn.ModuleList([
             nn.Sequential(nn.ReLU(), nn.Conv2d(features, features, 3, padding=1),
                           nn.ReLU(), nn.Conv2d(features, features, 3, padding=1)) for _ in range(blocks)])
         self.tail = nn.Conv2d(features, 2, 3, padding=1)
+        self.dropout, self.generator = float(dropout), generator
+        self.norm_weight = self.norm_bias = None
+        if norm:
+            self.norm_weight = nn.ParameterList([nn.Parameter(torch.ones(features)) for _ in range(blocks + 1)])
+            self.norm_bias = nn.ParameterList([nn.Parameter(torch.zeros(features)) for _ in range(blocks + 1)])
 
     def forward(self, x_ch):                      # (B, 2, T, 1, n1, n2)
         B, _, T, n0, n1, n2 = x_ch.shape
         h = x_ch.permute(0, 2, 3, 1, 4, 5).reshape(B * T * n0, 2, n1, n2)
         f = self.head(h)
-        for blk in self.blocks:
-            f = f + blk(f)
+        p = self.dropout if self.training else 0.0
+        if self.norm_weight is not None:
+            w, b = self.norm_weight, self.norm_bias
+            y = _p.layer_norm(f, w[0], b[0], dim=1)
+            for k, blk in enumerate(self.blocks):
+                y, f = _p.dropout_add_layer_norm(blk(y), f, w[k + 1], b[k + 1], p, self.generator, dim=1)
+            f = y
+        else:
+            for blk in self.blocks:
+                f = _p.dropout(blk(f), p, self.generator, residual=f) if p > 0.0 else f + blk(f)
         h = h + self.tail(f)
         return h.reshape(B, T, n0, 2, n1, n2).permute(0, 3, 1, 2, 4, 5).contiguous()
 
@@ -104,9 +127,9 @@ class ResidualPrior(nn.Module):
 class GleamModule(nn.Module):
     """`iterations` unrolled steps x <- f_theta_i(DC(x)) that are trained together (one greedy module)."""
 
-    def __init__(self, iterations=1, features=16, blocks=2):
+    def __init__(self, iterations=1, features=16, blocks=2, norm=False, dropout=0.0, generator=None):
         super().__init__()
-        self.priors = nn.ModuleList([ResidualPrior(features, blocks) for _ in range(iterations)])
+        self.priors = nn.ModuleList([ResidualPrior(features, blocks, norm, dropout, generator) for _ in range(iterations)])
 
     def forward(self, x_ch, step: DataConsistencyStep):
         for prior in self.priors:

@@ -116,6 +116,8 @@ def _same(x, t, view, dim, what):
 
 def _match(x, t, dim):
     """``t`` itself if the calls take it next to ``x``, else a copy in x's order (cotangents come in any order)."""
+    if t.shape != x.shape or (t.is_contiguous() and x.is_contiguous()):
+        return t
     view = _view(x, dim)
     try:
         v = _view(t, dim)
@@ -463,6 +465,7 @@ class _Dropout(torch.autograd.Function):
 class _Tail(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, residual, weight, bias, p, seed, offset, eps, dim, step):
+        residual = _match(x, residual, _features_axis(x, dim))
         y, total, mean, rstd = dropout_add_layer_norm_forward(x, residual, weight, bias, p, seed, offset, eps, dim, step)
         ctx.save_for_backward(total, weight, mean, rstd, step)
         ctx.args, ctx.dim = (p, seed, offset), dim

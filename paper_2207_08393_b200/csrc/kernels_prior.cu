@@ -121,7 +121,7 @@ static cudaError_t launch_rows(const Args& a, const RowPlan& p, bool tail, int* 
 }
 
 // How maps are dealt to tiles (prior_maps.cuh); vp = 0 where the features of a tile do not fit.
-struct MapPlan { int vp, items, warps; size_t shared; };
+struct MapPlan { int vp, items, warps; bool spread; size_t shared; };
 static MapPlan map_plan(const Args& a, bool vjp, bool tail, std::initializer_list<std::pair<const void*, long long>> arrays) {
     MapPlan p{};
     if (a.features > 32 * MAP_TILE_WARPS) return p;
@@ -129,26 +129,30 @@ static MapPlan map_plan(const Args& a, bool vjp, bool tail, std::initializer_lis
     p.items = !vjp && a.features <= 8 * MAP_TILE_WARPS ? 8 : a.features <= 16 * MAP_TILE_WARPS ? 16 : 32;
     p.warps = (int)((a.features + p.items - 1) / p.items);
     const int copies = (vjp ? 2 : 1) + tail;
-    // pieces of 16 bytes where two tiles fit on an SM, else of 8 and 4
-    for (int vp = 16 / (int)sizeof(T); vp >= 1; vp /= 2) {
-        bool ok = a.inner % vp == 0;
-        for (const auto& v : arrays) ok = ok && (!v.first || ((uintptr_t)v.first % (vp * sizeof(T)) == 0 && (a.outer == 1 || v.second % vp == 0)));
+    auto take = [&](int vp, bool spread) {
+        bool ok = spread || a.inner % vp == 0;
+        for (const auto& v : arrays) ok = ok && (spread || !v.first || ((uintptr_t)v.first % (vp * sizeof(T)) == 0 && (a.outer == 1 || v.second % vp == 0)));
+        // two tiles on an SM, but where it would take pieces of less than 4 bytes
         const size_t bytes = sizeof(float) * (map_exchange_floats(vp, p.warps) + 2 * (size_t)p.warps * p.items) + sizeof(T) * vp * 32 * (size_t)p.warps * p.items * copies;
-        if (!ok || bytes > (vp * sizeof(T) > 4 ? 112 : 226) * 1024u) continue;
-        p.vp = vp; p.shared = bytes;
-        return p;
-    }
+        if (!ok || bytes > (vp * sizeof(T) > 4 ? 112 : 226) * 1024u) return false;
+        p.vp = vp; p.spread = spread; p.shared = bytes;
+        return true;
+    };
+    // pieces of 16 bytes, else of 8; where slices begin anywhere, four positions element by element; else smaller pieces
+    for (int vp = 16 / (int)sizeof(T); vp >= 4; vp /= 2) if (take(vp, false)) return p;
+    if (a.inner >= 128 && take(4, true)) return p;
+    for (int vp = 2; vp >= 1; --vp) if (take(vp, false)) return p;
     return p;
 }
-template <bool VJP, bool TAIL, int VP, int ITEMS>
+template <bool VJP, bool TAIL, int VP, bool SPREAD, int ITEMS>
 static cudaError_t launch_maps(const Args& a, const MapPlan& p, int* blocks, cudaStream_t s) {
-    constexpr auto KERNEL = [] { if constexpr (VJP) return map_tile_vjp<T, VP, ITEMS, TAIL>; else return map_tile_forward<T, VP, ITEMS, TAIL>; }();
+    constexpr auto KERNEL = [] { if constexpr (VJP) return map_tile_vjp<T, VP, ITEMS, TAIL, SPREAD>; else return map_tile_forward<T, VP, ITEMS, TAIL, SPREAD>; }();
     constexpr size_t SM_BYTES = 227 * 1024;
     cudaError_t e = ensure_smem(KERNEL, SM_BYTES, kernel_state<KERNEL>);
     if (e != cudaSuccess) return e;
-    const long long tiles = (a.outer * a.inner / VP + 31) / 32;
+    const long long tiles = SPREAD ? a.outer * ((a.inner + 32 * VP - 1) / (32 * VP)) : (a.outer * a.inner / VP + 31) / 32;
     int fit = (int)(SM_BYTES / (p.shared + 1024));
-    const int threads = p.warps * 32, held = (!VJP && ITEMS <= 16 ? 1024 : 512) / threads;     // threads that the registers of an SM hold
+    const int threads = p.warps * 32, held = (!VJP && ITEMS <= 16 ? 1024 : 512) / threads;     // blocks that the registers of an SM hold
     if (fit > held) fit = held;
     const long long most = (long long)SMS * (fit < 1 ? 1 : fit);
     *blocks = (int)(tiles < most ? tiles : most);
@@ -156,16 +160,16 @@ static cudaError_t launch_maps(const Args& a, const MapPlan& p, int* blocks, cud
     PRIOR_LAUNCH(KERNEL, dim3((unsigned)*blocks), dim3(threads), p.shared, s, a);
     return cudaSuccess;
 }
-template <bool VJP, bool TAIL, int VP>
+template <bool VJP, bool TAIL, int VP, bool SPREAD>
 static cudaError_t launch_maps(const Args& a, const MapPlan& p, int* blocks, cudaStream_t s) {
-    if constexpr (!VJP) if (p.items == 8) return launch_maps<VJP, TAIL, VP, 8>(a, p, blocks, s);
-    return p.items == 16 ? launch_maps<VJP, TAIL, VP, 16>(a, p, blocks, s) : launch_maps<VJP, TAIL, VP, 32>(a, p, blocks, s);
+    if constexpr (!VJP) if (p.items == 8) return launch_maps<VJP, TAIL, VP, SPREAD, 8>(a, p, blocks, s);
+    return p.items == 16 ? launch_maps<VJP, TAIL, VP, SPREAD, 16>(a, p, blocks, s) : launch_maps<VJP, TAIL, VP, SPREAD, 32>(a, p, blocks, s);
 }
 template <bool VJP, bool TAIL>
 static cudaError_t launch_maps(const Args& a, const MapPlan& p, int* blocks, cudaStream_t s) {
-    if constexpr (sizeof(T) == 2) if (p.vp == 8) return launch_maps<VJP, TAIL, 8>(a, p, blocks, s);
-    return p.vp == 4 ? launch_maps<VJP, TAIL, 4>(a, p, blocks, s) : p.vp == 2 ? launch_maps<VJP, TAIL, 2>(a, p, blocks, s)
-                                                                             : launch_maps<VJP, TAIL, 1>(a, p, blocks, s);
+    if constexpr (sizeof(T) == 2) if (p.vp == 8) return launch_maps<VJP, TAIL, 8, false>(a, p, blocks, s);
+    return p.spread ? launch_maps<VJP, TAIL, 4, true>(a, p, blocks, s) : p.vp == 4 ? launch_maps<VJP, TAIL, 4, false>(a, p, blocks, s)
+         : p.vp == 2 ? launch_maps<VJP, TAIL, 2, false>(a, p, blocks, s) : launch_maps<VJP, TAIL, 1, false>(a, p, blocks, s);
 }
 
 static cudaError_t forward(const Args& given, bool tail, cudaStream_t s) {

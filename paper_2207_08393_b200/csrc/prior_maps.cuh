@@ -1,7 +1,8 @@
 // Layer norm and the residual tail on feature maps (inner > 1): a tile of neighbouring positions with all their features in
 // shared memory, so that every array passes once.
 //
-// A tile is 32 pieces of VP positions; lane l of every warp has piece l, and each warp ITEMS neighbouring features of it.  What a
+// A tile is 32 pieces of VP positions (SPREAD: 32 VP positions of one slice, of which lane l has l, l + 32, ...: for slices that
+// begin anywhere, element by element); lane l of every warp has piece l, and each warp ITEMS neighbouring features of it.  What a
 // thread will work on it copies into shared memory itself (no barrier); the warps exchange sums for each position, which the
 // first threads of the block add up, one position each.  A VJP keeps the sums of its features' weights in registers over all of its
 // block's tiles and adds them across lanes at the end; weight_grads (prior_norm.cuh) adds up the blocks.
@@ -49,15 +50,16 @@ __device__ __forceinline__ Piece<T, VP> piece_of(const Two (&v)[PAIRS<VP>]) {
 }
 // Where the elements of a piece stand in the mask: by counter where a piece begins one (VP >= 4, inner a multiple of four), else
 // by element.
-template <int VP>
+template <int VP, bool SPREAD>
 struct MaskPlace {
+    static constexpr bool BY_COUNTER = VP >= 4 && !SPREAD;
     uint64_t at;
-    __device__ __forceinline__ MaskPlace(const Args& a, uint64_t element) : at(VP >= 4 ? (element >> 2) + a.offset : element) {}
-    __device__ __forceinline__ void next(const Args& a) { at += VP >= 4 ? a.inner >> 2 : a.inner; }
+    __device__ __forceinline__ MaskPlace(const Args& a, uint64_t element) : at(BY_COUNTER ? (element >> 2) + a.offset : element) {}
+    __device__ __forceinline__ void next(const Args& a) { at += BY_COUNTER ? a.inner >> 2 : a.inner; }
 };
 // v = r + s v [s v] for the kept elements of a piece, r [0] for the others.
 template <bool RES, int VP>
-__device__ __forceinline__ void drop_piece(const Mask& mask, const MaskPlace<VP>& place, Two (&v)[PAIRS<VP>], const Two (&r)[PAIRS<VP>]) {
+__device__ __forceinline__ void drop_piece(const Mask& mask, const MaskPlace<VP, false>& place, Two (&v)[PAIRS<VP>], const Two (&r)[PAIRS<VP>]) {
     if constexpr (VP >= 4) mask.apply<RES, true>(place.at, v, r);
     else {
         const uint4 w = mask.words(mask.counter(place.at >> 2));
@@ -67,32 +69,56 @@ __device__ __forceinline__ void drop_piece(const Mask& mask, const MaskPlace<VP>
     }
 }
 
+// The same for a tile that is spread: the positions of a feature in it are 128 neighbours from element `first` on, so its 32 lanes
+// draw a counter each and one more where the first one is shared, and find their elements' bits by ballots.  All lanes call.
+template <bool RES>
+__device__ __forceinline__ void drop_spread(const Mask& mask, uint64_t first, int lane, Two (&v)[2], const Two (&r)[2]) {
+    const int shift = (int)(first & 3u);
+    const uint64_t counter = mask.counter(first >> 2);
+    const uint4 w = mask.words(counter + (uint32_t)lane);
+    const uint32_t b0 = __ballot_sync(0xffffffffu, mask.dropped(w, 0)), b1 = __ballot_sync(0xffffffffu, mask.dropped(w, 1));
+    const uint32_t b2 = __ballot_sync(0xffffffffu, mask.dropped(w, 2)), b3 = __ballot_sync(0xffffffffu, mask.dropped(w, 3));
+    const int which = (lane + shift) & 3, from = (lane + shift) >> 2;
+    const uint32_t mine = which == 0 ? b0 : which == 1 ? b1 : which == 2 ? b2 : b3;
+    bool beyond = false;
+    if (shift) beyond = mask.dropped(mask.words(counter + 32), which);
+    auto gone = [&](int m) { return from + 8 * m < 32 ? (mine >> (from + 8 * m)) & 1u : (uint32_t)beyond; };
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const Two kept = RES ? fma2(v[i], Two(mask.a.scale), r[i]) : v[i] * Two(mask.a.scale), none = RES ? r[i] : Two(0.f);
+        v[i] = Two(gone(2 * i) ? none.lo() : kept.lo(), gone(2 * i + 1) ? none.hi() : kept.hi());
+    }
+}
+
 constexpr int MAP_TILE_WARPS = 16;                       // warps of a block at most
 
 // A block's view of its tiles.
-template <class T, int VP, int ITEMS, int ARRAYS>
+template <class T, int VP, int ITEMS, int ARRAYS, bool SPREAD>
 struct MapTile {
     using P = Piece<T, VP>;
     P* slots;                            // this thread's pieces, a warp's width apart: the warps' shares lie one behind another
     uint32_t address;
     int lane, warp, first, items;        // first feature and number of features of the warp
-    long long pieces, o, k;              // pieces of an array; slice and position in it of this lane's piece of the tile
-    bool live;
+    int live;                            // positions that this lane has: VP or none (SPREAD: any number)
+    long long tiles, o, k;               // number of tiles; slice and position in it of this lane's piece (SPREAD: of its first one)
     __device__ __forceinline__ MapTile(const Args& a, void* shared) {
         lane = threadIdx.x & 31; warp = threadIdx.x >> 5;
         slots = static_cast<P*>(shared) + warp * (ARRAYS * ITEMS * 32) + lane;
         address = (uint32_t)__cvta_generic_to_shared(slots);
         first = warp * ITEMS;
         items = min(ITEMS, (int)a.features - first);
-        pieces = a.outer * a.inner / VP;
-        o = k = 0; live = false;
+        tiles = SPREAD ? a.outer * row(a) : (a.outer * row(a) + 31) / 32;
+        o = k = 0; live = 0;
     }
+    // pieces (SPREAD: tiles) of a slice
+    __device__ __forceinline__ long long row(const Args& a) const { return SPREAD ? (a.inner + 32 * VP - 1) / (32 * VP) : a.inner / VP; }
     __device__ __forceinline__ P& slot(int array, int j) const { return slots[(array * ITEMS + j) * 32]; }
     __device__ __forceinline__ void go(long long tile, const Args& a) {
-        const long long p = tile * 32 + lane, row = a.inner / VP;
-        live = p < pieces;
-        o = !live ? 0 : pieces <= 0xffffffffll ? (uint32_t)p / (uint32_t)row : p / row;
-        k = live ? (p - o * row) * VP : 0;
+        const long long p = SPREAD ? tile : tile * 32 + lane, n = row(a), all = a.outer * n;
+        live = p < all ? VP : 0;
+        o = !live ? 0 : all <= 0xffffffffll ? (uint32_t)p / (uint32_t)n : p / n;
+        k = !live ? 0 : SPREAD ? (p - o * n) * (32 * VP) + lane : (p - o * n) * VP;
+        if (SPREAD) live = (int)max(0ll, min((long long)VP, (a.inner - k + 31) / 32));
     }
     __device__ __forceinline__ const T* at(const void* array, long long pitch, const Args& a) const {
         return static_cast<const T*>(array) + (o * pitch + first * a.inner + k);
@@ -100,30 +126,56 @@ struct MapTile {
     __device__ __forceinline__ T* at(void* array, long long pitch, const Args& a) const {
         return static_cast<T*>(array) + (o * pitch + first * a.inner + k);
     }
-    // Whether all of the warp's features and lanes are there: then nothing is checked.
-    __device__ __forceinline__ bool full() const { return items == ITEMS && __all_sync(0xffffffffu, live); }
-    template <bool FULL> __device__ __forceinline__ bool has(int j) const { return FULL || (live && j < items); }
+    // Whether all of the warp's features and positions are there: then nothing is checked.
+    __device__ __forceinline__ bool full() const { return items == ITEMS && __all_sync(0xffffffffu, live == VP); }
+    // Features that a lane passes over; in a spread tile the lanes of a warp stay together.
+    template <bool FULL> __device__ __forceinline__ int count() const { return FULL ? ITEMS : SPREAD || live ? items : 0; }
     template <bool FULL>
     __device__ __forceinline__ void fetch(int array, const void* from, long long pitch, const Args& a) const {
         const T* p = at(from, pitch, a);
-        if constexpr (sizeof(P) >= 4) {
+        if constexpr (SPREAD && sizeof(T) == 4) {
 #pragma unroll
             for (int j = 0; j < ITEMS; ++j, p += a.inner) {
-                if (!has<FULL>(j)) continue;
+                if (!FULL && j >= items) break;
+#pragma unroll
+                for (int m = 0; m < VP; ++m)
+                    if (FULL || m < live) copy_small<4>(address + (array * ITEMS + j) * 32 * (uint32_t)sizeof(P) + 4 * m, p + 32 * m);
+            }
+        } else if constexpr (!SPREAD && sizeof(P) >= 4) {
+#pragma unroll
+            for (int j = 0; j < ITEMS; ++j, p += a.inner) {
+                if (!FULL && !(live && j < items)) continue;
                 const uint32_t to = address + (array * ITEMS + j) * 32 * (uint32_t)sizeof(P);
                 if constexpr (sizeof(P) == 16) copy16(to, p);
-                else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(p), "n"(sizeof(P) < 4 ? 4 : (int)sizeof(P)) : "memory");
+                else copy_small<(int)sizeof(P)>(to, p);
             }
         } else {                                         // two bytes: too few for a copy
-            T v[ITEMS];
+            constexpr int STEP = SPREAD ? 32 : 1;
+            P v[ITEMS];
 #pragma unroll
-            for (int j = 0; j < ITEMS; ++j, p += a.inner) if (has<FULL>(j)) v[j] = *p;
+            for (int j = 0; j < ITEMS; ++j, p += a.inner)
 #pragma unroll
-            for (int j = 0; j < ITEMS; ++j) if (has<FULL>(j)) slot(array, j).e[0] = v[j];
+                for (int m = 0; m < VP; ++m) v[j].e[m] = FULL || (m < live && j < items) ? p[STEP * m] : from_float<T>(0.f);
+#pragma unroll
+            for (int j = 0; j < ITEMS; ++j) slot(array, j) = v[j];
         }
     }
-    // number of the first element of the warp's first feature
-    __device__ __forceinline__ uint64_t element(const Args& a) const { return (uint64_t)((o * a.features + first) * a.inner + k); }
+    template <bool FULL>
+    __device__ __forceinline__ void store(T* p, const P& v) const {
+        if constexpr (SPREAD) {
+#pragma unroll
+            for (int m = 0; m < VP; ++m) if (FULL || m < live) p[32 * m] = v.e[m];
+        } else {
+            *reinterpret_cast<P*>(p) = v;
+        }
+    }
+    template <int BYTES> static __device__ __forceinline__ void copy_small(uint32_t to, const void* from) {
+        asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(from), "n"(BYTES) : "memory");
+    }
+    // number of the first element of the warp's first feature (SPREAD: of lane 0)
+    __device__ __forceinline__ uint64_t element(const Args& a) const { return (uint64_t)((o * a.features + first) * a.inner + k - (SPREAD ? lane : 0)); }
+    // position of number m of this lane, in the arrays of statistics
+    __device__ __forceinline__ long long position(int m, const Args& a) const { return o * a.inner + k + (SPREAD ? 32 * m : m); }
 };
 
 // Rounding can leave a sum of squares below zero; a NaN stays.
@@ -161,7 +213,7 @@ __device__ __forceinline__ void map_exchange(float* sums, int warps, int lane, i
 // Floats of the exchange.
 constexpr size_t map_exchange_floats(int vp, int warps) { return (size_t)(2 * warps + 2) * 32 * vp; }
 
-template <class T, int VP, int ITEMS, bool TAIL>
+template <class T, int VP, int ITEMS, bool TAIL, bool SPREAD>
 __global__ void __launch_bounds__(MAP_TILE_WARPS * 32, ITEMS <= 16 ? 2 : 1) map_tile_forward(const __grid_constant__ Args a) {
     grid_dependency_wait();
     extern __shared__ __align__(16) float shared[];
@@ -169,17 +221,16 @@ __global__ void __launch_bounds__(MAP_TILE_WARPS * 32, ITEMS <= 16 ? 2 : 1) map_
     float* sums = shared;
     float* wt = sums + map_exchange_floats(VP, warps);
     float* bs = wt + warps * ITEMS;
-    MapTile<T, VP, ITEMS, TAIL ? 2 : 1> t(a, bs + warps * ITEMS);
+    MapTile<T, VP, ITEMS, TAIL ? 2 : 1, SPREAD> t(a, bs + warps * ITEMS);
     for (int c = threadIdx.x; c < warps * ITEMS; c += blockDim.x) {
         wt[c] = c >= n ? 0.f : a.weight ? weight_at<T>(a.weight, a.weight_f32, c) : 1.f;
         bs[c] = c < n && a.bias ? weight_at<T>(a.bias, a.weight_f32, c) : 0.f;
     }
     const Mask mask(a);
     const float inv_count = 1.f / (float)n, here = (float)t.items, inv_here = 1.f / here;
-    const long long tiles = (t.pieces + 31) / 32;
     bool full = false;
     auto fetch = [&](long long tile) {
-        if (tile < tiles) {
+        if (tile < t.tiles) {
             t.go(tile, a);
             full = t.full();
             if (full) {
@@ -200,30 +251,33 @@ __global__ void __launch_bounds__(MAP_TILE_WARPS * 32, ITEMS <= 16 ? 2 : 1) map_
 #pragma unroll
         for (int i = 0; i < PAIRS<VP>; ++i) pivot[i] = s[i] = q[i] = Two(0.f);
         T* sum = TAIL ? t.at(a.out2, a.pout2, a) : nullptr;
-        MaskPlace<VP> place(a, TAIL ? t.element(a) : 0);
+        MaskPlace<VP, SPREAD> place(a, TAIL ? t.element(a) : 0);
         auto value = [&](int j, Two (&v)[PAIRS<VP>]) {
             unpack<T, VP>(t.slot(0, j), v);
             if (!TAIL) return;
             Two r[PAIRS<VP>];
             unpack<T, VP>(t.slot(1, j), r);
-            if (a.dropping) drop_piece<true, VP>(mask, place, v, r);
-            else {
+            if (a.dropping) {
+                if constexpr (SPREAD) drop_spread<true>(mask, place.at, t.lane, v, r);
+                else drop_piece<true, VP>(mask, place, v, r);
+            } else {
 #pragma unroll
                 for (int i = 0; i < PAIRS<VP>; ++i) v[i] = v[i] + r[i];
             }
             const Piece<T, VP> stored = piece_of<T, VP>(v);
             unpack<T, VP>(stored, v);
             t.slot(0, j) = stored;
-            *reinterpret_cast<Piece<T, VP>*>(sum) = stored;
+            t.template store<FULL>(sum, stored);
             sum += a.inner; place.next(a);
         };
-        if (t.template has<FULL>(0)) {
+        const int features = t.template count<FULL>();
+        if (FULL || features > 0) {
             value(0, pivot);
 #pragma unroll
             for (int i = 0; i < PAIRS<VP>; ++i) pivot[i] = pivot[i] * Two(-1.f);
             // two at a time: more of the mask's code than that does not stay in the instruction cache
 #pragma unroll 2
-            for (int j = 1; j < (FULL ? ITEMS : t.items); ++j) {
+            for (int j = 1; j < features; ++j) {
                 Two v[PAIRS<VP>];
                 value(j, v);
 #pragma unroll
@@ -243,26 +297,26 @@ __global__ void __launch_bounds__(MAP_TILE_WARPS * 32, ITEMS <= 16 ? 2 : 1) map_
 #pragma unroll
         for (int i = 0; i < PAIRS<VP>; ++i) less[i] = mean[i] * Two(-1.f);
 #pragma unroll 4
-        for (int j = 0; j < (FULL ? ITEMS : t.live ? t.items : 0); ++j, y += a.inner) {
+        for (int j = 0; j < t.template count<FULL>(); ++j, y += a.inner) {
             Two v[PAIRS<VP>];
             unpack<T, VP>(t.slot(0, j), v);
             const Two w(wt[t.first + j]), b(bs[t.first + j]);
 #pragma unroll
             for (int i = 0; i < PAIRS<VP>; ++i) v[i] = fma2((v[i] + less[i]) * rstd[i], w, b);
-            *reinterpret_cast<Piece<T, VP>*>(y) = piece_of<T, VP>(v);
+            t.template store<FULL>(y, piece_of<T, VP>(v));
         }
         if (t.warp == 0 && t.live && (a.mean || a.rstd)) {
-            const long long at = t.o * a.inner + t.k;
 #pragma unroll
             for (int i = 0; i < VP; ++i) {
-                if (a.mean) a.mean[at + i] = i % 2 ? mean[i / 2].hi() : mean[i / 2].lo();
-                if (a.rstd) a.rstd[at + i] = i % 2 ? rstd[i / 2].hi() : rstd[i / 2].lo();
+                if (SPREAD && i >= t.live) break;
+                if (a.mean) a.mean[t.position(i, a)] = i % 2 ? mean[i / 2].hi() : mean[i / 2].lo();
+                if (a.rstd) a.rstd[t.position(i, a)] = i % 2 ? rstd[i / 2].hi() : rstd[i / 2].lo();
             }
         }
     };
     fetch(blockIdx.x);
     __syncthreads();                                     // the weights
-    for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+    for (long long tile = blockIdx.x; tile < t.tiles; tile += gridDim.x) {
         copies_wait<0>();
         Two mean[PAIRS<VP>], dev[PAIRS<VP>], rstd[PAIRS<VP>];
         if (full) statistics(True{}, mean, dev);
@@ -286,23 +340,22 @@ __global__ void __launch_bounds__(MAP_TILE_WARPS * 32, ITEMS <= 16 ? 2 : 1) map_
     }
 }
 
-template <class T, int VP, int ITEMS, bool TAIL>
+template <class T, int VP, int ITEMS, bool TAIL, bool SPREAD>
 __global__ void __launch_bounds__(MAP_TILE_WARPS * 32, 1) map_tile_vjp(const __grid_constant__ Args a) {
     grid_dependency_wait();
     extern __shared__ __align__(16) float shared[];
     const int warps = blockDim.x >> 5, n = (int)a.features;
     float* sums = shared;
     float* wt = sums + map_exchange_floats(VP, warps);
-    MapTile<T, VP, ITEMS, TAIL ? 3 : 2> t(a, wt + warps * ITEMS * 2);
+    MapTile<T, VP, ITEMS, TAIL ? 3 : 2, SPREAD> t(a, wt + warps * ITEMS * 2);
     for (int c = threadIdx.x; c < warps * ITEMS; c += blockDim.x) wt[c] = c >= n ? 0.f : a.weight ? weight_at<T>(a.weight, a.weight_f32, c) : 1.f;
     const Mask mask(a);
     const bool added = TAIL && a.gsum;
     const float inv_count = 1.f / (float)n;
-    const long long tiles = (t.pieces + 31) / 32;
     Two less[PAIRS<VP>], rstd[PAIRS<VP>];
     bool full = false;
     auto fetch = [&](long long tile) {
-        if (tile < tiles) {
+        if (tile < t.tiles) {
             t.go(tile, a);
             full = t.full();
             if (full) {
@@ -315,11 +368,12 @@ __global__ void __launch_bounds__(MAP_TILE_WARPS * 32, 1) map_tile_vjp(const __g
                 if (added) t.template fetch<false>(2, a.gsum, a.pgsum, a);
             }
             if (t.live) {
-                const long long at = t.o * a.inner + t.k;
-                if constexpr (VP == 1) { less[0] = Two(-a.mean[at], 0.f); rstd[0] = Two(a.rstd[at], 0.f); }
+                auto mean = [&](int m) { return !SPREAD || m < t.live ? -a.mean[t.position(m, a)] : 0.f; };
+                auto root = [&](int m) { return !SPREAD || m < t.live ? a.rstd[t.position(m, a)] : 0.f; };
+                if constexpr (VP == 1) { less[0] = Two(mean(0), 0.f); rstd[0] = Two(root(0), 0.f); }
                 else {
 #pragma unroll
-                    for (int i = 0; i < VP / 2; ++i) { less[i] = Two(-a.mean[at + 2 * i], -a.mean[at + 2 * i + 1]); rstd[i] = Two(a.rstd[at + 2 * i], a.rstd[at + 2 * i + 1]); }
+                    for (int i = 0; i < VP / 2; ++i) { less[i] = Two(mean(2 * i), mean(2 * i + 1)); rstd[i] = Two(root(2 * i), root(2 * i + 1)); }
                 }
             }
         }
@@ -334,10 +388,18 @@ __global__ void __launch_bounds__(MAP_TILE_WARPS * 32, 1) map_tile_vjp(const __g
         for (int i = 0; i < PAIRS<VP>; ++i) s1[i] = s2[i] = Two(0.f);
 #pragma unroll
         for (int j = 0; j < ITEMS; ++j) {
-            if (!t.template has<FULL>(j)) continue;
+            if (!FULL && !(t.live && j < t.items)) continue;
             Two g[PAIRS<VP>], v[PAIRS<VP>], sw(0.f), sb(0.f);
             unpack<T, VP>(t.slot(0, j), g);
             unpack<T, VP>(t.slot(1, j), v);
+            if constexpr (SPREAD && !FULL) {             // positions that are not there hold anything
+                auto there = [&](Two (&u)[PAIRS<VP>]) {
+                    u[0] = Two(u[0].lo(), t.live > 1 ? u[0].hi() : 0.f);
+                    u[1] = Two(t.live > 2 ? u[1].lo() : 0.f, t.live > 3 ? u[1].hi() : 0.f);
+                };
+                there(g);
+                there(v);
+            }
             const Two w(wt[t.first + j]);
 #pragma unroll
             for (int i = 0; i < PAIRS<VP>; ++i) {
@@ -354,9 +416,9 @@ __global__ void __launch_bounds__(MAP_TILE_WARPS * 32, 1) map_tile_vjp(const __g
         constexpr bool FULL = decltype(whole_tile)::value;
         T* out = t.at(a.out, a.pout, a);
         T* out2 = TAIL ? t.at(a.out2, a.pout2, a) : nullptr;
-        MaskPlace<VP> place(a, TAIL ? t.element(a) : 0);
+        MaskPlace<VP, SPREAD> place(a, TAIL ? t.element(a) : 0);
 #pragma unroll 2
-        for (int j = 0; j < (FULL ? ITEMS : t.live ? t.items : 0); ++j, out += a.inner) {
+        for (int j = 0; j < t.template count<FULL>(); ++j, out += a.inner) {
             Two g[PAIRS<VP>], v[PAIRS<VP>];
             unpack<T, VP>(t.slot(0, j), g);
             unpack<T, VP>(t.slot(1, j), v);
@@ -370,16 +432,19 @@ __global__ void __launch_bounds__(MAP_TILE_WARPS * 32, 1) map_tile_vjp(const __g
 #pragma unroll
                     for (int i = 0; i < PAIRS<VP>; ++i) v[i] = v[i] + g[i];
                 }
-                *reinterpret_cast<Piece<T, VP>*>(out2) = piece_of<T, VP>(v);
-                if (a.dropping) drop_piece<false, VP>(mask, place, v, v);
+                t.template store<FULL>(out2, piece_of<T, VP>(v));
+                if (a.dropping) {
+                    if constexpr (SPREAD) drop_spread<false>(mask, place.at, t.lane, v, v);
+                    else drop_piece<false, VP>(mask, place, v, v);
+                }
                 out2 += a.inner; place.next(a);
             }
-            *reinterpret_cast<Piece<T, VP>*>(out) = piece_of<T, VP>(v);
+            t.template store<FULL>(out, piece_of<T, VP>(v));
         }
     };
     fetch(blockIdx.x);
     __syncthreads();                                     // the weights
-    for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+    for (long long tile = blockIdx.x; tile < t.tiles; tile += gridDim.x) {
         copies_wait<0>();
         Two c1[PAIRS<VP>], c2[PAIRS<VP>];
         if (full) sum_up(True{}, c1, c2);

@@ -132,9 +132,10 @@ static MapPlan map_plan(const Args& a, bool vjp, bool tail, std::initializer_lis
     auto take = [&](int vp, bool spread) {
         bool ok = spread || a.inner % vp == 0;
         for (const auto& v : arrays) ok = ok && (spread || !v.first || ((uintptr_t)v.first % (vp * sizeof(T)) == 0 && (a.outer == 1 || v.second % vp == 0)));
-        // two tiles on an SM, but where it would take pieces of less than 4 bytes
+        // two tiles on an SM with pieces of 16 bytes, else one with pieces of 8 (8 x 256 x 16384 in float32, VJP: one tile with 8
+        // bytes 87 us, three with 4 bytes 123; tail of 8 x 160 x 16384 in bf16, VJP: 72 and 123)
         const size_t bytes = sizeof(float) * (map_exchange_floats(vp, p.warps) + 2 * (size_t)p.warps * p.items) + sizeof(T) * vp * 32 * (size_t)p.warps * p.items * copies;
-        if (!ok || bytes > (vp * sizeof(T) > 4 ? 112 : 226) * 1024u) return false;
+        if (!ok || bytes > (vp * sizeof(T) > 8 ? 112 : 226) * 1024u) return false;
         p.vp = vp; p.spread = spread; p.shared = bytes;
         return true;
     };

@@ -227,7 +227,8 @@ __global__ void __launch_bounds__(MAP_TILE_WARPS * 32, ITEMS <= 16 ? 2 : 1) map_
         bs[c] = c < n && a.bias ? weight_at<T>(a.bias, a.weight_f32, c) : 0.f;
     }
     const Mask mask(a);
-    const float inv_count = 1.f / (float)n, here = (float)t.items, inv_here = 1.f / here;
+    const float count = (float)n, inv_count = 1.f / count, inv_here = 1.f / (float)t.items;
+    const float last_features = (float)(n - (warps - 1) * ITEMS), inv_last = 1.f / last_features;
     bool full = false;
     auto fetch = [&](long long tile) {
         if (tile < t.tiles) {
@@ -243,13 +244,14 @@ __global__ void __launch_bounds__(MAP_TILE_WARPS * 32, ITEMS <= 16 ? 2 : 1) map_
         }
         copies_commit();
     };
-    // the warp's features of every position: their mean and squared deviations from it.  Both are taken from the first feature on;
-    // as that is one of them, what the difference cancels is at most as many times the result as there are features.
-    auto statistics = [&](auto whole_tile, Two (&mean)[PAIRS<VP>], Two (&dev)[PAIRS<VP>]) {
+    // the warp's features of every position: their sum and the squared deviations from their mean.  The latter come from sums
+    // relative to the first feature; as that is one of them, what the difference cancels is at most as many times the result as
+    // there are features.
+    auto statistics = [&](auto whole_tile, Two (&sum_of)[PAIRS<VP>], Two (&dev)[PAIRS<VP>]) {
         constexpr bool FULL = decltype(whole_tile)::value;
         Two pivot[PAIRS<VP>], s[PAIRS<VP>], q[PAIRS<VP>];
 #pragma unroll
-        for (int i = 0; i < PAIRS<VP>; ++i) pivot[i] = s[i] = q[i] = Two(0.f);
+        for (int i = 0; i < PAIRS<VP>; ++i) pivot[i] = s[i] = q[i] = sum_of[i] = Two(0.f);
         T* sum = TAIL ? t.at(a.out2, a.pout2, a) : nullptr;
         MaskPlace<VP, SPREAD> place(a, TAIL ? t.element(a) : 0);
         auto value = [&](int j, Two (&v)[PAIRS<VP>]) {
@@ -274,21 +276,21 @@ __global__ void __launch_bounds__(MAP_TILE_WARPS * 32, ITEMS <= 16 ? 2 : 1) map_
         if (FULL || features > 0) {
             value(0, pivot);
 #pragma unroll
-            for (int i = 0; i < PAIRS<VP>; ++i) pivot[i] = pivot[i] * Two(-1.f);
+            for (int i = 0; i < PAIRS<VP>; ++i) { sum_of[i] = pivot[i]; pivot[i] = pivot[i] * Two(-1.f); }
             // two at a time: more of the mask's code than that does not stay in the instruction cache
 #pragma unroll 2
             for (int j = 1; j < features; ++j) {
                 Two v[PAIRS<VP>];
                 value(j, v);
 #pragma unroll
-                for (int i = 0; i < PAIRS<VP>; ++i) { const Two d = v[i] + pivot[i]; s[i] = s[i] + d; q[i] = fma2(d, d, q[i]); }
+                for (int i = 0; i < PAIRS<VP>; ++i) {
+                    const Two d = v[i] + pivot[i];
+                    sum_of[i] = sum_of[i] + v[i]; s[i] = s[i] + d; q[i] = fma2(d, d, q[i]);
+                }
             }
         }
 #pragma unroll
-        for (int i = 0; i < PAIRS<VP>; ++i) {
-            mean[i] = fma2(s[i], Two(inv_here), pivot[i] * Two(-1.f));
-            dev[i] = fma2(s[i] * Two(-inv_here), s[i], q[i]);
-        }
+        for (int i = 0; i < PAIRS<VP>; ++i) dev[i] = fma2(s[i] * Two(-inv_here), s[i], q[i]);
     };
     auto normalise = [&](auto whole_tile, const Two (&mean)[PAIRS<VP>], const Two (&rstd)[PAIRS<VP>]) {
         constexpr bool FULL = decltype(whole_tile)::value;
@@ -321,18 +323,18 @@ __global__ void __launch_bounds__(MAP_TILE_WARPS * 32, ITEMS <= 16 ? 2 : 1) map_
         Two mean[PAIRS<VP>], dev[PAIRS<VP>], rstd[PAIRS<VP>];
         if (full) statistics(True{}, mean, dev);
         else statistics(False{}, mean, dev);
-        // from the warps' means and deviations those of all, again relative to the first: the sum of (d + m_w - m)^2 is that of
-        // d^2 and n_w (m_w - m)^2
-        map_exchange<VP>(sums, warps, t.lane, t.warp, mean, dev, mean, rstd, [&](int, const float* pm, const float* pd, float* to, int N) {
-            const float m0 = pm[0];
-            float lin = 0.f, all = pd[0];
-            for (int u = 1; u < warps; ++u) {
-                const float nw = (float)min(ITEMS, n - u * ITEMS), d = pm[u * N] - m0;
-                lin = fmaf(nw, d, lin);
-                all += fmaf(nw * d, d, pd[u * N]);
+        // with m_w a warp's mean, the sum of (d + m_w - m)^2 is that of d^2 and n_w (m_w - m)^2
+        map_exchange<VP>(sums, warps, t.lane, t.warp, mean, dev, mean, rstd, [&](int, const float* ps, const float* pd, float* to, int N) {
+            float all = 0.f, q = 0.f;
+            for (int u = 0; u < warps; ++u) all += ps[u * N];
+            const float m = quotient(all, count, inv_count);
+            for (int u = 0; u < warps; ++u) {
+                const bool last = u == warps - 1;
+                const float d = fmaf(ps[u * N], last ? inv_last : 1.f / ITEMS, -m);
+                q += fmaf((last ? last_features : (float)ITEMS) * d, d, pd[u * N]);
             }
-            to[0] = fmaf(lin, inv_count, m0);
-            to[N] = inverse_root(not_negative(fmaf(-lin * inv_count, lin, all)) * inv_count + a.eps);
+            to[0] = m;
+            to[N] = inverse_root(not_negative(q) * inv_count + a.eps);
         });
         if (full) normalise(True{}, mean, rstd);
         else normalise(False{}, mean, rstd);

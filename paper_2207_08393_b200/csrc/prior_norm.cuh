@@ -9,7 +9,7 @@
 namespace gleam {
 namespace prior {
 
-constexpr int ROW_THREADS = 256, MAP_WARPS = 8;
+constexpr int ROW_THREADS = 256, MAP_WARPS = 32;
 
 // ---- rows (inner == 1), any number of features: a block per row, which it reads again for each sum -------------------------
 
@@ -117,7 +117,7 @@ __global__ void __launch_bounds__(256) row_weight_sums(const __grid_constant__ A
     }
 }
 
-// ---- maps (inner > 1): 32 neighbouring positions per block, its warps share the features -----------------------------------
+// ---- maps (inner > 1) of any number of features: 32 neighbouring positions per block, its warps share the features ----------
 
 // Sums of a pair over the warps of the block, for each lane (position), in every warp.
 __device__ __forceinline__ Pair warps_sum(Pair v, float (&buf)[2][MAP_WARPS][32]) {

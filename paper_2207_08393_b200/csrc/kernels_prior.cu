@@ -124,9 +124,9 @@ static cudaError_t launch_rows(const Args& a, const RowPlan& p, bool tail, int* 
 struct MapPlan { int vp, items, warps; bool spread; size_t shared; };
 static MapPlan map_plan(const Args& a, bool vjp, bool tail, std::initializer_list<std::pair<const void*, long long>> arrays) {
     MapPlan p{};
-    if (a.features > 32 * MAP_TILE_WARPS) return p;
+    if (a.features > MAP_FEATURES) return p;
     // a VJP has two sums more for each feature in registers: fewer threads, with 128 each
-    p.items = !vjp && a.features <= 8 * MAP_TILE_WARPS ? 8 : a.features <= 16 * MAP_TILE_WARPS ? 16 : 32;
+    p.items = !vjp && a.features <= 8 * MAP_TILE_WARPS ? 8 : a.features <= 16 * MAP_TILE_WARPS ? 16 : a.features <= 32 * MAP_TILE_WARPS ? 32 : MAP_ITEMS;
     p.warps = (int)((a.features + p.items - 1) / p.items);
     const int copies = (vjp ? 2 : 1) + tail;
     auto take = [&](int vp, bool spread) {
@@ -153,7 +153,7 @@ static cudaError_t launch_maps(const Args& a, const MapPlan& p, int* blocks, cud
     if (e != cudaSuccess) return e;
     const long long tiles = SPREAD ? a.outer * ((a.inner + 32 * VP - 1) / (32 * VP)) : (a.outer * a.inner / VP + 31) / 32;
     int fit = (int)(SM_BYTES / (p.shared + 1024));
-    const int threads = p.warps * 32, held = (!VJP && ITEMS <= 16 ? 1024 : 512) / threads;     // blocks that the registers of an SM hold
+    const int threads = p.warps * 32, held = (!VJP && ITEMS <= 16 ? 2 : 1) * MAP_TILE_WARPS * 32 / threads;     // blocks that the registers of an SM hold
     if (fit > held) fit = held;
     const long long most = (long long)SMS * (fit < 1 ? 1 : fit);
     *blocks = (int)(tiles < most ? tiles : most);
@@ -164,7 +164,8 @@ static cudaError_t launch_maps(const Args& a, const MapPlan& p, int* blocks, cud
 template <bool VJP, bool TAIL, int VP, bool SPREAD>
 static cudaError_t launch_maps(const Args& a, const MapPlan& p, int* blocks, cudaStream_t s) {
     if constexpr (!VJP) if (p.items == 8) return launch_maps<VJP, TAIL, VP, SPREAD, 8>(a, p, blocks, s);
-    return p.items == 16 ? launch_maps<VJP, TAIL, VP, SPREAD, 16>(a, p, blocks, s) : launch_maps<VJP, TAIL, VP, SPREAD, 32>(a, p, blocks, s);
+    return p.items == 16 ? launch_maps<VJP, TAIL, VP, SPREAD, 16>(a, p, blocks, s) : p.items == 32 ? launch_maps<VJP, TAIL, VP, SPREAD, 32>(a, p, blocks, s)
+                                                                                                  : launch_maps<VJP, TAIL, VP, SPREAD, MAP_ITEMS>(a, p, blocks, s);
 }
 template <bool VJP, bool TAIL>
 static cudaError_t launch_maps(const Args& a, const MapPlan& p, int* blocks, cudaStream_t s) {

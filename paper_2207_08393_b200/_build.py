@@ -71,6 +71,11 @@ def build(force: bool = False, verbose: bool = False) -> str:
         obj = os.path.join(BUILD, "kernels_prior%d.o" % kind)
         jobs.append((["nvcc"] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) +
                      ["-DGLEAM_PRIOR_TYPE=%d" % kind, "-c", os.path.join(CSRC, "kernels_prior.cu"), "-o", obj], obj))
+        for vjp in range(2):
+            obj = os.path.join(BUILD, "kernels_prior_maps%d%d.o" % (kind, vjp))
+            jobs.insert(0, (["nvcc"] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) +        # the longest of all: first
+                            ["-DGLEAM_PRIOR_TYPE=%d" % kind, "-DGLEAM_PRIOR_VJP=%d" % vjp, "-c",
+                             os.path.join(CSRC, "kernels_prior_maps.cu"), "-o", obj], obj))
     for name in ("gleam_dc", "kernels_fused", "modl_cg", "prior_ops"):
         obj = os.path.join(BUILD, name + ".o")
         jobs.append((["nvcc"] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) +

@@ -1,46 +1,11 @@
-// Instantiation unit of the prior's operators for one element type: GLEAM_PRIOR_TYPE is 0 (float32), 1 (float16) or 2 (bfloat16).
-#include "dc_entry.h"
-#include "launch_state.cuh"
-#include "prior_entry.h"
+// Rows, dropout and the choice of the kernels, for one element type (prior_unit.cuh).
+#include "prior_unit.cuh"
 #include "prior_dropout.cuh"
-#include "prior_maps.cuh"
 #include "prior_norm.cuh"
 #include "prior_rows.cuh"
 
-#include <initializer_list>
-#include <type_traits>
-#include <utility>
-
 namespace gleam {
 namespace prior {
-
-#if GLEAM_PRIOR_TYPE == 0
-using T = float;
-#define GLEAM_PRIOR_OPS ops_f32
-#elif GLEAM_PRIOR_TYPE == 1
-using T = __half;
-#define GLEAM_PRIOR_OPS ops_f16
-#else
-using T = __nv_bfloat16;
-#define GLEAM_PRIOR_OPS ops_bf16
-#endif
-
-#define PRIOR_LAUNCH(...) do { cudaError_t e_ = prof_mark(GLEAM_K_PRIOR, s); if (e_ == cudaSuccess) e_ = launch_overlapped(true, __VA_ARGS__); \
-                               if (e_ != cudaSuccess) return e_; } while (0)
-
-static unsigned bounded(long long n, long long most) { return (unsigned)(n < 1 ? 1 : n < most ? n : most); }
-constexpr long long GRID = 1ll << 20;                    // blocks of a launch at most; the kernels stride over what is beyond
-
-using yes = std::true_type;
-using no = std::false_type;
-template <int N> using number = std::integral_constant<int, N>;
-
-// Whether all the arrays (null: absent) start at 16 bytes and, where they step, step by multiples of them more than `beyond`.
-static bool packed(const Args& a, long long beyond, std::initializer_list<std::pair<const void*, long long>> arrays) {
-    for (const auto& v : arrays)
-        if (v.first && ((uintptr_t)v.first % 16 != 0 || (a.outer > 1 && (v.second - beyond) % VEC<T> != 0))) return false;
-    return true;
-}
 
 // How rows are dealt to teams of threads (prior_rows.cuh); fits = false where a row is too long for one.
 struct RowPlan {
@@ -80,8 +45,6 @@ static int row_grid(const Args& a, const RowPlan& p, bool vjp, int most) {
     return (int)(need < most ? need : most);
 }
 
-template <auto KERNEL> static PerDevice kernel_state;
-
 template <bool VJP, bool TAIL, bool EDGES, int TEAM>
 static cudaError_t launch_rows(const Args& a, const RowPlan& p, int* blocks, cudaStream_t s) {
     constexpr int FEATURES = row_features(TEAM);
@@ -120,60 +83,6 @@ static cudaError_t launch_rows(const Args& a, const RowPlan& p, bool tail, int* 
                 : (p.edges ? launch_rows<VJP, false, true>(a, p, blocks, s) : launch_rows<VJP, false, false>(a, p, blocks, s));
 }
 
-// How maps are dealt to tiles (prior_maps.cuh); vp = 0 where the features of a tile do not fit.
-struct MapPlan { int vp, items, warps; bool spread; size_t shared; };
-static MapPlan map_plan(const Args& a, bool vjp, bool tail, std::initializer_list<std::pair<const void*, long long>> arrays) {
-    MapPlan p{};
-    if (a.features > MAP_FEATURES) return p;
-    // a VJP has two sums more for each feature in registers: fewer threads, with 128 each
-    p.items = !vjp && a.features <= 8 * MAP_TILE_WARPS ? 8 : a.features <= 16 * MAP_TILE_WARPS ? 16 : a.features <= 32 * MAP_TILE_WARPS ? 32 : MAP_ITEMS;
-    p.warps = (int)((a.features + p.items - 1) / p.items);
-    const int copies = (vjp ? 2 : 1) + tail;
-    auto take = [&](int vp, bool spread) {
-        bool ok = spread || a.inner % vp == 0;
-        for (const auto& v : arrays) ok = ok && (spread || !v.first || ((uintptr_t)v.first % (vp * sizeof(T)) == 0 && (a.outer == 1 || v.second % vp == 0)));
-        // two tiles on an SM with pieces of 16 bytes, else one with pieces of 8 (8 x 256 x 16384 in float32, VJP: one tile with 8
-        // bytes 87 us, three with 4 bytes 123; tail of 8 x 160 x 16384 in bf16, VJP: 72 and 123)
-        const size_t bytes = sizeof(float) * (map_exchange_floats(vp, p.warps) + 2 * (size_t)p.warps * p.items) + sizeof(T) * vp * 32 * (size_t)p.warps * p.items * copies;
-        if (!ok || bytes > (vp * sizeof(T) > 8 ? 112 : 226) * 1024u) return false;
-        p.vp = vp; p.spread = spread; p.shared = bytes;
-        return true;
-    };
-    // pieces of 16 bytes, else of 8; where slices begin anywhere, four positions element by element; else smaller pieces
-    for (int vp = 16 / (int)sizeof(T); vp >= 4; vp /= 2) if (take(vp, false)) return p;
-    if (a.inner >= 128 && take(4, true)) return p;
-    for (int vp = 2; vp >= 1; --vp) if (take(vp, false)) return p;
-    return p;
-}
-template <bool VJP, bool TAIL, int VP, bool SPREAD, int ITEMS>
-static cudaError_t launch_maps(const Args& a, const MapPlan& p, int* blocks, cudaStream_t s) {
-    constexpr auto KERNEL = [] { if constexpr (VJP) return map_tile_vjp<T, VP, ITEMS, TAIL, SPREAD>; else return map_tile_forward<T, VP, ITEMS, TAIL, SPREAD>; }();
-    constexpr size_t SM_BYTES = 227 * 1024;
-    cudaError_t e = ensure_smem(KERNEL, SM_BYTES, kernel_state<KERNEL>);
-    if (e != cudaSuccess) return e;
-    const long long tiles = SPREAD ? a.outer * ((a.inner + 32 * VP - 1) / (32 * VP)) : (a.outer * a.inner / VP + 31) / 32;
-    int fit = (int)(SM_BYTES / (p.shared + 1024));
-    const int threads = p.warps * 32, held = (!VJP && ITEMS <= 16 ? 2 : 1) * MAP_TILE_WARPS * 32 / threads;     // blocks that the registers of an SM hold
-    if (fit > held) fit = held;
-    const long long most = (long long)SMS * (fit < 1 ? 1 : fit);
-    *blocks = (int)(tiles < most ? tiles : most);
-    if (VJP && *blocks > MAP_PARTS_MOST) *blocks = MAP_PARTS_MOST;
-    PRIOR_LAUNCH(KERNEL, dim3((unsigned)*blocks), dim3(threads), p.shared, s, a);
-    return cudaSuccess;
-}
-template <bool VJP, bool TAIL, int VP, bool SPREAD>
-static cudaError_t launch_maps(const Args& a, const MapPlan& p, int* blocks, cudaStream_t s) {
-    if constexpr (!VJP) if (p.items == 8) return launch_maps<VJP, TAIL, VP, SPREAD, 8>(a, p, blocks, s);
-    return p.items == 16 ? launch_maps<VJP, TAIL, VP, SPREAD, 16>(a, p, blocks, s) : p.items == 32 ? launch_maps<VJP, TAIL, VP, SPREAD, 32>(a, p, blocks, s)
-                                                                                                  : launch_maps<VJP, TAIL, VP, SPREAD, MAP_ITEMS>(a, p, blocks, s);
-}
-template <bool VJP, bool TAIL>
-static cudaError_t launch_maps(const Args& a, const MapPlan& p, int* blocks, cudaStream_t s) {
-    if constexpr (sizeof(T) == 2) if (p.vp == 8) return launch_maps<VJP, TAIL, 8, false>(a, p, blocks, s);
-    return p.spread ? launch_maps<VJP, TAIL, 4, true>(a, p, blocks, s) : p.vp == 4 ? launch_maps<VJP, TAIL, 4, false>(a, p, blocks, s)
-         : p.vp == 2 ? launch_maps<VJP, TAIL, 2, false>(a, p, blocks, s) : launch_maps<VJP, TAIL, 1, false>(a, p, blocks, s);
-}
-
 static cudaError_t forward(const Args& given, bool tail, cudaStream_t s) {
     Args a = given;
     cudaError_t e;
@@ -186,9 +95,9 @@ static cudaError_t forward(const Args& given, bool tail, cudaStream_t s) {
         if (tail) PRIOR_LAUNCH(row_forward<T, true>, grid, dim3(ROW_THREADS), 0, s, a);
         else PRIOR_LAUNCH(row_forward<T, false>, grid, dim3(ROW_THREADS), 0, s, a);
     } else {
-        const MapPlan p = map_plan(a, false, tail, {{a.x, a.px}, {a.res, a.pres}, {a.out, a.pout}, {a.out2, a.pout2}});
-        int blocks = 0;
-        if (p.vp) return (e = tail ? launch_maps<false, true>(a, p, &blocks, s) : launch_maps<false, false>(a, p, &blocks, s)) != cudaSuccess ? e : prof_mark(-1, s);
+        bool taken = false;
+        if ((e = Maps<T>::forward(a, tail, &taken, s)) != cudaSuccess) return e;
+        if (taken) return prof_mark(-1, s);
         const dim3 grid(bounded((a.outer * a.inner + 31) / 32, GRID));
         if (tail) PRIOR_LAUNCH(map_forward<T, true>, grid, dim3(MAP_WARPS * 32), 0, s, a);
         else PRIOR_LAUNCH(map_forward<T, false>, grid, dim3(MAP_WARPS * 32), 0, s, a);
@@ -214,10 +123,9 @@ static cudaError_t vjp(const Args& given, bool tail, cudaStream_t s) {
             return prof_mark(-1, s);
         }
     } else {
-        const MapPlan p = map_plan(a, true, tail, {{a.x, a.px}, {a.res, a.pres}, {a.gsum, a.pgsum}, {a.out, a.pout}, {a.out2, a.pout2}});
-        if (p.vp) {
-            int blocks = 0;
-            if ((e = tail ? launch_maps<true, true>(a, p, &blocks, s) : launch_maps<true, false>(a, p, &blocks, s)) != cudaSuccess) return e;
+        int blocks = 0;
+        if ((e = Maps<T>::vjp(a, tail, &blocks, s)) != cudaSuccess) return e;
+        if (blocks) {
             if ((a.gw || a.gb) && blocks > 1 && (e = weight_grads_from(a, blocks, s)) != cudaSuccess) return e;
             return prof_mark(-1, s);
         }
@@ -263,8 +171,16 @@ static cudaError_t dropout(const Args& given, cudaStream_t s) {
     return prof_mark(-1, s);
 }
 
-extern const Ops GLEAM_PRIOR_OPS;
-const Ops GLEAM_PRIOR_OPS = {forward, vjp, dropout};
+#if GLEAM_PRIOR_TYPE == 0
+extern const Ops ops_f32;
+const Ops ops_f32 = {forward, vjp, dropout};
+#elif GLEAM_PRIOR_TYPE == 1
+extern const Ops ops_f16;
+const Ops ops_f16 = {forward, vjp, dropout};
+#else
+extern const Ops ops_bf16;
+const Ops ops_bf16 = {forward, vjp, dropout};
+#endif
 
 }  // namespace prior
 }  // namespace gleam

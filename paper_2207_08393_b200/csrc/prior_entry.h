@@ -13,6 +13,12 @@ struct Ops {
 };
 extern const Ops ops_f32, ops_f16, ops_bf16;
 
+// Maps in tiles (kernels_prior_maps.cu).  Nothing is launched (taken = false, blocks = 0) where the features of a tile do not fit.
+template <class T> struct Maps {
+    static cudaError_t forward(const Args& a, bool tail, bool* taken, cudaStream_t s);
+    static cudaError_t vjp(const Args& a, bool tail, int* blocks, cudaStream_t s);
+};
+
 // Rows of partial sums of the weights' gradients that a VJP writes at most (its blocks come eight at a time in one form).
 constexpr int SMS = 148;
 constexpr int PARTS_MOST = 2 * SMS, MAP_PARTS_MOST = 8 * SMS;

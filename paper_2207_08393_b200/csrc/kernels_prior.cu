@@ -58,7 +58,7 @@ static cudaError_t launch_rows(const Args& a, const RowPlan& p, int* blocks, cud
     const cudaError_t e = ensure_smem(KERNEL, SM_BYTES, kernel_state<KERNEL>);
     if (e != cudaSuccess) return e;
     // blocks that are resident at once: what registers and shared memory hold
-    int resident = row_blocks(VJP, TEAM) * row_block(TEAM) / p.threads;
+    int resident = row_blocks(VJP, TEAM) * row_block(VJP, TEAM) / p.threads;
     const int fit = (int)(SM_BYTES / (shared + 1024));
     if (resident > fit) resident = fit;
     if (VJP && resident > PARTS_MOST / SMS) resident = PARTS_MOST / SMS;

@@ -251,7 +251,7 @@ __global__ void __launch_bounds__(GRAD_WARPS * 32) weight_grads(const __grid_con
     float t = 0.f;
     if (c < a.features) {
         const float* part = a.part + blockIdx.y * a.features + c;
-#pragma unroll 5
+#pragma unroll 10
         for (int p = warp; p < parts; p += GRAD_WARPS) t += part[(long long)p * 2 * a.features];
     }
     buf[lane][warp] = t;

@@ -23,9 +23,13 @@ using False = std::false_type;
 
 constexpr int ROW_BLOCK = 256, ROW_BLOCK_MOST = 512;     // threads a block: of teams inside a warp, and at most (one long row)
 // Features a thread: 32 in a team inside a warp, 16 where warps share a row.  There the latency of a row's steps counts, and twice
-// the warps on an SM hide it (2049 rows of 4096 and 4099 in float32, forward and VJP, with 32: 12.9 + 28.9 and 27.2 + 55.2 us).
+// the warps on an SM hide it (2049 rows of 4096 and 4099 in float32, forward and VJP: 13.1 + 25.2 and 19.6 + 31.6 us; with 32
+// features a thread 12.9 + 28.9 and 27.2 + 55.2).
 constexpr int row_features(int team) { return team ? 32 : 16; }
-constexpr int row_block(int team) { return team ? ROW_BLOCK : ROW_BLOCK_MOST; }
+// Threads that the registers of an SM are shared by.  A VJP of long rows has 96 registers, so that two blocks of nine warps fit, which
+// rows of 4096 features that begin anywhere need (VJP of the rows above with 128 registers, for two blocks of eight warps: 24.2 for
+// 4096 features, 38.4 us for 4099).
+constexpr int row_block(bool vjp, int team) { return team ? ROW_BLOCK : vjp ? 608 : ROW_BLOCK_MOST; }
 template <class T, int TEAM> constexpr int ROW_ITEMS = row_features(TEAM) / VEC<T>;     // pieces a thread
 
 __device__ __forceinline__ void team_barrier(int team, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "r"(threads) : "memory"); }
@@ -198,7 +202,7 @@ struct Ring {
     }
 };
 
-// Blocks of row_block(team) threads on an SM (registers), and rows in the ring: four, or as many as the shared memory holds beside
+// Blocks of row_block() threads on an SM (registers), and rows in the ring: four, or as many as the shared memory holds beside
 // the weights; two where warps share a row, for two blocks.
 constexpr int row_blocks(bool vjp, int team) { return team ? (vjp ? 1 : 3) : vjp ? 1 : 2; }
 constexpr int row_stages(bool vjp, bool tail, int size, int team) {
@@ -207,7 +211,7 @@ constexpr int row_stages(bool vjp, bool tail, int size, int team) {
 }
 
 template <class T, int TEAM, bool EDGES, bool TAIL>
-__global__ void __launch_bounds__(row_block(TEAM), row_blocks(false, TEAM)) row_team_forward(const __grid_constant__ Args a, int warps, int teams) {
+__global__ void __launch_bounds__(row_block(false, TEAM), row_blocks(false, TEAM)) row_team_forward(const __grid_constant__ Args a, int warps, int teams) {
     grid_dependency_wait();
     extern __shared__ __align__(16) float shared[];
     constexpr int V = VEC<T>, ITEMS = ROW_ITEMS<T, TEAM>, STAGES = row_stages(false, TAIL, sizeof(T), TEAM), ARRAYS = TAIL ? 2 : 1;
@@ -322,7 +326,7 @@ __global__ void __launch_bounds__(row_block(TEAM), row_blocks(false, TEAM)) row_
 }
 
 template <class T, int TEAM, bool EDGES, bool TAIL>
-__global__ void __launch_bounds__(row_block(TEAM), row_blocks(true, TEAM)) row_team_vjp(const __grid_constant__ Args a, int warps, int teams) {
+__global__ void __launch_bounds__(row_block(true, TEAM), row_blocks(true, TEAM)) row_team_vjp(const __grid_constant__ Args a, int warps, int teams) {
     grid_dependency_wait();
     extern __shared__ __align__(16) float shared[];
     constexpr int V = VEC<T>, ITEMS = ROW_ITEMS<T, TEAM>, STAGES = row_stages(true, TAIL, sizeof(T), TEAM), ARRAYS = TAIL ? 3 : 2;

@@ -115,8 +115,8 @@ def _same(x, t, view, dim, what):
 
 
 def _match(x, t, dim):
-    """``t`` itself if the calls take it next to ``x``, else a copy in x's order (cotangents come in any order)."""
-    if t.shape != x.shape or (t.is_contiguous() and x.is_contiguous()):
+    """``t`` itself if the calls take it next to ``x`` or refuse it, else a copy in x's order (cotangents come in any order)."""
+    if t.shape != x.shape or t.dtype != x.dtype or t.device != x.device or (t.is_contiguous() and x.is_contiguous()):
         return t
     view = _view(x, dim)
     try:

@@ -204,3 +204,12 @@ def test_generator_ranges_do_not_meet():
     assert int(gen.step) == 1
     with pytest.raises(RuntimeError):
         prior_ops.DropoutGenerator(3, device="cpu").advance()
+
+
+def test_only_an_order_is_changed_for_a_call():
+    x = torch.zeros(2, 3, 4)
+    turned = torch.arange(24.).view(2, 4, 3).transpose(1, 2)
+    got = prior_ops._match(x, turned, 1)
+    assert got.is_contiguous() and torch.equal(got, turned)
+    for other in (turned.double(), turned.to("meta"), turned[:1]):   # another type, device or shape is for the call to refuse
+        assert prior_ops._match(x, other, 1) is other

@@ -9,7 +9,9 @@
 // Bound by memory, if the instructions are few: what a row costs each thread apart from its features (about a hundred: the
 // sums across lanes, the ring, the statistics) is shared by 32 features, and the arithmetic is done two numbers at a time.
 // 51200 rows of 1024 in bf16, forward and VJP: eight features a thread with loads into registers 216 us, fetched ahead 177, 32
-// features a thread 142, two numbers at a time 96 (37 + 59; the bytes take 80 at copy rate).
+// features a thread 142, two numbers at a time 94 (36 + 58; the bytes take 80 at copy rate).  A tail of 12801 rows of 1000 in fp16
+// takes 26 + 38 us (its bytes 35).  Rows that begin anywhere cost more, as the pieces at their ends go element by element and are
+// copied for both of their rows (400000 rows in bf16: 96 features 32 + 51 us, 100 features 51 + 95).
 #pragma once
 #include "prior_common.cuh"
 

@@ -406,6 +406,10 @@ class DropoutGenerator:
     ``capturable=True`` adds a counter on the device that the kernels read when they run: a captured training step ends with
     ``advance()`` inside the graph, and every replay draws new masks with the ranges it was captured with.  The counter must
     not move between a forward call and its backward pass, and the generator lives as long as a graph that reads it.
+
+    A forward pass that is run again in the backward pass (activation checkpointing) has to take its first ranges again:
+    ``torch.utils.checkpoint.checkpoint(f, x, use_reentrant=False, context_fn=generator.recompute)``.  Without that it would
+    draw other masks than the outputs were made with.
     """
 
     def __init__(self, seed, device="cuda", capturable=False):
@@ -417,10 +421,42 @@ class DropoutGenerator:
         self.offset += (int(numel) + 3) // 4
         return offset
 
+    def recompute(self):
+        """The contexts of a forward pass and of its recomputation, in which the ranges of the former are taken again."""
+        first = _Ranges(self)
+        return first, _RangesAgain(first)
+
     def advance(self):
         if self.step is None:
             raise RuntimeError("advance() needs capturable=True")
         self.step.add_(1)
+
+
+class _Ranges:
+    """Notes where a generator stands."""
+
+    def __init__(self, generator):
+        self.generator, self.start = generator, None
+
+    def __enter__(self):
+        self.start = self.generator.offset
+
+    def __exit__(self, *a):
+        pass
+
+
+class _RangesAgain:
+    """The generator where it stood, for a while; a graph that is kept may ask for this more than once."""
+
+    def __init__(self, first):
+        self.first, self.held = first, []
+
+    def __enter__(self):
+        self.held.append(self.first.generator.offset)
+        self.first.generator.offset = self.first.start
+
+    def __exit__(self, *a):
+        self.first.generator.offset = self.held.pop()
 
 
 class _LayerNorm(torch.autograd.Function):

@@ -158,3 +158,26 @@ def test_a_captured_training_step_of_the_prior():
     assert any(float((a - b).norm()) > 1e-3 * float(n) for a, b, n in zip(seen[0], seen[1], norms))
     # the convolutions' gradients may add in any order
     assert all(float((a - b).norm()) <= 1e-4 * float(n) + 1e-12 for a, b, n in zip(seen[0], seen[2], norms))
+
+
+@pytest.mark.gpu
+def test_a_prior_under_activation_checkpointing():
+    """Recomputed blocks draw the masks of the forward pass: the same bits as without checkpointing."""
+    import paper_2207_08393_b200 as g
+    from paper_2207_08393_b200.gleam_loop import ResidualPrior
+    from torch.utils.checkpoint import checkpoint
+    x = torch.randn(2, 2, 3, 1, 12, 10, device="cuda", generator=torch.Generator("cuda").manual_seed(5))
+    got = []
+    for again in (False, True):
+        torch.manual_seed(2)
+        gen = g.DropoutGenerator(17)
+        priors = [ResidualPrior(8, 2, norm=norm, dropout=0.3, generator=gen).cuda() for norm in (True, False)]
+        leaf = x.clone().requires_grad_()
+        h = leaf
+        with torch.backends.cudnn.flags(enabled=True, benchmark=False, deterministic=True):
+            for prior in priors:
+                h = checkpoint(prior, h, use_reentrant=False, context_fn=gen.recompute) if again else prior(h)
+            h.square().sum().backward()
+        got.append([h.detach(), leaf.grad] + [p.grad for prior in priors for p in prior.parameters()])
+    for a, b in zip(*got):
+        assert torch.equal(a, b)

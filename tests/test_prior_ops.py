@@ -213,3 +213,24 @@ def test_only_an_order_is_changed_for_a_call():
     assert got.is_contiguous() and torch.equal(got, turned)
     for other in (turned.double(), turned.to("meta"), turned[:1]):   # another type, device or shape is for the call to refuse
         assert prior_ops._match(x, other, 1) is other
+
+
+def test_a_recomputed_pass_takes_its_ranges_again():
+    from torch.utils.checkpoint import checkpoint
+    gen, taken = prior_ops.DropoutGenerator(3, device="cpu"), []
+
+    def block(x):
+        for _ in range(2):
+            taken.append(gen.take(x.numel()))
+            x = x.sin()
+        return x
+
+    x = torch.ones(10, requires_grad=True)
+    y = checkpoint(block, x, use_reentrant=False, context_fn=gen.recompute)
+    z = checkpoint(block, y, use_reentrant=False, context_fn=gen.recompute)
+    assert taken == [0, 3, 6, 9] and gen.offset == 12
+    z.sum().backward(retain_graph=True)
+    again = taken[4:]
+    assert again == [6, 9, 0, 3] and gen.offset == 12
+    z.sum().backward()                                               # a kept graph runs its blocks again
+    assert set(taken[8:]) <= {0, 3, 6, 9} and gen.offset == 12

@@ -656,3 +656,39 @@ def test_autograd_in_other_orders_and_partial_gradients():
     step.advance()
     with pytest.raises(RuntimeError, match="inplace"):   # the counter moved before the backward pass
         z.sum().backward()
+
+
+def test_calls_from_several_threads():
+    """The calls release the interpreter's lock; threads on streams of their own get the bits of calls in turn."""
+    import threading
+    import paper_2207_08393_b200 as g
+    shapes = [(50, 96, 1), (3, 24, 260), (20, 1003, 1), (2, 33, 129)]
+    data = []
+    for k, shape in enumerate(shapes):
+        torch.manual_seed(k)
+        data.append([torch.randn(shape, device="cuda") for _ in range(4)] + [torch.rand(shape[1], device="cuda")])
+
+    def run(k):
+        x, r, dy, ds, w = data[k]
+        y, total, mean, rstd = g.dropout_add_layer_norm_forward(x, r, w, None, 0.3, 11, 4 * k, dim=1)
+        return (y, total) + g.dropout_add_layer_norm_vjp(dy, ds, total, w, mean, rstd, 0.3, 11, 4 * k, dim=1)
+
+    want = [run(k) for k in range(len(shapes))]
+    torch.cuda.synchronize()
+    got = [None] * len(shapes)
+
+    def work(k):
+        stream = torch.cuda.Stream()
+        with torch.cuda.stream(stream):
+            for _ in range(30):
+                got[k] = run(k)
+        stream.synchronize()
+
+    threads = [threading.Thread(target=work, args=(k,)) for k in range(len(shapes))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    for a, b in zip(want, got):
+        for u, v in zip(a, b):
+            assert torch.equal(u, v)

@@ -35,6 +35,17 @@ def _numel(sizes):
     return n
 
 
+def _steps(shape):
+    """Strides of a contiguous tensor."""
+    if len(shape) == 1:
+        return (1,)
+    steps, n = [], 1
+    for s in reversed(shape):
+        steps.append(n)
+        n *= s
+    return steps[::-1]
+
+
 def _slices(shape, strides, dim):
     """(outer, inner, pitch) if the axes from ``dim`` on are contiguous and those before step evenly, else None.  An axis of
     length one steps anywhere."""
@@ -282,7 +293,8 @@ class _Prepared:
         return out
 
     def statistics(self, x):
-        mean = x.new_empty(self.stats, dtype=torch.float32)
+        # the cheapest of torch's ways to new memory (1.4 us; torch.empty with a device takes 3.0, new_empty 2.3)
+        mean = torch.empty_strided(self.stats, _steps(self.stats), dtype=torch.float32, device=x.device)
         return mean, torch.empty_like(mean)
 
     def workspace(self, x, wanted):
@@ -290,7 +302,7 @@ class _Prepared:
             return None
         if self.scratch is None:
             return _workspace(x, self.dims, True)
-        ws = x.new_empty(self.scratch, dtype=torch.uint8)
+        ws = torch.empty_strided((self.scratch,), (1,), dtype=torch.uint8, device=x.device)
         self.dims.workspace, self.dims.workspace_bytes = ws.data_ptr(), self.scratch
         return ws
 

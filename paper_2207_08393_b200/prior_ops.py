@@ -417,7 +417,8 @@ class DropoutGenerator:
 
     ``capturable=True`` adds a counter on the device that the kernels read when they run: a captured training step ends with
     ``advance()`` inside the graph, and every replay draws new masks with the ranges it was captured with.  The counter must
-    not move between a forward call and its backward pass, and the generator lives as long as a graph that reads it.
+    not move between a forward call and its backward pass (autograd and ``recompute`` raise if it has, but do not see what a
+    replayed graph does to it), and the generator lives as long as a graph that reads it.
 
     A forward pass that is run again in the backward pass (activation checkpointing) has to take its first ranges again:
     ``torch.utils.checkpoint.checkpoint(f, x, use_reentrant=False, context_fn=generator.recompute)``.  Without that it would
@@ -448,10 +449,11 @@ class _Ranges:
     """Notes where a generator stands."""
 
     def __init__(self, generator):
-        self.generator, self.start = generator, None
+        self.generator, self.start, self.version = generator, None, None
 
     def __enter__(self):
         self.start = self.generator.offset
+        self.version = None if self.generator.step is None else self.generator.step._version
 
     def __exit__(self, *a):
         pass
@@ -464,8 +466,13 @@ class _RangesAgain:
         self.first, self.held = first, []
 
     def __enter__(self):
-        self.held.append(self.first.generator.offset)
-        self.first.generator.offset = self.first.start
+        gen = self.first.generator
+        # the check that autograd makes of a saved tensor: a recomputation saves the counter anew, so nobody else would see it
+        if gen.step is not None and gen.step._version != self.first.version:
+            raise RuntimeError("the generator's counter has moved since the forward pass that is recomputed: advance() belongs "
+                               "behind the backward pass")
+        self.held.append(gen.offset)
+        gen.offset = self.first.start
 
     def __exit__(self, *a):
         self.first.generator.offset = self.held.pop()

@@ -181,3 +181,30 @@ def test_a_prior_under_activation_checkpointing():
         got.append([h.detach(), leaf.grad] + [p.grad for prior in priors for p in prior.parameters()])
     for a, b in zip(*got):
         assert torch.equal(a, b)
+
+
+@pytest.mark.gpu
+def test_checkpointing_with_a_device_counter():
+    """Masks of the counter's value come back in the recomputation; a counter that moved before the backward pass raises."""
+    import paper_2207_08393_b200 as g
+    from paper_2207_08393_b200.gleam_loop import ResidualPrior
+    from torch.utils.checkpoint import checkpoint
+    x = torch.randn(1, 2, 2, 1, 12, 10, device="cuda", generator=torch.Generator("cuda").manual_seed(5))
+    got = []
+    for again, moved in ((False, False), (True, False), (True, True)):
+        torch.manual_seed(2)
+        gen = g.DropoutGenerator(17, capturable=True)
+        gen.advance()
+        prior = ResidualPrior(8, 2, norm=True, dropout=0.3, generator=gen).cuda()
+        leaf = x.clone().requires_grad_()
+        with torch.backends.cudnn.flags(enabled=True, benchmark=False, deterministic=True):
+            h = checkpoint(prior, leaf, use_reentrant=False, context_fn=gen.recompute) if again else prior(leaf)
+            if moved:
+                gen.advance()
+                with pytest.raises(RuntimeError, match="counter"):
+                    h.square().sum().backward()
+                continue
+            h.square().sum().backward()
+        got.append([h.detach(), leaf.grad] + [p.grad for p in prior.parameters()])
+    for a, b in zip(*got):
+        assert torch.equal(a, b)

@@ -234,3 +234,26 @@ def test_a_recomputed_pass_takes_its_ranges_again():
     assert again == [6, 9, 0, 3] and gen.offset == 12
     z.sum().backward()                                               # a kept graph runs its blocks again
     assert set(taken[8:]) <= {0, 3, 6, 9} and gen.offset == 12
+
+
+def test_a_recomputed_pass_after_the_counter_has_moved_is_refused():
+    """Masks of a capturable generator depend on its counter: a recomputation behind advance() would draw others than the
+    outputs were made with, so it raises; without advance() it runs."""
+    from torch.utils.checkpoint import checkpoint
+    for moved in (False, True):
+        gen = prior_ops.DropoutGenerator(3, device="cpu", capturable=True)
+
+        def block(x):
+            gen.take(x.numel())
+            return x.sin()
+
+        x = torch.ones(10, requires_grad=True)
+        y = checkpoint(block, x, use_reentrant=False, context_fn=gen.recompute)
+        if not moved:
+            y.sum().backward()
+            assert torch.allclose(x.grad, torch.ones(10).cos()) and gen.offset == 3
+            continue
+        gen.advance()
+        with pytest.raises(RuntimeError, match="counter"):
+            y.sum().backward()
+        assert gen.offset == 3 and gen.take(1) == 3              # the generator can be used on

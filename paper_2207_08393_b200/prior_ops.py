@@ -13,6 +13,8 @@ but the dropout mask, which numbers the elements in memory order.
 """
 from __future__ import annotations
 
+import threading
+
 import torch
 
 from . import binding as _b
@@ -413,7 +415,8 @@ def dropout_add_layer_norm_vjp(grad_y, grad_total, total, weight, mean, rstd, p,
 # ---- autograd ------------------------------------------------------------------------------------------------------------
 
 class DropoutGenerator:
-    """Counter ranges for the dropout sites of a model: every call takes the range behind the last one, so no two share a mask.
+    """Counter ranges for the dropout sites of a model: every call takes the range behind the last one, so no two share a mask,
+    whichever threads they come from.  A copy (``copy.deepcopy``, pickling) stands where the first one stood and goes its own way.
 
     ``capturable=True`` adds a counter on the device that the kernels read when they run: a captured training step ends with
     ``advance()`` inside the graph, and every replay draws new masks with the ranges it was captured with.  The counter must
@@ -428,10 +431,40 @@ class DropoutGenerator:
     def __init__(self, seed, device="cuda", capturable=False):
         self.seed, self.offset = int(seed), 0
         self.step = torch.zeros(1, dtype=torch.int64, device=device) if capturable else None
+        self._unshared()
+
+    def _unshared(self):
+        self._lock = threading.Lock()
+        self._here = threading.local()               # .passes: the passes that are under way in this thread, the outermost first
+
+    def __getstate__(self):
+        return {k: v for k, v in self.__dict__.items() if k not in ("_lock", "_here")}
+
+    def __setstate__(self, state):
+        self.__dict__.update(state)
+        self._unshared()
+
+    def _passes(self):
+        try:
+            return self._here.passes
+        except AttributeError:
+            self._here.passes = []
+            return self._here.passes
 
     def take(self, numel):
-        offset = self.offset
-        self.offset += (int(numel) + 3) // 4
+        count = (int(numel) + 3) // 4
+        told, offset = [], None
+        for p in reversed(self._passes()):
+            if isinstance(p, _Again):
+                offset = p.next(count, self.step)    # passes around this one had nothing to do with its first run
+                break
+            told.append(p)
+        if offset is None:
+            with self._lock:
+                offset = self.offset
+                self.offset += count
+        for p in told:
+            p.taken.append((offset, count, None if self.step is None else self.step._version))
         return offset
 
     def recompute(self):
@@ -446,36 +479,49 @@ class DropoutGenerator:
 
 
 class _Ranges:
-    """Notes where a generator stands."""
+    """Notes the ranges that a forward pass takes."""
 
     def __init__(self, generator):
-        self.generator, self.start, self.version = generator, None, None
+        self.generator, self.taken, self.passes = generator, [], None
 
     def __enter__(self):
-        self.start = self.generator.offset
-        self.version = None if self.generator.step is None else self.generator.step._version
+        self.passes = self.generator._passes()
+        self.passes.append(self)
 
     def __exit__(self, *a):
-        pass
+        # not always the innermost one: a pass that raised ends when its frames are released
+        self.passes.remove(self)
+
+
+class _Again:
+    """One recomputation of a pass: the ranges that it has not yet asked for."""
+
+    def __init__(self, first):
+        self.first, self.left = first, iter(first.taken)
+
+    def next(self, count, step):
+        offset, wanted, version = next(self.left, (None, None, None))
+        if count != wanted:
+            raise RuntimeError("the recomputed pass asks for other ranges than the forward pass did")
+        # the check that autograd makes of a saved tensor: a recomputation saves the counter anew, so nobody else would see it
+        if step is not None and step._version != version:
+            raise RuntimeError("the generator's counter has moved since the forward pass that is recomputed: advance() belongs "
+                               "behind the backward pass")
+        return offset
 
 
 class _RangesAgain:
-    """The generator where it stood, for a while; a graph that is kept may ask for this more than once."""
+    """The ranges of a noted pass once more; a graph that is kept may ask for this more than once."""
 
     def __init__(self, first):
-        self.first, self.held = first, []
+        self.first = first
 
     def __enter__(self):
-        gen = self.first.generator
-        # the check that autograd makes of a saved tensor: a recomputation saves the counter anew, so nobody else would see it
-        if gen.step is not None and gen.step._version != self.first.version:
-            raise RuntimeError("the generator's counter has moved since the forward pass that is recomputed: advance() belongs "
-                               "behind the backward pass")
-        self.held.append(gen.offset)
-        gen.offset = self.first.start
+        self.first.generator._passes().append(_Again(self.first))
 
     def __exit__(self, *a):
-        self.first.generator.offset = self.held.pop()
+        passes = self.first.generator._passes()
+        passes.remove(next(p for p in reversed(passes) if isinstance(p, _Again) and p.first is self.first))
 
 
 class _LayerNorm(torch.autograd.Function):

@@ -257,3 +257,128 @@ def test_a_recomputed_pass_after_the_counter_has_moved_is_refused():
         with pytest.raises(RuntimeError, match="counter"):
             y.sum().backward()
         assert gen.offset == 3 and gen.take(1) == 3              # the generator can be used on
+
+
+def in_a_thread(f):
+    import threading
+    t = threading.Thread(target=f)
+    t.start()
+    t.join(60)
+    assert not t.is_alive()
+
+
+def test_threads_get_ranges_of_their_own():
+    import sys
+    import threading
+    gen, taken = prior_ops.DropoutGenerator(3), []
+
+    class Size:                                                      # a size whose evaluation lets another thread in
+        def __int__(self):
+            in_a_thread(lambda: taken.append(gen.take(8)))
+            return 8
+
+    taken.append(gen.take(Size()))
+    assert sorted(taken) == [0, 2] and gen.offset == 4
+    before = sys.getswitchinterval()
+    sys.setswitchinterval(1e-6)
+    try:
+        many = [threading.Thread(target=lambda: taken.extend([gen.take(1) for _ in range(3000)])) for _ in range(4)]
+        for t in many:
+            t.start()
+        for t in many:
+            t.join()
+    finally:
+        sys.setswitchinterval(before)
+    assert sorted(taken) == [0, 2] + list(range(4, 12004)) and gen.offset == 12004
+
+
+def test_a_recomputed_pass_and_other_threads():
+    """What another thread takes during a forward pass or its recomputation belongs to neither."""
+    from torch.utils.checkpoint import checkpoint
+    gen, taken, other = prior_ops.DropoutGenerator(3, device="cpu"), [], []
+
+    def block(x):
+        for _ in range(2):
+            taken.append(gen.take(x.numel()))
+            in_a_thread(lambda: other.append(gen.take(4)))
+            x = x.sin()
+        return x
+
+    x = torch.ones(8, requires_grad=True)
+    checkpoint(block, x, use_reentrant=False, context_fn=gen.recompute).sum().backward()
+    assert taken == [0, 3, 0, 3] and other == [2, 5, 6, 7] and gen.offset == 8
+
+
+def test_nested_recomputations_take_their_ranges_again():
+    from torch.utils.checkpoint import checkpoint
+    gen, taken = prior_ops.DropoutGenerator(3, device="cpu"), []
+
+    def inner(x):
+        taken.append(gen.take(8))
+        return x.sin().sin()
+
+    def outer(x):
+        taken.append(gen.take(4))
+        x = checkpoint(inner, x.sin(), use_reentrant=False, context_fn=gen.recompute)
+        taken.append(gen.take(12))
+        return x.sin().sin()
+
+    x = torch.ones(8, requires_grad=True)
+    y = checkpoint(outer, x, use_reentrant=False, context_fn=gen.recompute)
+    assert taken == [0, 1, 3] and gen.offset == 6
+    y.sum().backward()
+    assert taken[3:6] == [0, 1, 3] and set(taken[6:]) <= {1} and gen.offset == 6
+    plain = torch.ones(8, requires_grad=True)
+    plain.sin().sin().sin().sin().sin().sum().backward()
+    assert torch.allclose(x.grad, plain.grad)
+
+
+def test_a_recomputed_pass_that_takes_other_ranges_is_refused():
+    gen = prior_ops.DropoutGenerator(3)
+    first, again = gen.recompute()
+    with first:
+        gen.take(8)
+        gen.take(4)
+    for sizes in ((4,), (8, 8), (8, 4, 1)):
+        with pytest.raises(RuntimeError, match="recomputed"):
+            with again:
+                for n in sizes:
+                    gen.take(n)
+        assert gen.offset == 3
+    with again:
+        assert (gen.take(8), gen.take(4)) == (0, 2)
+    assert gen.take(1) == 3
+
+
+def test_a_pass_that_fails_leaves_nothing_behind():
+    """A forward pass or recomputation that raises ends its context; later ranges are not theirs."""
+    gen = prior_ops.DropoutGenerator(3)
+    first, again = gen.recompute()
+    with pytest.raises(KeyError):
+        with first:
+            gen.take(8)
+            raise KeyError
+    gen.take(4)
+    with pytest.raises(KeyError):
+        with again:
+            assert gen.take(8) == 0
+            raise KeyError
+    assert gen.take(4) == 3 and gen.offset == 4
+    with again:
+        assert gen.take(8) == 0
+        with pytest.raises(RuntimeError):                            # only the one range is its own
+            gen.take(4)
+
+
+@pytest.mark.parametrize("how", ["deepcopy", "pickle"])
+def test_copies_of_a_generator(how):
+    """A copy, as of a module that holds the generator, stands where the first one stood and goes its own way."""
+    import copy
+    import pickle
+    gen = prior_ops.DropoutGenerator(3, device="cpu", capturable=True)
+    gen.take(8)
+    gen.advance()
+    other = copy.deepcopy(gen) if how == "deepcopy" else pickle.loads(pickle.dumps(gen))
+    gen.advance()
+    assert gen.take(4) == 2 and (other.seed, other.offset, int(other.step)) == (3, 2, 1)
+    assert other.take(4) == 2 and gen.offset == other.offset == 3

@@ -87,7 +87,8 @@ class ResidualPrior(nn.Module):
     For deeper priors, ``norm`` puts a layer norm over the features of every voxel in front of each block and of the last
     convolution, and ``dropout`` regularises what a block adds (while training).  Residual add, dropout and the next block's norm
     are then one operator of the library (``prior_ops.dropout_add_layer_norm``), which stores no mask: the backward pass
-    draws it again from ``generator`` (a ``prior_ops.DropoutGenerator``, shared by all priors of a network)."""
+    draws it again from ``generator`` (a ``prior_ops.DropoutGenerator``, shared by all priors of a network).  An evaluation takes
+    no range of the generator.  Either option leaves a prior that can be differentiated once."""
 
     def __init__(self, features=16, blocks=2, norm=False, dropout=0.0, generator=None):
         super().__init__()
@@ -115,7 +116,10 @@ class ResidualPrior(nn.Module):
             w, b = self.norm_weight, self.norm_bias
             y = _p.layer_norm(f, w[0], b[0], dim=1)
             for k, blk in enumerate(self.blocks):
-                y, f = _p.dropout_add_layer_norm(blk(y), f, w[k + 1], b[k + 1], p, self.generator, dim=1)
+                u = blk(y)
+                if p == 0.0 and self.training and self.generator is not None:
+                    self.generator.take(u.numel())    # the ranges of the sites behind do not depend on this prior's p
+                y, f = _p.dropout_add_layer_norm(u, f, w[k + 1], b[k + 1], p, self.generator, dim=1)
             f = y
         else:
             for blk in self.blocks:

@@ -415,8 +415,9 @@ def dropout_add_layer_norm_vjp(grad_y, grad_total, total, weight, mean, rstd, p,
 # ---- autograd ------------------------------------------------------------------------------------------------------------
 
 class DropoutGenerator:
-    """Counter ranges for the dropout sites of a model: every call takes the range behind the last one, so no two share a mask,
-    whichever threads they come from.  A copy (``copy.deepcopy``, pickling) stands where the first one stood and goes its own way.
+    """Counter ranges for the dropout sites of a model: every call that drops takes the range behind the last one, so no two share
+    a mask, whichever threads they come from; p = 0, as in an evaluation, takes none.  A copy (``copy.deepcopy``, pickling)
+    stands where the first one stood and goes its own way.
 
     ``capturable=True`` adds a counter on the device that the kernels read when they run: a captured training step ends with
     ``advance()`` inside the graph, and every replay draws new masks with the ranges it was captured with.  The counter must
@@ -594,14 +595,22 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, dim=-1):
     return _LayerNorm.apply(x, weight, bias, eps, dim)
 
 
-def dropout(x, p, generator: DropoutGenerator, residual=None):
-    """[residual +] dropout(x) with the next range of the generator; the backward pass draws the mask again."""
-    return _Dropout.apply(x, residual, p, generator.seed, generator.take(x.numel()), generator.step)
+def _site(x, p, generator):
+    """(seed, offset, step) of a call.  Where nothing is dropped there is no mask: no range is taken and no counter read."""
+    if p == 0:
+        return 0, 0, None
+    if generator is None:
+        raise ValueError("dropout needs a generator")
+    return generator.seed, generator.take(x.numel()), generator.step
+
+
+def dropout(x, p, generator=None, residual=None):
+    """[residual +] dropout(x) with the next range of the generator, which may be None where p is 0; the backward pass draws the
+    mask again."""
+    return _Dropout.apply(x, residual, p, *_site(x, p, generator))
 
 
 def dropout_add_layer_norm(x, residual, weight, bias, p, generator=None, eps=1e-5, dim=-1):
     """(y, total) of the residual tail, with gradients; ``generator`` may be None where p is 0."""
-    if generator is None and p != 0:
-        raise ValueError("dropout needs a generator")
-    seed, offset, step = (0, 0, None) if generator is None else (generator.seed, generator.take(x.numel()), generator.step)
+    seed, offset, step = _site(x, p, generator)
     return _Tail.apply(x, residual, weight, bias, p, seed, offset, eps, dim, step)

@@ -208,3 +208,35 @@ def test_checkpointing_with_a_device_counter():
         got.append([h.detach(), leaf.grad] + [p.grad for p in prior.parameters()])
     for a, b in zip(*got):
         assert torch.equal(a, b)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("norm", [True, False])
+def test_an_evaluation_leaves_the_masks_of_the_training_alone(norm):
+    import paper_2207_08393_b200 as g
+    from paper_2207_08393_b200.gleam_loop import ResidualPrior
+    x = torch.randn(1, 2, 2, 1, 12, 10, device="cuda", generator=torch.Generator("cuda").manual_seed(5))
+    gen = g.DropoutGenerator(17)
+    torch.manual_seed(2)
+    prior = ResidualPrior(8, 2, norm=norm, dropout=0.3, generator=gen).cuda()
+    with torch.backends.cudnn.flags(enabled=True, benchmark=False, deterministic=True):
+        want = prior(x)
+        taken = gen.offset
+        gen.offset = 0
+        for _ in range(3):
+            prior.eval()(x)
+        assert gen.offset == 0 and taken > 0
+        assert torch.equal(prior.train()(x), want) and gen.offset == taken
+
+
+@pytest.mark.gpu
+def test_without_dropout_the_counter_does_not_matter():
+    """p = 0 reads no mask in the backward pass either, so the counter may move before it."""
+    import paper_2207_08393_b200 as g
+    gen = g.DropoutGenerator(1, capturable=True)
+    t = torch.randn(3, 8, 20, device="cuda", requires_grad=True)
+    y, total = g.dropout_add_layer_norm(t, t.detach(), None, None, 0.0, gen, dim=1)
+    z = g.dropout(t, 0.0, gen)
+    gen.advance()
+    (total + z).sum().backward()
+    assert gen.offset == 0 and torch.equal(t.grad, torch.full_like(t, 2.0))

@@ -382,3 +382,20 @@ def test_copies_of_a_generator(how):
     gen.advance()
     assert gen.take(4) == 2 and (other.seed, other.offset, int(other.step)) == (3, 2, 1)
     assert other.take(4) == 2 and gen.offset == other.offset == 3
+
+
+def test_where_nothing_is_dropped_no_range_is_taken(monkeypatch):
+    """p = 0 draws no mask: no range, no counter; also without a generator."""
+    for name in ("_Dropout", "_Tail"):
+        monkeypatch.setattr(prior_ops, name, type("Node", (), {"apply": staticmethod(lambda *a: a)}))
+    gen = prior_ops.DropoutGenerator(3, device="cpu", capturable=True)
+    x = torch.zeros(4, 8)
+    for p, g_ in ((0.0, gen), (0.0, None), (0, gen)):
+        assert prior_ops.dropout(x, p, g_) == (x, None, p, 0, 0, None)
+        assert prior_ops.dropout_add_layer_norm(x, x, None, None, p, g_)[4:] == (p, 0, 0, 1e-5, -1, None)
+        assert gen.offset == 0
+    assert prior_ops.dropout(x, 0.5, gen)[2:] == (0.5, 3, 0, gen.step) and gen.offset == 8
+    assert prior_ops.dropout_add_layer_norm(x, x, None, None, 0.5, gen)[4:] == (0.5, 3, 8, 1e-5, -1, gen.step) and gen.offset == 16
+    for call in (lambda: prior_ops.dropout(x, 0.5, None), lambda: prior_ops.dropout_add_layer_norm(x, x, None, None, 0.5)):
+        with pytest.raises(ValueError, match="generator"):
+            call()

@@ -354,6 +354,26 @@ def _flat(first, *others):
                      % (tuple(first.shape), " and ".join(str(tuple(t.stride())) for t in (first,) + others)))
 
 
+def _dense(x):
+    """A tensor like x whose elements have x's order in memory, without gaps."""
+    if x.is_contiguous():
+        return torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    axes = _memory_order(x)
+    t = torch.empty([x.shape[k] for k in axes], dtype=x.dtype, device=x.device)
+    return t.permute([axes.index(k) for k in range(x.dim())])
+
+
+def _residual_beside(x, t):
+    """``t`` itself if dropout takes it next to ``x`` or refuses it, else a copy in x's order."""
+    if t is None or t.shape != x.shape or t.dtype != x.dtype or t.device != x.device or x.numel() == 0:
+        return t
+    try:
+        _flat(x, t)
+    except ValueError:
+        return _dense(x).copy_(t)
+    return t
+
+
 def dropout_forward(x, p, seed, offset, residual=None, step=None):
     """[residual +] dropout(x).  The call takes ceil(x.numel() / 4) counters from ``offset``."""
     if _plain(x, residual):
@@ -366,12 +386,7 @@ def dropout_forward(x, p, seed, offset, residual=None, step=None):
             _same_kind(x, residual, "residual")
             others = (residual,)
         outer, slice_, pitch = (1, 0, ()) if x.numel() == 0 else _flat(x, *others)
-        if x.is_contiguous():
-            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        else:                                        # dense, in x's order
-            axes = _memory_order(x)
-            out = torch.empty([x.shape[k] for k in axes], dtype=x.dtype, device=x.device)
-            out = out.permute([axes.index(k) for k in range(x.dim())])
+        out = _dense(x)
     args = _drop_args(x, p, seed, offset, step)
     with _On(x):
         dims = _b.gleam_feature_dims(1, _DTYPES[x.dtype], _b.GLEAM_F32, 0.0, outer, 1, slice_, tuple(pitch),
@@ -415,9 +430,9 @@ def dropout_add_layer_norm_vjp(grad_y, grad_total, total, weight, mean, rstd, p,
 # ---- autograd ------------------------------------------------------------------------------------------------------------
 
 class DropoutGenerator:
-    """Counter ranges for the dropout sites of a model: every call that drops takes the range behind the last one, so no two share
-    a mask, whichever threads they come from; p = 0, as in an evaluation, takes none.  A copy (``copy.deepcopy``, pickling)
-    stands where the first one stood and goes its own way.
+    """Counter ranges for the dropout sites of a model: every call that drops takes the range behind the last one (a call that is
+    then refused spends it), so no two share a mask, whichever threads they come from; p = 0, as in an evaluation, takes none.
+    A copy (``copy.deepcopy``, pickling) stands where the first one stood and goes its own way.
 
     ``capturable=True`` adds a counter on the device that the kernels read when they run: a captured training step ends with
     ``advance()`` inside the graph, and every replay draws new masks with the ranges it was captured with.  The counter must
@@ -546,7 +561,7 @@ class _LayerNorm(torch.autograd.Function):
 class _Dropout(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, residual, p, seed, offset, step):
-        out = dropout_forward(x, p, seed, offset, residual, step)
+        out = dropout_forward(x, p, seed, offset, _residual_beside(x, residual), step)
         ctx.save_for_backward(step)
         ctx.args = p, seed, offset
         ctx.axes = _memory_order(x)

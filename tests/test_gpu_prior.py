@@ -692,3 +692,21 @@ def test_calls_from_several_threads():
     for a, b in zip(want, got):
         for u, v in zip(a, b):
             assert torch.equal(u, v)
+
+
+@pytest.mark.parametrize("p", [0.0, 0.5])
+def test_dropout_takes_a_residual_in_any_order(p):
+    """As the tail does: a residual (or x) in another memory order gives the values and gradients of x's order."""
+    import paper_2207_08393_b200 as g
+    x, r, c = (make((2, 6, 4, 5), "float32", k)[0] for k in range(3))
+    last = lambda t: t.to(memory_format=torch.channels_last)
+    for xo, ro in ((x, last(r)), (last(x), r), (last(x), r.transpose(2, 3).contiguous().transpose(2, 3)), (x, r[:1].expand(2, 6, 4, 5))):
+        got, want = [], []
+        for res, out in ((ro, got), (torch.empty_like(xo).copy_(ro), want)):
+            leaves = [xo.detach().requires_grad_(), res.detach().requires_grad_()]
+            y = g.dropout(leaves[0], p, g.DropoutGenerator(5), residual=leaves[1])
+            (y * c).sum().backward()
+            out += [y.detach()] + [t.grad for t in leaves]
+        for a, b in zip(got, want):
+            assert a.shape == b.shape and torch.equal(a, b)
+        assert got[0].stride() == xo.stride()

@@ -399,3 +399,23 @@ def test_where_nothing_is_dropped_no_range_is_taken(monkeypatch):
     for call in (lambda: prior_ops.dropout(x, 0.5, None), lambda: prior_ops.dropout_add_layer_norm(x, x, None, None, 0.5)):
         with pytest.raises(ValueError, match="generator"):
             call()
+
+
+@pytest.mark.parametrize("make", [
+    lambda: torch.empty(2, 6, 4, 5), lambda: torch.empty(2, 6, 4, 5).to(memory_format=torch.channels_last), lambda: torch.empty(9, 6)[:, :4],
+    lambda: torch.empty(7, 4).t(), lambda: torch.empty(3, 1, 5), lambda: torch.empty(5, 1), lambda: torch.empty(0, 3)])
+def test_a_residual_is_brought_into_the_order_of_x(make):
+    """What the call takes as it is stays as it is; another order of the same shape is copied into x's."""
+    x = make()
+    shape = tuple(x.shape)
+    values = torch.arange(float(x.numel())).view(shape)
+    turned = torch.empty(shape[::-1]).permute(*range(len(shape) - 1, -1, -1)).copy_(values)
+    spread = torch.empty(shape[:-1] + (2 * shape[-1],))[..., ::2].copy_(values)
+    for t in (values, turned, spread, torch.zeros(1).expand(shape)):
+        got = prior_ops._residual_beside(x, t)
+        assert torch.equal(got, t)
+        prior_ops._flat(x, got)                                      # refuses what the call cannot take
+    wide = torch.empty_strided(shape, x.stride()).copy_(values)
+    assert prior_ops._residual_beside(x, wide) is wide and prior_ops._residual_beside(x, None) is None
+    for other in (values.double(), values.to("meta"), torch.zeros(shape + (2,))):
+        assert prior_ops._residual_beside(x, other) is other         # for the call to refuse

@@ -432,7 +432,9 @@ def dropout_add_layer_norm_vjp(grad_y, grad_total, total, weight, mean, rstd, p,
 class DropoutGenerator:
     """Counter ranges for the dropout sites of a model: every call that drops takes the range behind the last one (a call that is
     then refused spends it), so no two share a mask, whichever threads they come from; p = 0, as in an evaluation, takes none.
-    A copy (``copy.deepcopy``, pickling) stands where the first one stood and goes its own way.
+    A copy (``copy.deepcopy``, pickling) stands where the first one stood and goes its own way.  A generator is no part of a
+    module's state: a run that is resumed loads the ``state_dict()`` saved with the optimiser's, or it would draw its first
+    masks again.
 
     ``capturable=True`` adds a counter on the device that the kernels read when they run: a captured training step ends with
     ``advance()`` inside the graph, and every replay draws new masks with the ranges it was captured with.  The counter must
@@ -487,6 +489,20 @@ class DropoutGenerator:
         """The contexts of a forward pass and of its recomputation, in which the ranges of the former are taken again."""
         first = _Ranges(self)
         return first, _RangesAgain(first)
+
+    def state_dict(self):
+        """Where the generator stands, in plain numbers (waits for the device's counter)."""
+        with self._lock:
+            return {"seed": self.seed, "offset": self.offset, "step": None if self.step is None else int(self.step)}
+
+    def load_state_dict(self, state):
+        seed, offset, step = int(state["seed"]), int(state["offset"]), state["step"]
+        if (step is None) != (self.step is None):
+            raise ValueError("a state with%s a counter for a generator with capturable=%s" % ("out" * (step is None), self.step is not None))
+        with self._lock:
+            self.seed, self.offset = seed, offset
+            if step is not None:
+                self.step.fill_(int(step))
 
     def advance(self):
         if self.step is None:

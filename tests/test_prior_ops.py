@@ -419,3 +419,26 @@ def test_a_residual_is_brought_into_the_order_of_x(make):
     assert prior_ops._residual_beside(x, wide) is wide and prior_ops._residual_beside(x, None) is None
     for other in (values.double(), values.to("meta"), torch.zeros(shape + (2,))):
         assert prior_ops._residual_beside(x, other) is other         # for the call to refuse
+
+
+@pytest.mark.parametrize("capturable", [False, True])
+def test_a_resumed_run_goes_on_where_it_was(tmp_path, capturable):
+    """Saved and loaded next to a model's and an optimiser's state; the counter stays the tensor that a graph may read."""
+    gen = prior_ops.DropoutGenerator(2 ** 63 + 5, device="cpu", capturable=capturable)
+    gen.take(8)
+    if capturable:
+        gen.advance()
+    torch.save({"generator": gen.state_dict()}, tmp_path / "run.pt")
+    gen.take(80)
+    later = prior_ops.DropoutGenerator(1, device="cpu", capturable=capturable)
+    step = later.step
+    later.load_state_dict(torch.load(tmp_path / "run.pt", weights_only=True)["generator"])
+    assert (later.seed, later.offset) == (2 ** 63 + 5, 2) and later.step is step
+    assert not capturable or int(step) == 1
+    assert later.take(4) == 2
+    with pytest.raises(ValueError, match="capturable"):
+        prior_ops.DropoutGenerator(1, device="cpu", capturable=not capturable).load_state_dict(gen.state_dict())
+    for bad in ({}, {"seed": 1, "offset": 2}, {"seed": 1, "offset": "x", "step": 1 if capturable else None}):
+        with pytest.raises((KeyError, ValueError)):
+            later.load_state_dict(bad)
+        assert later.offset == 3 and later.seed == 2 ** 63 + 5       # nothing is half loaded

@@ -497,12 +497,13 @@ class DropoutGenerator:
 
     def load_state_dict(self, state):
         seed, offset, step = int(state["seed"]), int(state["offset"]), state["step"]
+        step = None if step is None else int(step)
         if (step is None) != (self.step is None):
             raise ValueError("a state with%s a counter for a generator with capturable=%s" % ("out" * (step is None), self.step is not None))
         with self._lock:
             self.seed, self.offset = seed, offset
             if step is not None:
-                self.step.fill_(int(step))
+                self.step.fill_(step)
 
     def advance(self):
         if self.step is None:

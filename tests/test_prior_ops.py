@@ -442,3 +442,10 @@ def test_a_resumed_run_goes_on_where_it_was(tmp_path, capturable):
         with pytest.raises((KeyError, ValueError)):
             later.load_state_dict(bad)
         assert later.offset == 3 and later.seed == 2 ** 63 + 5       # nothing is half loaded
+
+
+def test_a_bad_counter_leaves_a_generator_as_it_was():
+    gen = prior_ops.DropoutGenerator(3, device="cpu", capturable=True)
+    with pytest.raises(ValueError):
+        gen.load_state_dict({"seed": 4, "offset": 5, "step": "x"})
+    assert (gen.seed, gen.offset, int(gen.step)) == (3, 0, 0)

@@ -100,6 +100,12 @@ def _check_kind(x):
         raise ValueError("expected CUDA tensors: there is no CPU fallback")
     if x.dtype not in _DTYPES:
         raise ValueError("type %s is not supported" % x.dtype)
+    _check_sign(x)
+
+
+def _check_sign(t):
+    if t.is_neg():                                   # a view that torch negates when it reads it
+        raise ValueError("memory holds the negated values: call .resolve_neg()")
 
 
 def _features_axis(x, dim):
@@ -116,6 +122,7 @@ def _same_kind(x, t, what):
     if t.shape != x.shape or t.dtype != x.dtype or t.device != x.device:
         raise ValueError("%s: %s %s on %s where %s %s on %s is wanted" % (what, tuple(t.shape), t.dtype, t.device,
                                                                          tuple(x.shape), x.dtype, x.device))
+    _check_sign(t)
 
 
 def _same(x, t, view, dim, what):
@@ -129,6 +136,7 @@ def _same(x, t, view, dim, what):
 
 def _match(x, t, dim):
     """``t`` itself if the calls take it next to ``x`` or refuse it, else a copy in x's order (cotangents come in any order)."""
+    t = t.resolve_neg()
     if t.shape != x.shape or t.dtype != x.dtype or t.device != x.device or (t.is_contiguous() and x.is_contiguous()):
         return t
     view = _view(x, dim)
@@ -147,8 +155,9 @@ def _weight_type(x, features, weight, bias=None):
     for w in (weight, bias):
         if w is None:
             continue
-        if w.dim() != 1 or w.numel() != features or w.get_device() != x.get_device() or not w.is_contiguous():
-            raise ValueError("weights: a contiguous vector of %d features on %s is wanted" % (features, x.device))
+        if w.dim() != 1 or w.numel() != features or w.get_device() != x.get_device() or not w.is_contiguous() or w.is_neg():
+            raise ValueError("weights: a contiguous vector of %d features on %s is wanted (.contiguous(), .resolve_neg())"
+                             % (features, x.device))
         if w.dtype not in (torch.float32, x.dtype) or kind not in (None, w.dtype):
             raise ValueError("weights: %s where float32 or %s is wanted, the same for all" % (w.dtype, x.dtype))
         kind = w.dtype
@@ -157,8 +166,8 @@ def _weight_type(x, features, weight, bias=None):
 
 def _check_statistics(x, shape, mean, rstd):
     for t in (mean, rstd):
-        if t.shape != shape or t.dtype != torch.float32 or t.get_device() != x.get_device() or not t.is_contiguous():
-            raise ValueError("statistics: contiguous float32 of shape %s is wanted" % (tuple(shape),))
+        if t.shape != shape or t.dtype != torch.float32 or t.get_device() != x.get_device() or not t.is_contiguous() or t.is_neg():
+            raise ValueError("statistics: contiguous float32 of shape %s is wanted (.contiguous(), .resolve_neg())" % (tuple(shape),))
 
 
 class _On:
@@ -220,13 +229,13 @@ def _call(x, dim, wtype, eps):
 
 def _plain(x, *others):
     """Whether all tensors are contiguous CUDA tensors of x's shape and type on the current device (None: not there)."""
-    if not isinstance(x, torch.Tensor) or not x.is_cuda or not x.is_contiguous() or x.numel() == 0 or x.dtype not in _DTYPES:
+    if not isinstance(x, torch.Tensor) or not x.is_cuda or not x.is_contiguous() or x.numel() == 0 or x.dtype not in _DTYPES or x.is_neg():
         return False
     device = x.get_device()
     if device != _current_device():
         return False
     for t in others:
-        if t is not None and not (t.is_contiguous() and t.shape == x.shape and t.dtype is x.dtype and t.get_device() == device):
+        if t is not None and (not (t.is_contiguous() and t.shape == x.shape and t.dtype is x.dtype and t.get_device() == device) or t.is_neg()):
             return False
     return True
 
@@ -367,6 +376,7 @@ def _residual_beside(x, t):
     """``t`` itself if dropout takes it next to ``x`` or refuses it, else a copy in x's order."""
     if t is None or t.shape != x.shape or t.dtype != x.dtype or t.device != x.device or x.numel() == 0:
         return t
+    t = t.resolve_neg()
     try:
         _flat(x, t)
     except ValueError:
@@ -591,7 +601,7 @@ class _Dropout(torch.autograd.Function):
         gx = None
         if ctx.needs_input_grad[0]:
             axes = ctx.axes                              # the mask numbers elements in x's memory order
-            gx = dropout_vjp(grad.permute(axes).contiguous(), *ctx.args, step=step)
+            gx = dropout_vjp(grad.permute(axes).contiguous().resolve_neg(), *ctx.args, step=step)
             gx = gx.permute([axes.index(k) for k in range(len(axes))])
         return gx, grad if ctx.needs_input_grad[1] else None, None, None, None, None
 

@@ -710,3 +710,27 @@ def test_dropout_takes_a_residual_in_any_order(p):
         for a, b in zip(got, want):
             assert a.shape == b.shape and torch.equal(a, b)
         assert got[0].stride() == xo.stride()
+
+
+@pytest.mark.parametrize("n", [1, 7])
+def test_numbers_that_torch_negates_when_it_reads_them(n):
+    """The imaginary part of a conjugate is memory with a negative bit: refused by the calls, resolved by the autograd nodes."""
+    import paper_2207_08393_b200 as g
+    lazy = torch.randn(n, 1, dtype=torch.complex64, device="cuda").conj().imag
+    plain = lazy.clone()
+    w = torch.randn(1, dtype=torch.complex64, device="cuda").conj().imag
+    assert lazy.is_neg() and w.is_neg() and not plain.is_neg()
+    y, mean, rstd = g.layer_norm_forward(plain)
+    for call in (lambda: g.dropout_forward(lazy, 0.5, 1, 0), lambda: g.dropout_forward(plain, 0.5, 1, 0, residual=lazy),
+                 lambda: g.layer_norm_forward(lazy), lambda: g.layer_norm_forward(plain, w), lambda: g.layer_norm_forward(plain, None, w),
+                 lambda: g.layer_norm_vjp(lazy, plain, None, mean, rstd), lambda: g.layer_norm_vjp(plain, plain, w, mean, rstd),
+                 lambda: g.dropout_add_layer_norm_forward(plain, lazy, None, None, 0.5, 1, 0)):
+        with pytest.raises(ValueError, match="resolve_neg"):
+            call()
+    for f in (lambda x, r: g.dropout(x, 0.5, g.DropoutGenerator(5), residual=r), lambda x, r: g.dropout_add_layer_norm(x, r, None, None, 0.5, g.DropoutGenerator(5))[1]):
+        assert torch.equal(f(plain, lazy), f(plain, plain))
+    leaf = plain.clone().requires_grad_()
+    want = torch.autograd.grad(g.dropout(leaf, 0.5, g.DropoutGenerator(5)), leaf, plain)[0]
+    assert torch.equal(torch.autograd.grad(g.dropout(leaf, 0.5, g.DropoutGenerator(5)), leaf, lazy)[0], want)
+    y, total = g.dropout_add_layer_norm(leaf, plain, None, None, 0.0)
+    assert torch.equal(torch.autograd.grad(total, leaf, lazy)[0], plain)

@@ -449,3 +449,10 @@ def test_a_bad_counter_leaves_a_generator_as_it_was():
     with pytest.raises(ValueError):
         gen.load_state_dict({"seed": 4, "offset": 5, "step": "x"})
     assert (gen.seed, gen.offset, int(gen.step)) == (3, 0, 0)
+
+
+def test_a_residual_or_cotangent_that_torch_negates_is_resolved():
+    x = torch.zeros(4, 1)
+    for lazy in (torch.randn(4, 1, dtype=torch.complex64).conj().imag, torch._neg_view(torch.randn(4, 1))):
+        for got in (prior_ops._match(x, lazy, 1), prior_ops._residual_beside(x, lazy)):
+            assert not got.is_neg() and torch.equal(got, lazy)

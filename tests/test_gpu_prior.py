@@ -734,3 +734,135 @@ def test_numbers_that_torch_negates_when_it_reads_them(n):
     assert torch.equal(torch.autograd.grad(g.dropout(leaf, 0.5, g.DropoutGenerator(5)), leaf, lazy)[0], want)
     y, total = g.dropout_add_layer_norm(leaf, plain, None, None, 0.0)
     assert torch.equal(torch.autograd.grad(total, leaf, lazy)[0], plain)
+
+
+# Slices that begin anywhere: maps of 128 positions or more whose inner length is odd or whose memory begins between pieces.
+
+@pytest.mark.parametrize("dtype", list(HALF))
+@pytest.mark.parametrize("shape,wide", [((3, 24, 133), (3, 31, 133)), ((2, 70, 391), (2, 73, 391)), ((2, 300, 129), (2, 301, 129)), ((3, 24, 256), (3, 25, 256))])
+@pytest.mark.parametrize("shift", [0, 1, 8])
+def test_slices_of_wider_arrays_that_begin_anywhere(shape, wide, dtype, shift):
+    test_slices_of_wider_arrays(shape, wide, 1, dtype, shift)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("features,inner", [(16, 131), (60, 133), (100, 515), (300, 129), (600, 131)])
+@pytest.mark.parametrize("outer", [1, 5])
+def test_what_lies_behind_slices_that_begin_anywhere_stays(outer, features, inner, dtype):
+    test_what_lies_behind_the_last_slice_stays(outer, features, inner, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("shape", [(2, 24, 133), (1, 70, 391), (2, 300, 129)])
+def test_outputs_in_place_of_slices_that_begin_anywhere(shape, dtype):
+    test_outputs_in_place_of_inputs(shape, dtype)
+
+
+@pytest.mark.parametrize("shape", [(2, 20, 133), (1, 300, 391), (3, 16, 1023)])
+def test_bad_values_in_slices_that_begin_anywhere(shape):
+    test_dropped_elements_may_hold_anything(shape)
+    test_a_bad_value_stays_in_its_position(shape)
+
+
+# Variances.  The features are whole numbers whose sums are exact in 32 bits in any order, so a mean (of all, or of a part that is
+# joined to the others) is off by at most two roundings, 2 U max|x|.  Squares of deviations from a mean that is off by e give var +
+# e^2; a join of parts with means m_w gives further 2 (m_w - m) e_w, summed over the parts at most 4 sd e.  A part whose squares
+# are taken about its first feature, k numbers d, leaves sum d^2 - (sum d)^2 / k, which is at least 1 / (k + 1) of sum d^2: with 1.5
+# roundings of the product and parts of at most 40 features that is 62 U of what is left.  With R = max|x| / sd the variance is
+# thus off by at most (8 R + chain + 64) U + (2 R U)^2 of itself.
+
+def variance_tolerance(x, rstd):
+    r = np.abs(x).max(1) * rstd
+    return (8 * r + chain(x.shape[1]) + 64) * U + (2 * r * U) ** 2
+
+
+def check_variance(x64, dtype):
+    import paper_2207_08393_b200 as g
+    x = torch.from_numpy(x64).cuda().to(dt(dtype))
+    assert np.array_equal(as64(x), x64) and np.abs(x64).sum(1).max() < 2 ** 24
+    y, mean, rstd = g.layer_norm_forward(x, None, None, EPS, dim=1)
+    ones = np.ones(x64.shape[1])
+    ry, rm, rr = po.layer_norm(x64, ones, 0 * ones, EPS)
+    t = variance_tolerance(x64, rr)
+    big = np.abs(x64).max(1)
+    near(mean, rm, 2 * U * big, "mean")
+    near(rstd, rr, t * rr, "rstd")
+    h = np.abs(ry)
+    near(y, ry, (2 * U * big * rr)[:, None] + h * (t[:, None] + 4 * U) + HALF[dtype] * h * 1.01 + TINY[dtype], "y")
+    return rr, t
+
+
+@pytest.mark.parametrize("dtype,base,step", [("float32", None, 1), ("float16", 2048, 2), ("bfloat16", 255, 1)])
+@pytest.mark.parametrize("shape", [(90, 31, 1), (40, 160, 1), (12, 513, 1), (9, 4099, 1), (2, 9001, 1), (2, 31, 40), (1, 60, 391), (1, 200, 64), (1, 300, 72),
+                                   (1, 640, 40), (1, 1500, 33)])
+def test_a_far_mean_costs_no_digits_of_the_variance(shape, dtype, base, step):
+    """Whole numbers around a mean of 100 to 10^5 standard deviations, as far as their sums stay exact.  The mean of the squares
+    less the square of the mean, in 32 bits, is beyond the tolerance on the same numbers."""
+    d = shape[1]
+    base = min(base, 2 ** 23 // d // step * step) if base else 2 ** 23 // d
+    x64 = base + step * np.random.default_rng(d).integers(-1, 2, size=shape).astype(np.float64)
+    rr, t = check_variance(x64, dtype)
+    x32 = x64.astype(np.float32)
+    m, s = x32.sum(1, dtype=np.float32) / np.float32(d), (x32 * x32).sum(1, dtype=np.float32) / np.float32(d)
+    bad = 1.0 / np.sqrt(np.maximum(s - m * m, 0).astype(np.float64) + EPS)
+    assert (np.abs(bad - rr) > t * rr).any()
+
+
+@pytest.mark.parametrize("dtype", list(HALF))
+@pytest.mark.parametrize("part", [8, 16, 32, 40])
+@pytest.mark.parametrize("shape", [(5, 31, 1), (3, 1003, 1), (2, 60, 40), (1, 128, 391), (1, 200, 64), (1, 300, 72), (2, 640, 40), (1, 700, 64)])
+def test_features_that_stand_out(shape, part, dtype):
+    """Every part's first feature thirty standard deviations from the others."""
+    x64 = np.random.default_rng(part).integers(-3, 4, size=shape).astype(np.float64)
+    x64[:, ::part] += 64
+    check_variance(x64, dtype)
+
+
+def kept_at(start, count, p, seed, offset):
+    return po.words(count + 3, seed, offset + start // 4)[start % 4:][:count] >= np.uint64(int(p * 2 ** 32))
+
+
+@pytest.mark.parametrize("features,inner", [(4096, 1), (4099, 1), (24, 1), (9001, 1), (64, 2 ** 26 + 64), (64, 2 ** 26 + 65), (700, 2 ** 23)])
+def test_tails_beyond_32_bits(features, inner):
+    """The residual tail and its VJP on more than 2^32 elements in bf16, outputs in place of inputs, against the definition at
+    positions whose elements lie at both ends of the array and around the powers of two."""
+    import paper_2207_08393_b200 as g
+    from paper_2207_08393_b200 import binding
+    outer = 2 ** 32 // features + 3 if inner == 1 else 1
+    shape, p, seed, offset = (outer, features, inner), 0.5, 9, 2 ** 33 + 1
+    assert outer * features * inner > 2 ** 32
+    gen = torch.Generator("cuda").manual_seed(features)
+    x, res = (torch.empty(shape, dtype=torch.bfloat16, device="cuda").normal_(generator=gen) for _ in range(2))
+    w, w64, b, b64 = weights(features, "float32", 1)
+    if inner == 1:
+        at = sorted({0, 1, 2 ** 31 // features, 2 ** 32 // features - 1, 2 ** 32 // features, outer - 1})
+        pick = lambda t: t[at]
+        keep = np.stack([kept_at(r * features, features, p, seed, offset) for r in at])[:, :, None]
+        stats = lambda t: as64(t[at])
+    else:
+        runs = ((0, 64), (2 ** 31 % inner // 2 + 64, 8), (inner // 2, 8), (inner - 64, 64))
+        at = torch.cat([torch.arange(k, k + n) for k, n in runs]).cuda()
+        pick = lambda t: t[:, :, at]
+        keep = np.stack([np.concatenate([kept_at(c * inner + k, n, p, seed, offset) for k, n in runs]) for c in range(features)])[None]
+        stats = lambda t: as64(t[:, at])
+    x64, r64 = as64(pick(x)), as64(pick(res))
+    mean, rstd = (torch.empty((outer, inner), device="cuda") for _ in range(2))
+    m = g.make_dropout_args(p, seed, offset)
+    dims = binding.make_feature_dims(binding.GLEAM_BF16, 0, *shape, eps=EPS, stream=torch.cuda.current_stream())
+    g.gleam_dropout_add_layer_norm_forward(x, res, w, b, res, x, mean, rstd, m, dims)
+    want = torch.from_numpy((r64 + x64 * keep * 2.0).astype(np.float32)).to(torch.bfloat16)
+    assert torch.equal(pick(res).cpu(), want)
+    t64 = as64(want)
+    ry, rm, rr = po.layer_norm(t64, w64, b64, EPS)
+    ty, tm, tr = norm_tolerances(t64, w64, rm, rr, ry, "bfloat16")
+    near(pick(x), ry, ty + U * np.abs(b64)[None, :, None], "y")
+    near(torch.from_numpy(stats(mean)), rm, tm, "mean")
+    near(torch.from_numpy(stats(rstd)), rr, tr, "rstd")
+    x.normal_(generator=gen)                                   # the cotangent of y
+    dy64, m64, s64 = as64(pick(x)), stats(mean), stats(rstd)
+    g.gleam_dropout_add_layer_norm_vjp(x, None, res, w, mean, rstd, x, res, None, None, m, dims)
+    rx = po.layer_norm_vjp(dy64, t64, w64, m64, s64)[0]
+    td = vjp_tolerances(dy64, t64, w64, m64, s64, "bfloat16", "float32")[0]
+    near(pick(res), rx, td + HALF["bfloat16"] * np.abs(rx) * 1.01, "grad_residual")
+    rx = rx * keep * 2.0
+    near(pick(x), rx, 2 * td + HALF["bfloat16"] * np.abs(rx) * 1.01, "grad_x")

@@ -240,3 +240,77 @@ def test_without_dropout_the_counter_does_not_matter():
     gen.advance()
     (total + z).sum().backward()
     assert gen.offset == 0 and torch.equal(t.grad, torch.full_like(t, 2.0))
+
+
+def composite(prior, x, kept, scale):
+    """The prior with the library's operators restated in torch: the same convolutions, sums and norms in 64 bits that are rounded
+    where the operators round."""
+    def norm(v, k):
+        v64 = v.double()
+        mean = v64.mean(1, keepdim=True)
+        rstd = 1.0 / torch.sqrt(((v64 - mean) ** 2).mean(1, keepdim=True) + 1e-5)
+        w, b = prior.norm_weight[k].double().view(1, -1, 1, 1), prior.norm_bias[k].double().view(1, -1, 1, 1)
+        return ((v64 - mean) * rstd * w + b).float().to(v.dtype)
+
+    B, _, T, n0, n1, n2 = x.shape
+    h = x.permute(0, 2, 3, 1, 4, 5).reshape(B * T * n0, 2, n1, n2)
+    f = prior.head(h)
+    y = norm(f, 0) if prior.norm_weight is not None else f
+    for k, blk in enumerate(prior.blocks):
+        u = blk(y)
+        f = (f.double() + torch.where(kept[k], u.double() * scale, 0.0)).float().to(f.dtype)
+        y = norm(f, k + 1) if prior.norm_weight is not None else f
+    out = h + prior.tail(y)
+    return out.reshape(B, T, n0, 2, n1, n2).permute(0, 3, 1, 2, 4, 5)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("norm", [True, False])
+@pytest.mark.parametrize("last", [False, True])
+@pytest.mark.parametrize("kind", ["float32", "float16", "bfloat16"])
+def test_a_prior_under_autocast_and_with_features_last(kind, last, norm):
+    """Autocast hands the operators 16-bit maps with 32-bit weights, channels_last rows of features; the default 16 features.
+
+    Against the restatement on the same convolutions.  In 16 bits (u half a step) a value that the operators' 32 bits leave on the other
+    side of a border of the type is off by 2 u; fewer than one in a thousand are, so that a map is off by less than 0.1 u in L2, and
+    four norms and the convolutions between them make less than 4 u of it.  The restatement's gradients have up to two
+    roundings more in each of three blocks, threefold by the convolutions and norms: less than 20 u.  A wrong mask is
+    off by more than 0.3."""
+    import paper_2207_08393_b200 as g
+    from paper_2207_08393_b200 import gleam_loop as gl
+    p, seed, n1, n2 = 0.3, 23, 21, 26
+    torch.manual_seed(4)
+    gen = g.DropoutGenerator(seed)
+    gen.take(40)
+    prior = gl.ResidualPrior(16, 3, norm=norm, dropout=p, generator=gen).cuda()
+    for t in prior.parameters():
+        t.data.add_(0.05 * torch.randn_like(t))
+    if last:
+        prior = prior.to(memory_format=torch.channels_last)
+    x = torch.randn(2, 2, 3, 1, n1, n2, device="cuda")
+    shape, order = ((6, n1, n2, 16), (0, 3, 1, 2)) if last else ((6, 16, n1, n2), (0, 1, 2, 3))
+    count = 6 * 16 * n1 * n2 // 4
+    kept = [torch.from_numpy(po.kept(shape, p, seed, 10 + k * count)).cuda().permute(order) for k in range(3)]
+    half = {"float32": 2.0 ** -24, "float16": 2.0 ** -11, "bfloat16": 2.0 ** -8}[kind]
+    seen, grads, outs = [], [], []
+    prior.head.register_forward_hook(lambda m, i, o: seen.append(o))
+    cot = torch.randn_like(x)
+    allow = torch.backends.cudnn.allow_tf32
+    torch.backends.cudnn.allow_tf32 = False
+    try:
+        with torch.backends.cudnn.flags(enabled=True, benchmark=False, deterministic=True, allow_tf32=False):
+            for f in (prior, lambda v: composite(prior, v, kept, po.scale(p))):
+                leaf = x.clone().requires_grad_()
+                with torch.autocast("cuda", dtype=getattr(torch, kind), enabled=kind != "float32"):
+                    out = f(leaf)
+                outs.append(out.detach())
+                grads.append(torch.autograd.grad(out, [leaf] + list(prior.parameters()), cot))
+    finally:
+        torch.backends.cudnn.allow_tf32 = allow
+    assert seen[0].dtype == getattr(torch, kind)
+    assert seen[0].is_contiguous(memory_format=torch.channels_last if last else torch.contiguous_format)
+    off = lambda a, b: float((a.double() - b.double()).norm() / b.double().norm())
+    # 32 bits: convolutions in another order for another input leave some 1e-6
+    assert off(outs[0], outs[1]) <= (1e-5 if kind == "float32" else 4 * half)
+    for a, b in zip(*grads):
+        assert off(a, b) <= (1e-4 if kind == "float32" else 20 * half)

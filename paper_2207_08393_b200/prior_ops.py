@@ -151,11 +151,11 @@ def _match(x, t, dim):
 
 def _weight_type(x, features, weight, bias=None):
     """The type of the weights.  None stands for ones or zeros."""
-    kind = None
+    kind, device = None, x.get_device()
     for w in (weight, bias):
         if w is None:
             continue
-        if w.dim() != 1 or w.numel() != features or w.get_device() != x.get_device() or not w.is_contiguous() or w.is_neg():
+        if w.dim() != 1 or w.numel() != features or w.get_device() != device or not w.is_contiguous() or w.is_neg():
             raise ValueError("weights: a contiguous vector of %d features on %s is wanted (.contiguous(), .resolve_neg())"
                              % (features, x.device))
         if w.dtype not in (torch.float32, x.dtype) or kind not in (None, w.dtype):
@@ -165,8 +165,9 @@ def _weight_type(x, features, weight, bias=None):
 
 
 def _check_statistics(x, shape, mean, rstd):
+    device = x.get_device()
     for t in (mean, rstd):
-        if t.shape != shape or t.dtype != torch.float32 or t.get_device() != x.get_device() or not t.is_contiguous() or t.is_neg():
+        if t.shape != shape or t.dtype != torch.float32 or t.get_device() != device or not t.is_contiguous() or t.is_neg():
             raise ValueError("statistics: contiguous float32 of shape %s is wanted (.contiguous(), .resolve_neg())" % (tuple(shape),))
 
 
@@ -374,7 +375,9 @@ def _dense(x):
 
 def _residual_beside(x, t):
     """``t`` itself if dropout takes it next to ``x`` or refuses it, else a copy in x's order."""
-    if t is None or t.shape != x.shape or t.dtype != x.dtype or t.device != x.device or x.numel() == 0:
+    if t is None or (t.is_contiguous() and x.is_contiguous() and not t.is_neg()):
+        return t
+    if t.shape != x.shape or t.dtype != x.dtype or t.device != x.device:
         return t
     t = t.resolve_neg()
     try:

@@ -218,7 +218,7 @@ _new_dims = _b.gleam_feature_dims.from_buffer_copy
 
 
 def _call(x, dim, wtype, eps):
-    key = (x.shape, x.dtype, dim, wtype, eps)
+    key = (x.shape, x.dtype, dim, wtype, float(eps))
     c = _CALLS.get(key)
     if c is None:
         c = _Call(x, dim, wtype, eps)

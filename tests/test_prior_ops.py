@@ -456,3 +456,14 @@ def test_a_residual_or_cotangent_that_torch_negates_is_resolved():
     for lazy in (torch.randn(4, 1, dtype=torch.complex64).conj().imag, torch._neg_view(torch.randn(4, 1))):
         for got in (prior_ops._match(x, lazy, 1), prior_ops._residual_beside(x, lazy)):
             assert not got.is_neg() and torch.equal(got, lazy)
+
+
+def test_kept_structures_go_by_the_value_of_eps(monkeypatch):
+    """eps may be anything that is a number, a tensor too, whose value can change between calls."""
+    monkeypatch.setattr(prior_ops, "_check_kind", lambda x: None)
+    monkeypatch.setattr(prior_ops, "_stream", lambda x: 0)
+    x, eps = torch.zeros(4, 8), torch.tensor(0.5)
+    for value in (0.5, 0.25):
+        eps.fill_(value)
+        c = prior_ops._call(x, -1, torch.float32, eps)
+        assert prior_ops._new_dims(c.template).eps == value

@@ -167,7 +167,7 @@ def _weight_type(x, features, weight, bias=None):
 def _check_statistics(x, shape, mean, rstd):
     device = x.get_device()
     for t in (mean, rstd):
-        if t.shape != shape or t.dtype != torch.float32 or t.get_device() != device or not t.is_contiguous() or t.is_neg():
+        if t.shape != shape or t.dtype is not torch.float32 or t.get_device() != device or not t.is_contiguous() or t.is_neg():
             raise ValueError("statistics: contiguous float32 of shape %s is wanted (.contiguous(), .resolve_neg())" % (tuple(shape),))
 
 
@@ -229,14 +229,15 @@ def _call(x, dim, wtype, eps):
 
 
 def _plain(x, *others):
-    """Whether all tensors are contiguous CUDA tensors of x's shape and type on the current device (None: not there)."""
-    if not isinstance(x, torch.Tensor) or not x.is_cuda or not x.is_contiguous() or x.numel() == 0 or x.dtype not in _DTYPES or x.is_neg():
+    """Whether all tensors are contiguous CUDA tensors of x's shape and type on the current device (None: not there), with the
+    values that their memory holds."""
+    if not isinstance(x, torch.Tensor) or not x.is_cuda or not x.is_contiguous() or x.numel() == 0 or x.is_neg():
         return False
-    device = x.get_device()
-    if device != _current_device():
+    device, shape, dtype = x.get_device(), x.shape, x.dtype
+    if device != _current_device() or dtype not in _DTYPES:
         return False
     for t in others:
-        if t is not None and (not (t.is_contiguous() and t.shape == x.shape and t.dtype is x.dtype and t.get_device() == device) or t.is_neg()):
+        if t is not None and not (t.is_contiguous() and t.shape == shape and t.dtype is dtype and t.get_device() == device and not t.is_neg()):
             return False
     return True
 

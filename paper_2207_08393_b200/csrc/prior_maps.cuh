@@ -255,9 +255,11 @@ __global__ void __launch_bounds__(MAP_TILE_WARPS * 32, ITEMS <= 16 ? 2 : 1) map_
         }
         copies_commit();
     };
-    // the warp's features of every position: their sum and the squared deviations from their mean.  The latter come from sums
-    // relative to the first feature; as that is one of them, what the difference cancels is at most as many times the result as
-    // there are features.
+    // the warp's features of every position: their sum and the squared deviations from their mean, in one pass.  The latter come
+    // from sums relative to the first feature, q - s^2 / k of k numbers; as the first is one of them, the result is at least q / (k
+    // + 1), so that the rounding of s^2 / k costs up to k + 1 times itself (k is at most 40) where that feature stands out, and a
+    // far mean costs nothing.  Relative error of the variance, worst of 16384 positions: normal values 4e-7 (k = 8) to 7e-7 (40;
+    // two passes, as on rows, 3e-7), every share's first feature thirty standard deviations away 1e-6 to 1e-5.
     auto statistics = [&](auto whole_tile, Two (&sum_of)[PAIRS<VP>], Two (&dev)[PAIRS<VP>]) {
         constexpr bool FULL = decltype(whole_tile)::value;
         Two pivot[PAIRS<VP>], s[PAIRS<VP>], q[PAIRS<VP>];

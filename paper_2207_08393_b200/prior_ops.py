@@ -4,7 +4,7 @@ Two layers over the C calls (include/gleam.h states the formulas and the definit
 
 * ``*_forward`` / ``*_vjp``: one C call each on plain tensors; outputs are allocated, the workspace comes from torch's
   allocator for the current stream, nothing is kept between calls;
-* ``layer_norm``, ``dropout``, ``dropout_add_layer_norm``: the same as autograd nodes.
+* ``layer_norm``, ``dropout``, ``dropout_add_layer_norm``: the same as autograd nodes, which can be differentiated once.
 
 Tensors are CUDA tensors of float32, float16 or bfloat16, all of one type and shape; weights are float32 or of that type.
 ``dim`` is the axis of the features.  A tensor may be a slice of a wider one along an axis before ``dim`` or along ``dim`` itself,

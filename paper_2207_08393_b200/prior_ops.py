@@ -172,11 +172,11 @@ def _check_statistics(x, shape, mean, rstd):
 
 
 class _On:
-    """The tensor's device as the current one, for a call's duration."""
+    """The tensor's device as the current one, for a call's duration (None: it is)."""
     __slots__ = ("other",)
 
     def __init__(self, x):
-        self.other = None if x.get_device() == _current_device() else torch.cuda.device(x.device)
+        self.other = None if x is None or x.get_device() == _current_device() else torch.cuda.device(x.device)
 
     def __enter__(self):
         if self.other is not None:
@@ -185,6 +185,9 @@ class _On:
     def __exit__(self, *a):
         if self.other is not None:
             self.other.__exit__(*a)
+
+
+_HERE = _On(None)
 
 
 def _current_device():
@@ -274,7 +277,7 @@ def _workspace(x, dims, wanted):
 class _Prepared:
     """Views, outputs' layout and structure of one norm call on the tensors x, *others: the general way, or from the kept
     table where all are plain."""
-    __slots__ = ("dim", "features", "wtype", "stats", "view", "dims", "scratch")
+    __slots__ = ("dim", "features", "wtype", "stats", "view", "dims", "scratch", "device")
 
     def __init__(self, x, dim, eps, weight, bias, *others):
         if _plain(x, *[t for t, _ in others]):
@@ -285,6 +288,7 @@ class _Prepared:
             self.dim, self.features, self.stats, self.view, self.scratch = c.dim, c.features, c.stats, None, c.scratch
             self.dims = _new_dims(c.template)
             self.dims.stream = _b._current_stream_handle() or None
+            self.device = _HERE
             return
         self.dim = dim = _features_axis(x, dim)
         self.view = v = _view(x, dim)
@@ -294,6 +298,7 @@ class _Prepared:
         self.stats = x.shape[:dim] + x.shape[dim + 1:]
         self.scratch = None
         self.dims = _dims(x, self.wtype, v, eps, tuple([u.pitch for u in views]))
+        self.device = _On(x)
 
     def like(self, x):
         return torch.empty_like(x) if self.view is None else _like(x, self.dim, self.view)
@@ -327,7 +332,7 @@ def layer_norm_forward(x, weight=None, bias=None, eps=1e-5, dim=-1):
     c = _Prepared(x, dim, eps, weight, bias, (None, "x"))
     y = c.like(x)
     mean, rstd = c.statistics(x)
-    with _On(x):
+    with c.device:
         _b.gleam_layer_norm_forward(x, weight, bias, y, mean, rstd, c.dims)
     return y, mean, rstd
 
@@ -338,7 +343,7 @@ def layer_norm_vjp(grad_y, x, weight, mean, rstd, dim=-1, weight_grad=True, bias
     _check_statistics(x, c.stats, mean, rstd)
     gx = c.like(x)
     gw, gb = c.vectors(x, weight, weight_grad, bias_grad)
-    with _On(x):
+    with c.device:
         ws = c.workspace(x, weight_grad or bias_grad)
         _b.gleam_layer_norm_vjp(grad_y, x, weight, mean, rstd, gx, gw, gb, c.dims)
     del ws
@@ -391,7 +396,7 @@ def _residual_beside(x, t):
 def dropout_forward(x, p, seed, offset, residual=None, step=None):
     """[residual +] dropout(x).  The call takes ceil(x.numel() / 4) counters from ``offset``."""
     if _plain(x, residual):
-        outer, slice_, pitch = 1, x.numel(), ()
+        outer, slice_, pitch, device = 1, x.numel(), (), _HERE
         out = torch.empty_like(x)
     else:
         _check_kind(x)
@@ -400,9 +405,9 @@ def dropout_forward(x, p, seed, offset, residual=None, step=None):
             _same_kind(x, residual, "residual")
             others = (residual,)
         outer, slice_, pitch = (1, 0, ()) if x.numel() == 0 else _flat(x, *others)
-        out = _dense(x)
+        out, device = _dense(x), _On(x)
     args = _drop_args(x, p, seed, offset, step)
-    with _On(x):
+    with device:
         dims = _b.gleam_feature_dims(1, _DTYPES[x.dtype], _b.GLEAM_F32, 0.0, outer, 1, slice_, tuple(pitch),
                                      _stream(x) or None, None, 0)
         _b.gleam_dropout_forward(x, residual, out, args, dims)
@@ -421,7 +426,7 @@ def dropout_add_layer_norm_forward(x, residual, weight, bias, p, seed, offset, e
     args = _drop_args(x, p, seed, offset, step)
     y, total = c.like(x), c.like(x)
     mean, rstd = c.statistics(x)
-    with _On(x):
+    with c.device:
         _b.gleam_dropout_add_layer_norm_forward(x, residual, weight, bias, total, y, mean, rstd, args, c.dims)
     return y, total, mean, rstd
 
@@ -434,7 +439,7 @@ def dropout_add_layer_norm_vjp(grad_y, grad_total, total, weight, mean, rstd, p,
     args = _drop_args(total, p, seed, offset, step)
     gx, gr = c.like(total), c.like(total)
     gw, gb = c.vectors(total, weight, weight_grad, bias_grad)
-    with _On(total):
+    with c.device:
         ws = c.workspace(total, weight_grad or bias_grad)
         _b.gleam_dropout_add_layer_norm_vjp(grad_y, grad_total, total, weight, mean, rstd, gx, gr, gw, gb, args, c.dims)
     del ws

@@ -339,6 +339,51 @@ GLEAM_API int gleam_dropout_add_layer_norm_vjp(const void* grad_y, const void* g
                                                const gleam_feature_dims* dims);
 GLEAM_API int gleam_layer_norm_workspace_size(const gleam_feature_dims* dims, uint64_t* bytes);
 
+/* ---- gated recurrence: a prior that looks along frames, sections or tokens --------------------------------
+ * Arrays are (batch, channels, steps, inner) with contiguous inner: every (batch, channel, inner) index is a chain of its own along
+ * the steps.  inner = voxels: feature maps with the frames in between; channels = 1, inner = features: rows of features one
+ * after the other; inner = 1: series with the steps last in memory.
+ *
+ *   recurrence     f_t = 1 / (1 + exp(-gate_t)),  h_t = f_t h_(t-1) + (1 - f_t) x_t,  y = h in the arrays' type,  last = h behind
+ *                  the last step;  steps run 0, 1, ... or (reverse) the other way.  A gate of +inf keeps the state, one of -inf
+ *                  forgets it.
+ *   its VJP        D_t = grad_y_t + c_t,  c_t = f_(t+1) D_(t+1) (grad_last behind the last step),  grad_x = D (1 - f),
+ *                  grad_gate = D (h_(t-1) - x) f (1 - f),  grad_state = f_0 D_0
+ *   step           state <- f state + (1 - f) x,  y = state:  one step (steps = 1, no lengths) with the state updated in place
+ *
+ * lengths (int32, one for each example, device, read when the kernels run; below 0 counts as 0, above steps as steps): steps from
+ * lengths[b] on are not there.  Their x, gate and grad_y are not read, the state passes them unchanged, and y, grad_x and
+ * grad_gate are 0 there.  An example without steps returns its state as last.
+ *
+ * x, gate, y and their cotangents have type dtype; states, their cotangents and saved are float32, (batch, channels, inner),
+ * contiguous.  state, grad_last null = zeros; last, saved, grad_state null = not wanted.  All arithmetic is in 32 bits, the VJP's
+ * h_(t-1) included: the forward call saves the states at a few steps (saved, gleam_gated_scan_saved_size() bytes, 16-byte aligned),
+ * from which the VJP, given the same sizes, x, gate, state and lengths, computes the others again.  Nothing that a call writes
+ * may overlap anything else of the call, measured from an array's first to its last byte (GLEAM_ERR_ALIAS), but for the step's
+ * state.  Results are deterministic.  Two calls whose GPU work may overlap need workspaces of their own.
+ */
+#define GLEAM_SCAN_DIMS_VERSION 1
+typedef struct {
+    int32_t struct_version;   /* GLEAM_SCAN_DIMS_VERSION */
+    int32_t dtype;            /* GLEAM_F32, GLEAM_F16 or GLEAM_BF16 */
+    int32_t reverse;          /* 0 or 1 */
+    int32_t reserved;         /* 0 */
+    int64_t batch, channels, steps, inner;
+    int64_t stride[5][3];     /* elements from one example, channel, step to the next, for each activation array in the order of the
+                                 call's arguments; all three 0 = contiguous.  In any order of size, but no two elements share memory */
+    const int32_t* lengths;   /* or null */
+    void* stream;
+    void* workspace;          /* gleam_gated_scan_workspace_size() bytes, 256-byte aligned; not for the step */
+    uint64_t workspace_bytes;
+} gleam_scan_dims;
+GLEAM_API int gleam_gated_scan_forward(const void* x, const void* gate, const float* state, void* y, float* last, float* saved,
+                                       const gleam_scan_dims* dims);
+GLEAM_API int gleam_gated_scan_vjp(const void* grad_y, const float* grad_last, const void* x, const void* gate, const float* state,
+                                   const float* saved, void* grad_x, void* grad_gate, float* grad_state, const gleam_scan_dims* dims);
+GLEAM_API int gleam_gated_step(const void* x, const void* gate, float* state, void* y, const gleam_scan_dims* dims);
+GLEAM_API int gleam_gated_scan_workspace_size(const gleam_scan_dims* dims, uint64_t* bytes);
+GLEAM_API int gleam_gated_scan_saved_size(const gleam_scan_dims* dims, uint64_t* bytes);
+
 /* ---- gradients of Eq. 3 with respect to the step size and the measurements --------------------------
  * out = x - eta A^H (A x - y) is linear in eta and affine in y.  For a cotangent g = grad_out of the
  * output (conjugate-Wirtinger convention, as for gleam_dc_vjp):
@@ -407,7 +452,9 @@ enum {
     GLEAM_K_CG_VEC = 9,       /* image-sized vector kernels of the conjugate-gradient solve */
     GLEAM_K_FUSED3D = 10,     /* persistent kernel of the separable 3-D path (all three passes) */
     GLEAM_K_PRIOR = 11,       /* layer norm, dropout and residual tail of the learned prior */
-    GLEAM_K_CLASSES = 12
+    GLEAM_K_SCAN = 12,        /* gated recurrence */
+    GLEAM_K_ORTHO = 13,       /* orthogonalised updates */
+    GLEAM_K_CLASSES = 14
 };
 GLEAM_API uint64_t gleam_dc_launch_count(void);
 /* FP32 FMA throughput of the current device in TFLOP/s (2 flop per FMA), from a kernel of independent FMA

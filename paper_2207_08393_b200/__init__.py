@@ -20,3 +20,8 @@ from .prior_ops import (  # noqa: F401
     DropoutGenerator, dropout, dropout_add_layer_norm, dropout_add_layer_norm_forward, dropout_add_layer_norm_vjp,
     dropout_forward, dropout_vjp, layer_norm, layer_norm_forward, layer_norm_vjp,
 )
+from .binding import (  # noqa: F401
+    gleam_gated_scan_forward, gleam_gated_scan_saved_size, gleam_gated_scan_vjp, gleam_gated_scan_workspace_size,
+    gleam_gated_step, gleam_scan_dims, make_scan_dims,
+)
+from .scan_ops import gated_scan, gated_scan_forward, gated_scan_vjp, gated_step  # noqa: F401

@@ -76,7 +76,11 @@ def build(force: bool = False, verbose: bool = False) -> str:
             jobs.insert(0, (["nvcc"] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) +        # the longest of all: first
                             ["-DGLEAM_PRIOR_TYPE=%d" % kind, "-DGLEAM_PRIOR_VJP=%d" % vjp, "-c",
                              os.path.join(CSRC, "kernels_prior_maps.cu"), "-o", obj], obj))
-    for name in ("gleam_dc", "kernels_fused", "modl_cg", "prior_ops"):
+    for kind in range(3):
+        obj = os.path.join(BUILD, "kernels_scan%d.o" % kind)
+        jobs.append((["nvcc"] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) +
+                     ["-DGLEAM_SCAN_TYPE=%d" % kind, "-c", os.path.join(CSRC, "kernels_scan.cu"), "-o", obj], obj))
+    for name in ("gleam_dc", "kernels_fused", "modl_cg", "prior_ops", "scan_ops"):
         obj = os.path.join(BUILD, name + ".o")
         jobs.append((["nvcc"] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) +
                      ["-c", os.path.join(CSRC, name + ".cu"), "-o", obj], obj))

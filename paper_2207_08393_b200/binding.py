@@ -47,10 +47,12 @@ EXPORTS = ["gleam_dc_forward", "gleam_dc_vjp", "gleam_dc_workspace_size", "gleam
            "gleam_measure_fp32_peak", "gleam_dc_rowtile_split",
            "gleam_layer_norm_forward", "gleam_layer_norm_vjp", "gleam_layer_norm_workspace_size",
            "gleam_dropout_forward", "gleam_dropout_vjp",
-           "gleam_dropout_add_layer_norm_forward", "gleam_dropout_add_layer_norm_vjp"]
+           "gleam_dropout_add_layer_norm_forward", "gleam_dropout_add_layer_norm_vjp",
+           "gleam_gated_scan_forward", "gleam_gated_scan_vjp", "gleam_gated_step", "gleam_gated_scan_workspace_size",
+           "gleam_gated_scan_saved_size"]
 
 KERNEL_CLASSES = ["zmap", "col_z", "row_fused", "row_fwd", "col_mid_sep", "row_inv", "col_mid_full", "col_fwd",
-                  "col_inv", "cg_vec", "fused3d", "prior"]
+                  "col_inv", "cg_vec", "fused3d", "prior", "scan", "ortho"]
 
 
 class gleam_dims(ctypes.Structure):
@@ -91,6 +93,24 @@ class gleam_dropout_args(ctypes.Structure):
         ("seed", ctypes.c_uint64),
         ("offset", ctypes.c_uint64),
         ("step", ctypes.c_void_p),
+    ]
+
+
+class gleam_scan_dims(ctypes.Structure):
+    _fields_ = [
+        ("struct_version", ctypes.c_int32),
+        ("dtype", ctypes.c_int32),
+        ("reverse", ctypes.c_int32),
+        ("reserved", ctypes.c_int32),
+        ("batch", ctypes.c_int64),
+        ("channels", ctypes.c_int64),
+        ("steps", ctypes.c_int64),
+        ("inner", ctypes.c_int64),
+        ("stride", ctypes.c_int64 * 15),
+        ("lengths", ctypes.c_void_p),
+        ("stream", ctypes.c_void_p),
+        ("workspace", ctypes.c_void_p),
+        ("workspace_bytes", ctypes.c_uint64),
     ]
 
 
@@ -193,6 +213,14 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         lib.gleam_dropout_add_layer_norm_forward.restype = i32
         lib.gleam_dropout_add_layer_norm_vjp.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, mp, fp]
         lib.gleam_dropout_add_layer_norm_vjp.restype = i32
+        sp = ctypes.POINTER(gleam_scan_dims)
+        for name, arrays in (("forward", 6), ("vjp", 9)):
+            call = getattr(lib, "gleam_gated_scan_" + name)
+            call.argtypes, call.restype = [vp] * arrays + [sp], i32
+        lib.gleam_gated_step.argtypes, lib.gleam_gated_step.restype = [vp] * 4 + [sp], i32
+        for name in ("workspace", "saved"):
+            call = getattr(lib, "gleam_gated_scan_%s_size" % name)
+            call.argtypes, call.restype = [sp, ctypes.POINTER(u64)], i32
         lib.gleam_dc_launch_count.argtypes = []
         lib.gleam_dc_launch_count.restype = u64
         lib.gleam_dc_profile_begin.argtypes = []
@@ -421,6 +449,49 @@ def gleam_dropout_add_layer_norm_vjp(grad_y, grad_sum, total, weight, mean, rstd
     _check((_lib or load_library()).gleam_dropout_add_layer_norm_vjp(
         _addr(grad_y), _addr(grad_sum), _addr(total), _addr(weight), _addr(mean), _addr(rstd), _addr(grad_x),
         _addr(grad_residual), _addr(grad_weight), _addr(grad_bias), ctypes.byref(dropout), ctypes.byref(dims)))
+
+
+def make_scan_dims(dtype, batch, channels, steps, inner, reverse=False, strides=(), lengths=None, stream=None, workspace=None,
+                   workspace_bytes=0) -> gleam_scan_dims:
+    """Fills a ``gleam_scan_dims``; ``strides`` lists (batch, channel, step) of the call's activation arrays (missing or zeros =
+    contiguous), ``lengths`` is an int32 CUDA tensor, an address or None, the rest as for ``make_dims``."""
+    if stream is not None and not isinstance(stream, int):
+        stream = stream.cuda_stream
+    if workspace is not None and not isinstance(workspace, int):
+        workspace_bytes = workspace.numel() * workspace.element_size()
+        workspace = workspace.data_ptr()
+    flat = tuple(v for s in strides for v in s)
+    return gleam_scan_dims(1, dtype, int(reverse), 0, batch, channels, steps, inner, flat, _addr(lengths) or None, stream or None,
+                           workspace or None, workspace_bytes)
+
+
+def gleam_gated_scan_workspace_size(dims: gleam_scan_dims) -> int:
+    out = ctypes.c_uint64(0)
+    _check((_lib or load_library()).gleam_gated_scan_workspace_size(ctypes.byref(dims), ctypes.byref(out)))
+    return int(out.value)
+
+
+def gleam_gated_scan_saved_size(dims: gleam_scan_dims) -> int:
+    out = ctypes.c_uint64(0)
+    _check((_lib or load_library()).gleam_gated_scan_saved_size(ctypes.byref(dims), ctypes.byref(out)))
+    return int(out.value)
+
+
+def gleam_gated_scan_forward(x, gate, state, y, last, saved, dims: gleam_scan_dims) -> None:
+    """h_t = f_t h_(t-1) + (1 - f_t) x_t with f = sigmoid(gate); state, last and saved may be None."""
+    _check((_lib or load_library()).gleam_gated_scan_forward(_addr(x), _addr(gate), _addr(state), _addr(y), _addr(last),
+                                                             _addr(saved), ctypes.byref(dims)))
+
+
+def gleam_gated_scan_vjp(grad_y, grad_last, x, gate, state, saved, grad_x, grad_gate, grad_state, dims: gleam_scan_dims) -> None:
+    _check((_lib or load_library()).gleam_gated_scan_vjp(_addr(grad_y), _addr(grad_last), _addr(x), _addr(gate), _addr(state),
+                                                         _addr(saved), _addr(grad_x), _addr(grad_gate), _addr(grad_state),
+                                                         ctypes.byref(dims)))
+
+
+def gleam_gated_step(x, gate, state, y, dims: gleam_scan_dims) -> None:
+    """One step; state is updated in place."""
+    _check((_lib or load_library()).gleam_gated_step(_addr(x), _addr(gate), _addr(state), _addr(y), ctypes.byref(dims)))
 
 
 def gleam_dc_host_arena_size(dims: gleam_dims) -> int:

@@ -1,0 +1,151 @@
+// The gated recurrence for one element type: GLEAM_SCAN_TYPE is 0 (float32), 1 (float16) or 2 (bfloat16).
+#include "dc_entry.h"
+#include "launch_state.cuh"
+#include "scan_columns.cuh"
+#include "scan_entry.h"
+#include "scan_rows.cuh"
+
+#include <initializer_list>
+#include <type_traits>
+
+namespace gleam {
+namespace scan {
+
+#if GLEAM_SCAN_TYPE == 0
+using T = float;
+#define OPS ops_f32
+#elif GLEAM_SCAN_TYPE == 1
+using T = __half;
+#define OPS ops_f16
+#else
+using T = __nv_bfloat16;
+#define OPS ops_bf16
+#endif
+
+#define SCAN_LAUNCH(...) do { cudaError_t e_ = prof_mark(GLEAM_K_SCAN, s); if (e_ == cudaSuccess) e_ = launch_overlapped(true, __VA_ARGS__); \
+                              if (e_ != cudaSuccess) return e_; } while (0)
+
+constexpr int SMS = 148, WIDE = 8 / sizeof(T);           // chains a thread of columns takes where alignment allows
+
+static long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
+
+// Parts of the chains: where there are too few chains to fill the SMs.  Two more passes over part of the arrays (the maps, and joining
+// them) have to pay for themselves, so a part has two chunks or tiles at least.
+static void plan(Args& a, long long* saved, long long* scratch) {
+    a.rows = a.batch * a.channels * a.inner;
+    a.parts = 1; a.run = 1; a.chunk = 1; a.part = a.steps;
+    *saved = *scratch = 0;
+    if (a.rows == 0 || a.steps == 0) return;
+    long long units, threads;
+    if (a.inner > 1) {
+        a.chunk = chunk_steps(a.steps);
+        units = ceil_div(a.steps, a.chunk);
+        threads = a.rows / WIDE + 1;
+        *saved = (units - 1) * a.rows;
+    } else {
+        a.run = run_rows(a.rows, a.steps, TILE<T>);
+        a.chunk = TILE<T>;
+        units = ceil_div(a.steps, a.chunk);
+        threads = 32 * a.rows;
+        *saved = ceil_div(a.rows, a.run) * ceil_div(a.run * a.steps, a.chunk);
+    }
+    const long long wanted = SMS * 512;
+    if (a.run == 1 && units >= 4 && threads < wanted / 2) {
+        long long parts = wanted / threads;
+        if (parts > units / 2) parts = units / 2;
+        if (parts > 4096) parts = 4096;
+        a.part = ceil_div(units, parts) * a.chunk;
+        a.parts = (int)ceil_div(a.steps, a.part);
+    }
+    if (a.parts == 1) a.part = a.steps;
+    else *scratch = 2 * ceil_div(a.parts * a.rows, 64) * 64;
+}
+
+// Whether V neighbouring chains can be taken at once.
+struct Array { const void* p; const Strides* s; };
+static bool wide(const Args& a, int v, std::initializer_list<Array> arrays, std::initializer_list<const void*> states) {
+    if (a.inner % v) return false;
+    for (const Array& u : arrays) {
+        if (!u.p) continue;
+        if ((uintptr_t)u.p % (v * sizeof(T))) return false;
+        if ((a.batch > 1 && u.s->batch % v) || (a.channels > 1 && u.s->channel % v) || (a.steps > 1 && u.s->step % v)) return false;
+    }
+    for (const void* p : states)
+        if ((uintptr_t)p % (v * sizeof(float))) return false;
+    return true;
+}
+
+// Whether the steps lie without gaps from chain to chain, with runs and parts that begin at 16 bytes.
+static bool dense(const Args& a, std::initializer_list<Array> arrays) {
+    if (a.run == 1 && a.rows > 1 && a.steps % ROW_V<T>) return false;
+    for (const Array& u : arrays) {
+        if (!u.p) continue;
+        if ((uintptr_t)u.p % 16 || (a.steps > 1 && u.s->step != 1) || (a.channels > 1 && u.s->channel != a.steps) ||
+            (a.batch > 1 && u.s->batch != a.channels * a.steps)) return false;
+    }
+    return true;
+}
+
+template <class F> static cudaError_t by_bool(bool v, F f) { return v ? f(std::true_type{}) : f(std::false_type{}); }
+
+template <int V, bool REVERSE, bool BACK>
+static cudaError_t columns(const Args& a, cudaStream_t s) {
+    const dim3 grid((unsigned)ceil_div(a.rows / V, COLUMN_THREADS), (unsigned)a.parts), block(COLUMN_THREADS);
+    if (a.parts > 1) {
+        if constexpr (BACK) SCAN_LAUNCH(columns_vjp<T, V, REVERSE, true>, grid, block, 0, s, a);
+        else SCAN_LAUNCH(columns_forward<T, V, REVERSE, true>, grid, block, 0, s, a);
+        Args j = a;
+        j.descending = BACK; j.enter = BACK ? a.dlast : a.state;
+        SCAN_LAUNCH(join_parts<16>, dim3((unsigned)ceil_div(a.rows, COLUMN_THREADS)), block, 0, s, j);
+    }
+    if constexpr (BACK) SCAN_LAUNCH(columns_vjp<T, V, REVERSE, false>, grid, block, 0, s, a);
+    else SCAN_LAUNCH(columns_forward<T, V, REVERSE, false>, grid, block, 0, s, a);
+    return cudaSuccess;
+}
+
+template <bool REVERSE, bool DENSE, bool BACK>
+static cudaError_t rows(const Args& a, cudaStream_t s) {
+    const long long warps = a.run > 1 ? ceil_div(a.rows, a.run) : a.rows * a.parts;
+    const dim3 grid((unsigned)ceil_div(warps, ROW_WARPS)), block(32 * ROW_WARPS);
+    if (a.parts > 1) {
+        SCAN_LAUNCH(rows_kernel<T, REVERSE, DENSE, BACK ? MAP_VJP : MAP_FORWARD>, grid, block, 0, s, a);
+        Args j = a;
+        j.descending = BACK != REVERSE; j.enter = BACK ? a.dlast : a.state;      // parts are numbered from the first step
+        SCAN_LAUNCH(join_parts<16>, dim3((unsigned)ceil_div(a.rows, COLUMN_THREADS)), dim3(COLUMN_THREADS), 0, s, j);
+    }
+    SCAN_LAUNCH(rows_kernel<T, REVERSE, DENSE, BACK ? VJP : FORWARD>, grid, block, 0, s, a);
+    return cudaSuccess;
+}
+
+template <bool BACK>
+static cudaError_t chains(const Args& a, bool reverse, std::initializer_list<Array> arrays, std::initializer_list<const void*> states, cudaStream_t s) {
+    return by_bool(reverse, [&](auto r) {
+        constexpr bool R = decltype(r)::value;
+        if (a.inner == 1) return by_bool(dense(a, arrays), [&](auto d) { return rows<R, decltype(d)::value, BACK>(a, s); });
+        if (wide(a, WIDE, arrays, states)) return columns<WIDE, R, BACK>(a, s);
+        return columns<1, R, BACK>(a, s);
+    });
+}
+
+static cudaError_t forward(const Args& a, bool reverse, cudaStream_t s) {
+    return chains<false>(a, reverse, {{a.x, &a.sx}, {a.gate, &a.sgate}, {a.y, &a.sy}}, {a.state, a.last, a.saved}, s);
+}
+
+static cudaError_t vjp(const Args& a, bool reverse, cudaStream_t s) {
+    return chains<true>(a, reverse, {{a.x, &a.sx}, {a.gate, &a.sgate}, {a.dy, &a.sdy}, {a.dx, &a.sdx}, {a.dg, &a.sdg}},
+                        {a.state, a.saved, a.dlast, a.dstate}, s);
+}
+
+static cudaError_t step(const Args& a, cudaStream_t s) {
+    const bool w = wide(a, WIDE, {{a.x, &a.sx}, {a.gate, &a.sgate}, {a.y, &a.sy}}, {a.last});
+    const long long threads = w ? a.rows / WIDE : a.rows;
+    const dim3 grid((unsigned)ceil_div(threads, COLUMN_THREADS)), block(COLUMN_THREADS);
+    if (w) SCAN_LAUNCH(step_kernel<T, WIDE>, grid, block, 0, s, a);
+    else SCAN_LAUNCH(step_kernel<T, 1>, grid, block, 0, s, a);
+    return cudaSuccess;
+}
+
+const Ops OPS = {plan, forward, vjp, step};
+
+}  // namespace scan
+}  // namespace gleam

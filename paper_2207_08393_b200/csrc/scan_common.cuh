@@ -1,0 +1,60 @@
+// What the kernels of the gated recurrence share: arguments, the gate, strided addresses.
+//
+//     h_t = f_t h_(t-1) + (1 - f_t) x_t,   f_t = 1 / (1 + exp(-gate_t)),   t = 0, 1, ... or T - 1, T - 2, ... (reverse)
+//
+// and with D_t the cotangent of h_t and c what the step behind t hands back,
+//
+//     D_t = dy_t + c,   dx_t = D_t (1 - f_t),   dgate_t = D_t (h_(t-1) - x_t) f_t (1 - f_t),   c <- D_t f_t.
+//
+// Both are chains of maps s -> a s + b, which compose as (a2, b2) o (a1, b1) = (a2 a1, a2 b1 + b2): a chain can be cut into parts
+// whose maps are found side by side, joined, and run again from the right states.  States are 32-bit numbers throughout.  The VJP
+// needs h_(t-1): it is computed again from states that the forward call saves at few places, so that neither h as stored (rounded
+// to the arrays' type) nor another array of the same size is read.
+#pragma once
+#include "prior_common.cuh"
+
+namespace gleam {
+namespace scan {
+
+using prior::from_float;
+using prior::Pack;
+using prior::to_float;
+
+struct Strides { long long batch, channel, step; };
+
+struct Args {
+    const void* x; const void* gate; const void* dy;      // dy: VJP
+    void* y; void* dx; void* dg;
+    Strides sx, sgate, sdy, sy, sdx, sdg;
+    const float* state;                // initial states (rows) or null: zeros
+    float* last;                       // forward: last states, or null
+    const float* dlast; float* dstate; // VJP: their cotangents, or null
+    float* saved;                      // states at the chunks' (tiles') starts; forward: or null
+    float* maps_a; float* maps_b;      // (parts, rows): maps of the parts, then the state (b) that each part starts from
+    const int* lengths;                // valid steps of each example, or null
+    long long batch, channels, steps, inner, rows;        // rows = batch * channels * inner chains
+    int parts; long long part;         // parts of a chain and steps of a part (a multiple of the chunk)
+    int chunk;                         // columns: steps between saved states
+    long long run;                     // chains of one run where steps are contiguous
+    int descending;                    // the chain enters its last part first
+    const float* enter;                // join_parts: states at the chain's entry, or null
+};
+
+enum { MAP_FORWARD, MAP_VJP, FORWARD, VJP };       // MAP_*: only the parts' maps are formed
+
+// f and 1 - f, both to full relative precision; f is exactly 1 or 0 for an infinite gate.
+__device__ __forceinline__ void gate_of(float g, float& f, float& rest) {
+    const float e = __expf(-fabsf(g)), s = __fdividef(1.f, 1.f + e), t = e * s;
+    f = g < 0.f ? t : s;
+    rest = g < 0.f ? s : t;
+    if (g != g) f = rest = g;
+}
+
+__device__ __forceinline__ long long valid_steps(const Args& a, long long batch) {
+    if (!a.lengths) return a.steps;
+    const long long n = a.lengths[batch];
+    return n < 0 ? 0 : n > a.steps ? a.steps : n;
+}
+
+}  // namespace scan
+}  // namespace gleam

@@ -384,6 +384,49 @@ GLEAM_API int gleam_gated_step(const void* x, const void* gate, float* state, vo
 GLEAM_API int gleam_gated_scan_workspace_size(const gleam_scan_dims* dims, uint64_t* bytes);
 GLEAM_API int gleam_gated_scan_saved_size(const gleam_scan_dims* dims, uint64_t* bytes);
 
+/* ---- orthogonalised updates of a prior's matrices ---------------------------------------------------------
+ * A convolution's weights, as a matrix (features, inputs x taps), train well when every singular direction of the update gets the
+ * same length (K. Jordan et al., "Muon: an optimizer for hidden layers in neural networks", 2024).
+ *
+ *   orthogonalise  X_0 = U / (|U| + eps) (Frobenius norm), then `turns` times X <- a X + (b A + c A A) X with A = X X^T over the
+ *                  shorter side: singular values v -> a v + b v^3 + c v^5, singular vectors as they are
+ *   muon step      momentum <- mu momentum + grad,  U = grad + mu momentum (nesterov) or momentum,
+ *                  weight <- (1 - lr weight_decay) weight - lr scale orthogonalise(U)
+ *
+ * The pointers lie in host arrays, one device address for each of `count` matrices (rows, cols), contiguous.  x, out, weights and grads
+ * have type dtype, momenta are float32.  The norm is a 32-bit sum.  Products are as exact as 32-bit ones (float16 pieces of 22 bits,
+ * 32-bit sums); |a|, |b|, |c| <= 16, and singular values have to stay below 8 along the way (those of the usual coefficients stay below
+ * 1.3).  A matrix of zeros gives zeros; one with a NaN or an infinity gives NaN throughout, the others are untouched by it.  The shorter
+ * side is at most 16384, and there are at most 65535 blocks of 128 x 128 in a matrix.  Nothing that a call writes may overlap
+ * anything else of the call (GLEAM_ERR_ALIAS).  Results are deterministic.  Two calls whose GPU work may overlap need workspaces of
+ * their own.
+ */
+#define GLEAM_MATRIX_DIMS_VERSION 1
+typedef struct {
+    int32_t struct_version;   /* GLEAM_MATRIX_DIMS_VERSION */
+    int32_t dtype;            /* GLEAM_F32, GLEAM_F16 or GLEAM_BF16 */
+    int64_t count, rows, cols;
+    int32_t turns;            /* 1 ... 100 */
+    float a, b, c, eps;       /* eps > 0 */
+    void* stream;
+    void* workspace;          /* gleam_orthogonalise_workspace_size() bytes, 256-byte aligned */
+    uint64_t workspace_bytes;
+} gleam_matrix_dims;
+typedef struct {
+    float lr;                 /* >= 0 */
+    float momentum;           /* 0 <= mu < 1 */
+    float weight_decay;       /* >= 0 */
+    float scale;
+    int32_t nesterov;         /* 0 or 1 */
+} gleam_muon_args;
+GLEAM_API int gleam_orthogonalise(const void* const* x, void* const* out, const gleam_matrix_dims* dims);
+GLEAM_API int gleam_muon_step(void* const* weights, const void* const* grads, float* const* momenta, const gleam_muon_args* args,
+                              const gleam_matrix_dims* dims);
+/* Synchronises dims->stream; GLEAM_ERR_TIMEOUT if a kernel of the last such call with this workspace gave up waiting for its own
+ * copies or products (bounded by two seconds; its results are then undefined), else GLEAM_OK. */
+GLEAM_API int gleam_orthogonalise_check_status(const gleam_matrix_dims* dims);
+GLEAM_API int gleam_orthogonalise_workspace_size(const gleam_matrix_dims* dims, uint64_t* bytes);
+
 /* ---- gradients of Eq. 3 with respect to the step size and the measurements --------------------------
  * out = x - eta A^H (A x - y) is linear in eta and affine in y.  For a cotangent g = grad_out of the
  * output (conjugate-Wirtinger convention, as for gleam_dc_vjp):

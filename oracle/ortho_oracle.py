@@ -1,0 +1,49 @@
+"""Double-precision definitions of the orthogonalised update in numpy, turn by turn.  Test infrastructure; shares no code with the CUDA
+path."""
+import numpy as np
+
+COEFFICIENTS = (3.4445, -4.7750, 2.0315)
+
+
+def iterates(x, steps, coefficients=COEFFICIENTS, eps=1e-7):
+    """X_0, X_1, ... of one matrix, over its shorter side."""
+    a, b, c = coefficients
+    x = x.astype(np.float64)
+    x = x / (np.sqrt((x ** 2).sum()) + eps)
+    out = [x]
+    for _ in range(steps):
+        x = out[-1]
+        if x.shape[0] <= x.shape[1]:
+            g = x @ x.T
+            out.append(a * x + (b * g + c * g @ g) @ x)
+        else:
+            g = x.T @ x
+            out.append(a * x + x @ (b * g + c * g @ g))
+    return out
+
+
+def by_singular_values(x, steps, coefficients=COEFFICIENTS, eps=1e-7):
+    """The same from the singular value decomposition."""
+    a, b, c = coefficients
+    u, s, v = np.linalg.svd(x.astype(np.float64), full_matrices=False)
+    s = s / (np.sqrt((s ** 2).sum()) + eps)
+    for _ in range(steps):
+        s = a * s + b * s ** 3 + c * s ** 5
+    return (u * s) @ v
+
+
+def tolerance(its, coefficients=COEFFICIENTS):
+    """Frobenius norm of the error that pieces of 22 bits and 32-bit sums may leave, given the iterates in 64 bits.
+
+    A turn stores X, A and P (2^-22 of each value), leaves out lo lo (2^-22 of a product) and adds K values in groups of 16 that a sum may
+    cut off rather than round (2^-23 each, K / 16 groups over three sums of a block, twice): d = 5 * 2^-22 + (K / 24 + 4) * 2^-23 of
+    |a| |X| + |b| |X|^3 + |c| |X|^5 with |X| <= 1.3, less than 14 times the Frobenius norm of X.  A later turn stretches an error at most by the
+    largest derivative of a v + b v^3 + c v^5, max(|a|, ...) over the values met, 5 here."""
+    a, b, c = coefficients
+    k = max(its[0].shape)
+    d = 5 * 2.0 ** -22 + (k / 24 + 4) * 2.0 ** -23
+    grow = max(abs(a + 3 * b * v ** 2 + 5 * c * v ** 4) for v in np.linspace(0, 1.25, 100))
+    total = 0.0
+    for x in its[:-1]:
+        total = grow * total + 14 * d * np.sqrt((x ** 2).sum())
+    return total

@@ -25,3 +25,8 @@ from .binding import (  # noqa: F401
     gleam_gated_step, gleam_scan_dims, make_scan_dims,
 )
 from .scan_ops import gated_scan, gated_scan_forward, gated_scan_vjp, gated_step  # noqa: F401
+from .binding import (  # noqa: F401
+    gleam_matrix_dims, gleam_muon_args, gleam_muon_step, gleam_orthogonalise, gleam_orthogonalise_check_status,
+    gleam_orthogonalise_workspace_size, make_matrix_dims,
+)
+from .ortho_ops import Muon, muon_step, orthogonalise  # noqa: F401

@@ -80,7 +80,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
         obj = os.path.join(BUILD, "kernels_scan%d.o" % kind)
         jobs.append((["nvcc"] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) +
                      ["-DGLEAM_SCAN_TYPE=%d" % kind, "-c", os.path.join(CSRC, "kernels_scan.cu"), "-o", obj], obj))
-    for name in ("gleam_dc", "kernels_fused", "modl_cg", "prior_ops", "scan_ops"):
+    for name in ("gleam_dc", "kernels_fused", "modl_cg", "prior_ops", "scan_ops", "ortho_ops"):
         obj = os.path.join(BUILD, name + ".o")
         jobs.append((["nvcc"] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) +
                      ["-c", os.path.join(CSRC, name + ".cu"), "-o", obj], obj))

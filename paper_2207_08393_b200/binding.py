@@ -49,7 +49,8 @@ EXPORTS = ["gleam_dc_forward", "gleam_dc_vjp", "gleam_dc_workspace_size", "gleam
            "gleam_dropout_forward", "gleam_dropout_vjp",
            "gleam_dropout_add_layer_norm_forward", "gleam_dropout_add_layer_norm_vjp",
            "gleam_gated_scan_forward", "gleam_gated_scan_vjp", "gleam_gated_step", "gleam_gated_scan_workspace_size",
-           "gleam_gated_scan_saved_size"]
+           "gleam_gated_scan_saved_size",
+           "gleam_orthogonalise", "gleam_muon_step", "gleam_orthogonalise_check_status", "gleam_orthogonalise_workspace_size"]
 
 KERNEL_CLASSES = ["zmap", "col_z", "row_fused", "row_fwd", "col_mid_sep", "row_inv", "col_mid_full", "col_fwd",
                   "col_inv", "cg_vec", "fused3d", "prior", "scan", "ortho"]
@@ -111,6 +112,34 @@ class gleam_scan_dims(ctypes.Structure):
         ("stream", ctypes.c_void_p),
         ("workspace", ctypes.c_void_p),
         ("workspace_bytes", ctypes.c_uint64),
+    ]
+
+
+class gleam_matrix_dims(ctypes.Structure):
+    _fields_ = [
+        ("struct_version", ctypes.c_int32),
+        ("dtype", ctypes.c_int32),
+        ("count", ctypes.c_int64),
+        ("rows", ctypes.c_int64),
+        ("cols", ctypes.c_int64),
+        ("turns", ctypes.c_int32),
+        ("a", ctypes.c_float),
+        ("b", ctypes.c_float),
+        ("c", ctypes.c_float),
+        ("eps", ctypes.c_float),
+        ("stream", ctypes.c_void_p),
+        ("workspace", ctypes.c_void_p),
+        ("workspace_bytes", ctypes.c_uint64),
+    ]
+
+
+class gleam_muon_args(ctypes.Structure):
+    _fields_ = [
+        ("lr", ctypes.c_float),
+        ("momentum", ctypes.c_float),
+        ("weight_decay", ctypes.c_float),
+        ("scale", ctypes.c_float),
+        ("nesterov", ctypes.c_int32),
     ]
 
 
@@ -221,6 +250,11 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         for name in ("workspace", "saved"):
             call = getattr(lib, "gleam_gated_scan_%s_size" % name)
             call.argtypes, call.restype = [sp, ctypes.POINTER(u64)], i32
+        mdp = ctypes.POINTER(gleam_matrix_dims)
+        lib.gleam_orthogonalise.argtypes, lib.gleam_orthogonalise.restype = [vp, vp, mdp], i32
+        lib.gleam_muon_step.argtypes, lib.gleam_muon_step.restype = [vp, vp, vp, ctypes.POINTER(gleam_muon_args), mdp], i32
+        lib.gleam_orthogonalise_check_status.argtypes, lib.gleam_orthogonalise_check_status.restype = [mdp], i32
+        lib.gleam_orthogonalise_workspace_size.argtypes, lib.gleam_orthogonalise_workspace_size.restype = [mdp, ctypes.POINTER(u64)], i32
         lib.gleam_dc_launch_count.argtypes = []
         lib.gleam_dc_launch_count.restype = u64
         lib.gleam_dc_profile_begin.argtypes = []
@@ -492,6 +526,44 @@ def gleam_gated_scan_vjp(grad_y, grad_last, x, gate, state, saved, grad_x, grad_
 def gleam_gated_step(x, gate, state, y, dims: gleam_scan_dims) -> None:
     """One step; state is updated in place."""
     _check((_lib or load_library()).gleam_gated_step(_addr(x), _addr(gate), _addr(state), _addr(y), ctypes.byref(dims)))
+
+
+def make_matrix_dims(dtype, count, rows, cols, turns=5, coefficients=(3.4445, -4.7750, 2.0315), eps=1e-7, stream=None, workspace=None,
+                     workspace_bytes=0) -> gleam_matrix_dims:
+    """Fills a ``gleam_matrix_dims``; ``stream`` and ``workspace`` are as for ``make_dims``."""
+    if stream is not None and not isinstance(stream, int):
+        stream = stream.cuda_stream
+    if workspace is not None and not isinstance(workspace, int):
+        workspace_bytes = workspace.numel() * workspace.element_size()
+        workspace = workspace.data_ptr()
+    a, b, c = coefficients
+    return gleam_matrix_dims(1, dtype, count, rows, cols, turns, a, b, c, eps, stream or None, workspace or None, workspace_bytes)
+
+
+def _addresses(tensors):
+    """Host array of the matrices' device addresses."""
+    return (ctypes.c_void_p * max(len(tensors), 1))(*[_addr(t) for t in tensors])
+
+
+def gleam_orthogonalise_workspace_size(dims: gleam_matrix_dims) -> int:
+    out = ctypes.c_uint64(0)
+    _check((_lib or load_library()).gleam_orthogonalise_workspace_size(ctypes.byref(dims), ctypes.byref(out)))
+    return int(out.value)
+
+
+def gleam_orthogonalise_check_status(dims: gleam_matrix_dims) -> None:
+    _check((_lib or load_library()).gleam_orthogonalise_check_status(ctypes.byref(dims)))
+
+
+def gleam_orthogonalise(x, out, dims: gleam_matrix_dims) -> None:
+    """x, out: lists of dims.count matrices (tensors or addresses)."""
+    _check((_lib or load_library()).gleam_orthogonalise(_addresses(x), _addresses(out), ctypes.byref(dims)))
+
+
+def gleam_muon_step(weights, grads, momenta, args: gleam_muon_args, dims: gleam_matrix_dims) -> None:
+    """weights and momenta (lists of dims.count matrices) are updated in place."""
+    _check((_lib or load_library()).gleam_muon_step(_addresses(weights), _addresses(grads), _addresses(momenta), ctypes.byref(args),
+                                                    ctypes.byref(dims)))
 
 
 def gleam_dc_host_arena_size(dims: gleam_dims) -> int:

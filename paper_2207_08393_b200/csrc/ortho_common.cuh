@@ -1,0 +1,89 @@
+// What the kernels of the orthogonalised update share.
+//
+// With X of S x L (S the shorter side, L the longer one, tall matrices taken transposed), X_0 = U / (|U| + eps), every turn is
+//
+//     A = X X^T,   P = b A + c A A,   X <- a X + P X,
+//
+// which takes each singular value v to a v + b v^3 + c v^5 and leaves the singular vectors: after a few turns of suitable (a, b, c)
+// all values but the smallest are near 1 (K. Jordan et al., "Muon: an optimizer for hidden layers in neural networks", 2024).
+//
+// The products run on the tensor cores in float16 with 32-bit sums, and keep the precision of 32-bit numbers: X, A and P are stored as
+// two pieces, hi = x rounded to float16 and lo = x - hi rounded to float16 (22 bits), and a product is hi hi + hi lo + lo hi; what is
+// left out is 2^-22 of it.  All stored values are scaled by 2^10 (up to 64 in front of the scale), so that lo keeps its bits down
+// to values of 2^-13.  The term a X is added in 32 bits.  Against 64 bits the result is as near as 32-bit products are, or nearer;
+// float16 or bfloat16 products without the second piece would be off by 1e-3 or 1e-2.
+//
+// Matrices are stored in blocks of 128 x 128 with zeros beyond their sides: a block is 32 KB of hi and 32 KB of lo, each as 16 x 16 cores
+// of 8 rows by 8 columns, a row of a core 16 bytes: the shape that the matrix instructions read, along either side.  Any operand
+// tile is then a few contiguous runs of at least 1 KB.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <cstdint>
+
+#include "prior_common.cuh"
+
+namespace gleam {
+namespace ortho {
+
+using prior::from_float;
+using prior::to_float;
+
+constexpr int BLOCK = 128, CORE = 128, PIECE_BYTES = BLOCK * BLOCK * 2, BLOCK_BYTES = 2 * PIECE_BYTES;
+constexpr float SCALE = 1024.f;
+constexpr int GROUP = 64;                          // matrices of a launch
+constexpr int PARTS = 64;                          // partial sums of squares of a matrix at most
+
+struct Args {
+    const void* u[GROUP];                          // matrices or gradients
+    float* momentum[GROUP];                        // update: momenta, else null
+    void* out[GROUP];                              // results, or weights
+    long long rows, cols, S, L;
+    int tall, dtype;                               // GLEAM_F32, ...
+    int sblocks, lblocks, parts;
+    int update, nesterov;
+    float a, b, c, eps, mu, keep, move;            // weight <- keep weight - move result
+    unsigned char* x; unsigned char* y;            // X and its successor: (count, sblocks, lblocks) blocks
+    unsigned char* g; unsigned char* p;            // A and P: (count, sblocks, sblocks) blocks
+    float* part; int* status;
+};
+
+// Byte of element (r, c) of a piece.
+__host__ __device__ __forceinline__ int core_at(int r, int c) { return ((r >> 3) * 16 + (c >> 3)) * CORE + (r & 7) * 16 + (c & 7) * 2; }
+
+__device__ __forceinline__ float load_as(const void* p, int dtype, long long i) {
+    return dtype == 0 ? static_cast<const float*>(p)[i] : dtype == 1 ? __half2float(static_cast<const __half*>(p)[i])
+                                                                     : __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]);
+}
+__device__ __forceinline__ void store_as(void* p, int dtype, long long i, float v) {
+    if (dtype == 0) static_cast<float*>(p)[i] = v;
+    else if (dtype == 1) static_cast<__half*>(p)[i] = __float2half_rn(v);
+    else static_cast<__nv_bfloat16*>(p)[i] = __float2bfloat16_rn(v);
+}
+
+// Eight neighbours of a row as two pieces, and back.
+__device__ __forceinline__ void split8(const float (&v)[8], uint4& hi, uint4& lo) {
+    uint32_t h[4], l[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const __half2 a = __floats2half2_rn(v[2 * j], v[2 * j + 1]);
+        const float2 f = __half22float2(a);
+        const __half2 r = __floats2half2_rn(v[2 * j] - f.x, v[2 * j + 1] - f.y);
+        h[j] = reinterpret_cast<const uint32_t&>(a);
+        l[j] = reinterpret_cast<const uint32_t&>(r);
+    }
+    hi = make_uint4(h[0], h[1], h[2], h[3]);
+    lo = make_uint4(l[0], l[1], l[2], l[3]);
+}
+__device__ __forceinline__ void join8(const uint4& hi, const uint4& lo, float (&v)[8]) {
+    const uint32_t h[4] = {hi.x, hi.y, hi.z, hi.w}, l[4] = {lo.x, lo.y, lo.z, lo.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const float2 a = __half22float2(reinterpret_cast<const __half2&>(h[j])), b = __half22float2(reinterpret_cast<const __half2&>(l[j]));
+        v[2 * j] = a.x + b.x; v[2 * j + 1] = a.y + b.y;
+    }
+}
+
+}  // namespace ortho
+}  // namespace gleam

@@ -1,0 +1,182 @@
+// Orthogonalised updates: entry points, argument checks, workspace, launches.
+#include "../../include/gleam.h"
+#include "dc_entry.h"
+#include "launch_state.cuh"
+#include "ortho_gemm.cuh"
+#include "ortho_prepare.cuh"
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <vector>
+
+namespace gleam {
+namespace ortho {
+
+#define ORTHO_LAUNCH(...) do { cudaError_t e_ = prof_mark(GLEAM_K_ORTHO, s); if (e_ == cudaSuccess) e_ = (__VA_ARGS__); if (e_ != cudaSuccess) return e_; } while (0)
+
+template <int KIND>
+static cudaError_t gemm(const Args& a, int count, cudaStream_t s) {
+    static PerDevice done;
+    cudaError_t e = ensure_smem(gemm_kernel<KIND>, GEMM_SMEM, done);
+    if (e != cudaSuccess) return e;
+    const int tiles = tiles_of<KIND>(a), steps = steps_of<KIND>(a);
+    // blocks that share a sum over K: while there are SMs left and each has two steps at least
+    int ranks = 1;
+    if (KIND == GRAM || KIND == POLY)
+        while (ranks < 8 && tiles * count * ranks * 2 <= 148 && steps >= ranks * 4) ranks *= 2;
+    const dim3 grid((unsigned)ranks, (unsigned)tiles, (unsigned)count), block(GEMM_THREADS);
+    ORTHO_LAUNCH(launch_overlapped_cluster((unsigned)ranks, gemm_kernel<KIND>, grid, block, GEMM_SMEM, s, a));
+    return cudaSuccess;
+}
+
+template <bool UPDATE>
+static cudaError_t run(Args& a, int count, int turns, cudaStream_t s) {
+    ORTHO_LAUNCH(launch_overlapped(true, sums_kernel<UPDATE>, dim3((unsigned)a.parts, (unsigned)count), dim3(PREPARE_THREADS), 0, s, a));
+    const size_t tile = a.tall ? sizeof(float) * BLOCK * (BLOCK + 1) : 0;
+    static PerDevice done;
+    cudaError_t e = ensure_smem(first_kernel<UPDATE>, sizeof(float) * BLOCK * (BLOCK + 1), done);
+    if (e != cudaSuccess) return e;
+    ORTHO_LAUNCH(launch_overlapped(true, first_kernel<UPDATE>, dim3((unsigned)(a.sblocks * a.lblocks), (unsigned)count), dim3(PREPARE_THREADS), tile, s, a));
+    for (int k = 0; k < turns; ++k) {
+        if ((e = gemm<GRAM>(a, count, s)) != cudaSuccess || (e = gemm<POLY>(a, count, s)) != cudaSuccess) return e;
+        if ((e = k + 1 < turns ? gemm<APPLY>(a, count, s) : gemm<LAST>(a, count, s)) != cudaSuccess) return e;
+        std::swap(a.x, a.y);
+    }
+    return cudaSuccess;
+}
+
+struct Layout { int sblocks, lblocks, group; uint64_t x, square, part, status, total; };
+
+static int layout_of(const gleam_matrix_dims* d, Layout* l) {
+    if (!d) return GLEAM_ERR_NULL_POINTER;
+    if (d->struct_version != GLEAM_MATRIX_DIMS_VERSION || d->dtype < GLEAM_F32 || d->dtype > GLEAM_BF16) return GLEAM_ERR_BAD_DIMS;
+    if (d->count < 0 || d->rows < 0 || d->cols < 0 || d->count > (1 << 20) || d->rows > (1 << 20) || d->cols > (1 << 20)) return GLEAM_ERR_BAD_DIMS;
+    const long long S = std::min(d->rows, d->cols), L = std::max(d->rows, d->cols);
+    if (S > 16384) return GLEAM_ERR_BAD_DIMS;
+    if (d->turns < 1 || d->turns > 100) return GLEAM_ERR_BAD_DIMS;
+    for (const float v : {d->a, d->b, d->c})
+        if (!(std::fabs(v) <= 16.f)) return GLEAM_ERR_BAD_DIMS;
+    if (!(d->eps > 0.f) || !std::isfinite(d->eps)) return GLEAM_ERR_BAD_DIMS;
+    l->sblocks = (int)((S + BLOCK - 1) / BLOCK); l->lblocks = (int)((L + BLOCK - 1) / BLOCK);
+    // tiles of a launch are numbered by the y axis of its grid
+    if ((long long)l->sblocks * l->lblocks > 65535) return GLEAM_ERR_BAD_DIMS;
+    l->group = (int)std::min<long long>(d->count, GROUP);
+    l->x = (uint64_t)l->group * l->sblocks * l->lblocks * BLOCK_BYTES;
+    l->square = (uint64_t)l->group * l->sblocks * l->sblocks * BLOCK_BYTES;
+    l->part = (uint64_t)GROUP * PARTS * sizeof(float);
+    l->total = l->x && d->count ? 2 * l->x + 2 * l->square + l->part + 256 : 0;
+    return GLEAM_OK;
+}
+
+struct Span { uintptr_t at; uint64_t bytes; bool written; };
+
+// Every matrix of the call: on a device, aligned, and nothing written shared with anything else.
+static int check_memory(std::vector<Span>& spans) {
+    for (const Span& u : spans) {
+        const int rc = check_device_ptr((const void*)u.at);
+        if (rc != GLEAM_OK) return rc;
+    }
+    std::sort(spans.begin(), spans.end(), [](const Span& x, const Span& y) { return x.at < y.at; });
+    uintptr_t end = 0, written = 0;                 // first byte behind all spans so far, behind the written ones
+    for (const Span& u : spans) {
+        if (u.at < written || (u.written && u.at < end)) return GLEAM_ERR_ALIAS;
+        end = std::max<uintptr_t>(end, u.at + u.bytes);
+        if (u.written) written = std::max<uintptr_t>(written, u.at + u.bytes);
+    }
+    return GLEAM_OK;
+}
+
+static int orthogonal(const void* const* u, float* const* momenta, void* const* out, const gleam_muon_args* m, const gleam_matrix_dims* d) {
+    Layout l;
+    int rc = layout_of(d, &l);
+    if (rc != GLEAM_OK) return rc;
+    if (l.total == 0) return GLEAM_OK;
+    if (!u || !out || (m && !momenta) || !d->workspace) return GLEAM_ERR_NULL_POINTER;
+    if (d->workspace_bytes < l.total) return GLEAM_ERR_WORKSPACE_TOO_SMALL;
+    if ((uintptr_t)d->workspace & 255) return GLEAM_ERR_BAD_DIMS;
+    const uint64_t n = (uint64_t)d->rows * d->cols, esize = d->dtype == GLEAM_F32 ? 4 : 2;
+    {
+        std::vector<Span> spans;
+        spans.reserve((size_t)d->count * 3 + 1);
+        spans.push_back(Span{(uintptr_t)d->workspace, l.total, true});
+        for (int64_t i = 0; i < d->count; ++i) {
+            if (!u[i] || !out[i] || (m && !momenta[i])) return GLEAM_ERR_NULL_POINTER;
+            if ((uintptr_t)u[i] % esize || (uintptr_t)out[i] % esize || (m && (uintptr_t)momenta[i] % 4)) return GLEAM_ERR_BAD_DIMS;
+            spans.push_back(Span{(uintptr_t)u[i], n * esize, false});
+            spans.push_back(Span{(uintptr_t)out[i], n * esize, true});
+            if (m) spans.push_back(Span{(uintptr_t)momenta[i], n * 4, true});
+        }
+        if ((rc = check_memory(spans)) != GLEAM_OK) return rc;
+    }
+    Args a;
+    std::memset(&a, 0, sizeof a);
+    a.rows = d->rows; a.cols = d->cols; a.S = std::min(d->rows, d->cols); a.L = std::max(d->rows, d->cols);
+    a.tall = d->rows > d->cols; a.dtype = d->dtype;
+    a.sblocks = l.sblocks; a.lblocks = l.lblocks;
+    a.parts = (int)std::max<long long>(1, std::min<long long>(PARTS, (long long)(n / (8 * PREPARE_THREADS))));
+    a.a = d->a; a.b = d->b; a.c = d->c; a.eps = d->eps;
+    if (m) {
+        a.update = 1; a.nesterov = m->nesterov; a.mu = m->momentum;
+        a.keep = (float)(1.0 - (double)m->lr * m->weight_decay); a.move = (float)((double)m->lr * m->scale);
+    }
+    unsigned char* ws = (unsigned char*)d->workspace;
+    a.g = ws + 2 * l.x; a.p = a.g + l.square;
+    a.part = (float*)(a.p + l.square);
+    a.status = (int*)((unsigned char*)a.part + l.part);
+    for (int64_t i0 = 0; i0 < d->count; i0 += GROUP) {
+        const int count = (int)std::min<int64_t>(GROUP, d->count - i0);
+        a.x = ws; a.y = ws + l.x;
+        for (int k = 0; k < count; ++k) {
+            a.u[k] = u[i0 + k]; a.out[k] = out[i0 + k]; a.momentum[k] = m ? momenta[i0 + k] : nullptr;
+        }
+        const cudaError_t e = m ? run<true>(a, count, d->turns, (cudaStream_t)d->stream) : run<false>(a, count, d->turns, (cudaStream_t)d->stream);
+        if (e != cudaSuccess) return GLEAM_ERR_CUDA;
+    }
+    return GLEAM_OK;
+}
+
+}  // namespace ortho
+}  // namespace gleam
+
+using namespace gleam::ortho;
+
+extern "C" {
+
+GLEAM_API int gleam_orthogonalise_workspace_size(const gleam_matrix_dims* dims, uint64_t* bytes) {
+    if (!bytes) return GLEAM_ERR_NULL_POINTER;
+    Layout l;
+    const int rc = layout_of(dims, &l);
+    if (rc != GLEAM_OK) return rc;
+    *bytes = l.total;
+    return GLEAM_OK;
+}
+
+GLEAM_API int gleam_orthogonalise_check_status(const gleam_matrix_dims* dims) {
+    Layout l;
+    const int rc = layout_of(dims, &l);
+    if (rc != GLEAM_OK) return rc;
+    if (l.total == 0) return GLEAM_OK;
+    if (!dims->workspace) return GLEAM_ERR_NULL_POINTER;
+    if (dims->workspace_bytes < l.total) return GLEAM_ERR_WORKSPACE_TOO_SMALL;
+    int status = 0;
+    const unsigned char* at = (const unsigned char*)dims->workspace + l.total - 256;
+    if (cudaMemcpyAsync(&status, at, sizeof status, cudaMemcpyDeviceToHost, (cudaStream_t)dims->stream) != cudaSuccess ||
+        cudaStreamSynchronize((cudaStream_t)dims->stream) != cudaSuccess) return GLEAM_ERR_CUDA;
+    return status ? GLEAM_ERR_TIMEOUT : GLEAM_OK;
+}
+
+GLEAM_API int gleam_orthogonalise(const void* const* x, void* const* out, const gleam_matrix_dims* dims) {
+    return orthogonal(x, nullptr, out, nullptr, dims);
+}
+
+GLEAM_API int gleam_muon_step(void* const* weights, const void* const* grads, float* const* momenta, const gleam_muon_args* args,
+                              const gleam_matrix_dims* dims) {
+    if (!args) return GLEAM_ERR_NULL_POINTER;
+    for (const float v : {args->lr, args->momentum, args->weight_decay, args->scale})
+        if (!std::isfinite(v)) return GLEAM_ERR_BAD_DIMS;
+    if (args->lr < 0.f || !(args->momentum >= 0.f && args->momentum < 1.f) || args->weight_decay < 0.f || (args->nesterov != 0 && args->nesterov != 1)) return GLEAM_ERR_BAD_DIMS;
+    return orthogonal(grads, momenta, weights, args, dims);
+}
+
+}  // extern "C"

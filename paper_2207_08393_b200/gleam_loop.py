@@ -16,7 +16,9 @@ import torch
 import torch.nn as nn
 
 from . import binding as _b
+from . import ortho_ops as _o
 from . import prior_ops as _p
+from . import scan_ops as _s
 
 
 class _DCFunction(torch.autograd.Function):
@@ -59,12 +61,14 @@ class _L1Function(torch.autograd.Function):
 
 
 class DataConsistencyStep:
-    """One measurement setting (y, sens, mask, eta, reference) bound to the CUDA library for a problem shape."""
+    """One measurement setting (y, sens, mask, eta, reference) bound to the CUDA library for a problem shape.  ``lengths`` (int32, one for
+    each example, on the device) says how many frames an example has where shorter cines are padded: a recurrent prior stops there."""
 
-    def __init__(self, y, sens, mask, eta, ref, fft_rank=2, mask_kind=_b.GLEAM_MASK_READOUT_INVARIANT):
+    def __init__(self, y, sens, mask, eta, ref, fft_rank=2, mask_kind=_b.GLEAM_MASK_READOUT_INVARIANT, lengths=None):
         B, C, T = y.shape[0], y.shape[1], y.shape[2]
         n = tuple(y.shape[3:])
         self.y, self.sens, self.mask, self.eta, self.ref = y, sens, mask, float(eta), ref
+        self.lengths = lengths
         self.shape = (B, C, T, fft_rank, n)
         self.dc = _b.DataConsistency(B, C, T, fft_rank, n, 0, mask_kind)
         self._l1_ws = torch.empty(max(_b.gleam_l1_loss_workspace_size(), 256), dtype=torch.uint8, device=y.device)
@@ -88,10 +92,16 @@ class ResidualPrior(nn.Module):
     convolution, and ``dropout`` regularises what a block adds (while training).  Residual add, dropout and the next block's norm
     are then one operator of the library (``prior_ops.dropout_add_layer_norm``), which stores no mask: the backward pass
     draws it again from ``generator`` (a ``prior_ops.DropoutGenerator``, shared by all priors of a network).  An evaluation takes
-    no range of the generator.  Either option leaves a prior that can be differentiated once."""
+    no range of the generator.  Either option leaves a prior that can be differentiated once.
 
-    def __init__(self, features=16, blocks=2, norm=False, dropout=0.0, generator=None):
+    ``recurrent`` lets the frames of an example see one another in front of the blocks: a gated recurrence of the library
+    (``scan_ops.gated_scan``) runs along them for every feature and voxel, "causal" from the first frame on, "both" in both directions.
+    A causal prior also takes frames as they arrive (``live``)."""
+
+    def __init__(self, features=16, blocks=2, norm=False, dropout=0.0, generator=None, recurrent=None):
         super().__init__()
+        if recurrent not in (None, "causal", "both"):
+            raise ValueError("recurrent = %r is neither None, \"causal\" nor \"both\"" % (recurrent,))
         if not 0.0 <= dropout <= 1.0:
             raise ValueError("dropout = %r is not a probability" % (dropout,))
         if dropout > 0.0 and generator is None:
@@ -102,16 +112,58 @@ class ResidualPrior(nn.Module):
                           nn.ReLU(), nn.Conv2d(features, features, 3, padding=1)) for _ in range(blocks)])
         self.tail = nn.Conv2d(features, 2, 3, padding=1)
         self.dropout, self.generator = float(dropout), generator
+        self.recurrent, self.gates, self.mix = recurrent, None, None
+        if recurrent is not None:
+            self.gates = nn.Conv2d(features, (4 if recurrent == "both" else 2) * features, 3, padding=1)
+            self.mix = nn.Conv2d(features, features, 1)
         self.norm_weight = self.norm_bias = None
         if norm:
             self.norm_weight = nn.ParameterList([nn.Parameter(torch.ones(features)) for _ in range(blocks + 1)])
             self.norm_bias = nn.ParameterList([nn.Parameter(torch.zeros(features)) for _ in range(blocks + 1)])
 
-    def forward(self, x_ch):                      # (B, 2, T, 1, n1, n2)
+    def _along_frames(self, f, frames, lengths):
+        """Adds what the recurrence over the frames finds; (B T n0, features, n1, n2)."""
+        u = self.gates(f)
+        u = u.view((frames[0], frames[1], -1) + u.shape[1:])
+        F = f.shape[1]
+        parts = [u[:, :, :, k * F:(k + 1) * F] for k in range(u.shape[3] // F)]
+        y, _ = _s.gated_scan(parts[0], parts[1], None, lengths, dim=1)
+        if self.recurrent == "both":
+            y = y + _s.gated_scan(parts[2], parts[3], None, lengths, dim=1, reverse=True)[0]
+        return f + self.mix(y.reshape(f.shape))
+
+    @torch.no_grad()
+    def live(self, x_ch, state=None):
+        """(output, state) for one new frame, x_ch of one frame; ``state`` is what the frame before returned (None: there was none) and is
+        updated in place.  As an evaluation: nothing is dropped, no gradients."""
+        if self.recurrent != "causal":
+            raise RuntimeError("frames one at a time need recurrent=\"causal\"")
+        B, _, T, n0, n1, n2 = x_ch.shape
+        if T != 1:
+            raise ValueError("one frame is wanted (shape %s)" % (tuple(x_ch.shape),))
+        h = x_ch.permute(0, 2, 3, 1, 4, 5).reshape(B * n0, 2, n1, n2)
+        f = self.head(h)
+        u = self.gates(f)
+        if state is None:
+            state = torch.zeros(f.shape, dtype=torch.float32, device=f.device)
+        F = f.shape[1]
+        f = f + self.mix(_s.gated_step(u[:, :F], u[:, F:], state))
+        return self._finish(x_ch, h, self._blocks(f, 0.0)), state
+
+    def forward(self, x_ch, lengths=None):        # (B, 2, T, 1, n1, n2)
         B, _, T, n0, n1, n2 = x_ch.shape
         h = x_ch.permute(0, 2, 3, 1, 4, 5).reshape(B * T * n0, 2, n1, n2)
         f = self.head(h)
-        p = self.dropout if self.training else 0.0
+        if self.recurrent is not None:
+            f = self._along_frames(f, (B, T), lengths)
+        return self._finish(x_ch, h, self._blocks(f, self.dropout if self.training else 0.0))
+
+    def _finish(self, x_ch, h, f):
+        B, _, T, n0, n1, n2 = x_ch.shape
+        h = h + self.tail(f)
+        return h.reshape(B, T, n0, 2, n1, n2).permute(0, 3, 1, 2, 4, 5).contiguous()
+
+    def _blocks(self, f, p):
         if self.norm_weight is not None:
             w, b = self.norm_weight, self.norm_bias
             y = _p.layer_norm(f, w[0], b[0], dim=1)
@@ -124,21 +176,58 @@ class ResidualPrior(nn.Module):
         else:
             for blk in self.blocks:
                 f = _p.dropout(blk(f), p, self.generator, residual=f) if p > 0.0 else f + blk(f)
-        h = h + self.tail(f)
-        return h.reshape(B, T, n0, 2, n1, n2).permute(0, 3, 1, 2, 4, 5).contiguous()
+        return f
 
 
 class GleamModule(nn.Module):
     """`iterations` unrolled steps x <- f_theta_i(DC(x)) that are trained together (one greedy module)."""
 
-    def __init__(self, iterations=1, features=16, blocks=2, norm=False, dropout=0.0, generator=None):
+    def __init__(self, iterations=1, features=16, blocks=2, norm=False, dropout=0.0, generator=None, recurrent=None):
         super().__init__()
-        self.priors = nn.ModuleList([ResidualPrior(features, blocks, norm, dropout, generator) for _ in range(iterations)])
+        self.priors = nn.ModuleList([ResidualPrior(features, blocks, norm, dropout, generator, recurrent) for _ in range(iterations)])
 
     def forward(self, x_ch, step: DataConsistencyStep):
         for prior in self.priors:
-            x_ch = prior(step.apply(x_ch))
+            x_ch = step.apply(x_ch)
+            x_ch = prior(x_ch) if step.lengths is None else prior(x_ch, step.lengths)
         return x_ch
+
+
+class Optimizers:
+    """Several optimisers that step together, for loops that take one."""
+
+    def __init__(self, optimizers):
+        self.optimizers = list(optimizers)
+
+    def zero_grad(self, set_to_none=True):
+        for o in self.optimizers:
+            o.zero_grad(set_to_none=set_to_none)
+
+    def step(self):
+        for o in self.optimizers:
+            o.step()
+
+    def state_dict(self):
+        return [o.state_dict() for o in self.optimizers]
+
+    def load_state_dict(self, state):
+        if len(state) != len(self.optimizers):
+            raise ValueError("%d states for %d optimisers" % (len(state), len(self.optimizers)))
+        for o, s in zip(self.optimizers, state):
+            o.load_state_dict(s)
+
+
+def module_optimizer(module, lr=1e-3, weight_decay=0.0, **muon):
+    """Muon (``ortho_ops.Muon``, whose other arguments may be given) for the convolutions' weights of a module, Adam with the paper's
+    beta = (0.9, 0.999) for its vectors."""
+    params = [p for p in module.parameters() if p.requires_grad]
+    matrices, vectors = [p for p in params if p.dim() >= 2], [p for p in params if p.dim() < 2]
+    both = []
+    if matrices:
+        both.append(_o.Muon(matrices, lr=lr, weight_decay=weight_decay, **muon))
+    if vectors:
+        both.append(torch.optim.Adam(vectors, lr=lr, betas=(0.9, 0.999)))
+    return Optimizers(both)
 
 
 def greedy_step(modules, optimizers, x0_ch, step: DataConsistencyStep):

@@ -1,0 +1,242 @@
+"""Orthogonalised updates on the GPU against their definition in 64 bits (oracle.ortho_oracle states the tolerance)."""
+import numpy as np
+import pytest
+
+from oracle import ortho_oracle as oo
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+TYPES = {"float32": torch.float32, "float16": torch.float16, "bfloat16": torch.bfloat16}
+
+
+def host(t):
+    return t.detach().double().cpu().numpy()
+
+
+def close(got, its, dtype, what=""):
+    """The last iterate; storing rounds by half a step of the type (float16: or of its smallest numbers)."""
+    ref, got = its[-1], host(got)
+    norm = np.sqrt((ref ** 2).sum())
+    most = oo.tolerance(its)
+    if dtype != torch.float32:
+        most += torch.finfo(dtype).eps / 2 * norm + torch.finfo(dtype).smallest_normal * np.sqrt(ref.size)
+    assert np.isfinite(got).all() and got.shape == ref.shape, what
+    assert np.sqrt(((got - ref) ** 2).sum()) <= most + 2.0 ** -23 * norm, what
+
+
+def matrices(count, rows, cols, dtype=torch.float32, seed=0, spread=1.0):
+    """Singular values that fall off."""
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    n = min(rows, cols)
+    u, v = torch.randn(count, rows, n, generator=gen, device="cuda"), torch.randn(count, n, cols, generator=gen, device="cuda")
+    return (spread * (u / (1 + torch.arange(n, device="cuda"))) @ v).to(dtype)
+
+
+SHAPES = [(1, 1, 1), (1, 1, 200), (1, 200, 1), (3, 7, 5), (2, 64, 64), (2, 100, 900), (2, 900, 100), (1, 127, 129), (1, 129, 127), (1, 128, 128), (1, 130, 1000),
+          (1, 257, 300), (1, 300, 257), (1, 640, 651), (5, 2, 900), (2, 100, 18), (1, 60, 5000), (1, 384, 1024)]
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("steps", [1, 2, 5])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_orthogonalise(shape, steps, dtype):
+    import paper_2207_08393_b200 as g
+    x = matrices(*shape, dtype=TYPES[dtype])
+    before = x.clone()
+    y = g.orthogonalise(x, steps)
+    assert y.dtype == x.dtype and torch.equal(x, before)
+    for k in range(shape[0]):
+        close(y[k], oo.iterates(host(x[k]), steps), TYPES[dtype])
+
+
+@pytest.mark.parametrize("spread", [1e-12, 1e-4, 1e6, 1e12])
+def test_any_magnitude(spread):
+    import paper_2207_08393_b200 as g
+    x = matrices(1, 40, 70, spread=spread)
+    close(g.orthogonalise(x)[0], oo.iterates(host(x[0]), 5), torch.float32)
+
+
+def test_other_coefficients_and_many_turns():
+    """1.875, -1.25, 0.375 converge: after enough turns the rows are orthonormal."""
+    import paper_2207_08393_b200 as g
+    x = torch.randn(2, 50, 120, device="cuda")
+    y = g.orthogonalise(x, 20, (1.875, -1.25, 0.375))
+    eye = torch.eye(50, dtype=torch.float64, device="cuda")
+    assert float((y.double() @ y.double().mT - eye).abs().max()) < 1e-5
+    close(g.orthogonalise(x, 2, (2.0, -1.5, 0.5))[0], oo.iterates(host(x[0]), 2, (2.0, -1.5, 0.5)), torch.float32)
+
+
+def test_zeros_ones_and_matrices_that_are_not_numbers():
+    import paper_2207_08393_b200 as g
+    x = matrices(5, 130, 200)
+    want = g.orthogonalise(x)
+    x[1] = 0
+    x[2, 5, 7] = float("nan")
+    x[3, 129, 199] = float("inf")
+    y = g.orthogonalise(x)
+    assert int(torch.count_nonzero(y[1])) == 0
+    assert bool(torch.isnan(y[2]).all()) and bool(torch.isnan(y[3]).all())
+    assert torch.equal(y[0], want[0]) and torch.equal(y[4], want[4])
+    close(g.orthogonalise(torch.ones(1, 9, 33, device="cuda"))[0], oo.iterates(np.ones((9, 33)), 5), torch.float32)
+
+
+def test_more_matrices_than_a_launch_takes():
+    import paper_2207_08393_b200 as g
+    x = matrices(150, 12, 40)
+    y = g.orthogonalise(x.view(3, 50, 12, 40)).view(150, 12, 40)
+    for k in (0, 63, 64, 127, 128, 149):
+        assert torch.equal(y[k], g.orthogonalise(x[k].clone()))
+
+
+@pytest.mark.parametrize("shape", [(40, 90, 130), (2, 300, 700), (1, 1030, 2100), (70, 20, 30)])
+def test_the_bits_repeat_and_do_not_depend_on_the_neighbours(shape):
+    import paper_2207_08393_b200 as g
+    x = matrices(*shape)
+    y = g.orthogonalise(x)
+    assert torch.equal(y, g.orthogonalise(x))
+    close(y[-1], oo.iterates(host(x[-1]), 5), torch.float32)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("nesterov", [False, True])
+@pytest.mark.parametrize("shape", [(3, 60, 540), (2, 100, 18), (1, 2, 900), (2, 200, 150), (66, 5, 9)])
+def test_muon_step(shape, nesterov, dtype):
+    import paper_2207_08393_b200 as g
+    count, rows, cols = shape
+    t = TYPES[dtype]
+    w = [v.clone() for v in torch.randn(shape, device="cuda").to(t)]
+    grads = [v.clone() for v in matrices(*shape, dtype=t, seed=1)]
+    mom = [v.clone() for v in matrices(*shape, seed=2)]
+    keep = [[v.clone() for v in s] for s in (w, grads, mom)]
+    lr, mu, wd, scale = 0.125, 0.75, 0.25, 2.0
+    g.muon_step(w, grads, mom, lr, mu, nesterov, wd, scale, steps=2)
+    for k in (0, count - 1):
+        m = mu * host(keep[2][k]) + host(keep[1][k])
+        assert np.abs(host(mom[k]) - m).max() <= 2.0 ** -23 * np.abs(m).max()
+        its = oo.iterates(host(keep[1][k]) + mu * m if nesterov else m, 2)
+        ref = (1 - lr * wd) * host(keep[0][k]) - lr * scale * its[-1]
+        norm = np.sqrt((ref ** 2).sum())
+        # the source is rounded once more than in orthogonalise: 2^-23 of it, at most 14 times as much of a turn's result
+        most = lr * scale * (oo.tolerance(its) + 14 * 5 * 2.0 ** -23 * np.sqrt((its[1] ** 2).sum())) + (torch.finfo(t).eps / 2 + 2.0 ** -23) * norm
+        assert np.sqrt(((host(w[k]) - ref) ** 2).sum()) <= most
+    assert all(torch.equal(a, b) for a, b in zip(grads, keep[1]))
+
+
+def test_canaries_and_overlaps():
+    import paper_2207_08393_b200 as g
+    st = torch.cuda.current_stream()
+    for rows, cols in ((33, 70), (70, 33), (130, 257)):
+        n = rows * cols
+        d = g.make_matrix_dims(0, 2, rows, cols, stream=st)
+        need = g.gleam_orthogonalise_workspace_size(d)
+        ws = torch.full((need + 256,), 7, dtype=torch.uint8, device="cuda")
+        d.workspace, d.workspace_bytes = ws.data_ptr(), need
+        x = matrices(2, rows, cols)
+        out = torch.full((2 * n + 16,), 9.0, device="cuda")
+        parts = [out[4:4 + n], out[8 + n:8 + 2 * n]]
+        g.gleam_orthogonalise([x[0], x[1]], parts, d)
+        g.gleam_orthogonalise_check_status(d)
+        assert bool((ws[need:] == 7).all()) and bool((out[:4] == 9).all()) and bool((out[4 + n:8 + n] == 9).all()) and bool((out[8 + 2 * n:] == 9).all())
+        assert torch.equal(torch.stack(parts).view(2, rows, cols), g.orthogonalise(x))
+        for xs, outs in (([x[0], x[1]], [x[0], parts[1]]), ([x[0], x[1]], [parts[0], parts[0]]), ([x[0], x[1]], [out[:n], out[n - 1:]]), ([ws, x[1]], parts)):
+            with pytest.raises(g.GleamError) as e:
+                g.gleam_orthogonalise(xs, outs, d)
+            assert e.value.status == -6
+        g.gleam_orthogonalise([x[0], x[0]], parts, d)                   # the same matrix twice is read twice
+        assert torch.equal(parts[0], parts[1])
+
+
+def test_refusals():
+    import paper_2207_08393_b200 as g
+    x = torch.randn(4, 6, device="cuda")
+    for bad in (x[0], x.double(), x.t(), x[:, ::2]):
+        with pytest.raises(ValueError):
+            g.orthogonalise(bad)
+    m = torch.zeros(4, 6, device="cuda")
+    for w, gr, mo in ((x, x.half(), m), (x, x[:3], m), (x, x, m.half()), (x, x.t().contiguous().t(), m), (x.t().contiguous().t(), x, m), (x, x.cpu(), m), (x[0], x[0], m[0])):
+        with pytest.raises(ValueError):
+            g.muon_step([w], [gr], [mo], 0.1)
+    with pytest.raises(g.GleamError):
+        g.muon_step([x], [x.clone()], [m], 0.1, momentum=1.5)
+    with pytest.raises(g.GleamError):
+        g.muon_step([x, x], [x.clone(), x.clone()], [m, m.clone()], 0.1)
+    assert g.orthogonalise(torch.empty(0, 4, 6, device="cuda")).shape == (0, 4, 6)
+    assert g.orthogonalise(torch.empty(2, 0, 6, device="cuda")).shape == (2, 0, 6)
+    g.muon_step([], [], [], 0.1)
+
+
+def test_other_streams_and_graphs():
+    import paper_2207_08393_b200 as g
+    x = matrices(3, 150, 400)
+    first = g.orthogonalise(x)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        again = g.orthogonalise(x)
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(first, again)
+    graphs = []
+    for _ in range(2):
+        here, graph = x.clone(), torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = g.orthogonalise(here)
+        graphs.append((graph, here, out))
+    graphs[1][1].copy_(matrices(3, 150, 400, seed=9))
+    for graph, _, _ in graphs + graphs:
+        graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(first, graphs[0][2]) and torch.equal(g.orthogonalise(graphs[1][1]), graphs[1][2])
+
+
+def test_the_optimiser_is_the_step():
+    """Weights of several shapes and orders, a missing gradient, and a resumed run."""
+    import paper_2207_08393_b200 as g
+    torch.manual_seed(4)
+    shapes = [(16, 2, 3, 3), (16, 16, 3, 3), (16, 16, 3, 3), (2, 16, 3, 3), (12, 20), (5, 7)]
+
+    def params():
+        torch.manual_seed(5)
+        ps = [torch.nn.Parameter(torch.randn(s, device="cuda")) for s in shapes]
+        ps[1].data = ps[1].data.contiguous(memory_format=torch.channels_last)
+        return ps
+
+    torch.manual_seed(6)
+    grads = [[torch.randn(s, device="cuda") for s in shapes] for _ in range(4)]
+    kw = dict(lr=0.05, momentum=0.9, weight_decay=0.1)
+    a = params()
+    opt = g.Muon(a, **kw)
+    w = [p.detach().contiguous().clone() for p in a]
+    m = [torch.zeros_like(v) for v in w]
+    for turn in grads[:2]:
+        for p, v in zip(a[:-1], turn):
+            p.grad = v.contiguous(memory_format=torch.channels_last) if v.dim() == 4 else v.clone()
+        opt.step()
+        for k, v in enumerate(turn[:-1]):
+            g.muon_step([w[k]], [v], [m[k]], 0.05, 0.9, True, 0.1, 0.2 * max(w[k].shape[0], w[k][0].numel()) ** 0.5)
+    for p, v in zip(a, w):
+        assert torch.equal(p.detach().contiguous(), v)
+    b = params()
+    for p, q in zip(b, a):
+        p.data.copy_(q.data)
+    other = g.Muon(b, **kw)
+    other.load_state_dict(opt.state_dict())
+    for turn in grads[2:]:
+        for ps, o in ((a, opt), (b, other)):
+            for p, v in zip(ps[:-1], turn):
+                p.grad = v.clone()
+            o.step()
+    assert all(torch.equal(p, q) for p, q in zip(a, b))
+
+
+def test_half_precision_weights_keep_a_32_bit_momentum():
+    import paper_2207_08393_b200 as g
+    p = torch.nn.Parameter(torch.randn(8, 24, device="cuda", dtype=torch.bfloat16))
+    opt = g.Muon([p])
+    p.grad = torch.randn_like(p)
+    opt.step()
+    assert opt.state[p]["momentum"].dtype == torch.float32
+    again = g.Muon([p])
+    again.load_state_dict(opt.state_dict())
+    assert again.state[p]["momentum"].dtype == torch.float32
+    assert torch.equal(again.state[p]["momentum"], opt.state[p]["momentum"])

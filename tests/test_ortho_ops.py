@@ -1,0 +1,140 @@
+"""Orthogonalised updates without a GPU: the definition two ways, and the host-side refusals."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2207_08393_b200 as g
+from oracle import ortho_oracle as oo
+from paper_2207_08393_b200 import _build, binding
+
+
+@pytest.fixture(scope="module")
+def lib():
+    _build.build()
+    return g.load_library()
+
+
+@pytest.mark.parametrize("shape", [(1, 1), (5, 9), (9, 5), (7, 7)])
+def test_products_act_on_the_singular_values(shape):
+    x = np.random.default_rng(0).normal(size=shape)
+    for steps in (1, 3, 5):
+        assert np.allclose(oo.iterates(x, steps)[-1], oo.by_singular_values(x, steps), rtol=0, atol=1e-12)
+
+
+def test_five_turns_bring_singular_values_near_one():
+    x = np.random.default_rng(1).normal(size=(20, 50))
+    s = np.linalg.svd(oo.iterates(x, 5)[-1], compute_uv=False)
+    assert s.min() > 0.6 and s.max() < 1.25
+
+
+def test_struct_layouts_match_the_header():
+    d = binding.gleam_matrix_dims
+    assert (d.count.offset, d.turns.offset, d.eps.offset, d.stream.offset, d.workspace_bytes.offset) == (8, 32, 48, 56, 72)
+    assert ctypes.sizeof(d) == 80 and ctypes.sizeof(binding.gleam_muon_args) == 20
+
+
+A = 1 << 30                                         # addresses that are never dereferenced
+BAD, NULL = binding.GLEAM_ERR_BAD_DIMS, binding.GLEAM_ERR_NULL_POINTER
+
+
+def dims(**kw):
+    args = dict(dtype=0, count=2, rows=20, cols=30)
+    args.update(kw)
+    return g.make_matrix_dims(**args)
+
+
+def status(call, *args):
+    with pytest.raises(g.GleamError) as e:
+        call(*args)
+    return e.value.status
+
+
+def muon(**kw):
+    args = dict(lr=0.1, momentum=0.9, weight_decay=0.0, scale=1.0, nesterov=1)
+    args.update(kw)
+    return g.gleam_muon_args(**args)
+
+
+@pytest.mark.parametrize("kw", [dict(dtype=3), dict(dtype=-1), dict(count=-1), dict(rows=-1), dict(cols=-1), dict(rows=(1 << 20) + 1), dict(rows=16385, cols=20000),
+                                dict(rows=2000, cols=1 << 20), dict(turns=0), dict(turns=101), dict(eps=0.0), dict(eps=-1.0), dict(eps=float("nan")),
+                                dict(coefficients=(17.0, 0, 0)), dict(coefficients=(1.0, float("nan"), 0)), dict(coefficients=(1.0, 0, float("inf")))])
+def test_bad_sizes(lib, kw):
+    d = dims(workspace=8 * A, workspace_bytes=1 << 40, **kw)
+    assert status(g.gleam_orthogonalise_workspace_size, d) == BAD
+    assert status(g.gleam_orthogonalise, [A, 2 * A], [3 * A, 4 * A], d) == BAD
+    assert status(g.gleam_orthogonalise_check_status, d) == BAD
+    assert status(g.gleam_muon_step, [A, 2 * A], [3 * A, 4 * A], [5 * A, 6 * A], muon(), d) == BAD
+
+
+@pytest.mark.parametrize("kw", [dict(lr=-1.0), dict(lr=float("nan")), dict(momentum=1.0), dict(momentum=-0.1), dict(weight_decay=-0.1), dict(weight_decay=float("inf")),
+                                dict(scale=float("nan")), dict(nesterov=2)])
+def test_bad_steps(lib, kw):
+    assert status(g.gleam_muon_step, [A, 2 * A], [3 * A, 4 * A], [5 * A, 6 * A], muon(**kw), dims(workspace=8 * A, workspace_bytes=1 << 40)) == BAD
+
+
+def test_pointers_workspace_and_versions(lib):
+    need = g.gleam_orthogonalise_workspace_size(dims())
+    assert need > 0
+    assert status(g.gleam_orthogonalise, [A, 2 * A], [3 * A, 4 * A], dims()) == NULL
+    assert status(g.gleam_orthogonalise, [A, 2 * A], [3 * A, 4 * A], dims(workspace=8 * A, workspace_bytes=need - 1)) == binding.GLEAM_ERR_WORKSPACE_TOO_SMALL
+    assert status(g.gleam_orthogonalise_check_status, dims(workspace=8 * A, workspace_bytes=need - 1)) == binding.GLEAM_ERR_WORKSPACE_TOO_SMALL
+    assert status(g.gleam_orthogonalise, [A, 2 * A], [3 * A, 4 * A], dims(workspace=8 * A + 128, workspace_bytes=need)) == BAD
+    d = dims(workspace=8 * A, workspace_bytes=need)
+    for at in range(2):
+        for k in range(2):
+            lists = [[A, 2 * A], [3 * A, 4 * A]]
+            lists[at][k] = None
+            assert status(g.gleam_orthogonalise, *lists, d) == NULL
+            lists[at][k] = A + 2
+            assert status(g.gleam_orthogonalise, *lists, d) == BAD
+    for at in range(3):
+        lists = [[A, 2 * A], [3 * A, 4 * A], [5 * A, 6 * A]]
+        lists[at][1] = None
+        assert status(g.gleam_muon_step, *lists, muon(), d) == NULL
+    d.struct_version = 2
+    assert status(g.gleam_orthogonalise, [A, 2 * A], [3 * A, 4 * A], d) == BAD
+    assert lib.gleam_orthogonalise(None, None, None) == NULL
+    assert lib.gleam_muon_step(None, None, None, None, None) == NULL
+
+
+def test_nothing_to_do(lib):
+    for kw in (dict(count=0), dict(rows=0), dict(cols=0)):
+        d = dims(**kw)
+        assert g.gleam_orthogonalise_workspace_size(d) == 0
+        g.gleam_orthogonalise([], [], d)
+        g.gleam_orthogonalise_check_status(d)
+        g.gleam_muon_step([], [], [], muon(), d)
+
+
+def test_the_torch_layer_refuses():
+    x = torch.zeros(3, 4)
+    with pytest.raises(ValueError, match="CUDA"):
+        g.orthogonalise(x)
+    with pytest.raises(ValueError, match="CUDA"):
+        g.muon_step([x], [x], [x], 0.1)
+    with pytest.raises(ValueError, match="1 weights"):
+        g.muon_step([x], [], [x], 0.1)
+    p = torch.nn.Parameter(x)
+    for kw in (dict(lr=-1.0), dict(momentum=1.0), dict(weight_decay=-1.0), dict(scale="adam")):
+        with pytest.raises(ValueError):
+            g.Muon([p], **kw)
+    with pytest.raises(ValueError, match="another optimiser"):
+        g.Muon([torch.nn.Parameter(torch.zeros(5))])
+
+
+def test_priors_along_frames_are_asked_for():
+    from paper_2207_08393_b200 import gleam_loop as gl
+    with pytest.raises(ValueError, match="recurrent"):
+        gl.ResidualPrior(8, 2, recurrent="backward")
+    with pytest.raises(RuntimeError, match="causal"):
+        gl.ResidualPrior(8, 2, recurrent="both").live(torch.zeros(1, 2, 1, 1, 4, 4))
+    with pytest.raises(ValueError, match="one frame"):
+        gl.ResidualPrior(8, 2, recurrent="causal").live(torch.zeros(1, 2, 3, 1, 4, 4))
+    plain = gl.ResidualPrior(8, 2)
+    assert not any("gates" in k or "mix" in k for k in plain.state_dict())
+    opt = gl.module_optimizer(gl.GleamModule(2, 8, 1, norm=True, recurrent="both"), lr=0.01)
+    assert [type(o).__name__ for o in opt.optimizers] == ["Muon", "Adam"]
+    with pytest.raises(ValueError):
+        opt.load_state_dict([])

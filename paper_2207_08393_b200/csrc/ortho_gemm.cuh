@@ -4,6 +4,9 @@
 //
 // A and P are symmetric: the blocks below the diagonal and on it are computed and stored on both sides, and A A is A A^T, so that GRAM and
 // POLY read both operands the same way.
+//
+// One warp copies, one thread issues products, all eight warps finish: sums from tensor memory to shared memory, there added over the
+// cluster and blended with the old values, which were fetched while the products ran.
 #pragma once
 #include "launch_overlap.cuh"
 #include "ortho_common.cuh"
@@ -26,11 +29,12 @@ template <int KIND> __host__ inline int tiles_of(const Args& a) { return KIND ==
 // The sums as 32-bit numbers in shared memory: rows of 128, their 16-byte pieces in an order that keeps 32 rows apart.
 __device__ __forceinline__ int sum_at(int r, int c) { return r * BLOCK + ((((c >> 2) ^ r) & 31) << 2) + (c & 3); }
 
-template <int KIND>
+template <int KIND, int RANKS>
 __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_constant__ Args a) {
     extern __shared__ __align__(1024) unsigned char smem[];
+    constexpr int ranks = RANKS, ITEMS = BLOCK * BLOCK / 8 / RANKS / GEMM_THREADS;     // eights of a row that a thread finishes
     constexpr bool SIDES = KIND == GRAM || KIND == POLY;               // both operands are rows of one matrix
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, ranks = gridDim.x, rank = ranks > 1 ? (int)tc::cluster_rank() : 0, m = blockIdx.z;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = ranks > 1 ? (int)tc::cluster_rank() : 0, m = blockIdx.z;
     int bi, bj;
     if (SIDES) {
         bi = 0;
@@ -62,23 +66,30 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
     const bool one = SIDES && bi == bj;                                            // the operands are the same
     bool failed = false;
 
-    if (warp == 0) {
-        // 16 runs of 1 KB for each piece of an operand: half the columns (left; right of SIDES) or half the rows of a block
+    if (warp == 0 && lane == 0) {
+        // rows beyond the matrix are not copied where they are rows of the result: what stands there is not stored
+        const long long lrows = a.S - (long long)bi * BLOCK, rrows = a.S - (long long)bj * BLOCK;
+        const uint32_t lrun = (uint32_t)((lrows < BLOCK ? lrows + 7 : BLOCK) >> 3) * 1024, rrun = SIDES ? (uint32_t)((rrows < BLOCK ? rrows + 7 : BLOCK) >> 3) * 1024 : 8192;
         for (int i = 0; i < count; ++i) {
-            const int s = i % STAGES, k = first + i, kb = k >> 1, half = k & 1, piece = lane >> 4, run = lane & 15;
+            const int s = i % STAGES, k = first + i, kb = k >> 1, half = k & 1;
             if (i >= STAGES && !tc::barrier_wait(empty(s), (i / STAGES - 1) & 1)) { failed = true; break; }
-            const uint32_t to = stages + s * STAGE_BYTES + piece * (OPERAND_BYTES / 2) + run * 1024;
-            if (lane == 0) tc::barrier_expect(full(s), one ? OPERAND_BYTES : STAGE_BYTES);
-            __syncwarp();
-            tc::bulk_copy(to, left + ((long long)bi * lblocks + kb) * BLOCK_BYTES + piece * PIECE_BYTES + run * 2048 + half * 1024, 1024, full(s));
-            if (SIDES) {
-                if (!one) tc::bulk_copy(to + OPERAND_BYTES, right + ((long long)bj * lblocks + kb) * BLOCK_BYTES + piece * PIECE_BYTES + run * 2048 + half * 1024, 1024, full(s));
-            } else {
-                tc::bulk_copy(to + OPERAND_BYTES, right + ((long long)kb * a.lblocks + bj) * BLOCK_BYTES + piece * PIECE_BYTES + half * (PIECE_BYTES / 2) + run * 1024, 1024, full(s));
+            const uint32_t to = stages + s * STAGE_BYTES;
+            tc::barrier_expect(full(s), 2 * lrun + (SIDES ? one ? 0 : 2 * rrun : 4 * rrun));
+#pragma unroll
+            for (int piece = 0; piece < 2; ++piece) {
+                const uint32_t lo = piece * (OPERAND_BYTES / 2);
+                tc::bulk_copy(to + lo, left + ((long long)bi * lblocks + kb) * BLOCK_BYTES + piece * PIECE_BYTES + half * (PIECE_BYTES / 2), lrun, full(s));
+                if (SIDES) {
+                    if (!one) tc::bulk_copy(to + OPERAND_BYTES + lo, right + ((long long)bj * lblocks + kb) * BLOCK_BYTES + piece * PIECE_BYTES + half * (PIECE_BYTES / 2), rrun, full(s));
+                } else {
+                    // half the rows of both halves
+                    for (int h = 0; h < 2; ++h)
+                        tc::bulk_copy(to + OPERAND_BYTES + lo + h * 8192, right + ((long long)kb * a.lblocks + bj) * BLOCK_BYTES + piece * PIECE_BYTES + h * (PIECE_BYTES / 2) + half * 8192, 8192, full(s));
+                }
             }
         }
     } else if (warp == 1 && lane == 0) {
-        const uint32_t what = tc::instruction(BLOCK, !SIDES);
+        const uint32_t what = tc::instruction(SIDES ? BLOCK : BLOCK / 2, !SIDES);
         for (int i = 0; i < count; ++i) {
             const int s = i % STAGES;
             if (!tc::barrier_wait(full(s), (i / STAGES) & 1)) {
@@ -91,20 +102,36 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
             constexpr int HALF = OPERAND_BYTES / 2;                                 // from hi to lo
 #pragma unroll
             for (int q = 0; q < STEP / 16; ++q) {
-                // cores of left: 1024 bytes from one to the next along M, 128 along K; of right (!SIDES): 128 along N, 2048 along K
+                // cores of left: 1024 bytes from one to the next along M, 128 along K; of right (!SIDES): 128 along N, 1024 along K, its halves of
+                // 64 columns apart
                 const uint64_t lh = tc::descriptor(l + q * 256, 128, 1024), ll = tc::descriptor(l + HALF + q * 256, 128, 1024);
-                const uint64_t rh = SIDES ? tc::descriptor(r + q * 256, 128, 1024) : tc::descriptor(r + q * 4096, 2048, 128);
-                const uint64_t rl = SIDES ? tc::descriptor(r + HALF + q * 256, 128, 1024) : tc::descriptor(r + HALF + q * 4096, 2048, 128);
-                tc::product(sums + SUMS * BLOCK, ll, rh, what, i > 0 || q > 0);
-                tc::product(sums + SUMS * BLOCK, lh, rl, what, true);
-                tc::product(sums + i % SUMS * BLOCK, lh, rh, what, i >= SUMS || q > 0);
+#pragma unroll
+                for (int h = 0; h < (SIDES ? 1 : 2); ++h) {
+                    const uint64_t rh = SIDES ? tc::descriptor(r + q * 256, 128, 1024) : tc::descriptor(r + h * 8192 + q * 2048, 1024, 128);
+                    const uint64_t rl = SIDES ? tc::descriptor(r + HALF + q * 256, 128, 1024) : tc::descriptor(r + HALF + h * 8192 + q * 2048, 1024, 128);
+                    tc::product(sums + SUMS * BLOCK + h * 64, ll, rh, what, i > 0 || q > 0);
+                    tc::product(sums + SUMS * BLOCK + h * 64, lh, rl, what, true);
+                    tc::product(sums + i % SUMS * BLOCK + h * 64, lh, rh, what, i >= SUMS || q > 0);
+                }
             }
             tc::commit(empty(s));
         }
         tc::commit(done);
     }
     __syncwarp();
-    if (count > 0 && !tc::barrier_wait(done, 0)) failed = true;
+    // what is blended in is fetched while the products run
+    const unsigned char* old = KIND == POLY ? a.g + (square + (long long)bi * a.sblocks + bj) * BLOCK_BYTES : a.x + (wide + (long long)bi * a.lblocks + bj) * BLOCK_BYTES;
+    uint4 old_hi[ITEMS], old_lo[ITEMS];
+    auto row_of = [&](int k) { const int i = rank * ITEMS * GEMM_THREADS + k * GEMM_THREADS + threadIdx.x; return (i & 7) + (i >> 7) * 8; };
+    const int col = ((threadIdx.x >> 3) & 15) * 8;
+    if (KIND != GRAM) {
+#pragma unroll
+        for (int k = 0; k < ITEMS; ++k) {
+            old_hi[k] = *reinterpret_cast<const uint4*>(old + core_at(row_of(k), col));
+            old_lo[k] = *reinterpret_cast<const uint4*>(old + PIECE_BYTES + core_at(row_of(k), col));
+        }
+    }
+    if (!tc::barrier_wait(done, 0)) failed = true;
     tc::fence_after();
 
     // the sums, in units of the stored values
@@ -115,23 +142,18 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
         for (int c0 = (warp >> 2) * 64; c0 < (warp >> 2) * 64 + 64; c0 += 32) {
             const uint32_t at = sums + ((uint32_t)((warp & 3) * 32) << 16) + c0;
             float v[32], t[32];
-            if (count > 0) {
-                tc::read_columns(at, v);
+            tc::read_columns(at, v);
 #pragma unroll 1
-                for (int k = 1; k < SUMS && k < count; ++k) {
-                    tc::read_columns(at + k * BLOCK, t);
+            for (int k = 1; k < SUMS && k < count; ++k) {
+                tc::read_columns(at + k * BLOCK, t);
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) v[j] += t[j];
-                }
-                tc::read_columns(at + SUMS * BLOCK, t);
+                for (int j = 0; j < 32; ++j) v[j] += t[j];
             }
+            tc::read_columns(at + SUMS * BLOCK, t);
 #pragma unroll
-            for (int j = 0; j < 32; j += 4) {
-                float4 f;
-                f.x = count > 0 ? (v[j] + t[j]) * (1.f / SCALE) : 0.f; f.y = count > 0 ? (v[j + 1] + t[j + 1]) * (1.f / SCALE) : 0.f;
-                f.z = count > 0 ? (v[j + 2] + t[j + 2]) * (1.f / SCALE) : 0.f; f.w = count > 0 ? (v[j + 3] + t[j + 3]) * (1.f / SCALE) : 0.f;
-                *reinterpret_cast<float4*>(sum + sum_at(row, c0 + j)) = f;
-            }
+            for (int j = 0; j < 32; j += 4)
+                *reinterpret_cast<float4*>(sum + sum_at(row, c0 + j)) = make_float4((v[j] + t[j]) * (1.f / SCALE), (v[j + 1] + t[j + 1]) * (1.f / SCALE),
+                                                                                    (v[j + 2] + t[j + 2]) * (1.f / SCALE), (v[j + 3] + t[j + 3]) * (1.f / SCALE));
         }
     }
     tc::fence_before();
@@ -140,94 +162,99 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
     if (failed) atomicOr(a.status, 1);
     if (ranks > 1) tc::cluster_sync();
 
-    // eight columns of a row, summed over the cluster
-    auto take = [&](int r, int c, float (&v)[8]) {
-        float4 f[2];
-        const uint32_t at[2] = {base + 1024 + 4 * sum_at(r, c), base + 1024 + 4 * sum_at(r, c + 4)};
+    // four columns of a row, summed over the cluster in the order of its blocks
+    auto take = [&](int at) {
+        float4 f[RANKS];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            f[h] = ranks > 1 ? tc::read_remote(at[h], 0) : *reinterpret_cast<const float4*>(smem + (at[h] - base));
-            for (int k = 1; k < ranks; ++k) {
-                const float4 g = tc::read_remote(at[h], k);
-                f[h].x += g.x; f[h].y += g.y; f[h].z += g.z; f[h].w += g.w;
-            }
-        }
-        v[0] = f[0].x; v[1] = f[0].y; v[2] = f[0].z; v[3] = f[0].w; v[4] = f[1].x; v[5] = f[1].y; v[6] = f[1].z; v[7] = f[1].w;
+        for (int k = 0; k < RANKS; ++k) f[k] = RANKS > 1 ? tc::read_remote(base + 1024 + 4 * at, k) : *reinterpret_cast<const float4*>(sum + at);
+#pragma unroll
+        for (int k = 1; k < RANKS; ++k) { f[0].x += f[k].x; f[0].y += f[k].y; f[0].z += f[k].z; f[0].w += f[k].w; }
+        return f[0];
     };
-    auto blend = [&](const unsigned char* block, int r, int c, float by, float (&v)[8], float times) {
+    auto take8 = [&](int r, int c, float (&v)[8]) {
+        const float4 f = take(sum_at(r, c)), g = take(sum_at(r, c + 4));
+        v[0] = f.x; v[1] = f.y; v[2] = f.z; v[3] = f.w; v[4] = g.x; v[5] = g.y; v[6] = g.z; v[7] = g.w;
+    };
+    auto blend = [&](const uint4& hi, const uint4& lo, float by, float (&v)[8], float times) {
         float u[8];
-        join8(*reinterpret_cast<const uint4*>(block + core_at(r, c)), *reinterpret_cast<const uint4*>(block + PIECE_BYTES + core_at(r, c)), u);
+        join8(hi, lo, u);
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = fmaf(by, u[j], times * v[j]);
     };
-    auto put = [&](unsigned char* block, int r, int c, const float (&v)[8]) {
+    // zeros beyond the matrix
+    auto put = [&](unsigned char* block, int r, int c, float (&v)[8], long long rows, long long cols) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (r >= rows || c + j >= cols) v[j] = 0.f;
         uint4 hi, lo;
         split8(v, hi, lo);
         *reinterpret_cast<uint4*>(block + core_at(r, c)) = hi;
         *reinterpret_cast<uint4*>(block + PIECE_BYTES + core_at(r, c)) = lo;
     };
-    const int items = BLOCK * BLOCK / 8 / ranks;
+    const long long rows = a.S - (long long)bi * BLOCK, cols = (SIDES ? a.S : a.L) - (long long)bj * BLOCK;
     if (KIND != LAST) {
-        const unsigned char* old = KIND == POLY ? a.g + (square + (long long)bi * a.sblocks + bj) * BLOCK_BYTES : a.x + (wide + (long long)bi * a.lblocks + bj) * BLOCK_BYTES;
         unsigned char* to = KIND == APPLY ? a.y + (wide + (long long)bi * a.lblocks + bj) * BLOCK_BYTES
                                           : (KIND == GRAM ? a.g : a.p) + (square + (long long)bi * a.sblocks + bj) * BLOCK_BYTES;
-        for (int i = rank * items + threadIdx.x; i < (rank + 1) * items; i += GEMM_THREADS) {
-            const int r = (i & 7) + (i >> 7) * 8, c = ((i >> 3) & 15) * 8;
+#pragma unroll
+        for (int k = 0; k < ITEMS; ++k) {
             float v[8];
-            take(r, c, v);
-            if (KIND == POLY) blend(old, r, c, a.b, v, a.c);
-            if (KIND == APPLY) blend(old, r, c, a.a, v, 1.f);
-            put(to, r, c, v);
+            take8(row_of(k), col, v);
+            if (KIND == POLY) blend(old_hi[k], old_lo[k], a.b, v, a.c);
+            if (KIND == APPLY) blend(old_hi[k], old_lo[k], a.a, v, 1.f);
+            put(to, row_of(k), col, v, rows, cols);
         }
         if (SIDES && !one) {
             // the block on the other side of the diagonal
-            const unsigned char* mirror = a.g + (square + (long long)bj * a.sblocks + bi) * BLOCK_BYTES;
-            unsigned char* over = (KIND == GRAM ? a.g : a.p) + (square + (long long)bj * a.sblocks + bi) * BLOCK_BYTES;
-            for (int i = rank * items + threadIdx.x; i < (rank + 1) * items; i += GEMM_THREADS) {
-                const int r = (i & 7) + (i >> 7) * 8, c = ((i >> 3) & 15) * 8;
+            const long long at = (square + (long long)bj * a.sblocks + bi) * BLOCK_BYTES;
+            if (KIND == POLY) {
+#pragma unroll
+                for (int k = 0; k < ITEMS; ++k) {
+                    old_hi[k] = *reinterpret_cast<const uint4*>(a.g + at + core_at(row_of(k), col));
+                    old_lo[k] = *reinterpret_cast<const uint4*>(a.g + at + PIECE_BYTES + core_at(row_of(k), col));
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < ITEMS; ++k) {
+                const int r = row_of(k);
                 float v[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const uint32_t at = base + 1024 + 4 * (sum_at(c + j, r) & ~3);
-                    float s = 0.f;
-                    for (int k = 0; k < ranks; ++k) {
-                        const float4 f = ranks > 1 ? tc::read_remote(at, k) : *reinterpret_cast<const float4*>(smem + (at - base));
-                        const float g = (r & 3) == 0 ? f.x : (r & 3) == 1 ? f.y : (r & 3) == 2 ? f.z : f.w;
-                        s = k == 0 ? g : s + g;
-                    }
-                    v[j] = s;
+                    const float4 f = take(sum_at(col + j, r) & ~3);
+                    v[j] = (r & 3) == 0 ? f.x : (r & 3) == 1 ? f.y : (r & 3) == 2 ? f.z : f.w;
                 }
-                if (KIND == POLY) blend(mirror, r, c, a.b, v, a.c);
-                put(over, r, c, v);
+                if (KIND == POLY) blend(old_hi[k], old_lo[k], a.b, v, a.c);
+                put((KIND == GRAM ? a.g : a.p) + at, r, col, v, cols, rows);
             }
         }
     } else {
-        const unsigned char* old = a.x + (wide + (long long)bi * a.lblocks + bj) * BLOCK_BYTES;
-        const long long s0 = (long long)bi * BLOCK, l0 = (long long)bj * BLOCK;
-        auto finish = [&](long long at, float v) {
-            v *= 1.f / SCALE;
-            if (a.update) v = fmaf(a.keep, load_as(a.out[m], a.dtype, at), -a.move * v);
-            store_as(a.out[m], a.dtype, at, v);
-        };
-        for (int i = threadIdx.x; i < BLOCK * BLOCK / 8; i += GEMM_THREADS) {
-            const int r = a.tall ? (i & 7) + (i >> 7) * 8 : i >> 4, c = a.tall ? ((i >> 3) & 15) * 8 : (i & 15) * 8;
-            float v[8];
-            take(r, c, v);
-            blend(old, r, c, a.a, v, 1.f);
-            if (a.tall) {
-                *reinterpret_cast<float4*>(sum + sum_at(r, c)) = make_float4(v[0], v[1], v[2], v[3]);
-                *reinterpret_cast<float4*>(sum + sum_at(r, c + 4)) = make_float4(v[4], v[5], v[6], v[7]);
-            } else if (s0 + r < a.S) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (l0 + c + j < a.L) finish((s0 + r) * a.cols + l0 + c + j, v[j]);
-            }
+        for (int k = 0; k < ITEMS; ++k) {
+            float v[8];
+            take8(row_of(k), col, v);
+            blend(old_hi[k], old_lo[k], a.a, v, 1.f);
+            *reinterpret_cast<float4*>(sum + sum_at(row_of(k), col)) = make_float4(v[0], v[1], v[2], v[3]);
+            *reinterpret_cast<float4*>(sum + sum_at(row_of(k), col + 4)) = make_float4(v[4], v[5], v[6], v[7]);
         }
-        if (a.tall) {
-            __syncthreads();
-            for (int i = threadIdx.x; i < BLOCK * BLOCK; i += GEMM_THREADS) {
-                const int s = i & (BLOCK - 1), l = i / BLOCK;
-                if (s0 + s < a.S && l0 + l < a.L) finish((l0 + l) * a.cols + s0 + s, sum[sum_at(s, l)]);
+        __syncthreads();
+        // lanes along what is contiguous
+        constexpr int AT_ONCE = 16;
+        void* out = a.out[m];
+        const int dr = a.tall ? 0 : GEMM_THREADS / BLOCK, dc = a.tall ? GEMM_THREADS / BLOCK : 0, along = threadIdx.x & (BLOCK - 1), across = threadIdx.x / BLOCK;
+        const long long s0 = (long long)bi * BLOCK, l0 = (long long)bj * BLOCK;
+        for (int i = 0; i < BLOCK * BLOCK / GEMM_THREADS; i += AT_ONCE) {
+            float w[AT_ONCE];
+#pragma unroll
+            for (int k = 0; k < AT_ONCE; ++k) {
+                const int r = a.tall ? along : across + (i + k) * dr, c = a.tall ? across + (i + k) * dc : along;
+                w[k] = a.update && r < rows && c < cols ? load_as(out, a.dtype, a.tall ? (l0 + c) * a.cols + s0 + r : (s0 + r) * a.cols + l0 + c) : 0.f;
+            }
+#pragma unroll
+            for (int k = 0; k < AT_ONCE; ++k) {
+                const int r = a.tall ? along : across + (i + k) * dr, c = a.tall ? across + (i + k) * dc : along;
+                if (r >= rows || c >= cols) continue;
+                float v = sum[sum_at(r, c)] * (1.f / SCALE);
+                if (a.update) v = fmaf(a.keep, w[k], -a.move * v);
+                store_as(out, a.dtype, a.tall ? (l0 + c) * a.cols + s0 + r : (s0 + r) * a.cols + l0 + c, v);
             }
         }
     }

@@ -4,6 +4,7 @@
 #include "launch_state.cuh"
 #include "ortho_gemm.cuh"
 #include "ortho_prepare.cuh"
+#include "ortho_resident.cuh"
 
 #include <algorithm>
 #include <cmath>
@@ -15,23 +16,56 @@ namespace ortho {
 
 #define ORTHO_LAUNCH(...) do { cudaError_t e_ = prof_mark(GLEAM_K_ORTHO, s); if (e_ == cudaSuccess) e_ = (__VA_ARGS__); if (e_ != cudaSuccess) return e_; } while (0)
 
+constexpr int SMS = 148;
+
+template <int KIND, int RANKS>
+static cudaError_t gemm_of(const Args& a, int count, cudaStream_t s) {
+    static PerDevice done;
+    const cudaError_t e = ensure_smem(gemm_kernel<KIND, RANKS>, GEMM_SMEM, done);
+    if (e != cudaSuccess) return e;
+    const dim3 grid((unsigned)RANKS, (unsigned)tiles_of<KIND>(a), (unsigned)count), block(GEMM_THREADS);
+    ORTHO_LAUNCH(launch_overlapped_cluster((unsigned)RANKS, gemm_kernel<KIND, RANKS>, grid, block, GEMM_SMEM, s, a));
+    return cudaSuccess;
+}
 template <int KIND>
 static cudaError_t gemm(const Args& a, int count, cudaStream_t s) {
-    static PerDevice done;
-    cudaError_t e = ensure_smem(gemm_kernel<KIND>, GEMM_SMEM, done);
-    if (e != cudaSuccess) return e;
-    const int tiles = tiles_of<KIND>(a), steps = steps_of<KIND>(a);
-    // blocks that share a sum over K: while there are SMs left and each has two steps at least
-    int ranks = 1;
-    if (KIND == GRAM || KIND == POLY)
-        while (ranks < 8 && tiles * count * ranks * 2 <= 148 && steps >= ranks * 4) ranks *= 2;
-    const dim3 grid((unsigned)ranks, (unsigned)tiles, (unsigned)count), block(GEMM_THREADS);
-    ORTHO_LAUNCH(launch_overlapped_cluster((unsigned)ranks, gemm_kernel<KIND>, grid, block, GEMM_SMEM, s, a));
-    return cudaSuccess;
+    if constexpr (KIND == GRAM || KIND == POLY) {
+        // blocks that share a sum over K: while there are SMs left and each has two steps at least
+        const long long blocks = (long long)tiles_of<KIND>(a) * count, steps = steps_of<KIND>(a);
+        if (blocks * 8 <= SMS && steps >= 16) return gemm_of<KIND, 8>(a, count, s);
+        if (blocks * 4 <= SMS && steps >= 8) return gemm_of<KIND, 4>(a, count, s);
+        if (blocks * 2 <= SMS && steps >= 4) return gemm_of<KIND, 2>(a, count, s);
+    }
+    return gemm_of<KIND, 1>(a, count, s);
+}
+
+// Tiles of a block of the resident kernel, 0 where a matrix does not fit a cluster.  More tiles mean fewer blocks: a turn takes about
+// two units and one more for each tile of a block, once for each round of clusters.
+static int resident_tiles(long long S, long long L, int count) {
+    if (S > BLOCK) return 0;
+    const long long all = (L + BLOCK - 1) / BLOCK;
+    int best = 0;
+    long long least = 0;
+    for (int tiles = 1; tiles <= all && resident_bytes(resident_rows(S), tiles) <= RESIDENT_MOST; ++tiles) {
+        const long long ranks = (all + tiles - 1) / tiles, rounds = (count * ranks + SMS - RESIDENT_RANKS - 1) / (SMS - RESIDENT_RANKS);
+        if (ranks > RESIDENT_RANKS) continue;
+        const long long time = rounds * (2 + tiles);
+        if (best == 0 || time < least) { best = tiles; least = time; }
+    }
+    return best;
 }
 
 template <bool UPDATE>
 static cudaError_t run(Args& a, int count, int turns, cudaStream_t s) {
+    if (const int tiles = resident_tiles(a.S, a.L, count)) {
+        static PerDevice done;
+        const cudaError_t e = ensure_smem(resident_kernel<UPDATE>, RESIDENT_MOST, done);
+        if (e != cudaSuccess) return e;
+        const unsigned ranks = (unsigned)((a.lblocks + tiles - 1) / tiles);
+        ORTHO_LAUNCH(launch_overlapped_cluster(ranks, resident_kernel<UPDATE>, dim3(ranks, (unsigned)count), dim3(RESIDENT_THREADS),
+                                               (size_t)resident_bytes(resident_rows(a.S), tiles), s, a, tiles, turns));
+        return cudaSuccess;
+    }
     ORTHO_LAUNCH(launch_overlapped(true, sums_kernel<UPDATE>, dim3((unsigned)a.parts, (unsigned)count), dim3(PREPARE_THREADS), 0, s, a));
     const size_t tile = a.tall ? sizeof(float) * BLOCK * (BLOCK + 1) : 0;
     static PerDevice done;
@@ -62,10 +96,13 @@ static int layout_of(const gleam_matrix_dims* d, Layout* l) {
     // tiles of a launch are numbered by the y axis of its grid
     if ((long long)l->sblocks * l->lblocks > 65535) return GLEAM_ERR_BAD_DIMS;
     l->group = (int)std::min<long long>(d->count, GROUP);
+    l->x = l->square = l->part = 0;
+    l->total = d->count && S ? 256 : 0;
+    if (l->total == 0 || resident_tiles(S, L, 1)) return GLEAM_OK;
     l->x = (uint64_t)l->group * l->sblocks * l->lblocks * BLOCK_BYTES;
     l->square = (uint64_t)l->group * l->sblocks * l->sblocks * BLOCK_BYTES;
     l->part = (uint64_t)GROUP * PARTS * sizeof(float);
-    l->total = l->x && d->count ? 2 * l->x + 2 * l->square + l->part + 256 : 0;
+    l->total += 2 * l->x + 2 * l->square + l->part;
     return GLEAM_OK;
 }
 
@@ -114,7 +151,7 @@ static int orthogonal(const void* const* u, float* const* momenta, void* const* 
     a.rows = d->rows; a.cols = d->cols; a.S = std::min(d->rows, d->cols); a.L = std::max(d->rows, d->cols);
     a.tall = d->rows > d->cols; a.dtype = d->dtype;
     a.sblocks = l.sblocks; a.lblocks = l.lblocks;
-    a.parts = (int)std::max<long long>(1, std::min<long long>(PARTS, (long long)(n / (8 * PREPARE_THREADS))));
+    a.parts = (int)std::max<long long>(1, std::min<long long>(PARTS, (long long)(n / (4 * PREPARE_THREADS))));
     a.a = d->a; a.b = d->b; a.c = d->c; a.eps = d->eps;
     if (m) {
         a.update = 1; a.nesterov = m->nesterov; a.mu = m->momentum;
@@ -123,7 +160,7 @@ static int orthogonal(const void* const* u, float* const* momenta, void* const* 
     unsigned char* ws = (unsigned char*)d->workspace;
     a.g = ws + 2 * l.x; a.p = a.g + l.square;
     a.part = (float*)(a.p + l.square);
-    a.status = (int*)((unsigned char*)a.part + l.part);
+    a.status = (int*)(ws + l.total - 256);
     for (int64_t i0 = 0; i0 < d->count; i0 += GROUP) {
         const int count = (int)std::min<int64_t>(GROUP, d->count - i0);
         a.x = ws; a.y = ws + l.x;

@@ -22,12 +22,26 @@ __global__ void __launch_bounds__(PREPARE_THREADS) sums_kernel(const __grid_cons
     grid_dependency_wait();
     const int m = blockIdx.y;
     if (blockIdx.x == 0 && m == 0 && threadIdx.x == 0) *a.status = 0;
+    constexpr int AT_ONCE = 8;
     const long long n = a.rows * a.cols, step = (long long)gridDim.x * PREPARE_THREADS;
     float sum = 0.f;
-    for (long long i = (long long)blockIdx.x * PREPARE_THREADS + threadIdx.x; i < n; i += step) {
-        if (UPDATE) a.momentum[m][i] = fmaf(a.mu, a.momentum[m][i], load_as(a.u[m], a.dtype, i));
-        const float v = source<UPDATE>(a, m, i);
-        sum = fmaf(v, v, sum);
+    for (long long i0 = (long long)blockIdx.x * PREPARE_THREADS + threadIdx.x; i0 < n; i0 += AT_ONCE * step) {
+        float v[AT_ONCE], w[AT_ONCE];
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) {
+            const long long i = i0 + k * step;
+            v[k] = i < n ? load_as(a.u[m], a.dtype, i) : 0.f;
+            if (UPDATE) w[k] = i < n ? a.momentum[m][i] : 0.f;
+        }
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) {
+            if (UPDATE) {
+                w[k] = fmaf(a.mu, w[k], v[k]);
+                if (i0 + k * step < n) a.momentum[m][i0 + k * step] = w[k];
+                v[k] = a.nesterov ? fmaf(a.mu, w[k], v[k]) : w[k];
+            }
+            sum = fmaf(v[k], v[k], sum);
+        }
     }
     __shared__ float buf[2 * (PREPARE_THREADS / 32)];
     const prior::Pair t = prior::block_sum<PREPARE_THREADS / 32>(prior::Pair{sum, 0.f}, buf);
@@ -40,18 +54,22 @@ __global__ void __launch_bounds__(PREPARE_THREADS) first_kernel(const __grid_con
     grid_dependency_wait();
     extern __shared__ float tile[];                  // tall: 128 columns of the block with one number between them
     const int m = blockIdx.y, sb = blockIdx.x / a.lblocks, lb = blockIdx.x % a.lblocks;
-    double total = 0.0;
-    for (int k = 0; k < a.parts; ++k) total += (double)a.part[m * PARTS + k];
-    const float by = SCALE / (sqrtf((float)total) + a.eps);
+    float total = 0.f;
+    for (int k = threadIdx.x; k < a.parts; k += PREPARE_THREADS) total += a.part[m * PARTS + k];
+    __shared__ float buf[2 * (PREPARE_THREADS / 32)];
+    total = prior::block_sum<PREPARE_THREADS / 32>(prior::Pair{total, 0.f}, buf).a;
+    const float by = SCALE / (sqrtf(total) + a.eps);
     unsigned char* block = a.x + ((long long)(m * a.sblocks + sb) * a.lblocks + lb) * BLOCK_BYTES;
     const long long s0 = (long long)sb * BLOCK, l0 = (long long)lb * BLOCK;
     if (a.tall) {
+#pragma unroll 8
         for (int i = threadIdx.x; i < BLOCK * BLOCK; i += PREPARE_THREADS) {
             const int l = i / BLOCK, s = i % BLOCK;
             tile[l * (BLOCK + 1) + s] = s0 + s < a.S && l0 + l < a.L ? source<UPDATE>(a, m, (l0 + l) * a.cols + s0 + s) : 0.f;
         }
         __syncthreads();
     }
+#pragma unroll 2
     for (int i = threadIdx.x; i < BLOCK * BLOCK / 8; i += PREPARE_THREADS) {
         // eight lanes a core: rows of 16 bytes that lie side by side
         const int r = (i & 7) + (i >> 7) * 8, c = ((i >> 3) & 15) * 8;

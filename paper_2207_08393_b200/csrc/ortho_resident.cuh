@@ -1,0 +1,326 @@
+// The whole update of a matrix whose shorter side is at most 128 in one launch: a cluster of up to eight blocks keeps X in shared memory
+// through all turns.
+//
+// A block holds up to seven tiles of 128 columns of X (all R rows of them, R = S rounded up to 16) as pieces.  In a turn it
+//   - sums X X^T over its tiles on the tensor cores; the blocks add their sums through distributed shared memory, each a share of the
+//     rows, and write the pieces of A to all;
+//   - computes P = b A + c A A, which costs less than sharing it;
+//   - replaces its tiles by a X + P X.
+// Two barriers of the cluster a turn, nothing but the matrix itself through global memory, once each way.  Products of K <= 128 are
+// done within a microsecond: what the time goes to is moving sums from tensor memory and back to shared memory as pieces, by all
+// 16 warps, and barriers.
+#pragma once
+#include "ortho_gemm.cuh"
+
+namespace gleam {
+namespace ortho {
+
+constexpr int RESIDENT_THREADS = 512, RESIDENT_RANKS = 8, RESIDENT_HEAD = 1024;
+constexpr int RESIDENT_LEAST = 120 * 1024;       // shared memory that keeps a second block, which would wait for tensor memory, off the SM
+constexpr int RESIDENT_MOST = 227 * 1024;
+
+// Shared memory: head, sums in 32 bits, A (then P), tiles; a product reads 128 rows of an operand whatever R is, hence the end.
+__host__ __device__ inline int resident_rows(long long S) { return (int)((S + 15) / 16 * 16); }
+__host__ inline int resident_bytes(int R, int tiles) {
+    const int n = RESIDENT_HEAD + (2 + tiles) * R * 512 + (BLOCK - R) * 128;
+    return n < RESIDENT_LEAST ? RESIDENT_LEAST : n;
+}
+
+template <bool UPDATE>
+__global__ void __launch_bounds__(RESIDENT_THREADS, 1) resident_kernel(const __grid_constant__ Args a, int tiles, int turns) {
+    extern __shared__ __align__(1024) unsigned char smem[];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, ranks = gridDim.x, rank = ranks > 1 ? (int)tc::cluster_rank() : 0, m = blockIdx.y;
+    const int R = resident_rows(a.S), square = R * 512;                    // bytes of R rows of 128 as pieces, or in 32 bits
+    const uint32_t base = tc::shared_address(smem), done = base + 16;
+    unsigned char* A_ = smem + RESIDENT_HEAD + square;
+    unsigned char* X = A_ + square;
+    float* sum = reinterpret_cast<float*>(smem + RESIDENT_HEAD);
+    float* part = reinterpret_cast<float*>(smem + 64);                     // a rank's sum of squares; the block's sums behind it
+    const uint32_t a_at = base + RESIDENT_HEAD + square, x_at = a_at + square;
+    if (warp == 0) tc::take_columns(base, 512);
+    if (threadIdx.x == 0) {
+        tc::barrier_init(done, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    tc::fence_before();
+    __syncthreads();
+    tc::fence_after();
+    const uint32_t cols0 = *reinterpret_cast<volatile uint32_t*>(smem);    // tensor memory: hi hi and the rest, twice
+    grid_dependency_wait();
+
+    const long long first = (long long)rank * tiles;                       // this block's tiles
+    const int mine = (int)((a.L + BLOCK - 1) / BLOCK - first < tiles ? (a.L + BLOCK - 1) / BLOCK - first : tiles);
+    bool failed = false;
+    uint32_t phase = 0;
+    if (threadIdx.x == 0 && m == 0 && rank == 0) *a.status = 0;
+
+    // byte of element (r, c) of a piece of R rows
+    auto at = [&](int r, int c) { return (c >> 6) * (R * 128) + (r >> 3) * 1024 + ((c >> 3) & 7) * CORE + (r & 7) * 16; };
+    const int lo = R * 256;                                                // from hi to lo
+    auto wait = [&]() {
+        if (!failed && !tc::barrier_wait(done, phase)) failed = true;
+        phase ^= 1;
+        tc::fence_after();
+    };
+    // shared memory written by threads is there for the products; tensor memory that was read may be written
+    auto settle = [&]() {
+        tc::fence_shared();
+        tc::fence_before();
+        __syncthreads();
+        tc::fence_after();
+    };
+
+    // the source in 32 bits where its tile will stand, and the sum of squares
+    float squares = 0.f;
+    constexpr int AT_ONCE = 8;
+    for (int t = 0; t < mine; ++t) {
+        float* to = reinterpret_cast<float*>(X + t * square);
+        const long long l0 = (first + t) * BLOCK;
+        for (int i0 = threadIdx.x; i0 < R * BLOCK; i0 += AT_ONCE * RESIDENT_THREADS) {
+            float v[AT_ONCE], w[AT_ONCE];
+            long long from[AT_ONCE];
+#pragma unroll
+            for (int k = 0; k < AT_ONCE; ++k) {
+                const int i = i0 + k * RESIDENT_THREADS, r = a.tall ? i % R : i / BLOCK, c = a.tall ? i / R : i % BLOCK;
+                from[k] = i < R * BLOCK && r < a.S && l0 + c < a.L ? (a.tall ? (l0 + c) * a.cols + r : r * a.cols + l0 + c) : -1;
+                v[k] = from[k] >= 0 ? load_as(a.u[m], a.dtype, from[k]) : 0.f;
+                if (UPDATE) w[k] = from[k] >= 0 ? a.momentum[m][from[k]] : 0.f;
+            }
+#pragma unroll
+            for (int k = 0; k < AT_ONCE; ++k) {
+                const int i = i0 + k * RESIDENT_THREADS, r = a.tall ? i % R : i / BLOCK, c = a.tall ? i / R : i % BLOCK;
+                if (UPDATE) {
+                    w[k] = fmaf(a.mu, w[k], v[k]);
+                    if (from[k] >= 0) a.momentum[m][from[k]] = w[k];
+                    v[k] = a.nesterov ? fmaf(a.mu, w[k], v[k]) : w[k];
+                }
+                squares = fmaf(v[k], v[k], squares);
+                if (i < R * BLOCK) to[sum_at(r, c)] = v[k];
+            }
+        }
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) squares += __shfl_xor_sync(0xffffffffu, squares, o);
+    if (lane == 0) part[4 + warp] = squares;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        float s = 0.f;
+        for (int k = 0; k < RESIDENT_THREADS / 32; ++k) s += part[4 + k];
+        part[0] = s;
+    }
+    if (ranks > 1) tc::cluster_sync(); else __syncthreads();
+    float total = 0.f;
+    for (int k = 0; k < ranks; ++k) total += ranks > 1 ? tc::read_remote(base + 64, k).x : part[0];
+    const float by = SCALE / (sqrtf(total) + a.eps);
+
+    // ... and as pieces
+    const int eights = R * BLOCK / 8;
+    for (int t = 0; t < mine; ++t) {
+        constexpr int MOST = BLOCK * BLOCK / 8 / RESIDENT_THREADS;
+        float v[MOST][8];
+        unsigned char* tile = X + t * square;
+        const float* from = reinterpret_cast<const float*>(tile);
+#pragma unroll
+        for (int k = 0; k < MOST; ++k) {
+            const int i = threadIdx.x + k * RESIDENT_THREADS, r = (i & 7) + (i >> 7) * 8, c = ((i >> 3) & 15) * 8;
+            if (i < eights) {
+                const float4 f = *reinterpret_cast<const float4*>(from + sum_at(r, c)), g = *reinterpret_cast<const float4*>(from + sum_at(r, c + 4));
+                v[k][0] = f.x * by; v[k][1] = f.y * by; v[k][2] = f.z * by; v[k][3] = f.w * by;
+                v[k][4] = g.x * by; v[k][5] = g.y * by; v[k][6] = g.z * by; v[k][7] = g.w * by;
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < MOST; ++k) {
+            const int i = threadIdx.x + k * RESIDENT_THREADS, r = (i & 7) + (i >> 7) * 8, c = ((i >> 3) & 15) * 8;
+            if (i < eights) {
+                uint4 h, l;
+                split8(v[k], h, l);
+                *reinterpret_cast<uint4*>(tile + at(r, c)) = h;
+                *reinterpret_cast<uint4*>(tile + lo + at(r, c)) = l;
+            }
+        }
+    }
+
+    // a warp's part of a result: 32 rows, 32 columns
+    const int row = (warp & 3) * 32 + lane, col0 = (warp >> 2) * 32;
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+    auto read_sums = [&](uint32_t columns, float (&v)[32]) {
+        float u[32];
+        tc::read_columns(cols0 + lanes + columns + col0, v);
+        tc::read_columns(cols0 + lanes + columns + BLOCK + col0, u);
+#pragma unroll
+        for (int j = 0; j < 32; ++j) v[j] = (v[j] + u[j]) * (1.f / SCALE);
+    };
+    // eight of them joined with what stands at (row, c) of these pieces: v <- by old + times v
+    auto blend = [&](const unsigned char* from, int c, float by_, float times, const float* v, float (&w)[8]) {
+        join8(*reinterpret_cast<const uint4*>(from + at(row, c)), *reinterpret_cast<const uint4*>(from + lo + at(row, c)), w);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = fmaf(by_, w[j], times * v[j]);
+    };
+    auto put = [&](unsigned char* to, int c, const float (&w)[8]) {
+        uint4 h, l;
+        split8(w, h, l);
+        *reinterpret_cast<uint4*>(to + at(row, c)) = h;
+        *reinterpret_cast<uint4*>(to + lo + at(row, c)) = l;
+    };
+
+    for (int turn = 0; turn < turns; ++turn) {
+        settle();
+        if (threadIdx.x == 0) {
+            const uint32_t what = tc::instruction(R, false);
+            for (int t = 0; t < mine; ++t)
+                for (int k = 0; k < BLOCK / 16; ++k) {
+                    const uint32_t p = x_at + t * square + (k >> 2) * (R * 128) + (k & 3) * 256;
+                    const uint64_t h = tc::descriptor(p, 128, 1024), l = tc::descriptor(p + lo, 128, 1024);
+                    tc::product(cols0 + BLOCK, l, h, what, t > 0 || k > 0);
+                    tc::product(cols0 + BLOCK, h, l, what, true);
+                    tc::product(cols0, h, h, what, t > 0 || k > 0);
+                }
+            tc::commit(done);
+        }
+        wait();
+        if (col0 < R) {
+            float v[32];
+            read_sums(0, v);
+            if (row < R) {
+#pragma unroll
+                for (int j = 0; j < 32; j += 4)
+                    if (col0 + j < R) *reinterpret_cast<float4*>(sum + sum_at(row, col0 + j)) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+            }
+        }
+        // A = the sum over the cluster, in pieces, a share of it from each block to all blocks
+        if (ranks > 1) tc::cluster_sync(); else __syncthreads();
+        const int across = R / 8, all = R * across, share = (all + ranks - 1) / ranks, end = (rank + 1) * share < all ? (rank + 1) * share : all;
+        for (int i = rank * share + threadIdx.x; i < end; i += RESIDENT_THREADS) {
+            const int r = (i & 7) + (i >> 3) / across * 8, c = (i >> 3) % across * 8;
+            float4 f[RESIDENT_RANKS], g[RESIDENT_RANKS];
+            const uint32_t p = base + RESIDENT_HEAD + 4 * sum_at(r, c), q = base + RESIDENT_HEAD + 4 * sum_at(r, c + 4);
+#pragma unroll
+            for (int k = 0; k < RESIDENT_RANKS; ++k)
+                if (k < ranks) {
+                    f[k] = ranks > 1 ? tc::read_remote(p, k) : *reinterpret_cast<const float4*>(smem + (p - base));
+                    g[k] = ranks > 1 ? tc::read_remote(q, k) : *reinterpret_cast<const float4*>(smem + (q - base));
+                }
+#pragma unroll
+            for (int k = 1; k < RESIDENT_RANKS; ++k)
+                if (k < ranks) {
+                    f[0].x += f[k].x; f[0].y += f[k].y; f[0].z += f[k].z; f[0].w += f[k].w;
+                    g[0].x += g[k].x; g[0].y += g[k].y; g[0].z += g[k].z; g[0].w += g[k].w;
+                }
+            const float v[8] = {f[0].x, f[0].y, f[0].z, f[0].w, g[0].x, g[0].y, g[0].z, g[0].w};
+            uint4 h, l;
+            split8(v, h, l);
+            for (int k = 0; k < ranks; ++k) {
+                if (ranks > 1) {
+                    tc::write_remote(a_at + at(r, c), k, h);
+                    tc::write_remote(a_at + lo + at(r, c), k, l);
+                } else {
+                    *reinterpret_cast<uint4*>(A_ + at(r, c)) = h;
+                    *reinterpret_cast<uint4*>(A_ + lo + at(r, c)) = l;
+                }
+            }
+        }
+        if (ranks > 1) tc::cluster_sync();
+        settle();
+        if (threadIdx.x == 0) {
+            const uint32_t what = tc::instruction(R, false);
+            for (int k = 0; k < R / 16; ++k) {
+                const uint32_t p = a_at + (k >> 2) * (R * 128) + (k & 3) * 256;
+                const uint64_t h = tc::descriptor(p, 128, 1024), l = tc::descriptor(p + lo, 128, 1024);
+                tc::product(cols0 + 3 * BLOCK, l, h, what, k > 0);
+                tc::product(cols0 + 3 * BLOCK, h, l, what, true);
+                tc::product(cols0 + 2 * BLOCK, h, h, what, k > 0);
+            }
+            tc::commit(done);
+        }
+        wait();
+        if (col0 < R) {
+            float v[32];
+            read_sums(2 * BLOCK, v);
+            if (row < R) {
+#pragma unroll
+                for (int j = 0; j < 32; j += 8)
+                    if (col0 + j < R) {
+                        float w[8];
+                        blend(A_, col0 + j, a.b, a.c, v + j, w);
+                        put(A_, col0 + j, w);
+                    }
+            }
+        }
+        // two tiles at a time, as tensor memory allows
+        for (int t0 = 0; t0 < mine; t0 += 2) {
+            settle();
+            if (threadIdx.x == 0) {
+                const uint32_t what = tc::instruction(BLOCK / 2, true);
+                for (int t = t0; t < mine && t < t0 + 2; ++t)
+                    for (int k = 0; k < R / 16; ++k) {
+                        const uint32_t p = a_at + (k >> 2) * (R * 128) + (k & 3) * 256, q = x_at + t * square + k * 2048, to = cols0 + (t - t0) * 2 * BLOCK;
+                        const uint64_t ph = tc::descriptor(p, 128, 1024), pl = tc::descriptor(p + lo, 128, 1024);
+                        for (int h = 0; h < 2; ++h) {
+                            const uint64_t xh = tc::descriptor(q + h * (R * 128), 1024, 128), xl = tc::descriptor(q + lo + h * (R * 128), 1024, 128);
+                            tc::product(to + BLOCK + h * 64, pl, xh, what, k > 0);
+                            tc::product(to + BLOCK + h * 64, ph, xl, what, true);
+                            tc::product(to + h * 64, ph, xh, what, k > 0);
+                        }
+                    }
+                tc::commit(done);
+            }
+            wait();
+            for (int t = t0; t < mine && t < t0 + 2; ++t) {
+                float v[32];
+                read_sums((t - t0) * 2 * BLOCK, v);
+                if (turn + 1 < turns) {
+                    if (row < R) {
+#pragma unroll
+                        for (int j = 0; j < 32; j += 8) {
+                            float w[8];
+                            blend(X + t * square, col0 + j, a.a, 1.f, v + j, w);
+                            put(X + t * square, col0 + j, w);
+                        }
+                    }
+                    continue;
+                }
+                // the result, through shared memory so that lanes lie along what is contiguous
+                __syncthreads();
+                if (row < R) {
+#pragma unroll
+                    for (int j = 0; j < 32; j += 8) {
+                        float w[8];
+                        blend(X + t * square, col0 + j, a.a, 1.f, v + j, w);
+                        *reinterpret_cast<float4*>(sum + sum_at(row, col0 + j)) = make_float4(w[0], w[1], w[2], w[3]);
+                        *reinterpret_cast<float4*>(sum + sum_at(row, col0 + j + 4)) = make_float4(w[4], w[5], w[6], w[7]);
+                    }
+                }
+                __syncthreads();
+                const long long l0 = (first + t) * BLOCK;
+                for (int i0 = threadIdx.x; i0 < R * BLOCK; i0 += AT_ONCE * RESIDENT_THREADS) {
+                    float w[AT_ONCE];
+                    long long to[AT_ONCE];
+#pragma unroll
+                    for (int k = 0; k < AT_ONCE; ++k) {
+                        const int i = i0 + k * RESIDENT_THREADS, r = a.tall ? i % R : i / BLOCK, c = a.tall ? i / R : i % BLOCK;
+                        to[k] = i < R * BLOCK && r < a.S && l0 + c < a.L ? (a.tall ? (l0 + c) * a.cols + r : r * a.cols + l0 + c) : -1;
+                        w[k] = UPDATE && to[k] >= 0 ? load_as(a.out[m], a.dtype, to[k]) : 0.f;
+                    }
+#pragma unroll
+                    for (int k = 0; k < AT_ONCE; ++k) {
+                        const int i = i0 + k * RESIDENT_THREADS, r = a.tall ? i % R : i / BLOCK, c = a.tall ? i / R : i % BLOCK;
+                        if (to[k] < 0) continue;
+                        float x = sum[sum_at(r, c)] * (1.f / SCALE);
+                        if (UPDATE) x = fmaf(a.keep, w[k], -a.move * x);
+                        store_as(a.out[m], a.dtype, to[k], x);
+                    }
+                }
+            }
+        }
+    }
+    tc::fence_before();
+    __syncthreads();
+    if (warp == 0) tc::free_columns(cols0, 512);
+    if (failed) atomicOr(a.status, 1);
+    if (ranks > 1) tc::cluster_sync();             // nobody leaves while others may read or write its shared memory
+}
+
+}  // namespace ortho
+}  // namespace gleam

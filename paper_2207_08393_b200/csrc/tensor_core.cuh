@@ -95,5 +95,10 @@ __device__ __forceinline__ float4 read_remote(uint32_t address, uint32_t rank) {
     return v;
 }
 
+__device__ __forceinline__ void write_remote(uint32_t address, uint32_t rank, const uint4& v) {
+    asm volatile("{\n .reg .b32 a;\n mapa.shared::cluster.u32 a, %0, %1;\n st.shared::cluster.v4.b32 [a], {%2, %3, %4, %5};\n}\n"
+                 ::"r"(address), "r"(rank), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+
 }  // namespace tc
 }  // namespace gleam

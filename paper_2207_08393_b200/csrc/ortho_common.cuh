@@ -53,15 +53,8 @@ struct Args {
 // Byte of element (r, c) of a piece.
 __host__ __device__ __forceinline__ int core_at(int r, int c) { return ((c >> 6) * 128 + (r >> 3) * 8 + ((c >> 3) & 7)) * CORE + (r & 7) * 16 + (c & 7) * 2; }
 
-__device__ __forceinline__ float load_as(const void* p, int dtype, long long i) {
-    return dtype == 0 ? static_cast<const float*>(p)[i] : dtype == 1 ? __half2float(static_cast<const __half*>(p)[i])
-                                                                     : __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]);
-}
-__device__ __forceinline__ void store_as(void* p, int dtype, long long i, float v) {
-    if (dtype == 0) static_cast<float*>(p)[i] = v;
-    else if (dtype == 1) static_cast<__half*>(p)[i] = __float2half_rn(v);
-    else static_cast<__nv_bfloat16*>(p)[i] = __float2bfloat16_rn(v);
-}
+template <class T> __device__ __forceinline__ float load_at(const void* p, long long i) { return to_float(static_cast<const T*>(p)[i]); }
+template <class T> __device__ __forceinline__ void store_at(void* p, long long i, float v) { static_cast<T*>(p)[i] = from_float<T>(v); }
 
 // Eight neighbours of a row as two pieces, and back.
 __device__ __forceinline__ void split8(const float (&v)[8], uint4& hi, uint4& lo) {

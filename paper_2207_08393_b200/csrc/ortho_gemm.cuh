@@ -29,7 +29,8 @@ template <int KIND> __host__ inline int tiles_of(const Args& a) { return KIND ==
 // The sums as 32-bit numbers in shared memory: rows of 128, their 16-byte pieces in an order that keeps 32 rows apart.
 __device__ __forceinline__ int sum_at(int r, int c) { return r * BLOCK + ((((c >> 2) ^ r) & 31) << 2) + (c & 3); }
 
-template <int KIND, int RANKS>
+// T: the type of results (LAST)
+template <int KIND, int RANKS, class T>
 __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_constant__ Args a) {
     extern __shared__ __align__(1024) unsigned char smem[];
     constexpr int ranks = RANKS, ITEMS = BLOCK * BLOCK / 8 / RANKS / GEMM_THREADS;     // eights of a row that a thread finishes
@@ -246,7 +247,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
 #pragma unroll
             for (int k = 0; k < AT_ONCE; ++k) {
                 const int r = a.tall ? along : across + (i + k) * dr, c = a.tall ? across + (i + k) * dc : along;
-                w[k] = a.update && r < rows && c < cols ? load_as(out, a.dtype, a.tall ? (l0 + c) * a.cols + s0 + r : (s0 + r) * a.cols + l0 + c) : 0.f;
+                w[k] = a.update && r < rows && c < cols ? load_at<T>(out, a.tall ? (l0 + c) * a.cols + s0 + r : (s0 + r) * a.cols + l0 + c) : 0.f;
             }
 #pragma unroll
             for (int k = 0; k < AT_ONCE; ++k) {
@@ -254,7 +255,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
                 if (r >= rows || c >= cols) continue;
                 float v = sum[sum_at(r, c)] * (1.f / SCALE);
                 if (a.update) v = fmaf(a.keep, w[k], -a.move * v);
-                store_as(out, a.dtype, a.tall ? (l0 + c) * a.cols + s0 + r : (s0 + r) * a.cols + l0 + c, v);
+                store_at<T>(out, a.tall ? (l0 + c) * a.cols + s0 + r : (s0 + r) * a.cols + l0 + c, v);
             }
         }
     }

@@ -18,66 +18,94 @@ namespace ortho {
 
 constexpr int SMS = 148;
 
-template <int KIND, int RANKS>
+template <int KIND, int RANKS, class T>
 static cudaError_t gemm_of(const Args& a, int count, cudaStream_t s) {
     static PerDevice done;
-    const cudaError_t e = ensure_smem(gemm_kernel<KIND, RANKS>, GEMM_SMEM, done);
+    const cudaError_t e = ensure_smem(gemm_kernel<KIND, RANKS, T>, GEMM_SMEM, done);
     if (e != cudaSuccess) return e;
     const dim3 grid((unsigned)RANKS, (unsigned)tiles_of<KIND>(a), (unsigned)count), block(GEMM_THREADS);
-    ORTHO_LAUNCH(launch_overlapped_cluster((unsigned)RANKS, gemm_kernel<KIND, RANKS>, grid, block, GEMM_SMEM, s, a));
+    ORTHO_LAUNCH(launch_overlapped_cluster((unsigned)RANKS, gemm_kernel<KIND, RANKS, T>, grid, block, GEMM_SMEM, s, a));
     return cudaSuccess;
 }
-template <int KIND>
+template <int KIND, class T = float>
 static cudaError_t gemm(const Args& a, int count, cudaStream_t s) {
     if constexpr (KIND == GRAM || KIND == POLY) {
         // blocks that share a sum over K: while there are SMs left and each has two steps at least
         const long long blocks = (long long)tiles_of<KIND>(a) * count, steps = steps_of<KIND>(a);
-        if (blocks * 8 <= SMS && steps >= 16) return gemm_of<KIND, 8>(a, count, s);
-        if (blocks * 4 <= SMS && steps >= 8) return gemm_of<KIND, 4>(a, count, s);
-        if (blocks * 2 <= SMS && steps >= 4) return gemm_of<KIND, 2>(a, count, s);
+        if (blocks * 8 <= SMS && steps >= 16) return gemm_of<KIND, 8, T>(a, count, s);
+        if (blocks * 4 <= SMS && steps >= 8) return gemm_of<KIND, 4, T>(a, count, s);
+        if (blocks * 2 <= SMS && steps >= 4) return gemm_of<KIND, 2, T>(a, count, s);
     }
-    return gemm_of<KIND, 1>(a, count, s);
+    return gemm_of<KIND, 1, T>(a, count, s);
+}
+
+// Clusters of so many blocks, one block an SM, that the current device runs at once: its SMs come in groups that clusters do not
+// cross, so 16 clusters of 7 are more than 148 SMs may hold.
+static int clusters_at_once(int ranks) {
+    static PerDevice cache[RESIDENT_RANKS + 1];
+    std::atomic<int>* slot = cache[ranks].slot();
+    if (slot) { const int v = slot->load(std::memory_order_acquire); if (v > 0) return v; }
+    static PerDevice done;
+    constexpr auto KERNEL = resident_kernel<float, false>;
+    int n = 0;
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute at[2];
+    launch_config(cfg, at, false, dim3((unsigned)ranks), dim3(RESIDENT_THREADS), RESIDENT_MOST, nullptr, 2);
+    at[0].val.clusterDim.x = (unsigned)ranks;
+    if (ensure_smem(KERNEL, RESIDENT_MOST, done) != cudaSuccess || cudaOccupancyMaxActiveClusters(&n, KERNEL, &cfg) != cudaSuccess || n < 1) {
+        cudaGetLastError();
+        return SMS / ranks;
+    }
+    if (slot) slot->store(n, std::memory_order_release);
+    return n;
 }
 
 // Tiles of a block of the resident kernel, 0 where a matrix does not fit a cluster.  More tiles mean fewer blocks: a turn takes about
-// two units and one more for each tile of a block, once for each round of clusters.
-static int resident_tiles(long long S, long long L, int count) {
+// four units and one more for each tile of a block, once for each round of clusters (`counted`; else any number that fits).
+static int resident_tiles(long long S, long long L, int count, bool counted) {
     if (S > BLOCK) return 0;
     const long long all = (L + BLOCK - 1) / BLOCK;
     int best = 0;
     long long least = 0;
     for (int tiles = 1; tiles <= all && resident_bytes(resident_rows(S), tiles) <= RESIDENT_MOST; ++tiles) {
-        const long long ranks = (all + tiles - 1) / tiles, rounds = (count * ranks + SMS - RESIDENT_RANKS - 1) / (SMS - RESIDENT_RANKS);
+        const int ranks = (int)((all + tiles - 1) / tiles);
         if (ranks > RESIDENT_RANKS) continue;
-        const long long time = rounds * (2 + tiles);
+        if (!counted) return tiles;
+        const int at_once = clusters_at_once(ranks);
+        const long long time = (long long)((count + at_once - 1) / at_once) * (4 + tiles);
         if (best == 0 || time < least) { best = tiles; least = time; }
     }
     return best;
 }
 
-template <bool UPDATE>
+template <class T, bool UPDATE>
 static cudaError_t run(Args& a, int count, int turns, cudaStream_t s) {
-    if (const int tiles = resident_tiles(a.S, a.L, count)) {
+    if (const int tiles = resident_tiles(a.S, a.L, count, true)) {
         static PerDevice done;
-        const cudaError_t e = ensure_smem(resident_kernel<UPDATE>, RESIDENT_MOST, done);
+        const cudaError_t e = ensure_smem(resident_kernel<T, UPDATE>, RESIDENT_MOST, done);
         if (e != cudaSuccess) return e;
         const unsigned ranks = (unsigned)((a.lblocks + tiles - 1) / tiles);
-        ORTHO_LAUNCH(launch_overlapped_cluster(ranks, resident_kernel<UPDATE>, dim3(ranks, (unsigned)count), dim3(RESIDENT_THREADS),
+        ORTHO_LAUNCH(launch_overlapped_cluster(ranks, resident_kernel<T, UPDATE>, dim3(ranks, (unsigned)count), dim3(RESIDENT_THREADS),
                                                (size_t)resident_bytes(resident_rows(a.S), tiles), s, a, tiles, turns));
         return cudaSuccess;
     }
-    ORTHO_LAUNCH(launch_overlapped(true, sums_kernel<UPDATE>, dim3((unsigned)a.parts, (unsigned)count), dim3(PREPARE_THREADS), 0, s, a));
+    ORTHO_LAUNCH(launch_overlapped(true, sums_kernel<T, UPDATE>, dim3((unsigned)a.parts, (unsigned)count), dim3(PREPARE_THREADS), 0, s, a));
     const size_t tile = a.tall ? sizeof(float) * BLOCK * (BLOCK + 1) : 0;
     static PerDevice done;
-    cudaError_t e = ensure_smem(first_kernel<UPDATE>, sizeof(float) * BLOCK * (BLOCK + 1), done);
+    cudaError_t e = ensure_smem(first_kernel<T, UPDATE>, sizeof(float) * BLOCK * (BLOCK + 1), done);
     if (e != cudaSuccess) return e;
-    ORTHO_LAUNCH(launch_overlapped(true, first_kernel<UPDATE>, dim3((unsigned)(a.sblocks * a.lblocks), (unsigned)count), dim3(PREPARE_THREADS), tile, s, a));
+    ORTHO_LAUNCH(launch_overlapped(true, first_kernel<T, UPDATE>, dim3((unsigned)(a.sblocks * a.lblocks), (unsigned)count), dim3(PREPARE_THREADS), tile, s, a));
     for (int k = 0; k < turns; ++k) {
         if ((e = gemm<GRAM>(a, count, s)) != cudaSuccess || (e = gemm<POLY>(a, count, s)) != cudaSuccess) return e;
-        if ((e = k + 1 < turns ? gemm<APPLY>(a, count, s) : gemm<LAST>(a, count, s)) != cudaSuccess) return e;
+        if ((e = k + 1 < turns ? gemm<APPLY>(a, count, s) : gemm<LAST, T>(a, count, s)) != cudaSuccess) return e;
         std::swap(a.x, a.y);
     }
     return cudaSuccess;
+}
+
+template <class T>
+static cudaError_t run_for(Args& a, bool update, int count, int turns, cudaStream_t s) {
+    return update ? run<T, true>(a, count, turns, s) : run<T, false>(a, count, turns, s);
 }
 
 struct Layout { int sblocks, lblocks, group; uint64_t x, square, part, status, total; };
@@ -98,7 +126,7 @@ static int layout_of(const gleam_matrix_dims* d, Layout* l) {
     l->group = (int)std::min<long long>(d->count, GROUP);
     l->x = l->square = l->part = 0;
     l->total = d->count && S ? 256 : 0;
-    if (l->total == 0 || resident_tiles(S, L, 1)) return GLEAM_OK;
+    if (l->total == 0 || resident_tiles(S, L, 1, false)) return GLEAM_OK;
     l->x = (uint64_t)l->group * l->sblocks * l->lblocks * BLOCK_BYTES;
     l->square = (uint64_t)l->group * l->sblocks * l->sblocks * BLOCK_BYTES;
     l->part = (uint64_t)GROUP * PARTS * sizeof(float);
@@ -167,7 +195,10 @@ static int orthogonal(const void* const* u, float* const* momenta, void* const* 
         for (int k = 0; k < count; ++k) {
             a.u[k] = u[i0 + k]; a.out[k] = out[i0 + k]; a.momentum[k] = m ? momenta[i0 + k] : nullptr;
         }
-        const cudaError_t e = m ? run<true>(a, count, d->turns, (cudaStream_t)d->stream) : run<false>(a, count, d->turns, (cudaStream_t)d->stream);
+        const cudaStream_t s = (cudaStream_t)d->stream;
+        const cudaError_t e = d->dtype == GLEAM_F32 ? run_for<float>(a, m != nullptr, count, d->turns, s)
+                            : d->dtype == GLEAM_F16 ? run_for<__half>(a, m != nullptr, count, d->turns, s)
+                                                    : run_for<__nv_bfloat16>(a, m != nullptr, count, d->turns, s);
         if (e != cudaSuccess) return GLEAM_ERR_CUDA;
     }
     return GLEAM_OK;

@@ -9,15 +9,15 @@ namespace ortho {
 constexpr int PREPARE_THREADS = 256;
 
 // What is orthogonalised: the matrix itself, or gradient and momentum.
-template <bool UPDATE>
+template <class T, bool UPDATE>
 __device__ __forceinline__ float source(const Args& a, int m, long long i) {
-    if (!UPDATE) return load_as(a.u[m], a.dtype, i);
+    if (!UPDATE) return load_at<T>(a.u[m], i);
     const float v = a.momentum[m][i];
-    return a.nesterov ? fmaf(a.mu, v, load_as(a.u[m], a.dtype, i)) : v;
+    return a.nesterov ? fmaf(a.mu, v, load_at<T>(a.u[m], i)) : v;
 }
 
 // momentum <- mu momentum + gradient, and sums of squares of what is orthogonalised, in a fixed order.
-template <bool UPDATE>
+template <class T, bool UPDATE>
 __global__ void __launch_bounds__(PREPARE_THREADS) sums_kernel(const __grid_constant__ Args a) {
     grid_dependency_wait();
     const int m = blockIdx.y;
@@ -30,7 +30,7 @@ __global__ void __launch_bounds__(PREPARE_THREADS) sums_kernel(const __grid_cons
 #pragma unroll
         for (int k = 0; k < AT_ONCE; ++k) {
             const long long i = i0 + k * step;
-            v[k] = i < n ? load_as(a.u[m], a.dtype, i) : 0.f;
+            v[k] = i < n ? load_at<T>(a.u[m], i) : 0.f;
             if (UPDATE) w[k] = i < n ? a.momentum[m][i] : 0.f;
         }
 #pragma unroll
@@ -49,7 +49,7 @@ __global__ void __launch_bounds__(PREPARE_THREADS) sums_kernel(const __grid_cons
 }
 
 // One block of X_0 = U / (|U| + eps), in pieces.
-template <bool UPDATE>
+template <class T, bool UPDATE>
 __global__ void __launch_bounds__(PREPARE_THREADS) first_kernel(const __grid_constant__ Args a) {
     grid_dependency_wait();
     extern __shared__ float tile[];                  // tall: 128 columns of the block with one number between them
@@ -65,7 +65,7 @@ __global__ void __launch_bounds__(PREPARE_THREADS) first_kernel(const __grid_con
 #pragma unroll 8
         for (int i = threadIdx.x; i < BLOCK * BLOCK; i += PREPARE_THREADS) {
             const int l = i / BLOCK, s = i % BLOCK;
-            tile[l * (BLOCK + 1) + s] = s0 + s < a.S && l0 + l < a.L ? source<UPDATE>(a, m, (l0 + l) * a.cols + s0 + s) : 0.f;
+            tile[l * (BLOCK + 1) + s] = s0 + s < a.S && l0 + l < a.L ? source<T, UPDATE>(a, m, (l0 + l) * a.cols + s0 + s) : 0.f;
         }
         __syncthreads();
     }
@@ -77,7 +77,7 @@ __global__ void __launch_bounds__(PREPARE_THREADS) first_kernel(const __grid_con
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             if (a.tall) v[j] = tile[(c + j) * (BLOCK + 1) + r];
-            else v[j] = s0 + r < a.S && l0 + c + j < a.L ? source<UPDATE>(a, m, (s0 + r) * a.cols + l0 + c + j) : 0.f;
+            else v[j] = s0 + r < a.S && l0 + c + j < a.L ? source<T, UPDATE>(a, m, (s0 + r) * a.cols + l0 + c + j) : 0.f;
             v[j] *= by;
         }
         uint4 hi, lo;

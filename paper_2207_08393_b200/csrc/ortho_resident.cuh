@@ -6,9 +6,9 @@
 //     rows, and write the pieces of A to all;
 //   - computes P = b A + c A A, which costs less than sharing it;
 //   - replaces its tiles by a X + P X.
-// Two barriers of the cluster a turn, nothing but the matrix itself through global memory, once each way.  Products of K <= 128 are
-// done within a microsecond: what the time goes to is moving sums from tensor memory and back to shared memory as pieces, by all
-// 16 warps, and barriers.
+// Two barriers of the cluster a turn, nothing but the matrix itself through global memory, once each way.  A product instruction takes
+// some 65 cycles whatever N is, the reading of its operands from shared memory, so tiles are laid out for N = 128: cores of 8 rows
+// by 16 bytes, 16 of them along a row.
 #pragma once
 #include "ortho_gemm.cuh"
 
@@ -19,27 +19,29 @@ constexpr int RESIDENT_THREADS = 512, RESIDENT_RANKS = 8, RESIDENT_HEAD = 1024;
 constexpr int RESIDENT_LEAST = 120 * 1024;       // shared memory that keeps a second block, which would wait for tensor memory, off the SM
 constexpr int RESIDENT_MOST = 227 * 1024;
 
-// Shared memory: head, sums in 32 bits, A (then P), tiles; a product reads 128 rows of an operand whatever R is, hence the end.
+// Shared memory: head, tiles, A (then P), sums in 32 bits.  A product reads 128 rows of an operand whatever R is: into what stands behind
+// it, up to (128 - R) * 256 bytes, for rows of the result that nobody takes.
 __host__ __device__ inline int resident_rows(long long S) { return (int)((S + 15) / 16 * 16); }
 __host__ inline int resident_bytes(int R, int tiles) {
-    const int n = RESIDENT_HEAD + (2 + tiles) * R * 512 + (BLOCK - R) * 128;
+    const int beyond = (BLOCK - R) * 256 - R * 512, n = RESIDENT_HEAD + (2 + tiles) * R * 512 + (beyond > 0 ? beyond : 0);
     return n < RESIDENT_LEAST ? RESIDENT_LEAST : n;
 }
 
-template <bool UPDATE>
+template <class T, bool UPDATE>
 __global__ void __launch_bounds__(RESIDENT_THREADS, 1) resident_kernel(const __grid_constant__ Args a, int tiles, int turns) {
     extern __shared__ __align__(1024) unsigned char smem[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, ranks = gridDim.x, rank = ranks > 1 ? (int)tc::cluster_rank() : 0, m = blockIdx.y;
     const int R = resident_rows(a.S), square = R * 512;                    // bytes of R rows of 128 as pieces, or in 32 bits
-    const uint32_t base = tc::shared_address(smem), done = base + 16;
-    unsigned char* A_ = smem + RESIDENT_HEAD + square;
-    unsigned char* X = A_ + square;
-    float* sum = reinterpret_cast<float*>(smem + RESIDENT_HEAD);
+    const uint32_t base = tc::shared_address(smem), done = base + 16, second = base + 24;
+    unsigned char* X = smem + RESIDENT_HEAD;
+    unsigned char* A_ = X + tiles * square;
+    float* sum = reinterpret_cast<float*>(A_ + square);
     float* part = reinterpret_cast<float*>(smem + 64);                     // a rank's sum of squares; the block's sums behind it
-    const uint32_t a_at = base + RESIDENT_HEAD + square, x_at = a_at + square;
+    const uint32_t x_at = base + RESIDENT_HEAD, a_at = x_at + tiles * square, sum_from = a_at + square;
     if (warp == 0) tc::take_columns(base, 512);
     if (threadIdx.x == 0) {
         tc::barrier_init(done, 1);
+        tc::barrier_init(second, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     tc::fence_before();
@@ -51,15 +53,15 @@ __global__ void __launch_bounds__(RESIDENT_THREADS, 1) resident_kernel(const __g
     const long long first = (long long)rank * tiles;                       // this block's tiles
     const int mine = (int)((a.L + BLOCK - 1) / BLOCK - first < tiles ? (a.L + BLOCK - 1) / BLOCK - first : tiles);
     bool failed = false;
-    uint32_t phase = 0;
+    uint32_t phase = 0, second_phase = 0;
     if (threadIdx.x == 0 && m == 0 && rank == 0) *a.status = 0;
 
     // byte of element (r, c) of a piece of R rows
-    auto at = [&](int r, int c) { return (c >> 6) * (R * 128) + (r >> 3) * 1024 + ((c >> 3) & 7) * CORE + (r & 7) * 16; };
+    auto at = [&](int r, int c) { return (r >> 3) * 2048 + (c >> 3) * CORE + (r & 7) * 16; };
     const int lo = R * 256;                                                // from hi to lo
-    auto wait = [&]() {
-        if (!failed && !tc::barrier_wait(done, phase)) failed = true;
-        phase ^= 1;
+    auto wait = [&](uint32_t bar, uint32_t& turns_of) {
+        if (!failed && !tc::barrier_wait(bar, turns_of)) failed = true;
+        turns_of ^= 1;
         tc::fence_after();
     };
     // shared memory written by threads is there for the products; tensor memory that was read may be written
@@ -72,30 +74,35 @@ __global__ void __launch_bounds__(RESIDENT_THREADS, 1) resident_kernel(const __g
 
     // the source in 32 bits where its tile will stand, and the sum of squares
     float squares = 0.f;
-    constexpr int AT_ONCE = 8;
+    // Elements of a tile: lanes along what is contiguous in the matrix, four lines at a time.
+    constexpr int AT_ONCE = 16, LINES = RESIDENT_THREADS / BLOCK;
+    const int along = threadIdx.x & (BLOCK - 1), line0 = threadIdx.x / BLOCK, lines = a.tall ? BLOCK : R;
+    auto spot = [&](int line) { return a.tall ? sum_at(along, line) : sum_at(line, along); };
     for (int t = 0; t < mine; ++t) {
         float* to = reinterpret_cast<float*>(X + t * square);
         const long long l0 = (first + t) * BLOCK;
-        for (int i0 = threadIdx.x; i0 < R * BLOCK; i0 += AT_ONCE * RESIDENT_THREADS) {
+        const int width = a.L - l0 < BLOCK ? (int)(a.L - l0) : BLOCK, limit = along < (a.tall ? (int)a.S : width) ? (a.tall ? width : (int)a.S) : 0;
+        const long long corner = (a.tall ? l0 * a.cols : l0) + along;
+        const T* from = static_cast<const T*>(a.u[m]) + corner;
+        float* momentum = UPDATE ? a.momentum[m] + corner : nullptr;
+        for (int line = line0; line < lines; line += AT_ONCE * LINES) {
             float v[AT_ONCE], w[AT_ONCE];
-            long long from[AT_ONCE];
 #pragma unroll
             for (int k = 0; k < AT_ONCE; ++k) {
-                const int i = i0 + k * RESIDENT_THREADS, r = a.tall ? i % R : i / BLOCK, c = a.tall ? i / R : i % BLOCK;
-                from[k] = i < R * BLOCK && r < a.S && l0 + c < a.L ? (a.tall ? (l0 + c) * a.cols + r : r * a.cols + l0 + c) : -1;
-                v[k] = from[k] >= 0 ? load_as(a.u[m], a.dtype, from[k]) : 0.f;
-                if (UPDATE) w[k] = from[k] >= 0 ? a.momentum[m][from[k]] : 0.f;
+                const int n = line + k * LINES;
+                v[k] = n < limit ? to_float(from[n * a.cols]) : 0.f;
+                if (UPDATE) w[k] = n < limit ? momentum[n * a.cols] : 0.f;
             }
 #pragma unroll
             for (int k = 0; k < AT_ONCE; ++k) {
-                const int i = i0 + k * RESIDENT_THREADS, r = a.tall ? i % R : i / BLOCK, c = a.tall ? i / R : i % BLOCK;
+                const int n = line + k * LINES;
                 if (UPDATE) {
                     w[k] = fmaf(a.mu, w[k], v[k]);
-                    if (from[k] >= 0) a.momentum[m][from[k]] = w[k];
+                    if (n < limit) momentum[n * a.cols] = w[k];
                     v[k] = a.nesterov ? fmaf(a.mu, w[k], v[k]) : w[k];
                 }
                 squares = fmaf(v[k], v[k], squares);
-                if (i < R * BLOCK) to[sum_at(r, c)] = v[k];
+                if (n < lines && (!a.tall || along < R)) to[spot(n)] = v[k];
             }
         }
     }
@@ -171,15 +178,15 @@ __global__ void __launch_bounds__(RESIDENT_THREADS, 1) resident_kernel(const __g
             const uint32_t what = tc::instruction(R, false);
             for (int t = 0; t < mine; ++t)
                 for (int k = 0; k < BLOCK / 16; ++k) {
-                    const uint32_t p = x_at + t * square + (k >> 2) * (R * 128) + (k & 3) * 256;
-                    const uint64_t h = tc::descriptor(p, 128, 1024), l = tc::descriptor(p + lo, 128, 1024);
+                    const uint32_t p = x_at + t * square + k * 256;
+                    const uint64_t h = tc::descriptor(p, 128, 2048), l = tc::descriptor(p + lo, 128, 2048);
                     tc::product(cols0 + BLOCK, l, h, what, t > 0 || k > 0);
                     tc::product(cols0 + BLOCK, h, l, what, true);
                     tc::product(cols0, h, h, what, t > 0 || k > 0);
                 }
             tc::commit(done);
         }
-        wait();
+        wait(done, phase);
         if (col0 < R) {
             float v[32];
             read_sums(0, v);
@@ -189,36 +196,39 @@ __global__ void __launch_bounds__(RESIDENT_THREADS, 1) resident_kernel(const __g
                     if (col0 + j < R) *reinterpret_cast<float4*>(sum + sum_at(row, col0 + j)) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
             }
         }
-        // A = the sum over the cluster, in pieces, a share of it from each block to all blocks
-        if (ranks > 1) tc::cluster_sync(); else __syncthreads();
-        const int across = R / 8, all = R * across, share = (all + ranks - 1) / ranks, end = (rank + 1) * share < all ? (rank + 1) * share : all;
-        for (int i = rank * share + threadIdx.x; i < end; i += RESIDENT_THREADS) {
-            const int r = (i & 7) + (i >> 3) / across * 8, c = (i >> 3) % across * 8;
-            float4 f[RESIDENT_RANKS], g[RESIDENT_RANKS];
-            const uint32_t p = base + RESIDENT_HEAD + 4 * sum_at(r, c), q = base + RESIDENT_HEAD + 4 * sum_at(r, c + 4);
+        // A = the sum over the cluster: each block adds a share of the rows (eights of them), lanes along a row as remote reads want it, ...
+        const int g0 = R / 8 * rank / ranks, g1 = R / 8 * (rank + 1) / ranks;
+        if (ranks > 1) {
+            tc::cluster_sync();
+            for (int i = g0 * 256 + threadIdx.x; i < g1 * 256; i += RESIDENT_THREADS) {
+                if ((((i & 31) ^ (i >> 5)) & 31) * 4 >= R) continue;             // 16 bytes of a row beyond R
+                float4 f[RESIDENT_RANKS];
 #pragma unroll
-            for (int k = 0; k < RESIDENT_RANKS; ++k)
-                if (k < ranks) {
-                    f[k] = ranks > 1 ? tc::read_remote(p, k) : *reinterpret_cast<const float4*>(smem + (p - base));
-                    g[k] = ranks > 1 ? tc::read_remote(q, k) : *reinterpret_cast<const float4*>(smem + (q - base));
-                }
+                for (int k = 0; k < RESIDENT_RANKS; ++k)
+                    if (k < ranks) f[k] = tc::read_remote(sum_from + 16 * i, k);
 #pragma unroll
-            for (int k = 1; k < RESIDENT_RANKS; ++k)
-                if (k < ranks) {
-                    f[0].x += f[k].x; f[0].y += f[k].y; f[0].z += f[k].z; f[0].w += f[k].w;
-                    g[0].x += g[k].x; g[0].y += g[k].y; g[0].z += g[k].z; g[0].w += g[k].w;
-                }
-            const float v[8] = {f[0].x, f[0].y, f[0].z, f[0].w, g[0].x, g[0].y, g[0].z, g[0].w};
+                for (int k = 1; k < RESIDENT_RANKS; ++k)
+                    if (k < ranks) { f[0].x += f[k].x; f[0].y += f[k].y; f[0].z += f[k].z; f[0].w += f[k].w; }
+                reinterpret_cast<float4*>(sum)[i] = f[0];                         // these rows of this block's sums are nobody else's
+            }
+        }
+        __syncthreads();
+        // ... and writes its pieces to all
+        const int across = R / 8;
+        for (int i = threadIdx.x; i < (g1 - g0) * across * 8; i += RESIDENT_THREADS) {
+            const int r = (i & 7) + (g0 + (i >> 3) / across) * 8, c = (i >> 3) % across * 8;
+            const float4 f = *reinterpret_cast<const float4*>(sum + sum_at(r, c)), g = *reinterpret_cast<const float4*>(sum + sum_at(r, c + 4));
+            const float v[8] = {f.x, f.y, f.z, f.w, g.x, g.y, g.z, g.w};
             uint4 h, l;
             split8(v, h, l);
-            for (int k = 0; k < ranks; ++k) {
-                if (ranks > 1) {
+            if (ranks > 1) {
+                for (int k = 0; k < ranks; ++k) {
                     tc::write_remote(a_at + at(r, c), k, h);
                     tc::write_remote(a_at + lo + at(r, c), k, l);
-                } else {
-                    *reinterpret_cast<uint4*>(A_ + at(r, c)) = h;
-                    *reinterpret_cast<uint4*>(A_ + lo + at(r, c)) = l;
                 }
+            } else {
+                *reinterpret_cast<uint4*>(A_ + at(r, c)) = h;
+                *reinterpret_cast<uint4*>(A_ + lo + at(r, c)) = l;
             }
         }
         if (ranks > 1) tc::cluster_sync();
@@ -226,15 +236,15 @@ __global__ void __launch_bounds__(RESIDENT_THREADS, 1) resident_kernel(const __g
         if (threadIdx.x == 0) {
             const uint32_t what = tc::instruction(R, false);
             for (int k = 0; k < R / 16; ++k) {
-                const uint32_t p = a_at + (k >> 2) * (R * 128) + (k & 3) * 256;
-                const uint64_t h = tc::descriptor(p, 128, 1024), l = tc::descriptor(p + lo, 128, 1024);
+                const uint32_t p = a_at + k * 256;
+                const uint64_t h = tc::descriptor(p, 128, 2048), l = tc::descriptor(p + lo, 128, 2048);
                 tc::product(cols0 + 3 * BLOCK, l, h, what, k > 0);
                 tc::product(cols0 + 3 * BLOCK, h, l, what, true);
                 tc::product(cols0 + 2 * BLOCK, h, h, what, k > 0);
             }
             tc::commit(done);
         }
-        wait();
+        wait(done, phase);
         if (col0 < R) {
             float v[32];
             read_sums(2 * BLOCK, v);
@@ -252,22 +262,22 @@ __global__ void __launch_bounds__(RESIDENT_THREADS, 1) resident_kernel(const __g
         for (int t0 = 0; t0 < mine; t0 += 2) {
             settle();
             if (threadIdx.x == 0) {
-                const uint32_t what = tc::instruction(BLOCK / 2, true);
-                for (int t = t0; t < mine && t < t0 + 2; ++t)
+                const uint32_t what = tc::instruction(BLOCK, true);
+                for (int t = t0; t < mine && t < t0 + 2; ++t) {
                     for (int k = 0; k < R / 16; ++k) {
-                        const uint32_t p = a_at + (k >> 2) * (R * 128) + (k & 3) * 256, q = x_at + t * square + k * 2048, to = cols0 + (t - t0) * 2 * BLOCK;
-                        const uint64_t ph = tc::descriptor(p, 128, 1024), pl = tc::descriptor(p + lo, 128, 1024);
-                        for (int h = 0; h < 2; ++h) {
-                            const uint64_t xh = tc::descriptor(q + h * (R * 128), 1024, 128), xl = tc::descriptor(q + lo + h * (R * 128), 1024, 128);
-                            tc::product(to + BLOCK + h * 64, pl, xh, what, k > 0);
-                            tc::product(to + BLOCK + h * 64, ph, xl, what, true);
-                            tc::product(to + h * 64, ph, xh, what, k > 0);
-                        }
+                        // cores of P: 2048 bytes from one to the next along M, 128 along K; of X: 128 along N, 2048 along K
+                        const uint32_t p = a_at + k * 256, q = x_at + t * square + k * 4096, to = cols0 + (t - t0) * 2 * BLOCK;
+                        const uint64_t ph = tc::descriptor(p, 128, 2048), pl = tc::descriptor(p + lo, 128, 2048);
+                        const uint64_t xh = tc::descriptor(q, 2048, 128), xl = tc::descriptor(q + lo, 2048, 128);
+                        tc::product(to + BLOCK, pl, xh, what, k > 0);
+                        tc::product(to + BLOCK, ph, xl, what, true);
+                        tc::product(to, ph, xh, what, k > 0);
                     }
-                tc::commit(done);
+                    tc::commit(t == t0 ? done : second);
+                }
             }
-            wait();
             for (int t = t0; t < mine && t < t0 + 2; ++t) {
+                if (t == t0) wait(done, phase); else wait(second, second_phase);         // the second product runs while the first is stored
                 float v[32];
                 read_sums((t - t0) * 2 * BLOCK, v);
                 if (turn + 1 < turns) {
@@ -294,22 +304,22 @@ __global__ void __launch_bounds__(RESIDENT_THREADS, 1) resident_kernel(const __g
                 }
                 __syncthreads();
                 const long long l0 = (first + t) * BLOCK;
-                for (int i0 = threadIdx.x; i0 < R * BLOCK; i0 += AT_ONCE * RESIDENT_THREADS) {
+                const int width = a.L - l0 < BLOCK ? (int)(a.L - l0) : BLOCK, limit = along < (a.tall ? (int)a.S : width) ? (a.tall ? width : (int)a.S) : 0;
+                T* out = static_cast<T*>(a.out[m]) + (a.tall ? l0 * a.cols : l0) + along;
+                for (int line = line0; line < limit; line += AT_ONCE * LINES) {
                     float w[AT_ONCE];
-                    long long to[AT_ONCE];
 #pragma unroll
                     for (int k = 0; k < AT_ONCE; ++k) {
-                        const int i = i0 + k * RESIDENT_THREADS, r = a.tall ? i % R : i / BLOCK, c = a.tall ? i / R : i % BLOCK;
-                        to[k] = i < R * BLOCK && r < a.S && l0 + c < a.L ? (a.tall ? (l0 + c) * a.cols + r : r * a.cols + l0 + c) : -1;
-                        w[k] = UPDATE && to[k] >= 0 ? load_as(a.out[m], a.dtype, to[k]) : 0.f;
+                        const int n = line + k * LINES;
+                        w[k] = UPDATE && n < limit ? to_float(out[n * a.cols]) : 0.f;
                     }
 #pragma unroll
                     for (int k = 0; k < AT_ONCE; ++k) {
-                        const int i = i0 + k * RESIDENT_THREADS, r = a.tall ? i % R : i / BLOCK, c = a.tall ? i / R : i % BLOCK;
-                        if (to[k] < 0) continue;
-                        float x = sum[sum_at(r, c)] * (1.f / SCALE);
+                        const int n = line + k * LINES;
+                        if (n >= limit) break;
+                        float x = sum[spot(n)] * (1.f / SCALE);
                         if (UPDATE) x = fmaf(a.keep, w[k], -a.move * x);
-                        store_as(a.out[m], a.dtype, to[k], x);
+                        out[n * a.cols] = from_float<T>(x);
                     }
                 }
             }

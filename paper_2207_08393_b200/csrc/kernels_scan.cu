@@ -25,7 +25,8 @@ using T = __nv_bfloat16;
 #define SCAN_LAUNCH(...) do { cudaError_t e_ = prof_mark(GLEAM_K_SCAN, s); if (e_ == cudaSuccess) e_ = launch_overlapped(true, __VA_ARGS__); \
                               if (e_ != cudaSuccess) return e_; } while (0)
 
-constexpr int SMS = 148, WIDE = 8 / sizeof(T);           // chains a thread of columns takes where alignment allows
+constexpr int SMS = 148, WIDE = 8 / sizeof(T);           // chains of a thread's piece of 8 bytes
+constexpr int NARROW = 128;                              // rows of fewer chains, where they start anywhere, are no strips
 
 static long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
 
@@ -71,7 +72,7 @@ static bool wide(const Args& a, int v, std::initializer_list<Array> arrays, std:
         if ((a.batch > 1 && u.s->batch % v) || (a.channels > 1 && u.s->channel % v) || (a.steps > 1 && u.s->step % v)) return false;
     }
     for (const void* p : states)
-        if ((uintptr_t)p % (v * sizeof(float))) return false;
+        if ((uintptr_t)p % ((v < 4 ? v : 4) * sizeof(float))) return false;
     return true;
 }
 
@@ -88,18 +89,54 @@ static bool dense(const Args& a, std::initializer_list<Array> arrays) {
 
 template <class F> static cudaError_t by_bool(bool v, F f) { return v ? f(std::true_type{}) : f(std::false_type{}); }
 
-template <int V, bool REVERSE, bool BACK>
-static cudaError_t columns(const Args& a, cudaStream_t s) {
-    const dim3 grid((unsigned)ceil_div(a.rows / V, COLUMN_THREADS), (unsigned)a.parts), block(COLUMN_THREADS);
-    if (a.parts > 1) {
-        if constexpr (BACK) SCAN_LAUNCH(columns_vjp<T, V, REVERSE, true>, grid, block, 0, s, a);
-        else SCAN_LAUNCH(columns_forward<T, V, REVERSE, true>, grid, block, 0, s, a);
-        Args j = a;
-        j.descending = BACK; j.enter = BACK ? a.dlast : a.state;
-        SCAN_LAUNCH(join_parts<16>, dim3((unsigned)ceil_div(a.rows, COLUMN_THREADS)), block, 0, s, j);
+template <auto KERNEL> static PerDevice kernel_state;
+
+static cudaError_t join(const Args& a, bool back, bool descending, cudaStream_t s) {
+    Args j = a;
+    j.descending = descending; j.enter = back ? a.dlast : a.state;
+    SCAN_LAUNCH(join_parts<8>, dim3((unsigned)ceil_div(a.rows, 32)), dim3(32 * JOIN_WARPS), 0, s, j);
+    return cudaSuccess;
+}
+
+template <int V, bool REVERSE, bool STRIP, int KIND>
+static cudaError_t stream(const Args& a, dim3 grid, cudaStream_t s) {
+    if constexpr (KIND == VJP) {
+        constexpr auto KERNEL = stream_vjp<T, V, REVERSE, STRIP>;
+        const cudaError_t e = ensure_smem(KERNEL, vjp_smem<T, V, STRIP>(), kernel_state<KERNEL>);
+        if (e != cudaSuccess) return e;
+        SCAN_LAUNCH(KERNEL, grid, dim3(STREAM_THREADS), (size_t)vjp_smem<T, V, STRIP>(), s, a);
+    } else {
+        constexpr auto KERNEL = stream_kernel<T, V, REVERSE, STRIP, KIND>;
+        const cudaError_t e = ensure_smem(KERNEL, stream_smem<T, V, STRIP>(), kernel_state<KERNEL>);
+        if (e != cudaSuccess) return e;
+        SCAN_LAUNCH(KERNEL, grid, dim3(STREAM_THREADS), (size_t)stream_smem<T, V, STRIP>(), s, a);
     }
-    if constexpr (BACK) SCAN_LAUNCH(columns_vjp<T, V, REVERSE, false>, grid, block, 0, s, a);
-    else SCAN_LAUNCH(columns_forward<T, V, REVERSE, false>, grid, block, 0, s, a);
+    return cudaSuccess;
+}
+
+template <int V, bool REVERSE, bool STRIP, bool BACK>
+static cudaError_t streams(const Args& a, cudaStream_t s) {
+    const long long blocks = STRIP ? a.batch * a.channels * ceil_div(a.inner, STREAM_THREADS * V) : ceil_div(a.rows / V, STREAM_THREADS);
+    const dim3 grid((unsigned)blocks, (unsigned)a.parts);
+    cudaError_t e;
+    if (a.parts > 1) {
+        if ((e = stream<V, REVERSE, STRIP, BACK ? MAP_VJP : MAP_FORWARD>(a, grid, s)) != cudaSuccess) return e;
+        if ((e = join(a, BACK, BACK, s)) != cudaSuccess) return e;
+    }
+    return stream<V, REVERSE, STRIP, BACK ? VJP : FORWARD>(a, grid, s);
+}
+
+template <bool REVERSE, bool BACK>
+static cudaError_t columns(const Args& a, cudaStream_t s) {
+    const dim3 grid((unsigned)ceil_div(a.rows, COLUMN_THREADS), (unsigned)a.parts), block(COLUMN_THREADS);
+    cudaError_t e;
+    if (a.parts > 1) {
+        if constexpr (BACK) SCAN_LAUNCH(columns_vjp<T, REVERSE, true>, grid, block, 0, s, a);
+        else SCAN_LAUNCH(columns_forward<T, REVERSE, true>, grid, block, 0, s, a);
+        if ((e = join(a, BACK, BACK, s)) != cudaSuccess) return e;
+    }
+    if constexpr (BACK) SCAN_LAUNCH(columns_vjp<T, REVERSE, false>, grid, block, 0, s, a);
+    else SCAN_LAUNCH(columns_forward<T, REVERSE, false>, grid, block, 0, s, a);
     return cudaSuccess;
 }
 
@@ -109,9 +146,8 @@ static cudaError_t rows(const Args& a, cudaStream_t s) {
     const dim3 grid((unsigned)ceil_div(warps, ROW_WARPS)), block(32 * ROW_WARPS);
     if (a.parts > 1) {
         SCAN_LAUNCH(rows_kernel<T, REVERSE, DENSE, BACK ? MAP_VJP : MAP_FORWARD>, grid, block, 0, s, a);
-        Args j = a;
-        j.descending = BACK != REVERSE; j.enter = BACK ? a.dlast : a.state;      // parts are numbered from the first step
-        SCAN_LAUNCH(join_parts<16>, dim3((unsigned)ceil_div(a.rows, COLUMN_THREADS)), dim3(COLUMN_THREADS), 0, s, j);
+        const cudaError_t e = join(a, BACK, BACK != REVERSE, s);                 // parts are numbered from the first step
+        if (e != cudaSuccess) return e;
     }
     SCAN_LAUNCH(rows_kernel<T, REVERSE, DENSE, BACK ? VJP : FORWARD>, grid, block, 0, s, a);
     return cudaSuccess;
@@ -122,8 +158,11 @@ static cudaError_t chains(const Args& a, bool reverse, std::initializer_list<Arr
     return by_bool(reverse, [&](auto r) {
         constexpr bool R = decltype(r)::value;
         if (a.inner == 1) return by_bool(dense(a, arrays), [&](auto d) { return rows<R, decltype(d)::value, BACK>(a, s); });
-        if (wide(a, WIDE, arrays, states)) return columns<WIDE, R, BACK>(a, s);
-        return columns<1, R, BACK>(a, s);
+        if constexpr (!BACK)                   // pieces of 16 bytes where there are chains enough: fewer instructions
+            if (a.rows * a.parts / (2 * WIDE) >= SMS * 384 && wide(a, 2 * WIDE, arrays, states)) return streams<2 * WIDE, R, false, BACK>(a, s);
+        if (wide(a, WIDE, arrays, states)) return streams<WIDE, R, false, BACK>(a, s);
+        if (a.inner >= NARROW) return streams<WIDE, R, true, BACK>(a, s);
+        return columns<R, BACK>(a, s);
     });
 }
 

@@ -1,42 +1,12 @@
-// The gated recurrence where the chains lie side by side in memory (inner > 1): a thread runs V neighbouring chains.
+// The gated recurrence where rows of neighbouring chains are narrow (a few features or voxels between the steps): a thread runs one
+// chain with loads into registers.  And single steps.
 #pragma once
-#include "scan_common.cuh"
+#include "scan_stream.cuh"
 
 namespace gleam {
 namespace scan {
 
 constexpr int COLUMN_THREADS = 128;
-constexpr int CHUNK = 16;                  // steps whose loads a thread has under way, and between saved states
-
-// steps of a chunk: as few chunks as CHUNK allows, all alike
-inline int chunk_steps(long long steps) {
-    const long long n = (steps + CHUNK - 1) / CHUNK;
-    return n < 1 ? 1 : (int)((steps + n - 1) / n);
-}
-
-template <class T, int V> struct alignas(V * sizeof(T)) Piece { T e[V]; };
-
-template <class T, int V>
-__device__ __forceinline__ Piece<T, V> load_piece(const T* p) { return *reinterpret_cast<const Piece<T, V>*>(p); }
-template <class T, int V>
-__device__ __forceinline__ void store_piece(T* p, const Piece<T, V>& v) { *reinterpret_cast<Piece<T, V>*>(p) = v; }
-// V states; V > 1 only where their array starts at V * 4 bytes
-template <int V>
-__device__ __forceinline__ void load_states(const float* p, float (&v)[V]) {
-#pragma unroll
-    for (int j = 0; j < V; ++j) v[j] = 0.f;
-    if (!p) return;
-    const Piece<float, V> u = load_piece<float, V>(p);
-#pragma unroll
-    for (int j = 0; j < V; ++j) v[j] = u.e[j];
-}
-template <int V>
-__device__ __forceinline__ void store_states(float* p, const float (&v)[V]) {
-    Piece<float, V> u;
-#pragma unroll
-    for (int j = 0; j < V; ++j) u.e[j] = v[j];
-    store_piece<float, V>(p, u);
-}
 
 // A thread's V chains.
 struct Columns {
@@ -58,73 +28,57 @@ struct Columns {
 };
 
 // Forward, and the maps of parts for it.  Position q = 0, 1, ... of a chain is step q or T - 1 - q.
-template <class T, int V, bool REVERSE, bool MAPS>
+template <class T, bool REVERSE, bool MAPS>
 __global__ void __launch_bounds__(COLUMN_THREADS) columns_forward(const __grid_constant__ Args a) {
     grid_dependency_wait();
     Columns c{};
-    c.find<V>(a, (long long)blockIdx.x * COLUMN_THREADS + threadIdx.x);
+    c.find<1>(a, (long long)blockIdx.x * COLUMN_THREADS + threadIdx.x);
     if (!c.there) return;
     const T* x = c.at(static_cast<const T*>(a.x), a.sx);
     const T* gate = c.at(static_cast<const T*>(a.gate), a.sgate);
     T* y = MAPS ? nullptr : c.at(static_cast<T*>(a.y), a.sy);
     const long long valid = valid_steps(a, c.batch), steps = a.steps, part = blockIdx.y;
     const long long begin = part * a.part, end = begin + a.part < steps ? begin + a.part : steps;
-    float h[V], prod[V];
-    if (MAPS) {
-#pragma unroll
-        for (int j = 0; j < V; ++j) { h[j] = 0.f; prod[j] = 1.f; }
-    } else if (a.parts > 1) {
-        load_states(a.maps_b + (part * a.rows + c.row), h);
-    } else {
-        load_states(a.state ? a.state + c.row : nullptr, h);
-    }
+    float h = 0.f, prod = 1.f;
+    if (!MAPS && a.parts > 1) h = a.maps_b[part * a.rows + c.row];
+    else if (!MAPS && a.state) h = a.state[c.row];
     for (long long q0 = begin; q0 < end; q0 += a.chunk) {
         const int count = (int)(q0 + a.chunk < end ? a.chunk : end - q0);
-        Piece<T, V> xs[CHUNK], gs[CHUNK];
+        T xs[CHUNK], gs[CHUNK];
 #pragma unroll
         for (int k = 0; k < CHUNK; ++k) {
             const long long t = REVERSE ? steps - 1 - (q0 + k) : q0 + k;
-            if (k < count && t < valid) {
-                xs[k] = load_piece<T, V>(x + t * a.sx.step);
-                gs[k] = load_piece<T, V>(gate + t * a.sgate.step);
-            }
+            if (k < count && t < valid) { xs[k] = x[t * a.sx.step]; gs[k] = gate[t * a.sgate.step]; }
         }
-        if (!MAPS && a.saved && q0 > 0) store_states(a.saved + ((q0 / a.chunk - 1) * a.rows + c.row), h);
+        if (!MAPS && a.saved && q0 > 0) a.saved[(q0 / a.chunk - 1) * a.rows + c.row] = h;
 #pragma unroll
         for (int k = 0; k < CHUNK; ++k) {
             const long long t = REVERSE ? steps - 1 - (q0 + k) : q0 + k;
             if (k >= count) break;
-            Piece<T, V> out;
+            float out = 0.f;
             if (t < valid) {
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    float f, rest;
-                    gate_of(to_float(gs[k].e[j]), f, rest);
-                    h[j] = fmaf(f, h[j], rest * to_float(xs[k].e[j]));
-                    if (MAPS) prod[j] *= f;
-                    else out.e[j] = from_float<T>(h[j]);
-                }
-            } else {
-#pragma unroll
-                for (int j = 0; j < V; ++j) out.e[j] = from_float<T>(0.f);
+                float f, rest;
+                gate_of(to_float(gs[k]), f, rest);
+                out = h = fmaf(f, h, rest * to_float(xs[k]));
+                prod *= f;
             }
-            if (!MAPS) store_piece<T, V>(y + t * a.sy.step, out);
+            if (!MAPS) y[t * a.sy.step] = from_float<T>(out);
         }
     }
     if (MAPS) {
-        store_states(a.maps_a + (part * a.rows + c.row), prod);
-        store_states(a.maps_b + (part * a.rows + c.row), h);
+        a.maps_a[part * a.rows + c.row] = prod;
+        a.maps_b[part * a.rows + c.row] = h;
     } else if (a.last && end == steps) {
-        store_states(a.last + c.row, h);
+        a.last[c.row] = h;
     }
 }
 
 // VJP, and the maps of parts for it: part p covers the same positions as in the forward call, taken from its end.
-template <class T, int V, bool REVERSE, bool MAPS>
+template <class T, bool REVERSE, bool MAPS>
 __global__ void __launch_bounds__(COLUMN_THREADS) columns_vjp(const __grid_constant__ Args a) {
     grid_dependency_wait();
     Columns c{};
-    c.find<V>(a, (long long)blockIdx.x * COLUMN_THREADS + threadIdx.x);
+    c.find<1>(a, (long long)blockIdx.x * COLUMN_THREADS + threadIdx.x);
     if (!c.there) return;
     const T* x = MAPS ? nullptr : c.at(static_cast<const T*>(a.x), a.sx);
     const T* gate = c.at(static_cast<const T*>(a.gate), a.sgate);
@@ -133,42 +87,31 @@ __global__ void __launch_bounds__(COLUMN_THREADS) columns_vjp(const __grid_const
     T* dg = MAPS ? nullptr : c.at(static_cast<T*>(a.dg), a.sdg);
     const long long valid = valid_steps(a, c.batch), steps = a.steps, part = blockIdx.y;
     const long long begin = part * a.part, end = begin + a.part < steps ? begin + a.part : steps;
-    float back[V], prod[V];
-    if (MAPS) {
-#pragma unroll
-        for (int j = 0; j < V; ++j) { back[j] = 0.f; prod[j] = 1.f; }
-    } else if (a.parts > 1) {
-        load_states(a.maps_b + (part * a.rows + c.row), back);
-    } else {
-        load_states(a.dlast ? a.dlast + c.row : nullptr, back);
-    }
+    float back = 0.f, prod = 1.f;
+    if (!MAPS && a.parts > 1) back = a.maps_b[part * a.rows + c.row];
+    else if (!MAPS && a.dlast) back = a.dlast[c.row];
     for (long long q0 = begin + (end - begin - 1) / a.chunk * a.chunk; q0 >= begin; q0 -= a.chunk) {
         const int count = (int)(q0 + a.chunk < end ? a.chunk : end - q0);
-        Piece<T, V> xs[CHUNK], gs[CHUNK], ds[CHUNK];
+        T xs[CHUNK], gs[CHUNK], ds[CHUNK];
 #pragma unroll
         for (int k = 0; k < CHUNK; ++k) {
             const long long t = REVERSE ? steps - 1 - (q0 + k) : q0 + k;
             if (k < count && t < valid) {
-                gs[k] = load_piece<T, V>(gate + t * a.sgate.step);
-                ds[k] = load_piece<T, V>(dy + t * a.sdy.step);
-                if (!MAPS) xs[k] = load_piece<T, V>(x + t * a.sx.step);
+                gs[k] = gate[t * a.sgate.step]; ds[k] = dy[t * a.sdy.step];
+                if (!MAPS) xs[k] = x[t * a.sx.step];
             }
         }
-        float before[CHUNK][V];
-        if (!MAPS) {
-            float h[V];
-            load_states(q0 > 0 ? a.saved + ((q0 / a.chunk - 1) * a.rows + c.row) : a.state ? a.state + c.row : nullptr, h);
+        float f[CHUNK], rest[CHUNK], w[CHUNK], h = 0.f;                  // w: h_(t-1) - x_t
+        if (!MAPS) h = q0 > 0 ? a.saved[(q0 / a.chunk - 1) * a.rows + c.row] : a.state ? a.state[c.row] : 0.f;
 #pragma unroll
-            for (int k = 0; k < CHUNK; ++k) {
-                const long long t = REVERSE ? steps - 1 - (q0 + k) : q0 + k;
-                if (k < count && t < valid) {
-#pragma unroll
-                    for (int j = 0; j < V; ++j) {
-                        float f, rest;
-                        before[k][j] = h[j];
-                        gate_of(to_float(gs[k].e[j]), f, rest);
-                        h[j] = fmaf(f, h[j], rest * to_float(xs[k].e[j]));
-                    }
+        for (int k = 0; k < CHUNK; ++k) {
+            const long long t = REVERSE ? steps - 1 - (q0 + k) : q0 + k;
+            if (k < count && t < valid) {
+                gate_of(to_float(gs[k]), f[k], rest[k]);
+                if (!MAPS) {
+                    const float u = to_float(xs[k]);
+                    w[k] = h - u;
+                    h = fmaf(f[k], h, rest[k] * u);
                 }
             }
         }
@@ -176,54 +119,24 @@ __global__ void __launch_bounds__(COLUMN_THREADS) columns_vjp(const __grid_const
         for (int k = CHUNK - 1; k >= 0; --k) {
             if (k >= count) continue;
             const long long t = REVERSE ? steps - 1 - (q0 + k) : q0 + k;
-            Piece<T, V> ox, og;
+            float ox = 0.f, og = 0.f;
             if (t < valid) {
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    float f, rest;
-                    gate_of(to_float(gs[k].e[j]), f, rest);
-                    const float d = back[j] + to_float(ds[k].e[j]);
-                    back[j] = d * f;
-                    if (MAPS) { prod[j] *= f; continue; }
-                    const float e = d * rest;
-                    ox.e[j] = from_float<T>(e);
-                    og.e[j] = from_float<T>(e * f * (before[k][j] - to_float(xs[k].e[j])));
-                }
-            } else {
-#pragma unroll
-                for (int j = 0; j < V; ++j) { ox.e[j] = from_float<T>(0.f); og.e[j] = from_float<T>(0.f); }
+                const float d = back + to_float(ds[k]);
+                back = d * f[k];
+                prod *= f[k];
+                if (!MAPS) { ox = d * rest[k]; og = ox * f[k] * w[k]; }
             }
             if (!MAPS) {
-                store_piece<T, V>(dx + t * a.sdx.step, ox);
-                store_piece<T, V>(dg + t * a.sdg.step, og);
+                dx[t * a.sdx.step] = from_float<T>(ox);
+                dg[t * a.sdg.step] = from_float<T>(og);
             }
         }
     }
     if (MAPS) {
-        store_states(a.maps_a + (part * a.rows + c.row), prod);
-        store_states(a.maps_b + (part * a.rows + c.row), back);
+        a.maps_a[part * a.rows + c.row] = prod;
+        a.maps_b[part * a.rows + c.row] = back;
     } else if (a.dstate && begin == 0) {
-        store_states(a.dstate + c.row, back);
-    }
-}
-
-// The parts' maps joined: maps_b becomes the state that each part starts from.  A thread runs one chain.
-template <int AHEAD>
-__global__ void __launch_bounds__(COLUMN_THREADS) join_parts(const __grid_constant__ Args a) {
-    grid_dependency_wait();
-    const long long row = (long long)blockIdx.x * COLUMN_THREADS + threadIdx.x;
-    if (row >= a.rows) return;
-    float s = a.enter ? a.enter[row] : 0.f;
-    const long long step = a.descending ? -a.rows : a.rows;
-    long long at = (a.descending ? (a.parts - 1) * a.rows : 0) + row;
-    for (int p0 = 0; p0 < a.parts; p0 += AHEAD, at += AHEAD * step) {
-        float fa[AHEAD], fb[AHEAD];
-#pragma unroll
-        for (int k = 0; k < AHEAD; ++k)
-            if (p0 + k < a.parts) { fa[k] = a.maps_a[at + k * step]; fb[k] = a.maps_b[at + k * step]; }
-#pragma unroll
-        for (int k = 0; k < AHEAD; ++k)
-            if (p0 + k < a.parts) { a.maps_b[at + k * step] = s; s = fmaf(fa[k], s, fb[k]); }
+        a.dstate[c.row] = back;
     }
 }
 
@@ -234,20 +147,19 @@ __global__ void __launch_bounds__(COLUMN_THREADS) step_kernel(const __grid_const
     Columns c{};
     c.find<V>(a, (long long)blockIdx.x * COLUMN_THREADS + threadIdx.x);
     if (!c.there) return;
-    const Piece<T, V> x = load_piece<T, V>(c.at(static_cast<const T*>(a.x), a.sx));
-    const Piece<T, V> gate = load_piece<T, V>(c.at(static_cast<const T*>(a.gate), a.sgate));
-    float h[V];
-    load_states(a.last + c.row, h);
+    const Piece<T, V> x = *reinterpret_cast<const Piece<T, V>*>(c.at(static_cast<const T*>(a.x), a.sx));
+    const Piece<T, V> gate = *reinterpret_cast<const Piece<T, V>*>(c.at(static_cast<const T*>(a.gate), a.sgate));
+    Piece<float, V> h = *reinterpret_cast<const Piece<float, V>*>(a.last + c.row);
     Piece<T, V> out;
 #pragma unroll
     for (int j = 0; j < V; ++j) {
         float f, rest;
         gate_of(to_float(gate.e[j]), f, rest);
-        h[j] = fmaf(f, h[j], rest * to_float(x.e[j]));
-        out.e[j] = from_float<T>(h[j]);
+        h.e[j] = fmaf(f, h.e[j], rest * to_float(x.e[j]));
+        out.e[j] = from_float<T>(h.e[j]);
     }
-    store_states(a.last + c.row, h);
-    store_piece<T, V>(c.at(static_cast<T*>(a.y), a.sy), out);
+    *reinterpret_cast<Piece<float, V>*>(a.last + c.row) = h;
+    *reinterpret_cast<Piece<T, V>*>(c.at(static_cast<T*>(a.y), a.sy)) = out;
 }
 
 }  // namespace scan

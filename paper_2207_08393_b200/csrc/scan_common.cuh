@@ -42,12 +42,11 @@ struct Args {
 
 enum { MAP_FORWARD, MAP_VJP, FORWARD, VJP };       // MAP_*: only the parts' maps are formed
 
-// f and 1 - f, both to full relative precision; f is exactly 1 or 0 for an infinite gate.
+// f and 1 - f, both to full relative precision; f is exactly 1 or 0 for an infinite gate, and both are NaN for one that is none.
 __device__ __forceinline__ void gate_of(float g, float& f, float& rest) {
     const float e = __expf(-fabsf(g)), s = __fdividef(1.f, 1.f + e), t = e * s;
     f = g < 0.f ? t : s;
     rest = g < 0.f ? s : t;
-    if (g != g) f = rest = g;
 }
 
 __device__ __forceinline__ long long valid_steps(const Args& a, long long batch) {

@@ -99,31 +99,32 @@ static cudaError_t join(const Args& a, bool back, bool descending, cudaStream_t 
 }
 
 template <int V, bool REVERSE, bool STRIP, int KIND>
-static cudaError_t stream(const Args& a, dim3 grid, cudaStream_t s) {
+static cudaError_t stream(const Args& a, cudaStream_t s) {
+    constexpr int THREADS = KIND == VJP ? VJP_THREADS : STREAM_THREADS;
+    const long long blocks = STRIP ? a.batch * a.channels * ceil_div(a.inner, THREADS * V) : ceil_div(a.rows / V, THREADS);
+    const dim3 grid((unsigned)blocks, (unsigned)a.parts), block(THREADS);
     if constexpr (KIND == VJP) {
         constexpr auto KERNEL = stream_vjp<T, V, REVERSE, STRIP>;
         const cudaError_t e = ensure_smem(KERNEL, vjp_smem<T, V, STRIP>(), kernel_state<KERNEL>);
         if (e != cudaSuccess) return e;
-        SCAN_LAUNCH(KERNEL, grid, dim3(STREAM_THREADS), (size_t)vjp_smem<T, V, STRIP>(), s, a);
+        SCAN_LAUNCH(KERNEL, grid, block, (size_t)vjp_smem<T, V, STRIP>(), s, a);
     } else {
         constexpr auto KERNEL = stream_kernel<T, V, REVERSE, STRIP, KIND>;
         const cudaError_t e = ensure_smem(KERNEL, stream_smem<T, V, STRIP>(), kernel_state<KERNEL>);
         if (e != cudaSuccess) return e;
-        SCAN_LAUNCH(KERNEL, grid, dim3(STREAM_THREADS), (size_t)stream_smem<T, V, STRIP>(), s, a);
+        SCAN_LAUNCH(KERNEL, grid, block, (size_t)stream_smem<T, V, STRIP>(), s, a);
     }
     return cudaSuccess;
 }
 
 template <int V, bool REVERSE, bool STRIP, bool BACK>
 static cudaError_t streams(const Args& a, cudaStream_t s) {
-    const long long blocks = STRIP ? a.batch * a.channels * ceil_div(a.inner, STREAM_THREADS * V) : ceil_div(a.rows / V, STREAM_THREADS);
-    const dim3 grid((unsigned)blocks, (unsigned)a.parts);
     cudaError_t e;
     if (a.parts > 1) {
-        if ((e = stream<V, REVERSE, STRIP, BACK ? MAP_VJP : MAP_FORWARD>(a, grid, s)) != cudaSuccess) return e;
+        if ((e = stream<V, REVERSE, STRIP, BACK ? MAP_VJP : MAP_FORWARD>(a, s)) != cudaSuccess) return e;
         if ((e = join(a, BACK, BACK, s)) != cudaSuccess) return e;
     }
-    return stream<V, REVERSE, STRIP, BACK ? VJP : FORWARD>(a, grid, s);
+    return stream<V, REVERSE, STRIP, BACK ? VJP : FORWARD>(a, s);
 }
 
 template <bool REVERSE, bool BACK>

@@ -42,11 +42,24 @@ struct Args {
 
 enum { MAP_FORWARD, MAP_VJP, FORWARD, VJP };       // MAP_*: only the parts' maps are formed
 
-// f and 1 - f, both to full relative precision; f is exactly 1 or 0 for an infinite gate, and both are NaN for one that is none.
+// f and 1 - f, both to full relative precision, from e = exp(-gate): f = 1 / (1 + e), 1 - f = e f where e <= 1, the difference where
+// not (there it is exact, and holds for e = infinity).  f is exactly 1 or 0 for an infinite gate; both are NaN for one that is NaN.
+// Two at a time: sums and products of pairs take one instruction.
+using prior::fma2;
+using prior::Two;
+__device__ __forceinline__ float exp2_of(float x) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
+__device__ __forceinline__ float inverse_of(float x) { float r; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
+__device__ __forceinline__ void gates_of(Two g, Two& f, Two& rest) {
+    const Two x = g * Two(-1.4426950408889634f);
+    const Two e(exp2_of(x.lo()), exp2_of(x.hi())), d = e + Two(1.f);
+    f = Two(inverse_of(d.lo()), inverse_of(d.hi()));
+    const Two p = e * f, q = fma2(f, Two(-1.f), Two(1.f));
+    rest = Two(e.lo() > 1.f ? q.lo() : p.lo(), e.hi() > 1.f ? q.hi() : p.hi());
+}
 __device__ __forceinline__ void gate_of(float g, float& f, float& rest) {
-    const float e = __expf(-fabsf(g)), s = __fdividef(1.f, 1.f + e), t = e * s;
-    f = g < 0.f ? t : s;
-    rest = g < 0.f ? s : t;
+    const float e = exp2_of(g * -1.4426950408889634f);
+    f = inverse_of(1.f + e);
+    rest = e > 1.f ? 1.f - f : e * f;
 }
 
 __device__ __forceinline__ long long valid_steps(const Args& a, long long batch) {

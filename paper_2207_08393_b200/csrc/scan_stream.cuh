@@ -14,7 +14,7 @@
 namespace gleam {
 namespace scan {
 
-constexpr int STREAM_THREADS = 128;
+constexpr int STREAM_THREADS = 64, VJP_THREADS = 128;        // of a block
 constexpr int CHUNK = 8;                   // steps between saved states: what a VJP holds at a time
 constexpr int BATCH = 4, DEPTH = 4;        // steps of a copy group, and groups of the ring (forward)
 
@@ -34,11 +34,38 @@ __device__ __forceinline__ void copy_async(uint32_t to, const void* from) {
 __device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int LEFT> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
 
+__device__ __forceinline__ Two pair_of(const float* p) { return Two(p[0], p[1]); }
+__device__ __forceinline__ Two pair_of(const __half* p) { const float2 f = __half22float2(*reinterpret_cast<const __half2*>(p)); return Two(f.x, f.y); }
+__device__ __forceinline__ Two pair_of(const __nv_bfloat16* p) {
+    const uint32_t w = *reinterpret_cast<const uint32_t*>(p);
+    return Two(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+}
+__device__ __forceinline__ void round_pair(float* p, Two v) { p[0] = v.lo(); p[1] = v.hi(); }
+__device__ __forceinline__ void round_pair(__half* p, Two v) { *reinterpret_cast<__half2*>(p) = __floats2half2_rn(v.lo(), v.hi()); }
+__device__ __forceinline__ void round_pair(__nv_bfloat16* p, Two v) { *reinterpret_cast<__nv_bfloat162*>(p) = __floats2bfloat162_rn(v.lo(), v.hi()); }
+
+// Steps n = 0, 1, ... count - 1 of a part are steps t0 + n dt of the array; those from `first` on, `there` of them, are inside the
+// example's length.
+struct Span {
+    int count, first, there;
+    __device__ __forceinline__ bool has(int n) const { return (uint32_t)(n - first) < (uint32_t)there; }
+};
+__device__ __forceinline__ Span span_of(long long t0, int dt, int count, long long valid) {
+    Span s{count, 0, 0};
+    if (dt > 0) {
+        s.there = (int)(valid - t0 < 0 ? 0 : valid - t0 < count ? valid - t0 : count);
+    } else {
+        s.first = (int)(t0 - valid + 1 < 0 ? 0 : t0 - valid + 1 < count ? t0 - valid + 1 : count);
+        s.there = count - s.first;
+    }
+    return s;
+}
+
 // The chains of a block and a thread, and how rows of them pass through shared memory.
-template <class T, int V, bool STRIP>
+template <class T, int V, bool STRIP, int THREADS>
 struct Rows {
-    static constexpr int BYTES = V * sizeof(T), WIDTH = STREAM_THREADS * V;
-    static constexpr int SLOT = STREAM_THREADS * BYTES + (STRIP ? 16 : 0);       // bytes of a row in shared memory
+    static constexpr int BYTES = V * sizeof(T), WIDTH = THREADS * V;
+    static constexpr int SLOT = THREADS * BYTES + (STRIP ? 16 : 0);       // bytes of a row in shared memory
     long long row, batch;                    // the thread's first chain, its example
     long long at_batch, at_channel, at_i;    // ... (strips: the block's first chain)
     int there;                               // chains of the strip; private: whether there are any
@@ -50,7 +77,7 @@ struct Rows {
             there = (int)(a.inner - first < WIDTH ? a.inner - first : WIDTH);
             row = u * a.inner + first + threadIdx.x;
         } else {
-            row = ((long long)blockIdx.x * STREAM_THREADS + threadIdx.x) * V;
+            row = ((long long)blockIdx.x * THREADS + threadIdx.x) * V;
             there = row < a.rows;
             if (a.rows < (1ll << 32)) {
                 const uint32_t n = (uint32_t)a.inner, c = (uint32_t)a.channels, u = (uint32_t)row / n;
@@ -63,7 +90,7 @@ struct Rows {
         batch = at_batch;
     }
     template <class P> __device__ __forceinline__ P* at(P* base, const Strides& s) const { return base + (at_batch * s.batch + at_channel * s.channel + at_i); }
-    __device__ __forceinline__ bool has(int j) const { return STRIP ? (int)threadIdx.x + j * STREAM_THREADS < there : true; }
+    __device__ __forceinline__ bool has(int j) const { return STRIP ? (int)threadIdx.x + j * THREADS < there : true; }
 
     // private: the thread's piece of a row
     __device__ __forceinline__ void copy(uint32_t slot, const T* from) const { copy_async<BYTES>(slot + threadIdx.x * BYTES, from); }
@@ -80,47 +107,53 @@ struct Rows {
         for (int e = 0; e < 16; e += sizeof(T))
             if (x + e >= first && x + e < stop) *reinterpret_cast<T*>(slot + 16 * p + e) = *reinterpret_cast<const T*>(x + e);
     }
-    __device__ __forceinline__ void read(const unsigned char* slot, const T* from, float (&v)[V]) const {
+    __device__ __forceinline__ void read(const unsigned char* slot, const T* from, Two (&v)[V / 2]) const {
         if (STRIP) {
-            const T* s = reinterpret_cast<const T*>(slot + ((uintptr_t)from & 15)) + threadIdx.x;
+            const T* s = reinterpret_cast<const T*>(slot + ((uint32_t)(uintptr_t)from & 15u)) + threadIdx.x;
 #pragma unroll
-            for (int j = 0; j < V; ++j) v[j] = to_float(s[j * STREAM_THREADS]);
+            for (int j = 0; j < V; j += 2) v[j / 2] = Two(to_float(s[j * THREADS]), to_float(s[(j + 1) * THREADS]));
         } else {
             const Piece<T, V> p = *reinterpret_cast<const Piece<T, V>*>(slot + threadIdx.x * BYTES);
 #pragma unroll
-            for (int j = 0; j < V; ++j) v[j] = to_float(p.e[j]);
+            for (int j = 0; j < V; j += 2) v[j / 2] = pair_of(p.e + j);
         }
     }
-    __device__ __forceinline__ void write(T* to, const float (&v)[V]) const {
+    __device__ __forceinline__ void write(T* to, const Two (&v)[V / 2]) const {
         if (STRIP) {
 #pragma unroll
             for (int j = 0; j < V; ++j)
-                if (has(j)) to[threadIdx.x + j * STREAM_THREADS] = from_float<T>(v[j]);
+                if (has(j)) to[threadIdx.x + j * THREADS] = from_float<T>(j & 1 ? v[j / 2].hi() : v[j / 2].lo());
         } else {
             Piece<T, V> p;
 #pragma unroll
-            for (int j = 0; j < V; ++j) p.e[j] = from_float<T>(v[j]);
+            for (int j = 0; j < V; j += 2) round_pair(p.e + j, v[j / 2]);
             *reinterpret_cast<Piece<T, V>*>(to) = p;
         }
     }
     // states of the thread's chains; a null array holds zeros
-    __device__ __forceinline__ void read_states(const float* p, float (&v)[V]) const {
+    __device__ __forceinline__ void read_states(const float* p, Two (&to)[V / 2]) const {
+        float v[V];
 #pragma unroll
         for (int j = 0; j < V; ++j) v[j] = 0.f;
-        if (!p) return;
-        if (STRIP) {
+        if (!p) {
+        } else         if (STRIP) {
 #pragma unroll
-            for (int j = 0; j < V; ++j) if (has(j)) v[j] = p[row + j * STREAM_THREADS];
+            for (int j = 0; j < V; ++j) if (has(j)) v[j] = p[row + j * THREADS];
         } else {
             const Piece<float, (V > 4 ? 4 : V)>* q = reinterpret_cast<const Piece<float, (V > 4 ? 4 : V)>*>(p + row);
 #pragma unroll
             for (int j = 0; j < V; ++j) v[j] = q[j / 4].e[j % 4];
         }
+#pragma unroll
+        for (int j = 0; j < V; j += 2) to[j / 2] = Two(v[j], v[j + 1]);
     }
-    __device__ __forceinline__ void write_states(float* p, const float (&v)[V]) const {
+    __device__ __forceinline__ void write_states(float* p, const Two (&of)[V / 2]) const {
+        float v[V];
+#pragma unroll
+        for (int j = 0; j < V; j += 2) { v[j] = of[j / 2].lo(); v[j + 1] = of[j / 2].hi(); }
         if (STRIP) {
 #pragma unroll
-            for (int j = 0; j < V; ++j) if (has(j)) p[row + j * STREAM_THREADS] = v[j];
+            for (int j = 0; j < V; ++j) if (has(j)) p[row + j * THREADS] = v[j];
         } else {
 #pragma unroll
             for (int k = 0; k < V; k += 4) {
@@ -133,91 +166,98 @@ struct Rows {
     }
 };
 
-template <class T, int V, bool STRIP> constexpr int stream_smem() { return 2 * BATCH * DEPTH * Rows<T, V, STRIP>::SLOT; }
-template <class T, int V, bool STRIP> constexpr int vjp_smem() { return 3 * CHUNK * 2 * Rows<T, V, STRIP>::SLOT; }
+template <class T, int V, bool STRIP> constexpr int stream_smem() { return 2 * BATCH * DEPTH * Rows<T, V, STRIP, STREAM_THREADS>::SLOT; }
+template <class T, int V, bool STRIP> constexpr int vjp_smem() { return 3 * CHUNK * 2 * Rows<T, V, STRIP, VJP_THREADS>::SLOT; }
 
 // Forward, or the maps of parts for either direction (KIND: FORWARD, MAP_FORWARD, MAP_VJP).
 template <class T, int V, bool REVERSE, bool STRIP, int KIND>
 __global__ void __launch_bounds__(STREAM_THREADS) stream_kernel(const __grid_constant__ Args a) {
     extern __shared__ __align__(16) unsigned char ring[];
     grid_dependency_wait();
-    using R = Rows<T, V, STRIP>;
+    using R = Rows<T, V, STRIP, STREAM_THREADS>;
     constexpr bool MAPS = KIND != FORWARD, BACK = KIND == MAP_VJP;
+    constexpr int P = V / 2, dt = BACK != REVERSE ? -1 : 1;
     R c;
     c.find(a);
     if (!STRIP && !c.there) return;
-    const Strides& so = BACK ? a.sdy : a.sx;
-    const T* gate = c.at(static_cast<const T*>(a.gate), a.sgate);
-    const T* other = c.at(static_cast<const T*>(BACK ? a.dy : a.x), so);
-    T* y = MAPS ? nullptr : c.at(static_cast<T*>(a.y), a.sy);
-    const long long valid = valid_steps(a, c.batch), part = blockIdx.y, begin = part * a.part, end = begin + a.part < a.steps ? begin + a.part : a.steps;
-    // step n of the part, in the order in which it is taken, is t0 + n dt of the array
-    constexpr int dt = BACK != REVERSE ? -1 : 1;
+    const long long part = blockIdx.y, begin = part * a.part, end = begin + a.part < a.steps ? begin + a.part : a.steps;
     const long long q0 = BACK ? end - 1 : begin, t0 = REVERSE ? a.steps - 1 - q0 : q0;
-    const int count = (int)(end - begin);
-    float h[V], prod[V];
+    const Span span = span_of(t0, dt, (int)(end - begin), valid_steps(a, c.batch));
+    const Strides& so = BACK ? a.sdy : a.sx;
+    const T* gate = c.at(static_cast<const T*>(a.gate), a.sgate) + t0 * a.sgate.step;
+    const T* other = c.at(static_cast<const T*>(BACK ? a.dy : a.x), so) + t0 * so.step;
+    T* y = MAPS ? nullptr : c.at(static_cast<T*>(a.y), a.sy) + t0 * a.sy.step;
+    const long long gate_step = dt * a.sgate.step, other_step = dt * so.step, y_step = dt * a.sy.step;
+    Two h[P], prod[P];
 #pragma unroll
-    for (int j = 0; j < V; ++j) { h[j] = 0.f; prod[j] = 1.f; }
+    for (int j = 0; j < P; ++j) { h[j] = Two(0.f); prod[j] = Two(1.f); }
     if (!MAPS) c.read_states(a.parts > 1 ? a.maps_b + part * a.rows : a.state, h);
 
-    auto slot = [&](int n, int array) { return ring + (((n / BATCH) % DEPTH * BATCH + n % BATCH) * 2 + array) * R::SLOT; };
-    auto fetch = [&](int n0) {
+    // group g of BATCH steps: slots (g mod DEPTH, step, array)
+    const T* next_gate = gate;
+    const T* next_other = other;
+    auto fetch = [&](int group) {
+        unsigned char* slots = ring + group % DEPTH * (2 * BATCH * R::SLOT);
+        const int n0 = group * BATCH;
         if (STRIP) {
             const int pieces = R::pieces();
             for (int k = threadIdx.x; k < 2 * BATCH * pieces; k += STREAM_THREADS) {
-                const int row = k / pieces, n = n0 + (row >> 1), array = row & 1;
-                const long long t = t0 + (long long)n * dt;
-                if (n < count && t < valid) c.copy_piece(a, slot(n, array), array ? other + t * so.step : gate + t * a.sgate.step, k - row * pieces);
+                const int row = k / pieces, n = row >> 1, array = row & 1;
+                if (span.has(n0 + n)) c.copy_piece(a, slots + row * R::SLOT, array ? next_other + n * other_step : next_gate + n * gate_step, k - row * pieces);
             }
+            next_gate += BATCH * gate_step; next_other += BATCH * other_step;
         } else {
+            const uint32_t at = (uint32_t)__cvta_generic_to_shared(slots);
 #pragma unroll
             for (int k = 0; k < BATCH; ++k) {
-                const long long t = t0 + (long long)(n0 + k) * dt;
-                if (n0 + k < count && t < valid) {
-                    c.copy((uint32_t)__cvta_generic_to_shared(slot(n0 + k, 0)), gate + t * a.sgate.step);
-                    c.copy((uint32_t)__cvta_generic_to_shared(slot(n0 + k, 1)), other + t * so.step);
+                if (span.has(n0 + k)) {
+                    c.copy(at + 2 * k * R::SLOT, next_gate);
+                    c.copy(at + (2 * k + 1) * R::SLOT, next_other);
                 }
+                next_gate += gate_step; next_other += other_step;
             }
         }
         copies_end();
     };
-    for (int g = 0; g < DEPTH - 1; ++g) fetch(g * BATCH);
+    for (int g = 0; g < DEPTH - 1; ++g) fetch(g);
     int to_save = a.chunk;
     float* saved = !MAPS && a.saved ? a.saved + begin / a.chunk * a.rows : nullptr;
-    for (int n0 = 0; n0 < count; n0 += BATCH) {
-        fetch(n0 + (DEPTH - 1) * BATCH);
+    for (int n0 = 0, group = 0; n0 < span.count; n0 += BATCH, ++group) {
+        fetch(group + DEPTH - 1);
         copies_wait<DEPTH - 1>();
         if (STRIP) __syncthreads();
+        const unsigned char* slots = ring + group % DEPTH * (2 * BATCH * R::SLOT);
 #pragma unroll
         for (int k = 0; k < BATCH; ++k) {
             const int n = n0 + k;
-            const long long t = t0 + (long long)n * dt;
-            if (n >= count) break;
-            float out[V];
-            if (t < valid) {
-                float g[V], u[V];
-                c.read(slot(n, 0), gate + t * a.sgate.step, g);
-                c.read(slot(n, 1), other + t * so.step, u);
+            if (n >= span.count) break;
+            Two out[P];
+            if (span.has(n)) {
+                Two g[P], u[P];
+                c.read(slots + 2 * k * R::SLOT, gate, g);
+                c.read(slots + (2 * k + 1) * R::SLOT, other, u);
 #pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    float f, rest;
-                    gate_of(g[j], f, rest);
-                    h[j] = BACK ? f * (h[j] + u[j]) : fmaf(f, h[j], rest * u[j]);
-                    if (MAPS) prod[j] *= f;
+                for (int j = 0; j < P; ++j) {
+                    Two f, rest;
+                    gates_of(g[j], f, rest);
+                    h[j] = BACK ? f * (h[j] + u[j]) : fma2(f, h[j], rest * u[j]);
+                    if (MAPS) prod[j] = prod[j] * f;
                     out[j] = h[j];
                 }
             } else {
 #pragma unroll
-                for (int j = 0; j < V; ++j) out[j] = 0.f;
+                for (int j = 0; j < P; ++j) out[j] = Two(0.f);
             }
             if (!MAPS) {
-                c.write(y + t * a.sy.step, out);
+                c.write(y, out);
+                y += y_step;
                 if (--to_save == 0) {
                     to_save = a.chunk;
                     if (saved && begin + n + 1 < a.steps) c.write_states(saved, h);
                     if (saved) saved += a.rows;
                 }
             }
+            if (STRIP) { gate += gate_step; other += other_step; }      // their low bits say where a row lies in its slot
         }
         if (STRIP) __syncthreads();
     }
@@ -231,96 +271,104 @@ __global__ void __launch_bounds__(STREAM_THREADS) stream_kernel(const __grid_con
 
 // VJP: chunk by chunk from the part's end, the next chunk on its way.  The states before each step come from the saved one.
 template <class T, int V, bool REVERSE, bool STRIP>
-__global__ void __launch_bounds__(STREAM_THREADS, 3) stream_vjp(const __grid_constant__ Args a) {
+__global__ void __launch_bounds__(VJP_THREADS, 3) stream_vjp(const __grid_constant__ Args a) {
     extern __shared__ __align__(16) unsigned char ring[];
     grid_dependency_wait();
-    using R = Rows<T, V, STRIP>;
+    using R = Rows<T, V, STRIP, VJP_THREADS>;
+    constexpr int P = V / 2, dt = REVERSE ? -1 : 1;
     R c;
     c.find(a);
     if (!STRIP && !c.there) return;
-    const T* gate = c.at(static_cast<const T*>(a.gate), a.sgate);
-    const T* x = c.at(static_cast<const T*>(a.x), a.sx);
-    const T* dy = c.at(static_cast<const T*>(a.dy), a.sdy);
-    T* dx = c.at(static_cast<T*>(a.dx), a.sdx);
-    T* dg = c.at(static_cast<T*>(a.dg), a.sdg);
-    const long long valid = valid_steps(a, c.batch), part = blockIdx.y, begin = part * a.part, end = begin + a.part < a.steps ? begin + a.part : a.steps;
-    auto step = [&](long long q) { return REVERSE ? a.steps - 1 - q : q; };
-    auto slot = [&](int buffer, int k, int array) { return ring + ((buffer * CHUNK + k) * 3 + array) * R::SLOT; };
-    auto fetch = [&](long long q0, int buffer) {
-        if (q0 >= begin) {
-            const int count = (int)(end - q0 < a.chunk ? end - q0 : a.chunk);
+    const long long part = blockIdx.y, begin = part * a.part, end = begin + a.part < a.steps ? begin + a.part : a.steps;
+    const int last = (int)((end - begin - 1) / a.chunk) * a.chunk;                   // the part's last chunk begins there
+    const long long t0 = REVERSE ? a.steps - 1 - begin : begin;
+    const Span span = span_of(t0, dt, (int)(end - begin), valid_steps(a, c.batch));
+    // all pointers stand at the chunk's first step; copies are one chunk ahead
+    const T* gate = c.at(static_cast<const T*>(a.gate), a.sgate) + (t0 + dt * (long long)last) * a.sgate.step;
+    const T* x = c.at(static_cast<const T*>(a.x), a.sx) + (t0 + dt * (long long)last) * a.sx.step;
+    const T* dy = c.at(static_cast<const T*>(a.dy), a.sdy) + (t0 + dt * (long long)last) * a.sdy.step;
+    T* dx = c.at(static_cast<T*>(a.dx), a.sdx) + (t0 + dt * (long long)last) * a.sdx.step;
+    T* dg = c.at(static_cast<T*>(a.dg), a.sdg) + (t0 + dt * (long long)last) * a.sdg.step;
+    const long long gate_step = dt * a.sgate.step, x_step = dt * a.sx.step, dy_step = dt * a.sdy.step, dx_step = dt * a.sdx.step, dg_step = dt * a.sdg.step;
+    auto fetch = [&](int n0, int buffer, const T* g, const T* u, const T* d) {
+        if (n0 >= 0) {
+            unsigned char* slots = ring + buffer * (3 * CHUNK * R::SLOT);
+            const int count = span.count - n0 < a.chunk ? span.count - n0 : a.chunk;
             if (STRIP) {
                 const int pieces = R::pieces();
-                for (int i = threadIdx.x; i < 3 * count * pieces; i += STREAM_THREADS) {
+                for (int i = threadIdx.x; i < 3 * count * pieces; i += VJP_THREADS) {
                     const int row = i / pieces, k = row / 3, array = row - k * 3;
-                    const long long t = step(q0 + k);
-                    if (t < valid) c.copy_piece(a, slot(buffer, k, array), array == 0 ? gate + t * a.sgate.step : array == 1 ? x + t * a.sx.step : dy + t * a.sdy.step, i - row * pieces);
+                    if (span.has(n0 + k)) c.copy_piece(a, slots + row * R::SLOT, array == 0 ? g + k * gate_step : array == 1 ? u + k * x_step : d + k * dy_step, i - row * pieces);
                 }
             } else {
+                const uint32_t at = (uint32_t)__cvta_generic_to_shared(slots);
 #pragma unroll
                 for (int k = 0; k < CHUNK; ++k) {
-                    const long long t = step(q0 + k);
-                    if (k < count && t < valid) {
-                        c.copy((uint32_t)__cvta_generic_to_shared(slot(buffer, k, 0)), gate + t * a.sgate.step);
-                        c.copy((uint32_t)__cvta_generic_to_shared(slot(buffer, k, 1)), x + t * a.sx.step);
-                        c.copy((uint32_t)__cvta_generic_to_shared(slot(buffer, k, 2)), dy + t * a.sdy.step);
+                    if (k < count && span.has(n0 + k)) {
+                        c.copy(at + 3 * k * R::SLOT, g);
+                        c.copy(at + (3 * k + 1) * R::SLOT, u);
+                        c.copy(at + (3 * k + 2) * R::SLOT, d);
                     }
+                    g += gate_step; u += x_step; d += dy_step;
                 }
             }
         }
         copies_end();
     };
-    float back[V];
+    Two back[P];
     c.read_states(a.parts > 1 ? a.maps_b + part * a.rows : a.dlast, back);
-    const long long from = begin + (end - begin - 1) / a.chunk * a.chunk;
+    fetch(last, 0, gate, x, dy);
     int buffer = 0;
-    fetch(from, 0);
-    for (long long q0 = from; q0 >= begin; q0 -= a.chunk, buffer ^= 1) {
-        float h[V];
-        c.read_states(q0 > 0 ? a.saved + (q0 / a.chunk - 1) * a.rows : a.state, h);
-        fetch(q0 - a.chunk, buffer ^ 1);
+    for (int n0 = last; n0 >= 0; n0 -= a.chunk, buffer ^= 1) {
+        Two h[P];
+        const long long chunk = (begin + n0) / a.chunk;
+        c.read_states(chunk > 0 ? a.saved + (chunk - 1) * a.rows : a.state, h);
+        fetch(n0 - a.chunk, buffer ^ 1, gate - a.chunk * gate_step, x - a.chunk * x_step, dy - a.chunk * dy_step);
         copies_wait<1>();
         if (STRIP) __syncthreads();
-        const int count = (int)(end - q0 < a.chunk ? end - q0 : a.chunk);
-        float f[CHUNK][V], rest[CHUNK][V], w[CHUNK][V];               // w: h_(t-1) - x_t
+        const unsigned char* slots = ring + buffer * (3 * CHUNK * R::SLOT);
+        const int count = span.count - n0 < a.chunk ? span.count - n0 : a.chunk;
+        Two f[CHUNK][P], rest[CHUNK][P], w[CHUNK][P];                 // w: h_(t-1) - x_t
 #pragma unroll
         for (int k = 0; k < CHUNK; ++k) {
-            const long long t = step(q0 + k);
-            if (k < count && t < valid) {
-                float g[V], u[V];
-                c.read(slot(buffer, k, 0), gate + t * a.sgate.step, g);
-                c.read(slot(buffer, k, 1), x + t * a.sx.step, u);
+            if (k < count && span.has(n0 + k)) {
+                Two g[P], u[P];
+                c.read(slots + 3 * k * R::SLOT, gate + k * gate_step, g);
+                c.read(slots + (3 * k + 1) * R::SLOT, x + k * x_step, u);
 #pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    gate_of(g[j], f[k][j], rest[k][j]);
-                    w[k][j] = h[j] - u[j];
-                    h[j] = fmaf(f[k][j], h[j], rest[k][j] * u[j]);
+                for (int j = 0; j < P; ++j) {
+                    gates_of(g[j], f[k][j], rest[k][j]);
+                    w[k][j] = fma2(u[j], Two(-1.f), h[j]);
+                    h[j] = fma2(f[k][j], h[j], rest[k][j] * u[j]);
                 }
             }
         }
+        T* to_x = dx + (count - 1) * dx_step;
+        T* to_g = dg + (count - 1) * dg_step;
 #pragma unroll
         for (int k = CHUNK - 1; k >= 0; --k) {
             if (k >= count) continue;
-            const long long t = step(q0 + k);
-            float ox[V], og[V];
-            if (t < valid) {
-                float d[V];
-                c.read(slot(buffer, k, 2), dy + t * a.sdy.step, d);
+            Two ox[P], og[P];
+            if (span.has(n0 + k)) {
+                Two d[P];
+                c.read(slots + (3 * k + 2) * R::SLOT, dy + k * dy_step, d);
 #pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    d[j] += back[j];
+                for (int j = 0; j < P; ++j) {
+                    d[j] = d[j] + back[j];
                     back[j] = d[j] * f[k][j];
                     ox[j] = d[j] * rest[k][j];
                     og[j] = ox[j] * f[k][j] * w[k][j];
                 }
             } else {
 #pragma unroll
-                for (int j = 0; j < V; ++j) { ox[j] = 0.f; og[j] = 0.f; }
+                for (int j = 0; j < P; ++j) ox[j] = og[j] = Two(0.f);
             }
-            c.write(dx + t * a.sdx.step, ox);
-            c.write(dg + t * a.sdg.step, og);
+            c.write(to_x, ox);
+            c.write(to_g, og);
+            to_x -= dx_step; to_g -= dg_step;
         }
         if (STRIP) __syncthreads();
+        gate -= a.chunk * gate_step; x -= a.chunk * x_step; dy -= a.chunk * dy_step; dx -= a.chunk * dx_step; dg -= a.chunk * dg_step;
     }
     if (a.dstate && begin == 0) c.write_states(a.dstate, back);
 }

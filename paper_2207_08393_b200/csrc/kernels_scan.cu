@@ -44,19 +44,21 @@ static void plan(Args& a, long long* saved, long long* scratch) {
         threads = a.rows / WIDE + 1;
         *saved = (units - 1) * a.rows;
     } else {
+        if (a.steps <= SHORT_STEPS<T>) return;
         a.run = run_rows(a.rows, a.steps, TILE<T>);
         a.chunk = TILE<T>;
-        units = ceil_div(a.steps, a.chunk);
-        threads = 32 * a.rows;
-        *saved = ceil_div(a.rows, a.run) * ceil_div(a.run * a.steps, a.chunk);
+        units = run_tiles<T>(a.run, a.steps);
+        threads = 16 * a.rows;                       // half a warp: series take twice the warps of columns, a tile's shuffles are slow
+        *saved = ceil_div(a.rows, a.run) * units;
     }
     const long long wanted = SMS * 512;
     if (a.run == 1 && units >= 4 && threads < wanted / 2) {
         long long parts = wanted / threads;
         if (parts > units / 2) parts = units / 2;
         if (parts > 4096) parts = 4096;
-        a.part = ceil_div(units, parts) * a.chunk;
-        a.parts = (int)ceil_div(a.steps, a.part);
+        const long long each = ceil_div(units, parts);
+        a.part = each * a.chunk;
+        a.parts = (int)ceil_div(units, each);
     }
     if (a.parts == 1) a.part = a.steps;
     else *scratch = 2 * ceil_div(a.parts * a.rows, 64) * 64;
@@ -76,9 +78,8 @@ static bool wide(const Args& a, int v, std::initializer_list<Array> arrays, std:
     return true;
 }
 
-// Whether the steps lie without gaps from chain to chain, with runs and parts that begin at 16 bytes.
+// Whether the steps lie without gaps from chain to chain, from 16 bytes on.
 static bool dense(const Args& a, std::initializer_list<Array> arrays) {
-    if (a.run == 1 && a.rows > 1 && a.steps % ROW_V<T>) return false;
     for (const Array& u : arrays) {
         if (!u.p) continue;
         if ((uintptr_t)u.p % 16 || (a.steps > 1 && u.s->step != 1) || (a.channels > 1 && u.s->channel != a.steps) ||
@@ -141,17 +142,29 @@ static cudaError_t columns(const Args& a, cudaStream_t s) {
     return cudaSuccess;
 }
 
-template <bool REVERSE, bool DENSE, bool BACK>
-static cudaError_t rows(const Args& a, cudaStream_t s) {
-    const long long warps = a.run > 1 ? ceil_div(a.rows, a.run) : a.rows * a.parts;
+template <bool REVERSE, bool DENSE, bool SINGLE, bool BACK>
+static cudaError_t rows_of(const Args& a, cudaStream_t s) {
+    const long long warps = SINGLE ? a.rows * a.parts : ceil_div(a.rows, a.run);
     const dim3 grid((unsigned)ceil_div(warps, ROW_WARPS)), block(32 * ROW_WARPS);
-    if (a.parts > 1) {
-        SCAN_LAUNCH(rows_kernel<T, REVERSE, DENSE, BACK ? MAP_VJP : MAP_FORWARD>, grid, block, 0, s, a);
+    if (SINGLE && a.parts > 1) {
+        SCAN_LAUNCH(rows_kernel<T, REVERSE, DENSE, true, BACK ? MAP_VJP : MAP_FORWARD>, grid, block, 0, s, a);
         const cudaError_t e = join(a, BACK, BACK != REVERSE, s);                 // parts are numbered from the first step
         if (e != cudaSuccess) return e;
     }
-    SCAN_LAUNCH(rows_kernel<T, REVERSE, DENSE, BACK ? VJP : FORWARD>, grid, block, 0, s, a);
+    SCAN_LAUNCH(rows_kernel<T, REVERSE, DENSE, SINGLE, BACK ? VJP : FORWARD>, grid, block, 0, s, a);
     return cudaSuccess;
+}
+
+template <bool REVERSE, bool DENSE, bool BACK>
+static cudaError_t rows(const Args& a, cudaStream_t s) {
+    if (a.steps <= SHORT_STEPS<T>) {
+        constexpr auto KERNEL = short_kernel<T, REVERSE, DENSE, BACK ? VJP : FORWARD>;
+        const cudaError_t e = ensure_smem(KERNEL, short_smem<T, BACK ? VJP : FORWARD>(SHORT_STEPS<T>), kernel_state<KERNEL>);
+        if (e != cudaSuccess) return e;
+        SCAN_LAUNCH(KERNEL, dim3((unsigned)ceil_div(a.rows, SHORT_ROWS)), dim3(SHORT_ROWS), short_smem<T, BACK ? VJP : FORWARD>(a.steps), s, a);
+        return cudaSuccess;
+    }
+    return a.run == 1 ? rows_of<REVERSE, DENSE, true, BACK>(a, s) : rows_of<REVERSE, DENSE, false, BACK>(a, s);
 }
 
 template <bool BACK>

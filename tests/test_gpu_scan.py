@@ -63,11 +63,11 @@ def check(x, gate, dy, state, dlast, lengths=None, reverse=False, dim=2):
 
 
 # inner > 1: chunks of 16 steps; pieces of 8 bytes, or single chains where sizes are odd; parts where chains are few and long
-MAPS = [(1, 1, 1, 2), (1, 3, 20, 64), (2, 5, 16, 8), (2, 5, 17, 12), (3, 2, 33, 7), (1, 4, 21, 145), (2, 1, 1000, 6), (1, 1, 2049, 33),
+MAPS = [(1, 2, 21, 1025), (2, 1, 40, 259), (1, 1, 3000, 131), (3, 2, 9, 128), (1, 1, 1, 2), (1, 3, 20, 64), (2, 5, 16, 8), (2, 5, 17, 12), (3, 2, 33, 7), (1, 4, 21, 145), (2, 1, 1000, 6), (1, 1, 2049, 33),
         (2, 3, 65, 1026), (5, 1, 2, 2), (1, 40, 48, 1024)]
 # inner = 1: chains that share tiles, that fill some, that are cut into parts
 SERIES = [(1, 1, 1, 1), (1, 7, 1, 1), (1, 16, 20, 1), (3, 11, 21, 1), (2, 300, 64, 1), (1, 9, 255, 1), (1, 10, 256, 1), (2, 5, 257, 1), (1, 3, 4097, 1),
-          (1, 2, 20000, 1), (4, 1, 8192, 1), (2, 5000, 3, 1), (1, 1, 40001, 1), (1, 70, 600, 1)]
+          (1, 2, 20000, 1), (4, 1, 8192, 1), (2, 5000, 3, 1), (1, 1, 40001, 1), (1, 70, 600, 1), (1, 5, 33, 1), (3, 1, 65, 1), (2, 3, 1000, 1), (1, 33, 70, 1)]
 
 
 @pytest.mark.parametrize("dtype", list(TYPES))
@@ -83,7 +83,7 @@ def test_forward_and_vjp(shape, reverse, dtype):
 @pytest.mark.parametrize("reverse", [False, True])
 @pytest.mark.parametrize("shape,lengths", [
     ((3, 5, 21, 24), [21, 0, 7]), ((4, 2, 40, 9), [1, 40, 39, -5]), ((2, 1, 1000, 6), [999, 3]), ((3, 11, 21, 1), [20, 0, 21]), ((4, 3, 700, 1), [0, 699, 255, 1]),
-    ((2, 2, 9000, 1), [8999, 4097]), ((3, 40, 5, 1), [9, 2, 0])])
+    ((2, 2, 9000, 1), [8999, 4097]), ((3, 40, 5, 1), [9, 2, 0]), ((3, 2, 37, 257), [37, 8, 0]), ((2, 20, 70, 1), [69, 1]), ((2, 1, 77, 1), [0, 70])])
 def test_lengths(shape, lengths, reverse, dtype):
     """What is behind a length is not read: it holds NaN and infinities here."""
     x, gate, dy, state, dlast = inputs(shape, TYPES[dtype], 1)

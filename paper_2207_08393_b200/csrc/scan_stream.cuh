@@ -69,6 +69,7 @@ struct Rows {
     long long row, batch;                    // the thread's first chain, its example
     long long at_batch, at_channel, at_i;    // ... (strips: the block's first chain)
     int there;                               // chains of the strip; private: whether there are any
+    bool inside;                             // strips: they are as many as can be, and 16 bytes more of the row on both sides
 
     __device__ __forceinline__ void find(const Args& a) {
         if (STRIP) {
@@ -76,6 +77,7 @@ struct Rows {
             at_batch = u / a.channels; at_channel = u - at_batch * a.channels; at_i = first;
             there = (int)(a.inner - first < WIDTH ? a.inner - first : WIDTH);
             row = u * a.inner + first + threadIdx.x;
+            inside = first >= 16 && first + WIDTH + 16 <= a.inner;
         } else {
             row = ((long long)blockIdx.x * THREADS + threadIdx.x) * V;
             there = row < a.rows;
@@ -94,18 +96,23 @@ struct Rows {
 
     // private: the thread's piece of a row
     __device__ __forceinline__ void copy(uint32_t slot, const T* from) const { copy_async<BYTES>(slot + threadIdx.x * BYTES, from); }
-    // strips: piece p of those that the strip touches; what is not inside the row as a whole goes element by element
-    __device__ __forceinline__ static int pieces() { return (WIDTH * (int)sizeof(T) + 15) / 16 + 1; }
-    __device__ __forceinline__ void copy_piece(const Args& a, unsigned char* slot, const T* from, int p) const {
-        const uintptr_t first = (uintptr_t)from, begin = first - at_i * sizeof(T), end = begin + a.inner * sizeof(T), stop = first + there * sizeof(T);
-        const uintptr_t x = (first & ~(uintptr_t)15) + 16 * p;
-        if (x >= stop) return;
-        if (x >= begin && x + 16 <= end) {
-            copy_async<16>((uint32_t)__cvta_generic_to_shared(slot) + 16 * p, (const void*)x);
+    // strips: the 16-byte pieces that the strip touches in one row, by threads number `turn` of `turns`; what is not inside the row as a
+    // whole goes element by element
+    __device__ __forceinline__ void copy_row(const Args& a, unsigned char* slot, const T* from, int turn, int turns) const {
+        const uintptr_t first = (uintptr_t)from, stop = first + there * sizeof(T);
+        uintptr_t x = (first & ~(uintptr_t)15) + 16 * turn;
+        uint32_t to = (uint32_t)__cvta_generic_to_shared(slot) + 16 * turn;
+        if (inside) {
+            for (; x < stop; x += 16 * turns, to += 16 * turns) copy_async<16>(to, (const void*)x);
             return;
         }
-        for (int e = 0; e < 16; e += sizeof(T))
-            if (x + e >= first && x + e < stop) *reinterpret_cast<T*>(slot + 16 * p + e) = *reinterpret_cast<const T*>(x + e);
+        const uintptr_t begin = first - at_i * sizeof(T), end = begin + a.inner * sizeof(T);
+        for (unsigned char* s = slot + 16 * turn; x < stop; x += 16 * turns, to += 16 * turns, s += 16 * turns) {
+            if (x >= begin && x + 16 <= end) copy_async<16>(to, (const void*)x);
+            else
+                for (int e = 0; e < 16; e += sizeof(T))
+                    if (x + e >= first && x + e < stop) *reinterpret_cast<T*>(s + e) = *reinterpret_cast<const T*>(x + e);
+        }
     }
     __device__ __forceinline__ void read(const unsigned char* slot, const T* from, Two (&v)[V / 2]) const {
         if (STRIP) {
@@ -120,9 +127,15 @@ struct Rows {
     }
     __device__ __forceinline__ void write(T* to, const Two (&v)[V / 2]) const {
         if (STRIP) {
+            T* p = to + threadIdx.x;
+            if (inside) {
 #pragma unroll
-            for (int j = 0; j < V; ++j)
-                if (has(j)) to[threadIdx.x + j * THREADS] = from_float<T>(j & 1 ? v[j / 2].hi() : v[j / 2].lo());
+                for (int j = 0; j < V; ++j) p[j * THREADS] = from_float<T>(j & 1 ? v[j / 2].hi() : v[j / 2].lo());
+            } else {
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+                    if (has(j)) p[j * THREADS] = from_float<T>(j & 1 ? v[j / 2].hi() : v[j / 2].lo());
+            }
         } else {
             Piece<T, V> p;
 #pragma unroll
@@ -200,11 +213,9 @@ __global__ void __launch_bounds__(STREAM_THREADS) stream_kernel(const __grid_con
         unsigned char* slots = ring + group % DEPTH * (2 * BATCH * R::SLOT);
         const int n0 = group * BATCH;
         if (STRIP) {
-            const int pieces = R::pieces();
-            for (int k = threadIdx.x; k < 2 * BATCH * pieces; k += STREAM_THREADS) {
-                const int row = k / pieces, n = row >> 1, array = row & 1;
-                if (span.has(n0 + n)) c.copy_piece(a, slots + row * R::SLOT, array ? next_other + n * other_step : next_gate + n * gate_step, k - row * pieces);
-            }
+            constexpr int TURNS = STREAM_THREADS / (2 * BATCH);
+            const int row = threadIdx.x / TURNS, n = row >> 1;
+            if (span.has(n0 + n)) c.copy_row(a, slots + row * R::SLOT, row & 1 ? next_other + n * other_step : next_gate + n * gate_step, threadIdx.x % TURNS, TURNS);
             next_gate += BATCH * gate_step; next_other += BATCH * other_step;
         } else {
             const uint32_t at = (uint32_t)__cvta_generic_to_shared(slots);
@@ -295,11 +306,10 @@ __global__ void __launch_bounds__(VJP_THREADS, 3) stream_vjp(const __grid_consta
             unsigned char* slots = ring + buffer * (3 * CHUNK * R::SLOT);
             const int count = span.count - n0 < a.chunk ? span.count - n0 : a.chunk;
             if (STRIP) {
-                const int pieces = R::pieces();
-                for (int i = threadIdx.x; i < 3 * count * pieces; i += VJP_THREADS) {
-                    const int row = i / pieces, k = row / 3, array = row - k * 3;
-                    if (span.has(n0 + k)) c.copy_piece(a, slots + row * R::SLOT, array == 0 ? g + k * gate_step : array == 1 ? u + k * x_step : d + k * dy_step, i - row * pieces);
-                }
+                constexpr int TURNS = VJP_THREADS / (3 * CHUNK);
+                const int row = threadIdx.x / TURNS, k = row / 3, array = row - k * 3;
+                if (k < count && span.has(n0 + k))
+                    c.copy_row(a, slots + row * R::SLOT, array == 0 ? g + k * gate_step : array == 1 ? u + k * x_step : d + k * dy_step, threadIdx.x % TURNS, TURNS);
             } else {
                 const uint32_t at = (uint32_t)__cvta_generic_to_shared(slots);
 #pragma unroll

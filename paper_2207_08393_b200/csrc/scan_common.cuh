@@ -49,13 +49,17 @@ using prior::fma2;
 using prior::Two;
 __device__ __forceinline__ float exp2_of(float x) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
 __device__ __forceinline__ float inverse_of(float x) { float r; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
-__device__ __forceinline__ void gates_of(Two g, Two& f, Two& rest) {
+__device__ __forceinline__ Two exp_of_minus(Two g) {
     const Two x = g * Two(-1.4426950408889634f);
-    const Two e(exp2_of(x.lo()), exp2_of(x.hi())), d = e + Two(1.f);
+    return Two(exp2_of(x.lo()), exp2_of(x.hi()));
+}
+__device__ __forceinline__ void gates_from(Two e, Two& f, Two& rest) {
+    const Two d = e + Two(1.f);
     f = Two(inverse_of(d.lo()), inverse_of(d.hi()));
     const Two p = e * f, q = fma2(f, Two(-1.f), Two(1.f));
     rest = Two(e.lo() > 1.f ? q.lo() : p.lo(), e.hi() > 1.f ? q.hi() : p.hi());
 }
+__device__ __forceinline__ void gates_of(Two g, Two& f, Two& rest) { gates_from(exp_of_minus(g), f, rest); }
 __device__ __forceinline__ void gate_of(float g, float& f, float& rest) {
     const float e = exp2_of(g * -1.4426950408889634f);
     f = inverse_of(1.f + e);

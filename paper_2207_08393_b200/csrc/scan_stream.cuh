@@ -282,7 +282,7 @@ __global__ void __launch_bounds__(STREAM_THREADS) stream_kernel(const __grid_con
 
 // VJP: chunk by chunk from the part's end, the next chunk on its way.  The states before each step come from the saved one.
 template <class T, int V, bool REVERSE, bool STRIP>
-__global__ void __launch_bounds__(VJP_THREADS, 3) stream_vjp(const __grid_constant__ Args a) {
+__global__ void __launch_bounds__(VJP_THREADS, 4) stream_vjp(const __grid_constant__ Args a) {
     extern __shared__ __align__(16) unsigned char ring[];
     grid_dependency_wait();
     using R = Rows<T, V, STRIP, VJP_THREADS>;
@@ -338,7 +338,7 @@ __global__ void __launch_bounds__(VJP_THREADS, 3) stream_vjp(const __grid_consta
         if (STRIP) __syncthreads();
         const unsigned char* slots = ring + buffer * (3 * CHUNK * R::SLOT);
         const int count = span.count - n0 < a.chunk ? span.count - n0 : a.chunk;
-        Two f[CHUNK][P], rest[CHUNK][P], w[CHUNK][P];                 // w: h_(t-1) - x_t
+        Two e[CHUNK][P], w[CHUNK][P];            // exp(-gate), h_(t-1) - x_t: the gates once more cost less than 32 registers to keep them
 #pragma unroll
         for (int k = 0; k < CHUNK; ++k) {
             if (k < count && span.has(n0 + k)) {
@@ -347,9 +347,11 @@ __global__ void __launch_bounds__(VJP_THREADS, 3) stream_vjp(const __grid_consta
                 c.read(slots + (3 * k + 1) * R::SLOT, x + k * x_step, u);
 #pragma unroll
                 for (int j = 0; j < P; ++j) {
-                    gates_of(g[j], f[k][j], rest[k][j]);
+                    Two f, rest;
+                    e[k][j] = exp_of_minus(g[j]);
+                    gates_from(e[k][j], f, rest);
                     w[k][j] = fma2(u[j], Two(-1.f), h[j]);
-                    h[j] = fma2(f[k][j], h[j], rest[k][j] * u[j]);
+                    h[j] = fma2(f, h[j], rest * u[j]);
                 }
             }
         }
@@ -364,10 +366,12 @@ __global__ void __launch_bounds__(VJP_THREADS, 3) stream_vjp(const __grid_consta
                 c.read(slots + (3 * k + 2) * R::SLOT, dy + k * dy_step, d);
 #pragma unroll
                 for (int j = 0; j < P; ++j) {
+                    Two f, rest;
+                    gates_from(e[k][j], f, rest);
                     d[j] = d[j] + back[j];
-                    back[j] = d[j] * f[k][j];
-                    ox[j] = d[j] * rest[k][j];
-                    og[j] = ox[j] * f[k][j] * w[k][j];
+                    back[j] = d[j] * f;
+                    ox[j] = d[j] * rest;
+                    og[j] = ox[j] * f * w[k][j];
                 }
             } else {
 #pragma unroll

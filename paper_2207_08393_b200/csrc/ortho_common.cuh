@@ -13,10 +13,10 @@
 // to values of 2^-13.  The term a X is added in 32 bits.  Against 64 bits the result is as near as 32-bit products are, or nearer;
 // float16 or bfloat16 products without the second piece would be off by 1e-3 or 1e-2.
 //
-// Matrices are stored in blocks of 128 x 128 with zeros beyond their sides: a block is 32 KB of hi and 32 KB of lo, each two halves of 64
-// columns, a half 16 x 8 cores of 8 rows by 8 columns, a row of a core 16 bytes: the shape that the matrix instructions read, along
-// either side.  An operand's tile is then one run of up to 16 KB for a piece, or two of 8 KB where the sum runs over the block's rows: with runs
-// of 1 KB (cores of a block in plain order) the copies, not the products, took the time: 4 x 512 x 4608 89 us for A instead of 38.
+// Matrices are stored in blocks of 128 x 128 with zeros beyond their sides: a block is 32 KB of hi and 32 KB of lo, each as 16 x 16 cores
+// of 8 rows by 8 columns, a row of a core 16 bytes: the shape that the matrix instructions read, along either side.  An operand's tile
+// is one copy of 16 KB for a piece: half the rows lie in one run, half the columns in 16 runs of 1 KB, which a tiled copy takes at
+// once.  (With a copy for each run the copies, not the products, took the time: 4 x 512 x 4608, A: 89 us instead of 38.)
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -48,10 +48,14 @@ struct Args {
     unsigned char* x; unsigned char* y;            // X and its successor: (count, sblocks, lblocks) blocks
     unsigned char* g; unsigned char* p;            // A and P: (count, sblocks, sblocks) blocks
     float* part; int* status;
+    unsigned char* blocks;                         // all blocks of the workspace: what the tiled copies' map covers
 };
 
 // Byte of element (r, c) of a piece.
-__host__ __device__ __forceinline__ int core_at(int r, int c) { return ((c >> 6) * 128 + (r >> 3) * 8 + ((c >> 3) & 7)) * CORE + (r & 7) * 16 + (c & 7) * 2; }
+__host__ __device__ __forceinline__ int core_at(int r, int c) { return ((r >> 3) * 16 + (c >> 3)) * CORE + (r & 7) * 16 + (c & 7) * 2; }
+
+// A block's sums as 32-bit numbers in shared memory: rows of 128, their 16-byte pieces in an order that keeps 32 rows apart.
+__device__ __forceinline__ int sum_at(int r, int c) { return r * BLOCK + ((((c >> 2) ^ r) & 31) << 2) + (c & 3); }
 
 template <class T> __device__ __forceinline__ float load_at(const void* p, long long i) { return to_float(static_cast<const T*>(p)[i]); }
 template <class T> __device__ __forceinline__ void store_at(void* p, long long i, float v) { static_cast<T*>(p)[i] = from_float<T>(v); }

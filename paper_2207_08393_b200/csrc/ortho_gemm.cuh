@@ -26,12 +26,9 @@ constexpr int SUMS = 3;                                                 // hi hi
 template <int KIND> __host__ __device__ inline int steps_of(const Args& a) { return (int)(((KIND == GRAM ? a.L : a.S) + STEP - 1) / STEP); }
 template <int KIND> __host__ inline int tiles_of(const Args& a) { return KIND == GRAM || KIND == POLY ? a.sblocks * (a.sblocks + 1) / 2 : a.sblocks * a.lblocks; }
 
-// The sums as 32-bit numbers in shared memory: rows of 128, their 16-byte pieces in an order that keeps 32 rows apart.
-__device__ __forceinline__ int sum_at(int r, int c) { return r * BLOCK + ((((c >> 2) ^ r) & 31) << 2) + (c & 3); }
-
 // T: the type of results (LAST)
 template <int KIND, int RANKS, class T>
-__global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_constant__ Args a) {
+__global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap map) {
     extern __shared__ __align__(1024) unsigned char smem[];
     constexpr int ranks = RANKS, ITEMS = BLOCK * BLOCK / 8 / RANKS / GEMM_THREADS;     // eights of a row that a thread finishes
     constexpr bool SIDES = KIND == GRAM || KIND == POLY;               // both operands are rows of one matrix
@@ -68,29 +65,26 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
     bool failed = false;
 
     if (warp == 0 && lane == 0) {
-        // rows beyond the matrix are not copied where they are rows of the result: what stands there is not stored
-        const long long lrows = a.S - (long long)bi * BLOCK, rrows = a.S - (long long)bj * BLOCK;
-        const uint32_t lrun = (uint32_t)((lrows < BLOCK ? lrows + 7 : BLOCK) >> 3) * 1024, rrun = SIDES ? (uint32_t)((rrows < BLOCK ? rrows + 7 : BLOCK) >> 3) * 1024 : 8192;
+        // rows of 2 KB (eight rows of a block) from the first block to left's and right's
+        const long long lrow = (left - a.blocks) / 2048 + (long long)bi * lblocks * 32, rrow = (right - a.blocks) / 2048 + (long long)bj * lblocks * 32;
         for (int i = 0; i < count; ++i) {
             const int s = i % STAGES, k = first + i, kb = k >> 1, half = k & 1;
             if (i >= STAGES && !tc::barrier_wait(empty(s), (i / STAGES - 1) & 1)) { failed = true; break; }
             const uint32_t to = stages + s * STAGE_BYTES;
-            tc::barrier_expect(full(s), 2 * lrun + (SIDES ? one ? 0 : 2 * rrun : 4 * rrun));
+            tc::barrier_expect(full(s), one ? OPERAND_BYTES : STAGE_BYTES);
 #pragma unroll
             for (int piece = 0; piece < 2; ++piece) {
-                const uint32_t lo = piece * (OPERAND_BYTES / 2);
-                tc::bulk_copy(to + lo, left + ((long long)bi * lblocks + kb) * BLOCK_BYTES + piece * PIECE_BYTES + half * (PIECE_BYTES / 2), lrun, full(s));
+                const uint32_t at = to + piece * (OPERAND_BYTES / 2);
+                tc::tiled_copy(at, &map, half, (int)(lrow + kb * 32 + piece * 16), full(s));
                 if (SIDES) {
-                    if (!one) tc::bulk_copy(to + OPERAND_BYTES + lo, right + ((long long)bj * lblocks + kb) * BLOCK_BYTES + piece * PIECE_BYTES + half * (PIECE_BYTES / 2), rrun, full(s));
+                    if (!one) tc::tiled_copy(at + OPERAND_BYTES, &map, half, (int)(rrow + kb * 32 + piece * 16), full(s));
                 } else {
-                    // half the rows of both halves
-                    for (int h = 0; h < 2; ++h)
-                        tc::bulk_copy(to + OPERAND_BYTES + lo + h * 8192, right + ((long long)kb * a.lblocks + bj) * BLOCK_BYTES + piece * PIECE_BYTES + h * (PIECE_BYTES / 2) + half * 8192, 8192, full(s));
+                    tc::bulk_copy(at + OPERAND_BYTES, right + ((long long)kb * a.lblocks + bj) * BLOCK_BYTES + piece * PIECE_BYTES + half * (PIECE_BYTES / 2), OPERAND_BYTES / 2, full(s));
                 }
             }
         }
     } else if (warp == 1 && lane == 0) {
-        const uint32_t what = tc::instruction(SIDES ? BLOCK : BLOCK / 2, !SIDES);
+        const uint32_t what = tc::instruction(BLOCK, !SIDES);
         for (int i = 0; i < count; ++i) {
             const int s = i % STAGES;
             if (!tc::barrier_wait(full(s), (i / STAGES) & 1)) {
@@ -103,17 +97,13 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
             constexpr int HALF = OPERAND_BYTES / 2;                                 // from hi to lo
 #pragma unroll
             for (int q = 0; q < STEP / 16; ++q) {
-                // cores of left: 1024 bytes from one to the next along M, 128 along K; of right (!SIDES): 128 along N, 1024 along K, its halves of
-                // 64 columns apart
+                // cores of left: 1024 bytes from one to the next along M, 128 along K; of right (!SIDES): 128 along N, 2048 along K
                 const uint64_t lh = tc::descriptor(l + q * 256, 128, 1024), ll = tc::descriptor(l + HALF + q * 256, 128, 1024);
-#pragma unroll
-                for (int h = 0; h < (SIDES ? 1 : 2); ++h) {
-                    const uint64_t rh = SIDES ? tc::descriptor(r + q * 256, 128, 1024) : tc::descriptor(r + h * 8192 + q * 2048, 1024, 128);
-                    const uint64_t rl = SIDES ? tc::descriptor(r + HALF + q * 256, 128, 1024) : tc::descriptor(r + HALF + h * 8192 + q * 2048, 1024, 128);
-                    tc::product(sums + SUMS * BLOCK + h * 64, ll, rh, what, i > 0 || q > 0);
-                    tc::product(sums + SUMS * BLOCK + h * 64, lh, rl, what, true);
-                    tc::product(sums + i % SUMS * BLOCK + h * 64, lh, rh, what, i >= SUMS || q > 0);
-                }
+                const uint64_t rh = SIDES ? tc::descriptor(r + q * 256, 128, 1024) : tc::descriptor(r + q * 4096, 2048, 128);
+                const uint64_t rl = SIDES ? tc::descriptor(r + HALF + q * 256, 128, 1024) : tc::descriptor(r + HALF + q * 4096, 2048, 128);
+                tc::product(sums + SUMS * BLOCK, ll, rh, what, i > 0 || q > 0);
+                tc::product(sums + SUMS * BLOCK, lh, rl, what, true);
+                tc::product(sums + i % SUMS * BLOCK, lh, rh, what, i >= SUMS || q > 0);
             }
             tc::commit(empty(s));
         }
@@ -161,19 +151,24 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
     __syncthreads();
     if (warp == 0) tc::free_columns(sums, 512);
     if (failed) atomicOr(a.status, 1);
-    if (ranks > 1) tc::cluster_sync();
 
-    // four columns of a row, summed over the cluster in the order of its blocks
-    auto take = [&](int at) {
-        float4 f[RANKS];
+    // a cluster's blocks add a share of the rows each, lanes along a row as remote reads want it; these rows of a block's own sums are
+    // nobody else's
+    if (RANKS > 1) {
+        constexpr int SHARE = BLOCK / RANKS * (BLOCK / 4);
+        tc::cluster_sync();
+        for (int i = rank * SHARE + threadIdx.x; i < (rank + 1) * SHARE; i += GEMM_THREADS) {
+            float4 f[RANKS];
 #pragma unroll
-        for (int k = 0; k < RANKS; ++k) f[k] = RANKS > 1 ? tc::read_remote(base + 1024 + 4 * at, k) : *reinterpret_cast<const float4*>(sum + at);
+            for (int k = 0; k < RANKS; ++k) f[k] = tc::read_remote(base + 1024 + 16 * i, k);
 #pragma unroll
-        for (int k = 1; k < RANKS; ++k) { f[0].x += f[k].x; f[0].y += f[k].y; f[0].z += f[k].z; f[0].w += f[k].w; }
-        return f[0];
-    };
+            for (int k = 1; k < RANKS; ++k) { f[0].x += f[k].x; f[0].y += f[k].y; f[0].z += f[k].z; f[0].w += f[k].w; }
+            reinterpret_cast<float4*>(sum)[i] = f[0];
+        }
+        __syncthreads();
+    }
     auto take8 = [&](int r, int c, float (&v)[8]) {
-        const float4 f = take(sum_at(r, c)), g = take(sum_at(r, c + 4));
+        const float4 f = *reinterpret_cast<const float4*>(sum + sum_at(r, c)), g = *reinterpret_cast<const float4*>(sum + sum_at(r, c + 4));
         v[0] = f.x; v[1] = f.y; v[2] = f.z; v[3] = f.w; v[4] = g.x; v[5] = g.y; v[6] = g.z; v[7] = g.w;
     };
     auto blend = [&](const uint4& hi, const uint4& lo, float by, float (&v)[8], float times) {
@@ -205,26 +200,26 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
             put(to, row_of(k), col, v, rows, cols);
         }
         if (SIDES && !one) {
-            // the block on the other side of the diagonal
+            // the block on the other side of the diagonal: this block's rows are columns there
             const long long at = (square + (long long)bj * a.sblocks + bi) * BLOCK_BYTES;
+            constexpr int EIGHTS = BLOCK / 8 / RANKS;                      // of columns
+            auto mirror_row = [&](int k) { const int i = k * GEMM_THREADS + threadIdx.x; return (i & 7) + (i >> 3) / EIGHTS * 8; };
+            const int mirror_col = (rank * EIGHTS + (threadIdx.x >> 3) % EIGHTS) * 8;
             if (KIND == POLY) {
 #pragma unroll
                 for (int k = 0; k < ITEMS; ++k) {
-                    old_hi[k] = *reinterpret_cast<const uint4*>(a.g + at + core_at(row_of(k), col));
-                    old_lo[k] = *reinterpret_cast<const uint4*>(a.g + at + PIECE_BYTES + core_at(row_of(k), col));
+                    old_hi[k] = *reinterpret_cast<const uint4*>(a.g + at + core_at(mirror_row(k), mirror_col));
+                    old_lo[k] = *reinterpret_cast<const uint4*>(a.g + at + PIECE_BYTES + core_at(mirror_row(k), mirror_col));
                 }
             }
 #pragma unroll
             for (int k = 0; k < ITEMS; ++k) {
-                const int r = row_of(k);
+                const int r = mirror_row(k);
                 float v[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float4 f = take(sum_at(col + j, r) & ~3);
-                    v[j] = (r & 3) == 0 ? f.x : (r & 3) == 1 ? f.y : (r & 3) == 2 ? f.z : f.w;
-                }
+                for (int j = 0; j < 8; ++j) v[j] = sum[sum_at(mirror_col + j, r)];
                 if (KIND == POLY) blend(old_hi[k], old_lo[k], a.b, v, a.c);
-                put((KIND == GRAM ? a.g : a.p) + at, r, col, v, cols, rows);
+                put((KIND == GRAM ? a.g : a.p) + at, r, mirror_col, v, cols, rows);
             }
         }
     } else {
@@ -238,24 +233,25 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
         }
         __syncthreads();
         // lanes along what is contiguous
-        constexpr int AT_ONCE = 16;
-        void* out = a.out[m];
-        const int dr = a.tall ? 0 : GEMM_THREADS / BLOCK, dc = a.tall ? GEMM_THREADS / BLOCK : 0, along = threadIdx.x & (BLOCK - 1), across = threadIdx.x / BLOCK;
+        constexpr int AT_ONCE = 16, LINES = GEMM_THREADS / BLOCK;
         const long long s0 = (long long)bi * BLOCK, l0 = (long long)bj * BLOCK;
-        for (int i = 0; i < BLOCK * BLOCK / GEMM_THREADS; i += AT_ONCE) {
+        const int along = threadIdx.x & (BLOCK - 1), r1 = rows < BLOCK ? (int)rows : BLOCK, c1 = cols < BLOCK ? (int)cols : BLOCK;
+        const int limit = along < (a.tall ? r1 : c1) ? (a.tall ? c1 : r1) : 0;
+        T* out = static_cast<T*>(a.out[m]) + (a.tall ? l0 * a.cols + s0 : s0 * a.cols + l0) + along;
+        for (int line = threadIdx.x / BLOCK; line < limit; line += AT_ONCE * LINES) {
             float w[AT_ONCE];
 #pragma unroll
             for (int k = 0; k < AT_ONCE; ++k) {
-                const int r = a.tall ? along : across + (i + k) * dr, c = a.tall ? across + (i + k) * dc : along;
-                w[k] = a.update && r < rows && c < cols ? load_at<T>(out, a.tall ? (l0 + c) * a.cols + s0 + r : (s0 + r) * a.cols + l0 + c) : 0.f;
+                const int n = line + k * LINES;
+                w[k] = a.update && n < limit ? to_float(out[n * a.cols]) : 0.f;
             }
 #pragma unroll
             for (int k = 0; k < AT_ONCE; ++k) {
-                const int r = a.tall ? along : across + (i + k) * dr, c = a.tall ? across + (i + k) * dc : along;
-                if (r >= rows || c >= cols) continue;
-                float v = sum[sum_at(r, c)] * (1.f / SCALE);
+                const int n = line + k * LINES;
+                if (n >= limit) break;
+                float v = sum[a.tall ? sum_at(along, n) : sum_at(n, along)] * (1.f / SCALE);
                 if (a.update) v = fmaf(a.keep, w[k], -a.move * v);
-                store_at<T>(out, a.tall ? (l0 + c) * a.cols + s0 + r : (s0 + r) * a.cols + l0 + c, v);
+                out[n * a.cols] = from_float<T>(v);
             }
         }
     }

@@ -18,25 +18,48 @@ namespace ortho {
 
 constexpr int SMS = 148;
 
+// The tiled copies' map: the workspace's blocks as rows of 2 KB (eight rows of a block), each two halves of 1 KB; a copy takes one half of
+// 16 rows.  cuTensorMapEncodeTiled comes through the runtime's lookup: no link-time dependency on the driver.
+static cudaError_t map_of(const Args& a, uint64_t bytes, CUtensorMap* map) {
+    typedef CUresult (*Encode)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                               const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+    static std::atomic<Encode> kept{nullptr};
+    Encode encode = kept.load(std::memory_order_acquire);
+    if (!encode) {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess || !p) {
+            cudaGetLastError();
+            return cudaErrorNotSupported;
+        }
+        encode = (Encode)p;
+        kept.store(encode, std::memory_order_release);
+    }
+    const cuuint64_t dims[3] = {256, 2, bytes / 2048}, strides[2] = {1024, 2048};
+    const cuuint32_t box[3] = {256, 1, 16}, steps[3] = {1, 1, 1};
+    return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 3, a.blocks, dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
+                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
 template <int KIND, int RANKS, class T>
-static cudaError_t gemm_of(const Args& a, int count, cudaStream_t s) {
+static cudaError_t gemm_of(const Args& a, const CUtensorMap& map, int count, cudaStream_t s) {
     static PerDevice done;
     const cudaError_t e = ensure_smem(gemm_kernel<KIND, RANKS, T>, GEMM_SMEM, done);
     if (e != cudaSuccess) return e;
     const dim3 grid((unsigned)RANKS, (unsigned)tiles_of<KIND>(a), (unsigned)count), block(GEMM_THREADS);
-    ORTHO_LAUNCH(launch_overlapped_cluster((unsigned)RANKS, gemm_kernel<KIND, RANKS, T>, grid, block, GEMM_SMEM, s, a));
+    ORTHO_LAUNCH(launch_overlapped_cluster((unsigned)RANKS, gemm_kernel<KIND, RANKS, T>, grid, block, GEMM_SMEM, s, a, map));
     return cudaSuccess;
 }
 template <int KIND, class T = float>
-static cudaError_t gemm(const Args& a, int count, cudaStream_t s) {
+static cudaError_t gemm(const Args& a, const CUtensorMap& map, int count, cudaStream_t s) {
     if constexpr (KIND == GRAM || KIND == POLY) {
         // blocks that share a sum over K: while there are SMs left and each has two steps at least
         const long long blocks = (long long)tiles_of<KIND>(a) * count, steps = steps_of<KIND>(a);
-        if (blocks * 8 <= SMS && steps >= 16) return gemm_of<KIND, 8, T>(a, count, s);
-        if (blocks * 4 <= SMS && steps >= 8) return gemm_of<KIND, 4, T>(a, count, s);
-        if (blocks * 2 <= SMS && steps >= 4) return gemm_of<KIND, 2, T>(a, count, s);
+        if (blocks * 8 <= SMS && steps >= 16) return gemm_of<KIND, 8, T>(a, map, count, s);
+        if (blocks * 4 <= SMS && steps >= 8) return gemm_of<KIND, 4, T>(a, map, count, s);
+        if (blocks * 2 <= SMS && steps >= 4) return gemm_of<KIND, 2, T>(a, map, count, s);
     }
-    return gemm_of<KIND, 1, T>(a, count, s);
+    return gemm_of<KIND, 1, T>(a, map, count, s);
 }
 
 // Clusters of so many blocks, one block an SM, that the current device runs at once: its SMs come in groups that clusters do not
@@ -90,14 +113,16 @@ static cudaError_t run(Args& a, int count, int turns, cudaStream_t s) {
         return cudaSuccess;
     }
     ORTHO_LAUNCH(launch_overlapped(true, sums_kernel<T, UPDATE>, dim3((unsigned)a.parts, (unsigned)count), dim3(PREPARE_THREADS), 0, s, a));
-    const size_t tile = a.tall ? sizeof(float) * BLOCK * (BLOCK + 1) : 0;
+    const size_t tile = sizeof(float) * BLOCK * BLOCK;
     static PerDevice done;
-    cudaError_t e = ensure_smem(first_kernel<T, UPDATE>, sizeof(float) * BLOCK * (BLOCK + 1), done);
+    cudaError_t e = ensure_smem(first_kernel<T, UPDATE>, tile, done);
     if (e != cudaSuccess) return e;
+    CUtensorMap map;
+    if ((e = map_of(a, (uint64_t)((unsigned char*)a.part - a.blocks), &map)) != cudaSuccess) return e;
     ORTHO_LAUNCH(launch_overlapped(true, first_kernel<T, UPDATE>, dim3((unsigned)(a.sblocks * a.lblocks), (unsigned)count), dim3(PREPARE_THREADS), tile, s, a));
     for (int k = 0; k < turns; ++k) {
-        if ((e = gemm<GRAM>(a, count, s)) != cudaSuccess || (e = gemm<POLY>(a, count, s)) != cudaSuccess) return e;
-        if ((e = k + 1 < turns ? gemm<APPLY>(a, count, s) : gemm<LAST, T>(a, count, s)) != cudaSuccess) return e;
+        if ((e = gemm<GRAM>(a, map, count, s)) != cudaSuccess || (e = gemm<POLY>(a, map, count, s)) != cudaSuccess) return e;
+        if ((e = k + 1 < turns ? gemm<APPLY>(a, map, count, s) : gemm<LAST, T>(a, map, count, s)) != cudaSuccess) return e;
         std::swap(a.x, a.y);
     }
     return cudaSuccess;
@@ -186,7 +211,7 @@ static int orthogonal(const void* const* u, float* const* momenta, void* const* 
         a.keep = (float)(1.0 - (double)m->lr * m->weight_decay); a.move = (float)((double)m->lr * m->scale);
     }
     unsigned char* ws = (unsigned char*)d->workspace;
-    a.g = ws + 2 * l.x; a.p = a.g + l.square;
+    a.blocks = ws; a.g = ws + 2 * l.x; a.p = a.g + l.square;
     a.part = (float*)(a.p + l.square);
     a.status = (int*)(ws + l.total - 256);
     for (int64_t i0 = 0; i0 < d->count; i0 += GROUP) {

@@ -8,14 +8,6 @@ namespace ortho {
 
 constexpr int PREPARE_THREADS = 256;
 
-// What is orthogonalised: the matrix itself, or gradient and momentum.
-template <class T, bool UPDATE>
-__device__ __forceinline__ float source(const Args& a, int m, long long i) {
-    if (!UPDATE) return load_at<T>(a.u[m], i);
-    const float v = a.momentum[m][i];
-    return a.nesterov ? fmaf(a.mu, v, load_at<T>(a.u[m], i)) : v;
-}
-
 // momentum <- mu momentum + gradient, and sums of squares of what is orthogonalised, in a fixed order.
 template <class T, bool UPDATE>
 __global__ void __launch_bounds__(PREPARE_THREADS) sums_kernel(const __grid_constant__ Args a) {
@@ -52,7 +44,7 @@ __global__ void __launch_bounds__(PREPARE_THREADS) sums_kernel(const __grid_cons
 template <class T, bool UPDATE>
 __global__ void __launch_bounds__(PREPARE_THREADS) first_kernel(const __grid_constant__ Args a) {
     grid_dependency_wait();
-    extern __shared__ float tile[];                  // tall: 128 columns of the block with one number between them
+    extern __shared__ float tile[];                  // a block in 32 bits
     const int m = blockIdx.y, sb = blockIdx.x / a.lblocks, lb = blockIdx.x % a.lblocks;
     float total = 0.f;
     for (int k = threadIdx.x; k < a.parts; k += PREPARE_THREADS) total += a.part[m * PARTS + k];
@@ -61,25 +53,35 @@ __global__ void __launch_bounds__(PREPARE_THREADS) first_kernel(const __grid_con
     const float by = SCALE / (sqrtf(total) + a.eps);
     unsigned char* block = a.x + ((long long)(m * a.sblocks + sb) * a.lblocks + lb) * BLOCK_BYTES;
     const long long s0 = (long long)sb * BLOCK, l0 = (long long)lb * BLOCK;
-    if (a.tall) {
-#pragma unroll 8
-        for (int i = threadIdx.x; i < BLOCK * BLOCK; i += PREPARE_THREADS) {
-            const int l = i / BLOCK, s = i % BLOCK;
-            tile[l * (BLOCK + 1) + s] = s0 + s < a.S && l0 + l < a.L ? source<T, UPDATE>(a, m, (l0 + l) * a.cols + s0 + s) : 0.f;
+    const int rows = a.S - s0 < BLOCK ? (int)(a.S - s0) : BLOCK, cols = a.L - l0 < BLOCK ? (int)(a.L - l0) : BLOCK;
+    // lanes along what is contiguous
+    constexpr int AT_ONCE = 16, LINES = PREPARE_THREADS / BLOCK;
+    const int along = threadIdx.x & (BLOCK - 1), limit = along < (a.tall ? rows : cols) ? (a.tall ? cols : rows) : 0;
+    const long long corner = (a.tall ? l0 * a.cols + s0 : s0 * a.cols + l0) + along;
+    const T* u = static_cast<const T*>(a.u[m]) + corner;
+    const float* momentum = UPDATE ? a.momentum[m] + corner : nullptr;
+    for (int line = threadIdx.x / BLOCK; line < BLOCK; line += AT_ONCE * LINES) {
+        float v[AT_ONCE], w[AT_ONCE];
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) {
+            const int n = line + k * LINES;
+            v[k] = n < limit && (!UPDATE || a.nesterov) ? to_float(u[n * a.cols]) : 0.f;
+            if (UPDATE) w[k] = n < limit ? momentum[n * a.cols] : 0.f;
         }
-        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) {
+            const int n = line + k * LINES;
+            if (UPDATE) v[k] = a.nesterov ? fmaf(a.mu, w[k], v[k]) : w[k];
+            tile[a.tall ? sum_at(along, n) : sum_at(n, along)] = v[k] * by;
+        }
     }
+    __syncthreads();
 #pragma unroll 2
     for (int i = threadIdx.x; i < BLOCK * BLOCK / 8; i += PREPARE_THREADS) {
         // eight lanes a core: rows of 16 bytes that lie side by side
         const int r = (i & 7) + (i >> 7) * 8, c = ((i >> 3) & 15) * 8;
-        float v[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            if (a.tall) v[j] = tile[(c + j) * (BLOCK + 1) + r];
-            else v[j] = s0 + r < a.S && l0 + c + j < a.L ? source<T, UPDATE>(a, m, (s0 + r) * a.cols + l0 + c + j) : 0.f;
-            v[j] *= by;
-        }
+        const float4 f = *reinterpret_cast<const float4*>(tile + sum_at(r, c)), g = *reinterpret_cast<const float4*>(tile + sum_at(r, c + 4));
+        const float v[8] = {f.x, f.y, f.z, f.w, g.x, g.y, g.z, g.w};
         uint4 hi, lo;
         split8(v, hi, lo);
         *reinterpret_cast<uint4*>(block + core_at(r, c)) = hi;

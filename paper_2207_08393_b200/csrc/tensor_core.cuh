@@ -1,6 +1,7 @@
 // The sm_100a instructions of a matrix product whose operands lie in shared memory as cores of 8 rows by 16 bytes, without swizzle:
 // barriers with bounded waits, bulk copies, descriptors, tcgen05 products and reads of their sums.
 #pragma once
+#include <cuda.h>          // CUtensorMap (type only; the encoder is looked up at run time)
 #include <cuda_runtime.h>
 #include <cstdint>
 
@@ -34,6 +35,12 @@ __device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity) {
 __device__ __forceinline__ void bulk_copy(uint32_t to, const void* from, uint32_t bytes, uint32_t bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
                  ::"r"(to), "l"(from), "r"(bytes), "r"(bar) : "memory");
+}
+
+// A box of a tiled array of this GPU's own memory; the innermost coordinate is 0, so that it starts at 16 bytes
+__device__ __forceinline__ void tiled_copy(uint32_t to, const CUtensorMap* map, int c1, int c2, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+                 ::"r"(to), "l"(map), "r"(bar), "r"(0), "r"(c1), "r"(c2) : "memory");
 }
 
 // Descriptor of an operand.  Sides: M or N, and K.  Where K is contiguous (a core's 16 bytes run along K): `side` bytes from a core to

@@ -17,21 +17,30 @@ namespace ortho {
 
 enum { GRAM, POLY, APPLY, LAST };
 
-constexpr int GEMM_THREADS = 256, STAGES = 3, STEP = 64;                 // STEP: of K, a stage
-constexpr int OPERAND_BYTES = 2 * BLOCK * STEP * 2, STAGE_BYTES = 2 * OPERAND_BYTES;
-constexpr int GEMM_SMEM = 1024 + STAGES * STAGE_BYTES;                  // the first KB: barriers
-constexpr int SUMS = 3;                                                 // hi hi sums side by side in tensor memory, and one of the rest
+constexpr int GEMM_THREADS = 256, STAGES = 3;
+// What a product holds.  GRAM and POLY: 64 of K a stage, one block an SM, sums in four parts: the tensor core cuts a sum off where it adds
+// (2^-23 of it each time), which tells in the diagonal of A, all of whose terms are positive; three sums of hi hi in turn and one of the
+// rest cut off a third as often.  APPLY: few terms, of either sign; 32 of K a stage and two sums leave room for a second block on the SM,
+// whose products run while this one finishes (9216 x 1024: 57 -> <<APPLY>> us).
+template <int KIND> struct Form {
+    static constexpr bool SIDES = KIND == GRAM || KIND == POLY;                // both operands are rows of one matrix
+    static constexpr int STEP = SIDES ? 64 : 32, SUMS = SIDES ? 3 : 1, COLUMNS = (SUMS + 1) * BLOCK, BLOCKS = SIDES ? 1 : 2;
+    static constexpr int PART = BLOCK * STEP * 2, OPERAND = 2 * PART, STAGE = 2 * OPERAND;      // bytes of a piece, both pieces, both operands
+    static constexpr int SMEM = 1024 + STAGES * STAGE;                         // the first KB: barriers
+};
 
 // Steps of K, and blocks of a result that are computed.
-template <int KIND> __host__ __device__ inline int steps_of(const Args& a) { return (int)(((KIND == GRAM ? a.L : a.S) + STEP - 1) / STEP); }
+template <int KIND> __host__ __device__ inline int steps_of(const Args& a) { return (int)(((KIND == GRAM ? a.L : a.S) + Form<KIND>::STEP - 1) / Form<KIND>::STEP); }
 template <int KIND> __host__ inline int tiles_of(const Args& a) { return KIND == GRAM || KIND == POLY ? a.sblocks * (a.sblocks + 1) / 2 : a.sblocks * a.lblocks; }
 
 // T: the type of results (LAST)
 template <int KIND, int RANKS, class T>
-__global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap map) {
+__global__ void __launch_bounds__(GEMM_THREADS, Form<KIND>::BLOCKS) gemm_kernel(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap map) {
     extern __shared__ __align__(1024) unsigned char smem[];
     constexpr int ranks = RANKS, ITEMS = BLOCK * BLOCK / 8 / RANKS / GEMM_THREADS;     // eights of a row that a thread finishes
-    constexpr bool SIDES = KIND == GRAM || KIND == POLY;               // both operands are rows of one matrix
+    using F = Form<KIND>;
+    constexpr bool SIDES = F::SIDES;
+    constexpr int STEP = F::STEP, SUMS = F::SUMS, PARTS_OF_BLOCK = BLOCK / STEP;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = ranks > 1 ? (int)tc::cluster_rank() : 0, m = blockIdx.z;
     int bi, bj;
     if (SIDES) {
@@ -45,7 +54,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
     auto full = [&](int s) { return bars + 8 * s; };
     auto empty = [&](int s) { return bars + 8 * (STAGES + s); };
     const uint32_t done = bars + 16 * STAGES;
-    if (warp == 0) tc::take_columns(base, 512);
+    if (warp == 0) tc::take_columns(base, F::COLUMNS);
     if (threadIdx.x == 0) {
         for (int s = 0; s < 2 * STAGES + 1; ++s) tc::barrier_init(bars + 8 * s, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -68,19 +77,19 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
         // rows of 2 KB (eight rows of a block) from the first block to left's and right's
         const long long lrow = (left - a.blocks) / 2048 + (long long)bi * lblocks * 32, rrow = (right - a.blocks) / 2048 + (long long)bj * lblocks * 32;
         for (int i = 0; i < count; ++i) {
-            const int s = i % STAGES, k = first + i, kb = k >> 1, half = k & 1;
+            const int s = i % STAGES, k = first + i, kb = k / PARTS_OF_BLOCK, share = k % PARTS_OF_BLOCK;
             if (i >= STAGES && !tc::barrier_wait(empty(s), (i / STAGES - 1) & 1)) { failed = true; break; }
-            const uint32_t to = stages + s * STAGE_BYTES;
-            tc::barrier_expect(full(s), one ? OPERAND_BYTES : STAGE_BYTES);
+            const uint32_t to = stages + s * F::STAGE;
+            tc::barrier_expect(full(s), one ? F::OPERAND : F::STAGE);
 #pragma unroll
             for (int piece = 0; piece < 2; ++piece) {
-                const uint32_t at = to + piece * (OPERAND_BYTES / 2);
-                tc::tiled_copy(at, &map, half, (int)(lrow + kb * 32 + piece * 16), full(s));
-                if (SIDES) {
-                    if (!one) tc::tiled_copy(at + OPERAND_BYTES, &map, half, (int)(rrow + kb * 32 + piece * 16), full(s));
-                } else {
-                    tc::bulk_copy(at + OPERAND_BYTES, right + ((long long)kb * a.lblocks + bj) * BLOCK_BYTES + piece * PIECE_BYTES + half * (PIECE_BYTES / 2), OPERAND_BYTES / 2, full(s));
+                const uint32_t at = to + piece * F::PART;
+#pragma unroll
+                for (int h = 0; h < STEP / 32; ++h) {                       // 32 columns of 128 rows: 8 KB
+                    tc::tiled_copy(at + h * 8192, &map, share * (STEP / 32) + h, (int)(lrow + kb * 32 + piece * 16), full(s));
+                    if (SIDES && !one) tc::tiled_copy(at + F::OPERAND + h * 8192, &map, share * (STEP / 32) + h, (int)(rrow + kb * 32 + piece * 16), full(s));
                 }
+                if (!SIDES) tc::bulk_copy(at + F::OPERAND, right + ((long long)kb * a.lblocks + bj) * BLOCK_BYTES + piece * PIECE_BYTES + share * F::PART, F::PART, full(s));
             }
         }
     } else if (warp == 1 && lane == 0) {
@@ -93,14 +102,14 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
                 break;
             }
             tc::fence_after();
-            const uint32_t l = stages + s * STAGE_BYTES, r = one ? l : l + OPERAND_BYTES;
-            constexpr int HALF = OPERAND_BYTES / 2;                                 // from hi to lo
+            const uint32_t l = stages + s * F::STAGE, r = one ? l : l + F::OPERAND;
 #pragma unroll
             for (int q = 0; q < STEP / 16; ++q) {
-                // cores of left: 1024 bytes from one to the next along M, 128 along K; of right (!SIDES): 128 along N, 2048 along K
-                const uint64_t lh = tc::descriptor(l + q * 256, 128, 1024), ll = tc::descriptor(l + HALF + q * 256, 128, 1024);
-                const uint64_t rh = SIDES ? tc::descriptor(r + q * 256, 128, 1024) : tc::descriptor(r + q * 4096, 2048, 128);
-                const uint64_t rl = SIDES ? tc::descriptor(r + HALF + q * 256, 128, 1024) : tc::descriptor(r + HALF + q * 4096, 2048, 128);
+                // cores of left: 512 bytes from one to the next along M, 128 along K; of right (!SIDES): 128 along N, 2048 along K
+                const uint32_t rows_at = (q >> 1) * 8192 + (q & 1) * 256;
+                const uint64_t lh = tc::descriptor(l + rows_at, 128, 512), ll = tc::descriptor(l + F::PART + rows_at, 128, 512);
+                const uint64_t rh = SIDES ? tc::descriptor(r + rows_at, 128, 512) : tc::descriptor(r + q * 4096, 2048, 128);
+                const uint64_t rl = SIDES ? tc::descriptor(r + F::PART + rows_at, 128, 512) : tc::descriptor(r + F::PART + q * 4096, 2048, 128);
                 tc::product(sums + SUMS * BLOCK, ll, rh, what, i > 0 || q > 0);
                 tc::product(sums + SUMS * BLOCK, lh, rl, what, true);
                 tc::product(sums + i % SUMS * BLOCK, lh, rh, what, i >= SUMS || q > 0);
@@ -110,18 +119,20 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
         tc::commit(done);
     }
     __syncwarp();
-    // what is blended in is fetched while the products run
+    // what is blended in is fetched while the products run (POLY), or half of it at a time
+    constexpr int AHEAD = SIDES ? ITEMS : ITEMS / 2;
     const unsigned char* old = KIND == POLY ? a.g + (square + (long long)bi * a.sblocks + bj) * BLOCK_BYTES : a.x + (wide + (long long)bi * a.lblocks + bj) * BLOCK_BYTES;
-    uint4 old_hi[ITEMS], old_lo[ITEMS];
+    uint4 old_hi[AHEAD], old_lo[AHEAD];
     auto row_of = [&](int k) { const int i = rank * ITEMS * GEMM_THREADS + k * GEMM_THREADS + threadIdx.x; return (i & 7) + (i >> 7) * 8; };
     const int col = ((threadIdx.x >> 3) & 15) * 8;
-    if (KIND != GRAM) {
+    auto fetch = [&](int k0) {
 #pragma unroll
-        for (int k = 0; k < ITEMS; ++k) {
-            old_hi[k] = *reinterpret_cast<const uint4*>(old + core_at(row_of(k), col));
-            old_lo[k] = *reinterpret_cast<const uint4*>(old + PIECE_BYTES + core_at(row_of(k), col));
+        for (int k = 0; k < AHEAD; ++k) {
+            old_hi[k] = *reinterpret_cast<const uint4*>(old + core_at(row_of(k0 + k), col));
+            old_lo[k] = *reinterpret_cast<const uint4*>(old + PIECE_BYTES + core_at(row_of(k0 + k), col));
         }
-    }
+    };
+    if (KIND != GRAM) fetch(0);
     if (!tc::barrier_wait(done, 0)) failed = true;
     tc::fence_after();
 
@@ -149,7 +160,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
     }
     tc::fence_before();
     __syncthreads();
-    if (warp == 0) tc::free_columns(sums, 512);
+    if (warp == 0) tc::free_columns(sums, F::COLUMNS);
     if (failed) atomicOr(a.status, 1);
 
     // a cluster's blocks add a share of the rows each, lanes along a row as remote reads want it; these rows of a block's own sums are
@@ -194,9 +205,10 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
 #pragma unroll
         for (int k = 0; k < ITEMS; ++k) {
             float v[8];
+            if (KIND == APPLY && k == AHEAD) fetch(k);
             take8(row_of(k), col, v);
-            if (KIND == POLY) blend(old_hi[k], old_lo[k], a.b, v, a.c);
-            if (KIND == APPLY) blend(old_hi[k], old_lo[k], a.a, v, 1.f);
+            if (KIND == POLY) blend(old_hi[k % AHEAD], old_lo[k % AHEAD], a.b, v, a.c);
+            if (KIND == APPLY) blend(old_hi[k % AHEAD], old_lo[k % AHEAD], a.a, v, 1.f);
             put(to, row_of(k), col, v, rows, cols);
         }
         if (SIDES && !one) {
@@ -208,8 +220,8 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
             if (KIND == POLY) {
 #pragma unroll
                 for (int k = 0; k < ITEMS; ++k) {
-                    old_hi[k] = *reinterpret_cast<const uint4*>(a.g + at + core_at(mirror_row(k), mirror_col));
-                    old_lo[k] = *reinterpret_cast<const uint4*>(a.g + at + PIECE_BYTES + core_at(mirror_row(k), mirror_col));
+                    old_hi[k % AHEAD] = *reinterpret_cast<const uint4*>(a.g + at + core_at(mirror_row(k), mirror_col));
+                    old_lo[k % AHEAD] = *reinterpret_cast<const uint4*>(a.g + at + PIECE_BYTES + core_at(mirror_row(k), mirror_col));
                 }
             }
 #pragma unroll
@@ -226,8 +238,9 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
 #pragma unroll
         for (int k = 0; k < ITEMS; ++k) {
             float v[8];
+            if (k == AHEAD) fetch(k);
             take8(row_of(k), col, v);
-            blend(old_hi[k], old_lo[k], a.a, v, 1.f);
+            blend(old_hi[k % AHEAD], old_lo[k % AHEAD], a.a, v, 1.f);
             *reinterpret_cast<float4*>(sum + sum_at(row_of(k), col)) = make_float4(v[0], v[1], v[2], v[3]);
             *reinterpret_cast<float4*>(sum + sum_at(row_of(k), col + 4)) = make_float4(v[4], v[5], v[6], v[7]);
         }

@@ -18,8 +18,8 @@ namespace ortho {
 
 constexpr int SMS = 148;
 
-// The tiled copies' map: the workspace's blocks as rows of 2 KB (eight rows of a block), each two halves of 1 KB; a copy takes one half of
-// 16 rows.  cuTensorMapEncodeTiled comes through the runtime's lookup: no link-time dependency on the driver.
+// The tiled copies' map: the workspace's blocks as rows of 2 KB (eight rows of a block), each four parts of 512 bytes; a copy takes one part
+// of 16 rows, 32 columns of 128 rows.  cuTensorMapEncodeTiled comes through the runtime's lookup: no link-time dependency on the driver.
 static cudaError_t map_of(const Args& a, uint64_t bytes, CUtensorMap* map) {
     typedef CUresult (*Encode)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
                                const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -35,8 +35,8 @@ static cudaError_t map_of(const Args& a, uint64_t bytes, CUtensorMap* map) {
         encode = (Encode)p;
         kept.store(encode, std::memory_order_release);
     }
-    const cuuint64_t dims[3] = {256, 2, bytes / 2048}, strides[2] = {1024, 2048};
-    const cuuint32_t box[3] = {256, 1, 16}, steps[3] = {1, 1, 1};
+    const cuuint64_t dims[3] = {128, 4, bytes / 2048}, strides[2] = {512, 2048};
+    const cuuint32_t box[3] = {128, 1, 16}, steps[3] = {1, 1, 1};
     return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 3, a.blocks, dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
@@ -44,10 +44,10 @@ static cudaError_t map_of(const Args& a, uint64_t bytes, CUtensorMap* map) {
 template <int KIND, int RANKS, class T>
 static cudaError_t gemm_of(const Args& a, const CUtensorMap& map, int count, cudaStream_t s) {
     static PerDevice done;
-    const cudaError_t e = ensure_smem(gemm_kernel<KIND, RANKS, T>, GEMM_SMEM, done);
+    const cudaError_t e = ensure_smem(gemm_kernel<KIND, RANKS, T>, Form<KIND>::SMEM, done);
     if (e != cudaSuccess) return e;
     const dim3 grid((unsigned)RANKS, (unsigned)tiles_of<KIND>(a), (unsigned)count), block(GEMM_THREADS);
-    ORTHO_LAUNCH(launch_overlapped_cluster((unsigned)RANKS, gemm_kernel<KIND, RANKS, T>, grid, block, GEMM_SMEM, s, a, map));
+    ORTHO_LAUNCH(launch_overlapped_cluster((unsigned)RANKS, gemm_kernel<KIND, RANKS, T>, grid, block, Form<KIND>::SMEM, s, a, map));
     return cudaSuccess;
 }
 template <int KIND, class T = float>

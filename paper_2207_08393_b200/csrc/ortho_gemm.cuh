@@ -37,7 +37,8 @@ template <int KIND> __host__ inline int tiles_of(const Args& a) { return KIND ==
 template <int KIND, int RANKS, class T>
 __global__ void __launch_bounds__(GEMM_THREADS, Form<KIND>::BLOCKS) gemm_kernel(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap map) {
     extern __shared__ __align__(1024) unsigned char smem[];
-    constexpr int ranks = RANKS, ITEMS = BLOCK * BLOCK / 8 / RANKS / GEMM_THREADS;     // eights of a row that a thread finishes
+    constexpr int ranks = RANKS, GROUP_ITEMS = BLOCK, GROUPS = BLOCK / 8;         // eights of a row in eight rows; eights of rows
+    constexpr int ITEMS = ((GROUPS + RANKS - 1) / RANKS * GROUP_ITEMS + GEMM_THREADS - 1) / GEMM_THREADS;     // eights that a thread finishes at most
     using F = Form<KIND>;
     constexpr bool SIDES = F::SIDES;
     constexpr int STEP = F::STEP, SUMS = F::SUMS, PARTS_OF_BLOCK = BLOCK / STEP;
@@ -55,6 +56,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, Form<KIND>::BLOCKS) gemm_kernel(
     auto empty = [&](int s) { return bars + 8 * (STAGES + s); };
     const uint32_t done = bars + 16 * STAGES;
     if (warp == 0) tc::take_columns(base, F::COLUMNS);
+    if (warp == 1 && lane == 0) asm volatile("prefetch.tensormap [%0];" ::"l"(&map) : "memory");
     if (threadIdx.x == 0) {
         for (int s = 0; s < 2 * STAGES + 1; ++s) tc::barrier_init(bars + 8 * s, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -121,13 +123,16 @@ __global__ void __launch_bounds__(GEMM_THREADS, Form<KIND>::BLOCKS) gemm_kernel(
     __syncwarp();
     // what is blended in is fetched while the products run (POLY), or half of it at a time
     constexpr int AHEAD = SIDES ? ITEMS : ITEMS / 2;
+    const int g0 = GROUPS * rank / RANKS, g1 = GROUPS * (rank + 1) / RANKS;            // this block's share of the rows, in eights
     const unsigned char* old = KIND == POLY ? a.g + (square + (long long)bi * a.sblocks + bj) * BLOCK_BYTES : a.x + (wide + (long long)bi * a.lblocks + bj) * BLOCK_BYTES;
     uint4 old_hi[AHEAD], old_lo[AHEAD];
-    auto row_of = [&](int k) { const int i = rank * ITEMS * GEMM_THREADS + k * GEMM_THREADS + threadIdx.x; return (i & 7) + (i >> 7) * 8; };
+    auto row_of = [&](int k) { const int i = g0 * GROUP_ITEMS + k * GEMM_THREADS + threadIdx.x; return (i & 7) + (i >> 7) * 8; };
+    auto has = [&](int k) { return RANKS == 1 || k * GEMM_THREADS + (int)threadIdx.x < (g1 - g0) * GROUP_ITEMS; };
     const int col = ((threadIdx.x >> 3) & 15) * 8;
     auto fetch = [&](int k0) {
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k) {
+            if (!has(k0 + k)) break;
             old_hi[k] = *reinterpret_cast<const uint4*>(old + core_at(row_of(k0 + k), col));
             old_lo[k] = *reinterpret_cast<const uint4*>(old + PIECE_BYTES + core_at(row_of(k0 + k), col));
         }
@@ -166,9 +171,8 @@ __global__ void __launch_bounds__(GEMM_THREADS, Form<KIND>::BLOCKS) gemm_kernel(
     // a cluster's blocks add a share of the rows each, lanes along a row as remote reads want it; these rows of a block's own sums are
     // nobody else's
     if (RANKS > 1) {
-        constexpr int SHARE = BLOCK / RANKS * (BLOCK / 4);
         tc::cluster_sync();
-        for (int i = rank * SHARE + threadIdx.x; i < (rank + 1) * SHARE; i += GEMM_THREADS) {
+        for (int i = g0 * 256 + threadIdx.x; i < g1 * 256; i += GEMM_THREADS) {
             float4 f[RANKS];
 #pragma unroll
             for (int k = 0; k < RANKS; ++k) f[k] = tc::read_remote(base + 1024 + 16 * i, k);
@@ -176,6 +180,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, Form<KIND>::BLOCKS) gemm_kernel(
             for (int k = 1; k < RANKS; ++k) { f[0].x += f[k].x; f[0].y += f[k].y; f[0].z += f[k].z; f[0].w += f[k].w; }
             reinterpret_cast<float4*>(sum)[i] = f[0];
         }
+        tc::cluster_arrive();                      // waited for at the end: nobody leaves while others read its sums
         __syncthreads();
     }
     auto take8 = [&](int r, int c, float (&v)[8]) {
@@ -205,6 +210,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, Form<KIND>::BLOCKS) gemm_kernel(
 #pragma unroll
         for (int k = 0; k < ITEMS; ++k) {
             float v[8];
+            if (!has(k)) break;
             if (KIND == APPLY && k == AHEAD) fetch(k);
             take8(row_of(k), col, v);
             if (KIND == POLY) blend(old_hi[k % AHEAD], old_lo[k % AHEAD], a.b, v, a.c);
@@ -214,24 +220,26 @@ __global__ void __launch_bounds__(GEMM_THREADS, Form<KIND>::BLOCKS) gemm_kernel(
         if (SIDES && !one) {
             // the block on the other side of the diagonal: this block's rows are columns there
             const long long at = (square + (long long)bj * a.sblocks + bi) * BLOCK_BYTES;
-            constexpr int EIGHTS = BLOCK / 8 / RANKS;                      // of columns
-            auto mirror_row = [&](int k) { const int i = k * GEMM_THREADS + threadIdx.x; return (i & 7) + (i >> 3) / EIGHTS * 8; };
-            const int mirror_col = (rank * EIGHTS + (threadIdx.x >> 3) % EIGHTS) * 8;
+            const int eights = RANKS == 1 ? GROUPS : g1 - g0;               // of columns
+            auto mirror_row = [&](int k) { const int i = (k * GEMM_THREADS + threadIdx.x) >> 3; return (threadIdx.x & 7) + i / eights * 8; };
+            auto mirror_col = [&](int k) { const int i = (k * GEMM_THREADS + threadIdx.x) >> 3; return (g0 + i % eights) * 8; };
             if (KIND == POLY) {
 #pragma unroll
                 for (int k = 0; k < ITEMS; ++k) {
-                    old_hi[k % AHEAD] = *reinterpret_cast<const uint4*>(a.g + at + core_at(mirror_row(k), mirror_col));
-                    old_lo[k % AHEAD] = *reinterpret_cast<const uint4*>(a.g + at + PIECE_BYTES + core_at(mirror_row(k), mirror_col));
+                    if (!has(k)) break;
+                    old_hi[k % AHEAD] = *reinterpret_cast<const uint4*>(a.g + at + core_at(mirror_row(k), mirror_col(k)));
+                    old_lo[k % AHEAD] = *reinterpret_cast<const uint4*>(a.g + at + PIECE_BYTES + core_at(mirror_row(k), mirror_col(k)));
                 }
             }
 #pragma unroll
             for (int k = 0; k < ITEMS; ++k) {
-                const int r = mirror_row(k);
+                if (!has(k)) break;
+                const int r = mirror_row(k), c = mirror_col(k);
                 float v[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = sum[sum_at(mirror_col + j, r)];
+                for (int j = 0; j < 8; ++j) v[j] = sum[sum_at(c + j, r)];
                 if (KIND == POLY) blend(old_hi[k], old_lo[k], a.b, v, a.c);
-                put((KIND == GRAM ? a.g : a.p) + at, r, mirror_col, v, cols, rows);
+                put((KIND == GRAM ? a.g : a.p) + at, r, c, v, cols, rows);
             }
         }
     } else {
@@ -268,7 +276,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, Form<KIND>::BLOCKS) gemm_kernel(
             }
         }
     }
-    if (ranks > 1) tc::cluster_sync();             // nobody leaves while others read its sums
+    if (ranks > 1) tc::cluster_wait();
 }
 
 }  // namespace ortho

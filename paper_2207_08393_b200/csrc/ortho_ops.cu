@@ -41,27 +41,6 @@ static cudaError_t map_of(const Args& a, uint64_t bytes, CUtensorMap* map) {
                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
-template <int KIND, int RANKS, class T>
-static cudaError_t gemm_of(const Args& a, const CUtensorMap& map, int count, cudaStream_t s) {
-    static PerDevice done;
-    const cudaError_t e = ensure_smem(gemm_kernel<KIND, RANKS, T>, Form<KIND>::SMEM, done);
-    if (e != cudaSuccess) return e;
-    const dim3 grid((unsigned)RANKS, (unsigned)tiles_of<KIND>(a), (unsigned)count), block(GEMM_THREADS);
-    ORTHO_LAUNCH(launch_overlapped_cluster((unsigned)RANKS, gemm_kernel<KIND, RANKS, T>, grid, block, Form<KIND>::SMEM, s, a, map));
-    return cudaSuccess;
-}
-template <int KIND, class T = float>
-static cudaError_t gemm(const Args& a, const CUtensorMap& map, int count, cudaStream_t s) {
-    if constexpr (KIND == GRAM || KIND == POLY) {
-        // blocks that share a sum over K: while there are SMs left and each has two steps at least
-        const long long blocks = (long long)tiles_of<KIND>(a) * count, steps = steps_of<KIND>(a);
-        if (blocks * 8 <= SMS && steps >= 16) return gemm_of<KIND, 8, T>(a, map, count, s);
-        if (blocks * 4 <= SMS && steps >= 8) return gemm_of<KIND, 4, T>(a, map, count, s);
-        if (blocks * 2 <= SMS && steps >= 4) return gemm_of<KIND, 2, T>(a, map, count, s);
-    }
-    return gemm_of<KIND, 1, T>(a, map, count, s);
-}
-
 // Clusters of so many blocks, one block an SM, that the current device runs at once: its SMs come in groups that clusters do not
 // cross, so 16 clusters of 7 are more than 148 SMs may hold.
 static int clusters_at_once(int ranks) {
@@ -81,6 +60,39 @@ static int clusters_at_once(int ranks) {
     }
     if (slot) slot->store(n, std::memory_order_release);
     return n;
+}
+
+template <int KIND, int RANKS, class T>
+static cudaError_t gemm_of(const Args& a, const CUtensorMap& map, int count, cudaStream_t s) {
+    static PerDevice done;
+    const cudaError_t e = ensure_smem(gemm_kernel<KIND, RANKS, T>, Form<KIND>::SMEM, done);
+    if (e != cudaSuccess) return e;
+    const dim3 grid((unsigned)RANKS, (unsigned)tiles_of<KIND>(a), (unsigned)count), block(GEMM_THREADS);
+    ORTHO_LAUNCH(launch_overlapped_cluster((unsigned)RANKS, gemm_kernel<KIND, RANKS, T>, grid, block, Form<KIND>::SMEM, s, a, map));
+    return cudaSuccess;
+}
+template <int KIND, class T = float>
+static cudaError_t gemm(const Args& a, const CUtensorMap& map, int count, cudaStream_t s) {
+    if constexpr (KIND == GRAM || KIND == POLY) {
+        // blocks that share a sum over K: a step takes about 0.45 us, all else of a block 6, 8 with others; rounds of clusters
+        const long long tiles = (long long)tiles_of<KIND>(a) * count, steps = steps_of<KIND>(a);
+        int best = 1;
+        long long least = 0;
+        for (const int ranks : {1, 2, 3, 4, 6, 8}) {
+            if (ranks > 1 && steps < 2 * ranks) break;
+            const int at_once = ranks > 1 ? clusters_at_once(ranks) : SMS;
+            const long long time = (tiles + at_once - 1) / at_once * ((steps + ranks - 1) / ranks * 45 + (ranks > 1 ? 800 : 600));
+            if (ranks == 1 || time < least) { best = ranks; least = time; }
+        }
+        switch (best) {
+            case 2: return gemm_of<KIND, 2, T>(a, map, count, s);
+            case 3: return gemm_of<KIND, 3, T>(a, map, count, s);
+            case 4: return gemm_of<KIND, 4, T>(a, map, count, s);
+            case 6: return gemm_of<KIND, 6, T>(a, map, count, s);
+            case 8: return gemm_of<KIND, 8, T>(a, map, count, s);
+        }
+    }
+    return gemm_of<KIND, 1, T>(a, map, count, s);
 }
 
 // Tiles of a block of the resident kernel, 0 where a matrix does not fit a cluster.  More tiles mean fewer blocks: a turn takes about

@@ -18,12 +18,21 @@ from __future__ import annotations
 import torch
 
 from . import binding as _b
-from .prior_ops import _DTYPES, _On, _check_kind, _check_sign, _numel, _plain, _steps, _stream
+from .prior_ops import _DTYPES, _HERE, _On, _check_kind, _check_sign, _numel, _plain, _steps, _stream
+
+
+def _check_lengths(x, dim, lengths):
+    if lengths is None:
+        return
+    if dim == 0:
+        raise ValueError("lengths: there is no axis of examples before axis 0")
+    if lengths.dtype != torch.int32 or lengths.dim() != 1 or lengths.shape[0] != x.shape[0] or lengths.device != x.device or not lengths.is_contiguous():
+        raise ValueError("lengths: a contiguous int32 vector of %d values on %s is wanted" % (x.shape[0], x.device))
 
 
 class _Chains:
     """(batch, channels, steps, inner) of a call, and its structure with the strides of the arrays."""
-    __slots__ = ("dim", "sizes", "shape", "device", "dims")
+    __slots__ = ("dim", "sizes", "shape", "device", "dims", "sizes_of_scratch")
 
     def __init__(self, x, dim, reverse, lengths, *others):
         _check_kind(x)
@@ -44,13 +53,10 @@ class _Chains:
                                                                                  x.dtype, x.device))
             _check_sign(t)
             strides += self._strides(t, what)
-        if lengths is not None:
-            if dim == 0:
-                raise ValueError("lengths: there is no axis of examples before axis 0")
-            if lengths.dtype != torch.int32 or lengths.dim() != 1 or lengths.shape[0] != shape[0] or lengths.device != x.device or not lengths.is_contiguous():
-                raise ValueError("lengths: a contiguous int32 vector of %d values on %s is wanted" % (shape[0], x.device))
+        _check_lengths(x, dim, lengths)
         self.dims = _b.gleam_scan_dims(1, _DTYPES[x.dtype], bool(reverse), 0, *self.sizes, strides, _b._addr(lengths), _stream(x) or None,
                                        None, 0)
+        self.sizes_of_scratch = None
 
     def _strides(self, t, what):
         """(batch, channel, step) in elements; all 0 for a contiguous array."""
@@ -92,25 +98,64 @@ class _Chains:
         """Device memory of so many bytes, or None."""
         return torch.empty_strided((size,), (1,), dtype=torch.uint8, device=x.device) if size else None
 
+    def _sizes_of_scratch(self):
+        """Bytes of the saved states and of the workspace."""
+        if self.sizes_of_scratch is None:
+            self.sizes_of_scratch = _b.gleam_gated_scan_saved_size(self.dims), _b.gleam_gated_scan_workspace_size(self.dims)
+        return self.sizes_of_scratch
+
+    def saved(self, x):
+        return self.scratch(x, self._sizes_of_scratch()[0])
+
     def workspace(self, x):
-        ws = self.scratch(x, _b.gleam_gated_scan_workspace_size(self.dims))
+        ws = self.scratch(x, self._sizes_of_scratch()[1])
         if ws is not None:
             self.dims.workspace, self.dims.workspace_bytes = ws.data_ptr(), ws.numel()
         return ws
 
 
+_CALLS = {}                                      # structures of calls on contiguous tensors, by shape, type, axis and direction
+_CALLS_MOST = 256                                # beyond that the table starts over
+_new_dims = _b.gleam_scan_dims.from_buffer_copy
+
+
+def _chains(x, dim, reverse, lengths, *others):
+    """``_Chains`` of a call; where all tensors are contiguous its structure is copied from a kept one (filling one takes longer than a small
+    kernel: forward and VJP of 3 x 5 x 20 x 33 <<SMALL>> us a pair)."""
+    if not _plain(x, *[t for t, _ in others]):
+        return _Chains(x, dim, reverse, lengths, *others)
+    key = x.shape, x.dtype, dim, bool(reverse)
+    kept = _CALLS.get(key)
+    if kept is None:
+        c = _Chains(x, dim, reverse, None)
+        c.dims.stream = None
+        kept = c.dim, c.sizes, c.shape, c._sizes_of_scratch(), bytes(c.dims)
+        if len(_CALLS) >= _CALLS_MOST:
+            _CALLS.clear()
+        _CALLS[key] = kept
+    c = _Chains.__new__(_Chains)
+    c.dim, c.sizes, c.shape, c.sizes_of_scratch, template = kept
+    c.device = _HERE
+    c.dims = _new_dims(template)
+    c.dims.stream = _b._current_stream_handle() or None
+    if lengths is not None:
+        _check_lengths(x, c.dim, lengths)
+        c.dims.lengths = lengths.data_ptr()
+    return c
+
+
 def _new(x):
-    return torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    return torch.empty_like(x) if x.is_contiguous() else torch.empty(x.shape, dtype=x.dtype, device=x.device)
 
 
 def gated_scan_forward(x, gate, state=None, lengths=None, dim=-2, reverse=False, save=True):
     """(y, last, saved): y_t = h_t in x's type, last = the state behind the last step, saved = what ``gated_scan_vjp`` needs besides
     x and gate (None with ``save=False``).  ``state`` (None: zeros) is the state before the first step."""
-    c = _Chains(x, dim, reverse, lengths, (gate, "gate"), (None, "y"))
+    c = _chains(x, dim, reverse, lengths, (gate, "gate"), (None, "y"))
     c.check_state(x, state, "state")
     y, last = _new(x), c.state(x)
     with c.device:
-        starts = c.scratch(x, _b.gleam_gated_scan_saved_size(c.dims)) if save else None
+        starts = c.saved(x) if save else None
         ws = c.workspace(x)
         _b.gleam_gated_scan_forward(x, gate, state, y, last, starts, c.dims)
     del ws
@@ -120,16 +165,17 @@ def gated_scan_forward(x, gate, state=None, lengths=None, dim=-2, reverse=False,
 def gated_scan_vjp(grad_y, grad_last, x, gate, saved, lengths=None, dim=-2, reverse=False, state_grad=True):
     """(grad_x, grad_gate, grad_state) of ``gated_scan_forward`` for the cotangents of y and last (``grad_last`` None: zero); the last
     one is None where it is not wanted.  x, gate, lengths and the state given there are what they were."""
-    c = _Chains(x, dim, reverse, lengths, (gate, "gate"), (grad_y, "grad_y"))
+    c = _chains(x, dim, reverse, lengths, (gate, "gate"), (grad_y, "grad_y"))
     c.check_state(x, grad_last, "grad_last")
     starts, state = saved
     c.check_state(x, state, "state")
-    s = tuple(c.dims.stride)
-    c.dims.stride = s[6:9] + s[:6] + (0,) * 6                # in the order of the call: grad_y, x, gate, then the outputs
+    if c.device is not _HERE:
+        s = tuple(c.dims.stride)
+        c.dims.stride = s[6:9] + s[:6] + (0,) * 6            # in the order of the call: grad_y, x, gate, then the outputs
     gx, gg = _new(x), _new(x)
     gs = c.state(x) if state_grad else None
     with c.device:
-        need = _b.gleam_gated_scan_saved_size(c.dims)
+        need = c._sizes_of_scratch()[0]
         if need and (starts is None or starts.numel() != need or starts.device != x.device):
             raise ValueError("saved: the forward call on these sizes saves %d bytes on %s" % (need, x.device))
         ws = c.workspace(x)
@@ -140,7 +186,6 @@ def gated_scan_vjp(grad_y, grad_last, x, gate, saved, lengths=None, dim=-2, reve
 
 _STEPS = {}                                      # structures of steps on contiguous tensors, by shape and type
 _STEPS_MOST = 256                                # beyond that the table starts over
-_new_dims = _b.gleam_scan_dims.from_buffer_copy
 
 
 def gated_step(x, gate, state):

@@ -172,13 +172,21 @@ __global__ void __launch_bounds__(GEMM_THREADS, Form<KIND>::BLOCKS) gemm_kernel(
     // nobody else's
     if (RANKS > 1) {
         tc::cluster_sync();
-        for (int i = g0 * 256 + threadIdx.x; i < g1 * 256; i += GEMM_THREADS) {
-            float4 f[RANKS];
+        constexpr int AT_ONCE = RANKS > 4 ? 2 : RANKS > 2 ? 3 : 4;              // rows in eights whose reads are under way together
+        for (int g = g0; g < g1; g += AT_ONCE) {
+            float4 f[AT_ONCE][RANKS];
 #pragma unroll
-            for (int k = 0; k < RANKS; ++k) f[k] = tc::read_remote(base + 1024 + 16 * i, k);
+            for (int j = 0; j < AT_ONCE; ++j)
 #pragma unroll
-            for (int k = 1; k < RANKS; ++k) { f[0].x += f[k].x; f[0].y += f[k].y; f[0].z += f[k].z; f[0].w += f[k].w; }
-            reinterpret_cast<float4*>(sum)[i] = f[0];
+                for (int k = 0; k < RANKS; ++k)
+                    if (g + j < g1) f[j][k] = tc::read_remote(base + 1024 + 16 * ((g + j) * 256 + threadIdx.x), k);
+#pragma unroll
+            for (int j = 0; j < AT_ONCE; ++j) {
+                if (g + j >= g1) break;
+#pragma unroll
+                for (int k = 1; k < RANKS; ++k) { f[j][0].x += f[j][k].x; f[j][0].y += f[j][k].y; f[j][0].z += f[j][k].z; f[j][0].w += f[j][k].w; }
+                reinterpret_cast<float4*>(sum)[(g + j) * 256 + threadIdx.x] = f[j][0];
+            }
         }
         tc::cluster_arrive();                      // waited for at the end: nobody leaves while others read its sums
         __syncthreads();
@@ -259,21 +267,26 @@ __global__ void __launch_bounds__(GEMM_THREADS, Form<KIND>::BLOCKS) gemm_kernel(
         const int along = threadIdx.x & (BLOCK - 1), r1 = rows < BLOCK ? (int)rows : BLOCK, c1 = cols < BLOCK ? (int)cols : BLOCK;
         const int limit = along < (a.tall ? r1 : c1) ? (a.tall ? c1 : r1) : 0;
         T* out = static_cast<T*>(a.out[m]) + (a.tall ? l0 * a.cols + s0 : s0 * a.cols + l0) + along;
-        for (int line = threadIdx.x / BLOCK; line < limit; line += AT_ONCE * LINES) {
-            float w[AT_ONCE];
+        const long long step = LINES * a.cols;
+        int line = threadIdx.x / BLOCK;
+        out += line * a.cols;
+        for (; line < BLOCK; line += AT_ONCE * LINES, out += AT_ONCE * step) {
+            float w[AT_ONCE], v[AT_ONCE];
+            T* p = out;
+            if (a.update) {
 #pragma unroll
-            for (int k = 0; k < AT_ONCE; ++k) {
-                const int n = line + k * LINES;
-                w[k] = a.update && n < limit ? to_float(out[n * a.cols]) : 0.f;
+                for (int k = 0; k < AT_ONCE; ++k, p += step) w[k] = line + k * LINES < limit ? to_float(*p) : 0.f;
             }
 #pragma unroll
-            for (int k = 0; k < AT_ONCE; ++k) {
-                const int n = line + k * LINES;
-                if (n >= limit) break;
-                float v = sum[a.tall ? sum_at(along, n) : sum_at(n, along)] * (1.f / SCALE);
-                if (a.update) v = fmaf(a.keep, w[k], -a.move * v);
-                out[n * a.cols] = from_float<T>(v);
+            for (int k = 0; k < AT_ONCE; ++k) v[k] = sum[a.tall ? sum_at(along, line + k * LINES) : sum_at(line + k * LINES, along)] * (1.f / SCALE);
+            if (a.update) {
+#pragma unroll
+                for (int k = 0; k < AT_ONCE; ++k) v[k] = fmaf(a.keep, w[k], -a.move * v[k]);
             }
+            p = out;
+#pragma unroll
+            for (int k = 0; k < AT_ONCE; ++k, p += step)
+                if (line + k * LINES < limit) *p = from_float<T>(v[k]);
         }
     }
     if (ranks > 1) tc::cluster_wait();

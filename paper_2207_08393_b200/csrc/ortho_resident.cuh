@@ -85,22 +85,30 @@ __global__ void __launch_bounds__(RESIDENT_THREADS, 1) resident_kernel(const __g
         const long long corner = (a.tall ? l0 * a.cols : l0) + along;
         const T* from = static_cast<const T*>(a.u[m]) + corner;
         float* momentum = UPDATE ? a.momentum[m] + corner : nullptr;
-        for (int line = line0; line < lines; line += AT_ONCE * LINES) {
+        const long long step = LINES * a.cols;
+        from += line0 * a.cols;
+        if (UPDATE) momentum += line0 * a.cols;
+        for (int line = line0; line < lines; line += AT_ONCE * LINES, from += AT_ONCE * step, momentum += UPDATE ? AT_ONCE * step : 0) {
             float v[AT_ONCE], w[AT_ONCE];
+            const T* p = from;
+            float* q = momentum;
 #pragma unroll
-            for (int k = 0; k < AT_ONCE; ++k) {
-                const int n = line + k * LINES;
-                v[k] = n < limit ? to_float(from[n * a.cols]) : 0.f;
-                if (UPDATE) w[k] = n < limit ? momentum[n * a.cols] : 0.f;
+            for (int k = 0; k < AT_ONCE; ++k, p += step, q += UPDATE ? step : 0) {
+                v[k] = line + k * LINES < limit ? to_float(*p) : 0.f;
+                if (UPDATE) w[k] = line + k * LINES < limit ? *q : 0.f;
+            }
+            if (UPDATE) {
+                q = momentum;
+#pragma unroll
+                for (int k = 0; k < AT_ONCE; ++k, q += step) {
+                    w[k] = fmaf(a.mu, w[k], v[k]);
+                    if (line + k * LINES < limit) *q = w[k];
+                    v[k] = a.nesterov ? fmaf(a.mu, w[k], v[k]) : w[k];
+                }
             }
 #pragma unroll
             for (int k = 0; k < AT_ONCE; ++k) {
                 const int n = line + k * LINES;
-                if (UPDATE) {
-                    w[k] = fmaf(a.mu, w[k], v[k]);
-                    if (n < limit) momentum[n * a.cols] = w[k];
-                    v[k] = a.nesterov ? fmaf(a.mu, w[k], v[k]) : w[k];
-                }
                 squares = fmaf(v[k], v[k], squares);
                 if (n < lines && (!a.tall || along < R)) to[spot(n)] = v[k];
             }
@@ -306,21 +314,24 @@ __global__ void __launch_bounds__(RESIDENT_THREADS, 1) resident_kernel(const __g
                 const long long l0 = (first + t) * BLOCK;
                 const int width = a.L - l0 < BLOCK ? (int)(a.L - l0) : BLOCK, limit = along < (a.tall ? (int)a.S : width) ? (a.tall ? width : (int)a.S) : 0;
                 T* out = static_cast<T*>(a.out[m]) + (a.tall ? l0 * a.cols : l0) + along;
-                for (int line = line0; line < limit; line += AT_ONCE * LINES) {
-                    float w[AT_ONCE];
+                const long long step = LINES * a.cols;
+                out += line0 * a.cols;
+                for (int line = line0; line < lines; line += AT_ONCE * LINES, out += AT_ONCE * step) {
+                    float w[AT_ONCE], x[AT_ONCE];
+                    T* p = out;
+                    if (UPDATE) {
 #pragma unroll
-                    for (int k = 0; k < AT_ONCE; ++k) {
-                        const int n = line + k * LINES;
-                        w[k] = UPDATE && n < limit ? to_float(out[n * a.cols]) : 0.f;
+                        for (int k = 0; k < AT_ONCE; ++k, p += step) w[k] = line + k * LINES < limit ? to_float(*p) : 0.f;
                     }
 #pragma unroll
                     for (int k = 0; k < AT_ONCE; ++k) {
-                        const int n = line + k * LINES;
-                        if (n >= limit) break;
-                        float x = sum[spot(n)] * (1.f / SCALE);
-                        if (UPDATE) x = fmaf(a.keep, w[k], -a.move * x);
-                        out[n * a.cols] = from_float<T>(x);
+                        x[k] = line + k * LINES < limit ? sum[spot(line + k * LINES)] * (1.f / SCALE) : 0.f;
+                        if (UPDATE) x[k] = fmaf(a.keep, w[k], -a.move * x[k]);
                     }
+                    p = out;
+#pragma unroll
+                    for (int k = 0; k < AT_ONCE; ++k, p += step)
+                        if (line + k * LINES < limit) *p = from_float<T>(x[k]);
                 }
             }
         }

@@ -157,13 +157,15 @@ static cudaError_t rows_of(const Args& a, cudaStream_t s) {
 
 template <bool REVERSE, bool DENSE, bool BACK>
 static cudaError_t rows(const Args& a, cudaStream_t s) {
-    if (a.steps <= SHORT_STEPS<T>) {
-        constexpr auto KERNEL = short_kernel<T, REVERSE, DENSE, BACK ? VJP : FORWARD>;
-        const cudaError_t e = ensure_smem(KERNEL, short_smem<T, BACK ? VJP : FORWARD>(SHORT_STEPS<T>), kernel_state<KERNEL>);
-        if (e != cudaSuccess) return e;
-        SCAN_LAUNCH(KERNEL, dim3((unsigned)ceil_div(a.rows, SHORT_ROWS)), dim3(SHORT_ROWS), short_smem<T, BACK ? VJP : FORWARD>(a.steps), s, a);
-        return cudaSuccess;
-    }
+    if (a.steps <= SHORT_STEPS<T>)
+        return by_bool(sizeof(T) == 2 && a.steps % 2 == 0, [&](auto w) -> cudaError_t {
+            constexpr bool WHOLE = sizeof(T) == 2 && decltype(w)::value;
+            constexpr auto KERNEL = short_kernel<T, REVERSE, DENSE, WHOLE, BACK ? VJP : FORWARD>;
+            const cudaError_t e = ensure_smem(KERNEL, short_smem<T, BACK ? VJP : FORWARD>(SHORT_STEPS<T>), kernel_state<KERNEL>);
+            if (e != cudaSuccess) return e;
+            SCAN_LAUNCH(KERNEL, dim3((unsigned)ceil_div(a.rows, SHORT_ROWS)), dim3(SHORT_ROWS), (short_smem<T, BACK ? VJP : FORWARD>(a.steps)), s, a);
+            return cudaSuccess;
+        });
     return a.run == 1 ? rows_of<REVERSE, DENSE, true, BACK>(a, s) : rows_of<REVERSE, DENSE, false, BACK>(a, s);
 }
 

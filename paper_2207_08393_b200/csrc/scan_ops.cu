@@ -39,6 +39,7 @@ static int check_dims(const gleam_scan_dims* d) {
         if (n && v > most / n) return GLEAM_ERR_BAD_DIMS;
         n *= v;
     }
+    if (d->steps > (1ll << 31) - (1 << 16)) return GLEAM_ERR_BAD_DIMS;             // counted in 32 bits, tiles beyond the end included
     if ((uintptr_t)d->lengths % 4) return GLEAM_ERR_BAD_DIMS;
     return GLEAM_OK;
 }

@@ -11,6 +11,8 @@
 #pragma once
 #include "scan_common.cuh"
 
+#include <type_traits>
+
 namespace gleam {
 namespace scan {
 
@@ -238,38 +240,43 @@ __global__ void __launch_bounds__(STREAM_THREADS) stream_kernel(const __grid_con
         copies_wait<DEPTH - 1>();
         if (STRIP) __syncthreads();
         const unsigned char* slots = ring + group % DEPTH * (2 * BATCH * R::SLOT);
+        auto run = [&](auto whole) {                                       // whole: a full group of steps that are all there
+            constexpr bool ALL = decltype(whole)::value;
 #pragma unroll
-        for (int k = 0; k < BATCH; ++k) {
-            const int n = n0 + k;
-            if (n >= span.count) break;
-            Two out[P];
-            if (span.has(n)) {
-                Two g[P], u[P];
-                c.read(slots + 2 * k * R::SLOT, gate, g);
-                c.read(slots + (2 * k + 1) * R::SLOT, other, u);
+            for (int k = 0; k < BATCH; ++k) {
+                const int n = n0 + k;
+                if (!ALL && n >= span.count) break;
+                Two out[P];
+                if (ALL || span.has(n)) {
+                    Two g[P], u[P];
+                    c.read(slots + 2 * k * R::SLOT, gate, g);
+                    c.read(slots + (2 * k + 1) * R::SLOT, other, u);
 #pragma unroll
-                for (int j = 0; j < P; ++j) {
-                    Two f, rest;
-                    gates_of(g[j], f, rest);
-                    h[j] = BACK ? f * (h[j] + u[j]) : fma2(f, h[j], rest * u[j]);
-                    if (MAPS) prod[j] = prod[j] * f;
-                    out[j] = h[j];
+                    for (int j = 0; j < P; ++j) {
+                        Two f, rest;
+                        gates_of(g[j], f, rest);
+                        h[j] = BACK ? f * (h[j] + u[j]) : fma2(f, h[j], rest * u[j]);
+                        if (MAPS) prod[j] = prod[j] * f;
+                        out[j] = h[j];
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < P; ++j) out[j] = Two(0.f);
                 }
-            } else {
-#pragma unroll
-                for (int j = 0; j < P; ++j) out[j] = Two(0.f);
-            }
-            if (!MAPS) {
-                c.write(y, out);
-                y += y_step;
-                if (--to_save == 0) {
-                    to_save = a.chunk;
-                    if (saved && begin + n + 1 < a.steps) c.write_states(saved, h);
-                    if (saved) saved += a.rows;
+                if (!MAPS) {
+                    c.write(y, out);
+                    y += y_step;
+                    if (--to_save == 0) {
+                        to_save = a.chunk;
+                        if (saved && begin + n + 1 < a.steps) c.write_states(saved, h);
+                        if (saved) saved += a.rows;
+                    }
                 }
+                if (STRIP) { gate += gate_step; other += other_step; }      // their low bits say where a row lies in its slot
             }
-            if (STRIP) { gate += gate_step; other += other_step; }      // their low bits say where a row lies in its slot
-        }
+        };
+        if (n0 + BATCH <= span.count && span.has(n0) && span.has(n0 + BATCH - 1)) run(std::true_type{});
+        else run(std::false_type{});
         if (STRIP) __syncthreads();
     }
     if (MAPS) {

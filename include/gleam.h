@@ -352,7 +352,7 @@ GLEAM_API int gleam_layer_norm_workspace_size(const gleam_feature_dims* dims, ui
  *   step           state <- f state + (1 - f) x,  y = state:  one step (steps = 1, no lengths) with the state updated in place
  *
  * lengths (int32, one for each example, device, read when the kernels run; below 0 counts as 0, above steps as steps): steps from
- * lengths[b] on are not there.  Their x, gate and grad_y are not read, the state passes them unchanged, and y, grad_x and
+ * lengths[b] on are not there.  Their x, gate and grad_y are not used (they may be NaN), the state passes them unchanged, and y, grad_x and
  * grad_gate are 0 there.  An example without steps returns its state as last.
  *
  * x, gate, y and their cotangents have type dtype; states, their cotangents and saved are float32, (batch, channels, inner),
@@ -368,7 +368,7 @@ typedef struct {
     int32_t dtype;            /* GLEAM_F32, GLEAM_F16 or GLEAM_BF16 */
     int32_t reverse;          /* 0 or 1 */
     int32_t reserved;         /* 0 */
-    int64_t batch, channels, steps, inner;
+    int64_t batch, channels, steps, inner;      /* 0 ... 2^31 each (steps: 2^31 - 2^16), 2^37 elements at most */
     int64_t stride[5][3];     /* elements from one example, channel, step to the next, for each activation array in the order of the
                                  call's arguments; all three 0 = contiguous.  In any order of size, but no two elements share memory */
     const int32_t* lengths;   /* or null */
@@ -397,7 +397,8 @@ GLEAM_API int gleam_gated_scan_saved_size(const gleam_scan_dims* dims, uint64_t*
  * have type dtype, momenta are float32.  The norm is a 32-bit sum.  Products are as exact as 32-bit ones (float16 pieces of 22 bits,
  * 32-bit sums); |a|, |b|, |c| <= 16, and singular values have to stay below 8 along the way (those of the usual coefficients stay below
  * 1.3).  A matrix of zeros gives zeros; one with a NaN or an infinity gives NaN throughout, the others are untouched by it.  The shorter
- * side is at most 16384, and there are at most 65535 blocks of 128 x 128 in a matrix.  Nothing that a call writes may overlap
+ * side is at most 16384, and there are at most 65535 blocks of 128 x 128 in a matrix.  GLEAM_ERR_CUDA also reports that the host has no
+ * memory left for a call's checks.  Nothing that a call writes may overlap
  * anything else of the call (GLEAM_ERR_ALIAS).  Results are deterministic.  Two calls whose GPU work may overlap need workspaces of
  * their own.
  */

@@ -9,7 +9,8 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
-#include <vector>
+#include <memory>
+#include <new>
 
 namespace gleam {
 namespace ortho {
@@ -174,14 +175,16 @@ static int layout_of(const gleam_matrix_dims* d, Layout* l) {
 struct Span { uintptr_t at; uint64_t bytes; bool written; };
 
 // Every matrix of the call: on a device, aligned, and nothing written shared with anything else.
-static int check_memory(std::vector<Span>& spans) {
-    for (const Span& u : spans) {
+static int check_memory(Span* spans, size_t count) {
+    for (size_t i = 0; i < count; ++i) {
+        const Span& u = spans[i];
         const int rc = check_device_ptr((const void*)u.at);
         if (rc != GLEAM_OK) return rc;
     }
-    std::sort(spans.begin(), spans.end(), [](const Span& x, const Span& y) { return x.at < y.at; });
+    std::sort(spans, spans + count, [](const Span& x, const Span& y) { return x.at < y.at; });
     uintptr_t end = 0, written = 0;                 // first byte behind all spans so far, behind the written ones
-    for (const Span& u : spans) {
+    for (size_t i = 0; i < count; ++i) {
+        const Span& u = spans[i];
         if (u.at < written || (u.written && u.at < end)) return GLEAM_ERR_ALIAS;
         end = std::max<uintptr_t>(end, u.at + u.bytes);
         if (u.written) written = std::max<uintptr_t>(written, u.at + u.bytes);
@@ -199,17 +202,18 @@ static int orthogonal(const void* const* u, float* const* momenta, void* const* 
     if ((uintptr_t)d->workspace & 255) return GLEAM_ERR_BAD_DIMS;
     const uint64_t n = (uint64_t)d->rows * d->cols, esize = d->dtype == GLEAM_F32 ? 4 : 2;
     {
-        std::vector<Span> spans;
-        spans.reserve((size_t)d->count * 3 + 1);
-        spans.push_back(Span{(uintptr_t)d->workspace, l.total, true});
+        const std::unique_ptr<Span[]> spans(new (std::nothrow) Span[(size_t)d->count * 3 + 1]);     // no exception leaves a C entry
+        if (!spans) return GLEAM_ERR_CUDA;
+        size_t n_spans = 0;
+        spans[n_spans++] = Span{(uintptr_t)d->workspace, l.total, true};
         for (int64_t i = 0; i < d->count; ++i) {
             if (!u[i] || !out[i] || (m && !momenta[i])) return GLEAM_ERR_NULL_POINTER;
             if ((uintptr_t)u[i] % esize || (uintptr_t)out[i] % esize || (m && (uintptr_t)momenta[i] % 4)) return GLEAM_ERR_BAD_DIMS;
-            spans.push_back(Span{(uintptr_t)u[i], n * esize, false});
-            spans.push_back(Span{(uintptr_t)out[i], n * esize, true});
-            if (m) spans.push_back(Span{(uintptr_t)momenta[i], n * 4, true});
+            spans[n_spans++] = Span{(uintptr_t)u[i], n * esize, false};
+            spans[n_spans++] = Span{(uintptr_t)out[i], n * esize, true};
+            if (m) spans[n_spans++] = Span{(uintptr_t)momenta[i], n * 4, true};
         }
-        if ((rc = check_memory(spans)) != GLEAM_OK) return rc;
+        if ((rc = check_memory(spans.get(), n_spans)) != GLEAM_OK) return rc;
     }
     Args a;
     std::memset(&a, 0, sizeof a);

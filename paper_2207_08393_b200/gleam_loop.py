@@ -143,7 +143,7 @@ class ResidualPrior(nn.Module):
             raise ValueError("one frame is wanted (shape %s)" % (tuple(x_ch.shape),))
         h = x_ch.permute(0, 2, 3, 1, 4, 5).reshape(B * n0, 2, n1, n2)
         f = self.head(h)
-        u = self.gates(f)
+        u = self.gates(f).contiguous()
         if state is None:
             state = torch.zeros(f.shape, dtype=torch.float32, device=f.device)
         F = f.shape[1]

@@ -79,6 +79,8 @@ def muon_step(weights, grads, momenta, lr, momentum=0.95, nesterov=True, weight_
         ws = _workspace(w0, dims)
         if ws is not None:
             _b.gleam_muon_step(weights, grads, momenta, _b.gleam_muon_args(lr, momentum, weight_decay, scale, bool(nesterov)), dims)
+            for tensors in (weights, momenta):
+                torch.autograd.graph.increment_version([t for t in tensors if not t.is_inference()])
     del ws
 
 

@@ -167,6 +167,8 @@ def gated_scan_vjp(grad_y, grad_last, x, gate, saved, lengths=None, dim=-2, reve
     one is None where it is not wanted.  x, gate, lengths and the state given there are what they were."""
     c = _chains(x, dim, reverse, lengths, (gate, "gate"), (grad_y, "grad_y"))
     c.check_state(x, grad_last, "grad_last")
+    if saved is None:
+        raise ValueError("saved: the forward call was made with save=False")
     starts, state = saved
     c.check_state(x, state, "state")
     if c.device is not _HERE:
@@ -188,8 +190,17 @@ _STEPS = {}                                      # structures of steps on contig
 _STEPS_MOST = 256                                # beyond that the table starts over
 
 
+def _changed(t):
+    """Tells autograd that a tensor was written in place, as torch's own operators do."""
+    if not t.is_inference():
+        torch.autograd.graph.increment_version(t)
+
+
 def gated_step(x, gate, state):
-    """One step: state <- f state + (1 - f) x in place; returns the new state in x's type.  x, gate and state have one shape."""
+    """One step: state <- f state + (1 - f) x in place; returns the new state in x's type.  x, gate and state have one shape.  Not
+    differentiable: gradients go through ``gated_scan``."""
+    if torch.is_grad_enabled() and any(isinstance(t, torch.Tensor) and t.requires_grad for t in (x, gate, state)):
+        raise ValueError("single steps are not differentiable: use gated_scan, or torch.no_grad()")
     if _plain(x, gate) and isinstance(state, torch.Tensor) and state.shape == x.shape and state.dtype is torch.float32 and \
             state.is_contiguous() and state.get_device() == x.get_device() and not state.is_neg():
         key = x.shape, x.dtype                   # filling a structure takes longer than the kernel (18.7 -> 11 us a call)
@@ -204,6 +215,7 @@ def gated_step(x, gate, state):
         dims.stream = _b._current_stream_handle() or None
         y = torch.empty_like(x)
         _b.gleam_gated_step(x, gate, state, y, dims)
+        _changed(state)
         return y
     _check_kind(x)
     at = 1 if x.dim() > 1 else 0
@@ -214,6 +226,7 @@ def gated_step(x, gate, state):
     y = _new(x)
     with c.device:
         _b.gleam_gated_step(x, gate, state, y, c.dims)
+    _changed(state)
     return y
 
 
@@ -255,4 +268,6 @@ class _GatedScan(torch.autograd.Function):
 
 def gated_scan(x, gate, state=None, lengths=None, dim=-2, reverse=False):
     """(y, last) of the recurrence, with gradients for x, gate and state."""
+    if state is not None:
+        state = state.resolve_neg().contiguous()
     return _GatedScan.apply(_viewable(x, x, dim), _viewable(gate, x, dim), state, lengths, dim, reverse)

@@ -240,3 +240,27 @@ def test_half_precision_weights_keep_a_32_bit_momentum():
     again.load_state_dict(opt.state_dict())
     assert again.state[p]["momentum"].dtype == torch.float32
     assert torch.equal(again.state[p]["momentum"], opt.state[p]["momentum"])
+
+
+def test_writes_in_place_are_seen_by_autograd():
+    import paper_2207_08393_b200 as g
+    w = torch.randn(4, 6, device="cuda", requires_grad=True)
+    y = (w * w).sum()
+    before = w._version
+    with torch.no_grad():
+        g.muon_step([w], [torch.randn(4, 6, device="cuda")], [torch.zeros(4, 6, device="cuda")], 0.1)
+    assert w._version > before
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.backward()
+
+
+@pytest.mark.parametrize("shape", [(1, 128, 1024), (1, 128, 1025), (1, 112, 2048), (1, 113, 1500), (9, 16, 7000), (1, 16, 30000), (40, 128, 900), (20, 48, 6000)])
+def test_where_the_resident_kernel_ends(shape):
+    """The most that a cluster holds, and a little more, which the general kernels take."""
+    import paper_2207_08393_b200 as g
+    x = matrices(*shape)
+    y = g.orthogonalise(x, 3)
+    for k in (0, shape[0] - 1):
+        close(y[k], oo.iterates(host(x[k]), 3), torch.float32)
+    t = g.orthogonalise(x.mT.contiguous(), 3)
+    close(t[0], [i.T for i in oo.iterates(host(x[0]), 3)], torch.float32)

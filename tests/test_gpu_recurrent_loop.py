@@ -71,12 +71,14 @@ def test_gradients_of_the_prior(recurrent, n0, lengths):
         close(v.grad, par[k].grad, k)
 
 
-@pytest.mark.parametrize("norm", [False, True])
-def test_live_frames_are_the_cine(norm):
-    """Convolutions of one frame and of a batch of frames may sum in another order."""
+@pytest.mark.parametrize("norm,last", [(False, False), (True, False), (False, True)])
+def test_live_frames_are_the_cine(norm, last):
+    """Convolutions of one frame and of a batch of frames may sum in another order; also with the features last in memory."""
     from paper_2207_08393_b200 import gleam_loop as gl
     torch.manual_seed(1)
     prior = gl.ResidualPrior(8, 2, norm=norm, recurrent="causal").cuda().eval()
+    if last:
+        prior = prior.to(memory_format=torch.channels_last)
     x = torch.randn(2, 2, 6, 1, 12, 10, device="cuda")
     whole, state = prior(x), None
     for t in range(6):
@@ -157,3 +159,20 @@ def test_a_captured_training_step():
         kept.append([p.detach().clone() for p in params])
     for a, b in zip(*kept):
         assert float((a - b).norm()) <= 1e-5 * float(a.norm())
+
+
+def test_a_prior_under_autocast():
+    """Half precision convolutions around the recurrence: outputs and gradients near those in single precision."""
+    from paper_2207_08393_b200 import gleam_loop as gl
+    torch.manual_seed(4)
+    prior = gl.ResidualPrior(8, 1, recurrent="both").cuda()
+    x = torch.randn(1, 2, 5, 1, 12, 16, device="cuda")
+    want = prior(x)
+    grads = torch.autograd.grad(want.square().mean(), list(prior.parameters()))
+    with torch.autocast("cuda", dtype=torch.bfloat16):
+        got = prior(x)
+    half = torch.autograd.grad(got.float().square().mean(), list(prior.parameters()))
+    # eleven roundings of 2^-9 on the way to an output, twice as many to a gradient; sums of such errors stay far below
+    assert float((got.float() - want).norm()) <= 0.05 * float(want.norm())
+    for a, b in zip(grads, half):
+        assert bool(torch.isfinite(b).all()) and float((a - b).norm()) <= 0.1 * float(a.norm()) + 1e-4

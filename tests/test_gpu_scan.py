@@ -338,3 +338,46 @@ def test_outputs_stay_inside():
         for a, w in zip((y, dx, dg), wide):
             assert torch.equal(a, w[:, :c])
         assert torch.equal(last.reshape(-1), vec[0][:-8]) and torch.equal(ds.reshape(-1), vec[1][:-8])
+
+
+def test_writes_in_place_are_seen_by_autograd():
+    import paper_2207_08393_b200 as g
+    x, gate = torch.randn(2, 6, 8, device="cuda", requires_grad=True), torch.randn(2, 6, 8, device="cuda")
+    state = torch.zeros(2, 8, device="cuda")
+    y, _ = g.gated_scan(x, gate, state, dim=1)
+    with torch.no_grad():
+        g.gated_step(x[:, 0], gate[:, 0], state)                       # the state that the backward pass needs
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.sum().backward()
+    with pytest.raises(ValueError, match="gated_scan"):
+        g.gated_step(x[:, 0], gate[:, 0], state)
+    with torch.inference_mode():
+        s = torch.zeros(2, 8, device="cuda")
+        assert torch.equal(g.gated_step(x[:, 0], gate[:, 0], s), s)
+    with pytest.raises(ValueError, match="save=False"):
+        y, last, saved = g.gated_scan_forward(x.detach(), gate, dim=1, save=False)
+        g.gated_scan_vjp(y, None, x.detach(), gate, saved, dim=1)
+
+
+@pytest.mark.parametrize("shape", [(1, 1, 4, 1200000001), (1, 1, 4, 1200000000), (1, 1200000000, 4, 1), (2, 3100000, 700, 1)])
+def test_arrays_beyond_32_bits(shape):
+    """Over 2^32 elements: places in the first, the last and a middle chain, which take patterns of their own."""
+    import paper_2207_08393_b200 as g
+    b, c, t, n = shape
+    x = torch.zeros(shape, dtype=torch.float16, device="cuda")
+    gate = torch.full(shape, -1.0, dtype=torch.float16, device="cuda")
+    chains = [(0, 0, 0), (b - 1, c - 1, n - 1), (b - 1, c * 9 // 10, n * 9 // 10)]
+    torch.manual_seed(8)
+    for i, j, k in chains:
+        x[i, j, :, k] = torch.randn(t, device="cuda").half()
+        gate[i, j, :, k] = torch.randn(t, device="cuda").half()
+    y, last, saved = g.gated_scan_forward(x, gate)
+    dx, dg, _ = g.gated_scan_vjp(x, None, x, gate, saved, state_grad=False)
+    for i, j, k in chains:
+        cut = lambda v: host(v[i, j, :, k]).reshape(1, 1, t, 1)
+        ry, rlast, before = so.forward(cut(x), cut(gate))
+        rdx, rdg, _ = so.vjp(cut(x), None, cut(x), cut(gate), before)
+        for got, ref in ((y, ry), (dx, rdx), (dg, rdg)):
+            close(got[i, j, :, k].reshape(1, 1, t, 1), ref, torch.float16, 500.0, "chain %d %d %d" % (i, j, k))
+        assert abs(float(last[i, j, k]) - float(rlast[0, 0, 0])) < 1e-4
+    assert int(torch.count_nonzero(last)) <= 3

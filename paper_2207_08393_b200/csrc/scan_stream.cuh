@@ -7,7 +7,9 @@
 //             own V neighbouring chains, and no thread waits for another;
 //   strips    rows start anywhere (an odd number of voxels): a block copies the 16-byte pieces that its strip of a row touches and reads
 //             from them element by element, lanes side by side; a thread's V chains are a block's width apart.
-// 60 x 20 x 30720 float32, forward and VJP: 293 us with loads into registers, <<PRIVATE>>.
+// Loads into registers instead (forward + VJP): 60 x 20 x 30720 float32 80 + 219 us for 69 + 127; 4 x 160 x 81920 bf16 335 + 583 for 70 + 126.
+// What is left there to the 48 and 80 that memory takes: half of the issue slots, two thirds of that the exponentials' and reciprocals'
+// pairs and conversions, and 640 blocks on 592 places.
 #pragma once
 #include "scan_common.cuh"
 
@@ -18,7 +20,7 @@ namespace scan {
 
 constexpr int STREAM_THREADS = 64, VJP_THREADS = 128;        // of a block
 constexpr int CHUNK = 8;                   // steps between saved states: what a VJP holds at a time
-constexpr int BATCH = 4, DEPTH = 4;        // steps of a copy group, and groups of the ring (forward)
+constexpr int BATCH = 4, DEPTH = 3;        // steps of a copy group, and groups of the ring (forward): more groups cost warps, fewer steps instructions
 
 // steps of a chunk: as few chunks as CHUNK allows, all alike
 inline int chunk_steps(long long steps) {

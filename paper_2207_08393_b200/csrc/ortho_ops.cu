@@ -42,12 +42,18 @@ static cudaError_t map_of(const Args& a, uint64_t bytes, CUtensorMap* map) {
                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
+// More than eight blocks to a cluster have to be allowed kernel by kernel.
+template <class K>
+static cudaError_t allow_clusters(K kernel, int ranks) {
+    return ranks > RESIDENT_PORTABLE ? cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) : cudaSuccess;
+}
+
 // Clusters of so many blocks, one block an SM, that the current device runs at once: its SMs come in groups that clusters do not
 // cross, so 16 clusters of 7 are more than 148 SMs may hold.
 static int clusters_at_once(int ranks) {
-    static PerDevice cache[RESIDENT_RANKS + 1];
+    static PerDevice cache[RESIDENT_RANKS + 1];                       // one more than the number
     std::atomic<int>* slot = cache[ranks].slot();
-    if (slot) { const int v = slot->load(std::memory_order_acquire); if (v > 0) return v; }
+    if (slot) { const int v = slot->load(std::memory_order_acquire); if (v > 0) return v - 1; }
     static PerDevice done;
     constexpr auto KERNEL = resident_kernel<float, false>;
     int n = 0;
@@ -55,11 +61,12 @@ static int clusters_at_once(int ranks) {
     cudaLaunchAttribute at[2];
     launch_config(cfg, at, false, dim3((unsigned)ranks), dim3(RESIDENT_THREADS), RESIDENT_MOST, nullptr, 2);
     at[0].val.clusterDim.x = (unsigned)ranks;
-    if (ensure_smem(KERNEL, RESIDENT_MOST, done) != cudaSuccess || cudaOccupancyMaxActiveClusters(&n, KERNEL, &cfg) != cudaSuccess || n < 1) {
+    if (ensure_smem(KERNEL, RESIDENT_MOST, done) != cudaSuccess || allow_clusters(KERNEL, ranks) != cudaSuccess ||
+        cudaOccupancyMaxActiveClusters(&n, KERNEL, &cfg) != cudaSuccess || n < 1) {
         cudaGetLastError();
-        return SMS / ranks;
+        n = ranks > RESIDENT_PORTABLE ? 0 : SMS / ranks;
     }
-    if (slot) slot->store(n, std::memory_order_release);
+    if (slot) slot->store(n + 1, std::memory_order_release);
     return n;
 }
 
@@ -96,31 +103,43 @@ static cudaError_t gemm(const Args& a, const CUtensorMap& map, int count, cudaSt
     return gemm_of<KIND, 1, T>(a, map, count, s);
 }
 
-// Tiles of a block of the resident kernel, 0 where a matrix does not fit a cluster.  More tiles mean fewer blocks: a turn takes about
-// four units and one more for each tile of a block, once for each round of clusters (`counted`; else any number that fits).
-static int resident_tiles(long long S, long long L, int count, bool counted) {
+// Whether a matrix fits a cluster that every GPU of this kind takes (eight blocks).
+static bool resident_fits(long long S, long long L) {
+    if (S > BLOCK) return false;
+    const long long all = (L + BLOCK - 1) / BLOCK;
+    for (int tiles = 1; resident_bytes(resident_rows(S), tiles) <= RESIDENT_MOST; ++tiles)
+        if ((all + tiles - 1) / tiles <= RESIDENT_PORTABLE) return true;
+    return false;
+}
+// Such calls of up to so many matrices have no workspace for the general kernels, which would not be faster.
+constexpr long long RESIDENT_COUNT = 8;
+
+// Tiles of a block of the resident kernel for a launch, 0 where the general kernels (if there is a workspace for them) take less time.  In
+// 0.1 us, from measured calls of five turns: a round of clusters 580 and 110 for each tile of a block (8 x 128 x 1152 70 us, 1 x 112 x 3500
+// 82); the general kernels 850 and 2.3 for each tile of all matrices (8 x 128 x 1152 109 us, 32 x 128 x 2048 205).
+static int resident_tiles(long long S, long long L, int count, bool general) {
     if (S > BLOCK) return 0;
     const long long all = (L + BLOCK - 1) / BLOCK;
     int best = 0;
-    long long least = 0;
+    long long least = general ? 850 + 23 * all * count / 10 : 0;
     for (int tiles = 1; tiles <= all && resident_bytes(resident_rows(S), tiles) <= RESIDENT_MOST; ++tiles) {
-        const int ranks = (int)((all + tiles - 1) / tiles);
-        if (ranks > RESIDENT_RANKS) continue;
-        if (!counted) return tiles;
-        const int at_once = clusters_at_once(ranks);
-        const long long time = (long long)((count + at_once - 1) / at_once) * (4 + tiles);
-        if (best == 0 || time < least) { best = tiles; least = time; }
+        const int ranks = (int)((all + tiles - 1) / tiles), at_once = ranks <= RESIDENT_RANKS ? clusters_at_once(ranks) : 0;
+        if (at_once == 0) continue;
+        const long long time = (count + at_once - 1) / at_once * (580 + 110 * tiles);
+        if (least == 0 || time < least) { best = tiles; least = time; }
     }
     return best;
 }
 
 template <class T, bool UPDATE>
 static cudaError_t run(Args& a, int count, int turns, cudaStream_t s) {
-    if (const int tiles = resident_tiles(a.S, a.L, count, true)) {
+    if (const int tiles = resident_tiles(a.S, a.L, count, a.x != nullptr)) {
         static PerDevice done;
         const cudaError_t e = ensure_smem(resident_kernel<T, UPDATE>, RESIDENT_MOST, done);
         if (e != cudaSuccess) return e;
         const unsigned ranks = (unsigned)((a.lblocks + tiles - 1) / tiles);
+        const cudaError_t allowed = allow_clusters(resident_kernel<T, UPDATE>, (int)ranks);
+        if (allowed != cudaSuccess) return allowed;
         ORTHO_LAUNCH(launch_overlapped_cluster(ranks, resident_kernel<T, UPDATE>, dim3(ranks, (unsigned)count), dim3(RESIDENT_THREADS),
                                                (size_t)resident_bytes(resident_rows(a.S), tiles), s, a, tiles, turns));
         return cudaSuccess;
@@ -164,7 +183,7 @@ static int layout_of(const gleam_matrix_dims* d, Layout* l) {
     l->group = (int)std::min<long long>(d->count, GROUP);
     l->x = l->square = l->part = 0;
     l->total = d->count && S ? 256 : 0;
-    if (l->total == 0 || resident_tiles(S, L, 1, false)) return GLEAM_OK;
+    if (l->total == 0 || (d->count <= RESIDENT_COUNT && resident_fits(S, L))) return GLEAM_OK;
     l->x = (uint64_t)l->group * l->sblocks * l->lblocks * BLOCK_BYTES;
     l->square = (uint64_t)l->group * l->sblocks * l->sblocks * BLOCK_BYTES;
     l->part = (uint64_t)GROUP * PARTS * sizeof(float);
@@ -232,7 +251,7 @@ static int orthogonal(const void* const* u, float* const* momenta, void* const* 
     a.status = (int*)(ws + l.total - 256);
     for (int64_t i0 = 0; i0 < d->count; i0 += GROUP) {
         const int count = (int)std::min<int64_t>(GROUP, d->count - i0);
-        a.x = ws; a.y = ws + l.x;
+        if (l.x) { a.x = ws; a.y = ws + l.x; }                          // null: no workspace for the general kernels
         for (int k = 0; k < count; ++k) {
             a.u[k] = u[i0 + k]; a.out[k] = out[i0 + k]; a.momentum[k] = m ? momenta[i0 + k] : nullptr;
         }

@@ -1,4 +1,4 @@
-// The whole update of a matrix whose shorter side is at most 128 in one launch: a cluster of up to eight blocks keeps X in shared memory
+// The whole update of a matrix whose shorter side is at most 128 in one launch: a cluster of up to sixteen blocks keeps X in shared memory
 // through all turns.
 //
 // A block holds up to seven tiles of 128 columns of X (all R rows of them, R = S rounded up to 16) as pieces.  In a turn it
@@ -15,7 +15,7 @@
 namespace gleam {
 namespace ortho {
 
-constexpr int RESIDENT_THREADS = 512, RESIDENT_RANKS = 8, RESIDENT_HEAD = 1024;
+constexpr int RESIDENT_THREADS = 512, RESIDENT_RANKS = 16, RESIDENT_PORTABLE = 8, RESIDENT_HEAD = 1024;
 constexpr int RESIDENT_LEAST = 120 * 1024;       // shared memory that keeps a second block, which would wait for tensor memory, off the SM
 constexpr int RESIDENT_MOST = 227 * 1024;
 
@@ -210,14 +210,17 @@ __global__ void __launch_bounds__(RESIDENT_THREADS, 1) resident_kernel(const __g
             tc::cluster_sync();
             for (int i = g0 * 256 + threadIdx.x; i < g1 * 256; i += RESIDENT_THREADS) {
                 if ((((i & 31) ^ (i >> 5)) & 31) * 4 >= R) continue;             // 16 bytes of a row beyond R
-                float4 f[RESIDENT_RANKS];
+                float4 total{0.f, 0.f, 0.f, 0.f};
+                for (int k0 = 0; k0 < ranks; k0 += 8) {                           // eight reads under way together
+                    float4 f[8];
 #pragma unroll
-                for (int k = 0; k < RESIDENT_RANKS; ++k)
-                    if (k < ranks) f[k] = tc::read_remote(sum_from + 16 * i, k);
+                    for (int k = 0; k < 8; ++k)
+                        if (k0 + k < ranks) f[k] = tc::read_remote(sum_from + 16 * i, k0 + k);
 #pragma unroll
-                for (int k = 1; k < RESIDENT_RANKS; ++k)
-                    if (k < ranks) { f[0].x += f[k].x; f[0].y += f[k].y; f[0].z += f[k].z; f[0].w += f[k].w; }
-                reinterpret_cast<float4*>(sum)[i] = f[0];                         // these rows of this block's sums are nobody else's
+                    for (int k = 0; k < 8; ++k)
+                        if (k0 + k < ranks) { total.x += f[k].x; total.y += f[k].y; total.z += f[k].z; total.w += f[k].w; }
+                }
+                reinterpret_cast<float4*>(sum)[i] = total;                        // these rows of this block's sums are nobody else's
             }
         }
         __syncthreads();

@@ -36,12 +36,12 @@ def tolerance(its, coefficients=COEFFICIENTS):
     """Frobenius norm of the error that pieces of 22 bits and 32-bit sums may leave, given the iterates in 64 bits.
 
     A turn stores X, A and P (2^-22 of each value), leaves out lo lo (2^-22 of a product) and adds K values in groups of 16 that a sum may
-    cut off rather than round (2^-23 each, K / 16 groups over three sums of a block, twice): d = 5 * 2^-22 + (K / 24 + 4) * 2^-23 of
-    |a| |X| + |b| |X|^3 + |c| |X|^5 with |X| <= 1.3, less than 14 times the Frobenius norm of X.  A later turn stretches an error at most by the
+    cut off rather than round (2^-23 of the sum each; A: K / 16 groups over two sums of a block, so K / 32 of them for a sum of all; P X: at
+    most K / 16; together under K / 10): d = 5 * 2^-22 + (K / 10 + 4) * 2^-23 of |a| |X| + |b| |X|^3 + |c| |X|^5 with |X| <= 1.3, less than 14 times the Frobenius norm of X.  A later turn stretches an error at most by the
     largest derivative of a v + b v^3 + c v^5, max(|a|, ...) over the values met, 5 here."""
     a, b, c = coefficients
     k = max(its[0].shape)
-    d = 5 * 2.0 ** -22 + (k / 24 + 4) * 2.0 ** -23
+    d = 5 * 2.0 ** -22 + (k / 10 + 4) * 2.0 ** -23
     grow = max(abs(a + 3 * b * v ** 2 + 5 * c * v ** 4) for v in np.linspace(0, 1.25, 100))
     total = 0.0
     for x in its[:-1]:

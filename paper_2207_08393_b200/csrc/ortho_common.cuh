@@ -13,10 +13,13 @@
 // to values of 2^-13.  The term a X is added in 32 bits.  Against 64 bits the result is as near as 32-bit products are, or nearer;
 // float16 or bfloat16 products without the second piece would be off by 1e-3 or 1e-2.
 //
-// Matrices are stored in blocks of 128 x 128 with zeros beyond their sides: a block is 32 KB of hi and 32 KB of lo, each as 16 x 16 cores
-// of 8 rows by 8 columns, a row of a core 16 bytes: the shape that the matrix instructions read, along either side.  An operand's tile
-// is a few copies of 8 KB for a piece: some of the rows lie in one run, 32 of the columns in 16 runs of 512 bytes, which a tiled copy
-// takes at once.  (With a copy for each run the copies, not the products, took the time: 4 x 512 x 4608, A: 89 us instead of 38.)
+// Matrices are stored in blocks of 128 x 128 with zeros beyond their sides, 64 KB: 16 rows of cores, in each those of hi, then those of lo, 16
+// cores of 8 rows by 8 columns, a row of a core 16 bytes: the shape that the matrix instructions read, along either side.  An operand's
+// tile is a few copies of 8 or 16 KB: rows lie in one run with both their pieces, 32 of the columns in runs of 512 bytes, which a tiled
+// copy takes at once.  (With a copy for each run the copies, not the products, took the time: 4 x 512 x 4608, A: 89 us instead of 38.)
+// In shared memory an operand's hi and lo lie one behind the other, so that one instruction with N = 256 gives hi hi and hi lo side by
+// side, and one with N = 128 adds lo hi to the latter.  These run at the tensor core's rate (64 cycles for 128 x 128 x 16, 4096 products a
+// cycle); instructions with N = 64 take as long, for the 128 rows of their other operand.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -31,7 +34,7 @@ namespace ortho {
 using prior::from_float;
 using prior::to_float;
 
-constexpr int BLOCK = 128, CORE = 128, PIECE_BYTES = BLOCK * BLOCK * 2, BLOCK_BYTES = 2 * PIECE_BYTES;
+constexpr int BLOCK = 128, CORE = 128, LO = 16 * CORE, ROW_BYTES = 2 * LO, BLOCK_BYTES = 16 * ROW_BYTES;    // from hi to lo; a row of cores
 constexpr float SCALE = 1024.f;
 constexpr int GROUP = 64;                          // matrices of a launch
 constexpr int PARTS = 592;                         // partial sums of squares of a matrix at most
@@ -51,8 +54,8 @@ struct Args {
     unsigned char* blocks;                         // all blocks of the workspace: what the tiled copies' map covers
 };
 
-// Byte of element (r, c) of a piece.
-__host__ __device__ __forceinline__ int core_at(int r, int c) { return ((r >> 3) * 16 + (c >> 3)) * CORE + (r & 7) * 16 + (c & 7) * 2; }
+// Byte of element (r, c) of a block's hi.
+__host__ __device__ __forceinline__ int core_at(int r, int c) { return (r >> 3) * ROW_BYTES + (c >> 3) * CORE + (r & 7) * 16 + (c & 7) * 2; }
 
 // A block's sums as 32-bit numbers in shared memory: rows of 128, their 16-byte pieces in an order that keeps 32 rows apart.
 __device__ __forceinline__ int sum_at(int r, int c) { return r * BLOCK + ((((c >> 2) ^ r) & 31) << 2) + (c & 3); }

@@ -18,14 +18,13 @@ namespace ortho {
 enum { GRAM, POLY, APPLY, LAST };
 
 constexpr int GEMM_THREADS = 256, STAGES = 3;
-// What a product holds.  GRAM and POLY: 64 of K a stage, one block an SM, sums in four parts: the tensor core cuts a sum off where it adds
-// (2^-23 of it each time), which tells in the diagonal of A, all of whose terms are positive; three sums of hi hi in turn and one of the
-// rest cut off a third as often.  APPLY: few terms, of either sign; 32 of K a stage and two sums leave room for a second block on the SM,
-// whose products run while this one finishes (9216 x 1024: 57 -> 46 us).
+// What a product holds.  GRAM and POLY: 64 of K a stage, one block an SM, two sums in turn (each of hi hi and of the rest): the tensor core
+// cuts a sum off where it adds (2^-23 of it each time), which tells in the diagonal of A, all of whose terms are positive, and two sums cut
+// off half as often.  APPLY: few terms, of either sign; 32 of K a stage and one sum leave room for a second block on the SM, whose products run while this one finishes (9216 x 1024: 57 -> 46 us).
 template <int KIND> struct Form {
     static constexpr bool SIDES = KIND == GRAM || KIND == POLY;                // both operands are rows of one matrix
-    static constexpr int STEP = SIDES ? 64 : 32, SUMS = SIDES ? 3 : 1, COLUMNS = (SUMS + 1) * BLOCK, BLOCKS = SIDES ? 1 : 2;
-    static constexpr int PART = BLOCK * STEP * 2, OPERAND = 2 * PART, STAGE = 2 * OPERAND;      // bytes of a piece, both pieces, both operands
+    static constexpr int STEP = SIDES ? 64 : 32, SUMS = SIDES ? 2 : 1, COLUMNS = SUMS * 2 * BLOCK, BLOCKS = SIDES ? 1 : 2;
+    static constexpr int OPERAND = 2 * BLOCK * STEP * 2, STAGE = 2 * OPERAND;                   // bytes of an operand's pieces, of both operands
     static constexpr int SMEM = 1024 + STAGES * STAGE;                         // the first KB: barriers
 };
 
@@ -76,26 +75,27 @@ __global__ void __launch_bounds__(GEMM_THREADS, Form<KIND>::BLOCKS) gemm_kernel(
     bool failed = false;
 
     if (warp == 0 && lane == 0) {
-        // rows of 2 KB (eight rows of a block) from the first block to left's and right's
-        const long long lrow = (left - a.blocks) / 2048 + (long long)bi * lblocks * 32, rrow = (right - a.blocks) / 2048 + (long long)bj * lblocks * 32;
+        // rows of cores from the first block to left's and right's
+        const long long lrow = (left - a.blocks) / ROW_BYTES + (long long)bi * lblocks * 16, rrow = (right - a.blocks) / ROW_BYTES + (long long)bj * lblocks * 16;
         for (int i = 0; i < count; ++i) {
             const int s = i % STAGES, k = first + i, kb = k / PARTS_OF_BLOCK, share = k % PARTS_OF_BLOCK;
             if (i >= STAGES && !tc::barrier_wait(empty(s), (i / STAGES - 1) & 1)) { failed = true; break; }
             const uint32_t to = stages + s * F::STAGE;
             tc::barrier_expect(full(s), one ? F::OPERAND : F::STAGE);
 #pragma unroll
-            for (int piece = 0; piece < 2; ++piece) {
-                const uint32_t at = to + piece * F::PART;
+            for (int h = 0; h < STEP / 32; ++h) {
 #pragma unroll
-                for (int h = 0; h < STEP / 32; ++h) {                       // 32 columns of 128 rows: 8 KB
-                    tc::tiled_copy(at + h * 8192, &map, share * (STEP / 32) + h, (int)(lrow + kb * 32 + piece * 16), full(s));
-                    if (SIDES && !one) tc::tiled_copy(at + F::OPERAND + h * 8192, &map, share * (STEP / 32) + h, (int)(rrow + kb * 32 + piece * 16), full(s));
+                for (int piece = 0; piece < 2; ++piece) {                   // 32 columns of 128 rows: 8 KB
+                    const uint32_t at = to + h * 16384 + piece * 8192;
+                    const int part = piece * 4 + share * (STEP / 32) + h;
+                    tc::tiled_copy(at, &map, part, (int)(lrow + kb * 16), full(s));
+                    if (SIDES && !one) tc::tiled_copy(at + F::OPERAND, &map, part, (int)(rrow + kb * 16), full(s));
                 }
-                if (!SIDES) tc::bulk_copy(at + F::OPERAND, right + ((long long)kb * a.lblocks + bj) * BLOCK_BYTES + piece * PIECE_BYTES + share * F::PART, F::PART, full(s));
             }
+            if (!SIDES) tc::bulk_copy(to + F::OPERAND, right + ((long long)kb * a.lblocks + bj) * BLOCK_BYTES + share * F::OPERAND, F::OPERAND, full(s));
         }
     } else if (warp == 1 && lane == 0) {
-        const uint32_t what = tc::instruction(BLOCK, !SIDES);
+        const uint32_t both = tc::instruction(2 * BLOCK, !SIDES), what = tc::instruction(BLOCK, !SIDES);
         for (int i = 0; i < count; ++i) {
             const int s = i % STAGES;
             if (!tc::barrier_wait(full(s), (i / STAGES) & 1)) {
@@ -104,17 +104,15 @@ __global__ void __launch_bounds__(GEMM_THREADS, Form<KIND>::BLOCKS) gemm_kernel(
                 break;
             }
             tc::fence_after();
-            const uint32_t l = stages + s * F::STAGE, r = one ? l : l + F::OPERAND;
+            const uint32_t l = stages + s * F::STAGE, r = one ? l : l + F::OPERAND, to = sums + i % SUMS * 2 * BLOCK;
 #pragma unroll
             for (int q = 0; q < STEP / 16; ++q) {
-                // cores of left: 512 bytes from one to the next along M, 128 along K; of right (!SIDES): 128 along N, 2048 along K
-                const uint32_t rows_at = (q >> 1) * 8192 + (q & 1) * 256;
-                const uint64_t lh = tc::descriptor(l + rows_at, 128, 512), ll = tc::descriptor(l + F::PART + rows_at, 128, 512);
-                const uint64_t rh = SIDES ? tc::descriptor(r + rows_at, 128, 512) : tc::descriptor(r + q * 4096, 2048, 128);
-                const uint64_t rl = SIDES ? tc::descriptor(r + F::PART + rows_at, 128, 512) : tc::descriptor(r + F::PART + q * 4096, 2048, 128);
-                tc::product(sums + SUMS * BLOCK, ll, rh, what, i > 0 || q > 0);
-                tc::product(sums + SUMS * BLOCK, lh, rl, what, true);
-                tc::product(sums + i % SUMS * BLOCK, lh, rh, what, i >= SUMS || q > 0);
+                // cores of left: 512 bytes from one to the next along M, 128 along K; of right (!SIDES): 128 along N, 4096 along K
+                const uint32_t at = (q >> 1) * 16384 + (q & 1) * 256;
+                const uint64_t lh = tc::descriptor(l + at, 128, 512), ll = tc::descriptor(l + 8192 + at, 128, 512);
+                const uint64_t rb = SIDES ? tc::descriptor(r + at, 128, 512) : tc::descriptor(r + q * 8192, 4096, 128);       // hi, then lo
+                tc::product(to, lh, rb, both, i >= SUMS || q > 0);
+                tc::product(to + BLOCK, ll, rb, what, true);
             }
             tc::commit(empty(s));
         }
@@ -134,7 +132,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, Form<KIND>::BLOCKS) gemm_kernel(
         for (int k = 0; k < AHEAD; ++k) {
             if (!has(k0 + k)) break;
             old_hi[k] = *reinterpret_cast<const uint4*>(old + core_at(row_of(k0 + k), col));
-            old_lo[k] = *reinterpret_cast<const uint4*>(old + PIECE_BYTES + core_at(row_of(k0 + k), col));
+            old_lo[k] = *reinterpret_cast<const uint4*>(old + LO + core_at(row_of(k0 + k), col));
         }
     };
     if (KIND != GRAM) fetch(0);
@@ -150,13 +148,16 @@ __global__ void __launch_bounds__(GEMM_THREADS, Form<KIND>::BLOCKS) gemm_kernel(
             const uint32_t at = sums + ((uint32_t)((warp & 3) * 32) << 16) + c0;
             float v[32], t[32];
             tc::read_columns(at, v);
-#pragma unroll 1
-            for (int k = 1; k < SUMS && k < count; ++k) {
-                tc::read_columns(at + k * BLOCK, t);
+            tc::read_columns(at + BLOCK, t);
+            if (SUMS > 1 && count > 1) {
+                float u[32];
+                tc::read_columns(at + 2 * BLOCK, u);
 #pragma unroll
-                for (int j = 0; j < 32; ++j) v[j] += t[j];
+                for (int j = 0; j < 32; ++j) v[j] += u[j];
+                tc::read_columns(at + 3 * BLOCK, u);
+#pragma unroll
+                for (int j = 0; j < 32; ++j) t[j] += u[j];
             }
-            tc::read_columns(at + SUMS * BLOCK, t);
 #pragma unroll
             for (int j = 0; j < 32; j += 4)
                 *reinterpret_cast<float4*>(sum + sum_at(row, c0 + j)) = make_float4((v[j] + t[j]) * (1.f / SCALE), (v[j + 1] + t[j + 1]) * (1.f / SCALE),
@@ -209,7 +210,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, Form<KIND>::BLOCKS) gemm_kernel(
         uint4 hi, lo;
         split8(v, hi, lo);
         *reinterpret_cast<uint4*>(block + core_at(r, c)) = hi;
-        *reinterpret_cast<uint4*>(block + PIECE_BYTES + core_at(r, c)) = lo;
+        *reinterpret_cast<uint4*>(block + LO + core_at(r, c)) = lo;
     };
     const long long rows = a.S - (long long)bi * BLOCK, cols = (SIDES ? a.S : a.L) - (long long)bj * BLOCK;
     if (KIND != LAST) {
@@ -236,7 +237,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, Form<KIND>::BLOCKS) gemm_kernel(
                 for (int k = 0; k < ITEMS; ++k) {
                     if (!has(k)) break;
                     old_hi[k % AHEAD] = *reinterpret_cast<const uint4*>(a.g + at + core_at(mirror_row(k), mirror_col(k)));
-                    old_lo[k % AHEAD] = *reinterpret_cast<const uint4*>(a.g + at + PIECE_BYTES + core_at(mirror_row(k), mirror_col(k)));
+                    old_lo[k % AHEAD] = *reinterpret_cast<const uint4*>(a.g + at + LO + core_at(mirror_row(k), mirror_col(k)));
                 }
             }
 #pragma unroll

@@ -19,8 +19,8 @@ namespace ortho {
 
 constexpr int SMS = 148;
 
-// The tiled copies' map: the workspace's blocks as rows of 2 KB (eight rows of a block), each four parts of 512 bytes; a copy takes one part
-// of 16 rows, 32 columns of 128 rows.  cuTensorMapEncodeTiled comes through the runtime's lookup: no link-time dependency on the driver.
+// The tiled copies' map: the workspace's blocks as rows of cores, each eight parts of 512 bytes (32 columns, of hi and then of lo); a copy
+// takes one part of 16 rows.  cuTensorMapEncodeTiled comes through the runtime's lookup: no link-time dependency on the driver.
 static cudaError_t map_of(const Args& a, uint64_t bytes, CUtensorMap* map) {
     typedef CUresult (*Encode)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
                                const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -36,7 +36,7 @@ static cudaError_t map_of(const Args& a, uint64_t bytes, CUtensorMap* map) {
         encode = (Encode)p;
         kept.store(encode, std::memory_order_release);
     }
-    const cuuint64_t dims[3] = {128, 4, bytes / 2048}, strides[2] = {512, 2048};
+    const cuuint64_t dims[3] = {128, 8, bytes / ROW_BYTES}, strides[2] = {512, ROW_BYTES};
     const cuuint32_t box[3] = {128, 1, 16}, steps[3] = {1, 1, 1};
     return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 3, a.blocks, dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;

@@ -139,7 +139,7 @@ __global__ void __launch_bounds__(PREPARE_THREADS) first_kernel(const __grid_con
         uint4 hi, lo;
         split8(v, hi, lo);
         *reinterpret_cast<uint4*>(block + core_at(r, c)) = hi;
-        *reinterpret_cast<uint4*>(block + PIECE_BYTES + core_at(r, c)) = lo;
+        *reinterpret_cast<uint4*>(block + LO + core_at(r, c)) = lo;
     }
 }
 

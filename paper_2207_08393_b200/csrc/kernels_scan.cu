@@ -51,7 +51,7 @@ static void plan(Args& a, long long* saved, long long* scratch) {
         threads = 16 * a.rows;                       // half a warp: series take twice the warps of columns, a tile's shuffles are slow
         *saved = ceil_div(a.rows, a.run) * units;
     }
-    const long long wanted = SMS * 512;
+    const long long wanted = SMS * (a.inner > 1 ? 640 : 512);
     if (a.run == 1 && units >= 4 && threads < wanted / 2) {
         long long parts = wanted / threads;
         if (parts > units / 2) parts = units / 2;

@@ -18,7 +18,7 @@ namespace scan {
 
 // ---- short chains
 
-constexpr int SHORT_BYTES = 128, SHORT_ROWS = 128;
+constexpr int SHORT_BYTES = 128, SHORT_ROWS = 128, SHORT_CHUNK = 8;      // steps between the VJP's states
 template <class T> constexpr int SHORT_STEPS = SHORT_BYTES / sizeof(T);
 
 // Where byte b of the block's part of an array stands.  Neighbouring chains of 16, 32, 64 or 128 bytes would share their banks: there 16
@@ -29,7 +29,7 @@ template <class T> __host__ __device__ inline int short_array(long long steps) {
     return (skewed((int)(SHORT_ROWS * steps * sizeof(T)), short_skews((int)(steps * sizeof(T)))) + 31) / 16 * 16;
 }
 template <class T, int KIND> __host__ inline size_t short_smem(long long steps) {
-    return KIND == VJP ? 3 * (size_t)short_array<T>(steps) + sizeof(float) * SHORT_ROWS * (SHORT_STEPS<T> / CHUNK) : 2 * (size_t)short_array<T>(steps);
+    return KIND == VJP ? 3 * (size_t)short_array<T>(steps) + sizeof(float) * SHORT_ROWS * (SHORT_STEPS<T> / SHORT_CHUNK) : 2 * (size_t)short_array<T>(steps);
 }
 
 // Two neighbouring steps t and t + 1 of a chain.  WHOLE: as one number of 32 bits (16-bit types, an even number of steps).
@@ -123,7 +123,7 @@ __global__ void __launch_bounds__(SHORT_ROWS) short_kernel(const __grid_constant
             float* starts = reinterpret_cast<float*>(ring + 3 * bytes) + threadIdx.x;     // states at the chunks' starts
             for (int p = 0; p < pairs; ++p) {
                 const int t = low(p);
-                if (p % (CHUNK / 2) == 0) starts[p / (CHUNK / 2) * SHORT_ROWS] = h;
+                if (p % (SHORT_CHUNK / 2) == 0) starts[p / (SHORT_CHUNK / 2) * SHORT_ROWS] = h;
                 Two f, rest;
                 gates_of(turned(steps_at<T, WHOLE>(gs, t)), f, rest);
                 const Two u = rest * turned(steps_at<T, WHOLE>(xs, t));
@@ -143,11 +143,11 @@ __global__ void __launch_bounds__(SHORT_ROWS) short_kernel(const __grid_constant
                 xs[odd] = from_float<T>(ox);
                 gs[odd] = from_float<T>(og);
             }
-            for (int p0 = (pairs - 1) / (CHUNK / 2) * (CHUNK / 2); p0 >= 0 && pairs > 0; p0 -= CHUNK / 2) {
-                Two f[CHUNK / 2], rest[CHUNK / 2], w[CHUNK / 2];
-                h = starts[p0 / (CHUNK / 2) * SHORT_ROWS];
+            for (int p0 = (pairs - 1) / (SHORT_CHUNK / 2) * (SHORT_CHUNK / 2); p0 >= 0 && pairs > 0; p0 -= SHORT_CHUNK / 2) {
+                Two f[SHORT_CHUNK / 2], rest[SHORT_CHUNK / 2], w[SHORT_CHUNK / 2];
+                h = starts[p0 / (SHORT_CHUNK / 2) * SHORT_ROWS];
 #pragma unroll
-                for (int k = 0; k < CHUNK / 2; ++k) {
+                for (int k = 0; k < SHORT_CHUNK / 2; ++k) {
                     if (p0 + k >= pairs) break;
                     const int t = low(p0 + k);
                     gates_of(turned(steps_at<T, WHOLE>(gs, t)), f[k], rest[k]);
@@ -158,7 +158,7 @@ __global__ void __launch_bounds__(SHORT_ROWS) short_kernel(const __grid_constant
                     if (there(t, 1)) h = fmaf(f[k].hi(), h, u.hi());
                 }
 #pragma unroll
-                for (int k = CHUNK / 2 - 1; k >= 0; --k) {
+                for (int k = SHORT_CHUNK / 2 - 1; k >= 0; --k) {
                     if (p0 + k >= pairs) continue;
                     const int t = low(p0 + k);
                     const Two d = turned(steps_at<T, WHOLE>(ds, t));

@@ -19,7 +19,7 @@ namespace gleam {
 namespace scan {
 
 constexpr int STREAM_THREADS = 64, VJP_THREADS = 128;        // of a block
-constexpr int CHUNK = 8;                   // steps between saved states: what a VJP holds at a time
+constexpr int CHUNK = 6;                   // steps between saved states: what a VJP holds at a time
 constexpr int BATCH = 4, DEPTH = 3;        // steps of a copy group, and groups of the ring (forward): more groups cost warps, fewer steps instructions
 
 // steps of a chunk: as few chunks as CHUNK allows, all alike
@@ -291,7 +291,7 @@ __global__ void __launch_bounds__(STREAM_THREADS) stream_kernel(const __grid_con
 
 // VJP: chunk by chunk from the part's end, the next chunk on its way.  The states before each step come from the saved one.
 template <class T, int V, bool REVERSE, bool STRIP>
-__global__ void __launch_bounds__(VJP_THREADS, 4) stream_vjp(const __grid_constant__ Args a) {
+__global__ void __launch_bounds__(VJP_THREADS, STRIP ? 6 : 5) stream_vjp(const __grid_constant__ Args a) {
     extern __shared__ __align__(16) unsigned char ring[];
     grid_dependency_wait();
     using R = Rows<T, V, STRIP, VJP_THREADS>;

@@ -26,6 +26,7 @@ using T = __nv_bfloat16;
                               if (e_ != cudaSuccess) return e_; } while (0)
 
 constexpr int SMS = 148, WIDE = 8 / sizeof(T);           // chains of a thread's piece of 8 bytes
+constexpr int PARTS_MOST = 512;                         // more of them would take the launch that joins them longer than they save
 constexpr int NARROW = 128;                              // rows of fewer chains, where they start anywhere, are no strips
 
 static long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
@@ -55,7 +56,7 @@ static void plan(Args& a, long long* saved, long long* scratch) {
     if (a.run == 1 && units >= 4 && threads < wanted / 2) {
         long long parts = wanted / threads;
         if (parts > units / 2) parts = units / 2;
-        if (parts > 4096) parts = 4096;
+        if (parts > PARTS_MOST) parts = PARTS_MOST;
         const long long each = ceil_div(units, parts);
         a.part = each * a.chunk;
         a.parts = (int)ceil_div(units, each);

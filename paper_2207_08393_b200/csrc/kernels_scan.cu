@@ -119,12 +119,11 @@ static cudaError_t stream(const Args& a, cudaStream_t s) {
     return cudaSuccess;
 }
 
-// MAP_V: chains of a thread where the maps of parts are formed
-template <int V, bool REVERSE, bool STRIP, bool BACK, int MAP_V = V>
+template <int V, bool REVERSE, bool STRIP, bool BACK>
 static cudaError_t streams(const Args& a, cudaStream_t s) {
     cudaError_t e;
     if (a.parts > 1) {
-        if ((e = stream<MAP_V, REVERSE, STRIP, BACK ? MAP_VJP : MAP_FORWARD>(a, s)) != cudaSuccess) return e;
+        if ((e = stream<V, REVERSE, STRIP, BACK ? MAP_VJP : MAP_FORWARD>(a, s)) != cudaSuccess) return e;
         if ((e = join(a, BACK, BACK, s)) != cudaSuccess) return e;
     }
     return stream<V, REVERSE, STRIP, BACK ? VJP : FORWARD>(a, s);
@@ -176,9 +175,9 @@ static cudaError_t chains(const Args& a, bool reverse, std::initializer_list<Arr
     return by_bool(reverse, [&](auto r) {
         constexpr bool R = decltype(r)::value;
         if (a.inner == 1) return by_bool(dense(a, arrays), [&](auto d) { return rows<R, decltype(d)::value, BACK>(a, s); });
-        // pieces of 16 bytes where there are chains enough: fewer instructions (8 x 512 x 45000 float16 forward 275 -> 212 us; where there are
-        // not, 8000 x 2048, 35 -> 37).  The VJP keeps too much of each chain for that, but not the maps of its parts.
-        if (a.rows * a.parts / (2 * WIDE) >= SMS * 192 && wide(a, 2 * WIDE, arrays, states)) return streams<BACK ? WIDE : 2 * WIDE, R, false, BACK, 2 * WIDE>(a, s);
+        // pieces of 16 bytes where there are chains enough: fewer instructions (8 x 512 x 45000 float16: forward 275 -> 212 us, VJP 377 -> 344;
+        // where there are not, 8000 x 2048 bf16, forward 35 -> 37)
+        if (a.rows * a.parts / (2 * WIDE) >= SMS * 192 && wide(a, 2 * WIDE, arrays, states)) return streams<2 * WIDE, R, false, BACK>(a, s);
         if (wide(a, WIDE, arrays, states)) return streams<WIDE, R, false, BACK>(a, s);
         if (a.inner >= NARROW) return streams<WIDE, R, true, BACK>(a, s);
         return columns<R, BACK>(a, s);

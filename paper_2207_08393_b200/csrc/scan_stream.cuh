@@ -2,14 +2,15 @@
 // shared memory by asynchronous copies, several steps ahead of their use.
 //
 // What bounds it is memory; what it takes is bytes under way (about 40 KB an SM) that cost no registers, and enough warps that the
-// chains' arithmetic (some 12 instructions an element forward, 25 for the VJP) hides behind them.  Two forms:
+// chains' arithmetic (some 18 instructions an element forward, 35 for the VJP) hides behind them.  Two forms:
 //   private   every row of every array starts at a multiple of a thread's piece (16 or 8 bytes): a thread copies, reads and stores its
 //             own V neighbouring chains, and no thread waits for another;
 //   strips    rows start anywhere (an odd number of voxels): a block copies the 16-byte pieces that its strip of a row touches and reads
 //             from them element by element, lanes side by side; a thread's V chains are a block's width apart.
-// Loads into registers instead (forward + VJP): 60 x 20 x 30720 float32 80 + 219 us for 69 + 127; 4 x 160 x 81920 bf16 335 + 583 for 70 + 126.
-// What is left there to the 48 and 80 that memory takes: half of the issue slots, two thirds of that the exponentials' and reciprocals'
-// pairs and conversions, and 640 blocks on 592 places.
+// Loads into registers instead (forward + VJP): 60 x 20 x 30720 float32 80 + 219 us for 70 + 117; 4 x 160 x 81920 bf16 335 + 583 for 60 + 103.
+// What is left there to the 48 and 80 that memory takes: half of the issue slots, two thirds of that exponentials, reciprocals and
+// conversions, in as few warps as there are chains for. The VJP keeps two numbers an element of a chunk in registers: six steps leave room
+// for a fifth (pieces of 8 bytes) or third block (16) on the SM; with eight, 60 x 20 x 30720 took 127 and 4 x 160 x 81920 126.
 #pragma once
 #include "scan_common.cuh"
 
@@ -291,7 +292,7 @@ __global__ void __launch_bounds__(STREAM_THREADS) stream_kernel(const __grid_con
 
 // VJP: chunk by chunk from the part's end, the next chunk on its way.  The states before each step come from the saved one.
 template <class T, int V, bool REVERSE, bool STRIP>
-__global__ void __launch_bounds__(VJP_THREADS, STRIP ? 6 : 5) stream_vjp(const __grid_constant__ Args a) {
+__global__ void __launch_bounds__(VJP_THREADS, V * sizeof(T) == 16 ? 3 : STRIP ? 6 : 5) stream_vjp(const __grid_constant__ Args a) {
     extern __shared__ __align__(16) unsigned char ring[];
     grid_dependency_wait();
     using R = Rows<T, V, STRIP, VJP_THREADS>;

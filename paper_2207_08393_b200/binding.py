@@ -284,6 +284,11 @@ def _addr(t):
         return t
 
 
+def _at(t):
+    """``_addr`` where addresses and None are frequent: an exception costs more than the rest of a call's marshalling."""
+    return t if t is None or t.__class__ is int else t.data_ptr()
+
+
 def _check(status: int):
     if status:
         raise GleamError(status, gleam_status_string(status))
@@ -495,7 +500,7 @@ def make_scan_dims(dtype, batch, channels, steps, inner, reverse=False, strides=
         workspace_bytes = workspace.numel() * workspace.element_size()
         workspace = workspace.data_ptr()
     flat = tuple(v for s in strides for v in s)
-    return gleam_scan_dims(1, dtype, int(reverse), 0, batch, channels, steps, inner, flat, _addr(lengths) or None, stream or None,
+    return gleam_scan_dims(1, dtype, int(reverse), 0, batch, channels, steps, inner, flat, _at(lengths) or None, stream or None,
                            workspace or None, workspace_bytes)
 
 
@@ -513,19 +518,19 @@ def gleam_gated_scan_saved_size(dims: gleam_scan_dims) -> int:
 
 def gleam_gated_scan_forward(x, gate, state, y, last, saved, dims: gleam_scan_dims) -> None:
     """h_t = f_t h_(t-1) + (1 - f_t) x_t with f = sigmoid(gate); state, last and saved may be None."""
-    _check((_lib or load_library()).gleam_gated_scan_forward(_addr(x), _addr(gate), _addr(state), _addr(y), _addr(last),
-                                                             _addr(saved), ctypes.byref(dims)))
+    _check((_lib or load_library()).gleam_gated_scan_forward(_at(x), _at(gate), _at(state), _at(y), _at(last),
+                                                             _at(saved), ctypes.byref(dims)))
 
 
 def gleam_gated_scan_vjp(grad_y, grad_last, x, gate, state, saved, grad_x, grad_gate, grad_state, dims: gleam_scan_dims) -> None:
-    _check((_lib or load_library()).gleam_gated_scan_vjp(_addr(grad_y), _addr(grad_last), _addr(x), _addr(gate), _addr(state),
-                                                         _addr(saved), _addr(grad_x), _addr(grad_gate), _addr(grad_state),
+    _check((_lib or load_library()).gleam_gated_scan_vjp(_at(grad_y), _at(grad_last), _at(x), _at(gate), _at(state),
+                                                         _at(saved), _at(grad_x), _at(grad_gate), _at(grad_state),
                                                          ctypes.byref(dims)))
 
 
 def gleam_gated_step(x, gate, state, y, dims: gleam_scan_dims) -> None:
     """One step; state is updated in place."""
-    _check((_lib or load_library()).gleam_gated_step(_addr(x), _addr(gate), _addr(state), _addr(y), ctypes.byref(dims)))
+    _check((_lib or load_library()).gleam_gated_step(_at(x), _at(gate), _at(state), _at(y), ctypes.byref(dims)))
 
 
 def make_matrix_dims(dtype, count, rows, cols, turns=5, coefficients=(3.4445, -4.7750, 2.0315), eps=1e-7, stream=None, workspace=None,
@@ -542,7 +547,7 @@ def make_matrix_dims(dtype, count, rows, cols, turns=5, coefficients=(3.4445, -4
 
 def _addresses(tensors):
     """Host array of the matrices' device addresses."""
-    return (ctypes.c_void_p * max(len(tensors), 1))(*[_addr(t) for t in tensors])
+    return (ctypes.c_void_p * max(len(tensors), 1))(*[_at(t) for t in tensors])
 
 
 def gleam_orthogonalise_workspace_size(dims: gleam_matrix_dims) -> int:

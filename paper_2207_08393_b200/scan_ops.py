@@ -54,7 +54,7 @@ class _Chains:
             _check_sign(t)
             strides += self._strides(t, what)
         _check_lengths(x, dim, lengths)
-        self.dims = _b.gleam_scan_dims(1, _DTYPES[x.dtype], bool(reverse), 0, *self.sizes, strides, _b._addr(lengths), _stream(x) or None,
+        self.dims = _b.gleam_scan_dims(1, _DTYPES[x.dtype], bool(reverse), 0, *self.sizes, strides, _b._at(lengths), _stream(x) or None,
                                        None, 0)
         self.sizes_of_scratch = None
 

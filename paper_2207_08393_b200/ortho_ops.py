@@ -135,6 +135,13 @@ class Muon(torch.optim.Optimizer):
         return loss
 
     def load_state_dict(self, state):
+        names = [i for group in state["param_groups"] for i in group["params"]]
+        momenta = {i: s["momentum"] for i, s in state["state"].items() if "momentum" in s}
+        params = [p for group in self.param_groups for p in group["params"]]
+        for i, p in zip(names, params):
+            if i in momenta and momenta[i].shape != p.shape:
+                raise ValueError("momentum of shape %s for a parameter of shape %s" % (tuple(momenta[i].shape), tuple(p.shape)))
         super().load_state_dict(state)
-        for s in self.state.values():                      # the base class gives a state its parameter's type, and may share it
-            s["momentum"] = torch.empty(s["momentum"].shape, dtype=torch.float32, device=s["momentum"].device).copy_(s["momentum"])
+        for i, p in zip(names, params):                    # the base class rounds a state to its parameter's type, and may share it
+            if i in momenta:
+                self.state[p]["momentum"] = torch.empty(p.shape, dtype=torch.float32, device=p.device).copy_(momenta[i])

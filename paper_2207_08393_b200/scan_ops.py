@@ -121,7 +121,7 @@ _new_dims = _b.gleam_scan_dims.from_buffer_copy
 
 def _chains(x, dim, reverse, lengths, *others):
     """``_Chains`` of a call; where all tensors are contiguous its structure is copied from a kept one (filling one takes longer than a small
-    kernel: forward and VJP of 3 x 5 x 20 x 33 42 -> 32 us a pair)."""
+    kernel: forward and VJP of 3 x 5 x 20 x 33 55 -> 43 us a pair)."""
     if not _plain(x, *[t for t, _ in others]):
         return _Chains(x, dim, reverse, lengths, *others)
     key = x.shape, x.dtype, dim, bool(reverse)

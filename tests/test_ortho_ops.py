@@ -138,3 +138,29 @@ def test_priors_along_frames_are_asked_for():
     assert [type(o).__name__ for o in opt.optimizers] == ["Muon", "Adam"]
     with pytest.raises(ValueError):
         opt.load_state_dict([])
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16, torch.float32])
+def test_a_loaded_momentum_keeps_its_32_bits(dtype):
+    """Whatever the weights' type: a run that is taken up again goes on with the very same momenta."""
+    torch.manual_seed(3)
+    a = [torch.nn.Parameter(torch.randn(5, 7).to(dtype)) for _ in range(3)]
+    opt = g.Muon([{"params": a[:1]}, {"params": a[1:], "lr": 0.5}])
+    for p in a[:1] + a[2:]:                                        # one has not been updated yet
+        opt.state[p]["momentum"] = torch.randn(5, 7)
+    kept = opt.state_dict()
+    b = [torch.nn.Parameter(p.detach().clone()) for p in a]
+    other = g.Muon([{"params": b[:1]}, {"params": b[1:]}])
+    other.load_state_dict(kept)
+    assert other.param_groups[1]["lr"] == 0.5 and "momentum" not in other.state[b[1]]
+    for p, q in ((a[0], b[0]), (a[2], b[2])):
+        m = other.state[q]["momentum"]
+        assert m.dtype == torch.float32 and torch.equal(m, opt.state[p]["momentum"]) and m.data_ptr() != opt.state[p]["momentum"].data_ptr()
+
+
+def test_a_loaded_momentum_has_its_weights_shape():
+    a, b = torch.nn.Parameter(torch.zeros(4, 6)), torch.nn.Parameter(torch.zeros(6, 6))
+    opt = g.Muon([a])
+    opt.state[a]["momentum"] = torch.zeros(1, 6)
+    with pytest.raises(ValueError):
+        g.Muon([b]).load_state_dict(opt.state_dict())

@@ -394,13 +394,13 @@ GLEAM_API int gleam_gated_scan_saved_size(const gleam_scan_dims* dims, uint64_t*
  *                  weight <- (1 - lr weight_decay) weight - lr scale orthogonalise(U)
  *
  * The pointers lie in host arrays, one device address for each of `count` matrices (rows, cols), contiguous.  x, out, weights and grads
- * have type dtype, momenta are float32.  The norm is a 32-bit sum.  Products are as exact as 32-bit ones (float16 pieces of 22 bits,
- * 32-bit sums); |a|, |b|, |c| <= 16, and singular values have to stay below 8 along the way (those of the usual coefficients stay below
- * 1.3).  A matrix of zeros gives zeros; one with a NaN or an infinity gives NaN throughout, the others are untouched by it.  The shorter
- * side is at most 16384, and there are at most 65535 blocks of 128 x 128 in a matrix.  GLEAM_ERR_CUDA also reports that the host has no
- * memory left for a call's checks.  Nothing that a call writes may overlap
- * anything else of the call (GLEAM_ERR_ALIAS).  Results are deterministic.  Two calls whose GPU work may overlap need workspaces of
- * their own.
+ * have type dtype, momenta are float32.  The norm is a 32-bit sum of squares: a norm above 1.8e19 overflows and gives zeros, as in any
+ * such sum.  Products are as exact as 32-bit ones (float16 pieces of 22 bits, 32-bit sums); |a|, |b|, |c| <= 16, and singular
+ * values have to stay below 8 along the way (those of the usual coefficients stay below 1.3).  A matrix of zeros gives zeros; one with
+ * a NaN or an infinity gives NaN throughout, the others are untouched by it.  The shorter side is at most 16384, and there are at most
+ * 65535 blocks of 128 x 128 in a matrix.  GLEAM_ERR_CUDA also reports that the host has no memory left for a call's checks.
+ * Nothing that a call writes may overlap anything else of the call (GLEAM_ERR_ALIAS).  Results are deterministic.  Two calls whose
+ * GPU work may overlap need workspaces of their own.
  */
 #define GLEAM_MATRIX_DIMS_VERSION 1
 typedef struct {

@@ -47,6 +47,7 @@ struct Args {
     int tall, dtype;                               // GLEAM_F32, ...
     int sblocks, lblocks, parts;
     int update, nesterov;
+    int fresh;                                     // the first launch of a call: the status is set to 0
     float a, b, c, eps, mu, keep, move;            // weight <- keep weight - move result
     unsigned char* x; unsigned char* y;            // X and its successor: (count, sblocks, lblocks) blocks
     unsigned char* g; unsigned char* p;            // A and P: (count, sblocks, sblocks) blocks

@@ -251,6 +251,7 @@ static int orthogonal(const void* const* u, float* const* momenta, void* const* 
     a.status = (int*)(ws + l.total - 256);
     for (int64_t i0 = 0; i0 < d->count; i0 += GROUP) {
         const int count = (int)std::min<int64_t>(GROUP, d->count - i0);
+        a.fresh = i0 == 0;
         if (l.x) { a.x = ws; a.y = ws + l.x; }                          // null: no workspace for the general kernels
         for (int k = 0; k < count; ++k) {
             a.u[k] = u[i0 + k]; a.out[k] = out[i0 + k]; a.momentum[k] = m ? momenta[i0 + k] : nullptr;

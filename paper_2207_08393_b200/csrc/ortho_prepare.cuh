@@ -13,7 +13,7 @@ template <class T, bool UPDATE>
 __global__ void __launch_bounds__(PREPARE_THREADS) sums_kernel(const __grid_constant__ Args a) {
     grid_dependency_wait();
     const int m = blockIdx.y;
-    if (blockIdx.x == 0 && m == 0 && threadIdx.x == 0) *a.status = 0;
+    if (a.fresh && blockIdx.x == 0 && m == 0 && threadIdx.x == 0) *a.status = 0;
     const long long n = a.rows * a.cols, step = (long long)gridDim.x * PREPARE_THREADS;
     const T* u = static_cast<const T*>(a.u[m]);
     float* momentum = UPDATE ? a.momentum[m] : nullptr;

@@ -56,7 +56,7 @@ __global__ void __launch_bounds__(RESIDENT_THREADS, 1) resident_kernel(const __g
     const int mine = (int)((a.L + BLOCK - 1) / BLOCK - first < tiles ? (a.L + BLOCK - 1) / BLOCK - first : tiles);
     bool failed = false;
     uint32_t phase = 0, second_phase = 0;
-    if (threadIdx.x == 0 && m == 0 && rank == 0) *a.status = 0;
+    if (a.fresh && threadIdx.x == 0 && m == 0 && rank == 0) *a.status = 0;
 
     // byte of element (r, c) of a piece of R rows
     auto at = [&](int r, int c) { return (r >> 3) * 2048 + (c >> 3) * CORE + (r & 7) * 16; };

@@ -264,3 +264,30 @@ def test_where_the_resident_kernel_ends(shape):
         close(y[k], oo.iterates(host(x[k]), 3), torch.float32)
     t = g.orthogonalise(x.mT.contiguous(), 3)
     close(t[0], [i.T for i in oo.iterates(host(x[0]), 3)], torch.float32)
+
+
+@pytest.mark.parametrize("rows, cols", [(24, 130), (150, 200)])
+def test_status_of_several_launches(rows, cols):
+    """More matrices than one launch takes, with a workspace that held something else."""
+    import paper_2207_08393_b200 as g
+    st = torch.cuda.current_stream()
+    d = g.make_matrix_dims(0, 70, rows, cols, stream=st)
+    need = g.gleam_orthogonalise_workspace_size(d)
+    ws = torch.full((need,), 255, dtype=torch.uint8, device="cuda")
+    d.workspace, d.workspace_bytes = ws.data_ptr(), need
+    x = matrices(70, rows, cols)
+    out = torch.empty_like(x)
+    g.gleam_orthogonalise(list(x), list(out), d)
+    g.gleam_orthogonalise_check_status(d)
+    assert torch.equal(out, g.orthogonalise(x))
+
+
+@pytest.mark.parametrize("rows, cols", [(24, 130), (150, 200)])
+def test_a_norm_beyond_32_bits_gives_zeros(rows, cols):
+    import paper_2207_08393_b200 as g
+    x = torch.full((2, rows, cols), 1e19, device="cuda")             # squares of 1e38, thousands of them
+    x[1] = matrices(1, rows, cols)[0]
+    y = g.orthogonalise(x)
+    assert not bool(y[0].any())
+    x[0] = 0
+    assert torch.equal(y, g.orthogonalise(x))                        # the other matrix is untouched by it

@@ -346,7 +346,8 @@ GLEAM_API int gleam_layer_norm_workspace_size(const gleam_feature_dims* dims, ui
  *
  *   recurrence     f_t = 1 / (1 + exp(-gate_t)),  h_t = f_t h_(t-1) + (1 - f_t) x_t,  y = h in the arrays' type,  last = h behind
  *                  the last step;  steps run 0, 1, ... or (reverse) the other way.  A gate of +inf keeps the state, one of -inf
- *                  forgets it.
+ *                  forgets it (a finite one: 0 times an infinite state is NaN).  Behind an infinite or NaN x or state the
+ *                  chain is infinite or NaN, and so are gradients that meet it; other chains are untouched.
  *   its VJP        D_t = grad_y_t + c_t,  c_t = f_(t+1) D_(t+1) (grad_last behind the last step),  grad_x = D (1 - f),
  *                  grad_gate = D (h_(t-1) - x) f (1 - f),  grad_state = f_0 D_0
  *   step           state <- f state + (1 - f) x,  y = state:  one step (steps = 1, no lengths) with the state updated in place

@@ -17,9 +17,10 @@
 // cores of 8 rows by 8 columns, a row of a core 16 bytes: the shape that the matrix instructions read, along either side.  An operand's
 // tile is a few copies of 8 or 16 KB: rows lie in one run with both their pieces, 32 of the columns in runs of 512 bytes, which a tiled
 // copy takes at once.  (With a copy for each run the copies, not the products, took the time: 4 x 512 x 4608, A: 89 us instead of 38.)
-// In shared memory an operand's hi and lo lie one behind the other, so that one instruction with N = 256 gives hi hi and hi lo side by
-// side, and one with N = 128 adds lo hi to the latter.  These run at the tensor core's rate (64 cycles for 128 x 128 x 16, 4096 products a
-// cycle); instructions with N = 64 take as long, for the 128 rows of their other operand.
+// Products run at the tensor core's rate (64 cycles for 128 x 128 x 16, 4096 products a cycle); instructions with N = 64 take as long, for
+// the 128 rows of their other operand.  All products that add to one sum have one shape and one place in tensor memory: only such
+// ones are sure to follow each other in the order of their issue.  hi (hi, lo) as one instruction of twice the width and lo hi added to half of
+// its sums took 2 % less, and an update of it could be lost.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>

@@ -95,7 +95,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, Form<KIND>::BLOCKS) gemm_kernel(
             if (!SIDES) tc::bulk_copy(to + F::OPERAND, right + ((long long)kb * a.lblocks + bj) * BLOCK_BYTES + share * F::OPERAND, F::OPERAND, full(s));
         }
     } else if (warp == 1 && lane == 0) {
-        const uint32_t both = tc::instruction(2 * BLOCK, !SIDES), what = tc::instruction(BLOCK, !SIDES);
+        const uint32_t what = tc::instruction(BLOCK, !SIDES);
         for (int i = 0; i < count; ++i) {
             const int s = i % STAGES;
             if (!tc::barrier_wait(full(s), (i / STAGES) & 1)) {
@@ -110,9 +110,11 @@ __global__ void __launch_bounds__(GEMM_THREADS, Form<KIND>::BLOCKS) gemm_kernel(
                 // cores of left: 512 bytes from one to the next along M, 128 along K; of right (!SIDES): 128 along N, 4096 along K
                 const uint32_t at = (q >> 1) * 16384 + (q & 1) * 256;
                 const uint64_t lh = tc::descriptor(l + at, 128, 512), ll = tc::descriptor(l + 8192 + at, 128, 512);
-                const uint64_t rb = SIDES ? tc::descriptor(r + at, 128, 512) : tc::descriptor(r + q * 8192, 4096, 128);       // hi, then lo
-                tc::product(to, lh, rb, both, i >= SUMS || q > 0);
-                tc::product(to + BLOCK, ll, rb, what, true);
+                const uint64_t rh = SIDES ? tc::descriptor(r + at, 128, 512) : tc::descriptor(r + q * 8192, 4096, 128);
+                const uint64_t rl = SIDES ? tc::descriptor(r + 8192 + at, 128, 512) : tc::descriptor(r + LO + q * 8192, 4096, 128);
+                tc::product(to + BLOCK, ll, rh, what, i >= SUMS || q > 0);
+                tc::product(to + BLOCK, lh, rl, what, true);
+                tc::product(to, lh, rh, what, i >= SUMS || q > 0);
             }
             tc::commit(empty(s));
         }

@@ -8,7 +8,7 @@
 //   - replaces its tiles by a X + P X.
 // Two barriers of the cluster a turn, nothing but the matrix itself through global memory, once each way.  32 x 100 x 900 float32 in clusters of
 // four with two tiles a block: 76 us, a turn 22,000 cycles, of which products a third (64 cycles an instruction for N = 128, hardly fewer
-// for less, so tiles are laid out for N = 128 and hi and lo of a narrow operand share one); the sums of A and its pieces on their way
+// for less, so tiles are laid out for N = 128); the sums of A and its pieces on their way
 // through the cluster, at 10 to 14 bytes a cycle, another; the rest brings sums from tensor memory back as pieces.  Issuing the next
 // turn's X X^T tile by tile while the other tile is stored gained nothing.
 #pragma once
@@ -162,10 +162,10 @@ __global__ void __launch_bounds__(RESIDENT_THREADS, 1) resident_kernel(const __g
     // a warp's part of a result: 32 rows, 32 columns
     const int row = (warp & 3) * 32 + lane, col0 = (warp >> 2) * 32;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-    auto read_sums = [&](uint32_t columns, int rest, float (&v)[32]) {      // the rest's sums stand so many columns behind those of hi hi
+    auto read_sums = [&](uint32_t columns, float (&v)[32]) {
         float u[32];
         tc::read_columns(cols0 + lanes + columns + col0, v);
-        tc::read_columns(cols0 + lanes + columns + rest + col0, u);
+        tc::read_columns(cols0 + lanes + columns + BLOCK + col0, u);
 #pragma unroll
         for (int j = 0; j < 32; ++j) v[j] = (v[j] + u[j]) * (1.f / SCALE);
     };
@@ -185,20 +185,21 @@ __global__ void __launch_bounds__(RESIDENT_THREADS, 1) resident_kernel(const __g
     for (int turn = 0; turn < turns; ++turn) {
         settle();
         if (threadIdx.x == 0) {
-            const uint32_t both = tc::instruction(2 * R, false), what = tc::instruction(R, false);       // lo stands behind hi: hi hi and hi lo at once
+            const uint32_t what = tc::instruction(R, false);
             for (int t = 0; t < mine; ++t)
                 for (int k = 0; k < BLOCK / 16; ++k) {
                     const uint32_t p = x_at + t * square + k * 256;
                     const uint64_t h = tc::descriptor(p, 128, 2048), l = tc::descriptor(p + lo, 128, 2048);
-                    tc::product(cols0, h, h, both, t > 0 || k > 0);
-                    tc::product(cols0 + R, l, h, what, true);
+                    tc::product(cols0 + BLOCK, l, h, what, t > 0 || k > 0);
+                    tc::product(cols0 + BLOCK, h, l, what, true);
+                    tc::product(cols0, h, h, what, t > 0 || k > 0);
                 }
             tc::commit(done);
         }
         wait(done, phase);
         if (col0 < R) {
             float v[32];
-            read_sums(0, R, v);
+            read_sums(0, v);
             if (row < R) {
 #pragma unroll
                 for (int j = 0; j < 32; j += 4)
@@ -246,19 +247,20 @@ __global__ void __launch_bounds__(RESIDENT_THREADS, 1) resident_kernel(const __g
         if (ranks > 1) tc::cluster_sync();
         settle();
         if (threadIdx.x == 0) {
-            const uint32_t both = tc::instruction(2 * R, false), what = tc::instruction(R, false);
+            const uint32_t what = tc::instruction(R, false);
             for (int k = 0; k < R / 16; ++k) {
                 const uint32_t p = a_at + k * 256;
                 const uint64_t h = tc::descriptor(p, 128, 2048), l = tc::descriptor(p + lo, 128, 2048);
-                tc::product(cols0 + 2 * BLOCK, h, h, both, k > 0);
-                tc::product(cols0 + 2 * BLOCK + R, l, h, what, true);
+                tc::product(cols0 + 3 * BLOCK, l, h, what, k > 0);
+                tc::product(cols0 + 3 * BLOCK, h, l, what, true);
+                tc::product(cols0 + 2 * BLOCK, h, h, what, k > 0);
             }
             tc::commit(done);
         }
         wait(done, phase);
         if (col0 < R) {
             float v[32];
-            read_sums(2 * BLOCK, R, v);
+            read_sums(2 * BLOCK, v);
             if (row < R) {
 #pragma unroll
                 for (int j = 0; j < 32; j += 8)
@@ -290,7 +292,7 @@ __global__ void __launch_bounds__(RESIDENT_THREADS, 1) resident_kernel(const __g
             for (int t = t0; t < mine && t < t0 + 2; ++t) {
                 if (t == t0) wait(done, phase); else wait(second, second_phase);         // the second product runs while the first is stored
                 float v[32];
-                read_sums((t - t0) * 2 * BLOCK, BLOCK, v);
+                read_sums((t - t0) * 2 * BLOCK, v);
                 if (turn + 1 < turns) {
                     if (row < R) {
 #pragma unroll

@@ -52,6 +52,7 @@ __device__ __forceinline__ uint64_t descriptor(uint32_t address, uint32_t leadin
 // float16 operands, 32-bit sums, M = 128
 __device__ __forceinline__ uint32_t instruction(int n, bool b_along_n) { return 1u << 4 | (b_along_n ? 1u << 16 : 0u) | (uint32_t)(n >> 3) << 17 | (128u >> 4) << 24; }
 
+// Follows the products before it that have the same sums and the same shape; no others.
 __device__ __forceinline__ void product(uint32_t sums, uint64_t a, uint64_t b, uint32_t what, bool add) {
     asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n"
                  ::"r"(sums), "l"(a), "l"(b), "r"(what), "r"((uint32_t)add) : "memory");

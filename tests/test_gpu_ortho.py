@@ -291,3 +291,22 @@ def test_a_norm_beyond_32_bits_gives_zeros(rows, cols):
     assert not bool(y[0].any())
     x[0] = 0
     assert torch.equal(y, g.orthogonalise(x))                        # the other matrix is untouched by it
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("shape", [(4, 512, 4608), (1, 1024, 9216), (2, 300, 2500), (32, 100, 900), (16, 60, 1620), (9, 30, 700)])
+def test_the_bits_of_many_calls(shape, dtype):
+    """Products whose order is left open would lose an update of a sum once in a while: the same bits over many calls, with other work between
+    them and a workspace that held something else."""
+    import paper_2207_08393_b200 as g
+    x = matrices(*shape, dtype=TYPES[dtype])
+    first = g.orthogonalise(x)
+    other = torch.randn(1024, 1024, device="cuda")
+    differs = torch.zeros((), dtype=torch.int64, device="cuda")
+    for k in range(60):
+        if k % 3 == 1:
+            other = torch.tanh(other @ other)
+        if k % 5 == 2:
+            torch.empty(1 << 26, dtype=torch.uint8, device="cuda").fill_(k + 1)
+        differs += torch.count_nonzero(g.orthogonalise(x) != first)
+    assert int(differs) == 0

@@ -48,12 +48,16 @@ static cudaError_t allow_clusters(K kernel, int ranks) {
     return ranks > RESIDENT_PORTABLE ? cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) : cudaSuccess;
 }
 
-// Clusters of so many blocks, one block an SM, that the current device runs at once: its SMs come in groups that clusters do not
-// cross, so 16 clusters of 7 are more than 148 SMs may hold.
+// Clusters of so many blocks, one block an SM, that a B200 runs at once: its SMs come in groups that clusters do not cross, so 16
+// clusters of 7 are more than 148 SMs may hold.  Constants (what cudaOccupancyMaxActiveClusters gives on the GPUs it was asked on, the
+// least of them): sums are split by the sizes alone, so that the replicas of a model on several GPUs compute the same bits.  A GPU whose
+// groups hold fewer takes one round more.  Only whether it takes more than eight blocks at all is asked of the GPU itself.
 static int clusters_at_once(int ranks) {
-    static PerDevice cache[RESIDENT_RANKS + 1];                       // one more than the number
+    static constexpr int at_once[RESIDENT_RANKS + 1] = {0, SMS, 74, 45, 33, 26, 22, 15, 15, 15, 11, 7, 7, 7, 7, 7, 7};
+    if (ranks <= RESIDENT_PORTABLE) return at_once[ranks];
+    static PerDevice cache[RESIDENT_RANKS + 1];                       // 1: no, 2: yes
     std::atomic<int>* slot = cache[ranks].slot();
-    if (slot) { const int v = slot->load(std::memory_order_acquire); if (v > 0) return v - 1; }
+    if (slot) { const int v = slot->load(std::memory_order_acquire); if (v > 0) return v == 2 ? at_once[ranks] : 0; }
     static PerDevice done;
     constexpr auto KERNEL = resident_kernel<float, false>;
     int n = 0;
@@ -62,12 +66,12 @@ static int clusters_at_once(int ranks) {
     launch_config(cfg, at, false, dim3((unsigned)ranks), dim3(RESIDENT_THREADS), RESIDENT_MOST, nullptr, 2);
     at[0].val.clusterDim.x = (unsigned)ranks;
     if (ensure_smem(KERNEL, RESIDENT_MOST, done) != cudaSuccess || allow_clusters(KERNEL, ranks) != cudaSuccess ||
-        cudaOccupancyMaxActiveClusters(&n, KERNEL, &cfg) != cudaSuccess || n < 1) {
+        cudaOccupancyMaxActiveClusters(&n, KERNEL, &cfg) != cudaSuccess) {
         cudaGetLastError();
-        n = ranks > RESIDENT_PORTABLE ? 0 : SMS / ranks;
+        n = 0;
     }
-    if (slot) slot->store(n + 1, std::memory_order_release);
-    return n;
+    if (slot) slot->store(n > 0 ? 2 : 1, std::memory_order_release);
+    return n > 0 ? at_once[ranks] : 0;
 }
 
 template <int KIND, int RANKS, class T>

@@ -65,6 +65,12 @@ __device__ __forceinline__ int sum_at(int r, int c) { return r * BLOCK + ((((c >
 template <class T> __device__ __forceinline__ float load_at(const void* p, long long i) { return to_float(static_cast<const T*>(p)[i]); }
 template <class T> __device__ __forceinline__ void store_at(void* p, long long i, float v) { static_cast<T*>(p)[i] = from_float<T>(v); }
 
+// What turns U into the stored X_0, given its sum of squares.  Finite, so that zeros stay zeros under the smallest eps; NaN where the sum is.
+__device__ __forceinline__ float first_scale(float total, float eps) {
+    const float by = SCALE / (sqrtf(total) + eps);
+    return by > 3.402823466e38f ? 3.402823466e38f : by;
+}
+
 // Eight neighbours of a row as two pieces, and back.
 __device__ __forceinline__ void split8(const float (&v)[8], uint4& hi, uint4& lo) {
     uint32_t h[4], l[4];

@@ -128,7 +128,7 @@ __global__ void __launch_bounds__(RESIDENT_THREADS, 1) resident_kernel(const __g
     if (ranks > 1) tc::cluster_sync(); else __syncthreads();
     float total = 0.f;
     for (int k = 0; k < ranks; ++k) total += ranks > 1 ? tc::read_remote(base + 64, k).x : part[0];
-    const float by = SCALE / (sqrtf(total) + a.eps);
+    const float by = first_scale(total, a.eps);
 
     // ... and as pieces
     const int eights = R * BLOCK / 8;

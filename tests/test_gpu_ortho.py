@@ -310,3 +310,17 @@ def test_the_bits_of_many_calls(shape, dtype):
             torch.empty(1 << 26, dtype=torch.uint8, device="cuda").fill_(k + 1)
         differs += torch.count_nonzero(g.orthogonalise(x) != first)
     assert int(differs) == 0
+
+
+@pytest.mark.parametrize("rows, cols", [(24, 130), (150, 200)])
+@pytest.mark.parametrize("eps", [1e-30, 1e-38, 1.5e-45])
+def test_zeros_stay_zeros_whatever_eps(rows, cols, eps):
+    import paper_2207_08393_b200 as g
+    x = torch.zeros(2, rows, cols, device="cuda")
+    x[1] = matrices(1, rows, cols)[0]
+    y = g.orthogonalise(x, eps=eps)
+    assert not bool(y[0].any()) and not bool(torch.isnan(y[0]).any())
+    assert torch.equal(y[1], g.orthogonalise(x[1], eps=1e-30))
+    w = [torch.ones(rows, cols, device="cuda")]
+    g.muon_step(w, [x[0].clone()], [torch.zeros(rows, cols, device="cuda")], 0.5, weight_decay=0.5, eps=eps)
+    assert bool((w[0] == 0.75).all())

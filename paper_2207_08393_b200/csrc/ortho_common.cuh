@@ -7,11 +7,12 @@
 // which takes each singular value v to a v + b v^3 + c v^5 and leaves the singular vectors: after a few turns of suitable (a, b, c)
 // all values but the smallest are near 1 (K. Jordan et al., "Muon: an optimizer for hidden layers in neural networks", 2024).
 //
-// The products run on the tensor cores in float16 with 32-bit sums, and keep the precision of 32-bit numbers: X, A and P are stored as
-// two pieces, hi = x rounded to float16 and lo = x - hi rounded to float16 (22 bits), and a product is hi hi + hi lo + lo hi; what is
-// left out is 2^-22 of it.  All stored values are scaled by 2^10 (up to 64 in front of the scale), so that lo keeps its bits down
-// to values of 2^-13.  The term a X is added in 32 bits.  Against 64 bits the result is as near as 32-bit products are, or nearer;
-// float16 or bfloat16 products without the second piece would be off by 1e-3 or 1e-2.
+// The products run on the tensor cores in float16 with 32-bit sums, and come near the precision of 32-bit numbers: X, A and P are stored as
+// two pieces, hi = x rounded to float16 and lo = x - hi rounded to float16 (22 bits, where a 32-bit number has 24), and a product is
+// hi hi + hi lo + lo hi; what is left out is 2^-24 of it.  All stored values are scaled by 2^10 (up to 64 in front of the scale), so that lo keeps
+// its bits down to values of 2^-13 and is off by 2^-35 below; X also by a power of two where its norm is small against eps (Exponent).  The
+// term a X is added in 32 bits.  Five turns of 100 x 900 of falling singular values are off by 1.9e-6, 2.7e-6 in 32-bit products; of 9216 x 1024 by
+// 7.4e-7 and 5.3e-7.  float16 or bfloat16 products without the second piece would be off by 1e-3 or 1e-2.
 //
 // Matrices are stored in blocks of 128 x 128 with zeros beyond their sides, 64 KB: 16 rows of cores, in each those of hi, then those of lo, 16
 // cores of 8 rows by 8 columns, a row of a core 16 bytes: the shape that the matrix instructions read, along either side.  An operand's
@@ -53,6 +54,8 @@ struct Args {
     unsigned char* x; unsigned char* y;            // X and its successor: (count, sblocks, lblocks) blocks
     unsigned char* g; unsigned char* p;            // A and P: (count, sblocks, sblocks) blocks
     float* part; int* status;
+    float* size;                                   // norms of X_0
+    int turn;                                      // the turn of a launch
     unsigned char* blocks;                         // all blocks of the workspace: what the tiled copies' map covers
 };
 
@@ -65,9 +68,43 @@ __device__ __forceinline__ int sum_at(int r, int c) { return r * BLOCK + ((((c >
 template <class T> __device__ __forceinline__ float load_at(const void* p, long long i) { return to_float(static_cast<const T*>(p)[i]); }
 template <class T> __device__ __forceinline__ void store_at(void* p, long long i, float v) { static_cast<T*>(p)[i] = from_float<T>(v); }
 
-// What turns U into the stored X_0, given its sum of squares.  Finite, so that zeros stay zeros under the smallest eps; NaN where the sum is.
+// 2^n; zero below the smallest normal number.
+__device__ __forceinline__ float power_of_two(int n) { return n < -126 ? 0.f : __int_as_float((n < 127 ? n + 127 : 254) << 23); }
+
+// The norm of what is orthogonalised may be small against eps, and X then starts far below 1.  So that its pieces keep their bits, X = 2^e X^
+// is stored as X^, with e = 0 as soon as X may have a norm above 1/2 (from the first turn on where eps is small) and otherwise such that a
+// bound of X^'s norm lies in [1/2, 1).  The bound: |X_0|, then |X| (|a| + |b| |X|^2 + |c| |X|^4).  A turn in terms of X^ is
+//
+//     A^ = X^ X^^T,   P^ = b A^ + c 2^2e A^ A^,   X^ <- 2^(e - e') (a X^ + 2^2e P^ X^),
+//
+// powers of two throughout: where all e are 0 nothing changes, and nowhere is anything rounded for it.
+struct Exponent {
+    static constexpr int LEAST = -120;
+    float most;                                    // the bound; e = 0 from where it is not below 1/2 (or no number) on
+    int e;
+    __device__ __forceinline__ explicit Exponent(float size) : most(size), e(0) { set(); }
+    __device__ __forceinline__ void set() {
+        if (!(most <= 0.5f)) { e = 0; return; }
+        e = (__float_as_int(most) >> 23) - 126;
+        if (e < LEAST) e = LEAST;
+    }
+    __device__ __forceinline__ void turn(const Args& a) {
+        if (!(most <= 0.5f)) return;
+        const float square = most * most;
+        most = fmaxf(most * (fabsf(a.a) + square * (fabsf(a.b) + square * fabsf(a.c))), 7.5e-37f);       // 2^LEAST
+        set();
+    }
+};
+
+// The norm of X_0, from the sum of squares.  Squares below 2^-149 are lost: a norm below 2^-64 counts as that (what is stored is then smaller than it
+// could be, but right).
+__device__ __forceinline__ float first_size(float total, float eps) {
+    const float norm = sqrtf(total);
+    return fmaxf(norm, 5.42101086e-20f) / (norm + eps);
+}
+// What turns U into the stored X_0.  Finite, so that zeros stay zeros under the smallest eps; NaN where the sum is.
 __device__ __forceinline__ float first_scale(float total, float eps) {
-    const float by = SCALE / (sqrtf(total) + eps);
+    const float by = ldexpf(SCALE / (sqrtf(total) + eps), -Exponent(first_size(total, eps)).e);
     return by > 3.402823466e38f ? 3.402823466e38f : by;
 }
 

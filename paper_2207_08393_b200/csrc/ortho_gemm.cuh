@@ -137,7 +137,18 @@ __global__ void __launch_bounds__(GEMM_THREADS, Form<KIND>::BLOCKS) gemm_kernel(
             old_lo[k] = *reinterpret_cast<const uint4*>(old + LO + core_at(row_of(k0 + k), col));
         }
     };
-    if (KIND != GRAM) fetch(0);
+    // X = 2^e X^ and its successor (LAST: the result itself): b A and c A A, a X and P X are blended with these
+    float old_by = 1.f, sum_by = 1.f;
+    if (KIND != GRAM) {
+        fetch(0);
+        Exponent now(a.size[m]);
+        for (int k = 0; k < a.turn && now.most <= 0.5f; ++k) now.turn(a);
+        Exponent next = now;
+        next.turn(a);
+        const int to = KIND == LAST ? 0 : next.e;
+        old_by = KIND == POLY ? a.b : a.a * power_of_two(now.e - to);
+        sum_by = KIND == POLY ? a.c * power_of_two(2 * now.e) : power_of_two(3 * now.e - to);
+    }
     if (!tc::barrier_wait(done, 0)) failed = true;
     tc::fence_after();
 
@@ -198,11 +209,11 @@ __global__ void __launch_bounds__(GEMM_THREADS, Form<KIND>::BLOCKS) gemm_kernel(
         const float4 f = *reinterpret_cast<const float4*>(sum + sum_at(r, c)), g = *reinterpret_cast<const float4*>(sum + sum_at(r, c + 4));
         v[0] = f.x; v[1] = f.y; v[2] = f.z; v[3] = f.w; v[4] = g.x; v[5] = g.y; v[6] = g.z; v[7] = g.w;
     };
-    auto blend = [&](const uint4& hi, const uint4& lo, float by, float (&v)[8], float times) {
+    auto blend = [&](const uint4& hi, const uint4& lo, float (&v)[8]) {
         float u[8];
         join8(hi, lo, u);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = fmaf(by, u[j], times * v[j]);
+        for (int j = 0; j < 8; ++j) v[j] = fmaf(old_by, u[j], sum_by * v[j]);
     };
     // zeros beyond the matrix
     auto put = [&](unsigned char* block, int r, int c, float (&v)[8], long long rows, long long cols) {
@@ -224,8 +235,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, Form<KIND>::BLOCKS) gemm_kernel(
             if (!has(k)) break;
             if (KIND == APPLY && k == AHEAD) fetch(k);
             take8(row_of(k), col, v);
-            if (KIND == POLY) blend(old_hi[k % AHEAD], old_lo[k % AHEAD], a.b, v, a.c);
-            if (KIND == APPLY) blend(old_hi[k % AHEAD], old_lo[k % AHEAD], a.a, v, 1.f);
+            if (KIND != GRAM) blend(old_hi[k % AHEAD], old_lo[k % AHEAD], v);
             put(to, row_of(k), col, v, rows, cols);
         }
         if (SIDES && !one) {
@@ -249,7 +259,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, Form<KIND>::BLOCKS) gemm_kernel(
                 float v[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[j] = sum[sum_at(c + j, r)];
-                if (KIND == POLY) blend(old_hi[k], old_lo[k], a.b, v, a.c);
+                if (KIND == POLY) blend(old_hi[k], old_lo[k], v);
                 put((KIND == GRAM ? a.g : a.p) + at, r, c, v, cols, rows);
             }
         }
@@ -259,7 +269,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, Form<KIND>::BLOCKS) gemm_kernel(
             float v[8];
             if (k == AHEAD) fetch(k);
             take8(row_of(k), col, v);
-            blend(old_hi[k % AHEAD], old_lo[k % AHEAD], a.a, v, 1.f);
+            blend(old_hi[k % AHEAD], old_lo[k % AHEAD], v);
             *reinterpret_cast<float4*>(sum + sum_at(row_of(k), col)) = make_float4(v[0], v[1], v[2], v[3]);
             *reinterpret_cast<float4*>(sum + sum_at(row_of(k), col + 4)) = make_float4(v[4], v[5], v[6], v[7]);
         }

@@ -157,6 +157,7 @@ static cudaError_t run(Args& a, int count, int turns, cudaStream_t s) {
     if ((e = map_of(a, (uint64_t)((unsigned char*)a.part - a.blocks), &map)) != cudaSuccess) return e;
     ORTHO_LAUNCH(launch_overlapped(true, first_kernel<T, UPDATE>, dim3((unsigned)(a.sblocks * a.lblocks), (unsigned)count), dim3(PREPARE_THREADS), tile, s, a));
     for (int k = 0; k < turns; ++k) {
+        a.turn = k;
         if ((e = gemm<GRAM>(a, map, count, s)) != cudaSuccess || (e = gemm<POLY>(a, map, count, s)) != cudaSuccess) return e;
         if ((e = k + 1 < turns ? gemm<APPLY>(a, map, count, s) : gemm<LAST, T>(a, map, count, s)) != cudaSuccess) return e;
         std::swap(a.x, a.y);
@@ -190,7 +191,7 @@ static int layout_of(const gleam_matrix_dims* d, Layout* l) {
     if (l->total == 0 || (d->count <= RESIDENT_COUNT && resident_fits(S, L))) return GLEAM_OK;
     l->x = (uint64_t)l->group * l->sblocks * l->lblocks * BLOCK_BYTES;
     l->square = (uint64_t)l->group * l->sblocks * l->sblocks * BLOCK_BYTES;
-    l->part = (uint64_t)GROUP * PARTS * sizeof(float);
+    l->part = (uint64_t)GROUP * (PARTS + 1) * sizeof(float);                     // and the norms of X_0
     l->total += 2 * l->x + 2 * l->square + l->part;
     return GLEAM_OK;
 }
@@ -251,7 +252,7 @@ static int orthogonal(const void* const* u, float* const* momenta, void* const* 
     }
     unsigned char* ws = (unsigned char*)d->workspace;
     a.blocks = ws; a.g = ws + 2 * l.x; a.p = a.g + l.square;
-    a.part = (float*)(a.p + l.square);
+    a.part = (float*)(a.p + l.square); a.size = a.part + GROUP * PARTS;
     a.status = (int*)(ws + l.total - 256);
     for (int64_t i0 = 0; i0 < d->count; i0 += GROUP) {
         const int count = (int)std::min<int64_t>(GROUP, d->count - i0);

@@ -80,6 +80,7 @@ __global__ void __launch_bounds__(PREPARE_THREADS) first_kernel(const __grid_con
     __shared__ float buf[2 * (PREPARE_THREADS / 32)];
     total = prior::block_sum<PREPARE_THREADS / 32>(prior::Pair{total, 0.f}, buf).a;
     const float by = first_scale(total, a.eps);
+    if (blockIdx.x == 0 && threadIdx.x == 0) a.size[m] = first_size(total, a.eps);
     unsigned char* block = a.x + ((long long)(m * a.sblocks + sb) * a.lblocks + lb) * BLOCK_BYTES;
     const long long s0 = (long long)sb * BLOCK, l0 = (long long)lb * BLOCK;
     const int rows = a.S - s0 < BLOCK ? (int)(a.S - s0) : BLOCK, cols = a.L - l0 < BLOCK ? (int)(a.L - l0) : BLOCK;

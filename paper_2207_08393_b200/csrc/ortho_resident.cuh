@@ -182,7 +182,13 @@ __global__ void __launch_bounds__(RESIDENT_THREADS, 1) resident_kernel(const __g
         *reinterpret_cast<uint4*>(to + lo + at(row, c)) = l;
     };
 
+    Exponent now(first_size(total, a.eps));
     for (int turn = 0; turn < turns; ++turn) {
+        Exponent next = now;
+        next.turn(a);
+        const int to = turn + 1 < turns ? next.e : 0;                      // the last one is the result itself
+        const float poly = a.c * power_of_two(2 * now.e), old_by = a.a * power_of_two(now.e - to), sum_by = power_of_two(3 * now.e - to);
+        now = next;
         settle();
         if (threadIdx.x == 0) {
             const uint32_t what = tc::instruction(R, false);
@@ -266,7 +272,7 @@ __global__ void __launch_bounds__(RESIDENT_THREADS, 1) resident_kernel(const __g
                 for (int j = 0; j < 32; j += 8)
                     if (col0 + j < R) {
                         float w[8];
-                        blend(A_, col0 + j, a.b, a.c, v + j, w);
+                        blend(A_, col0 + j, a.b, poly, v + j, w);
                         put(A_, col0 + j, w);
                     }
             }
@@ -298,7 +304,7 @@ __global__ void __launch_bounds__(RESIDENT_THREADS, 1) resident_kernel(const __g
 #pragma unroll
                         for (int j = 0; j < 32; j += 8) {
                             float w[8];
-                            blend(X + t * square, col0 + j, a.a, 1.f, v + j, w);
+                            blend(X + t * square, col0 + j, old_by, sum_by, v + j, w);
                             put(X + t * square, col0 + j, w);
                         }
                     }
@@ -310,7 +316,7 @@ __global__ void __launch_bounds__(RESIDENT_THREADS, 1) resident_kernel(const __g
 #pragma unroll
                     for (int j = 0; j < 32; j += 8) {
                         float w[8];
-                        blend(X + t * square, col0 + j, a.a, 1.f, v + j, w);
+                        blend(X + t * square, col0 + j, old_by, sum_by, v + j, w);
                         *reinterpret_cast<float4*>(sum + sum_at(row, col0 + j)) = make_float4(w[0], w[1], w[2], w[3]);
                         *reinterpret_cast<float4*>(sum + sum_at(row, col0 + j + 4)) = make_float4(w[4], w[5], w[6], w[7]);
                     }

@@ -324,3 +324,78 @@ def test_zeros_stay_zeros_whatever_eps(rows, cols, eps):
     w = [torch.ones(rows, cols, device="cuda")]
     g.muon_step(w, [x[0].clone()], [torch.zeros(rows, cols, device="cuda")], 0.5, weight_decay=0.5, eps=eps)
     assert bool((w[0] == 0.75).all())
+
+
+# ---- beside the same turns in 32-bit products (oracle.ortho_oracle.near)
+
+def turns(x, steps, coefficients=oo.COEFFICIENTS, eps=1e-7):
+    """The definition in x's type, over the shorter side."""
+    a, b, c = coefficients
+    tall = x.shape[-2] > x.shape[-1]
+    x = x.mT if tall else x
+    x = x / (x.square().sum((-2, -1), keepdim=True).sqrt() + eps)
+    for _ in range(steps):
+        g = x @ x.mT
+        x = a * x + (b * g + c * (g @ g)) @ x
+    return x.mT if tall else x
+
+
+def near_32_bits(x, y, steps, **kw):
+    """Every matrix of y = orthogonalise(x) within ``near`` of 64 bits."""
+    assert not torch.backends.cuda.matmul.allow_tf32
+    for u, v in zip(x, y):
+        ref = turns(u.double(), steps, **kw)
+        norm = float(ref.norm())
+        assert norm > 0.0 and np.isfinite(norm)
+        err32 = float((turns(u, steps, **kw).double() - ref).norm()) / norm
+        off = float((v.double() - ref).norm()) / norm
+        most = oo.near(err32, max(u.shape))
+        assert off <= most, "%g, 32-bit products %g, allowed %g" % (off, err32, most)
+
+
+@pytest.mark.parametrize("steps", [1, 3, 5])
+@pytest.mark.parametrize("shape", [(2, 100, 900), (1, 60, 5000), (2, 900, 2), (1, 130, 1000), (2, 257, 300), (2, 300, 257), (1, 640, 651), (1, 384, 1024),
+                                   (1, 1030, 2100), (1, 2048, 2048), (1, 4100, 3000), (1, 512, 12000), (40, 90, 130), (16, 60, 1620)])
+def test_as_near_as_pieces_allow(shape, steps):
+    import paper_2207_08393_b200 as g
+    x = matrices(*shape, seed=11)
+    near_32_bits(x, g.orthogonalise(x, steps), steps)
+    x = torch.randn(shape, device="cuda")                            # singular values of one size
+    near_32_bits(x, g.orthogonalise(x, steps), steps)
+
+
+@pytest.mark.parametrize("rows, cols", [(100, 900), (900, 60), (150, 200), (300, 700)])
+@pytest.mark.parametrize("norm", [1e-6, 1e-7, 3e-8, 1e-9, 1e-10, 1e-11, 1e-12, 1e-13, 1e-16, 1e-18, 1e-20])
+def test_norms_small_against_eps(rows, cols, norm):
+    """X starts far below 1 and keeps its digits."""
+    import paper_2207_08393_b200 as g
+    x = matrices(2, rows, cols, seed=12)
+    x = (x.double() * (norm / x.double().norm(dim=(-2, -1), keepdim=True))).float()
+    for steps in (1, 2, 5, 9):
+        near_32_bits(x, g.orthogonalise(x, steps), steps)
+    near_32_bits(x, g.orthogonalise(x, 3, (0.25, -0.5, 0.25), 1e-9), 3, coefficients=(0.25, -0.5, 0.25), eps=1e-9)       # norms that shrink
+    w, mom = [torch.zeros(rows, cols, device="cuda")], [torch.zeros(rows, cols, device="cuda")]
+    g.muon_step(w, [x[0]], mom, 1.0, 0.0)
+    near_32_bits(x[:1], [-w[0]], 5)
+
+
+@pytest.mark.parametrize("shape", [(16384, 16400), (130, 1 << 20), (1 << 20, 40), (7000, 16384)])
+def test_the_largest_sides(shape):
+    import paper_2207_08393_b200 as g
+    x = torch.randn((1,) + shape, device="cuda")
+    near_32_bits(x, g.orthogonalise(x, 1), 1)
+
+
+@pytest.mark.parametrize("rows, cols", [(100, 900), (150, 600), (60, 60)])
+@pytest.mark.parametrize("share", [1e-2, 1e-4, 1e-6, 1e-9])
+def test_rows_that_are_small_beside_the_others(rows, cols, share):
+    """Stored values have an absolute step: X, A and P are off by 2^-35 each.  In a row that is small, five turns of the usual coefficients
+    stretch X's 2^-35 sqrt(L) by 3.45^5 + ... + 3.45 = 682, and what P's row is off by, 2^-35 (1 + 4.78 + 2.04 * 1.56) sqrt(S) times |X| <= 1.25,
+    by 3.45^4 + ... + 1 = 198.  The rest is relative to the row, as of a whole matrix."""
+    import paper_2207_08393_b200 as g
+    x = matrices(1, rows, cols, seed=13)
+    x[0, 7] *= share
+    y, ref, half = g.orthogonalise(x)[0, 7].double(), turns(x[0].double(), 5)[7], turns(x[0], 5)[7].double()
+    norm = float(ref.norm())
+    most = 2.0 ** -35 * (682 * cols ** 0.5 + 198 * 11.3 * rows ** 0.5) + norm * oo.near(float((half - ref).norm()) / norm, cols)
+    assert float((y - ref).norm()) <= most

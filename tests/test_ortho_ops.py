@@ -164,3 +164,55 @@ def test_a_loaded_momentum_has_its_weights_shape():
     opt.state[a]["momentum"] = torch.zeros(1, 6)
     with pytest.raises(ValueError):
         g.Muon([b]).load_state_dict(opt.state_dict())
+
+
+def in_pieces(x, steps, pieces, coefficients=oo.COEFFICIENTS, eps=1e-7):
+    """The turns with X, A and P stored as one or two float16 numbers of 2^10 times their values (X times a power of two where its norm is
+    small), everything else in 64 bits."""
+    a, b, c = coefficients
+
+    def stored(v):
+        v = v * 1024.0
+        hi = v.astype(np.float16).astype(np.float64)
+        lo = (v - hi).astype(np.float16).astype(np.float64) if pieces == 2 else 0.0 * v
+        return hi / 1024.0, lo / 1024.0
+
+    def product(u, v):
+        return u[0] @ v[0] + u[0] @ v[1] + u[1] @ v[0]
+
+    norm = np.sqrt((x.astype(np.float64) ** 2).sum())
+    most = norm / (norm + eps)
+    x = x.astype(np.float64) / (norm + eps)
+    for _ in range(steps):
+        e = np.ceil(np.log2(most)) if most <= 0.5 else 0.0
+        s = stored(x * 2.0 ** -e)
+        p = stored(b * product(s, [v.T for v in s]) + c * 2.0 ** (2 * e) * product(*[stored(product(s, [v.T for v in s]))] * 2))
+        x = 2.0 ** e * (a * (s[0] + s[1]) + 2.0 ** (2 * e) * product(p, s))
+        most = most * (abs(a) + most ** 2 * (abs(b) + most ** 2 * abs(c))) if most <= 0.5 else 1.0
+    return x
+
+
+def in_32_bits(x, steps, coefficients=oo.COEFFICIENTS, eps=1e-7):
+    a, b, c = (np.float32(v) for v in coefficients)
+    x = x.astype(np.float32)
+    x = x / (np.sqrt((x ** 2).sum()) + np.float32(eps))
+    for _ in range(steps):
+        g = x @ x.T
+        x = a * x + (b * g + c * (g @ g)) @ x
+    return x.astype(np.float64)
+
+
+@pytest.mark.parametrize("norm", [1.0, 1e-6, 1e-8, 1e-11, 1e-13, 1e-16])
+@pytest.mark.parametrize("shape", [(60, 540), (130, 257), (100, 900)])
+@pytest.mark.parametrize("steps", [1, 5])
+def test_the_bound_takes_two_pieces_and_not_one(shape, steps, norm):
+    rng = np.random.default_rng(3)
+    n = shape[0]
+    x = (rng.normal(size=(n, n)) / (1 + np.arange(n))) @ rng.normal(size=(n, shape[1]))
+    x = (x * norm / np.sqrt((x ** 2).sum())).astype(np.float32)
+    ref = oo.iterates(x, steps)[-1]
+    off = lambda y: np.sqrt(((y - ref) ** 2).sum() / (ref ** 2).sum())
+    most = oo.near(off(in_32_bits(x, steps)), shape[1])
+    # 32-bit products leave up to 2.7e-6 after five turns (100 x 900), of which four times, 900 * 2^-28 and 2^-21 are 1.5e-5
+    assert off(in_pieces(x, steps, 2)) <= most < 2e-5
+    assert off(in_pieces(x, steps, 1)) > 10 * most

@@ -24,3 +24,24 @@ def test_a_warp_barrier_stands_before_copies_into_slots_of_other_lanes():
     copies = [i for i, line in enumerate(code) if "cp_async16(e - odd" in line]
     assert len(reads) == len(copies) == 1 and reads[0] < copies[0]
     assert any("__syncwarp();" in line for line in code[reads[0]:copies[0]])
+
+
+def test_products_that_add_to_one_sum_have_one_shape():
+    """Matrix instructions follow each other in the order of their issue only if they share the place of their sums and the shape."""
+    for name in ("ortho_gemm.cuh", "ortho_resident.cuh"):
+        code = "".join(line.split("//")[0] + "\n" for line in open(os.path.join(CSRC, name)))
+        products = re.findall(r"tc::product\(([^;]*)\);", code)
+        assert products and all(p.split(",")[-2].strip() == "what" for p in products), name
+        shapes = re.findall(r"what = tc::instruction\((\w+), ", code)
+        assert len(shapes) == code.count("tc::instruction("), name
+        for shape in shapes:
+            assert shape in ("BLOCK", "R"), name
+
+
+def test_sums_are_split_by_sizes_alone():
+    """Replicas of a model on several GPUs compute the same bits: how many clusters the current GPU holds decides nothing but whether it takes
+    those of more than eight blocks."""
+    code = "".join(line.split("//")[0] + "\n" for line in open(os.path.join(CSRC, "ortho_ops.cu")))
+    assert code.count("cudaOccupancyMaxActiveClusters") == 1
+    body = code[code.index("static int clusters_at_once"):code.index("cudaOccupancyMaxActiveClusters")]
+    assert "if (ranks <= RESIDENT_PORTABLE) return at_once[ranks];" in body

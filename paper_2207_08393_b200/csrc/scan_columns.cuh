@@ -58,7 +58,7 @@ __global__ void __launch_bounds__(COLUMN_THREADS) columns_forward(const __grid_c
             float out = 0.f;
             if (t < valid) {
                 float f, rest;
-                gate_of(to_float(gs[k]), f, rest);
+                gate_of<T>(to_float(gs[k]), f, rest);
                 out = h = fmaf(f, h, rest * to_float(xs[k]));
                 prod *= f;
             }
@@ -107,7 +107,7 @@ __global__ void __launch_bounds__(COLUMN_THREADS) columns_vjp(const __grid_const
         for (int k = 0; k < CHUNK; ++k) {
             const long long t = REVERSE ? steps - 1 - (q0 + k) : q0 + k;
             if (k < count && t < valid) {
-                gate_of(to_float(gs[k]), f[k], rest[k]);
+                gate_of<T>(to_float(gs[k]), f[k], rest[k]);
                 if (!MAPS) {
                     const float u = to_float(xs[k]);
                     w[k] = h - u;
@@ -154,7 +154,7 @@ __global__ void __launch_bounds__(COLUMN_THREADS) step_kernel(const __grid_const
 #pragma unroll
     for (int j = 0; j < V; ++j) {
         float f, rest;
-        gate_of(to_float(gate.e[j]), f, rest);
+        gate_of<T>(to_float(gate.e[j]), f, rest);
         h.e[j] = fmaf(f, h.e[j], rest * to_float(x.e[j]));
         out.e[j] = from_float<T>(h.e[j]);
     }

@@ -42,14 +42,19 @@ struct Args {
 
 enum { MAP_FORWARD, MAP_VJP, FORWARD, VJP };       // MAP_*: only the parts' maps are formed
 
-// f and 1 - f, both to full relative precision, from e = exp(-gate): f = 1 / (1 + e), 1 - f = e f where e <= 1, the difference where
-// not (there it is exact, and holds for e = infinity).  f is exactly 1 or 0 for an infinite gate; both are NaN for one that is NaN.
-// Two at a time: sums and products of pairs take one instruction.
+// f and 1 - f from e = exp(-gate): f = 1 / (1 + e), 1 - f = e f where e <= 1, the difference where not (there it is exact, and holds for
+// e = infinity).  f is exactly 1 or 0 for an infinite gate; both are NaN for one that is NaN.  Two at a time: sums and products of pairs take
+// one instruction.
+//
+// With 32-bit gates e is CUDA's exponential, and f and 1 - f are good to 2^-21 of themselves wherever they are normal numbers.  Gates of
+// 16 bits are themselves off by 2^-12 or 2^-9 of their size; e is 2 to the power of -gate log2(e) rounded to 32 bits there, which costs |gate|
+// 2^-23 of e and six instructions less (4 x 160 x 81920 bf16, forward and VJP, 166 us; with CUDA's 174).
 using prior::fma2;
 using prior::Two;
 __device__ __forceinline__ float exp2_of(float x) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
 __device__ __forceinline__ float inverse_of(float x) { float r; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
-__device__ __forceinline__ Two exp_of_minus(Two g) {
+template <class T> __device__ __forceinline__ Two exp_of_minus(Two g) {
+    if constexpr (sizeof(T) == 4) return Two(expf(-g.lo()), expf(-g.hi()));
     const Two x = g * Two(-1.4426950408889634f);
     return Two(exp2_of(x.lo()), exp2_of(x.hi()));
 }
@@ -59,9 +64,9 @@ __device__ __forceinline__ void gates_from(Two e, Two& f, Two& rest) {
     const Two p = e * f, q = fma2(f, Two(-1.f), Two(1.f));
     rest = Two(e.lo() > 1.f ? q.lo() : p.lo(), e.hi() > 1.f ? q.hi() : p.hi());
 }
-__device__ __forceinline__ void gates_of(Two g, Two& f, Two& rest) { gates_from(exp_of_minus(g), f, rest); }
-__device__ __forceinline__ void gate_of(float g, float& f, float& rest) {
-    const float e = exp2_of(g * -1.4426950408889634f);
+template <class T> __device__ __forceinline__ void gates_of(Two g, Two& f, Two& rest) { gates_from(exp_of_minus<T>(g), f, rest); }
+template <class T> __device__ __forceinline__ void gate_of(float g, float& f, float& rest) {
+    const float e = sizeof(T) == 4 ? expf(-g) : exp2_of(g * -1.4426950408889634f);
     f = inverse_of(1.f + e);
     rest = e > 1.f ? 1.f - f : e * f;
 }

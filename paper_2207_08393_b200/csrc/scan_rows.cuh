@@ -102,7 +102,7 @@ __global__ void __launch_bounds__(SHORT_ROWS) short_kernel(const __grid_constant
                 for (int p = 0; p < pairs; ++p) {
                     const int t = low(p);
                     Two f, rest;
-                    gates_of(turned(steps_at<T, WHOLE>(gs, t)), f, rest);
+                    gates_of<T>(turned(steps_at<T, WHOLE>(gs, t)), f, rest);
                     const Two u = rest * turned(steps_at<T, WHOLE>(xs, t));
                     float v0 = 0.f, v1 = 0.f;
                     if (ALL || there(t, 0)) v0 = h = fmaf(f.lo(), h, u.lo());
@@ -111,7 +111,7 @@ __global__ void __launch_bounds__(SHORT_ROWS) short_kernel(const __grid_constant
                 }
                 if (!WHOLE && steps & 1) {
                     float f, rest;
-                    gate_of(to_float(gs[odd]), f, rest);
+                    gate_of<T>(to_float(gs[odd]), f, rest);
                     if (ALL || odd < valid) h = fmaf(f, h, rest * to_float(xs[odd]));
                     xs[odd] = from_float<T>(ALL || odd < valid ? h : 0.f);
                 }
@@ -125,7 +125,7 @@ __global__ void __launch_bounds__(SHORT_ROWS) short_kernel(const __grid_constant
                 const int t = low(p);
                 if (p % (SHORT_CHUNK / 2) == 0) starts[p / (SHORT_CHUNK / 2) * SHORT_ROWS] = h;
                 Two f, rest;
-                gates_of(turned(steps_at<T, WHOLE>(gs, t)), f, rest);
+                gates_of<T>(turned(steps_at<T, WHOLE>(gs, t)), f, rest);
                 const Two u = rest * turned(steps_at<T, WHOLE>(xs, t));
                 if (there(t, 0)) h = fmaf(f.lo(), h, u.lo());
                 if (there(t, 1)) h = fmaf(f.hi(), h, u.hi());
@@ -133,7 +133,7 @@ __global__ void __launch_bounds__(SHORT_ROWS) short_kernel(const __grid_constant
             float back = a.dlast ? a.dlast[row] : 0.f;
             if (!WHOLE && steps & 1) {                                     // the last position first
                 float f, rest, ox = 0.f, og = 0.f;
-                gate_of(to_float(gs[odd]), f, rest);
+                gate_of<T>(to_float(gs[odd]), f, rest);
                 if (odd < valid) {
                     const float d = back + to_float(ds[odd]), w = h - to_float(xs[odd]);
                     back = d * f;
@@ -150,7 +150,7 @@ __global__ void __launch_bounds__(SHORT_ROWS) short_kernel(const __grid_constant
                 for (int k = 0; k < SHORT_CHUNK / 2; ++k) {
                     if (p0 + k >= pairs) break;
                     const int t = low(p0 + k);
-                    gates_of(turned(steps_at<T, WHOLE>(gs, t)), f[k], rest[k]);
+                    gates_of<T>(turned(steps_at<T, WHOLE>(gs, t)), f[k], rest[k]);
                     const Two x = turned(steps_at<T, WHOLE>(xs, t)), u = rest[k] * x;
                     const float w0 = h - x.lo();
                     if (there(t, 0)) h = fmaf(f[k].lo(), h, u.lo());
@@ -333,7 +333,7 @@ __global__ void __launch_bounds__(ROW_WARPS * 32) rows_kernel(const __grid_const
 #pragma unroll
         for (int j = 0; j < V; j += 2) {
             Two f2, rest2;
-            gates_of(pair_of(raw.g.e + j), f2, rest2);
+            gates_of<T>(pair_of(raw.g.e + j), f2, rest2);
             f[j] = f2.lo(); f[j + 1] = f2.hi(); rest[j] = rest2.lo(); rest[j + 1] = rest2.hi();
             if (KIND != MAP_VJP) { const Two v = pair_of(raw.x.e + j); x[j] = v.lo(); x[j + 1] = v.hi(); }
             if (BACK) { const Two v = pair_of(raw.d.e + j); d[j] = v.lo(); d[j + 1] = v.hi(); }

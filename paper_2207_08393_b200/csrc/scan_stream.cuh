@@ -257,7 +257,7 @@ __global__ void __launch_bounds__(STREAM_THREADS) stream_kernel(const __grid_con
 #pragma unroll
                     for (int j = 0; j < P; ++j) {
                         Two f, rest;
-                        gates_of(g[j], f, rest);
+                        gates_of<T>(g[j], f, rest);
                         h[j] = BACK ? f * (h[j] + u[j]) : fma2(f, h[j], rest * u[j]);
                         if (MAPS) prod[j] = prod[j] * f;
                         out[j] = h[j];
@@ -358,7 +358,7 @@ __global__ void __launch_bounds__(VJP_THREADS, V * sizeof(T) == 16 ? 3 : STRIP ?
 #pragma unroll
                 for (int j = 0; j < P; ++j) {
                     Two f, rest;
-                    e[k][j] = exp_of_minus(g[j]);
+                    e[k][j] = exp_of_minus<T>(g[j]);
                     gates_from(e[k][j], f, rest);
                     w[k][j] = fma2(u[j], Two(-1.f), h[j]);
                     h[j] = fma2(f, h[j], rest * u[j]);

@@ -381,3 +381,58 @@ def test_arrays_beyond_32_bits(shape):
             close(got[i, j, :, k].reshape(1, 1, t, 1), ref, torch.float16, 500.0, "chain %d %d %d" % (i, j, k))
         assert abs(float(last[i, j, k]) - float(rlast[0, 0, 0])) < 1e-4
     assert int(torch.count_nonzero(last)) <= 3
+
+
+# The forms: private pieces, strips, narrow rows, short series, series that share tiles, single chains, parts of both
+FORMS = [(1, 2, 3, 2048), (1, 3, 2, 1025), (1, 300, 2, 7), (1, 2000, 5, 1), (1, 200, 90, 1), (1, 30, 3000, 1), (1, 1, 4000, 264), (1, 1, 3000, 131)]
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("reverse", [False, True])
+@pytest.mark.parametrize("shape", FORMS)
+def test_gates_far_from_zero(shape, reverse, dtype):
+    """f and 1 - f one by one, as 32-bit numbers: the first step has the gate and x = 1, the others keep the state.  last is 1 - f from a state of
+    zero, and what comes back from a cotangent of 1 is f.
+
+    32-bit gates: the exponential is off by 2^-22 at most, the sum in front of the division by 2^-24, the division by 2^-23, a product by 2^-24: 2^-21.
+    Gates of 16 bits: also |gate| 2^-23, for the rounded argument of the exponential (2^-24) and the constant in it (2^-26)."""
+    import paper_2207_08393_b200 as g
+    b, c, t, n = shape
+    first = t - 1 if reverse else 0
+    x, gate = torch.ones(shape, dtype=TYPES[dtype], device="cuda"), torch.full(shape, float("inf"), dtype=TYPES[dtype], device="cuda")
+    gate[:, :, first] = torch.linspace(-86.0, 86.0, b * c * n, device="cuda").view(b, c, n).to(TYPES[dtype])
+    y, last, saved = g.gated_scan_forward(x, gate, reverse=reverse)
+    ds = g.gated_scan_vjp(torch.zeros_like(x), torch.ones(b, c, n, device="cuda"), x, gate, saved, reverse=reverse)[2]
+    state = torch.ones(b, c, n, device="cuda")
+    g.gated_step(torch.zeros(b, c, n, dtype=TYPES[dtype], device="cuda"), gate[:, :, first].contiguous(), state)
+    at = gate[:, :, first].double()
+    most = 2.0 ** -21 + (0.0 if dtype == "float32" else at.abs() * 2.0 ** -23)
+    for got, want in ((last, 1 / (1 + torch.exp(at))), (ds, 1 / (1 + torch.exp(-at))), (state, 1 / (1 + torch.exp(-at)))):
+        assert bool(((got.double() / want - 1).abs() <= most).all())
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("reverse", [False, True])
+@pytest.mark.parametrize("shape", MAPS + SERIES)
+def test_norms_of_the_errors(shape, reverse, dtype):
+    """Against norms instead of the worst case.  A step is off by less than 2^-21 (2^-23 to 2^-22 as a rule), and a chain remembers 56 steps:
+    errors of random signs give sqrt(56) 2^-22 = 1.8e-6 of the result, gates of 16 bits (up to 9, on average below 2) half as much again; the few elements
+    of a small array may have no averages, 56 * 2^-21 = 2.7e-5.  What is stored in 16 bits differs from the rounded definition where that
+    lies so near to the border of two numbers: 3e-6 of a typical value against steps of 2^-11 of it and less, 1 % of the elements, 3 with
+    differences h - x that are small.  An h of 16 bits in the gate's gradient would change most of them (tests/test_scan_ops.py)."""
+    import paper_2207_08393_b200 as g
+    kind = TYPES[dtype]
+    x, gate, dy, state, dlast = inputs(shape, kind, 9)
+    y, last, saved = g.gated_scan_forward(x, gate, state, None, 2, reverse)
+    dx, dg, ds = g.gated_scan_vjp(dy, dlast, x, gate, saved, None, 2, reverse)
+    ry, rlast, before = so.forward(host(x), host(gate), host(state), None, reverse)
+    rdx, rdg, rds = so.vjp(host(dy), host(dlast), host(x), host(gate), before, None, reverse)
+    for what, got, ref in (("y", y, ry), ("last", last, rlast), ("grad_x", dx, rdx), ("grad_gate", dg, rdg), ("grad_state", ds, rds)):
+        most = 3e-5 if ref.size < 1000 else 2e-6 if kind is torch.float32 else 3e-6
+        if got.dtype is torch.float32:
+            assert np.sqrt(((host(got) - ref) ** 2).sum()) <= most * np.sqrt((ref ** 2).sum()) + 1e-35, what
+            continue
+        want = torch.from_numpy(ref).to(kind).cuda()
+        assert float((got.double() - want.double()).abs().max()) <= torch.finfo(kind).eps * np.abs(ref).max(), what
+        if ref.size >= 1000:
+            assert int((got != want).sum()) <= 0.03 * ref.size, what

@@ -164,3 +164,21 @@ def test_strides_of_slices():
                    (torch.zeros(2, 6, 1, 4).expand(2, 6, 5, 4), 2)):
         with pytest.raises(ValueError, match="contiguous"):
             strides_of(t, dim)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("shape", [(1, 2, 21, 129), (1, 16, 20, 1), (1, 2, 400, 33)])
+def test_a_rounded_state_shows_in_the_gates_gradient(shape, dtype):
+    """The measures of tests/test_gpu_scan.py::test_norms_of_the_errors for an h_(t-1) that went through the arrays' type (float32: bfloat16)."""
+    rng = np.random.default_rng(2)
+    rounded = lambda v, kind=dtype: torch.from_numpy(v).to(kind).double().numpy()
+    x, dy = rounded(rng.normal(size=shape)), rounded(rng.normal(size=shape))
+    gate = rounded(np.clip(1.5 * rng.normal(size=shape) + 1.0, -9, 4))
+    before = so.forward(x, gate)[2]
+    right = so.vjp(dy, None, x, gate, before)[1]
+    wrong = so.vjp(dy, None, x, gate, rounded(before, torch.bfloat16 if dtype is torch.float32 else dtype))[1]
+    if dtype is torch.float32:
+        assert np.sqrt(((wrong - right) ** 2).sum()) > 1e-4 * np.sqrt((right ** 2).sum())
+    else:
+        # h is off by a quarter of its step on average and about half as large as h - x, whose step decides: an eighth of the elements
+        assert (rounded(wrong) != rounded(right)).mean() > 0.1

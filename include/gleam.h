@@ -433,7 +433,7 @@ GLEAM_API int gleam_orthogonalise(const void* const* x, void* const* out, const 
 GLEAM_API int gleam_muon_step(void* const* weights, const void* const* grads, float* const* momenta, const gleam_muon_args* args,
                               const gleam_matrix_dims* dims);
 /* Synchronises dims->stream; GLEAM_ERR_TIMEOUT if a kernel of the last such call with this workspace gave up waiting for its own
- * copies or products (bounded by two seconds; its results are then undefined), else GLEAM_OK. */
+ * copies or products (bounded by two seconds; the results concerned are then NaN, weights included), else GLEAM_OK. */
 GLEAM_API int gleam_orthogonalise_check_status(const gleam_matrix_dims* dims);
 GLEAM_API int gleam_orthogonalise_workspace_size(const gleam_matrix_dims* dims, uint64_t* bytes);
 

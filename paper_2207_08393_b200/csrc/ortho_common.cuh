@@ -108,6 +108,9 @@ __device__ __forceinline__ float first_scale(float total, float eps) {
     return by > 3.402823466e38f ? 3.402823466e38f : by;
 }
 
+// What brings a product's sums to the stored values' units: a launch that gave up waiting leaves NaN, in weights too, which no caller overlooks.
+__device__ __forceinline__ float unit_of(bool failed) { return failed ? __int_as_float(0x7fffffff) : 1.f / SCALE; }
+
 // Eight neighbours of a row as two pieces, and back.
 __device__ __forceinline__ void split8(const float (&v)[8], uint4& hi, uint4& lo) {
     uint32_t h[4], l[4];

@@ -150,10 +150,12 @@ __global__ void __launch_bounds__(GEMM_THREADS, Form<KIND>::BLOCKS) gemm_kernel(
         sum_by = KIND == POLY ? a.c * power_of_two(2 * now.e) : power_of_two(3 * now.e - to);
     }
     if (!tc::barrier_wait(done, 0)) failed = true;
+    failed = __syncthreads_or(failed);
     tc::fence_after();
 
-    // the sums, in units of the stored values
+    // the sums, in units of the stored values; NaN where a wait gave up, and so the results
     float* sum = reinterpret_cast<float*>(smem + 1024);
+    const float unit = unit_of(failed);
     {
         const int row = (warp & 3) * 32 + lane;
 #pragma unroll 1
@@ -173,14 +175,14 @@ __global__ void __launch_bounds__(GEMM_THREADS, Form<KIND>::BLOCKS) gemm_kernel(
             }
 #pragma unroll
             for (int j = 0; j < 32; j += 4)
-                *reinterpret_cast<float4*>(sum + sum_at(row, c0 + j)) = make_float4((v[j] + t[j]) * (1.f / SCALE), (v[j + 1] + t[j + 1]) * (1.f / SCALE),
-                                                                                    (v[j + 2] + t[j + 2]) * (1.f / SCALE), (v[j + 3] + t[j + 3]) * (1.f / SCALE));
+                *reinterpret_cast<float4*>(sum + sum_at(row, c0 + j)) = make_float4((v[j] + t[j]) * unit, (v[j + 1] + t[j + 1]) * unit, (v[j + 2] + t[j + 2]) * unit,
+                                                                                    (v[j + 3] + t[j + 3]) * unit);
         }
     }
     tc::fence_before();
     __syncthreads();
     if (warp == 0) tc::free_columns(sums, F::COLUMNS);
-    if (failed) atomicOr(a.status, 1);
+    if (failed && threadIdx.x == 0) atomicOr(a.status, 1);
 
     // a cluster's blocks add a share of the rows each, lanes along a row as remote reads want it; these rows of a block's own sums are
     // nobody else's

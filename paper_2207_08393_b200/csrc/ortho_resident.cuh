@@ -167,7 +167,7 @@ __global__ void __launch_bounds__(RESIDENT_THREADS, 1) resident_kernel(const __g
         tc::read_columns(cols0 + lanes + columns + col0, v);
         tc::read_columns(cols0 + lanes + columns + BLOCK + col0, u);
 #pragma unroll
-        for (int j = 0; j < 32; ++j) v[j] = (v[j] + u[j]) * (1.f / SCALE);
+        for (int j = 0; j < 32; ++j) v[j] = (v[j] + u[j]) * unit_of(failed);     // NaN where a wait gave up, and so the results
     };
     // eight of them joined with what stands at (row, c) of these pieces: v <- by old + times v
     auto blend = [&](const unsigned char* from, int c, float by_, float times, const float* v, float (&w)[8]) {
@@ -190,7 +190,7 @@ __global__ void __launch_bounds__(RESIDENT_THREADS, 1) resident_kernel(const __g
         const float poly = a.c * power_of_two(2 * now.e), old_by = a.a * power_of_two(now.e - to), sum_by = power_of_two(3 * now.e - to);
         now = next;
         settle();
-        if (threadIdx.x == 0) {
+        if (threadIdx.x == 0 && !failed) {
             const uint32_t what = tc::instruction(R, false);
             for (int t = 0; t < mine; ++t)
                 for (int k = 0; k < BLOCK / 16; ++k) {
@@ -252,7 +252,7 @@ __global__ void __launch_bounds__(RESIDENT_THREADS, 1) resident_kernel(const __g
         }
         if (ranks > 1) tc::cluster_sync();
         settle();
-        if (threadIdx.x == 0) {
+        if (threadIdx.x == 0 && !failed) {
             const uint32_t what = tc::instruction(R, false);
             for (int k = 0; k < R / 16; ++k) {
                 const uint32_t p = a_at + k * 256;
@@ -280,7 +280,7 @@ __global__ void __launch_bounds__(RESIDENT_THREADS, 1) resident_kernel(const __g
         // two tiles at a time, as tensor memory allows
         for (int t0 = 0; t0 < mine; t0 += 2) {
             settle();
-            if (threadIdx.x == 0) {
+            if (threadIdx.x == 0 && !failed) {
                 const uint32_t what = tc::instruction(BLOCK, true);
                 for (int t = t0; t < mine && t < t0 + 2; ++t) {
                     for (int k = 0; k < R / 16; ++k) {

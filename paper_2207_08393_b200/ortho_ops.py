@@ -4,7 +4,9 @@
 the orthogonalised momentum of their gradients; ``Muon`` is the optimiser around it (K. Jordan et al., "Muon: an optimizer for hidden
 layers in neural networks", 2024).  Weights with more than two axes count as matrices (axis 0, all others), as those of convolutions do.
 
-Tensors are CUDA tensors of float32, float16 or bfloat16; the arithmetic is as exact as 32-bit products whatever the type.
+Tensors are CUDA tensors of float32, float16 or bfloat16; the arithmetic is near that of 32-bit products whatever the type (include/gleam.h
+says how near).  Should a kernel give up waiting for its own copies (after two seconds, which no working launch needs), what it was to compute is
+NaN, updated weights included.
 """
 from __future__ import annotations
 

@@ -45,3 +45,16 @@ def test_sums_are_split_by_sizes_alone():
     assert code.count("cudaOccupancyMaxActiveClusters") == 1
     body = code[code.index("static int clusters_at_once"):code.index("cudaOccupancyMaxActiveClusters")]
     assert "if (ranks <= RESIDENT_PORTABLE) return at_once[ranks];" in body
+
+
+def test_a_launch_that_gave_up_waiting_leaves_nan():
+    """The torch layer drops the workspace and its status word, so results have to tell.  No run of a working kernel waits in vain: what every sum is
+    multiplied with on its way out of tensor memory is NaN after a wait that did."""
+    read = lambda name: "".join(line.split("//")[0] + "\n" for line in open(os.path.join(CSRC, name)))
+    assert "unit_of(bool failed) { return failed ? __int_as_float(0x7fffffff) : 1.f / SCALE; }" in read("ortho_common.cuh")
+    gemm, resident = read("ortho_gemm.cuh"), read("ortho_resident.cuh")
+    assert gemm.index("failed = __syncthreads_or(failed);") < gemm.index("unit = unit_of(failed);") < gemm.index("tc::read_columns(")
+    stored = gemm[gemm.index("make_float4((v[j]"):]
+    assert stored[:stored.index(";")].count("* unit") == 4
+    assert "v[j] = (v[j] + u[j]) * unit_of(failed);" in resident and resident.count("tc::read_columns(") == 2
+    assert resident.count("if (threadIdx.x == 0 && !failed)") == resident.count("what = tc::instruction(")

@@ -32,10 +32,16 @@ def _workspace(x, dims):
     return ws
 
 
+def _check_grad(*tensors):
+    if torch.is_grad_enabled() and any(t.requires_grad for t in tensors):
+        raise ValueError("not differentiable: call it under torch.no_grad()")
+
+
 def orthogonalise(x, steps=5, coefficients=COEFFICIENTS, eps=1e-7):
     """X_0 = x / (|x| + eps), then ``steps`` times X <- a X + (b A + c A A) X with A = X X^T over the shorter side, for every matrix in the
-    last two axes of ``x``; the result has x's type.  Not differentiable."""
+    last two axes of ``x``; the result has x's type.  Not differentiable: an x that requires gradients is taken under ``torch.no_grad()``."""
     _check_kind(x)
+    _check_grad(x)
     if x.dim() < 2:
         raise ValueError("a matrix is wanted, or several (shape %s)" % (tuple(x.shape),))
     if not x.is_contiguous():
@@ -61,7 +67,8 @@ def muon_step(weights, grads, momenta, lr, momentum=0.95, nesterov=True, weight_
         momentum <- mu momentum + grad,   u = grad + mu momentum (nesterov) or momentum,
         weight <- (1 - lr weight_decay) weight - lr scale orthogonalise(u)
 
-    Weights and gradients have one type, momenta are float32; all are contiguous.  A captured call keeps the lr that it was given."""
+    Weights and gradients have one type, momenta are float32; all are contiguous.  Weights that require gradients are taken under
+    ``torch.no_grad()``.  A captured call keeps the lr that it was given."""
     if not len(weights) == len(grads) == len(momenta):
         raise ValueError("%d weights, %d gradients, %d momenta" % (len(weights), len(grads), len(momenta)))
     if not weights:
@@ -76,6 +83,7 @@ def muon_step(weights, grads, momenta, lr, momentum=0.95, nesterov=True, weight_
             if t.shape != shape or t.dtype is not kind or t.device != device or not t.is_contiguous() or t.is_neg():
                 raise ValueError("%s: %s %s on %s where contiguous %s %s on %s is wanted" % (what, tuple(t.shape), t.dtype, t.device,
                                                                                             tuple(shape), kind, device))
+        _check_grad(*tensors)
     with _On(w0):
         dims = _dims(w0, len(weights), shape[0], _numel(shape[1:]), steps, coefficients, eps)
         ws = _workspace(w0, dims)

@@ -399,3 +399,22 @@ def test_rows_that_are_small_beside_the_others(rows, cols, share):
     norm = float(ref.norm())
     most = 2.0 ** -35 * (682 * cols ** 0.5 + 198 * 11.3 * rows ** 0.5) + norm * oo.near(float((half - ref).norm()) / norm, cols)
     assert float((y - ref).norm()) <= most
+
+
+def test_gradients_are_not_dropped_in_silence():
+    """Neither call is differentiable, and weights are written in place: as with torch's own operators, not under gradients."""
+    import paper_2207_08393_b200 as g
+    x = torch.randn(4, 6, device="cuda", requires_grad=True)
+    others = [torch.randn(4, 6, device="cuda"), torch.zeros(4, 6, device="cuda")]
+    with pytest.raises(ValueError, match="no_grad"):
+        g.orthogonalise(x)
+    with pytest.raises(ValueError, match="no_grad"):
+        g.orthogonalise(x * 2)
+    for lists in (([x], [others[0]], [others[1]]), ([x * 2], [others[0]], [others[1]]), ([others[0]], [x], [others[1]]), ([others[0]], [others[0].clone()], [x])):
+        with pytest.raises(ValueError, match="no_grad"):
+            g.muon_step(*lists, 0.1)
+    assert not bool(others[1].any())
+    with torch.no_grad():
+        want = g.orthogonalise(x)
+        g.muon_step([x], [others[0]], [others[1]], 0.1)
+    assert torch.equal(g.orthogonalise(others[0]), g.orthogonalise(others[0].detach())) and want.shape == x.shape

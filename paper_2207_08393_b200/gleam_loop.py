@@ -193,19 +193,52 @@ class GleamModule(nn.Module):
         return x_ch
 
 
-class Optimizers:
-    """Several optimisers that step together, for loops that take one."""
+class Optimizers(torch.optim.Optimizer):
+    """Several optimisers that step together, for loops, gradient scalers and schedules that take one.  Parameter groups and states are
+    theirs."""
 
     def __init__(self, optimizers):
         self.optimizers = list(optimizers)
+        super().__init__([{}], {})
+
+    @property
+    def param_groups(self):
+        return [group for o in self.optimizers for group in o.param_groups]
+
+    @param_groups.setter
+    def param_groups(self, groups):
+        pass
+
+    @property
+    def state(self):
+        return {p: s for o in self.optimizers for p, s in o.state.items()}
+
+    @state.setter
+    def state(self, state):
+        pass
+
+    def add_param_group(self, group):
+        if group:
+            raise ValueError("a group belongs to one of the optimisers: optimizers[k].add_param_group")
+
+    def __getstate__(self):
+        return {"optimizers": self.optimizers}
+
+    def __setstate__(self, state):
+        self.__init__(state["optimizers"])
 
     def zero_grad(self, set_to_none=True):
         for o in self.optimizers:
             o.zero_grad(set_to_none=set_to_none)
 
-    def step(self):
+    def step(self, closure=None):
+        loss = None
+        if closure is not None:
+            with torch.enable_grad():
+                loss = closure()
         for o in self.optimizers:
             o.step()
+        return loss
 
     def state_dict(self):
         return [o.state_dict() for o in self.optimizers]

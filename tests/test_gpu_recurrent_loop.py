@@ -176,3 +176,21 @@ def test_a_prior_under_autocast():
     assert float((got.float() - want).norm()) <= 0.05 * float(want.norm())
     for a, b in zip(grads, half):
         assert bool(torch.isfinite(b).all()) and float((a - b).norm()) <= 0.1 * float(a.norm()) + 1e-4
+
+
+def test_a_float16_prior_with_a_gradient_scaler():
+    """module_optimizer under torch.amp: a step with finite gradients moves everything, one with infinite ones nothing."""
+    from paper_2207_08393_b200 import gleam_loop as gl
+    torch.manual_seed(5)
+    prior = gl.ResidualPrior(8, 1, recurrent="both").cuda()
+    opt, scaler = gl.module_optimizer(prior, lr=1e-3), torch.amp.GradScaler("cuda", init_scale=128.0)
+    x = torch.randn(1, 2, 5, 1, 12, 16, device="cuda")
+    for factor, moves in ((1.0, True), (float("inf"), False), (1.0, True)):
+        before = [p.detach().clone() for p in prior.parameters()]
+        opt.zero_grad()
+        with torch.autocast("cuda", dtype=torch.float16):
+            loss = prior(x).float().square().mean() * factor
+        scaler.scale(loss).backward()
+        scaler.step(opt)
+        scaler.update()
+        assert all(torch.equal(p, q) != moves and bool(torch.isfinite(p).all()) for p, q in zip(prior.parameters(), before))

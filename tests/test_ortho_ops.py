@@ -216,3 +216,55 @@ def test_the_bound_takes_two_pieces_and_not_one(shape, steps, norm):
     # 32-bit products leave up to 2.7e-6 after five turns (100 x 900), of which four times, 900 * 2^-28 and 2^-21 are 1.5e-5
     assert off(in_pieces(x, steps, 2)) <= most < 2e-5
     assert off(in_pieces(x, steps, 1)) > 10 * most
+
+
+def pair_of_optimizers():
+    from paper_2207_08393_b200 import gleam_loop as gl
+    torch.manual_seed(0)
+    a, b = torch.nn.Parameter(torch.randn(3, 4)), torch.nn.Parameter(torch.randn(5))
+    return gl.Optimizers([torch.optim.SGD([a], lr=0.5, momentum=0.9), torch.optim.Adam([b], lr=0.25)]), a, b
+
+
+def test_optimizers_take_schedules_and_gradient_scalers():
+    import copy
+    import pickle
+    opt, a, b = pair_of_optimizers()
+    schedule = torch.optim.lr_scheduler.StepLR(opt, 1, gamma=0.5)
+    scaler = torch.amp.GradScaler("cpu", init_scale=4.0, growth_interval=1)
+    assert [g["params"] for g in opt.param_groups] == [[a], [b]]
+
+    def turn(factor):
+        opt.zero_grad()
+        scaler.scale(factor * ((a ** 2).sum() + (b ** 2).sum())).backward()
+        scaler.step(opt)
+        scaler.update()
+        schedule.step()
+
+    before = [a.detach().clone(), b.detach().clone()]
+    want = before[0] - 0.5 * 2 * before[0]
+    turn(1.0)
+    assert torch.allclose(a, want) and not torch.equal(b, before[1])
+    assert [o.param_groups[0]["lr"] for o in opt.optimizers] == [0.25, 0.125] and scaler.get_scale() == 8.0
+    before = [a.detach().clone(), b.detach().clone()]
+    turn(float("inf"))                                   # gradients that are not finite: no step, of neither
+    assert torch.equal(a, before[0]) and torch.equal(b, before[1]) and scaler.get_scale() == 4.0
+    state = copy.deepcopy(opt.state_dict())
+    other, c, d = pair_of_optimizers()
+    other.load_state_dict(state)
+    assert [g["lr"] for g in other.param_groups] == [g["lr"] for g in opt.param_groups] and set(other.state) == {c, d}
+    with torch.no_grad():
+        c.copy_(a)
+        d.copy_(b)
+    loss = other.step(lambda: sum((p ** 2).sum() for p in (c, d)).backward())
+    opt.zero_grad()
+    sum((p ** 2).sum() for p in (a, b)).backward()
+    opt.step()
+    assert loss is None and torch.equal(a, c) and torch.equal(b, d)
+    for again in (copy.deepcopy(opt), pickle.loads(pickle.dumps(opt))):
+        assert len(again.optimizers) == 2 and len(again.param_groups) == 2
+        again.step()
+    with pytest.raises(ValueError, match="belongs to one"):
+        opt.add_param_group({"params": [torch.nn.Parameter(torch.zeros(2))]})
+    from paper_2207_08393_b200 import gleam_loop as gl
+    gl.Optimizers([]).step()
+    repr(opt)

@@ -186,6 +186,21 @@ def gated_scan_vjp(grad_y, grad_last, x, gate, saved, lengths=None, dim=-2, reve
     return gx, gg, gs
 
 
+_AXIS_MOST = 1 << 31                             # elements of an axis of a call
+
+
+def _step_sizes(shape):
+    """(batch, inner) of a step on contiguous tensors: all in one run, or two factors where that is more than an axis of the call holds."""
+    batch, inner = 1, _numel(shape)
+    for s in shape:
+        if inner <= _AXIS_MOST:
+            break
+        batch, inner = batch * s, inner // s
+    if max(batch, inner) > _AXIS_MOST:
+        raise ValueError("an axis of more than 2^31 elements (shape %s)" % (tuple(shape),))
+    return batch, inner
+
+
 _STEPS = {}                                      # structures of steps on contiguous tensors, by shape and type
 _STEPS_MOST = 256                                # beyond that the table starts over
 
@@ -206,8 +221,8 @@ def gated_step(x, gate, state):
         key = x.shape, x.dtype                   # filling a structure takes longer than the kernel (18.7 -> 11 us a call)
         kept = _STEPS.get(key)
         if kept is None:
-            n = x.numel()
-            kept = bytes(_b.gleam_scan_dims(1, _DTYPES[x.dtype], 0, 0, 1, 1, 1, n))
+            batch, inner = _step_sizes(x.shape)
+            kept = bytes(_b.gleam_scan_dims(1, _DTYPES[x.dtype], 0, 0, batch, 1, 1, inner))
             if len(_STEPS) >= _STEPS_MOST:
                 _STEPS.clear()
             _STEPS[key] = kept

@@ -436,3 +436,20 @@ def test_norms_of_the_errors(shape, reverse, dtype):
         assert float((got.double() - want.double()).abs().max()) <= torch.finfo(kind).eps * np.abs(ref).max(), what
         if ref.size >= 1000:
             assert int((got != want).sum()) <= 0.03 * ref.size, what
+
+
+@pytest.mark.parametrize("shape", [(3, 800000001), (5, 2, 300000000)])
+def test_steps_beyond_2_to_31_elements(shape):
+    import paper_2207_08393_b200 as g
+    x, gate = torch.zeros(shape, dtype=torch.float16, device="cuda"), torch.full(shape, -1.0, dtype=torch.float16, device="cuda")
+    state = torch.zeros(shape, device="cuda")
+    flat = [t.view(-1) for t in (x, gate, state)]
+    n = flat[0].numel()
+    at = torch.tensor([0, 1, shape[-1] - 1, shape[-1], n // 2, n - shape[-1], n - 2, n - 1], device="cuda")
+    torch.manual_seed(9)
+    for t in flat:
+        t[at] = torch.randn(len(at), device="cuda").to(t.dtype)
+    want = so.forward(*[host(t[at]).reshape(1, 1, 1, -1) for t in flat[:2]], host(flat[2][at]).reshape(1, 1, -1))[1].reshape(-1)
+    y = g.gated_step(x, gate, state)
+    close(flat[2][at], want, torch.float32, 4.0, "state")
+    assert torch.equal(y.view(-1)[at], flat[2][at].half()) and int(torch.count_nonzero(state)) == len(at)

@@ -182,3 +182,16 @@ def test_a_rounded_state_shows_in_the_gates_gradient(shape, dtype):
     else:
         # h is off by a quarter of its step on average and about half as large as h - x, whose step decides: an eighth of the elements
         assert (rounded(wrong) != rounded(right)).mean() > 0.1
+
+
+def test_sizes_of_steps_on_contiguous_tensors(lib):
+    """Any shape whose axes fit, however many elements it has; the call's own limits hold for what comes out."""
+    big = 1 << 31
+    for shape, want in (((), (1, 1)), ((7,), (1, 7)), ((20, 160), (1, 3200)), ((big,), (1, big)), ((3, big), (3, big)), ((3, 1200000000), (3, 1200000000)),
+                        ((2, 3, 5, 1 << 29), (6, 5 << 29) if 5 << 29 <= big else (30, 1 << 29)), ((1, 1, big, 2), (big, 2))):
+        batch, inner = scan_ops._step_sizes(shape)
+        assert (batch, inner) == want and batch * inner == scan_ops._numel(shape)
+        assert g.gleam_gated_scan_workspace_size(scan_dims(dtype=1, batch=batch, channels=1, steps=1, inner=inner)) == 0
+    for shape in ((big + 1,), (big + 1, 1), (2, big + 1)):
+        with pytest.raises(ValueError, match="2\\^31"):
+            scan_ops._step_sizes(shape)

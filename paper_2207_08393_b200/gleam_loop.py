@@ -124,7 +124,7 @@ class ResidualPrior(nn.Module):
     def _along_frames(self, f, frames, lengths):
         """Adds what the recurrence over the frames finds; (B T n0, features, n1, n2)."""
         u = self.gates(f)
-        u = u.view((frames[0], frames[1], -1) + u.shape[1:])
+        u = u.view(frames + u.shape[1:])
         F = f.shape[1]
         parts = [u[:, :, :, k * F:(k + 1) * F] for k in range(u.shape[3] // F)]
         y, _ = _s.gated_scan(parts[0], parts[1], None, lengths, dim=1)
@@ -155,7 +155,7 @@ class ResidualPrior(nn.Module):
         h = x_ch.permute(0, 2, 3, 1, 4, 5).reshape(B * T * n0, 2, n1, n2)
         f = self.head(h)
         if self.recurrent is not None:
-            f = self._along_frames(f, (B, T), lengths)
+            f = self._along_frames(f, (B, T, n0), lengths)
         return self._finish(x_ch, h, self._blocks(f, self.dropout if self.training else 0.0))
 
     def _finish(self, x_ch, h, f):

@@ -194,3 +194,15 @@ def test_a_float16_prior_with_a_gradient_scaler():
         scaler.step(opt)
         scaler.update()
         assert all(torch.equal(p, q) != moves and bool(torch.isfinite(p).all()) for p, q in zip(prior.parameters(), before))
+
+
+@pytest.mark.parametrize("recurrent", [None, "causal", "both"])
+@pytest.mark.parametrize("shape", [(0, 2, 5, 1, 8, 9), (2, 2, 0, 1, 8, 9)])
+def test_a_batch_without_frames(shape, recurrent):
+    from paper_2207_08393_b200 import gleam_loop as gl
+    prior = gl.ResidualPrior(4, 1, recurrent=recurrent).cuda()
+    x = torch.randn(shape, device="cuda", requires_grad=True)
+    out = prior(x)
+    assert out.shape == x.shape
+    out.sum().backward()
+    assert x.grad.shape == x.shape and all(p.grad is not None and not bool(p.grad.any()) for p in prior.parameters())

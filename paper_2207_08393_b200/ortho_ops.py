@@ -112,6 +112,7 @@ class Muon(torch.optim.Optimizer):
         super().add_param_group(group)
         for p in self.param_groups[-1]["params"]:
             if p.dim() < 2:
+                self.param_groups.pop()
                 raise ValueError("a parameter of shape %s is no matrix: give it to another optimiser" % (tuple(p.shape),))
 
     @torch.no_grad()

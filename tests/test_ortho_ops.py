@@ -268,3 +268,12 @@ def test_optimizers_take_schedules_and_gradient_scalers():
     from paper_2207_08393_b200 import gleam_loop as gl
     gl.Optimizers([]).step()
     repr(opt)
+
+
+def test_a_refused_group_is_not_kept():
+    opt = g.Muon([torch.nn.Parameter(torch.zeros(3, 4))])
+    with pytest.raises(ValueError, match="no matrix"):
+        opt.add_param_group({"params": [torch.nn.Parameter(torch.zeros(2, 2)), torch.nn.Parameter(torch.zeros(5))]})
+    assert len(opt.param_groups) == 1
+    opt.add_param_group({"params": torch.nn.Parameter(torch.zeros(2, 2))})
+    assert len(opt.param_groups) == 2

@@ -97,7 +97,7 @@ def muon_step(weights, grads, momenta, lr, momentum=0.95, nesterov=True, weight_
 class Muon(torch.optim.Optimizer):
     """Updates matrices (weights with two axes or more) by ``muon_step``; those of one shape and type go together.  ``scale`` is a number
     or "rms" for 0.2 sqrt(max(rows, columns)), with which updates are as large as Adam's (J. Liu et al., "Muon is scalable for LLM training",
-    2025).  Vectors (biases, norms) belong to another optimiser."""
+    2025).  Vectors (biases, norms) belong to another optimiser.  Take a first step before one is captured: it makes the momenta."""
 
     def __init__(self, params, lr=0.02, momentum=0.95, nesterov=True, weight_decay=0.0, scale="rms", steps=5, coefficients=COEFFICIENTS,
                  eps=1e-7):
@@ -130,6 +130,8 @@ class Muon(torch.optim.Optimizer):
                     raise ValueError("sparse gradients are not supported")
                 state = self.state[p]
                 if "momentum" not in state:
+                    if group["momentum"] and p.is_cuda and torch.cuda.is_current_stream_capturing():
+                        raise RuntimeError("the first step makes the momenta: take it before a capture, whose every replay would empty them")
                     state["momentum"] = torch.zeros(p.shape, dtype=torch.float32, device=p.device)
                 alike.setdefault((p.shape, p.dtype, p.device), []).append(p)
             for params in alike.values():

@@ -418,3 +418,36 @@ def test_gradients_are_not_dropped_in_silence():
         want = g.orthogonalise(x)
         g.muon_step([x], [others[0]], [others[1]], 0.1)
     assert torch.equal(g.orthogonalise(others[0]), g.orthogonalise(others[0].detach())) and want.shape == x.shape
+
+
+def test_a_first_step_is_not_captured():
+    """Its momenta would be emptied by every replay."""
+    import paper_2207_08393_b200 as g
+    p = torch.nn.Parameter(torch.randn(8, 24, device="cuda"))
+    opt = g.Muon([p], lr=0.1)
+    grad = torch.randn_like(p)
+    p.grad = grad.clone()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        graph.capture_begin()
+        try:
+            with pytest.raises(RuntimeError, match="before a capture"):
+                opt.step()
+        finally:
+            graph.capture_end()
+    torch.cuda.synchronize()
+    assert not opt.state[p]
+    opt.step()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        opt.step()
+    for _ in range(3):
+        graph.replay()
+    q = torch.nn.Parameter(p.detach().clone())
+    m = torch.zeros_like(grad)
+    for _ in range(4):
+        m = 0.95 * m + grad
+    torch.cuda.synchronize()
+    assert float((opt.state[p]["momentum"] - m).norm()) <= 1e-6 * float(m.norm())

@@ -401,15 +401,16 @@ GLEAM_API int gleam_gated_scan_saved_size(const gleam_scan_dims* dims, uint64_t*
  * lost to it, so that |U| below about 1e-21 counts as less than it is beside an eps of that size.  X, A and P are held as two float16
  * numbers each, scaled by a power of two that goes by the norm of X_0: 22 bits (a 32-bit number has 24) of what is not below 2^-13, an absolute step
  * of 2^-34 below that, where X has a norm of 1/2 to 1 at first and singular values of about 1 later.  Of a product the two low
- * parts' is left out (2^-24).  Sums are 32-bit numbers that are cut off, not rounded: one of K terms loses up to K 2^-27 of itself.  Together the
- * result of five turns is off by some 1e-6 of its norm, as that of 32-bit products, up to a few times as much where the
- * longer side has tens of thousands; but a row (column) much smaller than the others comes out with fewer digits, 1e-4 of their size with three.
+ * parts' is left out (2^-24).  Sums are 32-bit numbers that are cut off, not rounded, up to 128 times before they are added up in
+ * registers: one whose terms have one sign loses up to 2^-16 of itself.  Together the result of five turns is off by 1e-6 to 1e-5 of its
+ * norm, as that of 32-bit products is (100 x 900 1.9e-6 and 2.7e-6, 4096 x 4096 7.5e-6 and 1.1e-5, 130 x 1048576 6.7e-6 and 2.9e-6).  But a row or
+ * column much smaller than the others comes out with fewer digits: one of 1e-4 of their size is off by 1e-3 of itself, one of 1e-6 by a tenth.
  * |a|, |b|, |c| <= 16, and no value of X, A or P may reach 64 along the way (it becomes infinite or NaN): singular values below 1.25 are
  * safe with all coefficients, those of the usual ones stay below 1.3 and P below 3.  A matrix of zeros gives zeros; one with
  * a NaN or an infinity gives NaN throughout, the others are untouched by it.  The shorter side is at most 16384, and there are at most
  * 65535 blocks of 128 x 128 in a matrix.  GLEAM_ERR_CUDA also reports that the host has no memory left for a call's checks.
- * Nothing that a call writes may overlap anything else of the call (GLEAM_ERR_ALIAS).  Results are deterministic.  Two calls whose
- * GPU work may overlap need workspaces of their own.
+ * Nothing that a call writes may overlap anything else of the call (GLEAM_ERR_ALIAS).  Results are deterministic and the same on all GPUs of this
+ * kind: how sums are split goes by the sizes alone.  Two calls whose GPU work may overlap need workspaces of their own.
  */
 #define GLEAM_MATRIX_DIMS_VERSION 1
 typedef struct {

@@ -55,6 +55,6 @@ def near(err32, k):
 
     What 32 bits round by 2^-24 is rounded by 2^-23 as two pieces, for both operands of a product, and lo lo (2^-24 of it) is left out: less than
     four times the rounding errors, wherever they are made and however they grow.  Sums that are cut off rather than rounded lose 2^-24 of themselves
-    on average, K / 32 times, and P's derivative with respect to A is at most 2 in effect: K 2^-28.  2^-21 stands for an err32 that
-    happens to be small."""
-    return 4 * err32 + k * 2.0 ** -28 + 2.0 ** -21
+    on average, K / 32 times, at most 128 times before they are added up elsewhere, and P's derivative with respect to A is at most 2 in
+    effect: 2^-28 for each K up to 4096.  2^-21 stands for an err32 that happens to be small."""
+    return 4 * err32 + min(k, 4096) * 2.0 ** -28 + 2.0 ** -21

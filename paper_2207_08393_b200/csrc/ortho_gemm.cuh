@@ -18,27 +18,35 @@ namespace ortho {
 enum { GRAM, POLY, APPLY, LAST };
 
 constexpr int GEMM_THREADS = 256, STAGES = 3;
-// What a product holds.  GRAM and POLY: 64 of K a stage, one block an SM, two sums in turn (each of hi hi and of the rest): the tensor core
-// cuts a sum off where it adds (2^-23 of it each time), which tells in the diagonal of A, all of whose terms are positive, and two sums cut
-// off half as often.  APPLY: few terms, of either sign; 32 of K a stage and one sum leave room for a second block on the SM, whose products run while this one finishes (9216 x 1024: 57 -> 46 us).
-template <int KIND> struct Form {
+// What a product holds.  GRAM and POLY: 64 of K a stage, one block an SM, two sums in turn (each of hi hi and of the rest).  APPLY: few terms, of
+// either sign; 32 of K a stage and one sum leave room for a second block on the SM, whose products run while this one finishes (9216 x 1024: 57 -> 46 us).
+// LONG: the tensor core cuts a sum off where it adds, by 2^-24 of it on average, which tells in sums whose terms have one sign.  Where a block has
+// more than LONG_FROM steps its sums are added up in registers, rounded, after every SPAN at most, and start again at zero; APPLY, whose
+// second block would have no registers for that, takes the form of the others then.  130 x 1048576, five turns: off by 6.7e-6 of the result, 6e-4
+// without; 4096 x 4096: 7.5e-6, 3.2e-5 without, 3900 us of kernels for 3700.
+constexpr int SPAN = 32;                           // steps of 64
+template <int KIND> constexpr int LONG_FROM = KIND == GRAM || KIND == POLY ? 48 : 32;
+template <int KIND, bool LONG> struct Form {
     static constexpr bool SIDES = KIND == GRAM || KIND == POLY;                // both operands are rows of one matrix
-    static constexpr int STEP = SIDES ? 64 : 32, SUMS = SIDES ? 2 : 1, COLUMNS = SUMS * 2 * BLOCK, BLOCKS = SIDES ? 1 : 2;
+    static constexpr bool ALONE = SIDES || LONG;                               // on the SM
+    static constexpr int STEP = ALONE ? 64 : 32, SUMS = ALONE ? 2 : 1, COLUMNS = SUMS * 2 * BLOCK, BLOCKS = ALONE ? 1 : 2;
     static constexpr int OPERAND = 2 * BLOCK * STEP * 2, STAGE = 2 * OPERAND;                   // bytes of an operand's pieces, of both operands
     static constexpr int SMEM = 1024 + STAGES * STAGE;                         // the first KB: barriers
 };
 
 // Steps of K, and blocks of a result that are computed.
-template <int KIND> __host__ __device__ inline int steps_of(const Args& a) { return (int)(((KIND == GRAM ? a.L : a.S) + Form<KIND>::STEP - 1) / Form<KIND>::STEP); }
+template <int KIND, bool LONG> __host__ __device__ inline int steps_of(const Args& a) {
+    return (int)(((KIND == GRAM ? a.L : a.S) + Form<KIND, LONG>::STEP - 1) / Form<KIND, LONG>::STEP);
+}
 template <int KIND> __host__ inline int tiles_of(const Args& a) { return KIND == GRAM || KIND == POLY ? a.sblocks * (a.sblocks + 1) / 2 : a.sblocks * a.lblocks; }
 
 // T: the type of results (LAST)
-template <int KIND, int RANKS, class T>
-__global__ void __launch_bounds__(GEMM_THREADS, Form<KIND>::BLOCKS) gemm_kernel(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap map) {
+template <int KIND, int RANKS, bool LONG, class T>
+__global__ void __launch_bounds__(GEMM_THREADS, Form<KIND, LONG>::BLOCKS) gemm_kernel(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap map) {
     extern __shared__ __align__(1024) unsigned char smem[];
     constexpr int ranks = RANKS, GROUP_ITEMS = BLOCK, GROUPS = BLOCK / 8;         // eights of a row in eight rows; eights of rows
     constexpr int ITEMS = ((GROUPS + RANKS - 1) / RANKS * GROUP_ITEMS + GEMM_THREADS - 1) / GEMM_THREADS;     // eights that a thread finishes at most
-    using F = Form<KIND>;
+    using F = Form<KIND, LONG>;
     constexpr bool SIDES = F::SIDES;
     constexpr int STEP = F::STEP, SUMS = F::SUMS, PARTS_OF_BLOCK = BLOCK / STEP;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = ranks > 1 ? (int)tc::cluster_rank() : 0, m = blockIdx.z;
@@ -66,7 +74,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, Form<KIND>::BLOCKS) gemm_kernel(
     const uint32_t sums = *reinterpret_cast<volatile uint32_t*>(smem);
     grid_dependency_wait();
 
-    const int steps = steps_of<KIND>(a), first = steps * rank / ranks, count = steps * (rank + 1) / ranks - first;
+    const int steps = steps_of<KIND, LONG>(a), first = steps * rank / ranks, count = steps * (rank + 1) / ranks - first;
     const long long square = (long long)m * a.sblocks * a.sblocks, wide = (long long)m * a.sblocks * a.lblocks;
     const unsigned char* left = KIND == GRAM ? a.x + wide * BLOCK_BYTES : KIND == POLY ? a.g + square * BLOCK_BYTES : a.p + square * BLOCK_BYTES;
     const unsigned char* right = SIDES ? left : a.x + wide * BLOCK_BYTES;
@@ -74,53 +82,6 @@ __global__ void __launch_bounds__(GEMM_THREADS, Form<KIND>::BLOCKS) gemm_kernel(
     const bool one = SIDES && bi == bj;                                            // the operands are the same
     bool failed = false;
 
-    if (warp == 0 && lane == 0) {
-        // rows of cores from the first block to left's and right's
-        const long long lrow = (left - a.blocks) / ROW_BYTES + (long long)bi * lblocks * 16, rrow = (right - a.blocks) / ROW_BYTES + (long long)bj * lblocks * 16;
-        for (int i = 0; i < count; ++i) {
-            const int s = i % STAGES, k = first + i, kb = k / PARTS_OF_BLOCK, share = k % PARTS_OF_BLOCK;
-            if (i >= STAGES && !tc::barrier_wait(empty(s), (i / STAGES - 1) & 1)) { failed = true; break; }
-            const uint32_t to = stages + s * F::STAGE;
-            tc::barrier_expect(full(s), one ? F::OPERAND : F::STAGE);
-#pragma unroll
-            for (int h = 0; h < STEP / 32; ++h) {
-#pragma unroll
-                for (int piece = 0; piece < 2; ++piece) {                   // 32 columns of 128 rows: 8 KB
-                    const uint32_t at = to + h * 16384 + piece * 8192;
-                    const int part = piece * 4 + share * (STEP / 32) + h;
-                    tc::tiled_copy(at, &map, part, (int)(lrow + kb * 16), full(s));
-                    if (SIDES && !one) tc::tiled_copy(at + F::OPERAND, &map, part, (int)(rrow + kb * 16), full(s));
-                }
-            }
-            if (!SIDES) tc::bulk_copy(to + F::OPERAND, right + ((long long)kb * a.lblocks + bj) * BLOCK_BYTES + share * F::OPERAND, F::OPERAND, full(s));
-        }
-    } else if (warp == 1 && lane == 0) {
-        const uint32_t what = tc::instruction(BLOCK, !SIDES);
-        for (int i = 0; i < count; ++i) {
-            const int s = i % STAGES;
-            if (!tc::barrier_wait(full(s), (i / STAGES) & 1)) {
-                failed = true;
-                for (int k = i; k < count && k < i + STAGES; ++k) tc::barrier_wait(full(k % STAGES), (k / STAGES) & 1);     // copies under way
-                break;
-            }
-            tc::fence_after();
-            const uint32_t l = stages + s * F::STAGE, r = one ? l : l + F::OPERAND, to = sums + i % SUMS * 2 * BLOCK;
-#pragma unroll
-            for (int q = 0; q < STEP / 16; ++q) {
-                // cores of left: 512 bytes from one to the next along M, 128 along K; of right (!SIDES): 128 along N, 4096 along K
-                const uint32_t at = (q >> 1) * 16384 + (q & 1) * 256;
-                const uint64_t lh = tc::descriptor(l + at, 128, 512), ll = tc::descriptor(l + 8192 + at, 128, 512);
-                const uint64_t rh = SIDES ? tc::descriptor(r + at, 128, 512) : tc::descriptor(r + q * 8192, 4096, 128);
-                const uint64_t rl = SIDES ? tc::descriptor(r + 8192 + at, 128, 512) : tc::descriptor(r + LO + q * 8192, 4096, 128);
-                tc::product(to + BLOCK, ll, rh, what, i >= SUMS || q > 0);
-                tc::product(to + BLOCK, lh, rl, what, true);
-                tc::product(to, lh, rh, what, i >= SUMS || q > 0);
-            }
-            tc::commit(empty(s));
-        }
-        tc::commit(done);
-    }
-    __syncwarp();
     // what is blended in is fetched while the products run (POLY), or half of it at a time
     constexpr int AHEAD = SIDES ? ITEMS : ITEMS / 2;
     const int g0 = GROUPS * rank / RANKS, g1 = GROUPS * (rank + 1) / RANKS;            // this block's share of the rows, in eights
@@ -139,7 +100,8 @@ __global__ void __launch_bounds__(GEMM_THREADS, Form<KIND>::BLOCKS) gemm_kernel(
     };
     // X = 2^e X^ and its successor (LAST: the result itself): b A and c A A, a X and P X are blended with these
     float old_by = 1.f, sum_by = 1.f;
-    if (KIND != GRAM) {
+    auto prepare = [&]() {
+        if (KIND == GRAM) return;
         fetch(0);
         Exponent now(a.size[m]);
         for (int k = 0; k < a.turn && now.most <= 0.5f; ++k) now.turn(a);
@@ -148,37 +110,107 @@ __global__ void __launch_bounds__(GEMM_THREADS, Form<KIND>::BLOCKS) gemm_kernel(
         const int to = KIND == LAST ? 0 : next.e;
         old_by = KIND == POLY ? a.b : a.a * power_of_two(now.e - to);
         sum_by = KIND == POLY ? a.c * power_of_two(2 * now.e) : power_of_two(3 * now.e - to);
+    };
+    // a thread's row and half of the columns of the sums
+    auto read_sums = [&](int half, float (&v)[32]) {
+        const uint32_t at = sums + ((uint32_t)((warp & 3) * 32) << 16) + (warp >> 2) * 64 + half * 32;
+        float t[32];
+        tc::read_columns(at, v);
+        tc::read_columns(at + BLOCK, t);
+        if (SUMS > 1 && count > 1) {
+            float u[32];
+            tc::read_columns(at + 2 * BLOCK, u);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] += u[j];
+            tc::read_columns(at + 3 * BLOCK, u);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) t[j] += u[j];
+        }
+#pragma unroll
+        for (int j = 0; j < 32; ++j) v[j] += t[j];
+    };
+
+    float before[LONG ? 64 : 1] = {};                                              // the sums of the spans before
+    const int spans = LONG ? (count + SPAN - 1) / SPAN : 1;
+    for (int span = 0;; ++span) {
+        const int i0 = LONG ? (int)((long long)count * span / spans) : 0, i1 = LONG ? (int)((long long)count * (span + 1) / spans) : count;
+        if (warp == 0 && lane == 0) {
+            // rows of cores from the first block to left's and right's
+            const long long lrow = (left - a.blocks) / ROW_BYTES + (long long)bi * lblocks * 16, rrow = (right - a.blocks) / ROW_BYTES + (long long)bj * lblocks * 16;
+            for (int i = i0; i < i1; ++i) {
+                const int s = i % STAGES, k = first + i, kb = k / PARTS_OF_BLOCK, share = k % PARTS_OF_BLOCK;
+                if (i >= STAGES && !tc::barrier_wait(empty(s), (i / STAGES - 1) & 1)) { failed = true; break; }
+                const uint32_t to = stages + s * F::STAGE;
+                tc::barrier_expect(full(s), one ? F::OPERAND : F::STAGE);
+#pragma unroll
+                for (int h = 0; h < STEP / 32; ++h) {
+#pragma unroll
+                    for (int piece = 0; piece < 2; ++piece) {                   // 32 columns of 128 rows: 8 KB
+                        const uint32_t at = to + h * 16384 + piece * 8192;
+                        const int part = piece * 4 + share * (STEP / 32) + h;
+                        tc::tiled_copy(at, &map, part, (int)(lrow + kb * 16), full(s));
+                        if (SIDES && !one) tc::tiled_copy(at + F::OPERAND, &map, part, (int)(rrow + kb * 16), full(s));
+                    }
+                }
+                if (!SIDES) tc::bulk_copy(to + F::OPERAND, right + ((long long)kb * a.lblocks + bj) * BLOCK_BYTES + share * F::OPERAND, F::OPERAND, full(s));
+            }
+        } else if (warp == 1 && lane == 0) {
+            const uint32_t what = tc::instruction(BLOCK, !SIDES);
+            for (int i = i0; i < i1; ++i) {
+                const int s = i % STAGES;
+                if (!tc::barrier_wait(full(s), (i / STAGES) & 1)) {
+                    failed = true;
+                    for (int k = i; k < i1 && k < i + STAGES; ++k) tc::barrier_wait(full(k % STAGES), (k / STAGES) & 1);     // copies under way
+                    break;
+                }
+                tc::fence_after();
+                const uint32_t l = stages + s * F::STAGE, r = one ? l : l + F::OPERAND, to = sums + (i - i0) % SUMS * 2 * BLOCK;
+#pragma unroll
+                for (int q = 0; q < STEP / 16; ++q) {
+                    // cores of left: 512 bytes from one to the next along M, 128 along K; of right (!SIDES): 128 along N, 4096 along K
+                    const uint32_t at = (q >> 1) * 16384 + (q & 1) * 256;
+                    const uint64_t lh = tc::descriptor(l + at, 128, 512), ll = tc::descriptor(l + 8192 + at, 128, 512);
+                    const uint64_t rh = SIDES ? tc::descriptor(r + at, 128, 512) : tc::descriptor(r + q * 8192, 4096, 128);
+                    const uint64_t rl = SIDES ? tc::descriptor(r + 8192 + at, 128, 512) : tc::descriptor(r + LO + q * 8192, 4096, 128);
+                    tc::product(to + BLOCK, ll, rh, what, i - i0 >= SUMS || q > 0);
+                    tc::product(to + BLOCK, lh, rl, what, true);
+                    tc::product(to, lh, rh, what, i - i0 >= SUMS || q > 0);
+                }
+                tc::commit(empty(s));
+            }
+            tc::commit(done);
+        }
+        __syncwarp();
+        if (!LONG) prepare();
+        if (!tc::barrier_wait(done, span & 1)) failed = true;
+        failed = __syncthreads_or(failed);
+        tc::fence_after();
+        if (!LONG || span + 1 == spans || failed) break;
+#pragma unroll
+        for (int half = 0; half < (LONG ? 2 : 0); ++half) {
+            float v[32];
+            read_sums(half, v);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) before[(LONG ? half * 32 : 0) + (LONG ? j : 0)] += v[j];
+        }
+        tc::fence_before();
+        __syncthreads();                                                           // the next products start the sums again
     }
-    if (!tc::barrier_wait(done, 0)) failed = true;
-    failed = __syncthreads_or(failed);
-    tc::fence_after();
 
     // the sums, in units of the stored values; NaN where a wait gave up, and so the results
     float* sum = reinterpret_cast<float*>(smem + 1024);
     const float unit = unit_of(failed);
-    {
-        const int row = (warp & 3) * 32 + lane;
-#pragma unroll 1
-        for (int c0 = (warp >> 2) * 64; c0 < (warp >> 2) * 64 + 64; c0 += 32) {
-            const uint32_t at = sums + ((uint32_t)((warp & 3) * 32) << 16) + c0;
-            float v[32], t[32];
-            tc::read_columns(at, v);
-            tc::read_columns(at + BLOCK, t);
-            if (SUMS > 1 && count > 1) {
-                float u[32];
-                tc::read_columns(at + 2 * BLOCK, u);
+#pragma unroll (LONG ? 2 : 1)
+    for (int half = 0; half < 2; ++half) {
+        const int row = (warp & 3) * 32 + lane, c0 = (warp >> 2) * 64 + half * 32;
+        float v[32];
+        read_sums(half, v);
 #pragma unroll
-                for (int j = 0; j < 32; ++j) v[j] += u[j];
-                tc::read_columns(at + 3 * BLOCK, u);
+        for (int j = 0; j < 32; ++j) v[j] = (LONG ? v[j] + before[LONG ? half * 32 + j : 0] : v[j]) * unit;
 #pragma unroll
-                for (int j = 0; j < 32; ++j) t[j] += u[j];
-            }
-#pragma unroll
-            for (int j = 0; j < 32; j += 4)
-                *reinterpret_cast<float4*>(sum + sum_at(row, c0 + j)) = make_float4((v[j] + t[j]) * unit, (v[j + 1] + t[j + 1]) * unit, (v[j + 2] + t[j + 2]) * unit,
-                                                                                    (v[j + 3] + t[j + 3]) * unit);
-        }
+        for (int j = 0; j < 32; j += 4) *reinterpret_cast<float4*>(sum + sum_at(row, c0 + j)) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
     }
+    if (LONG) prepare();
     tc::fence_before();
     __syncthreads();
     if (warp == 0) tc::free_columns(sums, F::COLUMNS);

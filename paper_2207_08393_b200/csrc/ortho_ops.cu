@@ -74,20 +74,32 @@ static int clusters_at_once(int ranks) {
     return n > 0 ? at_once[ranks] : 0;
 }
 
-template <int KIND, int RANKS, class T>
+template <int KIND, int RANKS, bool LONG, class T>
 static cudaError_t gemm_of(const Args& a, const CUtensorMap& map, int count, cudaStream_t s) {
     static PerDevice done;
-    const cudaError_t e = ensure_smem(gemm_kernel<KIND, RANKS, T>, Form<KIND>::SMEM, done);
+    const cudaError_t e = ensure_smem(gemm_kernel<KIND, RANKS, LONG, T>, Form<KIND, LONG>::SMEM, done);
     if (e != cudaSuccess) return e;
     const dim3 grid((unsigned)RANKS, (unsigned)tiles_of<KIND>(a), (unsigned)count), block(GEMM_THREADS);
-    ORTHO_LAUNCH(launch_overlapped_cluster((unsigned)RANKS, gemm_kernel<KIND, RANKS, T>, grid, block, Form<KIND>::SMEM, s, a, map));
+    ORTHO_LAUNCH(launch_overlapped_cluster((unsigned)RANKS, gemm_kernel<KIND, RANKS, LONG, T>, grid, block, Form<KIND, LONG>::SMEM, s, a, map));
     return cudaSuccess;
+}
+// GRAM and POLY: blocks that share a sum over K
+template <int KIND, bool LONG>
+static cudaError_t gemm_in(int ranks, const Args& a, const CUtensorMap& map, int count, cudaStream_t s) {
+    switch (ranks) {
+        case 2: return gemm_of<KIND, 2, LONG, float>(a, map, count, s);
+        case 3: return gemm_of<KIND, 3, LONG, float>(a, map, count, s);
+        case 4: return gemm_of<KIND, 4, LONG, float>(a, map, count, s);
+        case 6: return gemm_of<KIND, 6, LONG, float>(a, map, count, s);
+        case 8: return gemm_of<KIND, 8, LONG, float>(a, map, count, s);
+    }
+    return gemm_of<KIND, 1, LONG, float>(a, map, count, s);
 }
 template <int KIND, class T = float>
 static cudaError_t gemm(const Args& a, const CUtensorMap& map, int count, cudaStream_t s) {
     if constexpr (KIND == GRAM || KIND == POLY) {
-        // blocks that share a sum over K: a step takes about 0.45 us, all else of a block 6, 8 with others; rounds of clusters
-        const long long tiles = (long long)tiles_of<KIND>(a) * count, steps = steps_of<KIND>(a);
+        // a step takes about 0.45 us, all else of a block 6, 8 with others; rounds of clusters
+        const long long tiles = (long long)tiles_of<KIND>(a) * count, steps = steps_of<KIND, false>(a);
         int best = 1;
         long long least = 0;
         for (const int ranks : {1, 2, 3, 4, 6, 8}) {
@@ -96,15 +108,10 @@ static cudaError_t gemm(const Args& a, const CUtensorMap& map, int count, cudaSt
             const long long time = (tiles + at_once - 1) / at_once * ((steps + ranks - 1) / ranks * 45 + (ranks > 1 ? 800 : 600));
             if (ranks == 1 || time < least) { best = ranks; least = time; }
         }
-        switch (best) {
-            case 2: return gemm_of<KIND, 2, T>(a, map, count, s);
-            case 3: return gemm_of<KIND, 3, T>(a, map, count, s);
-            case 4: return gemm_of<KIND, 4, T>(a, map, count, s);
-            case 6: return gemm_of<KIND, 6, T>(a, map, count, s);
-            case 8: return gemm_of<KIND, 8, T>(a, map, count, s);
-        }
+        return (steps + best - 1) / best > LONG_FROM<KIND> ? gemm_in<KIND, true>(best, a, map, count, s) : gemm_in<KIND, false>(best, a, map, count, s);
+    } else {
+        return steps_of<KIND, true>(a) > LONG_FROM<KIND> ? gemm_of<KIND, 1, true, T>(a, map, count, s) : gemm_of<KIND, 1, false, T>(a, map, count, s);
     }
-    return gemm_of<KIND, 1, T>(a, map, count, s);
 }
 
 // Whether a matrix fits a cluster that every GPU of this kind takes (eight blocks).

@@ -53,8 +53,8 @@ def test_a_launch_that_gave_up_waiting_leaves_nan():
     read = lambda name: "".join(line.split("//")[0] + "\n" for line in open(os.path.join(CSRC, name)))
     assert "unit_of(bool failed) { return failed ? __int_as_float(0x7fffffff) : 1.f / SCALE; }" in read("ortho_common.cuh")
     gemm, resident = read("ortho_gemm.cuh"), read("ortho_resident.cuh")
-    assert gemm.index("failed = __syncthreads_or(failed);") < gemm.index("unit = unit_of(failed);") < gemm.index("tc::read_columns(")
-    stored = gemm[gemm.index("make_float4((v[j]"):]
-    assert stored[:stored.index(";")].count("* unit") == 4
+    assert gemm.index("failed = __syncthreads_or(failed);") < gemm.index("unit = unit_of(failed);")
+    out = gemm[gemm.index("unit = unit_of(failed);"):]
+    assert out.index("read_sums(half, v);") < out.index(": v[j]) * unit;") < out.index("(sum + sum_at(row, c0 + j)) = ")
     assert "v[j] = (v[j] + u[j]) * unit_of(failed);" in resident and resident.count("tc::read_columns(") == 2
     assert resident.count("if (threadIdx.x == 0 && !failed)") == resident.count("what = tc::instruction(")

@@ -11,8 +11,8 @@
 // two pieces, hi = x rounded to float16 and lo = x - hi rounded to float16 (22 bits, where a 32-bit number has 24), and a product is
 // hi hi + hi lo + lo hi; what is left out is 2^-24 of it.  All stored values are scaled by 2^10 (up to 64 in front of the scale), so that lo keeps
 // its bits down to values of 2^-13 and is off by 2^-35 below; X also by a power of two where its norm is small against eps (Exponent).  The
-// term a X is added in 32 bits.  Five turns of 100 x 900 of falling singular values are off by 1.9e-6, 2.7e-6 in 32-bit products; of 9216 x 1024 by
-// 7.4e-7 and 5.3e-7.  float16 or bfloat16 products without the second piece would be off by 1e-3 or 1e-2.
+// term a X is added in 32 bits.  Five turns of 100 x 900 of falling singular values are off by 2.0e-6, 2.8e-6 in 32-bit products; of 9216 x 1024 by
+// 8.7e-6 and 6.1e-6.  float16 or bfloat16 products without the second piece would be off by 1e-3 or 1e-2.
 //
 // Matrices are stored in blocks of 128 x 128 with zeros beyond their sides, 64 KB: 16 rows of cores, in each those of hi, then those of lo, 16
 // cores of 8 rows by 8 columns, a row of a core 16 bytes: the shape that the matrix instructions read, along either side.  An operand's

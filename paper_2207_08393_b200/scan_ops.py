@@ -11,7 +11,7 @@ Three layers, as for the other operators of the prior:
 x, gate and their cotangents are CUDA tensors of one shape and type (float32, float16 or bfloat16); states are float32, contiguous, of that
 shape without axis ``dim``.  The axes behind ``dim`` are contiguous and those before it step evenly, apart from axis 0, which
 may step on its own: halves of a wider array along an axis before ``dim`` are fine.  ``lengths`` (int32, one for each index of
-axis 0) ends each example's chain early: behind its length y and the gradients are 0, nothing is read and the state stays.
+axis 0) ends each example's chain early: behind its length y and the gradients are 0, what stands there is not used and the state stays.
 """
 from __future__ import annotations
 

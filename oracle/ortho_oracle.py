@@ -49,6 +49,19 @@ def tolerance(its, coefficients=COEFFICIENTS):
     return total
 
 
+def in_32_bits(x, steps, coefficients=COEFFICIENTS, eps=1e-7):
+    """The last iterate by products of 32-bit numbers."""
+    if x.shape[0] > x.shape[1]:
+        return in_32_bits(x.T, steps, coefficients, eps).T
+    a, b, c = (np.float32(v) for v in coefficients)
+    x = x.astype(np.float32)
+    x = x / (np.sqrt((x ** 2).sum()) + np.float32(eps))
+    for _ in range(steps):
+        g = x @ x.T
+        x = a * x + (b * g + c * (g @ g)) @ x
+    return x.astype(np.float64)
+
+
 def near(err32, k):
     """Relative Frobenius norm of the error that may be left where the same turns in 32-bit products leave err32 on the same matrix; k is
     its longer side.

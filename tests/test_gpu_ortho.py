@@ -460,3 +460,13 @@ def test_sums_of_many_terms(shape):
     for x in (matrices(1, *shape, seed=14), torch.rand((1,) + shape, device="cuda")):
         for steps in (1, 5):
             near_32_bits(x, g.orthogonalise(x, steps), steps)
+
+
+@pytest.mark.parametrize("rows, cols", [(100, 900), (150, 200)])
+@pytest.mark.parametrize("eps", [0.5, 1.0, 3.0, 1e6, 1e20])
+def test_eps_that_are_large_beside_the_norm(rows, cols, eps):
+    import paper_2207_08393_b200 as g
+    x = matrices(2, rows, cols, seed=15)
+    x = x / x.norm(dim=(-2, -1), keepdim=True)
+    for steps in (1, 5, 8):
+        near_32_bits(x, g.orthogonalise(x, steps, eps=eps), steps, eps=eps)

@@ -192,16 +192,6 @@ def in_pieces(x, steps, pieces, coefficients=oo.COEFFICIENTS, eps=1e-7):
     return x
 
 
-def in_32_bits(x, steps, coefficients=oo.COEFFICIENTS, eps=1e-7):
-    a, b, c = (np.float32(v) for v in coefficients)
-    x = x.astype(np.float32)
-    x = x / (np.sqrt((x ** 2).sum()) + np.float32(eps))
-    for _ in range(steps):
-        g = x @ x.T
-        x = a * x + (b * g + c * (g @ g)) @ x
-    return x.astype(np.float64)
-
-
 @pytest.mark.parametrize("norm", [1.0, 1e-6, 1e-8, 1e-11, 1e-13, 1e-16])
 @pytest.mark.parametrize("shape", [(60, 540), (130, 257), (100, 900)])
 @pytest.mark.parametrize("steps", [1, 5])
@@ -212,7 +202,7 @@ def test_the_bound_takes_two_pieces_and_not_one(shape, steps, norm):
     x = (x * norm / np.sqrt((x ** 2).sum())).astype(np.float32)
     ref = oo.iterates(x, steps)[-1]
     off = lambda y: np.sqrt(((y - ref) ** 2).sum() / (ref ** 2).sum())
-    most = oo.near(off(in_32_bits(x, steps)), shape[1])
+    most = oo.near(off(oo.in_32_bits(x, steps)), shape[1])
     # 32-bit products leave up to 2.7e-6 after five turns (100 x 900), of which four times, 900 * 2^-28 and 2^-21 are 1.5e-5
     assert off(in_pieces(x, steps, 2)) <= most < 2e-5
     assert off(in_pieces(x, steps, 1)) > 10 * most

@@ -25,7 +25,7 @@ constexpr int GEMM_THREADS = 256, STAGES = 3;
 // second block would have no registers for that, takes the form of the others then.  130 x 1048576, five turns: off by 6.7e-6 of the result, 6e-4
 // without; 4096 x 4096: 7.5e-6, 3.2e-5 without, 3900 us of kernels for 3700.
 constexpr int SPAN = 32;                           // steps of 64
-template <int KIND> constexpr int LONG_FROM = KIND == GRAM || KIND == POLY ? 48 : 32;
+template <int KIND> constexpr int LONG_FROM = KIND == GRAM || KIND == POLY ? 56 : 32;
 template <int KIND, bool LONG> struct Form {
     static constexpr bool SIDES = KIND == GRAM || KIND == POLY;                // both operands are rows of one matrix
     static constexpr bool ALONE = SIDES || LONG;                               // on the SM
